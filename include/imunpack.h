@@ -327,6 +327,70 @@ int imunpack_recombine(const imunpack_plan_t *plan, const void *workspace,
                        float scale_A, float scale_B, int64_t *C_int, float *C_fp, int64_t ldc,
                        imunpack_stream_t stream);
 
+/* ================================================================================================
+ * Around the products of a Transformer: norm, optimiser's step
+ * ================================================================================================
+ * Types of arrays that come in more than one. */
+enum { IMUNPACK_F32 = 0, IMUNPACK_BF16 = 1 };
+
+/* ---- root-mean-square norm ----------------------------------------------------------------------
+ * For each of `rows` rows of d elements:  h = x + residual (residual may be NULL: h = x),
+ *     rstd = 1 / sqrt(mean_j h_j^2 + eps),   y_j = h_j rstd weight_j.
+ * x, residual, y, h: device, of type dtype (IMUNPACK_F32 or IMUNPACK_BF16), unit stride within a row, ld* elements from row to
+ * row (at least d; no alignment is asked for beyond that of an element).  weight: device, d elements of
+ * weight_dtype.  h (may be NULL) is the residual stream that goes on, rstd (fp32, may be NULL) is for the backward pass.  y or h may be x or residual.
+ * Statistics and products are binary32; y is computed from h before h is rounded to dtype.
+ * rows == 0 is allowed.  Errors: EINVAL (null pointers, d outside [1, 2^24], a pitch < d, eps < 0 or NaN, unknown types). */
+int imunpack_rmsnorm(const void *x, int64_t ldx, const void *residual, int64_t ldres, const void *weight,
+                     int64_t rows, int64_t d, int dtype, int weight_dtype, float eps,
+                     void *y, int64_t ldy, void *h, int64_t ldh, float *rstd, imunpack_stream_t stream);
+
+/* The same norm with its output as integers that are In-Bound for bit width b (Sec. 4: |q| <= 2^(b-1) - 1, so as an operand of
+ * imunpack_plan they are never split), in 8 bits with a step per row:
+ *     scale = max_j |y_j| / (2^(b-1) - 1),   q_j = rint(y_j / scale)        (binary32 division, half to even)
+ * scale: device, one fp32 per row; 1 for a row of zeros; NaN for a row that holds a NaN or an infinity (its q are 0).
+ * values (device, dtype, may be NULL): q_j * scale, for callers that go on in dtype.  Other arguments and errors as above
+ * (also EINVAL for b outside [2,8]). */
+int imunpack_rmsnorm_quantize(const void *x, int64_t ldx, const void *residual, int64_t ldres, const void *weight,
+                              int64_t rows, int64_t d, int dtype, int weight_dtype, float eps, int b,
+                              int8_t *q, int64_t ldq, float *scale, void *values, int64_t ldv, void *h, int64_t ldh,
+                              imunpack_stream_t stream);
+
+/* Gradients of imunpack_rmsnorm for gy, the gradient of y, and gh, that of h (NULL: none; the residual stream brings one).  The
+ * pass forms h = x + residual again from the same x and residual (in fp32, where h was not rounded, x = h without a residual
+ * does as well and is one array less to read):
+ *     gx_j = gh_j + rstd (gy_j w_j - h_j rstd^2 mean_k(gy_k w_k h_k))      (x and residual share it)
+ *     gweight_j = sum over rows of gy_j h_j rstd
+ * gweight: device, weight_dtype, may be NULL (then no workspace is needed).  The sums over rows are taken in a fixed order:
+ * equal inputs give equal bits.  gx may be gy or gh.  workspace: device, 16-byte aligned, of the size that
+ * imunpack_rmsnorm_backward_workspace gives.  Errors: EINVAL as above; ESMALL. */
+int imunpack_rmsnorm_backward_workspace(int64_t rows, int64_t d, int dtype, size_t *bytes);
+int imunpack_rmsnorm_backward(const void *gy, int64_t ldgy, const void *x, int64_t ldx, const void *residual, int64_t ldres,
+                              const void *gh, int64_t ldgh, const void *weight, const float *rstd, int64_t rows, int64_t d, int dtype, int weight_dtype,
+                              void *gx, int64_t ldgx, void *gweight, void *workspace, size_t workspace_bytes,
+                              imunpack_stream_t stream);
+
+/* ---- AdamW over many tensors ---------------------------------------------------------------------
+ * One step, t = step >= 1, for each of `count` tensors of numel[k] elements (numel[k] == 0 is skipped):
+ *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *     p = (1 - lr weight_decay) p - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * The arrays of pointers and numel are host memory and are not read after the call returns; what they point to is device memory,
+ * contiguous.  params: fp32.  grads: grad_dtype.  copies (NULL, or one bfloat16 tensor each): receive p rounded.
+ * state_bits 32: exp_avg[k] = m and exp_avg_sq[k] = v, fp32; m_scales and v_scales are not read.
+ * state_bits 8: exp_avg[k] holds m and exp_avg_sq[k] the square root of v, as 8-bit floating-point codes (e4m3) times a scale (fp32)
+ * for every IMUNPACK_ADAMW_BLOCK elements, m_scales[k] and v_scales[k]; codes go over whole blocks
+ * (ceil(numel / block) * block bytes, what lies behind the tensor's end zero).  Codes are rounded up or down at random, with the
+ * probability that leaves the mean unchanged, by a hash of seed, step, k and the element: the same call gives the same bits; a
+ * root that is not zero keeps at least the smallest code.  All zeros is the state before the first step.
+ * NaN and infinity in a gradient go into the element (32 bits) or the whole block (8 bits).
+ * Errors: EINVAL (null pointers, lr, eps or weight_decay negative or not finite, a beta outside [0, 1), step < 1, unknown
+ * types). */
+#define IMUNPACK_ADAMW_BLOCK 256
+int imunpack_adamw(int64_t count, float *const *params, const void *const *grads, void *const *exp_avg,
+                   void *const *exp_avg_sq, float *const *m_scales, float *const *v_scales, void *const *copies,
+                   const int64_t *numel, int grad_dtype, int state_bits, double lr, double beta1, double beta2,
+                   double eps, double weight_decay, int64_t step, uint32_t seed, imunpack_stream_t stream);
+
 /* ---- diagnostics ------------------------------------------------------------------------------- */
 /* Per-kernel device time of the last call of each stage on this plan is not kept; callers time
  * with events.  These two describe errors. */
