@@ -328,7 +328,7 @@ int imunpack_recombine(const imunpack_plan_t *plan, const void *workspace,
                        imunpack_stream_t stream);
 
 /* ================================================================================================
- * Around the products of a Transformer: norm, optimiser's step
+ * Around the products of a Transformer: norm, optimiser's step, loss over a vocabulary
  * ================================================================================================
  * Types of arrays that come in more than one. */
 enum { IMUNPACK_F32 = 0, IMUNPACK_BF16 = 1 };
@@ -390,6 +390,32 @@ int imunpack_adamw(int64_t count, float *const *params, const void *const *grads
                    void *const *exp_avg_sq, float *const *m_scales, float *const *v_scales, void *const *copies,
                    const int64_t *numel, int grad_dtype, int state_bits, double lr, double beta1, double beta2,
                    double eps, double weight_decay, int64_t step, uint32_t seed, imunpack_stream_t stream);
+
+/* ---- softmax cross entropy over a vocabulary -------------------------------------------------------
+ * With logits l = x W^T (x: rows x d, W: vocab x d, never kept) and target (device int64, one per row):
+ *     loss_t = log sum_v exp l[t, v] - l[t, target_t]
+ * and, for the gradient g_t of loss_t,  gx = G W,  gW = G^T x  with  G[t, v] = (softmax(l)[t, v] - [v = target_t]) g_t.
+ * Rows whose target is ignore_index take no part, whatever x holds there: loss 0, gradient 0.  A target outside [0, vocab) makes the
+ * row's loss (and a sum or mean) NaN and adds nothing to the gradients.
+ * x, W, gx, gW: device, of type dtype, unit stride within a row, ld* elements from row to row (at least d).
+ * bfloat16: products of bfloat16 operands, G rounded to bfloat16, sums in fp32.  fp32: within what fp32 sums of fp32 products give
+ * (operands as sums of two binary16 numbers each, scaled by a power of two per operand).
+ * reduction: IMUNPACK_NONE: loss has one fp32 per row; SUM, MEAN (over the rows that take part; 0 if there are none): one fp32.
+ * loss, grad: device.  imunpack_xent_backward takes grad, the gradient of loss (as many values), and `saved` as imunpack_xent left it with
+ * want_grad != 0 and the same W, sizes, type and reduction; it may be called again on it.  gx or gW may be NULL.
+ * saved and workspace: device, 16-byte aligned, of the sizes that imunpack_xent_workspace gives.  saved holds x and W in the forms the
+ * products read; workspace a piece of G (about 1 GiB at most, unless 256 columns of the vocabulary take more) and partial sums of gx.
+ * All sums are taken in a fixed order: equal inputs give equal bits.  rows == 0 is allowed.
+ * Errors: EINVAL (null pointers, rows or vocab above 2^22, d above 2^20, a pitch < d, unknown types); ESMALL; EHIP. */
+enum { IMUNPACK_NONE = 0, IMUNPACK_SUM = 1, IMUNPACK_MEAN = 2 };
+int imunpack_xent_workspace(const void *w, int64_t ldw, int64_t rows, int64_t d, int64_t vocab, int dtype, int want_grad,
+                            size_t *saved_bytes, size_t *backward_bytes);
+int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t ldw, const int64_t *target, int64_t rows, int64_t d,
+                  int64_t vocab, int dtype, int64_t ignore_index, int reduction, int want_grad, float *loss,
+                  void *saved, size_t saved_bytes, imunpack_stream_t stream);
+int imunpack_xent_backward(const void *w, int64_t ldw, int64_t rows, int64_t d, int64_t vocab, int dtype, int reduction,
+                           const float *grad, void *saved, size_t saved_bytes, void *gx, int64_t ldgx, void *gw, int64_t ldgw,
+                           void *workspace, size_t workspace_bytes, imunpack_stream_t stream);
 
 /* ---- diagnostics ------------------------------------------------------------------------------- */
 /* Per-kernel device time of the last call of each stage on this plan is not kept; callers time

@@ -32,6 +32,7 @@ EXPORTS = [
     "imunpack_gemm_batched", "imunpack_batch_destroy", "imunpack_quantize_pair", "imunpack_plan_set_digits",
     "imunpack_plan_digits", "imunpack_plan_keep_weights", "imunpack_plan_weights_reused", "imunpack_diag_gemm_parts", "imunpack_diag_gemm_halves", "imunpack_diag_list_columns",
     "imunpack_rmsnorm", "imunpack_rmsnorm_quantize", "imunpack_rmsnorm_backward_workspace", "imunpack_rmsnorm_backward", "imunpack_adamw",
+    "imunpack_xent_workspace", "imunpack_xent", "imunpack_xent_backward",
 ]
 DIGITS_INT8, DIGITS_FP6 = 0, 1
 
@@ -86,6 +87,9 @@ _lib.imunpack_rmsnorm_backward_workspace.argtypes = [_i64, _i64, _i32, C.POINTER
 _lib.imunpack_rmsnorm_backward.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i32, _i32, _vp, _i64, _vp, _vp, _sz, _vp]
 _lib.imunpack_adamw.argtypes = [_i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, C.c_double, C.c_double, C.c_double, C.c_double,
                                 C.c_double, _i64, C.c_uint32, _vp]
+_lib.imunpack_xent_workspace.argtypes = [_vp, _i64, _i64, _i64, _i64, _i32, _i32, C.POINTER(_sz), C.POINTER(_sz)]
+_lib.imunpack_xent.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _i32, _i64, _i32, _i32, _vp, _vp, _sz, _vp]
+_lib.imunpack_xent_backward.argtypes = [_vp, _i64, _i64, _i64, _i64, _i32, _i32, _vp, _vp, _sz, _vp, _i64, _vp, _i64, _vp, _sz, _vp]
 for _name in EXPORTS:
     if _name != "imunpack_strerror":
         getattr(_lib, _name).restype = C.c_int
@@ -703,3 +707,60 @@ def imunpack_adamw(params, grads, exp_avg, exp_avg_sq, step: int, lr: float = 1e
     tables = (p, g, m, v, ms, vs, cp, array.array("q", numel))   # (held until the call has read them)
     _check(_lib.imunpack_adamw(n, *[t.buffer_info()[0] if t is not None else None for t in tables], _DTYPES[gt], 8 if eight else 32, lr, beta1, beta2, eps,
                                weight_decay, step, seed & 0xFFFFFFFF, _stream()), "imunpack_adamw")
+
+
+REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
+
+
+@dataclass
+class XentSaved:
+    """What imunpack_xent_backward takes from the forward pass: one opaque buffer and the sizes it was laid out for."""
+    buffer: torch.Tensor
+    backward_bytes: int
+    reduction: str
+
+
+def _xent_args(x, w):
+    if x.dtype not in _DTYPES or w.dtype != x.dtype or not (x.is_cuda and w.is_cuda):
+        raise ValueError("xent takes x and W as device tensors, both fp32 or both bfloat16")
+    if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
+        raise ValueError(f"x of shape {tuple(x.shape)} and W of shape {tuple(w.shape)} have no product x W^T")
+    return w.shape[1], w.shape[0]
+
+
+def imunpack_xent(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, ignore_index: int = -100, reduction: str = "mean", want_grad: bool = False):
+    """Softmax cross entropy of x W^T against target (int64, x's leading shape), without keeping the logits.  Returns (loss, saved):
+    loss fp32, one per row ("none") or one; saved goes to imunpack_xent_backward (None without want_grad)."""
+    d, vocab = _xent_args(x, w)
+    if target.dtype != torch.int64 or target.shape != x.shape[:-1] or not target.is_cuda:
+        raise ValueError("target is an int64 device tensor of x's leading shape")
+    if reduction not in REDUCTIONS:
+        raise ValueError("reduction is none, sum or mean")
+    x2, ldx = _spread(x, d)
+    w2, ldw = _spread(w, d)
+    rows, dtype, how = target.numel(), _DTYPES[x.dtype], REDUCTIONS[reduction]
+    size, back = _sz(), _sz()
+    _check(_lib.imunpack_xent_workspace(w2.data_ptr(), ldw, rows, d, vocab, dtype, want_grad, C.byref(size), C.byref(back)), "imunpack_xent_workspace")
+    loss = torch.empty(target.shape if how == 0 else (), dtype=torch.float32, device=x.device)
+    buffer = torch.empty(size.value, dtype=torch.uint8, device=x.device)
+    target = target.contiguous()
+    _check(_lib.imunpack_xent(x2.data_ptr(), ldx, w2.data_ptr(), ldw, target.data_ptr(), rows, d, vocab, dtype, ignore_index, how, want_grad,
+                              loss.data_ptr(), buffer.data_ptr(), size.value, _stream()), "imunpack_xent")
+    return loss, XentSaved(buffer, back.value, reduction) if want_grad else None
+
+
+def imunpack_xent_backward(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, saved: XentSaved, grad: torch.Tensor, want_x: bool = True,
+                           want_w: bool = True):
+    """Gradients (gx, gw) of imunpack_xent(..., want_grad=True) for grad, the gradient of its loss (fp32); None where not wanted."""
+    d, vocab = _xent_args(x, w)
+    rows, dtype, how = target.numel(), _DTYPES[x.dtype], REDUCTIONS[saved.reduction]
+    if grad.dtype != torch.float32 or not grad.is_cuda or grad.numel() != (rows if how == 0 else 1):
+        raise ValueError("grad is fp32 and shaped like the loss")
+    w2, ldw = _spread(w, d)
+    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_x else None
+    gw = torch.empty(w.shape, dtype=w.dtype, device=x.device) if want_w else None
+    grad = grad.contiguous()
+    ws = torch.empty(saved.backward_bytes, dtype=torch.uint8, device=x.device)
+    _check(_lib.imunpack_xent_backward(w2.data_ptr(), ldw, rows, d, vocab, dtype, how, grad.data_ptr(), saved.buffer.data_ptr(), saved.buffer.numel(),
+                                       _ptr(gx), d, _ptr(gw), d, ws.data_ptr(), saved.backward_bytes, _stream()), "imunpack_xent_backward")
+    return gx, gw

@@ -1,0 +1,181 @@
+// Product of two 16-bit operands with the contraction contiguous in both, C = sum over segments of A_s B_s^T, accumulated in
+// binary32 on v_mfma_f32_32x32x16: the loop that the loss over a vocabulary is made of.  Tiles of (64 TM) x (64 TN), 2 x 2 waves of
+// (32 TM) x (32 TN) each.
+//
+// The walk over the contraction is that of the int8 GEMM, whose fragments have the same bytes: k-tiles of 128 bytes (64 elements) of a row,
+// loaded straight into LDS, a ring of five half-stages (A and B of a k-tile in slots of their own), one barrier to a k-tile, loads
+// two k-tiles ahead.  16-byte piece c of row r lies at slot c ^ ((r >> 1) & 7) of the row, so that the 32 rows of a fragment fall on
+// different banks.
+//
+// Segments: an operand may come in two pieces, A = A_0 + A_1 and B = B_0 + B_1 (binary32 values as the sums of two binary16 ones); the contraction is then
+// walked three times, A_1 B_0, A_0 B_1 and A_0 B_0 (A_1 B_1 lies below the last bit).  The small products come first.
+#pragma once
+#include "common.h"
+
+namespace imu {
+#if defined(__HIPCC__)
+typedef float v16f32 __attribute__((ext_vector_type(16)));
+typedef _Float16 v8f16 __attribute__((ext_vector_type(8)));
+typedef __bf16 v8bf16 __attribute__((ext_vector_type(8)));
+typedef int v4i32 __attribute__((ext_vector_type(4)));
+
+constexpr int kStageBytes = 128;   // of a row and k-tile
+constexpr int kStageCols = 64;     // 16-bit elements of it
+constexpr int kProductThreads = 256;
+constexpr int product_lds(int tm, int tn) { return 5 * 64 * (tm > tn ? tm : tn) * kStageBytes; }
+
+// One operand: rows of 16-bit elements, `pitch` bytes apart (a multiple of 16, as is the base), in one piece or two (`second` bytes
+// behind the first).  Rows from `rows` on are not read (the last one is, in their place).
+struct Operand {
+    const char *base;
+    int64_t pitch, second;
+    int rows;
+};
+
+template <bool F16>
+__device__ __forceinline__ void mfma16(const v4i32 &a, const v4i32 &b, v16f32 &c) {
+    if constexpr (F16) c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8f16, a), __builtin_bit_cast(v8f16, b), c, 0, 0, 0);
+    else c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf16, a), __builtin_bit_cast(v8bf16, b), c, 0, 0, 0);
+}
+
+// Every lane fetches 16 bytes from base + off; the wave's kilobyte lands at LDS byte `lds` (lane l at lds + 16 l).
+__device__ __forceinline__ void fetch_to_lds(unsigned lds, unsigned off, const char *base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ const char *uniform_address(const char *p) {
+    const uint64_t v = (uint64_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);  // (unsigned: the builtin's int would be extended by its sign)
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (const char *)(((uint64_t)hi << 32) | lo);
+}
+
+// XCD-aware order of tiles: workgroups are dealt to the 8 XCDs in turn, those of an XCD get consecutive tiles, which walk bands of
+// four tile rows so that an XCD's workgroups share operands in its L2.
+__device__ __forceinline__ void tile_at(int wg, int mtiles, int ntiles, int &tm, int &tn) {
+    const int total = mtiles * ntiles, xcd = wg & 7, idx = wg >> 3, per = total >> 3, rem = total & 7;
+    const int at = xcd * per + min(xcd, rem) + idx, size = 4 * ntiles, band = at / size, first = band * 4;
+    const int rows = min(4, mtiles - first), in = at - band * size;
+    tm = first + in % rows;
+    tn = in / rows;
+}
+
+// acc[i][j] of the wave: register r of lane l is the sum at row 32 i + (r / 4) * 8 + (l / 32) * 4 + r % 4 and column 32 j + l % 32 of the
+// wave's part of the tile.  k-tiles [k0, k1) of the contraction (which is k1 - k0 for each segment).
+template <bool F16, int TM, int TN, int SEGS>
+__device__ __forceinline__ void product_tile(const Operand &A, const Operand &B, int m0, int n0, int k0, int k1, char *smem, v16f32 (&acc)[TM][TN]) {
+    constexpr int kSlot = 64 * (TM > TN ? TM : TN) * kStageBytes;  // bytes of a slot of the ring
+    constexpr int LA = 2 * TM, LB = 2 * TN;                        // loads of a wave for its share of a half-stage: 16 TM (16 TN) rows
+    constexpr int NF = TM + TN, NM = TM * TN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    const int K = k1 - k0, total = SEGS * K;
+    if (K <= 0) return;
+    const unsigned lds0 = (unsigned)(size_t)smem;
+    unsigned offA[LA], offB[LB];
+#pragma unroll
+    for (int u = 0; u < LA; ++u) {
+        const int row = 16 * TM * wave + 8 * u + (lane >> 3);
+        offA[u] = (unsigned)(min(row, A.rows - 1 - m0) * A.pitch) + (unsigned)(((lane & 7) ^ ((row >> 1) & 7)) * 16);
+    }
+#pragma unroll
+    for (int u = 0; u < LB; ++u) {
+        const int row = 16 * TN * wave + 8 * u + (lane >> 3);
+        offB[u] = (unsigned)(min(row, B.rows - 1 - n0) * B.pitch) + (unsigned)(((lane & 7) ^ ((row >> 1) & 7)) * 16);
+    }
+    const char *gA = A.base + m0 * A.pitch + (int64_t)k0 * kStageBytes, *gB = B.base + n0 * B.pitch + (int64_t)k0 * kStageBytes;
+    auto ring = [](int slot, int k) { slot += k; return slot >= 5 ? slot - 5 : slot; };
+    const char *pg = nullptr;
+    unsigned dl = 0;
+    // k-tile kt (of all segments; past the last one it is loaded again, into a slot that is not read) of A or B into a slot
+    auto setup = [&](bool isA, int kt, int slot) {
+        int k = min(kt, total - 1);
+        int64_t second = 0;
+        if constexpr (SEGS == 3) {
+            const int s = k >= 2 * K ? 2 : k >= K ? 1 : 0;
+            k -= s * K;
+            second = s == (isA ? 0 : 1) ? (isA ? A.second : B.second) : 0;
+        }
+        pg = uniform_address((isA ? gA : gB) + second + (int64_t)k * kStageBytes);
+        dl = __builtin_amdgcn_readfirstlane(lds0 + (unsigned)(slot * kSlot) + (unsigned)(wave * (isA ? LA : LB) * 1024));
+    };
+    auto fetch = [&](bool isA, int u) { fetch_to_lds(dl + u * 1024, isA ? offA[u] : offB[u], pg); };
+
+    const int lrow = lane & 31, lhalf = lane >> 5, swz = (lrow >> 1) & 7;
+    const unsigned baseA = (unsigned)((wm * 32 * TM + lrow) * kStageBytes), baseB = (unsigned)((wn * 32 * TN + lrow) * kStageBytes);
+    unsigned piece[4];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) piece[ks] = (unsigned)(((2 * ks + lhalf) ^ swz) << 4);
+    v4i32 fa[2][TM], fb[2][TN];
+    // fragment q of a k-step, in the order in which the products need them
+    auto fragment = [&](const char *sa, const char *sb, int ks, int buf, int q) {
+        constexpr int isA4[8] = {1, 0, 0, 1, 0, 0, 1, 1}, idx4[8] = {0, 0, 1, 1, 2, 3, 2, 3};
+        const bool isA = (TM == 4 && TN == 4) ? isA4[q] : q == 0 || q > TN;
+        const int idx = (TM == 4 && TN == 4) ? idx4[q] : q == 0 ? 0 : q > TN ? q - TN : q - 1;
+        if (isA) fa[buf][idx] = *reinterpret_cast<const v4i32 *>(sa + baseA + idx * 32 * kStageBytes + piece[ks]);
+        else fb[buf][idx] = *reinterpret_cast<const v4i32 *>(sb + baseB + idx * 32 * kStageBytes + piece[ks]);
+    };
+    auto multiply = [&](int buf, int m) {
+        constexpr int mi4[16] = {0, 0, 1, 1, 0, 0, 1, 1, 2, 2, 3, 3, 2, 2, 3, 3}, mj4[16] = {0, 1, 0, 1, 2, 3, 2, 3, 0, 1, 0, 1, 2, 3, 2, 3};
+        const int i = (TM == 4 && TN == 4) ? mi4[m] : m / TN, j = (TM == 4 && TN == 4) ? mj4[m] : m % TN;
+        mfma16<F16>(fa[buf][i], fb[buf][j], acc[i][j]);
+    };
+    // the products of a k-step, the fragments of the next one and `count` loads from number `from` on among them
+    auto step = [&](int cur, const char *sa, const char *sb, int next_ks, bool isA, int from, int count) {
+#pragma unroll
+        for (int q = 0; q < NF; ++q) {
+            fragment(sa, sb, next_ks, cur ^ 1, q);
+#pragma unroll
+            for (int m = q * NM / NF; m < (q + 1) * NM / NF; ++m) {
+                multiply(cur, m);
+                if (m == q * NM / NF && q < count) fetch(isA, from + q);
+            }
+            if (NM < NF && q * NM / NF == (q + 1) * NM / NF && q < count) fetch(isA, from + q);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // k-tile 0 landed, k-tile 1 on its way
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        setup(true, p, 2 * p);
+#pragma unroll
+        for (int u = 0; u < LA; ++u) fetch(true, u);
+        setup(false, p, 2 * p + 1);
+#pragma unroll
+        for (int u = 0; u < LB; ++u) fetch(false, u);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"i"(LA + LB) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int q = 0; q < NF; ++q) fragment(smem, smem + kSlot, 0, 0, q);
+    // Steps 0 to 2 load A(kt + 2) into the slot that is free.  Behind them every fragment of k-tile kt has been read and this
+    // wave's parts of k-tile kt + 1 have landed (all but the newest loads); past the barrier that holds for all waves, so that step 3 may read k-tile
+    // kt + 1 and load B(kt + 2) into the slot of A(kt).
+    constexpr int c0 = (LA + 2) / 3, c1 = (LA - c0 + 1) / 2, c2 = LA - c0 - c1;
+    int sa = 0;
+    for (int kt = 0; kt < total; ++kt) {
+        const char *stA = smem + sa * kSlot, *stB = smem + ring(sa, 1) * kSlot;
+        const char *stA1 = smem + ring(sa, 2) * kSlot, *stB1 = smem + ring(sa, 3) * kSlot;
+        setup(true, kt + 2, ring(sa, 4));
+        __builtin_amdgcn_sched_barrier(0);
+        step(0, stA, stB, 1, true, 0, c0);
+        step(1, stA, stB, 2, true, c0, c1);
+        step(0, stA, stB, 3, true, c0 + c1, c2);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(LA) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        setup(false, kt + 2, sa);
+        __builtin_amdgcn_sched_barrier(0);
+        step(1, stA1, stB1, 0, false, 0, LB);
+        sa = ring(sa, 2);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may land in LDS any more
+    __syncthreads();
+}
+#endif
+}  // namespace imu

@@ -1,0 +1,272 @@
+"""Softmax cross entropy over a vocabulary: loss and gradients against the formulas in binary64.
+
+Tolerances, in units of u = 2^-24, element by element.
+A product of K terms: the terms are exact (bfloat16) or off by 5 u of their magnitude (fp32 as two binary16 numbers: 2^-23 for each operand, 2^-24 for
+what is left out), and the sum passes 2 K / 16 accumulations a segment, three segments for fp32, each off by u of at most the sum S of
+the terms' magnitudes.  So a logit is off by dl = c(K) S with c(K) = (2 K / 16) u or (5 + 6 K / 16) u.
+lse: the largest dl of the row, an exponential with an argument off by 3 u |l - top| where exp counts it (x exp(-x) < 0.4: 2 u of the
+sum), and a sum through 64 registers, 8 exchanges and the parts of the vocabulary (V / 512 of them): 100 + V / 512.
+loss: lse's, the target's dl and 2 u of either.
+G: p off by dl + dlse + 3 u |l - lse| + 4 u of itself, 2 u of g; rounded to bfloat16: 2^-8 of it, as two binary16 numbers: 2^-22 and 2^-39 of 1.
+gx, gW: G's error through the product and c(K) of the magnitudes again; bfloat16 results rounded: 2^-8."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+F = torch.float64
+
+
+@pytest.fixture(scope="module")
+def imu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2403_07339_amd import binding
+    return binding
+
+
+def inputs(rows, d, vocab, dtype, share, seed, spread=2.0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, d, generator=g)
+    w = torch.randn(vocab, d, generator=g) * (spread / d ** 0.5)
+    target = torch.randint(0, vocab, (rows,), generator=g)
+    target[torch.rand(rows, generator=g) >= share] = -100
+    grad = torch.randn(rows, generator=g)
+    return x.to(dtype).cuda(), w.to(dtype).cuda(), target.cuda(), grad.cuda()
+
+
+def sums(k, dtype):
+    return (2 * k / 16 + 2) * U if dtype == torch.bfloat16 else (5 + 6 * k / 16 + 6) * U
+
+
+def reference(x, w, target, grad, dtype):
+    """loss per row, gx, gw for the gradient `grad` of each row's loss, and the bounds of their errors; grad 0 and x whatever it is in rows without a target."""
+    valid = (target >= 0) & (target < w.shape[0])
+    x6, w6 = torch.where(valid[:, None], x.to(F), 0.0), w.to(F)
+    g = torch.where(valid, grad.to(F), 0.0)
+    d, vocab, low = w.shape[1], w.shape[0], dtype == torch.bfloat16
+    l = x6 @ w6.t()
+    dl = sums(d, dtype) * (x6.abs() @ w6.abs().t())
+    lse = torch.logsumexp(l, 1)
+    dlse = dl.amax(1) + (102 + vocab / 512) * U + 2 * U * lse.abs()
+    at = torch.where(valid, target, 0)[:, None]
+    hit = l.gather(1, at)[:, 0]
+    loss = torch.where(valid, lse - hit, 0.0)
+    dloss = torch.where(valid, dlse + dl.gather(1, at)[:, 0] + 2 * U * (lse.abs() + hit.abs()), 0.0)
+    p = torch.exp(l - lse[:, None])
+    dp = p * (dl + dlse[:, None] + 3 * U * (l - lse[:, None]).abs() + 4 * U)
+    G = p.scatter_add(1, at, torch.full_like(at, -1.0, dtype=F)) * g[:, None]
+    dG = (dp + 2 * U) * g.abs()[:, None] + (2.0 ** -8 * G.abs() if low else 2.0 ** -22 * G.abs() + 2.0 ** -38 * g.abs().max())
+    gx, gw = G @ w6, G.t() @ x6
+    dgx = dG @ w6.abs() + sums(vocab, dtype) * (G.abs() @ w6.abs()) + (2.0 ** -8 if low else U) * gx.abs()
+    dgw = dG.t() @ x6.abs() + sums(x.shape[0], dtype) * (G.abs().t() @ x6.abs()) + (2.0 ** -8 if low else U) * gw.abs()
+    return valid, (loss, dloss), (gx, dgx), (gw, dgw)
+
+
+def within(got, want):
+    assert torch.isfinite(got).all()
+    off = (got.to(F) - want[0]).abs()
+    assert (off <= want[1]).all(), float((off / want[1].clamp_min(1e-300)).max())
+
+
+# rows, features, vocabulary: single ones, odd sizes, sizes around the tiles, large tiles in all three products
+SIZES = [(1, 1, 1), (1, 64, 100), (2, 7, 3), (3, 65, 257), (64, 64, 64), (197, 256, 1000), (130, 100, 513), (300, 768, 3001), (1000, 129, 130), (17, 2050, 300),
+         (1100, 1024, 8300)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,d,vocab", SIZES)
+def test_loss_and_gradients(imu, rows, d, vocab, dtype):
+    for share in (1.0, 0.4) if rows > 3 else (1.0,):
+        x, w, target, grad = inputs(rows, d, vocab, dtype, share, rows + d + vocab)
+        if share < 1.0:
+            x[target == -100] = float("nan")     # masked rows do not matter
+        valid, loss, gx, gw = reference(x, w, target, grad, dtype)
+        got, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+        within(got, loss)
+        a, b = imu.imunpack_xent_backward(x, w, target, saved, grad)
+        within(a, gx)
+        within(b, gw)
+        assert not a[~valid].any()
+        again = imu.imunpack_xent_backward(x, w, target, saved, grad)     # equal inputs, equal bits
+        assert torch.equal(again[0], a) and torch.equal(again[1], b)
+        alone, none = imu.imunpack_xent(x, w, target, reduction="none")
+        assert none is None and torch.equal(alone, got)
+        # one value: the sum, the mean, and their gradients
+        n, scale = int(valid.sum()), torch.tensor(-3.0, device="cuda")
+        for reduction, div in (("sum", 1.0), ("mean", float(n))):
+            one, saved = imu.imunpack_xent(x, w, target, reduction=reduction, want_grad=True)
+            assert abs(float(one) - float(loss[0].sum()) / div) <= (float(loss[1].sum()) + (n / 1024 + 20) * U * float(loss[0].abs().sum())) / div
+            _, _, gx, gw = reference(x, w, target, torch.full_like(grad, -3.0 / div), dtype)
+            a, b = imu.imunpack_xent_backward(x, w, target, saved, scale)
+            within(a, gx)
+            within(b, gw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_pieces_of_the_vocabulary(imu, dtype):
+    """A vocabulary whose G does not fit one piece: 4096 rows of 32 KiB (fp32; 16 KiB bfloat16) a column."""
+    rows, d, vocab = 4096, 64, 33000 if dtype == torch.float32 else 66000
+    x, w, target, grad = inputs(rows, d, vocab, dtype, 1.0, 3)
+    got, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+    a, b = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    for part in range(0, rows, 1024):     # (the reference of all rows at once takes too much memory)
+        r = slice(part, part + 1024)
+        _, loss, gx, gw = reference(x[r], w, target[r], grad[r], dtype)
+        within(got[r], loss)
+        within(a[r], gx)
+        total = gw if part == 0 else (total[0] + gw[0], total[1] + gw[1])
+    within(b, (total[0], total[1] + sums(rows, dtype) * total[0].abs()))
+
+
+def test_nothing_to_learn_from_and_targets_outside(imu):
+    x, w, target, grad = inputs(70, 96, 150, torch.float32, 1.0, 5)
+    none = torch.full_like(target, -100)
+    x[3] = float("inf")
+    for reduction in ("none", "sum", "mean"):
+        loss, saved = imu.imunpack_xent(x, w, none, reduction=reduction, want_grad=True)
+        assert not loss.any()
+        gx, gw = imu.imunpack_xent_backward(x, w, none, saved, grad if reduction == "none" else grad[0])
+        assert not gx.any() and not gw.any()
+        loss, saved = imu.imunpack_xent(x[:0], w, none[:0], reduction=reduction, want_grad=True)
+        gx, gw = imu.imunpack_xent_backward(x[:0], w, none[:0], saved, grad[:0] if reduction == "none" else grad[0])
+        assert gx.shape == (0, 96) and not gw.any() and (loss.numel() == 0 or float(loss) == 0.0)
+    x[3] = 0.0
+    bad = target.clone()
+    bad[[4, 60]] = torch.tensor([150, -1], device="cuda")
+    loss, saved = imu.imunpack_xent(x, w, bad, reduction="none", want_grad=True)
+    assert torch.isnan(loss[[4, 60]]).all() and torch.isfinite(loss[5:60]).all()
+    _, want, gx, gw = reference(x, w, bad, grad, torch.float32)
+    a, b = imu.imunpack_xent_backward(x, w, bad, saved, grad)
+    within(a, gx)
+    within(b, gw)
+    assert torch.isnan(imu.imunpack_xent(x, w, bad)[0])
+    # another value stands for "no target", one that the vocabulary has as well
+    other = target.clone()
+    other[::2] = 7
+    loss, _ = imu.imunpack_xent(x, w, other, ignore_index=7, reduction="none")
+    assert not loss[::2].any() and (loss[1::2][other[1::2] != 7] > 0).all()
+
+
+def test_bad_values_stay_in_their_rows(imu):
+    x, w, target, grad = inputs(50, 64, 200, torch.bfloat16, 1.0, 6)
+    clean, _ = imu.imunpack_xent(x, w, target, reduction="none")
+    x[7, 3] = float("nan")
+    loss, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+    keep = torch.arange(50, device="cuda") != 7
+    assert torch.isnan(loss[7]) and torch.equal(loss[keep], clean[keep])
+    gx, _ = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    assert torch.isnan(gx[7]).all() and torch.isfinite(gx[keep]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("scale", [1e-30, 1e-4, 300.0])
+def test_sizes_of_values(imu, dtype, scale):
+    """x far below and above one (the logits with it: a softmax that is flat, or all in one place), W the other way round."""
+    x, w, target, grad = inputs(200, 128, 500, dtype, 1.0, 8, spread=0.5)
+    x = (x.float() * scale).to(dtype)
+    x[0] = 0.0
+    valid, loss, gx, gw = reference(x, w, target, grad, dtype)
+    got, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+    within(got, loss)
+    a, b = imu.imunpack_xent_backward(x, w, target, saved, grad * 1e-20)
+    within(a.to(F) * 1e20, (gx[0], gx[1] + 1e-5 * gx[0].abs() + 1e-15))
+    within(b.to(F) * 1e20, (gw[0], gw[1] + 1e-5 * gw[0].abs() + 1e-15 * max(1.0, scale)))
+
+
+def test_strides_and_leading_dimensions(imu):
+    for dtype in (torch.float32, torch.bfloat16):
+        x, w, target, grad = inputs(60, 72, 300, dtype, 0.8, 9)
+        loss, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+        want = imu.imunpack_xent_backward(x, w, target, saved, grad)
+        xs = torch.cat([x, x, x], 1)[:, 72:144]
+        ws = torch.nn.functional.pad(w, (1, 2))[:, 1:73]       # rows at addresses that are not multiples of four
+        got, saved = imu.imunpack_xent(xs, ws, target, reduction="none", want_grad=True)
+        assert torch.equal(got, loss)
+        a, b = imu.imunpack_xent_backward(xs, ws, target, saved, grad)
+        assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+        got, saved = imu.imunpack_xent(x.view(3, 20, 72), w.t().contiguous().t(), target.view(3, 20), reduction="none", want_grad=True)
+        assert torch.equal(got, loss.view(3, 20))
+        a, b = imu.imunpack_xent_backward(x.view(3, 20, 72), w, target.view(3, 20), saved, grad.view(3, 20))
+        assert torch.equal(a.view(60, 72), want[0]) and torch.equal(b, want[1])
+        a, none = imu.imunpack_xent_backward(x, w, target, saved, grad, want_w=False)
+        assert none is None and torch.equal(a, want[0])
+        none, b = imu.imunpack_xent_backward(x, w, target, saved, grad, want_x=False)
+        assert none is None and torch.equal(b, want[1])
+
+
+def test_weights_read_in_place(imu):
+    """bfloat16 weights whose rows are whole pieces of 128 bytes are read where they lie: with a pitch, too."""
+    x, w, target, grad = inputs(90, 128, 400, torch.bfloat16, 1.0, 10)
+    loss, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+    want = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    wide = torch.cat([w, torch.full_like(w, float("nan"))], 1)[:, :128]
+    got, saved = imu.imunpack_xent(x, wide, target, reduction="none", want_grad=True)
+    a, b = imu.imunpack_xent_backward(x, wide, target, saved, grad)
+    assert torch.equal(got, loss) and torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
+def test_another_stream_and_a_graph(imu):
+    x, w, target, grad = inputs(220, 128, 700, torch.float32, 0.5, 11)
+    loss, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+    want = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+        a, b = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, loss) and torch.equal(a, want[0]) and torch.equal(b, want[1])
+    xs, ts = x.clone(), target.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got, saved = imu.imunpack_xent(xs, w, ts, reduction="none", want_grad=True)
+        a, b = imu.imunpack_xent_backward(xs, w, ts, saved, grad)
+    for k in range(3):
+        xs.copy_(x * (1.0 + k))
+        ts.copy_(target.roll(7 * k))      # as many rows, others
+        if k == 2:
+            ts[: 100] = -100
+        graph.replay()
+        e, keep = imu.imunpack_xent(xs, w, ts, reduction="none", want_grad=True)
+        ea, eb = imu.imunpack_xent_backward(xs, w, ts, keep, grad)
+        torch.cuda.synchronize()
+        assert torch.equal(got, e) and torch.equal(a, ea) and torch.equal(b, eb)
+
+
+def test_module_against_autograd_and_differences(imu):
+    from paper_2403_07339_amd import loss as L
+    x, _, target, _ = inputs(48, 64, 200, torch.float32, 0.7, 12)
+    head = L.LinearCrossEntropy(64, 200, device="cuda")
+    x.requires_grad_()
+    value = head(x.view(2, 24, 64), target.view(2, 24))
+    (value * 2.0).backward()
+    x6, w6 = x.detach().to(F).requires_grad_(), head.weight.detach().to(F).requires_grad_()
+    ref = torch.nn.functional.cross_entropy(x6 @ w6.t(), target)
+    (ref * 2.0).backward()
+    assert abs(float(value.detach()) - float(ref.detach())) < 1e-5
+    for got, want in ((x.grad, x6.grad), (head.weight.grad, w6.grad)):
+        assert float((got.to(F) - want).norm() / want.norm()) < 1e-5
+    # central differences of the kernel's own loss: truncation t^2 / 6 of a third derivative of order one, rounding 2^-22 of a loss of
+    # about 6 over t: below 1e-3 of the slope's scale for t = 1/16
+    way, t = torch.randn(48, 64, generator=torch.Generator().manual_seed(2)).cuda(), 1.0 / 16
+    at = lambda y: float(L.linear_cross_entropy(y, head.weight.detach(), target, reduction="sum"))  # noqa: E731
+    n = int((target >= 0).sum())
+    slope = (at(x.detach() + t * way) - at(x.detach() - t * way)) / (2 * t)
+    assert abs(slope - n / 2.0 * float((x.grad.to(F) * way.to(F)).sum())) < 1e-3 * n / 2.0 * float(x.grad.norm() * way.norm())
+
+
+def test_refusals(imu):
+    x, w, t = torch.zeros(4, 8, device="cuda"), torch.zeros(5, 8, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    for args in ((x.half(), w.half(), t), (x, w.bfloat16(), t), (x, w[:, :7], t), (x, w, t.int()), (x, w, t[:3]), (x.cpu(), w, t), (x, w, t.cpu())):
+        with pytest.raises(ValueError):
+            imu.imunpack_xent(*args)
+    with pytest.raises(ValueError):
+        imu.imunpack_xent(x, w, t, reduction="median")
+    _, saved = imu.imunpack_xent(x, w, t, want_grad=True)
+    with pytest.raises(ValueError):
+        imu.imunpack_xent_backward(x, w, t, saved, torch.ones(4, device="cuda"))
+    with pytest.raises(ValueError):
+        imu.imunpack_xent_backward(x, w, t, saved, torch.ones((), device="cuda").double())
+    with pytest.raises(imu.ImunpackError):
+        imu.imunpack_xent_backward(x, w, t, imu.XentSaved(saved.buffer[:256], saved.backward_bytes, "mean"), torch.ones((), device="cuda"))
