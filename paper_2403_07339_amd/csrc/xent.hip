@@ -17,35 +17,83 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 namespace imu {
 constexpr int64_t kPieceBytes = 1ll << 30;  // G of a piece of the vocabulary, both ways round, at most (or 256 columns)
 constexpr int kTop = 14;                    // the largest magnitude of a scaled operand is below 2^(kTop + 1)
-constexpr int kXentSlots = 256;             // parts of the tiles of gx that go at a time: one to a CU
+constexpr int kXentSlots = 256;             // parts of the tiles of a gradient that go at a time: one to a CU
+constexpr int kPartTiles = 8;               // k-tiles of a part at least: below that its sums cost more than its products
+constexpr int kScanGroups = 512, kScanX = 64;  // workgroups that look for the largest magnitudes, those of x first
+constexpr int kJoinRows = 8;
 
 struct XentHeader {
     int32_t count;    // rows with a target
     int32_t bad;      // rows whose target is outside the vocabulary
     uint32_t amax[2]; // bits of the largest magnitude of x (rows with a target) and of W
-    int32_t gexp;     // exponent of the largest gradient of a row
-    int32_t pad[59];
+    int32_t gexp;     // exponent of the largest gradient of a row (where each has its own)
+    uint32_t joined;  // workgroups that have left the losses of their rows
+    int32_t pad[58];
+    uint32_t found[kScanGroups];  // largest magnitudes as the workgroups found them
 };
-static_assert(sizeof(XentHeader) == 256, "header");
+static_assert(sizeof(XentHeader) == 256 + 4 * kScanGroups, "header");
 
 // What 2 to its power an operand is multiplied by before it is split.
 __device__ __forceinline__ int scale_exponent(uint32_t amax) { return min(kTop - ((int)(amax >> 23) - 127), 126); }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// Rows with a target in order, their targets, and for every row its place among them (-1: none, -2: a target outside the vocabulary).
-__global__ __launch_bounds__(1024) void xent_rows_kernel(const int64_t *target, int rows, int64_t vocab, int64_t ignore, XentHeader *hdr, int32_t *source,
-                                                         int32_t *place, int32_t *wanted, float *loss) {
+struct ScanArgs {
+    const int64_t *target;
+    int64_t vocab, ignore;
+    XentHeader *hdr;
+    int32_t *source, *place, *wanted;
+    float *loss;                 // where each row has a loss of its own
+    const float *x, *w;          // fp32: whose largest magnitudes are wanted
+    int64_t ldx, ldw;
+    int rows, d, nx;             // nx: workgroups that look at x
+};
+__device__ __forceinline__ bool has_target(const ScanArgs &a, int64_t v) { return v >= 0 && v < a.vocab && v != a.ignore; }
+
+// The largest magnitude of rows first, first + step, ... of a matrix; x: of those with a target.  A wave takes four rows at a time.
+template <bool X>
+__device__ __forceinline__ float largest(const ScanArgs &a, const float *m, int64_t ld, int64_t rows, int first, int step) {
+    const int lane = threadIdx.x & 63;
+    float top = 0.0f;
+    for (int64_t row = (int64_t)first * 4; row < rows; row += (int64_t)step * 4) {
+        int n[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) n[r] = row + r < rows && (!X || has_target(a, a.target[row + r])) ? a.d : 0;
+        for (int col = lane * 4; col < a.d; col += 256) {
+            piece_t<float, 4> f[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) f[r] = load_piece<float, 4>(m + (row + r) * ld + col, n[r] - col);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) top = fmaxf(top, fabsf(f[r][k]));
+        }
+    }
+    return top;
+}
+
+// Workgroup 0: rows with a target in order, their targets, and for every row its place among them (-1: none, -2: a target outside the
+// vocabulary).  The others (fp32): the largest magnitudes of x and W.
+__global__ __launch_bounds__(1024) void xent_scan_kernel(const ScanArgs a) {
     __shared__ int32_t sums[2][16];
+    __shared__ float lds[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (blockIdx.x > 0) {
+        const int g = blockIdx.x - 1, nx = a.nx;
+        float m = g < nx ? largest<true>(a, a.x, a.ldx, a.rows, g * 16 + wave, nx * 16) : largest<false>(a, a.w, a.ldw, a.vocab, (g - nx) * 16 + wave, ((int)gridDim.x - 1 - nx) * 16);
+        m = reduce_threads<1024, true>(m, lds);
+        if (threadIdx.x == 0) a.hdr->found[g] = __float_as_uint(m);
+        return;
+    }
     int base = 0, bad = 0, turn = 0;
-    for (int t0 = 0; t0 < rows; t0 += 1024, turn ^= 1) {
+    for (int t0 = 0; t0 < a.rows; t0 += 1024, turn ^= 1) {
         const int t = t0 + threadIdx.x;
-        const int64_t v = t < rows ? target[t] : ignore;
-        const bool inside = v >= 0 && v < vocab && v != ignore, outside = !inside && v != ignore;
+        const int64_t v = t < a.rows ? a.target[t] : a.ignore;
+        const bool inside = has_target(a, v), outside = !inside && v != a.ignore;
         const uint64_t mask = __ballot(inside);
         bad |= __ballot(outside) != 0;
         if (lane == 0) sums[turn][wave] = __builtin_popcountll(mask);
@@ -58,64 +106,52 @@ __global__ __launch_bounds__(1024) void xent_rows_kernel(const int64_t *target, 
         }
         const int at = before + __builtin_popcountll(mask & ((1ull << lane) - 1));
         if (inside) {
-            source[at] = t;
-            wanted[at] = (int)v;
+            a.source[at] = t;
+            a.wanted[at] = (int)v;
         }
-        if (t < rows) {
-            place[t] = inside ? at : outside ? -2 : -1;
-            if (loss && !inside) loss[t] = outside ? __builtin_nanf("") : 0.0f;
+        if (t < a.rows) {
+            a.place[t] = inside ? at : outside ? -2 : -1;
+            if (a.loss && !inside) a.loss[t] = outside ? __builtin_nanf("") : 0.0f;
         }
         base += all;
     }
     bad = __syncthreads_or(bad);
     if (threadIdx.x == 0) {
-        hdr->count = base;
-        hdr->bad = bad;
-        hdr->amax[0] = hdr->amax[1] = 0;
+        a.hdr->count = base;
+        a.hdr->bad = bad;
+        a.hdr->joined = 0;
     }
-}
-
-// Largest magnitudes of x (rows with a target) and W.
-__global__ __launch_bounds__(256) void xent_amax_kernel(const float *x, int64_t ldx, const float *w, int64_t ldw, int d, int64_t vocab, XentHeader *hdr,
-                                                        const int32_t *source, int xgroups) {
-    __shared__ float lds[4];
-    const bool isX = (int)blockIdx.x < xgroups;
-    const int64_t rows = isX ? hdr->count : vocab, step = isX ? xgroups : gridDim.x - xgroups;
-    float m = 0.0f;
-    for (int64_t row = isX ? blockIdx.x : blockIdx.x - xgroups; row < rows; row += step) {
-        const float *p = isX ? x + (int64_t)source[row] * ldx : w + row * ldw;
-        for (int col = threadIdx.x * 4; col < d; col += 1024) {
-            float f[4];
-            load_upto<float, 4>(p + col, f, d - col);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) m = fmaxf(m, fabsf(f[k]));
-        }
-    }
-    m = reduce_threads<256, true>(m, lds);
-    if (threadIdx.x == 0 && m > 0.0f) atomicMax(&hdr->amax[isX ? 0 : 1], __float_as_uint(m));
 }
 
 struct PrepareArgs {
     const void *x, *w;
     int64_t ldx, ldw;
-    const XentHeader *hdr;
+    XentHeader *hdr;
     const int32_t *source;
     char *px, *pw, *tx, *tw;               // rows and columns of x and W in 16 bits; nullptr: not wanted
     int64_t px2, pw2, tx2, tw2;            // from the first piece of a value to the second, bytes
     int64_t pitch_p, pitch_tx, pitch_tw;   // bytes from row to row
     int64_t vocab;
-    int d, xtiles;
+    int d, xtiles, nx, nw;                 // nx, nw: workgroups that looked for the largest magnitudes
 };
 // 64 rows by 64 columns of x (gathered) or W: in 16 bits, one or two numbers to a value, row by row and transposed; zeros around.
 template <class T>
 __global__ __launch_bounds__(256) void xent_prepare_kernel(const PrepareArgs a) {
     constexpr bool SPLIT = sizeof(T) == 4;
     __shared__ uint32_t tile[64][65];
+    __shared__ float lds[4];
     const bool isX = (int)blockIdx.x < a.xtiles;
+    float scale = 1.0f;
+    if constexpr (SPLIT) {  // the first workgroup of either operand leaves the largest magnitude for the kernels behind
+        float m = 0.0f;
+        for (int k = threadIdx.x; k < (isX ? a.nx : a.nw); k += 256) m = fmaxf(m, __uint_as_float(a.hdr->found[isX ? k : a.nx + k]));
+        m = reduce_threads<256, true>(m, lds);
+        scale = power_of_two(scale_exponent(__float_as_uint(m)));
+        if (threadIdx.x == 0 && blockIdx.y == 0 && (int)blockIdx.x == (isX ? 0 : a.xtiles)) a.hdr->amax[isX ? 0 : 1] = __float_as_uint(m);
+    }
     const int64_t rows = isX ? a.hdr->count : a.vocab, row0 = (int64_t)(isX ? blockIdx.x : blockIdx.x - a.xtiles) * 64;
     if (row0 >= rows) return;
     const int col0 = blockIdx.y * 64, r = threadIdx.x >> 2, c = (threadIdx.x & 3) * 16;
-    const float scale = SPLIT ? power_of_two(scale_exponent(a.hdr->amax[isX ? 0 : 1])) : 1.0f;
     const int64_t row = row0 + r;
     const T *p = isX ? (const T *)a.x + (row < rows ? (int64_t)a.source[row] : 0) * a.ldx : (const T *)a.w + row * a.ldw;
     const int have = row < rows ? a.d - (col0 + c) : 0;
@@ -166,12 +202,23 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(const PrepareArgs a) 
     if (SPLIT) put(to + (isX ? a.tx2 : a.tw2), q, true);
 }
 
+// The gradient of each row's loss, as a factor between -2 and 2 and a power of two that the results are multiplied with at the end.
+struct Upstream {
+    const float *grad, *g;  // g: the rows' factors where each has a gradient of its own, else nullptr
+    int mean;
+    __device__ __forceinline__ float whole(const XentHeader *hdr) const { return mean ? *grad / (float)max(hdr->count, 1) : *grad; }
+    __device__ __forceinline__ static int exponent_of(float m) { return fabsf(m) > 0.0f ? (int)(__float_as_uint(fabsf(m)) >> 23) - 127 : 0; }
+    __device__ __forceinline__ int exponent(const XentHeader *hdr) const { return g ? hdr->gexp : exponent_of(whole(hdr)); }
+    __device__ __forceinline__ float one(const XentHeader *hdr) const { return ldexpf(whole(hdr), -exponent_of(whole(hdr))); }
+};
+
 struct LogitArgs {
     Operand w, x;             // rows of the vocabulary (of this piece) and of x
     const XentHeader *hdr;
     const int32_t *wanted;
     float *stats, *hit;       // forward: [part of the vocabulary][row] largest logit and sum; the target's logit
-    const float *lse, *g;     // backward
+    const float *lse;         // backward
+    Upstream up;
     char *G, *GT;             // [row][vocabulary of the piece] and [vocabulary of the piece][row]
     int64_t G2, GT2, pitch_G, pitch_GT;
     int64_t stride;           // rows there is room for
@@ -180,6 +227,21 @@ struct LogitArgs {
 };
 constexpr float kLog2e = 1.44269504088896340736f;
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+template <class E>
+__device__ __forceinline__ uint32_t pack(E a, E b) {
+    return (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
+}
+// Four lanes hold a row of four 16-bit elements each (lo: 0 and 1, hi: 2 and 3); afterwards lane k of them holds element k of all four.
+__device__ __forceinline__ void quad_transpose(uint32_t &lo, uint32_t &hi, int lane) {
+    const uint32_t pick = lane & 1 ? 0x03020706u : 0x05040100u;  // odd: the neighbour's upper half below one's own; even: one's own lower half below the neighbour's
+    const uint32_t nlo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)lo, 0xB1, 0xf, 0xf, true), nhi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)hi, 0xB1, 0xf, 0xf, true);
+    const uint32_t a = __builtin_amdgcn_perm(nlo, lo, pick), b = __builtin_amdgcn_perm(nhi, hi, pick);
+    const bool upper = lane & 2;
+    const uint32_t r = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(upper ? a : b), 0x4E, 0xf, 0xf, true);
+    lo = upper ? r : a;
+    hi = upper ? b : r;
+}
 
 // A tile of logits, vocabulary down, rows of x across: a lane holds one row of x per column block, so that the sums over the
 // vocabulary are sums over its registers and one exchange between the halves of the wave.
@@ -197,90 +259,129 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
     x.rows = count;
     v16f32 acc[T][T];
     product_tile<F16, T, T, F16 ? 3 : 1>(a.w, x, tm * kEdge, tn * kEdge, 0, a.ktiles, smem, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lrow = lane & 31, lhalf = lane >> 5;
-    const int vbase = tm * kEdge + (wave >> 1) * 32 * T + 4 * lhalf, tbase = tn * kEdge + (wave & 1) * 32 * T + lrow;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, lhalf = lane >> 5;
+    const int vwave = tm * kEdge + (wave >> 1) * 32 * T, twave = tn * kEdge + (wave & 1) * 32 * T;  // the wave's first column of the piece and row
+    const float all = BACK && !a.up.g ? a.up.one(a.hdr) : 0.0f;
     const int down = F16 ? -(scale_exponent(a.hdr->amax[0]) + scale_exponent(a.hdr->amax[1])) : 0;
+    auto logit = [&](float x) __attribute__((always_inline)) { return F16 ? ldexpf(x, down) : x; };
+    // FULL: no column behind the vocabulary and no row behind the last one in the wave's part (nothing to compare)
+    auto finish = [&](auto full) __attribute__((always_inline)) {
+        constexpr bool FULL = decltype(full)::value;
 #pragma unroll
-    for (int j = 0; j < T; ++j) {
-        const int t = tbase + 32 * j;
-        const int target = t < count ? a.wanted[t] - a.v0 : -1;  // in columns of the piece
-        if constexpr (!BACK) {
-            float top = -__builtin_inff(), sum = 0.0f, hit = 0.0f;
+        for (int j = 0; j < T; ++j) {
+            const int t = twave + 32 * j + lrow;
+            const bool in_rows = FULL || t < count;
+            const int hit_at = in_rows ? a.wanted[t] - a.v0 - vwave : -1;   // the target among the wave's columns
+            const bool hits = hit_at >= 0 && hit_at < 32 * T, any_hits = __ballot(hits) != 0;
+            const int vlane = vwave + 4 * lhalf, left = vocab - vlane, own = hit_at - 4 * lhalf;  // column 32 i + 8 q + k of the lane
+            if constexpr (!BACK) {
+                float top = -__builtin_inff(), sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < T; ++i)
+                for (int i = 0; i < T; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int v = vbase + 32 * i + (r >> 2) * 8 + (r & 3);
-                    if (F16) acc[i][j][r] = ldexpf(acc[i][j][r], down);
-                    if (v < vocab) top = fmaxf(top, acc[i][j][r]);
-                    if (v == target) hit = acc[i][j][r];
+                    for (int r = 0; r < 16; ++r)
+                        if (FULL || 32 * i + (r >> 2) * 8 + (r & 3) < left) top = fmaxf(top, acc[i][j][r]);
+                top = logit(fmaxf(top, __shfl_xor(top, 32)));
+                const float from = top == -__builtin_inff() ? 0.0f : -top * kLog2e;  // (nothing of the vocabulary in this part)
+#pragma unroll
+                for (int i = 0; i < T; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (FULL || 32 * i + (r >> 2) * 8 + (r & 3) < left) sum += __builtin_amdgcn_exp2f(fmaf(logit(acc[i][j][r]), kLog2e, from));
+                sum += __shfl_xor(sum, 32);
+                if (any_hits) {
+                    float hit = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < T; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (32 * i + (r >> 2) * 8 + (r & 3) == own) hit = acc[i][j][r];
+                    if (hits && ((hit_at >> 2) & 1) == lhalf) a.hit[t] = logit(hit);
                 }
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float from = top == -__builtin_inff() ? 0.0f : top;  // (nothing of the vocabulary in this part)
+                if (in_rows && lhalf == 0)
+                    *reinterpret_cast<float2 *>(a.stats + ((int64_t)(2 * tm + (wave >> 1)) * a.stride + t) * 2) = make_float2(top, sum);
+            } else {
+                const float lse = in_rows ? -a.lse[t] * kLog2e : 0.0f, g = !a.up.g ? all : in_rows ? a.up.g[t] : 0.0f;
+                const float scaled = !in_rows ? 0.0f : F16 ? g * power_of_two(kTop) : g;
+                const int64_t trow = t * a.pitch_G, twidth = (count + 63) / 64 * 64;
+                const int tquad = t & ~3;
 #pragma unroll
-            for (int i = 0; i < T; ++i)
+                for (int i = 0; i < T; ++i) {
+                    // in binary32 first: the lane's sixteen columns
+                    float p[16];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int v = vbase + 32 * i + (r >> 2) * 8 + (r & 3);
-                    sum += v < vocab ? fast_exp(acc[i][j][r] - from) : 0.0f;
-                }
-            sum += __shfl_xor(sum, 32);
-            if (t >= count) continue;
-            if (lhalf == 0) {
-                float *to = a.stats + ((int64_t)(2 * tm + (wave >> 1)) * a.stride + t) * 2;
-                to[0] = top;
-                to[1] = sum;
-            }
-            const int in = target - vbase + 4 * lhalf;  // of the wave's columns
-            if (in >= 0 && in < 32 * T && ((in >> 2) & 1) == lhalf) a.hit[t] = hit;
-        } else {
-            const float lse = t < count ? a.lse[t] : 0.0f, g = t < count ? a.g[t] : 0.0f, scaled = F16 ? g * power_of_two(kTop) : g;
+                    for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(logit(acc[i][j][r]), kLog2e, lse));
+                    if (any_hits)
 #pragma unroll
-            for (int i = 0; i < T; ++i)
+                        for (int r = 0; r < 16; ++r)
+                            if (32 * i + (r >> 2) * 8 + (r & 3) == own) p[r] -= 1.0f;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int v = vbase + 32 * i + 8 * q;
-                    uint16_t hi[4], lo[4];
+                    for (int r = 0; r < 16; ++r) p[r] = FULL || (in_rows && 32 * i + (r >> 2) * 8 + (r & 3) < left) ? p[r] * scaled : 0.0f;
+                    auto put = [&](const uint32_t (&w)[8], int64_t offG, int64_t offGT) __attribute__((always_inline)) {
+                        // G: columns 8 q .. 8 q + 7 lie in both halves of the wave; they trade, and each half has eight in a row
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        float l = acc[i][j][4 * q + k];
-                        if (F16) l = ldexpf(l, down);
-                        float p = fast_exp(l - lse) - (v + k == target ? 1.0f : 0.0f);
-                        p = v + k < vocab && t < count ? p * scaled : 0.0f;
-                        if constexpr (F16) {
-                            const _Float16 h = (_Float16)p;
-                            hi[k] = __builtin_bit_cast(uint16_t, h);
-                            lo[k] = __builtin_bit_cast(uint16_t, (_Float16)(p - (float)h));
-                        } else {
-                            hi[k] = __builtin_bit_cast(uint16_t, (__bf16)p);
-                            lo[k] = 0;
+                        for (int q = 0; q < 4; q += 2) {
+                            const auto x = __builtin_amdgcn_permlane32_swap(w[2 * q], w[2 * q + 2], false, false);
+                            const auto y = __builtin_amdgcn_permlane32_swap(w[2 * q + 1], w[2 * q + 3], false, false);
+                            const int v = vwave + 32 * i + 8 * q + 8 * lhalf;
+                            if (FULL || (in_rows && v < a.vlimit))
+                                *reinterpret_cast<v4i32 *>(a.G + offG + trow + v * 2) = v4i32{(int)x[0], (int)y[0], (int)x[1], (int)y[1]};
                         }
-                    }
-                    auto put = [&](const uint16_t (&e)[4], int64_t offG, int64_t offGT) {
-                        if (t < count && v < a.vlimit)
-                            *reinterpret_cast<uint2 *>(a.G + offG + t * a.pitch_G + v * 2) =
-                                make_uint2((uint32_t)e[0] | (uint32_t)e[1] << 16, (uint32_t)e[2] | (uint32_t)e[3] << 16);
+                        // G^T: four rows of x by four columns trade places among four lanes
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (v + k < vocab && t < (count + 63) / 64 * 64) *reinterpret_cast<uint16_t *>(a.GT + offGT + (v + k) * a.pitch_GT + t * 2) = e[k];
+                        for (int q = 0; q < 4; ++q) {
+                            uint32_t lo = w[2 * q], hi = w[2 * q + 1];
+                            quad_transpose(lo, hi, lane);
+                            const int v = vlane + 32 * i + 8 * q + (lane & 3);
+                            if (FULL || (v < vocab && tquad < twidth)) *reinterpret_cast<uint2 *>(a.GT + offGT + v * a.pitch_GT + tquad * 2) = make_uint2(lo, hi);
+                        }
                     };
-                    put(hi, 0, 0);
-                    if (F16) put(lo, a.G2, a.GT2);
+                    uint32_t w[8];
+                    if constexpr (F16) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const _Float16 h0 = (_Float16)p[2 * k], h1 = (_Float16)p[2 * k + 1];
+                            w[k] = pack(h0, h1);
+                            p[2 * k] -= (float)h0;
+                            p[2 * k + 1] -= (float)h1;
+                        }
+                        put(w, 0, 0);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) w[k] = pack((_Float16)p[2 * k], (_Float16)p[2 * k + 1]);
+                        put(w, a.G2, a.GT2);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) w[k] = pack((__bf16)p[2 * k], (__bf16)p[2 * k + 1]);
+                        put(w, 0, 0);
+                    }
                 }
+            }
         }
-    }
+    };
+    if (vwave + 32 * T <= vocab && twave + 32 * T <= count) finish(std::true_type());
+    else finish(std::false_type());
 }
 
-// lse and loss of 32 rows from the parts of the vocabulary, eight threads to a row.
-__global__ __launch_bounds__(256) void xent_join_kernel(const float *stats, const float *hit, int parts, int64_t stride, const XentHeader *hdr, const int32_t *source,
-                                                        float *lse, float *row_loss, float *loss) {
-    __shared__ float tops[8][32], sums[8][32];
-    const int r = threadIdx.x & 31, g = threadIdx.x >> 5, t = blockIdx.x * 32 + r, count = hdr->count;
-    if ((int)blockIdx.x * 32 >= count) return;
+struct JoinArgs {
+    const float *stats, *hit;
+    int parts, how;
+    int64_t stride;
+    XentHeader *hdr;
+    const int32_t *source;
+    float *lse, *row_loss, *loss;
+};
+// lse and loss of eight rows from the parts of the vocabulary, 32 threads to a row.  Where one value is wanted, the workgroup that comes last
+// adds the rows' losses, in a fixed order.
+__global__ __launch_bounds__(256) void xent_join_kernel(const JoinArgs a) {
+    __shared__ float tops[32][kJoinRows], sums[32][kJoinRows], lds[4];
+    __shared__ int last;
+    const int r = threadIdx.x % kJoinRows, g = threadIdx.x / kJoinRows, t = blockIdx.x * kJoinRows + r, count = a.hdr->count;
+    const int groups = max(1, (count + kJoinRows - 1) / kJoinRows);
+    if ((int)blockIdx.x >= groups) return;
     float top = -__builtin_inff(), sum = 0.0f;
     if (t < count)
-        for (int k = g; k < parts; k += 8) {
-            const float2 s = *reinterpret_cast<const float2 *>(stats + ((int64_t)k * stride + t) * 2);
+        for (int k = g; k < a.parts; k += 32) {
+            const float2 s = *reinterpret_cast<const float2 *>(a.stats + ((int64_t)k * a.stride + t) * 2);
             const float next = fmaxf(top, s.x);
             if (next > -__builtin_inff()) sum = sum * fast_exp(top - next) + s.y * fast_exp(s.x - next);
             else sum += s.y;  // (NaN stays)
@@ -289,137 +390,167 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float *stats, cons
     tops[g][r] = top;
     sums[g][r] = sum;
     __syncthreads();
-    if (g != 0 || t >= count) return;
+    if (g == 0 && t < count) {
 #pragma unroll
-    for (int k = 1; k < 8; ++k) top = fmaxf(top, tops[k][r]);
-    sum = 0.0f;
-    const float from = top == -__builtin_inff() ? 0.0f : top;
+        for (int k = 1; k < 32; ++k) top = fmaxf(top, tops[k][r]);
+        sum = 0.0f;
+        const float from = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum += sums[k][r] * fast_exp(tops[k][r] - from);
-    const float l = from + logf(sum);
-    lse[t] = l;
-    const float v = l - hit[t];
-    row_loss[t] = v;
-    if (loss) loss[source[t]] = v;
-}
-
-// The sum (mean) over the rows with a target, in a fixed order.
-__global__ __launch_bounds__(1024) void xent_sum_kernel(const float *row_loss, const XentHeader *hdr, int mean, float *loss) {
-    __shared__ float lds[16];
-    const int count = hdr->count;
-    float s = 0.0f;
-    for (int t = threadIdx.x; t < count; t += 1024) s += row_loss[t];
-    s = reduce_threads<1024, false>(s, lds);
-    if (threadIdx.x == 0) *loss = hdr->bad ? __builtin_nanf("") : mean && count > 0 ? s / (float)count : s;
-}
-
-// The gradient of each row's loss, divided by a power of two that the results are multiplied with at the end.
-__global__ __launch_bounds__(1024) void xent_factor_kernel(const float *grad, int reduction, XentHeader *hdr, const int32_t *source, float *g) {
-    __shared__ float lds[16];
-    const int count = hdr->count;
-    const float one = reduction == IMUNPACK_NONE ? 0.0f : reduction == IMUNPACK_MEAN ? *grad / (float)max(count, 1) : *grad;
-    float m = fabsf(one);
-    if (reduction == IMUNPACK_NONE)
-        for (int t = threadIdx.x; t < count; t += 1024) m = fmaxf(m, fabsf(grad[source[t]]));
-    m = reduce_threads<1024, true>(m, lds);
-    const int e = m > 0.0f ? (int)(__float_as_uint(m) >> 23) - 127 : 0;
-    if (threadIdx.x == 0) hdr->gexp = e;
-    for (int t = threadIdx.x; t < count; t += 1024) g[t] = ldexpf(reduction == IMUNPACK_NONE ? grad[source[t]] : one, -e);
-}
-
-// How the tiles of gx are cut along the vocabulary, so that every CU has a part.
-__device__ __forceinline__ int gx_parts(int tiles, int slots) { return tiles > 0 ? max(1, slots / tiles) : 1; }
-
-struct GradXArgs {
-    Operand G, wt;     // [row][vocabulary of the piece], [feature][vocabulary of the piece]
-    const XentHeader *hdr;
-    float *parts;      // [slot][tile]
-    int ktiles, slots, first;
-};
-template <bool F16, int T>
-__global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_grad_x_kernel(const GradXArgs a) {
-    extern __shared__ __attribute__((aligned(1024))) char smem[];
-    constexpr int kEdge = 64 * T;
-    const int count = a.hdr->count, mtiles = (count + kEdge - 1) / kEdge, ntiles = (a.wt.rows + kEdge - 1) / kEdge, tiles = mtiles * ntiles;
-    const int parts = gx_parts(tiles, a.slots);
-    if ((int)blockIdx.x >= tiles * parts) return;
-    // workgroups of an XCD: consecutive tiles of one part of the vocabulary
-    const int xcd = blockIdx.x & 7, idx = blockIdx.x >> 3, per = tiles * parts >> 3, rem = (tiles * parts) & 7;
-    const int slot = __builtin_amdgcn_readfirstlane(xcd * per + min(xcd, rem) + idx);
-    const int part = slot / tiles, tile = slot - part * tiles, tn = tile / mtiles, tm = tile - tn * mtiles;
-    Operand G = a.G;
-    G.rows = count;
-    v16f32 acc[T][T];
-    const int k0 = (int)((int64_t)a.ktiles * part / parts), k1 = (int)((int64_t)a.ktiles * (part + 1) / parts);
-    product_tile<F16, T, T, F16 ? 3 : 1>(G, a.wt, tm * kEdge, tn * kEdge, k0, k1, smem, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    float *to = a.parts + (int64_t)slot * kEdge * kEdge + ((wave >> 1) * 32 * T + 4 * (lane >> 5)) * kEdge + (wave & 1) * 32 * T + (lane & 31);
-#pragma unroll
-    for (int i = 0; i < T; ++i)
-#pragma unroll
-        for (int j = 0; j < T; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float *p = to + (32 * i + (r >> 2) * 8 + (r & 3)) * kEdge + 32 * j;
-                *p = a.first ? acc[i][j][r] : *p + acc[i][j][r];
-            }
-}
-
-// Rows of gx from the parts of its tiles; zeros for rows without a target.
-template <class T>
-__global__ __launch_bounds__(256) void xent_fold_x_kernel(const float *parts, const XentHeader *hdr, const int32_t *place, int d, int edge, int slots, T *gx, int64_t ldgx) {
-    const int64_t row = blockIdx.x;
-    const int col = (blockIdx.y * 256 + threadIdx.x) * 4, at = place[row];
-    if (col >= d) return;
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (at >= 0) {
-        const int mtiles = (hdr->count + edge - 1) / edge, ntiles = (d + edge - 1) / edge, tiles = mtiles * ntiles, n = gx_parts(tiles, slots);
-        const int tile = col / edge * mtiles + at / edge;
-        const float *p = parts + (int64_t)tile * edge * edge + (at % edge) * edge + col % edge;
-        for (int k = 0; k < n; ++k) {
-            const float4 f = *reinterpret_cast<const float4 *>(p + (int64_t)k * tiles * edge * edge);
-            s[0] += f.x; s[1] += f.y; s[2] += f.z; s[3] += f.w;
-        }
-        const int e = hdr->gexp - (sizeof(T) == 4 ? kTop + scale_exponent(hdr->amax[1]) : 0);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) s[k] = ldexpf(s[k], e);
+        for (int k = 0; k < 32; ++k) sum += sums[k][r] * fast_exp(tops[k][r] - from);
+        const float l = from + logf(sum), v = l - a.hit[t];
+        a.lse[t] = l;
+        __hip_atomic_store(a.row_loss + t, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // (past this XCD's cache: no fence has to write it back)
+        if (a.how == IMUNPACK_NONE) a.loss[a.source[t]] = v;
     }
-    store_upto<T, 4>(gx + row * ldgx + col, s, d - col);
+    if (a.how == IMUNPACK_NONE) return;
+    stores_done();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(&a.hdr->joined, 1u) == (unsigned)groups - 1;
+    __syncthreads();
+    if (!last) return;
+    float s = 0.0f;
+    for (int k = threadIdx.x; k < count; k += 256) s += __hip_atomic_load(a.row_loss + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s = reduce_threads<256, false>(s, lds);
+    if (threadIdx.x == 0) *a.loss = a.hdr->bad ? __builtin_nanf("") : a.how == IMUNPACK_MEAN && count > 0 ? s / (float)count : s;
 }
 
-struct GradWArgs {
-    Operand GT, xt;    // [vocabulary of the piece][row], [feature][row]
+// Factors and exponent of the rows' own gradients.
+__global__ __launch_bounds__(1024) void xent_factor_kernel(const float *grad, XentHeader *hdr, const int32_t *source, float *g) {
+    __shared__ float lds[16];
+    const int count = hdr->count;
+    float m = 0.0f;
+    for (int t = threadIdx.x; t < count; t += 1024) m = fmaxf(m, fabsf(grad[source[t]]));
+    m = reduce_threads<1024, true>(m, lds);
+    const int e = Upstream::exponent_of(m);
+    if (threadIdx.x == 0) hdr->gexp = e;
+    for (int t = threadIdx.x; t < count; t += 1024) g[t] = ldexpf(grad[source[t]], -e);
+}
+
+// Into how many parts the tiles of a gradient are cut along the contraction, so that every CU has one.
+__host__ __device__ __forceinline__ int parts_of(int tiles, int slots, int ktiles) {
+    const int most = tiles > 0 ? slots / tiles : 1, able = ktiles / kPartTiles;
+    const int n = most < able ? most : able;
+    return n > 1 ? n : 1;
+}
+
+struct GradArgs {
+    Operand G, wt;     // gx: [row][vocabulary of the piece], [feature][vocabulary of the piece]
+    Operand GT, xt;    // gW: [vocabulary of the piece][row], [feature][row]
     const XentHeader *hdr;
-    void *gw;          // the piece's first row
+    Upstream up;
+    float *xparts, *wparts;  // [slot][tile]; wparts only where the tiles of gW are cut
+    void *gw;                // the piece's first row
     int64_t ldgw;
+    int ktiles, cut_ktiles, xslots, wcut, first;  // k-tiles of gx's contraction: of this piece, and those that its tiles are cut by
 };
+// Both gradients of a piece: the first xslots workgroups take parts of the tiles of gx, those behind them tiles of gW (parts of them,
+// where there are few), so that neither waits for the other's last ones.
 template <bool F16, int T>
-__global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_grad_w_kernel(const GradWArgs a) {
+__global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_grads_kernel(const GradArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     constexpr int kEdge = 64 * T;
-    const int mtiles = (a.GT.rows + kEdge - 1) / kEdge, ntiles = (a.xt.rows + kEdge - 1) / kEdge;
-    int tm, tn;
-    tile_at(blockIdx.x, mtiles, ntiles, tm, tn);
+    const bool isX = (int)blockIdx.x < a.xslots;
+    const int count = a.hdr->count, wg = isX ? blockIdx.x : blockIdx.x - a.xslots;
+    Operand A = isX ? a.G : a.GT, B = isX ? a.wt : a.xt;
+    if (isX) A.rows = count;
+    const int mtiles = (A.rows + kEdge - 1) / kEdge, ntiles = (B.rows + kEdge - 1) / kEdge, tiles = mtiles * ntiles;
+    const int ktiles = isX ? a.ktiles : (count + kStageCols - 1) / kStageCols, parts = isX ? parts_of(tiles, a.xslots, a.cut_ktiles) : a.wcut;
+    if (wg >= tiles * parts) return;
+    int tm, tn, part = 0, slot = 0;
+    if (parts == 1) {
+        tile_at(wg, mtiles, ntiles, tm, tn);
+        slot = tn * mtiles + tm;
+    } else {  // workgroups of an XCD: consecutive tiles of one part of the contraction
+        const int xcd = wg & 7, idx = wg >> 3, per = tiles * parts >> 3, rem = (tiles * parts) & 7;
+        slot = xcd * per + min(xcd, rem) + idx;
+        part = slot / tiles;
+        const int tile = slot - part * tiles;
+        tn = tile / mtiles;
+        tm = tile - tn * mtiles;
+    }
     tm = __builtin_amdgcn_readfirstlane(tm);
     tn = __builtin_amdgcn_readfirstlane(tn);
+    const int k0 = (int)((int64_t)ktiles * part / parts), k1 = (int)((int64_t)ktiles * (part + 1) / parts);
     v16f32 acc[T][T];
-    product_tile<F16, T, T, F16 ? 3 : 1>(a.GT, a.xt, tm * kEdge, tn * kEdge, 0, (a.hdr->count + kStageCols - 1) / kStageCols, smem, acc);
+    product_tile<F16, T, T, F16 ? 3 : 1>(A, B, tm * kEdge, tn * kEdge, __builtin_amdgcn_readfirstlane(k0), __builtin_amdgcn_readfirstlane(k1), smem, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int v0 = tm * kEdge + (wave >> 1) * 32 * T + 4 * (lane >> 5), c0 = tn * kEdge + (wave & 1) * 32 * T + (lane & 31);
-    const int e = a.hdr->gexp - (F16 ? kTop + scale_exponent(a.hdr->amax[0]) : 0);
-    using Out = std::conditional_t<F16, float, __bf16>;
+    const int r0 = (wave >> 1) * 32 * T + 4 * (lane >> 5), c0 = (wave & 1) * 32 * T + (lane & 31);
+    if (isX || a.wcut > 1) {
+        float *to = (isX ? a.xparts : a.wparts) + (int64_t)slot * kEdge * kEdge + r0 * kEdge + c0;
+        const bool add = isX && !a.first;
+#pragma unroll
+        for (int i = 0; i < T; ++i)
+#pragma unroll
+            for (int j = 0; j < T; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    float *p = to + (32 * i + (r >> 2) * 8 + (r & 3)) * kEdge + 32 * j;
+                    *p = add ? *p + acc[i][j][r] : acc[i][j][r];
+                }
+        return;
+    }
+    const int e = a.up.exponent(a.hdr) - (F16 ? kTop + scale_exponent(a.hdr->amax[0]) : 0);
+    const int v0 = tm * kEdge + r0, f0 = tn * kEdge + c0;
 #pragma unroll
     for (int i = 0; i < T; ++i)
 #pragma unroll
         for (int j = 0; j < T; ++j) {
-            const int col = c0 + 32 * j;
-            if (col >= a.xt.rows) continue;
+            if constexpr (F16) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int64_t v = v0 + 32 * i + (r >> 2) * 8 + (r & 3);
-                if (v < a.GT.rows) ((Out *)a.gw)[v * a.ldgw + col] = (Out)ldexpf(acc[i][j][r], e);
+                for (int r = 0; r < 16; ++r) {
+                    const int64_t v = v0 + 32 * i + (r >> 2) * 8 + (r & 3);
+                    if (v < A.rows && f0 + 32 * j < B.rows) ((float *)a.gw)[v * a.ldgw + f0 + 32 * j] = ldexpf(acc[i][j][r], e);
+                }
+            } else {  // four rows by four columns trade places among four lanes: 8 bytes to a store
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t lo = pack((__bf16)ldexpf(acc[i][j][4 * q], e), (__bf16)ldexpf(acc[i][j][4 * q + 1], e));
+                    uint32_t hi = pack((__bf16)ldexpf(acc[i][j][4 * q + 2], e), (__bf16)ldexpf(acc[i][j][4 * q + 3], e));
+                    quad_transpose(lo, hi, lane);
+                    const int64_t v = v0 + 32 * i + 8 * q + (lane & 3);
+                    const int f = (f0 & ~3) + 32 * j;
+                    if (v >= A.rows) continue;
+                    uint16_t *to = (uint16_t *)a.gw + v * a.ldgw + f;
+                    const piece_t<uint16_t, 4> x = __builtin_bit_cast(piece_t<uint16_t, 4>, make_uint2(lo, hi));
+                    if (f + 4 <= B.rows) *reinterpret_cast<piece_t<uint16_t, 4> *>(to) = x;
+                    else
+                        for (int k = 0; k < 4; ++k)
+                            if (f + k < B.rows) to[k] = x[k];
+                }
             }
         }
+}
+
+struct FoldArgs {
+    const float *xparts, *wparts;
+    const XentHeader *hdr;
+    Upstream up;
+    const int32_t *place;
+    void *gx, *gw;
+    int64_t ldgx, ldgw, xrows, wrows;  // rows of gx and gW that are made here
+    int d, edge, ktiles, xslots, wcut;
+};
+// Rows of gx (zeros for those without a target) and of gW from the parts of their tiles.
+template <class T>
+__global__ __launch_bounds__(256) void xent_fold_kernel(const FoldArgs a) {
+    const bool isX = (int64_t)blockIdx.x < a.xrows;
+    const int64_t row = isX ? blockIdx.x : blockIdx.x - a.xrows;
+    const int col = (blockIdx.y * 256 + threadIdx.x) * 4, at = isX ? a.place[row] : (int)row, edge = a.edge;
+    if (col >= a.d) return;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (at >= 0) {
+        const int mtiles = ((isX ? a.hdr->count : (int)a.wrows) + edge - 1) / edge, ntiles = (a.d + edge - 1) / edge, tiles = mtiles * ntiles;
+        const int n = isX ? parts_of(tiles, a.xslots, a.ktiles) : a.wcut, tile = col / edge * mtiles + at / edge;
+        const float *p = (isX ? a.xparts : a.wparts) + (int64_t)tile * edge * edge + (at % edge) * edge + col % edge;
+        for (int k = 0; k < n; ++k) {
+            const float4 f = *reinterpret_cast<const float4 *>(p + (int64_t)k * tiles * edge * edge);
+            s[0] += f.x; s[1] += f.y; s[2] += f.z; s[3] += f.w;
+        }
+        const int e = a.up.exponent(a.hdr) - (sizeof(T) == 4 ? kTop + scale_exponent(a.hdr->amax[isX ? 1 : 0]) : 0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[k] = ldexpf(s[k], e);
+    }
+    store_upto<T, 4>((T *)(isX ? a.gx : a.gw) + row * (isX ? a.ldgx : a.ldgw) + col, s, a.d - col);
 }
 
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -431,11 +562,11 @@ struct XentLayout {
     int64_t pitch_p, pitch_tx, pitch_tw;
     size_t source, place, wanted, lse, row_loss, hit, stats, px, pw, tx, tw, bytes;
     size_t px2, pw2, tx2, tw2;
-    int edge_l, edge_x, edge_w;   // tile edges of the three products
+    int edge_l, edge_g;           // tile edges of the logits and of the gradients
     int parts_v;                  // parts of the vocabulary whose sums are joined
     int64_t piece, pieces;        // columns of the vocabulary to a piece
-    int slots;
-    size_t g, G, GT, G2, GT2, gparts, back_bytes;
+    int xslots, wcut;             // parts of tiles of gx that go at a time; into how many parts the tiles of gW are cut
+    size_t g, G, GT, G2, GT2, xparts, wparts, back_bytes;
     int64_t pitch_G, pitch_GT;
 };
 // Large tiles where they fill the CUs.
@@ -451,8 +582,7 @@ static XentLayout xent_layout(const void *w, int64_t ldw, int64_t rows, int64_t 
     l.vp = up(vocab, 256);
     l.direct = !l.split && d % kStageCols == 0 && ldw % 8 == 0 && (size_t)w % 16 == 0;
     l.edge_l = tile_edge(vocab, rows);
-    l.edge_x = tile_edge(rows, d) == 256 || rows * d * vocab >= 1ll << 33 ? 256 : 128;
-    l.edge_w = tile_edge(vocab, d);
+    l.edge_g = rows * d * vocab >= 1ll << 33 ? 256 : 128;
     l.parts_v = (int)(2 * (up(vocab, l.edge_l) / l.edge_l));
     size_t at = sizeof(XentHeader);
     auto take = [&](int64_t bytes) { const size_t here = at; at = (at + (size_t)bytes + 255) & ~(size_t)255; return here; };
@@ -484,9 +614,11 @@ static XentLayout xent_layout(const void *w, int64_t ldw, int64_t rows, int64_t 
     l.G = take((int64_t)l.G2 * pieces);
     l.GT2 = (size_t)(l.piece * l.pitch_GT);
     l.GT = take((int64_t)l.GT2 * pieces);
-    const int64_t tiles = up(rows, l.edge_x) / l.edge_x * (up(d, l.edge_x) / l.edge_x);
-    l.slots = (int)std::max<int64_t>(tiles, kXentSlots);
-    l.gparts = take((int64_t)l.slots * l.edge_x * l.edge_x * 4);
+    const int64_t edge = l.edge_g, xtiles = l.tp / edge * (up(d, edge) / edge), wtiles = up(vocab, edge) / edge * (up(d, edge) / edge);
+    l.xslots = (int)std::max<int64_t>(up(xtiles, 8), kXentSlots);
+    l.wcut = l.pieces == 1 && wtiles <= kXentSlots / 2 ? parts_of((int)wtiles, kXentSlots, (int)(up(rows, kStageCols) / kStageCols)) : 1;
+    l.xparts = take(l.xslots * edge * edge * 4);
+    l.wparts = take(l.wcut > 1 ? l.wcut * wtiles * edge * edge * 4 : 0);
     l.back_bytes = at;
     return l;
 }
@@ -505,8 +637,7 @@ template <bool F16, int T>
 static int xent_lds() {
     IMU_TRY(more_lds(xent_logits_kernel<F16, T, false>, product_lds(T, T)));
     IMU_TRY(more_lds(xent_logits_kernel<F16, T, true>, product_lds(T, T)));
-    IMU_TRY(more_lds(xent_grad_x_kernel<F16, T>, product_lds(T, T)));
-    return more_lds(xent_grad_w_kernel<F16, T>, product_lds(T, T));
+    return more_lds(xent_grads_kernel<F16, T>, product_lds(T, T));
 }
 static int xent_lds_opt_in() {
     static std::atomic<int> done{0};  // (the attribute is idempotent: two threads set the same)
@@ -556,20 +687,22 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
     char *s = (char *)saved;
     XentHeader *hdr = (XentHeader *)s;
     int32_t *source = (int32_t *)(s + l.source), *place = (int32_t *)(s + l.place), *wanted = (int32_t *)(s + l.wanted);
-    hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, st, target, (int)rows, vocab, ignore_index, hdr, source, place, wanted,
-                       reduction == IMUNPACK_NONE ? loss : nullptr);
+    ScanArgs c = {};
+    c.target = target; c.vocab = vocab; c.ignore = ignore_index; c.hdr = hdr; c.source = source; c.place = place; c.wanted = wanted;
+    c.loss = reduction == IMUNPACK_NONE ? loss : nullptr;
+    c.x = (const float *)x; c.w = (const float *)w; c.ldx = ldx; c.ldw = ldw; c.rows = (int)rows; c.d = (int)d;
+    // (workgroups of 16 waves, a wave to four rows)
+    const int nx = (int)std::min<int64_t>(up(rows, 64) / 64, kScanX), nw = (int)std::min<int64_t>(up(vocab, 64) / 64, kScanGroups - kScanX);
+    c.nx = nx;
+    hipLaunchKernelGGL(xent_scan_kernel, dim3(l.split && rows > 0 ? 1 + nx + nw : 1), dim3(1024), 0, st, c);
     if (rows > 0) {
-        if (l.split) {
-            const int xg = (int)std::min<int64_t>(rows, 256), wg = (int)std::min<int64_t>(vocab, 1024);
-            hipLaunchKernelGGL(xent_amax_kernel, dim3(xg + wg), dim3(256), 0, st, (const float *)x, ldx, (const float *)w, ldw, (int)d, vocab, hdr, source, xg);
-        }
         PrepareArgs p = {};
         p.x = x; p.w = w; p.ldx = ldx; p.ldw = ldw; p.hdr = hdr; p.source = source;
         p.px = s + l.px; p.px2 = l.px2;
         p.pw = l.direct ? nullptr : s + l.pw; p.pw2 = l.pw2;
         if (want_grad) { p.tx = s + l.tx; p.tx2 = l.tx2; p.tw = s + l.tw; p.tw2 = l.tw2; }
         p.pitch_p = l.pitch_p; p.pitch_tx = l.pitch_tx; p.pitch_tw = l.pitch_tw;
-        p.vocab = vocab; p.d = (int)d; p.xtiles = (int)(up(rows, 64) / 64);
+        p.vocab = vocab; p.d = (int)d; p.xtiles = (int)(up(rows, 64) / 64); p.nx = nx; p.nw = nw;
         const unsigned wtiles = p.pw || p.tw ? (unsigned)(up(vocab, 64) / 64) : 0;
         const dim3 grid(p.xtiles + wtiles, (unsigned)(l.dp / 64));
         if (l.split) hipLaunchKernelGGL(xent_prepare_kernel<float>, grid, dim3(256), 0, st, p);
@@ -581,11 +714,13 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
         a.stats = (float *)(s + l.stats); a.hit = (float *)(s + l.hit);
         a.stride = l.tp; a.ktiles = (int)(l.dp / kStageCols);
         IMU_TRY(logits(a, l.split, l.edge_l, false, rows, st));
-        hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)(up(rows, 32) / 32)), dim3(256), 0, st, (const float *)a.stats, (const float *)a.hit, l.parts_v, l.tp, hdr, source,
-                           (float *)(s + l.lse), (float *)(s + l.row_loss), reduction == IMUNPACK_NONE ? loss : nullptr);
     }
-    if (reduction != IMUNPACK_NONE)
-        hipLaunchKernelGGL(xent_sum_kernel, dim3(1), dim3(1024), 0, st, (const float *)(s + l.row_loss), hdr, reduction == IMUNPACK_MEAN, loss);
+    if (rows > 0 || reduction != IMUNPACK_NONE) {
+        JoinArgs j = {};
+        j.stats = (const float *)(s + l.stats); j.hit = (const float *)(s + l.hit); j.parts = l.parts_v; j.how = reduction; j.stride = l.tp;
+        j.hdr = hdr; j.source = source; j.lse = (float *)(s + l.lse); j.row_loss = (float *)(s + l.row_loss); j.loss = loss;
+        hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)(up(std::max<int64_t>(rows, 1), kJoinRows) / kJoinRows)), dim3(256), 0, st, j);
+    }
     return launch_status();
 }
 
@@ -603,8 +738,14 @@ extern "C" int imunpack_xent_backward(const void *w, int64_t ldw, int64_t rows, 
     char *s = (char *)saved, *b = (char *)workspace;
     XentHeader *hdr = (XentHeader *)s;
     const int32_t *source = (const int32_t *)(s + l.source), *place = (const int32_t *)(s + l.place);
-    float *g = (float *)(b + l.g), *parts = (float *)(b + l.gparts);
-    hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, grad, reduction, hdr, source, g);
+    Upstream upstream = {grad, nullptr, reduction == IMUNPACK_MEAN};
+    if (reduction == IMUNPACK_NONE) {
+        upstream.g = (const float *)(b + l.g);
+        hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, grad, hdr, source, (float *)(b + l.g));
+    }
+    const int xslots = gx && rows > 0 ? l.xslots : 0;
+    // the tiles of gx are cut alike in every piece; the last, shorter one leaves some parts with nothing to add
+    const int cut_ktiles = (int)(up(std::min(l.piece, vocab), kStageCols) / kStageCols);
     for (int64_t p = 0; p < l.pieces; ++p) {
         const int64_t v0 = p * l.piece, n = std::min(l.piece, vocab - v0);
         const int ktiles = (int)(up(n, kStageCols) / kStageCols);
@@ -613,50 +754,42 @@ extern "C" int imunpack_xent_backward(const void *w, int64_t ldw, int64_t rows, 
             a.w = {l.direct ? (const char *)w + v0 * ldw * 2 : s + l.pw + v0 * l.pitch_p, l.direct ? ldw * 2 : l.pitch_p, (int64_t)l.pw2, (int)n};
             a.x = {s + l.px, l.pitch_p, (int64_t)l.px2, 0};
             a.hdr = hdr; a.wanted = (const int32_t *)(s + l.wanted);
-            a.lse = (const float *)(s + l.lse); a.g = g;
+            a.lse = (const float *)(s + l.lse); a.up = upstream;
             a.G = b + l.G; a.GT = b + l.GT; a.G2 = l.G2; a.GT2 = l.GT2;
             a.pitch_G = l.pitch_G; a.pitch_GT = l.pitch_GT;
             a.v0 = (int)v0; a.ktiles = (int)(l.dp / kStageCols); a.vlimit = ktiles * kStageCols;
             IMU_TRY(logits(a, l.split, l.edge_l, true, rows, st));
         }
-        if (gx && rows > 0) {
-            GradXArgs a = {};
-            a.G = {b + l.G, l.pitch_G, (int64_t)l.G2, 0};
-            a.wt = {s + l.tw + v0 * 2, l.pitch_tw, (int64_t)l.tw2, (int)d};
-            a.hdr = hdr; a.parts = parts; a.ktiles = ktiles; a.slots = l.slots; a.first = p == 0;
-            const dim3 grid((unsigned)l.slots), block(kProductThreads);
-            const int lds = product_lds(l.edge_x / 64, l.edge_x / 64);
-            if (l.split) {
-                if (l.edge_x == 256) hipLaunchKernelGGL((xent_grad_x_kernel<true, 4>), grid, block, lds, st, a);
-                else hipLaunchKernelGGL((xent_grad_x_kernel<true, 2>), grid, block, lds, st, a);
-            } else {
-                if (l.edge_x == 256) hipLaunchKernelGGL((xent_grad_x_kernel<false, 4>), grid, block, lds, st, a);
-                else hipLaunchKernelGGL((xent_grad_x_kernel<false, 2>), grid, block, lds, st, a);
-            }
-            IMU_TRY(launch_status());
+        GradArgs a = {};
+        a.G = {b + l.G, l.pitch_G, (int64_t)l.G2, 0};
+        a.wt = {s + l.tw + v0 * 2, l.pitch_tw, (int64_t)l.tw2, (int)d};
+        a.GT = {b + l.GT, l.pitch_GT, (int64_t)l.GT2, (int)n};
+        a.xt = {s + l.tx, l.pitch_tx, (int64_t)l.tx2, (int)d};
+        a.hdr = hdr; a.up = upstream; a.xparts = (float *)(b + l.xparts); a.wparts = (float *)(b + l.wparts);
+        a.gw = (char *)gw + v0 * ldgw * (l.split ? 4 : 2); a.ldgw = ldgw;
+        a.ktiles = ktiles; a.cut_ktiles = cut_ktiles; a.xslots = xslots; a.wcut = l.wcut; a.first = p == 0;
+        const int64_t edge = l.edge_g, wgroups = gw ? up(n, edge) / edge * (up(d, edge) / edge) * l.wcut : 0;
+        const dim3 grid((unsigned)(xslots + wgroups)), block(kProductThreads);
+        const int lds = product_lds(l.edge_g / 64, l.edge_g / 64);
+        if (grid.x == 0) continue;
+        if (l.split) {
+            if (edge == 256) hipLaunchKernelGGL((xent_grads_kernel<true, 4>), grid, block, lds, st, a);
+            else hipLaunchKernelGGL((xent_grads_kernel<true, 2>), grid, block, lds, st, a);
+        } else {
+            if (edge == 256) hipLaunchKernelGGL((xent_grads_kernel<false, 4>), grid, block, lds, st, a);
+            else hipLaunchKernelGGL((xent_grads_kernel<false, 2>), grid, block, lds, st, a);
         }
-        if (gw) {
-            GradWArgs a = {};
-            a.GT = {b + l.GT, l.pitch_GT, (int64_t)l.GT2, (int)n};
-            a.xt = {s + l.tx, l.pitch_tx, (int64_t)l.tx2, (int)d};
-            a.hdr = hdr; a.gw = (char *)gw + v0 * ldgw * (l.split ? 4 : 2); a.ldgw = ldgw;
-            const int edge = l.edge_w;
-            const dim3 grid((unsigned)(up(n, edge) / edge * (up(d, edge) / edge))), block(kProductThreads);
-            const int lds = product_lds(edge / 64, edge / 64);
-            if (l.split) {
-                if (edge == 256) hipLaunchKernelGGL((xent_grad_w_kernel<true, 4>), grid, block, lds, st, a);
-                else hipLaunchKernelGGL((xent_grad_w_kernel<true, 2>), grid, block, lds, st, a);
-            } else {
-                if (edge == 256) hipLaunchKernelGGL((xent_grad_w_kernel<false, 4>), grid, block, lds, st, a);
-                else hipLaunchKernelGGL((xent_grad_w_kernel<false, 2>), grid, block, lds, st, a);
-            }
-            IMU_TRY(launch_status());
-        }
+        IMU_TRY(launch_status());
     }
-    if (gx && rows > 0) {
-        const dim3 grid((unsigned)rows, (unsigned)(up(d, 1024) / 1024));
-        if (l.split) hipLaunchKernelGGL(xent_fold_x_kernel<float>, grid, dim3(256), 0, st, parts, hdr, place, (int)d, l.edge_x, l.slots, (float *)gx, ldgx);
-        else hipLaunchKernelGGL(xent_fold_x_kernel<__bf16>, grid, dim3(256), 0, st, parts, hdr, place, (int)d, l.edge_x, l.slots, (__bf16 *)gx, ldgx);
+    FoldArgs f = {};
+    f.xparts = (const float *)(b + l.xparts); f.wparts = (const float *)(b + l.wparts); f.hdr = hdr; f.up = upstream; f.place = place;
+    f.gx = gx; f.gw = gw; f.ldgx = ldgx; f.ldgw = ldgw;
+    f.xrows = xslots ? rows : 0; f.wrows = gw && l.wcut > 1 ? vocab : 0;
+    f.d = (int)d; f.edge = l.edge_g; f.ktiles = cut_ktiles; f.xslots = l.xslots; f.wcut = l.wcut;
+    if (f.xrows + f.wrows > 0) {
+        const dim3 grid((unsigned)(f.xrows + f.wrows), (unsigned)(up(d, 1024) / 1024));
+        if (l.split) hipLaunchKernelGGL(xent_fold_kernel<float>, grid, dim3(256), 0, st, f);
+        else hipLaunchKernelGGL(xent_fold_kernel<__bf16>, grid, dim3(256), 0, st, f);
     }
     return launch_status();
 }
