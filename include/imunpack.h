@@ -392,30 +392,30 @@ int imunpack_adamw(int64_t count, float *const *params, const void *const *grads
                    double eps, double weight_decay, int64_t step, uint32_t seed, imunpack_stream_t stream);
 
 /* ---- softmax cross entropy over a vocabulary -------------------------------------------------------
- * With logits l = x W^T (x: rows x d, W: vocab x d, never kept) and target (device int64, one per row):
+ * With logits l = x W^T (x: rows x d, W: vocab x d, never kept as a whole) and target (device int64, one per row):
  *     loss_t = log sum_v exp l[t, v] - l[t, target_t]
  * and, for the gradient g_t of loss_t,  gx = G W,  gW = G^T x  with  G[t, v] = (softmax(l)[t, v] - [v = target_t]) g_t.
  * Rows whose target is ignore_index take no part, whatever x holds there: loss 0, gradient 0.  A target outside [0, vocab) makes the
  * row's loss (and a sum or mean) NaN and adds nothing to the gradients.
  * x, W, gx, gW: device, of type dtype, unit stride within a row, ld* elements from row to row (at least d).
- * bfloat16: products of bfloat16 operands, G rounded to bfloat16, sums in fp32.  fp32: within what fp32 sums of fp32 products give
- * (operands as sums of two binary16 numbers each, scaled by a power of two per operand).
+ * bfloat16: products of bfloat16 operands, exponentials and G rounded to bfloat16, sums in fp32.  fp32: within what fp32 sums of fp32
+ * products give (operands and G as sums of two binary16 numbers each, scaled by a power of two per operand).
  * reduction: IMUNPACK_NONE: loss has one fp32 per row; SUM, MEAN (over the rows that take part; 0 if there are none): one fp32.
- * loss, grad: device.  imunpack_xent_backward takes grad, the gradient of loss (as many values), and `saved` as imunpack_xent left it with
- * want_grad != 0 and the same W, sizes, type and reduction; it may be called again on it.  gx or gW may be NULL.
- * saved and workspace: device, 16-byte aligned, of the sizes that imunpack_xent_workspace gives.  saved holds x and W in the forms the
- * products read; workspace a piece of G (about 1 GiB at most, unless 256 columns of the vocabulary take more) and partial sums of gx.
+ * loss (device) may be NULL if gradients are asked for, gx and gW (device) may each be NULL.  The gradients are made in the same call,
+ * with the logits in memory for some rows at a time: they are those for grad, the gradient of loss (device, as many values; NULL: 1, not
+ * with NONE).  imunpack_xent_rescale multiplies gradients that were made for 1 with *grad, in place, and leaves them alone if that is 1.
+ * workspace: device, 16-byte aligned, of the size that imunpack_xent_workspace gives: x and W in the forms the products read and, for
+ * gradients, G of a piece of the rows (2 GiB at most, unless 256 rows take more) and partial sums.
  * All sums are taken in a fixed order: equal inputs give equal bits.  rows == 0 is allowed.
  * Errors: EINVAL (null pointers, rows or vocab above 2^22, d above 2^20, a pitch < d, unknown types); ESMALL; EHIP. */
 enum { IMUNPACK_NONE = 0, IMUNPACK_SUM = 1, IMUNPACK_MEAN = 2 };
 int imunpack_xent_workspace(const void *w, int64_t ldw, int64_t rows, int64_t d, int64_t vocab, int dtype, int want_grad,
-                            size_t *saved_bytes, size_t *backward_bytes);
+                            size_t *bytes);
 int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t ldw, const int64_t *target, int64_t rows, int64_t d,
-                  int64_t vocab, int dtype, int64_t ignore_index, int reduction, int want_grad, float *loss,
-                  void *saved, size_t saved_bytes, imunpack_stream_t stream);
-int imunpack_xent_backward(const void *w, int64_t ldw, int64_t rows, int64_t d, int64_t vocab, int dtype, int reduction,
-                           const float *grad, void *saved, size_t saved_bytes, void *gx, int64_t ldgx, void *gw, int64_t ldgw,
-                           void *workspace, size_t workspace_bytes, imunpack_stream_t stream);
+                  int64_t vocab, int dtype, int64_t ignore_index, int reduction, float *loss, const float *grad,
+                  void *gx, int64_t ldgx, void *gw, int64_t ldgw, void *workspace, size_t workspace_bytes,
+                  imunpack_stream_t stream);
+int imunpack_xent_rescale(const float *grad, void *gx, int64_t nx, void *gw, int64_t nw, int dtype, imunpack_stream_t stream);
 
 /* ---- diagnostics ------------------------------------------------------------------------------- */
 /* Per-kernel device time of the last call of each stage on this plan is not kept; callers time

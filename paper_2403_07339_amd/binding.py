@@ -32,7 +32,7 @@ EXPORTS = [
     "imunpack_gemm_batched", "imunpack_batch_destroy", "imunpack_quantize_pair", "imunpack_plan_set_digits",
     "imunpack_plan_digits", "imunpack_plan_keep_weights", "imunpack_plan_weights_reused", "imunpack_diag_gemm_parts", "imunpack_diag_gemm_halves", "imunpack_diag_list_columns",
     "imunpack_rmsnorm", "imunpack_rmsnorm_quantize", "imunpack_rmsnorm_backward_workspace", "imunpack_rmsnorm_backward", "imunpack_adamw",
-    "imunpack_xent_workspace", "imunpack_xent", "imunpack_xent_backward",
+    "imunpack_xent_workspace", "imunpack_xent", "imunpack_xent_rescale",
 ]
 DIGITS_INT8, DIGITS_FP6 = 0, 1
 
@@ -87,9 +87,9 @@ _lib.imunpack_rmsnorm_backward_workspace.argtypes = [_i64, _i64, _i32, C.POINTER
 _lib.imunpack_rmsnorm_backward.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i32, _i32, _vp, _i64, _vp, _vp, _sz, _vp]
 _lib.imunpack_adamw.argtypes = [_i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, C.c_double, C.c_double, C.c_double, C.c_double,
                                 C.c_double, _i64, C.c_uint32, _vp]
-_lib.imunpack_xent_workspace.argtypes = [_vp, _i64, _i64, _i64, _i64, _i32, _i32, C.POINTER(_sz), C.POINTER(_sz)]
-_lib.imunpack_xent.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _i32, _i64, _i32, _i32, _vp, _vp, _sz, _vp]
-_lib.imunpack_xent_backward.argtypes = [_vp, _i64, _i64, _i64, _i64, _i32, _i32, _vp, _vp, _sz, _vp, _i64, _vp, _i64, _vp, _sz, _vp]
+_lib.imunpack_xent_workspace.argtypes = [_vp, _i64, _i64, _i64, _i64, _i32, _i32, C.POINTER(_sz)]
+_lib.imunpack_xent.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _i32, _i64, _i32, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _sz, _vp]
+_lib.imunpack_xent_rescale.argtypes = [_vp, _vp, _i64, _vp, _i64, _i32, _vp]
 for _name in EXPORTS:
     if _name != "imunpack_strerror":
         getattr(_lib, _name).restype = C.c_int
@@ -714,53 +714,67 @@ REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
 
 @dataclass
 class XentSaved:
-    """What imunpack_xent_backward takes from the forward pass: one opaque buffer and the sizes it was laid out for."""
-    buffer: torch.Tensor
-    backward_bytes: int
+    """What imunpack_xent_backward takes from the forward pass: the gradients for a gradient of 1 (once: the first call takes them; None
+    where every row's loss has a gradient of its own) and what a call that makes them anew has to know."""
+    ignore_index: int
     reduction: str
+    gx: torch.Tensor | None = None
+    gw: torch.Tensor | None = None
 
 
-def _xent_args(x, w):
+def _xent_args(x, w, target):
     if x.dtype not in _DTYPES or w.dtype != x.dtype or not (x.is_cuda and w.is_cuda):
         raise ValueError("xent takes x and W as device tensors, both fp32 or both bfloat16")
     if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
         raise ValueError(f"x of shape {tuple(x.shape)} and W of shape {tuple(w.shape)} have no product x W^T")
+    if target.dtype != torch.int64 or target.shape != x.shape[:-1] or not target.is_cuda:
+        raise ValueError("target is an int64 device tensor of x's leading shape")
     return w.shape[1], w.shape[0]
 
 
-def imunpack_xent(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, ignore_index: int = -100, reduction: str = "mean", want_grad: bool = False):
-    """Softmax cross entropy of x W^T against target (int64, x's leading shape), without keeping the logits.  Returns (loss, saved):
-    loss fp32, one per row ("none") or one; saved goes to imunpack_xent_backward (None without want_grad)."""
-    d, vocab = _xent_args(x, w)
-    if target.dtype != torch.int64 or target.shape != x.shape[:-1] or not target.is_cuda:
-        raise ValueError("target is an int64 device tensor of x's leading shape")
-    if reduction not in REDUCTIONS:
-        raise ValueError("reduction is none, sum or mean")
+def _xent(x, w, target, ignore_index, how, loss, grad, want_x, want_w):
+    """One call of the library: loss (a tensor to fill, or None) and the gradients that are wanted."""
+    d, vocab = _xent_args(x, w, target)
     x2, ldx = _spread(x, d)
     w2, ldw = _spread(w, d)
-    rows, dtype, how = target.numel(), _DTYPES[x.dtype], REDUCTIONS[reduction]
-    size, back = _sz(), _sz()
-    _check(_lib.imunpack_xent_workspace(w2.data_ptr(), ldw, rows, d, vocab, dtype, want_grad, C.byref(size), C.byref(back)), "imunpack_xent_workspace")
-    loss = torch.empty(target.shape if how == 0 else (), dtype=torch.float32, device=x.device)
-    buffer = torch.empty(size.value, dtype=torch.uint8, device=x.device)
     target = target.contiguous()
-    _check(_lib.imunpack_xent(x2.data_ptr(), ldx, w2.data_ptr(), ldw, target.data_ptr(), rows, d, vocab, dtype, ignore_index, how, want_grad,
-                              loss.data_ptr(), buffer.data_ptr(), size.value, _stream()), "imunpack_xent")
-    return loss, XentSaved(buffer, back.value, reduction) if want_grad else None
+    rows, dtype, size, at = target.numel(), _DTYPES[x.dtype], _sz(), w2.data_ptr()
+    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_x else None
+    gw = torch.empty(w.shape, dtype=w.dtype, device=x.device) if want_w else None
+    _check(_lib.imunpack_xent_workspace(at, ldw, rows, d, vocab, dtype, want_x or want_w, C.byref(size)), "imunpack_xent_workspace")
+    workspace = torch.empty(size.value, dtype=torch.uint8, device=x.device)
+    _check(_lib.imunpack_xent(x2.data_ptr(), ldx, at, ldw, target.data_ptr(), rows, d, vocab, dtype, ignore_index, how, _ptr(loss), _ptr(grad),
+                              _ptr(gx), d, _ptr(gw), d, workspace.data_ptr(), size.value, _stream()), "imunpack_xent")
+    return gx, gw
+
+
+def imunpack_xent(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, ignore_index: int = -100, reduction: str = "mean", want_grad: bool = False,
+                  want_x: bool = True, want_w: bool = True):
+    """Softmax cross entropy of x W^T against target (int64, x's leading shape), without keeping the logits.  Returns (loss, saved):
+    loss fp32, one per row ("none") or one; saved goes to imunpack_xent_backward (None without want_grad).  With want_grad and one loss the
+    gradients (of x and W, as far as wanted) are made in this call."""
+    if reduction not in REDUCTIONS:
+        raise ValueError("reduction is none, sum or mean")
+    how = REDUCTIONS[reduction]
+    now = want_grad and how != 0
+    loss = torch.empty(target.shape if how == 0 else (), dtype=torch.float32, device=x.device)
+    gx, gw = _xent(x, w, target, ignore_index, how, loss, None, now and want_x, now and want_w)
+    return loss, XentSaved(ignore_index, reduction, gx, gw) if want_grad else None
 
 
 def imunpack_xent_backward(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, saved: XentSaved, grad: torch.Tensor, want_x: bool = True,
                            want_w: bool = True):
-    """Gradients (gx, gw) of imunpack_xent(..., want_grad=True) for grad, the gradient of its loss (fp32); None where not wanted."""
-    d, vocab = _xent_args(x, w)
-    rows, dtype, how = target.numel(), _DTYPES[x.dtype], REDUCTIONS[saved.reduction]
-    if grad.dtype != torch.float32 or not grad.is_cuda or grad.numel() != (rows if how == 0 else 1):
+    """Gradients (gx, gw) of imunpack_xent(..., want_grad=True) for grad, the gradient of its loss (fp32); None where not wanted.  The
+    first call for one loss hands out what the forward pass made, times grad; another one makes them anew."""
+    _xent_args(x, w, target)
+    if grad.dtype != torch.float32 or not grad.is_cuda or grad.numel() != (target.numel() if saved.reduction == "none" else 1):
         raise ValueError("grad is fp32 and shaped like the loss")
-    w2, ldw = _spread(w, d)
-    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_x else None
-    gw = torch.empty(w.shape, dtype=w.dtype, device=x.device) if want_w else None
     grad = grad.contiguous()
-    ws = torch.empty(saved.backward_bytes, dtype=torch.uint8, device=x.device)
-    _check(_lib.imunpack_xent_backward(w2.data_ptr(), ldw, rows, d, vocab, dtype, how, grad.data_ptr(), saved.buffer.data_ptr(), saved.buffer.numel(),
-                                       _ptr(gx), d, _ptr(gw), d, ws.data_ptr(), saved.backward_bytes, _stream()), "imunpack_xent_backward")
+    gx, gw = saved.gx if want_x else None, saved.gw if want_w else None
+    if (want_x and gx is None) or (want_w and gw is None):
+        return _xent(x, w, target, saved.ignore_index, REDUCTIONS[saved.reduction], None, grad, want_x, want_w)
+    saved.gx = saved.gw = None
+    if want_x or want_w:
+        _check(_lib.imunpack_xent_rescale(grad.data_ptr(), _ptr(gx), gx.numel() if want_x else 0, _ptr(gw), gw.numel() if want_w else 0, _DTYPES[x.dtype],
+                                          _stream()), "imunpack_xent_rescale")
     return gx, gw

@@ -4,9 +4,11 @@
 //   G[t, v] = (exp(l[t, v] - lse[t]) - [v = target[t]]) g[t],   gx = G W,   gW = G^T x            (g: the gradient of loss[t])
 //
 // Rows without a target take no part: those with one are gathered first, and how many there are is known on the device alone.
-// Forward: a tile of the product keeps, per row t, the largest logit and the sum of exponentials of its part of the vocabulary, and a
-// small kernel joins them.  Backward: a tile is made again and G leaves it in 16 bits, both ways round, for one piece of the vocabulary at a
-// time (at most kPieceBytes); gx and the piece's rows of gW are products of it.  8 T V d operations in all, all on the matrix cores.
+// A tile of the product l keeps, per row t, the largest logit and the sum of exponentials of its part of the vocabulary, and a small kernel
+// joins them to lse: for the loss alone nothing else of l is left.  For the gradients the rows go through in pieces (as many as kPieceBytes
+// allows): the tiles leave their exponentials in 16 bits, relative to the largest of the row and part; once lse stands they become G, both
+// ways round; gx and gW are products of it, and the next piece takes the same memory.  So l is made once: 6 T V d operations,
+// all on the matrix cores, and what is held does not grow with the rows.
 //
 // bfloat16 operands: products in bfloat16, G rounded to bfloat16.  fp32 operands: each value is the sum of two binary16 numbers
 // (22 bits of it; scaled by a power of two so that the operand's largest lies below 2^15) and a product is three of them, which is within
@@ -20,7 +22,7 @@
 #include <type_traits>
 
 namespace imu {
-constexpr int64_t kPieceBytes = 1ll << 30;  // G of a piece of the vocabulary, both ways round, at most (or 256 columns)
+constexpr int64_t kPieceBytes = 2ll << 30;  // G of a piece of the rows, both ways round, at most (or 256 rows)
 constexpr int kTop = 14;                    // the largest magnitude of a scaled operand is below 2^(kTop + 1)
 constexpr int kXentSlots = 256;             // parts of the tiles of a gradient that go at a time: one to a CU
 constexpr int kPartTiles = 8;               // k-tiles of a part at least: below that its sums cost more than its products
@@ -37,6 +39,8 @@ struct XentHeader {
     uint32_t found[kScanGroups];  // largest magnitudes as the workgroups found them
 };
 static_assert(sizeof(XentHeader) == 256 + 4 * kScanGroups, "header");
+// Rows of the piece that begins at row `first` and has room for `room`.
+__device__ __forceinline__ int rows_of(const XentHeader *hdr, int first, int room) { return max(0, min(hdr->count - first, room)); }
 
 // What 2 to its power an operand is multiplied by before it is split.
 __device__ __forceinline__ int scale_exponent(uint32_t amax) { return min(kTop - ((int)(amax >> 23) - 127), 126); }
@@ -134,6 +138,14 @@ struct PrepareArgs {
     int64_t vocab;
     int d, xtiles, nx, nw;                 // nx, nw: workgroups that looked for the largest magnitudes
 };
+// Sixteen values in a row: the lower halves of the words, or (second) the upper ones.
+__device__ __forceinline__ void put16(char *to, const uint32_t (&v)[16], bool second) {
+    v4i32 s[2];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s[k >> 2][k & 3] = (int)__builtin_amdgcn_perm(v[2 * k + 1], v[2 * k], second ? 0x07060302u : 0x05040100u);
+    *reinterpret_cast<v4i32 *>(to) = s[0];
+    *reinterpret_cast<v4i32 *>(to + 16) = s[1];
+}
 // 64 rows by 64 columns of x (gathered) or W: in 16 bits, one or two numbers to a value, row by row and transposed; zeros around.
 template <class T>
 __global__ __launch_bounds__(256) void xent_prepare_kernel(const PrepareArgs a) {
@@ -173,21 +185,11 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(const PrepareArgs a) 
 #pragma unroll
         for (int k = 0; k < 16; ++k) q[k] = __builtin_bit_cast(uint16_t, (__bf16)f[k >> 3][k & 7]);
     }
-    auto put = [&](char *to, const uint32_t (&v)[16], bool second) {
-        v4i32 s[2];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint32_t lo = second ? v[2 * k] >> 16 : v[2 * k] & 0xffffu, hi = second ? v[2 * k + 1] & 0xffff0000u : v[2 * k + 1] << 16;
-            s[k >> 2][k & 3] = (int)(lo | hi);
-        }
-        *reinterpret_cast<v4i32 *>(to) = s[0];
-        *reinterpret_cast<v4i32 *>(to + 16) = s[1];
-    };
     char *out = isX ? a.px : a.pw;
     if (out && (isX || row < rows)) {  // (rows of zeros behind the last of x; there is no room behind W's)
         char *to = out + row * a.pitch_p + (col0 + c) * 2;
-        put(to, q, false);
-        if (SPLIT) put(to + (isX ? a.px2 : a.pw2), q, true);
+        put16(to, q, false);
+        if (SPLIT) put16(to + (isX ? a.px2 : a.pw2), q, true);
     }
     out = isX ? a.tx : a.tw;
     if (!out) return;
@@ -198,32 +200,32 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(const PrepareArgs a) 
 #pragma unroll
     for (int k = 0; k < 16; ++k) q[k] = tile[c + k][r];
     char *to = out + (int64_t)(col0 + r) * (isX ? a.pitch_tx : a.pitch_tw) + (row0 + c) * 2;
-    put(to, q, false);
-    if (SPLIT) put(to + (isX ? a.tx2 : a.tw2), q, true);
+    put16(to, q, false);
+    if (SPLIT) put16(to + (isX ? a.tx2 : a.tw2), q, true);
 }
 
 // The gradient of each row's loss, as a factor between -2 and 2 and a power of two that the results are multiplied with at the end.
 struct Upstream {
-    const float *grad, *g;  // g: the rows' factors where each has a gradient of its own, else nullptr
+    const float *grad, *g;  // grad: nullptr for 1; g: the rows' factors where each has a gradient of its own, else nullptr
     int mean;
-    __device__ __forceinline__ float whole(const XentHeader *hdr) const { return mean ? *grad / (float)max(hdr->count, 1) : *grad; }
+    __device__ __forceinline__ float whole(const XentHeader *hdr) const {
+        const float one = grad ? *grad : 1.0f;
+        return mean ? one / (float)max(hdr->count, 1) : one;
+    }
     __device__ __forceinline__ static int exponent_of(float m) { return fabsf(m) > 0.0f ? (int)(__float_as_uint(fabsf(m)) >> 23) - 127 : 0; }
     __device__ __forceinline__ int exponent(const XentHeader *hdr) const { return g ? hdr->gexp : exponent_of(whole(hdr)); }
     __device__ __forceinline__ float one(const XentHeader *hdr) const { return ldexpf(whole(hdr), -exponent_of(whole(hdr))); }
 };
 
 struct LogitArgs {
-    Operand w, x;             // rows of the vocabulary (of this piece) and of x
+    Operand w, x;             // rows of the vocabulary and of the piece
     const XentHeader *hdr;
     const int32_t *wanted;
-    float *stats, *hit;       // forward: [part of the vocabulary][row] largest logit and sum; the target's logit
-    const float *lse;         // backward
-    Upstream up;
-    char *G, *GT;             // [row][vocabulary of the piece] and [vocabulary of the piece][row]
-    int64_t G2, GT2, pitch_G, pitch_GT;
-    int64_t stride;           // rows there is room for
-    int v0, ktiles;           // first column of the piece
-    int vlimit;               // columns of the piece, rounded up to whole k-tiles (what is stored of G)
+    float *stats, *hit;       // [part of the vocabulary][row of the piece] largest logit and sum; the target's logit
+    char *P;                  // [row of the piece][vocabulary] exponentials, relative to the largest of the row and part, times 2^kTop where they are binary16
+    int64_t P2, pitch_P;
+    int first, room;          // the piece's first row, and for how many there is room
+    int ktiles;
 };
 constexpr float kLog2e = 1.44269504088896340736f;
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
@@ -245,11 +247,11 @@ __device__ __forceinline__ void quad_transpose(uint32_t &lo, uint32_t &hi, int l
 
 // A tile of logits, vocabulary down, rows of x across: a lane holds one row of x per column block, so that the sums over the
 // vocabulary are sums over its registers and one exchange between the halves of the wave.
-template <bool F16, int T, bool BACK>
+template <bool F16, int T, bool KEEP>
 __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_kernel(const LogitArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     constexpr int kEdge = 64 * T;
-    const int count = a.hdr->count, vocab = a.w.rows, mtiles = (vocab + kEdge - 1) / kEdge, ntiles = (count + kEdge - 1) / kEdge;
+    const int count = rows_of(a.hdr, a.first, a.room), vocab = a.w.rows, mtiles = (vocab + kEdge - 1) / kEdge, ntiles = (count + kEdge - 1) / kEdge;
     if ((int)blockIdx.x >= mtiles * ntiles) return;
     int tm, tn;
     tile_at(blockIdx.x, mtiles, ntiles, tm, tn);
@@ -260,8 +262,7 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
     v16f32 acc[T][T];
     product_tile<F16, T, T, F16 ? 3 : 1>(a.w, x, tm * kEdge, tn * kEdge, 0, a.ktiles, smem, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, lhalf = lane >> 5;
-    const int vwave = tm * kEdge + (wave >> 1) * 32 * T, twave = tn * kEdge + (wave & 1) * 32 * T;  // the wave's first column of the piece and row
-    const float all = BACK && !a.up.g ? a.up.one(a.hdr) : 0.0f;
+    const int vwave = tm * kEdge + (wave >> 1) * 32 * T, twave = tn * kEdge + (wave & 1) * 32 * T;  // the wave's first column and row of the piece
     const int down = F16 ? -(scale_exponent(a.hdr->amax[0]) + scale_exponent(a.hdr->amax[1])) : 0;
     auto logit = [&](float x) __attribute__((always_inline)) { return F16 ? ldexpf(x, down) : x; };
     // FULL: no column behind the vocabulary and no row behind the last one in the wave's part (nothing to compare)
@@ -271,91 +272,70 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
         for (int j = 0; j < T; ++j) {
             const int t = twave + 32 * j + lrow;
             const bool in_rows = FULL || t < count;
-            const int hit_at = in_rows ? a.wanted[t] - a.v0 - vwave : -1;   // the target among the wave's columns
-            const bool hits = hit_at >= 0 && hit_at < 32 * T, any_hits = __ballot(hits) != 0;
-            const int vlane = vwave + 4 * lhalf, left = vocab - vlane, own = hit_at - 4 * lhalf;  // column 32 i + 8 q + k of the lane
-            if constexpr (!BACK) {
-                float top = -__builtin_inff(), sum = 0.0f;
+            const int hit_at = in_rows ? a.wanted[a.first + t] - vwave : -1;   // the target among the wave's columns
+            const bool hits = hit_at >= 0 && hit_at < 32 * T;
+            const int left = vocab - vwave - 4 * lhalf, own = hit_at - 4 * lhalf;  // the lane has columns 32 i + 8 q + k
+            float top = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < T; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (FULL || 32 * i + (r >> 2) * 8 + (r & 3) < left) top = fmaxf(top, acc[i][j][r]);
+            top = logit(fmaxf(top, __shfl_xor(top, 32)));
+            const float from = top == -__builtin_inff() ? 0.0f : -top * kLog2e;  // (nothing of the vocabulary in this part)
+            if (__ballot(hits) != 0) {
+                float hit = 0.0f;
 #pragma unroll
                 for (int i = 0; i < T; ++i)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (FULL || 32 * i + (r >> 2) * 8 + (r & 3) < left) top = fmaxf(top, acc[i][j][r]);
-                top = logit(fmaxf(top, __shfl_xor(top, 32)));
-                const float from = top == -__builtin_inff() ? 0.0f : -top * kLog2e;  // (nothing of the vocabulary in this part)
+                        if (32 * i + (r >> 2) * 8 + (r & 3) == own) hit = acc[i][j][r];
+                if (hits && ((hit_at >> 2) & 1) == lhalf) a.hit[a.first + t] = logit(hit);
+            }
+            char *to = a.P + t * a.pitch_P + (vwave + 8 * lhalf) * 2;
 #pragma unroll
-                for (int i = 0; i < T; ++i)
+            for (int i = 0; i < T; ++i) {
+                float p[16];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (FULL || 32 * i + (r >> 2) * 8 + (r & 3) < left) sum += __builtin_amdgcn_exp2f(fmaf(logit(acc[i][j][r]), kLog2e, from));
-                sum += __shfl_xor(sum, 32);
-                if (any_hits) {
-                    float hit = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < T; ++i)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (32 * i + (r >> 2) * 8 + (r & 3) == own) hit = acc[i][j][r];
-                    if (hits && ((hit_at >> 2) & 1) == lhalf) a.hit[t] = logit(hit);
+                for (int r = 0; r < 16; ++r) {
+                    p[r] = __builtin_amdgcn_exp2f(fmaf(logit(acc[i][j][r]), kLog2e, from));
+                    if (FULL || 32 * i + (r >> 2) * 8 + (r & 3) < left) sum += p[r];
                 }
-                if (in_rows && lhalf == 0)
-                    *reinterpret_cast<float2 *>(a.stats + ((int64_t)(2 * tm + (wave >> 1)) * a.stride + t) * 2) = make_float2(top, sum);
-            } else {
-                const float lse = in_rows ? -a.lse[t] * kLog2e : 0.0f, g = !a.up.g ? all : in_rows ? a.up.g[t] : 0.0f;
-                const float scaled = !in_rows ? 0.0f : F16 ? g * power_of_two(kTop) : g;
-                const int64_t trow = t * a.pitch_G, twidth = (count + 63) / 64 * 64;
-                const int tquad = t & ~3;
-#pragma unroll
-                for (int i = 0; i < T; ++i) {
-                    // in binary32 first: the lane's sixteen columns
-                    float p[16];
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(logit(acc[i][j][r]), kLog2e, lse));
-                    if (any_hits)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (32 * i + (r >> 2) * 8 + (r & 3) == own) p[r] -= 1.0f;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) p[r] = FULL || (in_rows && 32 * i + (r >> 2) * 8 + (r & 3) < left) ? p[r] * scaled : 0.0f;
-                    auto put = [&](const uint32_t (&w)[8], int64_t offG, int64_t offGT) __attribute__((always_inline)) {
-                        // G: columns 8 q .. 8 q + 7 lie in both halves of the wave; they trade, and each half has eight in a row
+                if constexpr (KEEP) {
+                    // columns 8 q .. 8 q + 7 lie in both halves of the wave; the halves trade, and each has eight in a row: 16 bytes to a store
+                    auto put = [&](const uint32_t (&w)[8], int64_t off) __attribute__((always_inline)) {
 #pragma unroll
                         for (int q = 0; q < 4; q += 2) {
                             const auto x = __builtin_amdgcn_permlane32_swap(w[2 * q], w[2 * q + 2], false, false);
                             const auto y = __builtin_amdgcn_permlane32_swap(w[2 * q + 1], w[2 * q + 3], false, false);
-                            const int v = vwave + 32 * i + 8 * q + 8 * lhalf;
-                            if (FULL || (in_rows && v < a.vlimit))
-                                *reinterpret_cast<v4i32 *>(a.G + offG + trow + v * 2) = v4i32{(int)x[0], (int)y[0], (int)x[1], (int)y[1]};
-                        }
-                        // G^T: four rows of x by four columns trade places among four lanes
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            uint32_t lo = w[2 * q], hi = w[2 * q + 1];
-                            quad_transpose(lo, hi, lane);
-                            const int v = vlane + 32 * i + 8 * q + (lane & 3);
-                            if (FULL || (v < vocab && tquad < twidth)) *reinterpret_cast<uint2 *>(a.GT + offGT + v * a.pitch_GT + tquad * 2) = make_uint2(lo, hi);
+                            if (FULL || in_rows)
+                                *reinterpret_cast<v4i32 *>(to + off + (32 * i + 8 * q) * 2) = v4i32{(int)x[0], (int)y[0], (int)x[1], (int)y[1]};
                         }
                     };
                     uint32_t w[8];
                     if constexpr (F16) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
-                            const _Float16 h0 = (_Float16)p[2 * k], h1 = (_Float16)p[2 * k + 1];
+                            const float p0 = p[2 * k] * power_of_two(kTop), p1 = p[2 * k + 1] * power_of_two(kTop);
+                            const _Float16 h0 = (_Float16)p0, h1 = (_Float16)p1;
                             w[k] = pack(h0, h1);
-                            p[2 * k] -= (float)h0;
-                            p[2 * k + 1] -= (float)h1;
+                            p[2 * k] = p0 - (float)h0;
+                            p[2 * k + 1] = p1 - (float)h1;
                         }
-                        put(w, 0, 0);
+                        put(w, 0);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) w[k] = pack((_Float16)p[2 * k], (_Float16)p[2 * k + 1]);
-                        put(w, a.G2, a.GT2);
+                        put(w, a.P2);
                     } else {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) w[k] = pack((__bf16)p[2 * k], (__bf16)p[2 * k + 1]);
-                        put(w, 0, 0);
+                        put(w, 0);
                     }
                 }
             }
+            sum += __shfl_xor(sum, 32);
+            if (in_rows && lhalf == 0)
+                *reinterpret_cast<float2 *>(a.stats + ((int64_t)(2 * tm + (wave >> 1)) * a.room + t) * 2) = make_float2(top, sum);
         }
     };
     if (vwave + 32 * T <= vocab && twave + 32 * T <= count) finish(std::true_type());
@@ -364,8 +344,7 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
 
 struct JoinArgs {
     const float *stats, *hit;
-    int parts, how;
-    int64_t stride;
+    int parts, how, first, room;
     XentHeader *hdr;
     const int32_t *source;
     float *lse, *row_loss, *loss;
@@ -375,13 +354,13 @@ struct JoinArgs {
 __global__ __launch_bounds__(256) void xent_join_kernel(const JoinArgs a) {
     __shared__ float tops[32][kJoinRows], sums[32][kJoinRows], lds[4];
     __shared__ int last;
-    const int r = threadIdx.x % kJoinRows, g = threadIdx.x / kJoinRows, t = blockIdx.x * kJoinRows + r, count = a.hdr->count;
-    const int groups = max(1, (count + kJoinRows - 1) / kJoinRows);
-    if ((int)blockIdx.x >= groups) return;
+    const int r = threadIdx.x % kJoinRows, g = threadIdx.x / kJoinRows, at = blockIdx.x * kJoinRows + r, t = a.first + at, count = a.hdr->count;
+    const int groups = max(1, (count + kJoinRows - 1) / kJoinRows);  // of all pieces
+    if ((int)blockIdx.x + a.first / kJoinRows >= groups) return;
     float top = -__builtin_inff(), sum = 0.0f;
     if (t < count)
         for (int k = g; k < a.parts; k += 32) {
-            const float2 s = *reinterpret_cast<const float2 *>(a.stats + ((int64_t)k * a.stride + t) * 2);
+            const float2 s = *reinterpret_cast<const float2 *>(a.stats + ((int64_t)k * a.room + at) * 2);
             const float next = fmaxf(top, s.x);
             if (next > -__builtin_inff()) sum = sum * fast_exp(top - next) + s.y * fast_exp(s.x - next);
             else sum += s.y;  // (NaN stays)
@@ -400,7 +379,7 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const JoinArgs a) {
         const float l = from + logf(sum), v = l - a.hit[t];
         a.lse[t] = l;
         __hip_atomic_store(a.row_loss + t, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // (past this XCD's cache: no fence has to write it back)
-        if (a.how == IMUNPACK_NONE) a.loss[a.source[t]] = v;
+        if (a.how == IMUNPACK_NONE && a.loss) a.loss[a.source[t]] = v;
     }
     if (a.how == IMUNPACK_NONE) return;
     stores_done();
@@ -426,6 +405,70 @@ __global__ __launch_bounds__(1024) void xent_factor_kernel(const float *grad, Xe
     for (int t = threadIdx.x; t < count; t += 1024) g[t] = ldexpf(grad[source[t]], -e);
 }
 
+struct TurnArgs {
+    const XentHeader *hdr;
+    const int32_t *wanted;
+    const float *stats, *lse;
+    Upstream up;
+    char *P, *GT;             // P becomes G; G^T: [vocabulary][row of the piece]
+    int64_t P2, GT2, pitch_P, pitch_GT;
+    int first, room, vocab, part;  // part: columns that share a largest logit
+};
+// 64 rows by 64 columns of exponentials become G where they lie, and G^T.
+template <bool F16>
+__global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
+    __shared__ uint32_t tile[64][65];
+    const int rows = rows_of(a.hdr, a.first, a.room), row0 = blockIdx.y * 64, col0 = blockIdx.x * 64;
+    if (row0 >= rows) return;
+    const int r = threadIdx.x >> 2, c = (threadIdx.x & 3) * 16, t = row0 + r, left = a.vocab - (col0 + c);
+    uint32_t q[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) q[k] = 0;
+    if (t < rows) {
+        char *p = a.P + t * a.pitch_P + (col0 + c) * 2;
+        v4i32 hi[2], lo[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            hi[k] = *reinterpret_cast<const v4i32 *>(p + 16 * k);
+            if (F16) lo[k] = *reinterpret_cast<const v4i32 *>(p + a.P2 + 16 * k);
+        }
+        const float top = a.stats[((int64_t)(col0 / a.part) * a.room + t) * 2];
+        const float g = a.up.g ? a.up.g[a.first + t] : a.up.one(a.hdr);
+        const float down = __builtin_amdgcn_exp2f((top - a.lse[a.first + t]) * kLog2e) * g, one = F16 ? g * power_of_two(kTop) : g;
+        const int own = a.wanted[a.first + t] - (col0 + c);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const uint16_t h = (uint16_t)((uint32_t)hi[k >> 3][(k >> 1) & 3] >> (16 * (k & 1)));
+            float v;
+            if constexpr (F16) {
+                const uint16_t l = (uint16_t)((uint32_t)lo[k >> 3][(k >> 1) & 3] >> (16 * (k & 1)));
+                v = (float)__builtin_bit_cast(_Float16, h) + (float)__builtin_bit_cast(_Float16, l);
+            } else {
+                v = (float)__builtin_bit_cast(__bf16, h);
+            }
+            v = v * down - (k == own ? one : 0.0f);
+            if (k >= left) v = 0.0f;
+            if constexpr (F16) {
+                const _Float16 x = (_Float16)v;
+                q[k] = pack(x, (_Float16)(v - (float)x));
+            } else {
+                q[k] = __builtin_bit_cast(uint16_t, (__bf16)v);
+            }
+        }
+        put16(p, q, false);
+        if (F16) put16(p + a.P2, q, true);
+    }
+#pragma unroll
+    for (int k = 0; k < 16; ++k) tile[r][c + k] = q[k];
+    __syncthreads();
+    if (col0 + r >= a.vocab) return;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) q[k] = tile[c + k][r];
+    char *to = a.GT + (int64_t)(col0 + r) * a.pitch_GT + (row0 + c) * 2;
+    put16(to, q, false);
+    if (F16) put16(to + a.GT2, q, true);
+}
+
 // Into how many parts the tiles of a gradient are cut along the contraction, so that every CU has one.
 __host__ __device__ __forceinline__ int parts_of(int tiles, int slots, int ktiles) {
     const int most = tiles > 0 ? slots / tiles : 1, able = ktiles / kPartTiles;
@@ -434,27 +477,29 @@ __host__ __device__ __forceinline__ int parts_of(int tiles, int slots, int ktile
 }
 
 struct GradArgs {
-    Operand G, wt;     // gx: [row][vocabulary of the piece], [feature][vocabulary of the piece]
-    Operand GT, xt;    // gW: [vocabulary of the piece][row], [feature][row]
+    Operand G, wt;     // gx: [row of the piece][vocabulary], [feature][vocabulary]
+    Operand GT, xt;    // gW: [vocabulary][row of the piece], [feature][row of the piece]
     const XentHeader *hdr;
     Upstream up;
-    float *xparts, *wparts;  // [slot][tile]; wparts only where the tiles of gW are cut
-    void *gw;                // the piece's first row
+    float *xparts, *wparts;  // [slot][tile]; wparts: where the tiles of gW are cut, or are sums over several pieces
+    void *gw;
     int64_t ldgw;
-    int ktiles, cut_ktiles, xslots, wcut, first;  // k-tiles of gx's contraction: of this piece, and those that its tiles are cut by
+    int ktiles, xslots, wcut, first, room;  // k-tiles of gx's contraction
+    bool through;            // gW goes through wparts
 };
-// Both gradients of a piece: the first xslots workgroups take parts of the tiles of gx, those behind them tiles of gW (parts of them,
-// where there are few), so that neither waits for the other's last ones.
+// Both gradients from a piece of the rows: the first xslots workgroups take parts of the tiles of gx, those behind them tiles of gW (parts of
+// them, where there are few), so that neither waits for the other's last ones.
 template <bool F16, int T>
 __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_grads_kernel(const GradArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     constexpr int kEdge = 64 * T;
     const bool isX = (int)blockIdx.x < a.xslots;
-    const int count = a.hdr->count, wg = isX ? blockIdx.x : blockIdx.x - a.xslots;
+    const int count = rows_of(a.hdr, a.first, a.room), wg = isX ? blockIdx.x : blockIdx.x - a.xslots;
     Operand A = isX ? a.G : a.GT, B = isX ? a.wt : a.xt;
     if (isX) A.rows = count;
+    else if (count == 0 && a.first > 0) return;  // (the first piece writes zeros)
     const int mtiles = (A.rows + kEdge - 1) / kEdge, ntiles = (B.rows + kEdge - 1) / kEdge, tiles = mtiles * ntiles;
-    const int ktiles = isX ? a.ktiles : (count + kStageCols - 1) / kStageCols, parts = isX ? parts_of(tiles, a.xslots, a.cut_ktiles) : a.wcut;
+    const int ktiles = isX ? a.ktiles : (count + kStageCols - 1) / kStageCols, parts = isX ? parts_of(tiles, a.xslots, a.ktiles) : a.wcut;
     if (wg >= tiles * parts) return;
     int tm, tn, part = 0, slot = 0;
     if (parts == 1) {
@@ -475,9 +520,9 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_grads_ke
     product_tile<F16, T, T, F16 ? 3 : 1>(A, B, tm * kEdge, tn * kEdge, __builtin_amdgcn_readfirstlane(k0), __builtin_amdgcn_readfirstlane(k1), smem, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r0 = (wave >> 1) * 32 * T + 4 * (lane >> 5), c0 = (wave & 1) * 32 * T + (lane & 31);
-    if (isX || a.wcut > 1) {
+    if (isX || a.through) {
         float *to = (isX ? a.xparts : a.wparts) + (int64_t)slot * kEdge * kEdge + r0 * kEdge + c0;
-        const bool add = isX && !a.first;
+        const bool add = !isX && a.first > 0;
 #pragma unroll
         for (int i = 0; i < T; ++i)
 #pragma unroll
@@ -528,18 +573,19 @@ struct FoldArgs {
     const int32_t *place;
     void *gx, *gw;
     int64_t ldgx, ldgw, xrows, wrows;  // rows of gx and gW that are made here
-    int d, edge, ktiles, xslots, wcut;
+    int d, edge, ktiles, xslots, wcut, first, room;
 };
-// Rows of gx (zeros for those without a target) and of gW from the parts of their tiles.
+// Rows of gx that belong to the piece (the first: zeros for those without a target) and of gW from the parts of their tiles.
 template <class T>
 __global__ __launch_bounds__(256) void xent_fold_kernel(const FoldArgs a) {
     const bool isX = (int64_t)blockIdx.x < a.xrows;
     const int64_t row = isX ? blockIdx.x : blockIdx.x - a.xrows;
-    const int col = (blockIdx.y * 256 + threadIdx.x) * 4, at = isX ? a.place[row] : (int)row, edge = a.edge;
-    if (col >= a.d) return;
+    const int col = (blockIdx.y * 256 + threadIdx.x) * 4, place = isX ? a.place[row] : (int)row, edge = a.edge;
+    const int rows = isX ? rows_of(a.hdr, a.first, a.room) : (int)a.wrows, at = isX && place >= 0 ? place - a.first : place;
+    if (col >= a.d || (isX && (place < 0 ? a.first > 0 : at < 0 || at >= rows))) return;
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (at >= 0) {
-        const int mtiles = ((isX ? a.hdr->count : (int)a.wrows) + edge - 1) / edge, ntiles = (a.d + edge - 1) / edge, tiles = mtiles * ntiles;
+        const int mtiles = (rows + edge - 1) / edge, ntiles = (a.d + edge - 1) / edge, tiles = mtiles * ntiles;
         const int n = isX ? parts_of(tiles, a.xslots, a.ktiles) : a.wcut, tile = col / edge * mtiles + at / edge;
         const float *p = (isX ? a.xparts : a.wparts) + (int64_t)tile * edge * edge + (at % edge) * edge + col % edge;
         for (int k = 0; k < n; ++k) {
@@ -553,30 +599,44 @@ __global__ __launch_bounds__(256) void xent_fold_kernel(const FoldArgs a) {
     store_upto<T, 4>((T *)(isX ? a.gx : a.gw) + row * (isX ? a.ldgx : a.ldgw) + col, s, a.d - col);
 }
 
+// What the gradients, which may have been made for a gradient of 1, are multiplied with.
+template <class T>
+__global__ __launch_bounds__(256) void xent_rescale_kernel(const float *grad, T *gx, int64_t nx, T *gw, int64_t nw) {
+    const float g = *grad;
+    if (g == 1.0f) return;
+    constexpr int N = kVec<T>;
+    for (int64_t k = ((int64_t)blockIdx.x * 256 + threadIdx.x) * N; k < nx + nw; k += (int64_t)gridDim.x * 256 * N) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const int64_t at = k + e;
+            if (at >= nx + nw) break;
+            T *p = at < nx ? gx + at : gw + (at - nx);
+            *p = (T)((float)*p * g);
+        }
+    }
+}
+
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-// Where everything lies in the forward pass's buffer, which the backward pass reads, and in the backward pass's own.
+// Where everything lies in the workspace.
 struct XentLayout {
     int64_t dp, tp, vp;           // features, rows, vocabulary rounded up to what the products read
     bool split, direct;           // two numbers to a value; W read in place
-    int64_t pitch_p, pitch_tx, pitch_tw;
-    size_t source, place, wanted, lse, row_loss, hit, stats, px, pw, tx, tw, bytes;
-    size_t px2, pw2, tx2, tw2;
+    int64_t pitch_p, pitch_tx, pitch_tw, pitch_P, pitch_GT;
     int edge_l, edge_g;           // tile edges of the logits and of the gradients
     int parts_v;                  // parts of the vocabulary whose sums are joined
-    int64_t piece, pieces;        // columns of the vocabulary to a piece
+    int64_t room, pieces;         // rows to a piece, pieces
     int xslots, wcut;             // parts of tiles of gx that go at a time; into how many parts the tiles of gW are cut
-    size_t g, G, GT, G2, GT2, xparts, wparts, back_bytes;
-    int64_t pitch_G, pitch_GT;
+    bool through;                 // gW goes through sums in fp32
+    size_t source, place, wanted, lse, row_loss, hit, g, stats, px, pw, tx, tw, P, GT, xparts, wparts, bytes;
+    size_t px2, pw2, tx2, tw2, P2, GT2;
 };
-// Large tiles where they fill the CUs.
-static int tile_edge(int64_t m, int64_t n) {
-    const int64_t large = up(m, 256) / 256 * (up(n, 256) / 256);
-    return large >= 128 ? 256 : 128;
-}
+// Large tiles where they fill half of the CUs at least.
+static int tile_edge(int64_t m, int64_t n) { return up(m, 256) / 256 * (up(n, 256) / 256) >= 128 ? 256 : 128; }
 static XentLayout xent_layout(const void *w, int64_t ldw, int64_t rows, int64_t d, int64_t vocab, int dtype, bool grad) {
     XentLayout l = {};
     l.split = dtype == IMUNPACK_F32;
+    const int64_t numbers = l.split ? 2 : 1;
     l.dp = up(d, kStageCols);
     l.tp = up(std::max<int64_t>(rows, 1), 256);
     l.vp = up(vocab, 256);
@@ -584,42 +644,39 @@ static XentLayout xent_layout(const void *w, int64_t ldw, int64_t rows, int64_t 
     l.edge_l = tile_edge(vocab, rows);
     l.edge_g = rows * d * vocab >= 1ll << 33 ? 256 : 128;
     l.parts_v = (int)(2 * (up(vocab, l.edge_l) / l.edge_l));
+    l.room = !grad ? l.tp : std::min(l.tp, std::max<int64_t>(256, kPieceBytes / (4 * numbers * l.vp) / 256 * 256));
+    l.pieces = (l.tp + l.room - 1) / l.room;
     size_t at = sizeof(XentHeader);
     auto take = [&](int64_t bytes) { const size_t here = at; at = (at + (size_t)bytes + 255) & ~(size_t)255; return here; };
     l.source = take(rows * 4); l.place = take(rows * 4); l.wanted = take(rows * 4);
-    l.lse = take(rows * 4); l.row_loss = take(rows * 4); l.hit = take(rows * 4);
-    l.stats = take((int64_t)l.parts_v * l.tp * 8);
-    const int pieces = l.split ? 2 : 1;
+    l.lse = take(rows * 4); l.row_loss = take(rows * 4); l.hit = take(rows * 4); l.g = take(rows * 4);
+    l.stats = take((int64_t)l.parts_v * l.room * 8);
     l.pitch_p = l.dp * 2;
     l.px2 = (size_t)(l.tp * l.pitch_p);
-    l.px = take((int64_t)l.px2 * pieces);
+    l.px = take((int64_t)l.px2 * numbers);
     l.pw2 = (size_t)up(vocab * l.pitch_p, 256);
-    l.pw = take(l.direct ? 0 : (int64_t)l.pw2 * pieces);
-    l.pitch_tx = l.tp * 2;
-    l.pitch_tw = l.vp * 2;
-    l.tx2 = (size_t)(d * l.pitch_tx);
-    l.tx = take(grad ? (int64_t)l.tx2 * pieces : 0);
-    l.tw2 = (size_t)(d * l.pitch_tw);
-    l.tw = take(grad ? (int64_t)l.tw2 * pieces : 0);
+    l.pw = take(l.direct ? 0 : (int64_t)l.pw2 * numbers);
+    if (grad) {
+        l.pitch_tx = l.tp * 2;
+        l.pitch_tw = l.vp * 2;
+        l.tx2 = (size_t)(d * l.pitch_tx);
+        l.tx = take((int64_t)l.tx2 * numbers);
+        l.tw2 = (size_t)(d * l.pitch_tw);
+        l.tw = take((int64_t)l.tw2 * numbers);
+        l.pitch_P = l.vp * 2;
+        l.pitch_GT = l.room * 2;
+        l.P2 = (size_t)(l.room * l.pitch_P);
+        l.P = take((int64_t)l.P2 * numbers);
+        l.GT2 = (size_t)(l.vp * l.pitch_GT);
+        l.GT = take((int64_t)l.GT2 * numbers);
+        const int64_t edge = l.edge_g, xtiles = up(l.room, edge) / edge * (up(d, edge) / edge), wtiles = up(vocab, edge) / edge * (up(d, edge) / edge);
+        l.xslots = (int)std::max<int64_t>(up(xtiles, 8), kXentSlots);
+        l.wcut = l.pieces == 1 && wtiles <= kXentSlots / 2 ? parts_of((int)wtiles, kXentSlots, (int)(up(rows, kStageCols) / kStageCols)) : 1;
+        l.through = l.wcut > 1 || l.pieces > 1;
+        l.xparts = take(l.xslots * edge * edge * 4);
+        l.wparts = take(l.through ? l.wcut * wtiles * edge * edge * 4 : 0);
+    }
     l.bytes = at;
-    // backward
-    const int64_t column = l.tp * 2 * 2 * pieces;  // bytes of a column of G
-    l.piece = std::min(l.vp, std::max<int64_t>(256, kPieceBytes / column / 256 * 256));
-    l.pieces = (vocab + l.piece - 1) / l.piece;
-    l.pitch_G = l.piece * 2;
-    l.pitch_GT = l.tp * 2;
-    at = 0;
-    l.g = take(rows * 4);
-    l.G2 = (size_t)(l.tp * l.pitch_G);
-    l.G = take((int64_t)l.G2 * pieces);
-    l.GT2 = (size_t)(l.piece * l.pitch_GT);
-    l.GT = take((int64_t)l.GT2 * pieces);
-    const int64_t edge = l.edge_g, xtiles = l.tp / edge * (up(d, edge) / edge), wtiles = up(vocab, edge) / edge * (up(d, edge) / edge);
-    l.xslots = (int)std::max<int64_t>(up(xtiles, 8), kXentSlots);
-    l.wcut = l.pieces == 1 && wtiles <= kXentSlots / 2 ? parts_of((int)wtiles, kXentSlots, (int)(up(rows, kStageCols) / kStageCols)) : 1;
-    l.xparts = take(l.xslots * edge * edge * 4);
-    l.wparts = take(l.wcut > 1 ? l.wcut * wtiles * edge * edge * 4 : 0);
-    l.back_bytes = at;
     return l;
 }
 
@@ -651,40 +708,38 @@ static int xent_lds_opt_in() {
 }
 
 template <bool F16, int T>
-static void launch_logits(const LogitArgs &a, bool back, int64_t rows, hipStream_t st) {
+static void launch_logits(const LogitArgs &a, bool keep, int64_t rows, hipStream_t st) {
     const dim3 grid((unsigned)(up(a.w.rows, 64 * T) / (64 * T) * (up(rows, 64 * T) / (64 * T))));
-    if (back) hipLaunchKernelGGL((xent_logits_kernel<F16, T, true>), grid, dim3(kProductThreads), product_lds(T, T), st, a);
+    if (keep) hipLaunchKernelGGL((xent_logits_kernel<F16, T, true>), grid, dim3(kProductThreads), product_lds(T, T), st, a);
     else hipLaunchKernelGGL((xent_logits_kernel<F16, T, false>), grid, dim3(kProductThreads), product_lds(T, T), st, a);
 }
-static int logits(const LogitArgs &a, bool f16, int edge, bool back, int64_t rows, hipStream_t st) {
-    if (f16) edge == 256 ? launch_logits<true, 4>(a, back, rows, st) : launch_logits<true, 2>(a, back, rows, st);
-    else edge == 256 ? launch_logits<false, 4>(a, back, rows, st) : launch_logits<false, 2>(a, back, rows, st);
-    return launch_status();
+template <bool F16, int T>
+static void launch_grads(const GradArgs &a, unsigned groups, hipStream_t st) {
+    hipLaunchKernelGGL((xent_grads_kernel<F16, T>), dim3(groups), dim3(kProductThreads), product_lds(T, T), st, a);
 }
 }  // namespace imu
 
 using namespace imu;
 
-extern "C" int imunpack_xent_workspace(const void *w, int64_t ldw, int64_t rows, int64_t d, int64_t vocab, int dtype, int want_grad, size_t *saved_bytes,
-                                       size_t *backward_bytes) {
-    if (!xent_sizes(rows, d, vocab, dtype) || ldw < d || !saved_bytes) return IMUNPACK_EINVAL;
-    const XentLayout l = xent_layout(w, ldw, rows, d, vocab, dtype, want_grad != 0);
-    *saved_bytes = l.bytes;
-    if (backward_bytes) *backward_bytes = l.back_bytes;
+extern "C" int imunpack_xent_workspace(const void *w, int64_t ldw, int64_t rows, int64_t d, int64_t vocab, int dtype, int want_grad, size_t *bytes) {
+    if (!xent_sizes(rows, d, vocab, dtype) || ldw < d || !bytes) return IMUNPACK_EINVAL;
+    *bytes = xent_layout(w, ldw, rows, d, vocab, dtype, want_grad != 0).bytes;
     return IMUNPACK_OK;
 }
 
 extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t ldw, const int64_t *target, int64_t rows, int64_t d, int64_t vocab,
-                             int dtype, int64_t ignore_index, int reduction, int want_grad, float *loss, void *saved, size_t saved_bytes,
-                             imunpack_stream_t stream) {
-    if (!xent_sizes(rows, d, vocab, dtype) || ldx < d || ldw < d || reduction < IMUNPACK_NONE || reduction > IMUNPACK_MEAN || !w || !saved || (size_t)saved % 16 ||
-        (rows > 0 && (!x || !target)) || (!loss && (rows > 0 || reduction != IMUNPACK_NONE)))
+                             int dtype, int64_t ignore_index, int reduction, float *loss, const float *grad, void *gx, int64_t ldgx, void *gw,
+                             int64_t ldgw, void *workspace, size_t workspace_bytes, imunpack_stream_t stream) {
+    if (!xent_sizes(rows, d, vocab, dtype) || ldx < d || ldw < d || reduction < IMUNPACK_NONE || reduction > IMUNPACK_MEAN || !w || !workspace ||
+        (size_t)workspace % 16 || (gx && ldgx < d) || (gw && ldgw < d) || (rows > 0 && (!x || !target)) || (!loss && !gx && !gw && rows > 0) ||
+        ((gx || gw) && !grad && rows > 0 && reduction == IMUNPACK_NONE))
         return IMUNPACK_EINVAL;
-    const XentLayout l = xent_layout(w, ldw, rows, d, vocab, dtype, want_grad != 0);
-    if (saved_bytes < l.bytes) return IMUNPACK_ESMALL;
+    const bool back = gx || gw;
+    const XentLayout l = xent_layout(w, ldw, rows, d, vocab, dtype, back);
+    if (workspace_bytes < l.bytes) return IMUNPACK_ESMALL;
     IMU_TRY(xent_lds_opt_in());
     hipStream_t st = (hipStream_t)stream;
-    char *s = (char *)saved;
+    char *s = (char *)workspace;
     XentHeader *hdr = (XentHeader *)s;
     int32_t *source = (int32_t *)(s + l.source), *place = (int32_t *)(s + l.place), *wanted = (int32_t *)(s + l.wanted);
     ScanArgs c = {};
@@ -695,101 +750,90 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
     const int nx = (int)std::min<int64_t>(up(rows, 64) / 64, kScanX), nw = (int)std::min<int64_t>(up(vocab, 64) / 64, kScanGroups - kScanX);
     c.nx = nx;
     hipLaunchKernelGGL(xent_scan_kernel, dim3(l.split && rows > 0 ? 1 + nx + nw : 1), dim3(1024), 0, st, c);
+    Upstream upstream = {grad, nullptr, reduction == IMUNPACK_MEAN};
+    if (back && reduction == IMUNPACK_NONE) {
+        upstream.g = (const float *)(s + l.g);
+        hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, grad, hdr, source, (float *)(s + l.g));
+    }
     if (rows > 0) {
         PrepareArgs p = {};
         p.x = x; p.w = w; p.ldx = ldx; p.ldw = ldw; p.hdr = hdr; p.source = source;
         p.px = s + l.px; p.px2 = l.px2;
         p.pw = l.direct ? nullptr : s + l.pw; p.pw2 = l.pw2;
-        if (want_grad) { p.tx = s + l.tx; p.tx2 = l.tx2; p.tw = s + l.tw; p.tw2 = l.tw2; }
+        p.tx = gw ? s + l.tx : nullptr; p.tx2 = l.tx2;
+        p.tw = gx ? s + l.tw : nullptr; p.tw2 = l.tw2;
         p.pitch_p = l.pitch_p; p.pitch_tx = l.pitch_tx; p.pitch_tw = l.pitch_tw;
         p.vocab = vocab; p.d = (int)d; p.xtiles = (int)(up(rows, 64) / 64); p.nx = nx; p.nw = nw;
+        // (fp32: a workgroup of W's leaves its largest magnitude for the kernels behind; with W read in place there is none)
         const unsigned wtiles = p.pw || p.tw ? (unsigned)(up(vocab, 64) / 64) : 0;
         const dim3 grid(p.xtiles + wtiles, (unsigned)(l.dp / 64));
         if (l.split) hipLaunchKernelGGL(xent_prepare_kernel<float>, grid, dim3(256), 0, st, p);
         else hipLaunchKernelGGL(xent_prepare_kernel<__bf16>, grid, dim3(256), 0, st, p);
-        LogitArgs a = {};
-        a.w = {l.direct ? (const char *)w : s + l.pw, l.direct ? ldw * 2 : l.pitch_p, (int64_t)l.pw2, (int)vocab};
-        a.x = {s + l.px, l.pitch_p, (int64_t)l.px2, 0};
-        a.hdr = hdr; a.wanted = wanted;
-        a.stats = (float *)(s + l.stats); a.hit = (float *)(s + l.hit);
-        a.stride = l.tp; a.ktiles = (int)(l.dp / kStageCols);
-        IMU_TRY(logits(a, l.split, l.edge_l, false, rows, st));
     }
-    if (rows > 0 || reduction != IMUNPACK_NONE) {
-        JoinArgs j = {};
-        j.stats = (const float *)(s + l.stats); j.hit = (const float *)(s + l.hit); j.parts = l.parts_v; j.how = reduction; j.stride = l.tp;
-        j.hdr = hdr; j.source = source; j.lse = (float *)(s + l.lse); j.row_loss = (float *)(s + l.row_loss); j.loss = loss;
-        hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)(up(std::max<int64_t>(rows, 1), kJoinRows) / kJoinRows)), dim3(256), 0, st, j);
+    for (int64_t piece = 0; piece < l.pieces; ++piece) {
+        const int64_t first = piece * l.room, n = std::min(l.room, rows - first);  // rows of the piece at most
+        if (n > 0) {
+            LogitArgs a = {};
+            a.w = {l.direct ? (const char *)w : s + l.pw, l.direct ? ldw * 2 : l.pitch_p, (int64_t)l.pw2, (int)vocab};
+            a.x = {s + l.px + first * l.pitch_p, l.pitch_p, (int64_t)l.px2, 0};
+            a.hdr = hdr; a.wanted = wanted; a.stats = (float *)(s + l.stats); a.hit = (float *)(s + l.hit);
+            a.P = s + l.P; a.P2 = l.P2; a.pitch_P = l.pitch_P;
+            a.first = (int)first; a.room = (int)l.room; a.ktiles = (int)(l.dp / kStageCols);
+            if (l.split) l.edge_l == 256 ? launch_logits<true, 4>(a, back, n, st) : launch_logits<true, 2>(a, back, n, st);
+            else l.edge_l == 256 ? launch_logits<false, 4>(a, back, n, st) : launch_logits<false, 2>(a, back, n, st);
+        }
+        if (n > 0 || (loss && reduction != IMUNPACK_NONE)) {
+            JoinArgs j = {};
+            j.stats = (const float *)(s + l.stats); j.hit = (const float *)(s + l.hit); j.parts = l.parts_v; j.first = (int)first; j.room = (int)l.room;
+            j.how = loss ? reduction : IMUNPACK_NONE;
+            j.hdr = hdr; j.source = source; j.lse = (float *)(s + l.lse); j.row_loss = (float *)(s + l.row_loss); j.loss = loss;
+            hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)(up(std::max<int64_t>(n, 1), kJoinRows) / kJoinRows)), dim3(256), 0, st, j);
+        }
+        if (!back) continue;
+        if (n > 0) {
+            TurnArgs t = {};
+            t.hdr = hdr; t.wanted = wanted; t.stats = (const float *)(s + l.stats); t.lse = (const float *)(s + l.lse); t.up = upstream;
+            t.P = s + l.P; t.GT = s + l.GT; t.P2 = l.P2; t.GT2 = l.GT2; t.pitch_P = l.pitch_P; t.pitch_GT = l.pitch_GT;
+            t.first = (int)first; t.room = (int)l.room; t.vocab = (int)vocab; t.part = l.edge_l / 2;
+            const dim3 grid((unsigned)(up(vocab, 64) / 64), (unsigned)(up(n, 64) / 64));
+            if (l.split) hipLaunchKernelGGL(xent_turn_kernel<true>, grid, dim3(256), 0, st, t);
+            else hipLaunchKernelGGL(xent_turn_kernel<false>, grid, dim3(256), 0, st, t);
+        }
+        GradArgs a = {};
+        a.G = {s + l.P, l.pitch_P, (int64_t)l.P2, 0};
+        a.wt = {s + l.tw, l.pitch_tw, (int64_t)l.tw2, (int)d};
+        a.GT = {s + l.GT, l.pitch_GT, (int64_t)l.GT2, (int)vocab};
+        a.xt = {s + l.tx + first * 2, l.pitch_tx, (int64_t)l.tx2, (int)d};
+        a.hdr = hdr; a.up = upstream; a.xparts = (float *)(s + l.xparts); a.wparts = (float *)(s + l.wparts);
+        a.gw = gw; a.ldgw = ldgw; a.ktiles = (int)(up(vocab, kStageCols) / kStageCols);
+        a.xslots = gx && n > 0 ? l.xslots : 0; a.wcut = l.wcut; a.through = l.through; a.first = (int)first; a.room = (int)l.room;
+        const int64_t edge = l.edge_g, wgroups = gw ? up(vocab, edge) / edge * (up(d, edge) / edge) * l.wcut : 0;
+        const unsigned groups = (unsigned)(a.xslots + wgroups);
+        if (groups > 0) {
+            if (l.split) edge == 256 ? launch_grads<true, 4>(a, groups, st) : launch_grads<true, 2>(a, groups, st);
+            else edge == 256 ? launch_grads<false, 4>(a, groups, st) : launch_grads<false, 2>(a, groups, st);
+        }
+        FoldArgs f = {};
+        f.xparts = a.xparts; f.wparts = a.wparts; f.hdr = hdr; f.up = upstream; f.place = place;
+        f.gx = gx; f.gw = gw; f.ldgx = ldgx; f.ldgw = ldgw;
+        f.xrows = a.xslots ? rows : 0; f.wrows = gw && l.through && piece + 1 == l.pieces ? vocab : 0;
+        f.d = (int)d; f.edge = l.edge_g; f.ktiles = a.ktiles; f.xslots = l.xslots; f.wcut = l.wcut; f.first = a.first; f.room = a.room;
+        if (f.xrows + f.wrows > 0) {
+            const dim3 grid((unsigned)(f.xrows + f.wrows), (unsigned)(up(d, 1024) / 1024));
+            if (l.split) hipLaunchKernelGGL(xent_fold_kernel<float>, grid, dim3(256), 0, st, f);
+            else hipLaunchKernelGGL(xent_fold_kernel<__bf16>, grid, dim3(256), 0, st, f);
+        }
     }
     return launch_status();
 }
 
-extern "C" int imunpack_xent_backward(const void *w, int64_t ldw, int64_t rows, int64_t d, int64_t vocab, int dtype, int reduction, const float *grad, void *saved,
-                                      size_t saved_bytes, void *gx, int64_t ldgx, void *gw, int64_t ldgw, void *workspace, size_t workspace_bytes,
-                                      imunpack_stream_t stream) {
-    if (!xent_sizes(rows, d, vocab, dtype) || ldw < d || (gx && ldgx < d) || (gw && ldgw < d) || reduction < IMUNPACK_NONE || reduction > IMUNPACK_MEAN || !w || !saved ||
-        !workspace || (size_t)saved % 16 || (size_t)workspace % 16 || (!grad && (rows > 0 || reduction != IMUNPACK_NONE)))
-        return IMUNPACK_EINVAL;
-    const XentLayout l = xent_layout(w, ldw, rows, d, vocab, dtype, true);
-    if (saved_bytes < l.bytes || workspace_bytes < l.back_bytes) return IMUNPACK_ESMALL;
-    if (!gx && !gw) return IMUNPACK_OK;
-    IMU_TRY(xent_lds_opt_in());
+extern "C" int imunpack_xent_rescale(const float *grad, void *gx, int64_t nx, void *gw, int64_t nw, int dtype, imunpack_stream_t stream) {
+    if (!grad || nx < 0 || nw < 0 || (nx > 0 && !gx) || (nw > 0 && !gw) || (dtype != IMUNPACK_F32 && dtype != IMUNPACK_BF16)) return IMUNPACK_EINVAL;
+    if (nx + nw == 0) return IMUNPACK_OK;
+    const int64_t pieces = (nx + nw + 1023) / 1024;
+    const dim3 grid((unsigned)std::min<int64_t>(pieces, 2048));
     hipStream_t st = (hipStream_t)stream;
-    char *s = (char *)saved, *b = (char *)workspace;
-    XentHeader *hdr = (XentHeader *)s;
-    const int32_t *source = (const int32_t *)(s + l.source), *place = (const int32_t *)(s + l.place);
-    Upstream upstream = {grad, nullptr, reduction == IMUNPACK_MEAN};
-    if (reduction == IMUNPACK_NONE) {
-        upstream.g = (const float *)(b + l.g);
-        hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, grad, hdr, source, (float *)(b + l.g));
-    }
-    const int xslots = gx && rows > 0 ? l.xslots : 0;
-    // the tiles of gx are cut alike in every piece; the last, shorter one leaves some parts with nothing to add
-    const int cut_ktiles = (int)(up(std::min(l.piece, vocab), kStageCols) / kStageCols);
-    for (int64_t p = 0; p < l.pieces; ++p) {
-        const int64_t v0 = p * l.piece, n = std::min(l.piece, vocab - v0);
-        const int ktiles = (int)(up(n, kStageCols) / kStageCols);
-        if (rows > 0) {
-            LogitArgs a = {};
-            a.w = {l.direct ? (const char *)w + v0 * ldw * 2 : s + l.pw + v0 * l.pitch_p, l.direct ? ldw * 2 : l.pitch_p, (int64_t)l.pw2, (int)n};
-            a.x = {s + l.px, l.pitch_p, (int64_t)l.px2, 0};
-            a.hdr = hdr; a.wanted = (const int32_t *)(s + l.wanted);
-            a.lse = (const float *)(s + l.lse); a.up = upstream;
-            a.G = b + l.G; a.GT = b + l.GT; a.G2 = l.G2; a.GT2 = l.GT2;
-            a.pitch_G = l.pitch_G; a.pitch_GT = l.pitch_GT;
-            a.v0 = (int)v0; a.ktiles = (int)(l.dp / kStageCols); a.vlimit = ktiles * kStageCols;
-            IMU_TRY(logits(a, l.split, l.edge_l, true, rows, st));
-        }
-        GradArgs a = {};
-        a.G = {b + l.G, l.pitch_G, (int64_t)l.G2, 0};
-        a.wt = {s + l.tw + v0 * 2, l.pitch_tw, (int64_t)l.tw2, (int)d};
-        a.GT = {b + l.GT, l.pitch_GT, (int64_t)l.GT2, (int)n};
-        a.xt = {s + l.tx, l.pitch_tx, (int64_t)l.tx2, (int)d};
-        a.hdr = hdr; a.up = upstream; a.xparts = (float *)(b + l.xparts); a.wparts = (float *)(b + l.wparts);
-        a.gw = (char *)gw + v0 * ldgw * (l.split ? 4 : 2); a.ldgw = ldgw;
-        a.ktiles = ktiles; a.cut_ktiles = cut_ktiles; a.xslots = xslots; a.wcut = l.wcut; a.first = p == 0;
-        const int64_t edge = l.edge_g, wgroups = gw ? up(n, edge) / edge * (up(d, edge) / edge) * l.wcut : 0;
-        const dim3 grid((unsigned)(xslots + wgroups)), block(kProductThreads);
-        const int lds = product_lds(l.edge_g / 64, l.edge_g / 64);
-        if (grid.x == 0) continue;
-        if (l.split) {
-            if (edge == 256) hipLaunchKernelGGL((xent_grads_kernel<true, 4>), grid, block, lds, st, a);
-            else hipLaunchKernelGGL((xent_grads_kernel<true, 2>), grid, block, lds, st, a);
-        } else {
-            if (edge == 256) hipLaunchKernelGGL((xent_grads_kernel<false, 4>), grid, block, lds, st, a);
-            else hipLaunchKernelGGL((xent_grads_kernel<false, 2>), grid, block, lds, st, a);
-        }
-        IMU_TRY(launch_status());
-    }
-    FoldArgs f = {};
-    f.xparts = (const float *)(b + l.xparts); f.wparts = (const float *)(b + l.wparts); f.hdr = hdr; f.up = upstream; f.place = place;
-    f.gx = gx; f.gw = gw; f.ldgx = ldgx; f.ldgw = ldgw;
-    f.xrows = xslots ? rows : 0; f.wrows = gw && l.wcut > 1 ? vocab : 0;
-    f.d = (int)d; f.edge = l.edge_g; f.ktiles = cut_ktiles; f.xslots = l.xslots; f.wcut = l.wcut;
-    if (f.xrows + f.wrows > 0) {
-        const dim3 grid((unsigned)(f.xrows + f.wrows), (unsigned)(up(d, 1024) / 1024));
-        if (l.split) hipLaunchKernelGGL(xent_fold_kernel<float>, grid, dim3(256), 0, st, f);
-        else hipLaunchKernelGGL(xent_fold_kernel<__bf16>, grid, dim3(256), 0, st, f);
-    }
+    if (dtype == IMUNPACK_F32) hipLaunchKernelGGL(xent_rescale_kernel<float>, grid, dim3(256), 0, st, grad, (float *)gx, nx, (float *)gw, nw);
+    else hipLaunchKernelGGL(xent_rescale_kernel<__bf16>, grid, dim3(256), 0, st, grad, (__bf16 *)gx, nx, (__bf16 *)gw, nw);
     return launch_status();
 }

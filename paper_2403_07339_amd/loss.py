@@ -2,7 +2,8 @@
 
     loss_t = log sum_v exp(x_t . W_v) - x_t . W_target(t)
 
-The head's product and its two gradients run inside the library, a piece of the vocabulary at a time; rows whose target is
+The head's product and its two gradients run inside the library, a piece of the rows at a time; the gradients of a mean or a sum are made
+by the forward pass, while the product is there, and multiplied with what arrives from above by the backward pass.  Rows whose target is
 ``ignore_index`` take no part.  fp32 or bfloat16 (both operands alike).
 """
 from __future__ import annotations
@@ -17,18 +18,16 @@ from . import binding as imu
 class _LossFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, target, ignore_index, reduction):
-        wanted = ctx.needs_input_grad[0] or ctx.needs_input_grad[1]
-        loss, saved = imu.imunpack_xent(x, weight, target, ignore_index, reduction, want_grad=wanted)
-        if wanted:
-            ctx.save_for_backward(x, weight, target, saved.buffer)
-            ctx.saved = (saved.backward_bytes, reduction)
+        want = ctx.needs_input_grad[:2]
+        loss, ctx.saved = imu.imunpack_xent(x, weight, target, ignore_index, reduction, any(want), *want)
+        if any(want):
+            ctx.save_for_backward(x, weight, target)
         return loss
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
-        x, weight, target, buffer = ctx.saved_tensors
-        gx, gw = imu.imunpack_xent_backward(x, weight, target, imu.XentSaved(buffer, *ctx.saved), grad, ctx.needs_input_grad[0], ctx.needs_input_grad[1])
+        gx, gw = imu.imunpack_xent_backward(*ctx.saved_tensors, ctx.saved, grad, *ctx.needs_input_grad[:2])
         return gx, gw, None, None, None
 
 

@@ -7,7 +7,8 @@ the terms' magnitudes.  So a logit is off by dl = c(K) S with c(K) = (2 K / 16) 
 lse: the largest dl of the row, an exponential with an argument off by 3 u |l - top| where exp counts it (x exp(-x) < 0.4: 2 u of the
 sum), and a sum through 64 registers, 8 exchanges and the parts of the vocabulary (V / 512 of them): 100 + V / 512.
 loss: lse's, the target's dl and 2 u of either.
-G: p off by dl + dlse + 3 u |l - lse| + 4 u of itself, 2 u of g; rounded to bfloat16: 2^-8 of it, as two binary16 numbers: 2^-22 and 2^-39 of 1.
+G: p off by dl + dlse + 3 u |l - lse| + 4 u of itself, 2 u of g; the exponential rounded to bfloat16: 2^-8 of p, and G again: 2^-8 of it; as two
+binary16 numbers: 2^-22 and 2^-39 of 1 each time.
 gx, gW: G's error through the product and c(K) of the magnitudes again; bfloat16 results rounded: 2^-8."""
 import pytest
 import torch
@@ -56,6 +57,7 @@ def reference(x, w, target, grad, dtype):
     p = torch.exp(l - lse[:, None])
     dp = p * (dl + dlse[:, None] + 3 * U * (l - lse[:, None]).abs() + 4 * U)
     G = p.scatter_add(1, at, torch.full_like(at, -1.0, dtype=F)) * g[:, None]
+    dp = dp + (2.0 ** -8 * p * 1.01 if low else 2.0 ** -22 * p + 2.0 ** -39)
     dG = (dp + 2 * U) * g.abs()[:, None] + (2.0 ** -8 * G.abs() if low else 2.0 ** -22 * G.abs() + 2.0 ** -38 * g.abs().max())
     gx, gw = G @ w6, G.t() @ x6
     dgx = dG @ w6.abs() + sums(vocab, dtype) * (G.abs() @ w6.abs()) + (2.0 ** -8 if low else U) * gx.abs()
@@ -99,15 +101,33 @@ def test_loss_and_gradients(imu, rows, d, vocab, dtype):
             assert abs(float(one) - float(loss[0].sum()) / div) <= (float(loss[1].sum()) + (n / 1024 + 20) * U * float(loss[0].abs().sum())) / div
             _, _, gx, gw = reference(x, w, target, torch.full_like(grad, -3.0 / div), dtype)
             a, b = imu.imunpack_xent_backward(x, w, target, saved, scale)
+            more = (2.0 ** -8 if dtype == torch.bfloat16 else U)      # the gradients for 1, rounded, times -3
+            within(a, (gx[0], gx[1] + more * gx[0].abs()))
+            within(b, (gw[0], gw[1] + more * gw[0].abs()))
+            again, b2 = imu.imunpack_xent_backward(x, w, target, saved, scale)   # made anew, with the -3 in G
+            within(again, gx)
+            within(b2, gw)
+            # the gradients for 1, and one of the two alone
+            _, saved = imu.imunpack_xent(x, w, target, reduction=reduction, want_grad=True)
+            _, _, gx, gw = reference(x, w, target, torch.full_like(grad, 1.0 / div), dtype)
+            a, b = imu.imunpack_xent_backward(x, w, target, saved, torch.ones((), device="cuda"))
             within(a, gx)
             within(b, gw)
+            _, saved = imu.imunpack_xent(x, w, target, reduction=reduction, want_grad=True, want_x=False)
+            none, b2 = imu.imunpack_xent_backward(x, w, target, saved, torch.ones((), device="cuda"), want_x=False)
+            assert none is None and torch.equal(b, b2)
+            _, saved = imu.imunpack_xent(x, w, target, reduction=reduction, want_grad=True, want_w=False)
+            a2, none = imu.imunpack_xent_backward(x, w, target, saved, torch.ones((), device="cuda"), want_w=False)
+            assert none is None and torch.equal(a, a2)
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-def test_pieces_of_the_vocabulary(imu, dtype):
-    """A vocabulary whose G does not fit one piece: 4096 rows of 32 KiB (fp32; 16 KiB bfloat16) a column."""
-    rows, d, vocab = 4096, 64, 33000 if dtype == torch.float32 else 66000
-    x, w, target, grad = inputs(rows, d, vocab, dtype, 1.0, 3)
+@pytest.mark.parametrize("share", [1.0, 0.3])
+def test_pieces_of_the_rows(imu, dtype, share):
+    """More rows than G of a piece has room for (8 bytes a column and row in fp32, 4 in bfloat16, 2 GiB in all); with a third of them the
+    later pieces are empty."""
+    rows, d, vocab = (4300, 70, 66000) if dtype == torch.float32 else (8500, 64, 66000)
+    x, w, target, grad = inputs(rows, d, vocab, dtype, share, 3)
     got, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
     a, b = imu.imunpack_xent_backward(x, w, target, saved, grad)
     for part in range(0, rows, 1024):     # (the reference of all rows at once takes too much memory)
@@ -117,6 +137,8 @@ def test_pieces_of_the_vocabulary(imu, dtype):
         within(a[r], gx)
         total = gw if part == 0 else (total[0] + gw[0], total[1] + gw[1])
     within(b, (total[0], total[1] + sums(rows, dtype) * total[0].abs()))
+    one, saved = imu.imunpack_xent(x, w, target, reduction="sum", want_grad=True)
+    assert abs(float(one) - float(got.to(F).sum())) <= (rows / 256 + 20) * U * float(got.sum())
 
 
 def test_nothing_to_learn_from_and_targets_outside(imu):
@@ -189,9 +211,9 @@ def test_strides_and_leading_dimensions(imu):
         assert torch.equal(got, loss.view(3, 20))
         a, b = imu.imunpack_xent_backward(x.view(3, 20, 72), w, target.view(3, 20), saved, grad.view(3, 20))
         assert torch.equal(a.view(60, 72), want[0]) and torch.equal(b, want[1])
-        a, none = imu.imunpack_xent_backward(x, w, target, saved, grad, want_w=False)
-        assert none is None and torch.equal(a, want[0])
-        none, b = imu.imunpack_xent_backward(x, w, target, saved, grad, want_x=False)
+        a, none = imu.imunpack_xent_backward(x.view(3, 20, 72), w, target.view(3, 20), saved, grad.view(3, 20), want_w=False)
+        assert none is None and torch.equal(a.view(60, 72), want[0])
+        none, b = imu.imunpack_xent_backward(x.view(3, 20, 72), w, target.view(3, 20), saved, grad.view(3, 20), want_x=False)
         assert none is None and torch.equal(b, want[1])
 
 
@@ -268,5 +290,5 @@ def test_refusals(imu):
         imu.imunpack_xent_backward(x, w, t, saved, torch.ones(4, device="cuda"))
     with pytest.raises(ValueError):
         imu.imunpack_xent_backward(x, w, t, saved, torch.ones((), device="cuda").double())
-    with pytest.raises(imu.ImunpackError):
-        imu.imunpack_xent_backward(x, w, t, imu.XentSaved(saved.buffer[:256], saved.backward_bytes, "mean"), torch.ones((), device="cuda"))
+    with pytest.raises(ValueError):
+        imu.imunpack_xent_backward(x, w[:, :7], t, saved, torch.ones((), device="cuda"))

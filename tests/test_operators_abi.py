@@ -72,22 +72,21 @@ def test_adamw(lib):
 
 
 def test_xent(lib):
-    size, back = C.c_size_t(), C.c_size_t()
-    call = caller(lib.imunpack_xent_workspace, [vp, i64, i64, i64, i64, i32, i32, vp, vp],
-                  dict(w=FAKE, ldw=64, rows=4, d=64, vocab=100, dtype=0, grad=1, size=C.addressof(size), back=C.addressof(back)))
+    size = C.c_size_t()
+    call = caller(lib.imunpack_xent_workspace, [vp, i64, i64, i64, i64, i32, i32, vp], dict(w=FAKE, ldw=64, rows=4, d=64, vocab=100, dtype=0, grad=1, size=C.addressof(size)))
     for bad in (dict(ldw=63), dict(rows=-1), dict(rows=(1 << 22) + 1), dict(d=0), dict(vocab=0), dict(vocab=(1 << 22) + 1), dict(dtype=2), dict(size=None)):
         assert call(**bad) == EINVAL, bad
-    assert call(rows=0) == 0 and call(back=None) == 0 and call() == 0 and size.value > 0 and back.value > 0
-    call = caller(lib.imunpack_xent, [vp, i64, vp, i64, vp, i64, i64, i64, i32, i64, i32, i32, vp, vp, C.c_size_t, vp],
-                  dict(x=FAKE, ldx=64, w=FAKE, ldw=64, target=FAKE, rows=4, d=64, vocab=100, dtype=0, ignore=-100, how=2, grad=1, loss=FAKE, saved=FAKE, bytes=size.value, st=None))
-    for bad in (dict(x=None), dict(w=None), dict(target=None), dict(loss=None), dict(saved=None), dict(saved=FAKE + 8), dict(ldx=63), dict(ldw=63), dict(how=3), dict(how=-1),
-                dict(dtype=-1), dict(d=0), dict(rows=-1)):
+    assert call(rows=0) == 0 and call(grad=0) == 0
+    least = size.value
+    assert call() == 0 and size.value > least > 0
+    call = caller(lib.imunpack_xent, [vp, i64, vp, i64, vp, i64, i64, i64, i32, i64, i32, vp, vp, vp, i64, vp, i64, vp, C.c_size_t, vp],
+                  dict(x=FAKE, ldx=64, w=FAKE, ldw=64, target=FAKE, rows=4, d=64, vocab=100, dtype=0, ignore=-100, how=2, loss=FAKE, grad=None, gx=FAKE, ldgx=64, gw=FAKE, ldgw=64,
+                       ws=FAKE, bytes=size.value, st=None))
+    for bad in (dict(x=None), dict(w=None), dict(target=None), dict(loss=None, gx=None, gw=None), dict(ws=None), dict(ws=FAKE + 8), dict(ldx=63), dict(ldw=63), dict(ldgx=63),
+                dict(ldgw=63), dict(how=3), dict(how=-1), dict(how=0), dict(dtype=-1), dict(d=0), dict(rows=-1), dict(vocab=-5)):
         assert call(**bad) == EINVAL, bad
     assert call(bytes=size.value - 1) == ESMALL
-    call = caller(lib.imunpack_xent_backward, [vp, i64, i64, i64, i64, i32, i32, vp, vp, C.c_size_t, vp, i64, vp, i64, vp, C.c_size_t, vp],
-                  dict(w=FAKE, ldw=64, rows=4, d=64, vocab=100, dtype=0, how=2, grad=FAKE, saved=FAKE, bytes=size.value, gx=FAKE, ldgx=64, gw=FAKE, ldgw=64, ws=FAKE,
-                       wbytes=back.value, st=None))
-    for bad in (dict(w=None), dict(grad=None), dict(saved=None), dict(ws=None), dict(ws=FAKE + 4), dict(ldgx=63), dict(ldgw=63), dict(how=7), dict(vocab=-5)):
+    call = caller(lib.imunpack_xent_rescale, [vp, vp, i64, vp, i64, i32, vp], dict(grad=FAKE, gx=FAKE, nx=4, gw=FAKE, nw=4, dtype=0, st=None))
+    for bad in (dict(grad=None), dict(gx=None), dict(gw=None), dict(nx=-1), dict(nw=-1), dict(dtype=3)):
         assert call(**bad) == EINVAL, bad
-    assert call(bytes=size.value - 1) == ESMALL and call(wbytes=back.value - 1) == ESMALL
-    assert call(gx=None, gw=None) == 0
+    assert call(nx=0, nw=0) == 0
