@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libimunpack.so: argument marshalling only.
+"""Thin binding of libimunpack.so (ctypes; for calls whose host time counts, C++ in _tensors.so): argument marshalling only.
 
 Function names and argument order follow ``include/imunpack.h``.  PyTorch is used for device
 memory and streams; every step of the path runs in the library's HIP kernels.  Importing this
@@ -7,7 +7,6 @@ is no CPU fallback.
 """
 from __future__ import annotations
 
-import array
 import ctypes as C
 import os
 from dataclasses import dataclass
@@ -19,9 +18,11 @@ OK, EINVAL, ERANGE, ENOMEM, EHIP, ESMALL = 0, -1, -2, -3, -4, -5
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("IMUNPACK_LIB") or os.path.join(_HERE, "libimunpack.so")
-if not os.path.exists(LIB_PATH):
-    raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2403_07339_amd.build`")
+for _path in (LIB_PATH, os.path.join(_HERE, "_tensors.so")):
+    if not os.path.exists(_path):
+        raise ImportError(f"{_path} is missing: build it with `python -m paper_2403_07339_amd.build`")
 _lib = C.CDLL(LIB_PATH)
+from . import _tensors  # noqa: E402
 
 EXPORTS = [
     "imunpack_quantize", "imunpack_scan", "imunpack_plan", "imunpack_plan_dims", "imunpack_plan_export",
@@ -575,28 +576,6 @@ _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 ADAMW_BLOCK = 256
 
 
-def _norm_args(x, weight, residual):
-    d = x.shape[-1]
-    if x.dtype not in _DTYPES or weight.dtype not in _DTYPES or not x.is_cuda or not weight.is_cuda:
-        raise ValueError("rmsnorm takes fp32 or bfloat16 device tensors")
-    if weight.shape != (d,) or not weight.is_contiguous():
-        raise ValueError(f"weight of shape {tuple(weight.shape)} for rows of {d}")
-    if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype or not residual.is_cuda):
-        raise ValueError("residual must be like x")
-    return d
-
-
-def _spread(t: torch.Tensor | None, d: int):
-    """t as rows of d elements with unit stride, a pitch apart: (tensor, pitch); laid out anew where its strides are others."""
-    if t is None or t.is_contiguous():
-        return t, d
-    if t.dim() != 2:
-        t = t.reshape(-1, d)
-    if (t.stride(1) != 1 and d > 1) or (t.shape[0] > 1 and t.stride(0) < d):
-        t = t.contiguous()
-    return t, t.stride(0) if t.shape[0] > 1 else d
-
-
 @dataclass
 class NormSaved:
     """What the backward pass of a norm takes from the forward pass: 1 / sqrt(mean(h^2) + eps) per row and, where h was rounded,
@@ -606,18 +585,14 @@ class NormSaved:
     residual: torch.Tensor | None = None
 
 
+_tensors.bind(ImunpackError, *[C.cast(getattr(_lib, _name), _vp).value for _name in (
+    "imunpack_rmsnorm", "imunpack_rmsnorm_quantize", "imunpack_rmsnorm_backward_workspace", "imunpack_rmsnorm_backward", "imunpack_adamw")])
+
+
 def imunpack_rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None):
     """y = h / sqrt(mean(h^2) + eps) * weight over the last dimension, h = x + residual.  Returns (y, h, saved): h is x itself
     without a residual; saved goes to imunpack_rmsnorm_backward."""
-    d = _norm_args(x, weight, residual)
-    x2, ldx = _spread(x, d)
-    r2, ldr = _spread(residual, d)
-    y = torch.empty_like(x, memory_format=torch.contiguous_format)
-    h = x if residual is None else torch.empty_like(y)
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    _check(_lib.imunpack_rmsnorm(x2.data_ptr(), ldx, _ptr(r2), ldr, weight.data_ptr(), rstd.numel(), d, _DTYPES[x.dtype], _DTYPES[weight.dtype],
-                                 eps, y.data_ptr(), d, None if residual is None else h.data_ptr(), d, rstd.data_ptr(), _stream()),
-           "imunpack_rmsnorm")
+    y, h, rstd = _tensors.rmsnorm(x, weight, eps, residual, _stream())
     return y, h, NormSaved(rstd) if residual is None or x.dtype == torch.float32 else NormSaved(rstd, x, residual)
 
 
@@ -625,17 +600,7 @@ def imunpack_rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, eps: float 
                               want_values: bool = False):
     """The norm with its output as In-Bound integers of b bits and a step per row.  Returns (q int8, scale fp32 per row, h, values):
     y is about q * scale; h is x itself without a residual; values (q * scale in x's type) only if wanted, else None."""
-    d = _norm_args(x, weight, residual)
-    x2, ldx = _spread(x, d)
-    r2, ldr = _spread(residual, d)
-    q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
-    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    h = x if residual is None else torch.empty_like(x, memory_format=torch.contiguous_format)
-    values = torch.empty_like(x, memory_format=torch.contiguous_format) if want_values else None
-    _check(_lib.imunpack_rmsnorm_quantize(x2.data_ptr(), ldx, _ptr(r2), ldr, weight.data_ptr(), scale.numel(), d, _DTYPES[x.dtype],
-                                          _DTYPES[weight.dtype], eps, b, q.data_ptr(), d, scale.data_ptr(), _ptr(values), d,
-                                          None if residual is None else h.data_ptr(), d, _stream()), "imunpack_rmsnorm_quantize")
-    return q, scale, h, values
+    return _tensors.rmsnorm_quantize(x, weight, eps, b, residual, want_values, _stream())
 
 
 def imunpack_rmsnorm_backward(gy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, saved: NormSaved, gh: torch.Tensor | None = None,
@@ -643,42 +608,7 @@ def imunpack_rmsnorm_backward(gy: torch.Tensor, h: torch.Tensor, weight: torch.T
     """Gradients of imunpack_rmsnorm: (gx, gweight) for gy, the gradient of y, and gh, that of h (what the residual stream
     brings).  gx is the gradient of x and of the residual alike."""
     x, residual = (h, None) if saved.x is None else (saved.x, saved.residual)
-    d = _norm_args(x, weight, residual)
-    if gy.shape != x.shape or gy.dtype != x.dtype or h.shape != x.shape or (gh is not None and (gh.shape != x.shape or gh.dtype != x.dtype)):
-        raise ValueError("h, gy and gh must be like x")
-    rstd = saved.rstd
-    if rstd.dtype != torch.float32 or rstd.shape != x.shape[:-1] or not rstd.is_contiguous():
-        raise ValueError("saved must be what imunpack_rmsnorm returned")
-    if not gy.is_cuda or (gh is not None and not gh.is_cuda):
-        raise ValueError("gradients must be device tensors")
-    g2, ldg = _spread(gy, d)
-    x2, ldx = _spread(x, d)
-    r2, ldr = _spread(residual, d)
-    b2, ldb = _spread(gh, d)
-    rows, dtype = rstd.numel(), _DTYPES[x.dtype]
-    gx = torch.empty_like(x, memory_format=torch.contiguous_format)
-    gw = ws = None
-    need = _sz(0)
-    if want_weight:
-        gw = torch.empty_like(weight)
-        _check(_lib.imunpack_rmsnorm_backward_workspace(rows, d, dtype, C.byref(need)), "imunpack_rmsnorm_backward_workspace")
-        ws = torch.empty(need.value, dtype=torch.uint8, device=x.device)
-    _check(_lib.imunpack_rmsnorm_backward(g2.data_ptr(), ldg, x2.data_ptr(), ldx, _ptr(r2), ldr, _ptr(b2), ldb, weight.data_ptr(), rstd.data_ptr(),
-                                          rows, d, dtype, _DTYPES[weight.dtype], gx.data_ptr(), d, _ptr(gw), _ptr(ws), need.value, _stream()),
-           "imunpack_rmsnorm_backward")
-    return gx, gw
-
-
-_ptrs, _numels, _dense, _devices = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.get_device
-
-
-def _table(tensors, dtype, sizes, device, what):
-    """The addresses of tensors of one type, of given sizes, on one GPU, for a call over many of them.  (Built-in loops, no line of
-    Python per tensor: hundreds of them come with every step.)"""
-    if ({t.dtype for t in tensors} != {dtype} or set(map(_devices, tensors)) != {device} or device < 0 or not all(map(_dense, tensors)) or
-            list(map(_numels, tensors)) != sizes):
-        raise ValueError(f"adamw: {what}: a tensor of the wrong type, size, device or layout")
-    return array.array("Q", map(_ptrs, tensors))
+    return _tensors.rmsnorm_backward(gy, x, residual, gh, weight, saved.rstd, want_weight, _stream())
 
 
 def imunpack_adamw(params, grads, exp_avg, exp_avg_sq, step: int, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
@@ -687,26 +617,18 @@ def imunpack_adamw(params, grads, exp_avg, exp_avg_sq, step: int, lr: float = 1e
     bfloat16; copies: bfloat16 tensors that receive the new params, or None.  Without m_scales / v_scales the states are fp32, like
     the params.  With them they are 8 bits: exp_avg and exp_avg_sq hold codes (torch.float8_e4m3fn) over whole blocks of
     ADAMW_BLOCK elements, m_scales and v_scales one fp32 per block (exp_avg_sq: of the root of the second moment)."""
-    eight = m_scales is not None
-    n = len(params)
-    if eight != (v_scales is not None) or any(len(x) != n for x in (grads, exp_avg, exp_avg_sq, m_scales, v_scales, copies) if x is not None):
-        raise ValueError("lists of different lengths")
-    if n == 0:
-        return
-    f32, gt = torch.float32, grads[0].dtype
-    if gt not in _DTYPES:
-        raise ValueError("adamw: gradients are fp32 or bfloat16")
-    numel = list(map(_numels, params))
-    blocks = [-(-k // ADAMW_BLOCK) for k in numel] if eight else None
-    held, st = ([ADAMW_BLOCK * k for k in blocks], torch.float8_e4m3fn) if eight else (numel, f32)
-    at = params[0].get_device()
-    p, g = _table(params, f32, numel, at, "params"), _table(grads, gt, numel, at, "grads")
-    m, v = _table(exp_avg, st, held, at, "exp_avg"), _table(exp_avg_sq, st, held, at, "exp_avg_sq")
-    ms, vs = (_table(m_scales, f32, blocks, at, "m_scales"), _table(v_scales, f32, blocks, at, "v_scales")) if eight else (None, None)
-    cp = _table(copies, torch.bfloat16, numel, at, "copies") if copies is not None else None
-    tables = (p, g, m, v, ms, vs, cp, array.array("q", numel))   # (held until the call has read them)
-    _check(_lib.imunpack_adamw(n, *[t.buffer_info()[0] if t is not None else None for t in tables], _DTYPES[gt], 8 if eight else 32, lr, beta1, beta2, eps,
-                               weight_decay, step, seed & 0xFFFFFFFF, _stream()), "imunpack_adamw")
+    _tensors.adamw(params, grads, exp_avg, exp_avg_sq, m_scales, v_scales, copies, lr, beta1, beta2, eps, weight_decay, step, seed & 0xFFFFFFFF, _stream())
+
+
+def _spread(t: torch.Tensor, d: int):
+    """t as rows of d elements with unit stride, a pitch apart: (tensor, pitch); laid out anew where its strides are others."""
+    if t.is_contiguous():
+        return t, d
+    if t.dim() != 2:
+        t = t.reshape(-1, d)
+    if (t.stride(1) != 1 and d > 1) or (t.shape[0] > 1 and t.stride(0) < d):
+        t = t.contiguous()
+    return t, t.stride(0) if t.shape[0] > 1 else d
 
 
 REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}

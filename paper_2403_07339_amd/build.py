@@ -1,18 +1,31 @@
-"""Builds libimunpack.so (gfx950) in-tree with hipcc."""
+"""Builds libimunpack.so (gfx950) in-tree with hipcc, and the module that marshals torch tensors for it (host code) with the C++ compiler."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libimunpack.so")
 SOURCES = ["api.hip", "percentile.hip", "quantize.hip", "plan.hip", "unpack.hip", "gemm.hip", "batched.hip", "norm.hip", "adamw.hip", "xent.hip"]
+TENSORS = os.path.join(HERE, "_tensors.so")
+CXX = os.environ.get("CXX", "g++")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fno-fast-math",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-result"]
+
+
+def _tensors_command() -> list[str]:
+    """The compiler's call for _tensors.so: a Python extension on torch's headers."""
+    import torch
+    from torch.utils import cpp_extension
+    libs = cpp_extension.library_paths()
+    return [CXX, "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            *[f"-isystem{p}" for p in cpp_extension.include_paths()], "-isystem" + sysconfig.get_paths()["include"], os.path.join(CSRC, "tensors.cpp"), "-o", TENSORS,
+            *[f"-L{p}" for p in libs], *[f"-Wl,-rpath,{p}" for p in libs], "-lc10", "-ltorch_cpu", "-ltorch_python"]
 
 
 def build(verbose: bool = False) -> str:
@@ -26,6 +39,7 @@ def build(verbose: bool = False) -> str:
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
         objs.append(obj)
+    procs.append(("tensors.cpp", subprocess.Popen(_tensors_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
     failed = False
     for src, pr in procs:
         out = pr.communicate()[0].decode()
@@ -36,7 +50,7 @@ def build(verbose: bool = False) -> str:
         elif verbose and text:
             print(f"--- {src}\n{text}")
     if failed:
-        raise RuntimeError("hipcc failed")
+        raise RuntimeError("the compiler failed")
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     subprocess.run(cmd, check=True)
     return LIB

@@ -1,0 +1,278 @@
+// The argument marshalling of the calls whose host time counts, in C++: a norm of a few rows takes the GPU five microseconds, an optimiser's
+// step takes six lists of hundreds of tensors, and as lines of Python their checks, allocations and addresses took 10 and 165 us more than
+// the launches.  What is checked and what is raised is the binding's: ValueError for tensors that do not fit, the binding's own error for a code that
+// the library returns.  No arithmetic, no GPU code; the library's functions come as addresses from the binding, which has loaded it.
+#include <Python.h>
+#include <ATen/ATen.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <array>
+#include <stdexcept>
+#include <string>
+#include <vector>
+
+#include "../../include/imunpack.h"
+
+namespace {
+PyObject *g_error = nullptr;  // the binding's error class, called with (code, where)
+decltype(&imunpack_rmsnorm) g_rmsnorm = nullptr;
+decltype(&imunpack_rmsnorm_quantize) g_rmsnorm_quantize = nullptr;
+decltype(&imunpack_rmsnorm_backward_workspace) g_rmsnorm_backward_workspace = nullptr;
+decltype(&imunpack_rmsnorm_backward) g_rmsnorm_backward = nullptr;
+decltype(&imunpack_adamw) g_adamw = nullptr;
+
+struct Refused : std::runtime_error {  // becomes a ValueError
+    using std::runtime_error::runtime_error;
+};
+struct Raised {};                      // a Python error is set already
+
+void check(int code, const char *where) {
+    if (code == IMUNPACK_OK) return;
+    if (PyObject *e = PyObject_CallFunction(g_error, "is", code, where)) {
+        PyErr_SetObject(g_error, e);
+        Py_DECREF(e);
+    }
+    throw Raised();
+}
+void need(bool ok, const char *what) {
+    if (!ok) throw Refused(what);
+}
+
+const at::Tensor &tensor(PyObject *o, const char *what) {
+    if (!THPVariable_Check(o)) throw Refused(std::string(what) + ": not a tensor");
+    return THPVariable_Unpack(o);
+}
+at::Tensor maybe(PyObject *o, const char *what) { return o == Py_None ? at::Tensor() : tensor(o, what); }
+double number(PyObject *o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Raised();
+    return v;
+}
+long long whole(PyObject *o) {
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Raised();
+    return v;
+}
+bool truth(PyObject *o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Raised();
+    return v != 0;
+}
+void *address(PyObject *o) {
+    void *p = PyLong_AsVoidPtr(o);
+    if (!p && PyErr_Occurred()) throw Raised();
+    return p;
+}
+void *data(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+PyObject *wrap(const at::Tensor &t) {
+    if (!t.defined()) Py_RETURN_NONE;
+    return THPVariable_Wrap(t);
+}
+template <size_t N>
+PyObject *wrapped(const std::array<at::Tensor, N> &ts) {
+    PyObject *r = PyTuple_New(N);
+    if (!r) throw Raised();
+    for (size_t k = 0; k < N; ++k) {
+        PyObject *o = wrap(ts[k]);
+        if (!o) {
+            Py_DECREF(r);
+            throw Raised();
+        }
+        PyTuple_SET_ITEM(r, k, o);
+    }
+    return r;
+}
+
+// IMUNPACK_F32, IMUNPACK_BF16 or a refusal.
+int type_of(const at::Tensor &t, const char *what) {
+    if (t.scalar_type() == at::kFloat) return IMUNPACK_F32;
+    if (t.scalar_type() == at::kBFloat16) return IMUNPACK_BF16;
+    throw Refused(std::string(what) + ": fp32 or bfloat16");
+}
+// A tensor as rows of d elements with unit stride, a pitch apart; laid out anew where its strides are others.
+struct Rows {
+    at::Tensor t;
+    int64_t pitch = 0;
+    void *p = nullptr;
+};
+Rows spread(const at::Tensor &t, int64_t d) {
+    Rows r;
+    r.pitch = d;
+    if (!t.defined()) return r;
+    r.t = t;
+    if (!t.is_contiguous()) {
+        if (t.dim() != 2) r.t = t.reshape({-1, d});
+        if ((r.t.stride(1) != 1 && d > 1) || (r.t.size(0) > 1 && r.t.stride(0) < d)) r.t = r.t.contiguous();
+        r.pitch = r.t.size(0) > 1 ? r.t.stride(0) : d;
+    }
+    r.p = r.t.data_ptr();
+    return r;
+}
+at::Tensor dense_like(const at::Tensor &t, at::ScalarType type) { return at::empty(t.sizes(), t.options().dtype(type).requires_grad(false)); }
+
+struct Norm {  // the arguments that every norm takes, checked
+    int64_t d;
+    int type, weight_type;
+};
+Norm norm_arguments(const at::Tensor &x, const at::Tensor &weight, const at::Tensor &residual) {
+    need(x.is_cuda() && weight.is_cuda(), "rmsnorm takes fp32 or bfloat16 device tensors");
+    need(x.dim() >= 1, "rmsnorm: x has no dimension");
+    const Norm n = {x.size(-1), type_of(x, "rmsnorm: x"), type_of(weight, "rmsnorm: weight")};
+    need(weight.dim() == 1 && weight.size(0) == n.d && weight.is_contiguous(), "rmsnorm: weight is one dense row like x's");
+    need(!residual.defined() || (residual.is_cuda() && residual.scalar_type() == x.scalar_type() && residual.sizes() == x.sizes()), "rmsnorm: residual must be like x");
+    return n;
+}
+at::Tensor per_row(const at::Tensor &x) { return at::empty(x.sizes().slice(0, x.dim() - 1), x.options().dtype(at::kFloat).requires_grad(false)); }
+
+PyObject *rmsnorm(PyObject *const *a) {  // x, weight, eps, residual, stream -> y, h, rstd
+    const at::Tensor &x = tensor(a[0], "rmsnorm: x"), &weight = tensor(a[1], "rmsnorm: weight");
+    const at::Tensor residual = maybe(a[3], "rmsnorm: residual");
+    const Norm n = norm_arguments(x, weight, residual);
+    const Rows rx = spread(x, n.d), rr = spread(residual, n.d);
+    const at::Tensor y = dense_like(x, x.scalar_type()), h = residual.defined() ? dense_like(x, x.scalar_type()) : x, rstd = per_row(x);
+    check(g_rmsnorm(rx.p, rx.pitch, rr.p, rr.pitch, weight.data_ptr(), rstd.numel(), n.d, n.type, n.weight_type, (float)number(a[2]), y.data_ptr(), n.d,
+                    residual.defined() ? h.data_ptr() : nullptr, n.d, (float *)rstd.data_ptr(), address(a[4])), "imunpack_rmsnorm");
+    return wrapped<3>({y, h, rstd});
+}
+
+PyObject *rmsnorm_quantize(PyObject *const *a) {  // x, weight, eps, b, residual, want_values, stream -> q, scale, h, values
+    const at::Tensor &x = tensor(a[0], "rmsnorm: x"), &weight = tensor(a[1], "rmsnorm: weight");
+    const at::Tensor residual = maybe(a[4], "rmsnorm: residual");
+    const Norm n = norm_arguments(x, weight, residual);
+    const Rows rx = spread(x, n.d), rr = spread(residual, n.d);
+    const at::Tensor q = dense_like(x, at::kChar), scale = per_row(x), h = residual.defined() ? dense_like(x, x.scalar_type()) : x;
+    const at::Tensor values = truth(a[5]) ? dense_like(x, x.scalar_type()) : at::Tensor();
+    check(g_rmsnorm_quantize(rx.p, rx.pitch, rr.p, rr.pitch, weight.data_ptr(), scale.numel(), n.d, n.type, n.weight_type, (float)number(a[2]), (int)whole(a[3]),
+                             (int8_t *)q.data_ptr(), n.d, (float *)scale.data_ptr(), data(values), n.d, residual.defined() ? h.data_ptr() : nullptr, n.d,
+                             address(a[6])), "imunpack_rmsnorm_quantize");
+    return wrapped<4>({q, scale, h, values});
+}
+
+PyObject *rmsnorm_backward(PyObject *const *a) {  // gy, x, residual, gh, weight, rstd, want_weight, stream -> gx, gweight
+    const at::Tensor &gy = tensor(a[0], "rmsnorm: gy"), &x = tensor(a[1], "rmsnorm: x"), &weight = tensor(a[4], "rmsnorm: weight"), &rstd = tensor(a[5], "rmsnorm: rstd");
+    const at::Tensor residual = maybe(a[2], "rmsnorm: residual"), gh = maybe(a[3], "rmsnorm: gh");
+    const Norm n = norm_arguments(x, weight, residual);
+    auto like = [&](const at::Tensor &t) { return t.is_cuda() && t.scalar_type() == x.scalar_type() && t.sizes() == x.sizes(); };
+    need(like(gy) && (!gh.defined() || like(gh)), "rmsnorm: h, gy and gh must be like x");
+    need(rstd.is_cuda() && rstd.scalar_type() == at::kFloat && rstd.is_contiguous() && rstd.sizes() == x.sizes().slice(0, x.dim() - 1),
+         "rmsnorm: saved must be what imunpack_rmsnorm returned");
+    const Rows rg = spread(gy, n.d), rx = spread(x, n.d), rr = spread(residual, n.d), rh = spread(gh, n.d);
+    const int64_t rows = rstd.numel();
+    const at::Tensor gx = dense_like(x, x.scalar_type());
+    at::Tensor gw, ws;
+    size_t bytes = 0;
+    if (truth(a[6])) {
+        gw = dense_like(weight, weight.scalar_type());
+        check(g_rmsnorm_backward_workspace(rows, n.d, n.type, &bytes), "imunpack_rmsnorm_backward_workspace");
+        ws = at::empty({(int64_t)bytes}, x.options().dtype(at::kByte).requires_grad(false));
+    }
+    check(g_rmsnorm_backward(rg.p, rg.pitch, rx.p, rx.pitch, rr.p, rr.pitch, rh.p, rh.pitch, weight.data_ptr(), (const float *)rstd.data_ptr(), rows, n.d, n.type,
+                             n.weight_type, gx.data_ptr(), n.d, data(gw), data(ws), bytes, address(a[7])), "imunpack_rmsnorm_backward");
+    return wrapped<2>({gx, gw});
+}
+
+// The addresses of a list of dense tensors of one type, of given sizes, on one GPU.
+std::vector<void *> table(PyObject *list, at::ScalarType type, const std::vector<int64_t> &sizes, const at::Device &device, const char *what) {
+    PyObject *seq = PySequence_Fast(list, "adamw takes lists of tensors");
+    if (!seq) throw Raised();
+    struct Held {
+        PyObject *o;
+        ~Held() { Py_DECREF(o); }
+    } held{seq};
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
+    if ((size_t)n != sizes.size()) throw Refused("adamw: lists of different lengths");
+    std::vector<void *> at(n);
+    for (Py_ssize_t k = 0; k < n; ++k) {
+        const at::Tensor &t = tensor(PySequence_Fast_GET_ITEM(seq, k), what);
+        if (t.scalar_type() != type || t.device() != device || !t.is_contiguous() || t.numel() != sizes[k])
+            throw Refused(std::string("adamw: ") + what + ": a tensor of the wrong type, size, device or layout");
+        at[k] = t.data_ptr();
+    }
+    return at;
+}
+
+PyObject *adamw(PyObject *const *a) {  // params, grads, exp_avg, exp_avg_sq, m_scales, v_scales, copies, lr, beta1, beta2, eps, decay, step, seed, stream
+    PyObject *params = PySequence_Fast(a[0], "adamw takes lists of tensors");
+    if (!params) throw Raised();
+    std::vector<int64_t> numel, held, blocks;
+    at::Device device(at::kCPU);
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(params);
+    const bool eight = a[4] != Py_None;
+    bool tensors = true;
+    for (Py_ssize_t k = 0; k < n && tensors; ++k) {
+        PyObject *o = PySequence_Fast_GET_ITEM(params, k);
+        tensors = THPVariable_Check(o);
+        if (!tensors) break;
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (k == 0) device = t.device();
+        numel.push_back(t.numel());
+        blocks.push_back((t.numel() + IMUNPACK_ADAMW_BLOCK - 1) / IMUNPACK_ADAMW_BLOCK);
+        held.push_back(eight ? blocks.back() * IMUNPACK_ADAMW_BLOCK : t.numel());
+    }
+    Py_DECREF(params);
+    need(tensors, "adamw: params: not a tensor");
+    need(eight == (a[5] != Py_None), "adamw: scales for both states or for none");
+    const at::ScalarType state = eight ? at::kFloat8_e4m3fn : at::kFloat;
+    at::ScalarType gtype = at::kFloat;
+    if (n > 0) {
+        need(device.is_cuda(), "adamw takes device tensors");
+        PyObject *first = PySequence_GetItem(a[1], 0);
+        if (!first) {
+            PyErr_Clear();
+            throw Refused("adamw: lists of different lengths");
+        }
+        const bool is = THPVariable_Check(first);
+        if (is) gtype = THPVariable_Unpack(first).scalar_type();
+        Py_DECREF(first);
+        need(is && (gtype == at::kFloat || gtype == at::kBFloat16), "adamw: gradients are fp32 or bfloat16 tensors");
+    }
+    const auto p = table(a[0], at::kFloat, numel, device, "params"), g = table(a[1], gtype, numel, device, "grads");
+    const auto m = table(a[2], state, held, device, "exp_avg"), v = table(a[3], state, held, device, "exp_avg_sq");
+    std::vector<void *> ms, vs, copies;
+    if (eight) {
+        ms = table(a[4], at::kFloat, blocks, device, "m_scales");
+        vs = table(a[5], at::kFloat, blocks, device, "v_scales");
+    }
+    if (a[6] != Py_None) copies = table(a[6], at::kBFloat16, numel, device, "copies");
+    check(g_adamw(n, (float *const *)p.data(), g.data(), m.data(), v.data(), eight ? (float *const *)ms.data() : nullptr, eight ? (float *const *)vs.data() : nullptr,
+                  a[6] != Py_None ? copies.data() : nullptr, numel.data(), gtype == at::kFloat ? IMUNPACK_F32 : IMUNPACK_BF16, eight ? 8 : 32, number(a[7]), number(a[8]),
+                  number(a[9]), number(a[10]), number(a[11]), whole(a[12]), (uint32_t)whole(a[13]), address(a[14])), "imunpack_adamw");
+    Py_RETURN_NONE;
+}
+
+// error class, then the addresses of the library's functions
+PyObject *bind(PyObject *const *a) {
+    Py_INCREF(a[0]);
+    Py_XDECREF(g_error);
+    g_error = a[0];
+    g_rmsnorm = (decltype(g_rmsnorm))address(a[1]);
+    g_rmsnorm_quantize = (decltype(g_rmsnorm_quantize))address(a[2]);
+    g_rmsnorm_backward_workspace = (decltype(g_rmsnorm_backward_workspace))address(a[3]);
+    g_rmsnorm_backward = (decltype(g_rmsnorm_backward))address(a[4]);
+    g_adamw = (decltype(g_adamw))address(a[5]);
+    Py_RETURN_NONE;
+}
+
+template <PyObject *(*F)(PyObject *const *), Py_ssize_t N>
+PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    try {
+        need(n == N, "wrong number of arguments");
+        return F(args);
+    } catch (const Raised &) {
+    } catch (const Refused &e) {
+        PyErr_SetString(PyExc_ValueError, e.what());
+    } catch (const std::exception &e) {  // torch's own (memory, a view that cannot be)
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    }
+    return nullptr;
+}
+template <PyObject *(*F)(PyObject *const *), Py_ssize_t N>
+PyMethodDef method(const char *name) {
+    return {name, (PyCFunction)(void (*)(void))entry<F, N>, METH_FASTCALL, nullptr};
+}
+PyMethodDef g_methods[] = {method<bind, 6>("bind"), method<rmsnorm, 5>("rmsnorm"), method<rmsnorm_quantize, 7>("rmsnorm_quantize"),
+                           method<rmsnorm_backward, 8>("rmsnorm_backward"), method<adamw, 15>("adamw"), {nullptr, nullptr, 0, nullptr}};
+PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_tensors", "Argument marshalling of the calls whose host time counts.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
+}  // namespace
+
+PyMODINIT_FUNC PyInit__tensors(void) { return PyModule_Create(&g_module); }
