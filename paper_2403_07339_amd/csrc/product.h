@@ -3,8 +3,8 @@
 // (32 TM) x (32 TN) each.
 //
 // The walk over the contraction is that of the int8 GEMM, whose fragments have the same bytes: k-tiles of 128 bytes (64 elements) of a row,
-// loaded straight into LDS, a ring of five half-stages (A and B of a k-tile in slots of their own), one barrier to a k-tile, loads
-// two k-tiles ahead.  16-byte piece c of row r lies at slot c ^ ((r >> 1) & 7) of the row, so that the 32 rows of a fragment fall on
+// loaded straight into LDS, a ring of 2 DEPTH + 1 half-stages (A and B of a k-tile in slots of their own), one barrier to a k-tile, loads
+// DEPTH k-tiles ahead: two, and four where a product has so few tiles that a CU has one small one to itself, whose time is that of its loads.  16-byte piece c of row r lies at slot c ^ ((r >> 1) & 7) of the row, so that the 32 rows of a fragment fall on
 // different banks.
 //
 // Segments: an operand may come in two pieces, A = A_0 + A_1 and B = B_0 + B_1 (binary32 values as the sums of two binary16 ones); the contraction is then
@@ -22,7 +22,7 @@ typedef int v4i32 __attribute__((ext_vector_type(4)));
 constexpr int kStageBytes = 128;   // of a row and k-tile
 constexpr int kStageCols = 64;     // 16-bit elements of it
 constexpr int kProductThreads = 256;
-constexpr int product_lds(int tm, int tn) { return 5 * 64 * (tm > tn ? tm : tn) * kStageBytes; }
+constexpr int product_lds(int tm, int tn, int depth) { return (2 * depth + 1) * 64 * (tm > tn ? tm : tn) * kStageBytes; }
 
 // One operand: rows of 16-bit elements, `pitch` bytes apart (a multiple of 16, as is the base), in one piece or two (`second` bytes
 // behind the first).  Rows from `rows` on are not read (the last one is, in their place).
@@ -61,11 +61,11 @@ __device__ __forceinline__ void tile_at(int wg, int mtiles, int ntiles, int &tm,
 
 // acc[i][j] of the wave: register r of lane l is the sum at row 32 i + (r / 4) * 8 + (l / 32) * 4 + r % 4 and column 32 j + l % 32 of the
 // wave's part of the tile.  k-tiles [k0, k1) of the contraction (which is k1 - k0 for each segment).
-template <bool F16, int TM, int TN, int SEGS>
+template <bool F16, int TM, int TN, int SEGS, int DEPTH>
 __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B, int m0, int n0, int k0, int k1, char *smem, v16f32 (&acc)[TM][TN]) {
     constexpr int kSlot = 64 * (TM > TN ? TM : TN) * kStageBytes;  // bytes of a slot of the ring
     constexpr int LA = 2 * TM, LB = 2 * TN;                        // loads of a wave for its share of a half-stage: 16 TM (16 TN) rows
-    constexpr int NF = TM + TN, NM = TM * TN;
+    constexpr int NF = TM + TN, NM = TM * TN, RING = 2 * DEPTH + 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -88,7 +88,7 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B,
         offB[u] = (unsigned)(min(row, B.rows - 1 - n0) * B.pitch) + (unsigned)(((lane & 7) ^ ((row >> 1) & 7)) * 16);
     }
     const char *gA = A.base + m0 * A.pitch + (int64_t)k0 * kStageBytes, *gB = B.base + n0 * B.pitch + (int64_t)k0 * kStageBytes;
-    auto ring = [](int slot, int k) { slot += k; return slot >= 5 ? slot - 5 : slot; };
+    auto ring = [](int slot, int k) { slot += k; return slot >= RING ? slot - RING : slot; };
     const char *pg = nullptr;
     unsigned dl = 0;
     // k-tile kt (of all segments; past the last one it is loaded again, into a slot that is not read) of A or B into a slot
@@ -138,9 +138,9 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B,
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // k-tile 0 landed, k-tile 1 on its way
+    // k-tile 0 landed, the next ones on their way
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
+    for (int p = 0; p < DEPTH; ++p) {
         setup(true, p, 2 * p);
 #pragma unroll
         for (int u = 0; u < LA; ++u) fetch(true, u);
@@ -148,28 +148,28 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B,
 #pragma unroll
         for (int u = 0; u < LB; ++u) fetch(false, u);
     }
-    asm volatile("s_waitcnt vmcnt(%0)" ::"i"(LA + LB) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"i"((DEPTH - 1) * (LA + LB)) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int q = 0; q < NF; ++q) fragment(smem, smem + kSlot, 0, 0, q);
-    // Steps 0 to 2 load A(kt + 2) into the slot that is free.  Behind them every fragment of k-tile kt has been read and this
+    // Steps 0 to 2 load A(kt + DEPTH) into the slot that is free.  Behind them every fragment of k-tile kt has been read and this
     // wave's parts of k-tile kt + 1 have landed (all but the newest loads); past the barrier that holds for all waves, so that step 3 may read k-tile
-    // kt + 1 and load B(kt + 2) into the slot of A(kt).
+    // kt + 1 and load B(kt + DEPTH) into the slot of A(kt).
     constexpr int c0 = (LA + 2) / 3, c1 = (LA - c0 + 1) / 2, c2 = LA - c0 - c1;
     int sa = 0;
     for (int kt = 0; kt < total; ++kt) {
         const char *stA = smem + sa * kSlot, *stB = smem + ring(sa, 1) * kSlot;
         const char *stA1 = smem + ring(sa, 2) * kSlot, *stB1 = smem + ring(sa, 3) * kSlot;
-        setup(true, kt + 2, ring(sa, 4));
+        setup(true, kt + DEPTH, ring(sa, 2 * DEPTH));
         __builtin_amdgcn_sched_barrier(0);
         step(0, stA, stB, 1, true, 0, c0);
         step(1, stA, stB, 2, true, c0, c1);
         step(0, stA, stB, 3, true, c0 + c1, c2);
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(LA) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"((DEPTH - 2) * (LA + LB) + LA) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        setup(false, kt + 2, sa);
+        setup(false, kt + DEPTH, sa);
         __builtin_amdgcn_sched_barrier(0);
         step(1, stA1, stB1, 0, false, 0, LB);
         sa = ring(sa, 2);

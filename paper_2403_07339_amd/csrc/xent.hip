@@ -24,8 +24,9 @@
 namespace imu {
 constexpr int64_t kPieceBytes = 2ll << 30;  // G of a piece of the rows, both ways round, at most (or 256 rows)
 constexpr int kTop = 14;                    // the largest magnitude of a scaled operand is below 2^(kTop + 1)
+constexpr unsigned kCus = 256;
 constexpr int kXentSlots = 256;             // parts of the tiles of a gradient that go at a time: one to a CU
-constexpr int kPartTiles = 8;               // k-tiles of a part at least: below that its sums cost more than its products
+constexpr int kPartTiles = 2;               // k-tiles of a part at least: below that its sums cost more than its products
 constexpr int kScanGroups = 512, kScanX = 64;  // workgroups that look for the largest magnitudes, those of x first
 constexpr int kJoinRows = 8;
 
@@ -247,8 +248,8 @@ __device__ __forceinline__ void quad_transpose(uint32_t &lo, uint32_t &hi, int l
 
 // A tile of logits, vocabulary down, rows of x across: a lane holds one row of x per column block, so that the sums over the
 // vocabulary are sums over its registers and one exchange between the halves of the wave.
-template <bool F16, int T, bool KEEP>
-__global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_kernel(const LogitArgs a) {
+template <bool F16, int T, int DEPTH, bool KEEP>
+__global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void xent_logits_kernel(const LogitArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     constexpr int kEdge = 64 * T;
     const int count = rows_of(a.hdr, a.first, a.room), vocab = a.w.rows, mtiles = (vocab + kEdge - 1) / kEdge, ntiles = (count + kEdge - 1) / kEdge;
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
     Operand x = a.x;
     x.rows = count;
     v16f32 acc[T][T];
-    product_tile<F16, T, T, F16 ? 3 : 1>(a.w, x, tm * kEdge, tn * kEdge, 0, a.ktiles, smem, acc);
+    product_tile<F16, T, T, F16 ? 3 : 1, DEPTH>(a.w, x, tm * kEdge, tn * kEdge, 0, a.ktiles, smem, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, lhalf = lane >> 5;
     const int vwave = tm * kEdge + (wave >> 1) * 32 * T, twave = tn * kEdge + (wave & 1) * 32 * T;  // the wave's first column and row of the piece
     const int down = F16 ? -(scale_exponent(a.hdr->amax[0]) + scale_exponent(a.hdr->amax[1])) : 0;
@@ -484,17 +485,17 @@ struct GradArgs {
     float *xparts, *wparts;  // [slot][tile]; wparts: where the tiles of gW are cut, or are sums over several pieces
     void *gw;
     int64_t ldgw;
-    int ktiles, xslots, wcut, first, room;  // k-tiles of gx's contraction
+    int ktiles, xslots, xgroups, wcut, first, room;  // k-tiles of gx's contraction; parts of its tiles at a time, workgroups there are for them
     bool through;            // gW goes through wparts
 };
-// Both gradients from a piece of the rows: the first xslots workgroups take parts of the tiles of gx, those behind them tiles of gW (parts of
+// Both gradients from a piece of the rows: the first xgroups workgroups take parts of the tiles of gx, those behind them tiles of gW (parts of
 // them, where there are few), so that neither waits for the other's last ones.
-template <bool F16, int T>
-__global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_grads_kernel(const GradArgs a) {
+template <bool F16, int T, int DEPTH>
+__global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void xent_grads_kernel(const GradArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     constexpr int kEdge = 64 * T;
-    const bool isX = (int)blockIdx.x < a.xslots;
-    const int count = rows_of(a.hdr, a.first, a.room), wg = isX ? blockIdx.x : blockIdx.x - a.xslots;
+    const bool isX = (int)blockIdx.x < a.xgroups;
+    const int count = rows_of(a.hdr, a.first, a.room), wg = isX ? blockIdx.x : blockIdx.x - a.xgroups;
     Operand A = isX ? a.G : a.GT, B = isX ? a.wt : a.xt;
     if (isX) A.rows = count;
     else if (count == 0 && a.first > 0) return;  // (the first piece writes zeros)
@@ -517,7 +518,7 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_grads_ke
     tn = __builtin_amdgcn_readfirstlane(tn);
     const int k0 = (int)((int64_t)ktiles * part / parts), k1 = (int)((int64_t)ktiles * (part + 1) / parts);
     v16f32 acc[T][T];
-    product_tile<F16, T, T, F16 ? 3 : 1>(A, B, tm * kEdge, tn * kEdge, __builtin_amdgcn_readfirstlane(k0), __builtin_amdgcn_readfirstlane(k1), smem, acc);
+    product_tile<F16, T, T, F16 ? 3 : 1, DEPTH>(A, B, tm * kEdge, tn * kEdge, __builtin_amdgcn_readfirstlane(k0), __builtin_amdgcn_readfirstlane(k1), smem, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r0 = (wave >> 1) * 32 * T + 4 * (lane >> 5), c0 = (wave & 1) * 32 * T + (lane & 31);
     if (isX || a.through) {
@@ -626,7 +627,7 @@ struct XentLayout {
     int edge_l, edge_g;           // tile edges of the logits and of the gradients
     int parts_v;                  // parts of the vocabulary whose sums are joined
     int64_t room, pieces;         // rows to a piece, pieces
-    int xslots, wcut;             // parts of tiles of gx that go at a time; into how many parts the tiles of gW are cut
+    int xslots, xgroups, wcut;    // parts of tiles of gx that go at a time, and as many as there can be of this problem; into how many parts the tiles of gW are cut
     bool through;                 // gW goes through sums in fp32
     size_t source, place, wanted, lse, row_loss, hit, g, stats, px, pw, tx, tw, P, GT, xparts, wparts, bytes;
     size_t px2, pw2, tx2, tw2, P2, GT2;
@@ -670,10 +671,12 @@ static XentLayout xent_layout(const void *w, int64_t ldw, int64_t rows, int64_t 
         l.GT2 = (size_t)(l.vp * l.pitch_GT);
         l.GT = take((int64_t)l.GT2 * numbers);
         const int64_t edge = l.edge_g, xtiles = up(l.room, edge) / edge * (up(d, edge) / edge), wtiles = up(vocab, edge) / edge * (up(d, edge) / edge);
-        l.xslots = (int)std::max<int64_t>(up(xtiles, 8), kXentSlots);
+        l.xslots = (int)std::max<int64_t>(xtiles, kXentSlots);
+        const int64_t able = std::max<int64_t>(1, up(vocab, kStageCols) / kStageCols / kPartTiles);  // (as parts_of; a multiple of the XCDs)
+        l.xgroups = (int)up(std::max(xtiles, std::min<int64_t>(l.xslots, xtiles * able)), 8);
         l.wcut = l.pieces == 1 && wtiles <= kXentSlots / 2 ? parts_of((int)wtiles, kXentSlots, (int)(up(rows, kStageCols) / kStageCols)) : 1;
         l.through = l.wcut > 1 || l.pieces > 1;
-        l.xparts = take(l.xslots * edge * edge * 4);
+        l.xparts = take((int64_t)l.xgroups * edge * edge * 4);
         l.wparts = take(l.through ? l.wcut * wtiles * edge * edge * 4 : 0);
     }
     l.bytes = at;
@@ -690,32 +693,46 @@ static int more_lds(K kernel, int bytes) {
     IMU_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
     return IMUNPACK_OK;
 }
-template <bool F16, int T>
+template <bool F16, int T, int DEPTH>
 static int xent_lds() {
-    IMU_TRY(more_lds(xent_logits_kernel<F16, T, false>, product_lds(T, T)));
-    IMU_TRY(more_lds(xent_logits_kernel<F16, T, true>, product_lds(T, T)));
-    return more_lds(xent_grads_kernel<F16, T>, product_lds(T, T));
+    IMU_TRY(more_lds(xent_logits_kernel<F16, T, DEPTH, false>, product_lds(T, T, DEPTH)));
+    IMU_TRY(more_lds(xent_logits_kernel<F16, T, DEPTH, true>, product_lds(T, T, DEPTH)));
+    return more_lds(xent_grads_kernel<F16, T, DEPTH>, product_lds(T, T, DEPTH));
 }
 static int xent_lds_opt_in() {
     static std::atomic<int> done{0};  // (the attribute is idempotent: two threads set the same)
     if (done.load(std::memory_order_acquire)) return IMUNPACK_OK;
-    IMU_TRY((xent_lds<false, 4>()));
-    IMU_TRY((xent_lds<false, 2>()));
-    IMU_TRY((xent_lds<true, 4>()));
-    IMU_TRY((xent_lds<true, 2>()));
+    IMU_TRY((xent_lds<false, 4, 2>()));
+    IMU_TRY((xent_lds<false, 2, 2>()));
+    IMU_TRY((xent_lds<false, 2, 4>()));
+    IMU_TRY((xent_lds<true, 4, 2>()));
+    IMU_TRY((xent_lds<true, 2, 2>()));
+    IMU_TRY((xent_lds<true, 2, 4>()));
     done.store(1, std::memory_order_release);
     return IMUNPACK_OK;
 }
 
-template <bool F16, int T>
-static void launch_logits(const LogitArgs &a, bool keep, int64_t rows, hipStream_t st) {
-    const dim3 grid((unsigned)(up(a.w.rows, 64 * T) / (64 * T) * (up(rows, 64 * T) / (64 * T))));
-    if (keep) hipLaunchKernelGGL((xent_logits_kernel<F16, T, true>), grid, dim3(kProductThreads), product_lds(T, T), st, a);
-    else hipLaunchKernelGGL((xent_logits_kernel<F16, T, false>), grid, dim3(kProductThreads), product_lds(T, T), st, a);
+template <bool F16, int T, int DEPTH>
+static void launch_logits(const LogitArgs &a, bool keep, unsigned groups, hipStream_t st) {
+    if (keep) hipLaunchKernelGGL((xent_logits_kernel<F16, T, DEPTH, true>), dim3(groups), dim3(kProductThreads), product_lds(T, T, DEPTH), st, a);
+    else hipLaunchKernelGGL((xent_logits_kernel<F16, T, DEPTH, false>), dim3(groups), dim3(kProductThreads), product_lds(T, T, DEPTH), st, a);
 }
-template <bool F16, int T>
+template <bool F16>
+static void launch_logits(const LogitArgs &a, int edge, bool keep, int64_t rows, hipStream_t st) {
+    const unsigned groups = (unsigned)(up(a.w.rows, edge) / edge * (up(rows, edge) / edge));
+    if (edge == 256) launch_logits<F16, 4, 2>(a, keep, groups, st);
+    else if (groups > kCus) launch_logits<F16, 2, 2>(a, keep, groups, st);
+    else launch_logits<F16, 2, 4>(a, keep, groups, st);
+}
+template <bool F16, int T, int DEPTH>
 static void launch_grads(const GradArgs &a, unsigned groups, hipStream_t st) {
-    hipLaunchKernelGGL((xent_grads_kernel<F16, T>), dim3(groups), dim3(kProductThreads), product_lds(T, T), st, a);
+    hipLaunchKernelGGL((xent_grads_kernel<F16, T, DEPTH>), dim3(groups), dim3(kProductThreads), product_lds(T, T, DEPTH), st, a);
+}
+template <bool F16>
+static void launch_grads(const GradArgs &a, int edge, unsigned groups, hipStream_t st) {
+    if (edge == 256) launch_grads<F16, 4, 2>(a, groups, st);
+    else if (groups > kCus) launch_grads<F16, 2, 2>(a, groups, st);
+    else launch_grads<F16, 2, 4>(a, groups, st);
 }
 }  // namespace imu
 
@@ -779,8 +796,7 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
             a.hdr = hdr; a.wanted = wanted; a.stats = (float *)(s + l.stats); a.hit = (float *)(s + l.hit);
             a.P = s + l.P; a.P2 = l.P2; a.pitch_P = l.pitch_P;
             a.first = (int)first; a.room = (int)l.room; a.ktiles = (int)(l.dp / kStageCols);
-            if (l.split) l.edge_l == 256 ? launch_logits<true, 4>(a, back, n, st) : launch_logits<true, 2>(a, back, n, st);
-            else l.edge_l == 256 ? launch_logits<false, 4>(a, back, n, st) : launch_logits<false, 2>(a, back, n, st);
+            l.split ? launch_logits<true>(a, l.edge_l, back, n, st) : launch_logits<false>(a, l.edge_l, back, n, st);
         }
         if (n > 0 || (loss && reduction != IMUNPACK_NONE)) {
             JoinArgs j = {};
@@ -806,17 +822,16 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
         a.xt = {s + l.tx + first * 2, l.pitch_tx, (int64_t)l.tx2, (int)d};
         a.hdr = hdr; a.up = upstream; a.xparts = (float *)(s + l.xparts); a.wparts = (float *)(s + l.wparts);
         a.gw = gw; a.ldgw = ldgw; a.ktiles = (int)(up(vocab, kStageCols) / kStageCols);
-        a.xslots = gx && n > 0 ? l.xslots : 0; a.wcut = l.wcut; a.through = l.through; a.first = (int)first; a.room = (int)l.room;
+        a.xslots = l.xslots; a.xgroups = gx && n > 0 ? l.xgroups : 0; a.wcut = l.wcut; a.through = l.through; a.first = (int)first; a.room = (int)l.room;
         const int64_t edge = l.edge_g, wgroups = gw ? up(vocab, edge) / edge * (up(d, edge) / edge) * l.wcut : 0;
-        const unsigned groups = (unsigned)(a.xslots + wgroups);
+        const unsigned groups = (unsigned)(a.xgroups + wgroups);
         if (groups > 0) {
-            if (l.split) edge == 256 ? launch_grads<true, 4>(a, groups, st) : launch_grads<true, 2>(a, groups, st);
-            else edge == 256 ? launch_grads<false, 4>(a, groups, st) : launch_grads<false, 2>(a, groups, st);
+            l.split ? launch_grads<true>(a, l.edge_g, groups, st) : launch_grads<false>(a, l.edge_g, groups, st);
         }
         FoldArgs f = {};
         f.xparts = a.xparts; f.wparts = a.wparts; f.hdr = hdr; f.up = upstream; f.place = place;
         f.gx = gx; f.gw = gw; f.ldgx = ldgx; f.ldgw = ldgw;
-        f.xrows = a.xslots ? rows : 0; f.wrows = gw && l.through && piece + 1 == l.pieces ? vocab : 0;
+        f.xrows = a.xgroups ? rows : 0; f.wrows = gw && l.through && piece + 1 == l.pieces ? vocab : 0;
         f.d = (int)d; f.edge = l.edge_g; f.ktiles = a.ktiles; f.xslots = l.xslots; f.wcut = l.wcut; f.first = a.first; f.room = a.room;
         if (f.xrows + f.wrows > 0) {
             const dim3 grid((unsigned)(f.xrows + f.wrows), (unsigned)(up(d, 1024) / 1024));
