@@ -10,7 +10,8 @@
 // element, so that a step can be repeated.  A root that is not zero keeps the smallest code at least: as zero it would leave eps alone
 // below m in the next step.
 //
-// Bound by memory: 28 bytes an element with 32-bit states and gradients, 16 with 8-bit states.  A wave takes 256 elements at a time,
+// Bound by memory: 28 bytes an element with 32-bit states and gradients, 16 with 8-bit states.  More than the last-level cache holds is read and
+// written past the caches (85 million elements: 464 -> 410 us with 32-bit states; 157 million 478 -> 461 with 8-bit ones).  A wave takes 256 elements at a time,
 // four to a lane, which is a block of the 8-bit states; tensors come as a table in the kernel's arguments, 4096 elements to a
 // workgroup.
 #include "common.h"
@@ -72,17 +73,21 @@ __device__ __forceinline__ uint32_t encode(const float (&f)[4]) {
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w, true);
 }
+template <bool ONCE>
 __device__ __forceinline__ uint32_t load_codes(const void *p, int64_t at) {
-    return __builtin_bit_cast(uint32_t, *reinterpret_cast<const piece_t<uint8_t, 4> *>((const uint8_t *)p + at));
+    return __builtin_bit_cast(uint32_t, load_piece<uint8_t, 4, ONCE>((const uint8_t *)p + at, 4));
 }
+template <bool ONCE>
 __device__ __forceinline__ void store_codes(void *p, int64_t at, uint32_t w) {
-    *reinterpret_cast<piece_t<uint8_t, 4> *>((uint8_t *)p + at) = __builtin_bit_cast(piece_t<uint8_t, 4>, w);
+    piece_t<uint8_t, 4> *to = reinterpret_cast<piece_t<uint8_t, 4> *>((uint8_t *)p + at);
+    if constexpr (ONCE) __builtin_nontemporal_store(__builtin_bit_cast(piece_t<uint8_t, 4>, w), to);
+    else *to = __builtin_bit_cast(piece_t<uint8_t, 4>, w);
 }
 
 // (No sum is contracted into a fused multiply-add: a state near the edge between two codes would go one way here and another
 // way where the same formula is written out elsewhere, and a step of a code is an eighth of its value.)
 #pragma clang fp contract(off)
-template <bool EIGHT, class G>
+template <bool EIGHT, class G, bool ONCE>
 __global__ __launch_bounds__(256) void adamw_kernel(const AdamArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     // which tensor the workgroup belongs to: lane k looks at tensor k
@@ -103,20 +108,20 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamArgs a) {
     for (int i = 0; i < kAdamBlocks; ++i) {
         const int64_t at = at0 + i * 4 * kAdamBlock, block = at / kAdamBlock;
         const int have = (int)min((int64_t)4, n - at);
-        load_upto<float, 4>(p + at, P[i], have);
-        g4[i] = load_piece<G, 4>(g + at, have);
+        to_floats<float, 4>(load_piece<float, 4, ONCE>(p + at, have), P[i]);
+        g4[i] = load_piece<G, 4, ONCE>(g + at, have);
         if constexpr (EIGHT) {
             mw[i] = vw[i] = 0;
             msc[i] = vsc[i] = 0.0f;
             if (block * kAdamBlock < n) {  // the states go over whole blocks
-                mw[i] = load_codes(a.m[k], at);
-                vw[i] = load_codes(a.v[k], at);
+                mw[i] = load_codes<ONCE>(a.m[k], at);
+                vw[i] = load_codes<ONCE>(a.v[k], at);
                 msc[i] = a.ms[k][block];
                 vsc[i] = a.vs[k][block];
             }
         } else {
-            load_upto<float, 4>((const float *)a.m[k] + at, M[i], have);
-            load_upto<float, 4>((const float *)a.v[k] + at, V[i], have);
+            to_floats<float, 4>(load_piece<float, 4, ONCE>((const float *)a.m[k] + at, have), M[i]);
+            to_floats<float, 4>(load_piece<float, 4, ONCE>((const float *)a.v[k] + at, have), V[i]);
         }
     }
 #pragma unroll
@@ -139,8 +144,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamArgs a) {
             root[j] = sqrtf(V[i][j]);
             P[i][j] = P[i][j] * a.decay - a.rate * (M[i][j] / (root[j] * a.root_scale + a.eps));
         }
-        store_upto<float, 4>(p + at, P[i], have);
-        if (copy) store_upto<__bf16, 4>(copy + at, P[i], have);
+        store_upto<float, 4, ONCE>(p + at, P[i], have);
+        if (copy) store_upto<__bf16, 4, ONCE>(copy + at, P[i], have);
         if constexpr (EIGHT) {
             const float mmax = block_max(M[i]), vmax = block_max(root);
             const float mi = mmax >= kNothing ? (1.0f / mmax) * kE4m3Max : mmax == mmax ? 0.0f : mmax;
@@ -152,17 +157,23 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamArgs a) {
                 mq[j] = round_e4m3(M[i][j] * mi, (float)(bits & 0xffffu) * 0x1p-16f, 0.0f);
                 vq[j] = round_e4m3(root[j] * vi, (float)(bits >> 16) * 0x1p-16f, 1.0f);
             }
-            store_codes(a.m[k], at, encode(mq));
-            store_codes(a.v[k], at, encode(vq));
+            store_codes<ONCE>(a.m[k], at, encode(mq));
+            store_codes<ONCE>(a.v[k], at, encode(vq));
             if (lane == 0) {
                 a.ms[k][block] = mmax >= kNothing || mmax != mmax ? mmax * (1.0f / kE4m3Max) : 0.0f;
                 a.vs[k][block] = vmax >= kNothing || vmax != vmax ? vmax * (1.0f / kE4m3Max) : 0.0f;
             }
         } else {
-            store_upto<float, 4>((float *)a.m[k] + at, M[i], have);
-            store_upto<float, 4>((float *)a.v[k] + at, V[i], have);
+            store_upto<float, 4, ONCE>((float *)a.m[k] + at, M[i], have);
+            store_upto<float, 4, ONCE>((float *)a.v[k] + at, V[i], have);
         }
     }
+}
+
+template <bool EIGHT, class G>
+static void launch_adamw(const AdamArgs &a, unsigned groups, bool once, hipStream_t st) {
+    if (once) hipLaunchKernelGGL((adamw_kernel<EIGHT, G, true>), dim3(groups), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((adamw_kernel<EIGHT, G, false>), dim3(groups), dim3(256), 0, st, a);
 }
 }  // namespace imu
 
@@ -177,11 +188,15 @@ extern "C" int imunpack_adamw(int64_t count, float *const *params, const void *c
         !std::isfinite(lr) || !std::isfinite(eps) || !std::isfinite(weight_decay))
         return IMUNPACK_EINVAL;
     if (count > 0 && (!params || !grads || !exp_avg || !exp_avg_sq || !numel || (state_bits == 8 && (!m_scales || !v_scales)))) return IMUNPACK_EINVAL;
+    int64_t total = 0;
     for (int64_t k = 0; k < count; ++k) {
         if (numel[k] < 0 || numel[k] > (int64_t)1 << 40) return IMUNPACK_EINVAL;
         if (numel[k] > 0 && (!params[k] || !grads[k] || !exp_avg[k] || !exp_avg_sq[k] || (state_bits == 8 && (!m_scales[k] || !v_scales[k])) || (copies && !copies[k])))
             return IMUNPACK_EINVAL;
+        total += numel[k];
     }
+    // bytes that are read, not counting the copies: what does not fit the caches is not brought into them
+    const bool once = total * (4 + (grad_dtype == IMUNPACK_F32 ? 4 : 2) + (state_bits == 8 ? 2 : 8)) > kLastLevelCache;
     hipStream_t st = (hipStream_t)stream;
     AdamArgs a;
     a.key = mix32(seed + (uint32_t)step * kGolden);
@@ -209,14 +224,9 @@ extern "C" int imunpack_adamw(int64_t count, float *const *params, const void *c
             ++a.count;
         }
         if (groups == 0) continue;
-        const dim3 grid((unsigned)groups), block(256);
-        if (state_bits == 8) {
-            if (grad_dtype == IMUNPACK_F32) hipLaunchKernelGGL((adamw_kernel<true, float>), grid, block, 0, st, a);
-            else hipLaunchKernelGGL((adamw_kernel<true, __bf16>), grid, block, 0, st, a);
-        } else {
-            if (grad_dtype == IMUNPACK_F32) hipLaunchKernelGGL((adamw_kernel<false, float>), grid, block, 0, st, a);
-            else hipLaunchKernelGGL((adamw_kernel<false, __bf16>), grid, block, 0, st, a);
-        }
+        const bool bf16 = grad_dtype == IMUNPACK_BF16;
+        if (state_bits == 8) bf16 ? launch_adamw<true, __bf16>(a, (unsigned)groups, once, st) : launch_adamw<true, float>(a, (unsigned)groups, once, st);
+        else bf16 ? launch_adamw<false, __bf16>(a, (unsigned)groups, once, st) : launch_adamw<false, float>(a, (unsigned)groups, once, st);
         IMU_TRY(launch_status());
     }
     return IMUNPACK_OK;

@@ -4,6 +4,8 @@
 #include "common.h"
 
 namespace imu {
+constexpr int64_t kLastLevelCache = 256ll << 20;  // bytes that the memory side's cache holds
+
 #if defined(__HIPCC__)
 template <class T>
 constexpr int kVec = 16 / (int)sizeof(T);  // elements of one load
@@ -21,9 +23,13 @@ using piece_t = typename Pieces<T, N>::type;
 
 // A piece of a row of which `have` elements are left; those behind them are zero.  Pieces are asked for one after the other and
 // turned into binary32 only then: each load stands in a branch of its own, and a conversion beside it would wait for it there.
-template <class T, int N>
+// ONCE: the caches are not asked to keep it.
+template <class T, int N, bool ONCE = false>
 __device__ __forceinline__ piece_t<T, N> load_piece(const T *p, int have) {
-    if (have >= N) return *reinterpret_cast<const piece_t<T, N> *>(p);
+    if (have >= N) {
+        if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const piece_t<T, N> *>(p));
+        else return *reinterpret_cast<const piece_t<T, N> *>(p);
+    }
     piece_t<T, N> x;
 #pragma unroll
     for (int k = 0; k < N; ++k) x[k] = k < have ? p[k] : (T)0;
@@ -35,19 +41,19 @@ __device__ __forceinline__ void to_floats(const piece_t<T, N> &x, float (&f)[N])
     for (int k = 0; k < N; ++k) f[k] = (float)x[k];
 }
 template <class T, int N>
-__device__ __forceinline__ void store_elements(T *p, const float (&f)[N]) {
-    piece_t<T, N> x;
-#pragma unroll
-    for (int k = 0; k < N; ++k) x[k] = (T)f[k];
-    *reinterpret_cast<piece_t<T, N> *>(p) = x;
-}
-template <class T, int N>
 __device__ __forceinline__ void load_upto(const T *p, float (&f)[N], int have) {
     to_floats<T, N>(load_piece<T, N>(p, have), f);
 }
-template <class T, int N>
+template <class T, int N, bool ONCE = false>
 __device__ __forceinline__ void store_upto(T *p, const float (&f)[N], int have) {
-    if (have >= N) return store_elements<T, N>(p, f);
+    if (have >= N) {
+        piece_t<T, N> x;
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = (T)f[k];
+        if constexpr (ONCE) __builtin_nontemporal_store(x, reinterpret_cast<piece_t<T, N> *>(p));
+        else *reinterpret_cast<piece_t<T, N> *>(p) = x;
+        return;
+    }
 #pragma unroll
     for (int k = 0; k < N; ++k)
         if (k < have) p[k] = (T)f[k];

@@ -10,12 +10,14 @@
 //
 // Bound by memory: every array is read once and written once.  A row stays in the registers of one wave (up to 256 pieces of 16
 // bytes), of a workgroup of 256 threads (up to 1024) or of 1024 threads (up to 4096) between the sums over it and its use;
-// longer rows are read again for each.  Sums, statistics and products are binary32; what is stored as bfloat16 is rounded once, from
+// longer rows are read again for each.  Results leave past the caches where a call moves as much as the last-level cache holds (8192 x 4096
+// bfloat16, forward and backward: 121 -> 111 us; 12608 x 768 fp32, whose backward pass finds them there: 64, 69 that way).  Sums, statistics and products are binary32; what is stored as bfloat16 is rounded once, from
 // the binary32 value (y from the unrounded h).
 #include "common.h"
 #include "elements.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace imu {
 constexpr int kNormThreads = 256;   // of a workgroup whose waves take a row each
@@ -38,7 +40,7 @@ __device__ __forceinline__ float quant_scale(float amax, bool finite, float qmax
     const float s = amax / qmax;
     return !finite ? __builtin_nanf("") : s > 0.0f ? s : 1.0f;
 }
-template <class T, int N>
+template <class T, int N, bool ONCE>
 __device__ __forceinline__ void store_quantised(const NormArgs &a, int64_t row, int col, const float (&y)[N], float scale, int have) {
     float q[N], v[N];
 #pragma unroll
@@ -47,11 +49,11 @@ __device__ __forceinline__ void store_quantised(const NormArgs &a, int64_t row, 
         v[k] = q[k] * scale;
         if (!(fabsf(q[k]) <= 127.0f)) q[k] = 0.0f;  // a row with NaN or infinity: its scale says so
     }
-    store_upto<int8_t, N>(a.q + row * a.ldq + col, q, have);
-    if (a.values) store_upto<T, N>((T *)a.values + row * a.ldv + col, v, have);
+    store_upto<int8_t, N, ONCE>(a.q + row * a.ldq + col, q, have);
+    if (a.values) store_upto<T, N, ONCE>((T *)a.values + row * a.ldv + col, v, have);
 }
 
-template <class T, int TPR, int NV, bool QUANT>
+template <class T, int TPR, int NV, bool QUANT, bool ONCE>
 __global__ __launch_bounds__(TPR == 64 ? kNormThreads : TPR) void norm_kernel(const NormArgs a) {
     constexpr int N = kVec<T>, kRows = TPR == 64 ? kNormThreads / 64 : 1;
     __shared__ float lds[2][TPR / 64];
@@ -87,7 +89,7 @@ __global__ __launch_bounds__(TPR == 64 ? kNormThreads : TPR) void norm_kernel(co
         if (a.rstd && t == 0) a.rstd[row] = r;
         if (a.h) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) store_upto<T, N>((T *)a.h + row * a.ldh + (i * TPR + t) * N, h[i], a.d - (i * TPR + t) * N);
+            for (int i = 0; i < NV; ++i) store_upto<T, N, ONCE>((T *)a.h + row * a.ldh + (i * TPR + t) * N, h[i], a.d - (i * TPR + t) * N);
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -95,7 +97,7 @@ __global__ __launch_bounds__(TPR == 64 ? kNormThreads : TPR) void norm_kernel(co
             for (int k = 0; k < N; ++k) h[i][k] = h[i][k] * r * w[i][k];
         if constexpr (!QUANT) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) store_upto<T, N>((T *)a.y + row * a.ldy + (i * TPR + t) * N, h[i], a.d - (i * TPR + t) * N);
+            for (int i = 0; i < NV; ++i) store_upto<T, N, ONCE>((T *)a.y + row * a.ldy + (i * TPR + t) * N, h[i], a.d - (i * TPR + t) * N);
         } else {
             float amax = 0.0f;  // infinity stands for NaN as well, which a maximum would lose
 #pragma unroll
@@ -106,7 +108,7 @@ __global__ __launch_bounds__(TPR == 64 ? kNormThreads : TPR) void norm_kernel(co
             const float scale = quant_scale(amax, amax < __builtin_inff(), a.qmax);
             if (t == 0) a.scale[row] = scale;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) store_quantised<T, N>(a, row, (i * TPR + t) * N, h[i], scale, a.d - (i * TPR + t) * N);
+            for (int i = 0; i < NV; ++i) store_quantised<T, N, ONCE>(a, row, (i * TPR + t) * N, h[i], scale, a.d - (i * TPR + t) * N);
         }
     }
 }
@@ -160,7 +162,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormArgs a) {
             if (a.h) store_upto<T, N>((T *)a.h + row * a.ldh + col, h, a.d - col);
 #pragma unroll
             for (int k = 0; k < N; ++k) h[k] = h[k] * r * w[k];
-            if constexpr (QUANT) store_quantised<T, N>(a, row, col, h, scale, a.d - col);
+            if constexpr (QUANT) store_quantised<T, N, false>(a, row, col, h, scale, a.d - col);
             else store_upto<T, N>((T *)a.y + row * a.ldy + col, h, a.d - col);
         }
         __syncthreads();
@@ -177,7 +179,7 @@ struct NormBackArgs {
     int d, w_bf16;
 };
 
-template <class T, int TPR, int NV>
+template <class T, int TPR, int NV, bool ONCE>
 __global__ __launch_bounds__(TPR == 64 ? kNormThreads : TPR) void norm_back_kernel(const NormBackArgs a) {
     constexpr int N = kVec<T>, kRows = TPR == 64 ? kNormThreads / 64 : 1;
     __shared__ float lds[2][TPR / 64];
@@ -230,7 +232,7 @@ __global__ __launch_bounds__(TPR == 64 ? kNormThreads : TPR) void norm_back_kern
                 const float v = r * (g[i][k] - h[i][k] * dot);
                 f[k] = a.gh ? (float)pgh[i][k] + v : v;
             }
-            store_upto<T, N>((T *)a.gx + row * a.ldgx + (i * TPR + t) * N, f, a.d - (i * TPR + t) * N);
+            store_upto<T, N, ONCE>((T *)a.gx + row * a.ldgx + (i * TPR + t) * N, f, a.d - (i * TPR + t) * N);
         }
     }
     if (!a.partial) return;
@@ -307,7 +309,13 @@ __global__ __launch_bounds__(1024) void norm_fold_kernel(const float *partial, i
     const int c = threadIdx.x & 31, p = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
     float s = 0.0f;
     if (col < d)
-        for (int k = p; k < parts; k += 32) s += partial[(int64_t)k * d + col];
+        for (int k0 = p; k0 < parts; k0 += 512) {  // sixteen loads at a time
+            float f[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) f[k] = k0 + 32 * k < parts ? partial[(int64_t)(k0 + 32 * k) * d + col] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) s += f[k];
+        }
     lds[p][c] = s;
     __syncthreads();
     if (p != 0 || col >= d) return;
@@ -325,15 +333,15 @@ static int back_groups(int64_t rows, int pieces) {
     return (int)std::min<int64_t>((rows + per - 1) / per, kNormPartials);
 }
 
-template <class T, bool QUANT>
+template <class T, bool QUANT, bool ONCE>
 static int launch_norm(const NormArgs &a, int pieces, hipStream_t st) {
     const int64_t groups = pieces <= 256 ? (a.rows + kNormThreads / 64 - 1) / (kNormThreads / 64) : a.rows;
     const dim3 grid((unsigned)std::min<int64_t>(groups, kNormGroups));
     auto go = [&](auto nv) {
         constexpr int NV = decltype(nv)::value;
-        if (pieces <= 256) hipLaunchKernelGGL((norm_kernel<T, 64, NV, QUANT>), grid, dim3(kNormThreads), 0, st, a);
-        else if (pieces <= 1024) hipLaunchKernelGGL((norm_kernel<T, 256, NV, QUANT>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((norm_kernel<T, 1024, NV, QUANT>), grid, dim3(1024), 0, st, a);
+        if (pieces <= 256) hipLaunchKernelGGL((norm_kernel<T, 64, NV, QUANT, ONCE>), grid, dim3(kNormThreads), 0, st, a);
+        else if (pieces <= 1024) hipLaunchKernelGGL((norm_kernel<T, 256, NV, QUANT, ONCE>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((norm_kernel<T, 1024, NV, QUANT, ONCE>), grid, dim3(1024), 0, st, a);
     };
     const int tpr = pieces <= 256 ? 64 : pieces <= 1024 ? 256 : 1024;
     switch ((pieces + tpr - 1) / tpr) {
@@ -346,14 +354,14 @@ static int launch_norm(const NormArgs &a, int pieces, hipStream_t st) {
     return launch_status();
 }
 
-template <class T>
+template <class T, bool ONCE>
 static int launch_norm_back(const NormBackArgs &a, int pieces, int groups, hipStream_t st) {
     const dim3 grid((unsigned)groups);
     auto go = [&](auto nv) {
         constexpr int NV = decltype(nv)::value;
-        if (pieces <= 256) hipLaunchKernelGGL((norm_back_kernel<T, 64, NV>), grid, dim3(kNormThreads), 0, st, a);
-        else if (pieces <= 1024) hipLaunchKernelGGL((norm_back_kernel<T, 256, NV>), grid, dim3(256), 0, st, a);
-        else if constexpr (NV * kVec<T> <= (kVec<T> == 4 ? 12 : 16)) hipLaunchKernelGGL((norm_back_kernel<T, 1024, NV>), grid, dim3(1024), 0, st, a);
+        if (pieces <= 256) hipLaunchKernelGGL((norm_back_kernel<T, 64, NV, ONCE>), grid, dim3(kNormThreads), 0, st, a);
+        else if (pieces <= 1024) hipLaunchKernelGGL((norm_back_kernel<T, 256, NV, ONCE>), grid, dim3(256), 0, st, a);
+        else if constexpr (NV * kVec<T> <= (kVec<T> == 4 ? 12 : 16)) hipLaunchKernelGGL((norm_back_kernel<T, 1024, NV, ONCE>), grid, dim3(1024), 0, st, a);
         else hipLaunchKernelGGL((norm_back_long_kernel<T>), grid, dim3(1024), 0, st, a);  // (more would not fit the 128 registers of a thread)
     };
     const int tpr = pieces <= 256 ? 64 : pieces <= 1024 ? 256 : 1024;
@@ -380,8 +388,16 @@ static int norm_forward(NormArgs &a, int64_t d, int dtype, int w_dtype, hipStrea
     a.d = (int)d;
     a.w_bf16 = w_dtype == IMUNPACK_BF16;
     const int pieces = norm_pieces(a.d, dtype);
-    if (dtype == IMUNPACK_F32) return a.qmax > 0.0f ? launch_norm<float, true>(a, pieces, st) : launch_norm<float, false>(a, pieces, st);
-    return a.qmax > 0.0f ? launch_norm<__bf16, true>(a, pieces, st) : launch_norm<__bf16, false>(a, pieces, st);
+    const int64_t size = dtype == IMUNPACK_F32 ? 4 : 2;
+    const int64_t moved = a.rows * d * (size * (1 + (a.res != nullptr) + (a.y != nullptr) + (a.h != nullptr) + (a.values != nullptr)) + (a.q != nullptr));
+    const bool once = moved >= kLastLevelCache;
+    auto go = [&](auto type, auto quant) {
+        using T = decltype(type);
+        constexpr bool QUANT = decltype(quant)::value;
+        return once ? launch_norm<T, QUANT, true>(a, pieces, st) : launch_norm<T, QUANT, false>(a, pieces, st);
+    };
+    if (dtype == IMUNPACK_F32) return a.qmax > 0.0f ? go(float(), std::true_type()) : go(float(), std::false_type());
+    return a.qmax > 0.0f ? go(__bf16(), std::true_type()) : go(__bf16(), std::false_type());
 }
 
 extern "C" int imunpack_rmsnorm(const void *x, int64_t ldx, const void *residual, int64_t ldres, const void *weight,
@@ -437,8 +453,9 @@ extern "C" int imunpack_rmsnorm_backward(const void *gy, int64_t ldgy, const voi
     a.ldgy = ldgy; a.ldx = ldx; a.ldres = ldres; a.ldgh = ldgh; a.ldgx = ldgx;
     a.rows = rows; a.d = (int)d; a.w_bf16 = weight_dtype == IMUNPACK_BF16;
     if (rows > 0) {
-        if (dtype == IMUNPACK_F32) IMU_TRY(launch_norm_back<float>(a, pieces, groups, st));
-        else IMU_TRY(launch_norm_back<__bf16>(a, pieces, groups, st));
+        const bool once = rows * d * (dtype == IMUNPACK_F32 ? 4 : 2) * (3 + (residual != nullptr) + (gh != nullptr)) >= kLastLevelCache;
+        if (dtype == IMUNPACK_F32) IMU_TRY((once ? launch_norm_back<float, true> : launch_norm_back<float, false>)(a, pieces, groups, st));
+        else IMU_TRY((once ? launch_norm_back<__bf16, true> : launch_norm_back<__bf16, false>)(a, pieces, groups, st));
     }
     if (gweight) {  // (no rows: zeros)
         hipLaunchKernelGGL(norm_fold_kernel, dim3((unsigned)((d + 31) / 32)), dim3(1024), 0, st, a.partial, groups, (int)d, gweight, a.w_bf16);
