@@ -1,16 +1,22 @@
-// Product of two 16-bit operands with the contraction contiguous in both, C = sum over segments of A_s B_s^T, accumulated in
-// binary32 on v_mfma_f32_32x32x16: the loop that the loss over a vocabulary is made of.  Tiles of (64 TM) x (64 TN), 2 x 2 waves of
-// (32 TM) x (32 TN) each.
+// Product of two 16-bit operands, C = sum over segments of A_s B_s^T, accumulated in binary32 on v_mfma_f32_32x32x16: the loop that the
+// loss over a vocabulary is made of.  Tiles of (64 TM) x (64 TN), 2 x 2 waves of (32 TM) x (32 TN) each.
 //
-// The walk over the contraction is that of the int8 GEMM, whose fragments have the same bytes: k-tiles of 128 bytes (64 elements) of a row,
-// loaded straight into LDS, a ring of 2 DEPTH + 1 half-stages (A and B of a k-tile in slots of their own), one barrier to a k-tile, loads
-// DEPTH k-tiles ahead: two, and four where a product has so few tiles that a CU has one small one to itself, whose time is that of its loads.  16-byte piece c of row r lies at slot c ^ ((r >> 1) & 7) of the row, so that the 32 rows of a fragment fall on
-// different banks.
+// Either operand may lie with the contraction contiguous (a row of memory is a row of the operand) or across (a row of memory is one
+// place of the contraction, the operand's rows side by side): in the second case the fragments come out of LDS through ds_read_b64_tr_b16, whose
+// sixteen lanes read four rows of sixteen elements and get a column of four each.  So no operand is ever transposed in memory.
+//
+// The walk over the contraction is that of the int8 GEMM, whose fragments have the same bytes: k-tiles of 64 places (128 bytes of a row, or 64
+// rows), loaded straight into LDS, a ring of 2 DEPTH + 1 half-stages (A and B of a k-tile in slots of their own), one barrier to a k-tile, loads
+// DEPTH k-tiles ahead: two, and four where a product has so few tiles that a CU has one small one to itself, whose time is that of its loads.
+// 16-byte piece c of row r lies at slot c ^ ((r >> 1) & 7) of the row (contraction contiguous: the 32 rows of a fragment fall on different banks)
+// or c ^ ((r & 3) << 2) (across: the four rows of a read do).
 //
 // Segments: an operand may come in two pieces, A = A_0 + A_1 and B = B_0 + B_1 (binary32 values as the sums of two binary16 ones); the contraction is then
 // walked three times, A_1 B_0, A_0 B_1 and A_0 B_0 (A_1 B_1 lies below the last bit).  The small products come first.
 #pragma once
 #include "common.h"
+
+#include <type_traits>
 
 namespace imu {
 #if defined(__HIPCC__)
@@ -18,18 +24,21 @@ typedef float v16f32 __attribute__((ext_vector_type(16)));
 typedef _Float16 v8f16 __attribute__((ext_vector_type(8)));
 typedef __bf16 v8bf16 __attribute__((ext_vector_type(8)));
 typedef int v4i32 __attribute__((ext_vector_type(4)));
+typedef int v2i32 __attribute__((ext_vector_type(2)));
+typedef short v4i16 __attribute__((ext_vector_type(4)));
 
 constexpr int kStageBytes = 128;   // of a row and k-tile
 constexpr int kStageCols = 64;     // 16-bit elements of it
 constexpr int kProductThreads = 256;
 constexpr int product_lds(int tm, int tn, int depth) { return (2 * depth + 1) * 64 * (tm > tn ? tm : tn) * kStageBytes; }
 
-// One operand: rows of 16-bit elements, `pitch` bytes apart (a multiple of 16, as is the base), in one piece or two (`second` bytes
-// behind the first).  Rows from `rows` on are not read (the last one is, in their place).
+// One operand: rows of memory of 16-bit elements, `pitch` bytes apart (a multiple of 16, as is the base), in one piece or two (`second` bytes
+// behind the first).  Rows from `rows` on are not read (the last one is, in their place); across, nor are pieces of 16 bytes that hold
+// nothing of the first `cols` elements of a row.
 struct Operand {
     const char *base;
     int64_t pitch, second;
-    int rows;
+    int rows, cols;
 };
 
 template <bool F16>
@@ -60,8 +69,8 @@ __device__ __forceinline__ void tile_at(int wg, int mtiles, int ntiles, int &tm,
 }
 
 // acc[i][j] of the wave: register r of lane l is the sum at row 32 i + (r / 4) * 8 + (l / 32) * 4 + r % 4 and column 32 j + l % 32 of the
-// wave's part of the tile.  k-tiles [k0, k1) of the contraction (which is k1 - k0 for each segment).
-template <bool F16, int TM, int TN, int SEGS, int DEPTH>
+// wave's part of the tile.  k-tiles [k0, k1) of the contraction (which is k1 - k0 for each segment).  XA, XB: the operand lies across.
+template <bool F16, int TM, int TN, int SEGS, int DEPTH, bool XA, bool XB>
 __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B, int m0, int n0, int k0, int k1, char *smem, v16f32 (&acc)[TM][TN]) {
     constexpr int kSlot = 64 * (TM > TN ? TM : TN) * kStageBytes;  // bytes of a slot of the ring
     constexpr int LA = 2 * TM, LB = 2 * TN;                        // loads of a wave for its share of a half-stage: 16 TM (16 TN) rows
@@ -76,21 +85,29 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B,
     const int K = k1 - k0, total = SEGS * K;
     if (K <= 0) return;
     const unsigned lds0 = (unsigned)(size_t)smem;
-    unsigned offA[LA], offB[LB];
+    // what lane l of the wave fetches with its load u: contiguous, eight rows of 128 bytes; across, 1 KiB / (128 T) rows
+    unsigned offA[LA], offB[LB], colA[2] = {0, 0}, colB[2] = {0, 0};
+    auto offsets = [&](auto &off, auto &col, auto across, auto t, const Operand &op, int first) __attribute__((always_inline)) {
+        constexpr int T = decltype(t)::value, L = 2 * T, kPieces = 8 * T, kRows = 64 / kPieces;  // pieces of a row of memory, rows to a load
 #pragma unroll
-    for (int u = 0; u < LA; ++u) {
-        const int row = 16 * TM * wave + 8 * u + (lane >> 3);
-        offA[u] = (unsigned)(min(row, A.rows - 1 - m0) * A.pitch) + (unsigned)(((lane & 7) ^ ((row >> 1) & 7)) * 16);
-    }
-#pragma unroll
-    for (int u = 0; u < LB; ++u) {
-        const int row = 16 * TN * wave + 8 * u + (lane >> 3);
-        offB[u] = (unsigned)(min(row, B.rows - 1 - n0) * B.pitch) + (unsigned)(((lane & 7) ^ ((row >> 1) & 7)) * 16);
-    }
-    const char *gA = A.base + m0 * A.pitch + (int64_t)k0 * kStageBytes, *gB = B.base + n0 * B.pitch + (int64_t)k0 * kStageBytes;
+        for (int u = 0; u < L; ++u) {
+            if constexpr (decltype(across)::value) {
+                const int row = 16 * wave + kRows * u + lane / kPieces;
+                off[u] = (unsigned)(row * op.pitch);
+                if (u < 2) col[u] = (unsigned)(min((lane % kPieces) ^ ((row & 3) << 2), (op.cols * 2 - 1) / 16 - first / 8) * 16);
+            } else {
+                const int row = 16 * T * wave + 8 * u + (lane >> 3);
+                off[u] = (unsigned)(min(row, op.rows - 1 - first) * op.pitch) + (unsigned)(((lane & 7) ^ ((row >> 1) & 7)) * 16);
+            }
+        }
+    };
+    offsets(offA, colA, std::bool_constant<XA>(), std::integral_constant<int, TM>(), A, m0);
+    offsets(offB, colB, std::bool_constant<XB>(), std::integral_constant<int, TN>(), B, n0);
+    const int64_t stepA = XA ? kStageCols * A.pitch : kStageBytes, stepB = XB ? kStageCols * B.pitch : kStageBytes;
+    const char *gA = A.base + (XA ? m0 * 2 : m0 * A.pitch) + k0 * stepA, *gB = B.base + (XB ? n0 * 2 : n0 * B.pitch) + k0 * stepB;
     auto ring = [](int slot, int k) { slot += k; return slot >= RING ? slot - RING : slot; };
     const char *pg = nullptr;
-    unsigned dl = 0;
+    unsigned dl = 0, last_row = 0;
     // k-tile kt (of all segments; past the last one it is loaded again, into a slot that is not read) of A or B into a slot
     auto setup = [&](bool isA, int kt, int slot) {
         int k = min(kt, total - 1);
@@ -100,10 +117,18 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B,
             k -= s * K;
             second = s == (isA ? 0 : 1) ? (isA ? A.second : B.second) : 0;
         }
-        pg = uniform_address((isA ? gA : gB) + second + (int64_t)k * kStageBytes);
+        pg = uniform_address((isA ? gA : gB) + second + k * (isA ? stepA : stepB));
+        if (isA ? XA : XB) {
+            const Operand &op = isA ? A : B;
+            last_row = __builtin_amdgcn_readfirstlane((unsigned)(min(op.rows - 1 - (k0 + k) * kStageCols, kStageCols) * op.pitch));
+        }
         dl = __builtin_amdgcn_readfirstlane(lds0 + (unsigned)(slot * kSlot) + (unsigned)(wave * (isA ? LA : LB) * 1024));
     };
-    auto fetch = [&](bool isA, int u) { fetch_to_lds(dl + u * 1024, isA ? offA[u] : offB[u], pg); };
+    auto fetch = [&](bool isA, int u) __attribute__((always_inline)) {
+        unsigned off = isA ? offA[u] : offB[u];
+        if (isA ? XA : XB) off = min(off, last_row) + (isA ? colA[u & 1] : colB[u & 1]);
+        fetch_to_lds(dl + u * 1024, off, pg);
+    };
 
     const int lrow = lane & 31, lhalf = lane >> 5, swz = (lrow >> 1) & 7;
     const unsigned baseA = (unsigned)((wm * 32 * TM + lrow) * kStageBytes), baseB = (unsigned)((wn * 32 * TN + lrow) * kStageBytes);
@@ -111,13 +136,32 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B,
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) piece[ks] = (unsigned)(((2 * ks + lhalf) ^ swz) << 4);
     v4i32 fa[2][TM], fb[2][TN];
+    // across: the lane's row of four and its 8 bytes within a block of 32 columns; blocks trade places by the row
+    const int xrow = (lane >> 2) & 3, xlane = ((lane >> 5) * 8 + xrow), xcol = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    unsigned acrossA[TM], acrossB[TN];
+    if constexpr (XA)
+#pragma unroll
+        for (int i = 0; i < TM; ++i) acrossA[i] = (unsigned)(xlane * 128 * TM + ((wm * TM + i) ^ xrow) * 64 + xcol);
+    if constexpr (XB)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acrossB[j] = (unsigned)(xlane * 128 * TN + ((wn * TN + j) ^ xrow) * 64 + xcol);
+    auto turned = [&](const char *p, int ks, int row) __attribute__((always_inline)) {  // places 16 ks + 0 .. 7 (8 .. 15) of the lane's row of the operand
+        const v2i32 lo = __builtin_bit_cast(v2i32, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16 *)(p + ks * 16 * row)));
+        const v2i32 hi = __builtin_bit_cast(v2i32, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16 *)(p + (ks * 16 + 4) * row)));
+        return v4i32{lo[0], lo[1], hi[0], hi[1]};
+    };
     // fragment q of a k-step, in the order in which the products need them
-    auto fragment = [&](const char *sa, const char *sb, int ks, int buf, int q) {
+    auto fragment = [&](const char *sa, const char *sb, int ks, int buf, int q) __attribute__((always_inline)) {
         constexpr int isA4[8] = {1, 0, 0, 1, 0, 0, 1, 1}, idx4[8] = {0, 0, 1, 1, 2, 3, 2, 3};
         const bool isA = (TM == 4 && TN == 4) ? isA4[q] : q == 0 || q > TN;
         const int idx = (TM == 4 && TN == 4) ? idx4[q] : q == 0 ? 0 : q > TN ? q - TN : q - 1;
-        if (isA) fa[buf][idx] = *reinterpret_cast<const v4i32 *>(sa + baseA + idx * 32 * kStageBytes + piece[ks]);
-        else fb[buf][idx] = *reinterpret_cast<const v4i32 *>(sb + baseB + idx * 32 * kStageBytes + piece[ks]);
+        if (isA) {
+            if constexpr (XA) fa[buf][idx] = turned(sa + acrossA[idx], ks, 128 * TM);
+            else fa[buf][idx] = *reinterpret_cast<const v4i32 *>(sa + baseA + idx * 32 * kStageBytes + piece[ks]);
+        } else {
+            if constexpr (XB) fb[buf][idx] = turned(sb + acrossB[idx], ks, 128 * TN);
+            else fb[buf][idx] = *reinterpret_cast<const v4i32 *>(sb + baseB + idx * 32 * kStageBytes + piece[ks]);
+        }
     };
     auto multiply = [&](int buf, int m) {
         constexpr int mi4[16] = {0, 0, 1, 1, 0, 0, 1, 1, 2, 2, 3, 3, 2, 2, 3, 3}, mj4[16] = {0, 1, 0, 1, 2, 3, 2, 3, 0, 1, 0, 1, 2, 3, 2, 3};

@@ -6,8 +6,8 @@
 // Rows without a target take no part: those with one are gathered first, and how many there are is known on the device alone.
 // A tile of the product l keeps, per row t, the largest logit and the sum of exponentials of its part of the vocabulary, and a small kernel
 // joins them to lse: for the loss alone nothing else of l is left.  For the gradients the rows go through in pieces (as many as kPieceBytes
-// allows): the tiles leave their exponentials in 16 bits, relative to the largest of the row and part; once lse stands they become G, both
-// ways round; gx and gW are products of it, and the next piece takes the same memory.  So l is made once: 6 T V d operations,
+// allows): the tiles leave their exponentials in 16 bits, relative to the largest of the row and part; once lse stands they become G where
+// they lie; gx and gW are products of it, and the next piece takes the same memory.  So l is made once: 6 T V d operations,
 // all on the matrix cores, and what is held does not grow with the rows.
 //
 // bfloat16 operands: products in bfloat16, G rounded to bfloat16.  fp32 operands: each value is the sum of two binary16 numbers
@@ -22,7 +22,7 @@
 #include <type_traits>
 
 namespace imu {
-constexpr int64_t kPieceBytes = 2ll << 30;  // G of a piece of the rows, both ways round, at most (or 256 rows)
+constexpr int64_t kPieceBytes = 2ll << 30;  // G of a piece of the rows at most (or 256 rows)
 constexpr int kTop = 14;                    // the largest magnitude of a scaled operand is below 2^(kTop + 1)
 constexpr unsigned kCus = 256;
 constexpr int kXentSlots = 256;             // parts of the tiles of a gradient that go at a time: one to a CU
@@ -128,81 +128,73 @@ __global__ __launch_bounds__(1024) void xent_scan_kernel(const ScanArgs a) {
     }
 }
 
+template <class E>
+__device__ __forceinline__ uint32_t pack(E a, E b) {
+    return (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
+}
+
 struct PrepareArgs {
     const void *x, *w;
     int64_t ldx, ldw;
     XentHeader *hdr;
     const int32_t *source;
-    char *px, *pw, *tx, *tw;               // rows and columns of x and W in 16 bits; nullptr: not wanted
-    int64_t px2, pw2, tx2, tw2;            // from the first piece of a value to the second, bytes
-    int64_t pitch_p, pitch_tx, pitch_tw;   // bytes from row to row
-    int64_t vocab;
-    int d, xtiles, nx, nw;                 // nx, nw: workgroups that looked for the largest magnitudes
+    char *px, *pw;            // x (gathered) and W in 16 bits, rows of `pieces` times 16 bytes
+    int64_t px2, pw2;         // from the first number of a value to the second, bytes
+    int64_t xrows, wrows;     // rows there is room for; rows of W that are wanted
+    int d, pieces, xgroups, nx, nw;  // workgroups that work on x; nx, nw: workgroups that looked for the largest magnitudes
 };
-// Sixteen values in a row: the lower halves of the words, or (second) the upper ones.
-__device__ __forceinline__ void put16(char *to, const uint32_t (&v)[16], bool second) {
-    v4i32 s[2];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s[k >> 2][k & 3] = (int)__builtin_amdgcn_perm(v[2 * k + 1], v[2 * k], second ? 0x07060302u : 0x05040100u);
-    *reinterpret_cast<v4i32 *>(to) = s[0];
-    *reinterpret_cast<v4i32 *>(to + 16) = s[1];
-}
-// 64 rows by 64 columns of x (gathered) or W: in 16 bits, one or two numbers to a value, row by row and transposed; zeros around.
+constexpr int kPrepareTurns = 4;
+// Eight columns of a row at a time: binary32 as two binary16 numbers, bfloat16 as it is; zeros behind the last column and, to a whole
+// k-tile, behind the last row of x.
 template <class T>
 __global__ __launch_bounds__(256) void xent_prepare_kernel(const PrepareArgs a) {
     constexpr bool SPLIT = sizeof(T) == 4;
-    __shared__ uint32_t tile[64][65];
     __shared__ float lds[4];
-    const bool isX = (int)blockIdx.x < a.xtiles;
+    const bool isX = (int)blockIdx.x < a.xgroups;
+    const int group = isX ? blockIdx.x : blockIdx.x - a.xgroups;
+    const int64_t count = isX ? a.hdr->count : a.wrows, rows = isX ? min((count + kStageCols - 1) / kStageCols * kStageCols, a.xrows) : count;
     float scale = 1.0f;
     if constexpr (SPLIT) {  // the first workgroup of either operand leaves the largest magnitude for the kernels behind
         float m = 0.0f;
         for (int k = threadIdx.x; k < (isX ? a.nx : a.nw); k += 256) m = fmaxf(m, __uint_as_float(a.hdr->found[isX ? k : a.nx + k]));
         m = reduce_threads<256, true>(m, lds);
         scale = power_of_two(scale_exponent(__float_as_uint(m)));
-        if (threadIdx.x == 0 && blockIdx.y == 0 && (int)blockIdx.x == (isX ? 0 : a.xtiles)) a.hdr->amax[isX ? 0 : 1] = __float_as_uint(m);
+        if (threadIdx.x == 0 && group == 0) a.hdr->amax[isX ? 0 : 1] = __float_as_uint(m);
     }
-    const int64_t rows = isX ? a.hdr->count : a.vocab, row0 = (int64_t)(isX ? blockIdx.x : blockIdx.x - a.xtiles) * 64;
-    if (row0 >= rows) return;
-    const int col0 = blockIdx.y * 64, r = threadIdx.x >> 2, c = (threadIdx.x & 3) * 16;
-    const int64_t row = row0 + r;
-    const T *p = isX ? (const T *)a.x + (row < rows ? (int64_t)a.source[row] : 0) * a.ldx : (const T *)a.w + row * a.ldw;
-    const int have = row < rows ? a.d - (col0 + c) : 0;
-    uint32_t q[16];
-    if constexpr (SPLIT) {
-        piece_t<float, 4> f[4];
+    const int64_t at0 = (int64_t)group * 256 * kPrepareTurns + threadIdx.x;
+    int64_t row[kPrepareTurns];
+    int col[kPrepareTurns];
+    piece_t<T, 4> f[kPrepareTurns][2];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) f[k] = load_piece<float, 4>(p + col0 + c + 4 * k, have - 4 * k);
+    for (int i = 0; i < kPrepareTurns; ++i) {
+        const int64_t at = at0 + 256 * i;
+        row[i] = at / a.pieces;
+        col[i] = (int)(at - row[i] * a.pieces) * 8;
+        const T *p = isX ? (const T *)a.x + (row[i] < count ? (int64_t)a.source[row[i]] : 0) * a.ldx : (const T *)a.w + row[i] * a.ldw;
+        const int have = row[i] < count ? a.d - col[i] : 0;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const float v = f[k >> 2][k & 3] * scale;
-            const _Float16 h = (_Float16)v, l = (_Float16)(v - (float)h);
-            q[k] = (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
+        for (int k = 0; k < 2; ++k) f[i][k] = load_piece<T, 4>(p + col[i] + 4 * k, have - 4 * k);
+    }
+#pragma unroll
+    for (int i = 0; i < kPrepareTurns; ++i) {
+        if (row[i] >= rows) continue;
+        char *to = (isX ? a.px : a.pw) + (row[i] * a.pieces * 8 + col[i]) * 2;
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const T u = f[i][k >> 1][2 * (k & 1)], v = f[i][k >> 1][2 * (k & 1) + 1];
+            if constexpr (SPLIT) {
+                const float a0 = u * scale, a1 = v * scale;
+                const _Float16 h0 = (_Float16)a0, h1 = (_Float16)a1;
+                hi[k] = pack(h0, h1);
+                lo[k] = pack((_Float16)(a0 - (float)h0), (_Float16)(a1 - (float)h1));
+            } else {
+                hi[k] = pack(u, v);
+            }
         }
-    } else {
-        piece_t<__bf16, 8> f[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) f[k] = load_piece<__bf16, 8>(p + col0 + c + 8 * k, have - 8 * k);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) q[k] = __builtin_bit_cast(uint16_t, (__bf16)f[k >> 3][k & 7]);
+        *reinterpret_cast<v4i32 *>(to) = v4i32{(int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+        if constexpr (SPLIT) *reinterpret_cast<v4i32 *>(to + (isX ? a.px2 : a.pw2)) = v4i32{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3]};
     }
-    char *out = isX ? a.px : a.pw;
-    if (out && (isX || row < rows)) {  // (rows of zeros behind the last of x; there is no room behind W's)
-        char *to = out + row * a.pitch_p + (col0 + c) * 2;
-        put16(to, q, false);
-        if (SPLIT) put16(to + (isX ? a.px2 : a.pw2), q, true);
-    }
-    out = isX ? a.tx : a.tw;
-    if (!out) return;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) tile[r][c + k] = q[k];
-    __syncthreads();
-    if (col0 + r >= a.d) return;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) q[k] = tile[c + k][r];
-    char *to = out + (int64_t)(col0 + r) * (isX ? a.pitch_tx : a.pitch_tw) + (row0 + c) * 2;
-    put16(to, q, false);
-    if (SPLIT) put16(to + (isX ? a.tx2 : a.tw2), q, true);
 }
 
 // The gradient of each row's loss, as a factor between -2 and 2 and a power of two that the results are multiplied with at the end.
@@ -231,10 +223,6 @@ struct LogitArgs {
 constexpr float kLog2e = 1.44269504088896340736f;
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
-template <class E>
-__device__ __forceinline__ uint32_t pack(E a, E b) {
-    return (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
-}
 // Four lanes hold a row of four 16-bit elements each (lo: 0 and 1, hi: 2 and 3); afterwards lane k of them holds element k of all four.
 __device__ __forceinline__ void quad_transpose(uint32_t &lo, uint32_t &hi, int lane) {
     const uint32_t pick = lane & 1 ? 0x03020706u : 0x05040100u;  // odd: the neighbour's upper half below one's own; even: one's own lower half below the neighbour's
@@ -261,7 +249,7 @@ __global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void 
     Operand x = a.x;
     x.rows = count;
     v16f32 acc[T][T];
-    product_tile<F16, T, T, F16 ? 3 : 1, DEPTH>(a.w, x, tm * kEdge, tn * kEdge, 0, a.ktiles, smem, acc);
+    product_tile<F16, T, T, F16 ? 3 : 1, DEPTH, false, false>(a.w, x, tm * kEdge, tn * kEdge, 0, a.ktiles, smem, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, lhalf = lane >> 5;
     const int vwave = tm * kEdge + (wave >> 1) * 32 * T, twave = tn * kEdge + (wave & 1) * 32 * T;  // the wave's first column and row of the piece
     const int down = F16 ? -(scale_exponent(a.hdr->amax[0]) + scale_exponent(a.hdr->amax[1])) : 0;
@@ -411,63 +399,61 @@ struct TurnArgs {
     const int32_t *wanted;
     const float *stats, *lse;
     Upstream up;
-    char *P, *GT;             // P becomes G; G^T: [vocabulary][row of the piece]
-    int64_t P2, GT2, pitch_P, pitch_GT;
+    char *P;
+    int64_t P2, pitch_P;
     int first, room, vocab, part;  // part: columns that share a largest logit
 };
-// 64 rows by 64 columns of exponentials become G where they lie, and G^T.
+constexpr int kTurnRows = 32;
+// Exponentials become G where they lie, 256 columns of 32 rows to a workgroup, eight columns to a lane: zeros behind the vocabulary and, to a
+// whole k-tile, behind the last row.
 template <bool F16>
 __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
-    __shared__ uint32_t tile[64][65];
-    const int rows = rows_of(a.hdr, a.first, a.room), row0 = blockIdx.y * 64, col0 = blockIdx.x * 64;
-    if (row0 >= rows) return;
-    const int r = threadIdx.x >> 2, c = (threadIdx.x & 3) * 16, t = row0 + r, left = a.vocab - (col0 + c);
-    uint32_t q[16];
+    const int rows = rows_of(a.hdr, a.first, a.room), last = (rows + kStageCols - 1) / kStageCols * kStageCols;
+    const int row0 = blockIdx.y * kTurnRows + (threadIdx.x >> 5), v0 = blockIdx.x * 256 + (threadIdx.x & 31) * 8, left = a.vocab - v0;
+    if ((int)blockIdx.y * kTurnRows >= last || v0 >= (a.vocab + kStageCols - 1) / kStageCols * kStageCols) return;
+    const float all = a.up.g ? 0.0f : a.up.one(a.hdr);
+    constexpr int kTurns = kTurnRows / 8;
+    v4i32 hi[kTurns], lo[kTurns];
+    char *const p0 = a.P + v0 * 2;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) q[k] = 0;
-    if (t < rows) {
-        char *p = a.P + t * a.pitch_P + (col0 + c) * 2;
-        v4i32 hi[2], lo[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            hi[k] = *reinterpret_cast<const v4i32 *>(p + 16 * k);
-            if (F16) lo[k] = *reinterpret_cast<const v4i32 *>(p + a.P2 + 16 * k);
-        }
-        const float top = a.stats[((int64_t)(col0 / a.part) * a.room + t) * 2];
-        const float g = a.up.g ? a.up.g[a.first + t] : a.up.one(a.hdr);
-        const float down = __builtin_amdgcn_exp2f((top - a.lse[a.first + t]) * kLog2e) * g, one = F16 ? g * power_of_two(kTop) : g;
-        const int own = a.wanted[a.first + t] - (col0 + c);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const uint16_t h = (uint16_t)((uint32_t)hi[k >> 3][(k >> 1) & 3] >> (16 * (k & 1)));
-            float v;
-            if constexpr (F16) {
-                const uint16_t l = (uint16_t)((uint32_t)lo[k >> 3][(k >> 1) & 3] >> (16 * (k & 1)));
-                v = (float)__builtin_bit_cast(_Float16, h) + (float)__builtin_bit_cast(_Float16, l);
-            } else {
-                v = (float)__builtin_bit_cast(__bf16, h);
-            }
-            v = v * down - (k == own ? one : 0.0f);
-            if (k >= left) v = 0.0f;
-            if constexpr (F16) {
-                const _Float16 x = (_Float16)v;
-                q[k] = pack(x, (_Float16)(v - (float)x));
-            } else {
-                q[k] = __builtin_bit_cast(uint16_t, (__bf16)v);
-            }
-        }
-        put16(p, q, false);
-        if (F16) put16(p + a.P2, q, true);
+    for (int i = 0; i < kTurns; ++i) {
+        const int t = row0 + 8 * i;
+        if (t >= rows) continue;
+        hi[i] = *reinterpret_cast<const v4i32 *>(p0 + t * a.pitch_P);
+        if (F16) lo[i] = *reinterpret_cast<const v4i32 *>(p0 + t * a.pitch_P + a.P2);
     }
 #pragma unroll
-    for (int k = 0; k < 16; ++k) tile[r][c + k] = q[k];
-    __syncthreads();
-    if (col0 + r >= a.vocab) return;
+    for (int i = 0; i < kTurns; ++i) {
+        const int t = row0 + 8 * i;
+        if (t >= last) continue;
+        uint32_t qh[4] = {0, 0, 0, 0}, ql[4] = {0, 0, 0, 0};
+        if (t < rows) {
+            const float top = a.stats[((int64_t)(v0 / a.part) * a.room + t) * 2];
+            const float g = a.up.g ? a.up.g[a.first + t] : all;
+            const float down = __builtin_amdgcn_exp2f((top - a.lse[a.first + t]) * kLog2e) * g, one = F16 ? g * power_of_two(kTop) : g;
+            const int own = a.wanted[a.first + t] - v0;
+            float v[8];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) q[k] = tile[c + k][r];
-    char *to = a.GT + (int64_t)(col0 + r) * a.pitch_GT + (row0 + c) * 2;
-    put16(to, q, false);
-    if (F16) put16(to + a.GT2, q, true);
+            for (int k = 0; k < 8; ++k) {
+                const uint16_t h = (uint16_t)((uint32_t)hi[i][k >> 1] >> (16 * (k & 1)));
+                if constexpr (F16) v[k] = (float)__builtin_bit_cast(_Float16, h) + (float)__builtin_bit_cast(_Float16, (uint16_t)((uint32_t)lo[i][k >> 1] >> (16 * (k & 1))));
+                else v[k] = (float)__builtin_bit_cast(__bf16, h);
+                v[k] = k < left ? v[k] * down - (k == own ? one : 0.0f) : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (F16) {
+                    const _Float16 h0 = (_Float16)v[2 * k], h1 = (_Float16)v[2 * k + 1];
+                    qh[k] = pack(h0, h1);
+                    ql[k] = pack((_Float16)(v[2 * k] - (float)h0), (_Float16)(v[2 * k + 1] - (float)h1));
+                } else {
+                    qh[k] = pack((__bf16)v[2 * k], (__bf16)v[2 * k + 1]);
+                }
+            }
+        }
+        *reinterpret_cast<v4i32 *>(p0 + t * a.pitch_P) = v4i32{(int)qh[0], (int)qh[1], (int)qh[2], (int)qh[3]};
+        if (F16) *reinterpret_cast<v4i32 *>(p0 + t * a.pitch_P + a.P2) = v4i32{(int)ql[0], (int)ql[1], (int)ql[2], (int)ql[3]};
+    }
 }
 
 // Into how many parts the tiles of a gradient are cut along the contraction, so that every CU has one.
@@ -478,8 +464,7 @@ __host__ __device__ __forceinline__ int parts_of(int tiles, int slots, int ktile
 }
 
 struct GradArgs {
-    Operand G, wt;     // gx: [row of the piece][vocabulary], [feature][vocabulary]
-    Operand GT, xt;    // gW: [vocabulary][row of the piece], [feature][row of the piece]
+    Operand G, w, x;   // [row of the piece][vocabulary], [vocabulary][feature], [row of the piece][feature]
     const XentHeader *hdr;
     Upstream up;
     float *xparts, *wparts;  // [slot][tile]; wparts: where the tiles of gW are cut, or are sums over several pieces
@@ -488,19 +473,15 @@ struct GradArgs {
     int ktiles, xslots, xgroups, wcut, first, room;  // k-tiles of gx's contraction; parts of its tiles at a time, workgroups there are for them
     bool through;            // gW goes through wparts
 };
-// Both gradients from a piece of the rows: the first xgroups workgroups take parts of the tiles of gx, those behind them tiles of gW (parts of
-// them, where there are few), so that neither waits for the other's last ones.
-template <bool F16, int T, int DEPTH>
-__global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void xent_grads_kernel(const GradArgs a) {
-    extern __shared__ __attribute__((aligned(1024))) char smem[];
+// A tile (or part of one) of gx = G W, with W across, or of gW = G^T x, both across and with rows of zeros to whole k-tiles.
+template <bool F16, int T, int DEPTH, bool X>
+__device__ __forceinline__ void grad_tile(const GradArgs &a, int wg, char *smem) {
     constexpr int kEdge = 64 * T;
-    const bool isX = (int)blockIdx.x < a.xgroups;
-    const int count = rows_of(a.hdr, a.first, a.room), wg = isX ? blockIdx.x : blockIdx.x - a.xgroups;
-    Operand A = isX ? a.G : a.GT, B = isX ? a.wt : a.xt;
-    if (isX) A.rows = count;
-    else if (count == 0 && a.first > 0) return;  // (the first piece writes zeros)
-    const int mtiles = (A.rows + kEdge - 1) / kEdge, ntiles = (B.rows + kEdge - 1) / kEdge, tiles = mtiles * ntiles;
-    const int ktiles = isX ? a.ktiles : (count + kStageCols - 1) / kStageCols, parts = isX ? parts_of(tiles, a.xslots, a.ktiles) : a.wcut;
+    const int count = rows_of(a.hdr, a.first, a.room);
+    if (!X && count == 0 && a.first > 0) return;  // (the first piece writes zeros)
+    const int height = X ? count : a.w.rows, width = a.w.cols;  // of the gradient
+    const int mtiles = (height + kEdge - 1) / kEdge, ntiles = (width + kEdge - 1) / kEdge, tiles = mtiles * ntiles;
+    const int rtiles = (count + kStageCols - 1) / kStageCols, ktiles = X ? a.ktiles : rtiles, parts = X ? parts_of(tiles, a.xslots, a.ktiles) : a.wcut;
     if (wg >= tiles * parts) return;
     int tm, tn, part = 0, slot = 0;
     if (parts == 1) {
@@ -516,21 +497,24 @@ __global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void 
     }
     tm = __builtin_amdgcn_readfirstlane(tm);
     tn = __builtin_amdgcn_readfirstlane(tn);
-    const int k0 = (int)((int64_t)ktiles * part / parts), k1 = (int)((int64_t)ktiles * (part + 1) / parts);
+    const int k0 = __builtin_amdgcn_readfirstlane((int)((int64_t)ktiles * part / parts)), k1 = __builtin_amdgcn_readfirstlane((int)((int64_t)ktiles * (part + 1) / parts));
+    Operand G = a.G, x = a.x;
+    G.rows = X ? count : rtiles * kStageCols;
+    x.rows = rtiles * kStageCols;
     v16f32 acc[T][T];
-    product_tile<F16, T, T, F16 ? 3 : 1, DEPTH>(A, B, tm * kEdge, tn * kEdge, __builtin_amdgcn_readfirstlane(k0), __builtin_amdgcn_readfirstlane(k1), smem, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int r0 = (wave >> 1) * 32 * T + 4 * (lane >> 5), c0 = (wave & 1) * 32 * T + (lane & 31);
-    if (isX || a.through) {
-        float *to = (isX ? a.xparts : a.wparts) + (int64_t)slot * kEdge * kEdge + r0 * kEdge + c0;
-        const bool add = !isX && a.first > 0;
+    product_tile<F16, T, T, F16 ? 3 : 1, DEPTH, !X, true>(G, X ? a.w : x, tm * kEdge, tn * kEdge, k0, k1, smem, acc);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r0 = (wave >> 1) * 32 * T, rl = 4 * (lane >> 5), c0 = (wave & 1) * 32 * T + (lane & 31);
+    if (X || a.through) {
+        float *to = (X ? a.xparts : a.wparts) + (int64_t)slot * kEdge * kEdge + r0 * kEdge;
+        const bool add = !X && a.first > 0;
 #pragma unroll
         for (int i = 0; i < T; ++i)
 #pragma unroll
-            for (int j = 0; j < T; ++j)
+            for (int r = 0; r < 16; ++r)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float *p = to + (32 * i + (r >> 2) * 8 + (r & 3)) * kEdge + 32 * j;
+                for (int j = 0; j < T; ++j) {
+                    float *p = to + (32 * i + (r >> 2) * 8 + (r & 3)) * kEdge + (rl * kEdge + c0 + 32 * j);
                     *p = add ? *p + acc[i][j][r] : acc[i][j][r];
                 }
         return;
@@ -540,31 +524,40 @@ __global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void 
 #pragma unroll
     for (int i = 0; i < T; ++i)
 #pragma unroll
-        for (int j = 0; j < T; ++j) {
+        for (int q = 0; q < 4; ++q) {
             if constexpr (F16) {
+                float *to = (float *)a.gw + (int64_t)(v0 + 32 * i + 8 * q) * a.ldgw;  // (the lane's row is rl further)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int64_t v = v0 + 32 * i + (r >> 2) * 8 + (r & 3);
-                    if (v < A.rows && f0 + 32 * j < B.rows) ((float *)a.gw)[v * a.ldgw + f0 + 32 * j] = ldexpf(acc[i][j][r], e);
-                }
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int j = 0; j < T; ++j)
+                        if (v0 + 32 * i + 8 * q + rl + k < height && f0 + 32 * j < width) to[(rl + k) * a.ldgw + f0 + 32 * j] = ldexpf(acc[i][j][4 * q + k], e);
             } else {  // four rows by four columns trade places among four lanes: 8 bytes to a store
+                const int v = v0 + 32 * i + 8 * q + rl + (lane & 3);
+                uint16_t *to = (uint16_t *)a.gw + (int64_t)v * a.ldgw;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int j = 0; j < T; ++j) {
                     uint32_t lo = pack((__bf16)ldexpf(acc[i][j][4 * q], e), (__bf16)ldexpf(acc[i][j][4 * q + 1], e));
                     uint32_t hi = pack((__bf16)ldexpf(acc[i][j][4 * q + 2], e), (__bf16)ldexpf(acc[i][j][4 * q + 3], e));
                     quad_transpose(lo, hi, lane);
-                    const int64_t v = v0 + 32 * i + 8 * q + (lane & 3);
                     const int f = (f0 & ~3) + 32 * j;
-                    if (v >= A.rows) continue;
-                    uint16_t *to = (uint16_t *)a.gw + v * a.ldgw + f;
-                    const piece_t<uint16_t, 4> x = __builtin_bit_cast(piece_t<uint16_t, 4>, make_uint2(lo, hi));
-                    if (f + 4 <= B.rows) *reinterpret_cast<piece_t<uint16_t, 4> *>(to) = x;
+                    if (v >= height) continue;
+                    const piece_t<uint16_t, 4> x4 = __builtin_bit_cast(piece_t<uint16_t, 4>, make_uint2(lo, hi));
+                    if (f + 4 <= width) *reinterpret_cast<piece_t<uint16_t, 4> *>(to + f) = x4;
                     else
                         for (int k = 0; k < 4; ++k)
-                            if (f + k < B.rows) to[k] = x[k];
+                            if (f + k < width) to[f + k] = x4[k];
                 }
             }
         }
+}
+// Both gradients from a piece of the rows: the first xgroups workgroups take parts of the tiles of gx, those behind them tiles of gW (parts of
+// them, where there are few), so that neither waits for the other's last ones.
+template <bool F16, int T, int DEPTH>
+__global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void xent_grads_kernel(const GradArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    if ((int)blockIdx.x < a.xgroups) grad_tile<F16, T, DEPTH, true>(a, blockIdx.x, smem);
+    else grad_tile<F16, T, DEPTH, false>(a, blockIdx.x - a.xgroups, smem);
 }
 
 struct FoldArgs {
@@ -623,14 +616,14 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct XentLayout {
     int64_t dp, tp, vp;           // features, rows, vocabulary rounded up to what the products read
     bool split, direct;           // two numbers to a value; W read in place
-    int64_t pitch_p, pitch_tx, pitch_tw, pitch_P, pitch_GT;
+    int64_t pitch_p, pitch_P;     // bytes from row to row of x and W in 16 bits, and of G
     int edge_l, edge_g;           // tile edges of the logits and of the gradients
     int parts_v;                  // parts of the vocabulary whose sums are joined
     int64_t room, pieces;         // rows to a piece, pieces
     int xslots, xgroups, wcut;    // parts of tiles of gx that go at a time, and as many as there can be of this problem; into how many parts the tiles of gW are cut
     bool through;                 // gW goes through sums in fp32
-    size_t source, place, wanted, lse, row_loss, hit, g, stats, px, pw, tx, tw, P, GT, xparts, wparts, bytes;
-    size_t px2, pw2, tx2, tw2, P2, GT2;
+    size_t source, place, wanted, lse, row_loss, hit, g, stats, px, pw, P, xparts, wparts, bytes;
+    size_t px2, pw2, P2;
 };
 // Large tiles where they fill half of the CUs at least.
 static int tile_edge(int64_t m, int64_t n) { return up(m, 256) / 256 * (up(n, 256) / 256) >= 128 ? 256 : 128; }
@@ -645,7 +638,7 @@ static XentLayout xent_layout(const void *w, int64_t ldw, int64_t rows, int64_t 
     l.edge_l = tile_edge(vocab, rows);
     l.edge_g = rows * d * vocab >= 1ll << 33 ? 256 : 128;
     l.parts_v = (int)(2 * (up(vocab, l.edge_l) / l.edge_l));
-    l.room = !grad ? l.tp : std::min(l.tp, std::max<int64_t>(256, kPieceBytes / (4 * numbers * l.vp) / 256 * 256));
+    l.room = !grad ? l.tp : std::min(l.tp, std::max<int64_t>(256, kPieceBytes / (2 * numbers * l.vp) / 256 * 256));
     l.pieces = (l.tp + l.room - 1) / l.room;
     size_t at = sizeof(XentHeader);
     auto take = [&](int64_t bytes) { const size_t here = at; at = (at + (size_t)bytes + 255) & ~(size_t)255; return here; };
@@ -658,18 +651,9 @@ static XentLayout xent_layout(const void *w, int64_t ldw, int64_t rows, int64_t 
     l.pw2 = (size_t)up(vocab * l.pitch_p, 256);
     l.pw = take(l.direct ? 0 : (int64_t)l.pw2 * numbers);
     if (grad) {
-        l.pitch_tx = l.tp * 2;
-        l.pitch_tw = l.vp * 2;
-        l.tx2 = (size_t)(d * l.pitch_tx);
-        l.tx = take((int64_t)l.tx2 * numbers);
-        l.tw2 = (size_t)(d * l.pitch_tw);
-        l.tw = take((int64_t)l.tw2 * numbers);
         l.pitch_P = l.vp * 2;
-        l.pitch_GT = l.room * 2;
         l.P2 = (size_t)(l.room * l.pitch_P);
         l.P = take((int64_t)l.P2 * numbers);
-        l.GT2 = (size_t)(l.vp * l.pitch_GT);
-        l.GT = take((int64_t)l.GT2 * numbers);
         const int64_t edge = l.edge_g, xtiles = up(l.room, edge) / edge * (up(d, edge) / edge), wtiles = up(vocab, edge) / edge * (up(d, edge) / edge);
         l.xslots = (int)std::max<int64_t>(xtiles, kXentSlots);
         const int64_t able = std::max<int64_t>(1, up(vocab, kStageCols) / kStageCols / kPartTiles);  // (as parts_of; a multiple of the XCDs)
@@ -776,23 +760,21 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
         PrepareArgs p = {};
         p.x = x; p.w = w; p.ldx = ldx; p.ldw = ldw; p.hdr = hdr; p.source = source;
         p.px = s + l.px; p.px2 = l.px2;
-        p.pw = l.direct ? nullptr : s + l.pw; p.pw2 = l.pw2;
-        p.tx = gw ? s + l.tx : nullptr; p.tx2 = l.tx2;
-        p.tw = gx ? s + l.tw : nullptr; p.tw2 = l.tw2;
-        p.pitch_p = l.pitch_p; p.pitch_tx = l.pitch_tx; p.pitch_tw = l.pitch_tw;
-        p.vocab = vocab; p.d = (int)d; p.xtiles = (int)(up(rows, 64) / 64); p.nx = nx; p.nw = nw;
-        // (fp32: a workgroup of W's leaves its largest magnitude for the kernels behind; with W read in place there is none)
-        const unsigned wtiles = p.pw || p.tw ? (unsigned)(up(vocab, 64) / 64) : 0;
-        const dim3 grid(p.xtiles + wtiles, (unsigned)(l.dp / 64));
+        p.pw = s + l.pw; p.pw2 = l.pw2;
+        p.xrows = l.tp; p.wrows = l.direct ? 0 : vocab; p.d = (int)d; p.pieces = (int)(l.dp / 8); p.nx = nx; p.nw = nw;
+        const int64_t per = 256 * kPrepareTurns;
+        p.xgroups = (int)((up(rows, kStageCols) * p.pieces + per - 1) / per);
+        const dim3 grid((unsigned)(p.xgroups + (p.wrows * p.pieces + per - 1) / per));
         if (l.split) hipLaunchKernelGGL(xent_prepare_kernel<float>, grid, dim3(256), 0, st, p);
         else hipLaunchKernelGGL(xent_prepare_kernel<__bf16>, grid, dim3(256), 0, st, p);
     }
     for (int64_t piece = 0; piece < l.pieces; ++piece) {
         const int64_t first = piece * l.room, n = std::min(l.room, rows - first);  // rows of the piece at most
+        const Operand whole = {l.direct ? (const char *)w : s + l.pw, l.direct ? ldw * 2 : l.pitch_p, (int64_t)l.pw2, (int)vocab, (int)d};
+        const Operand part = {s + l.px + first * l.pitch_p, l.pitch_p, (int64_t)l.px2, 0, (int)d};
         if (n > 0) {
             LogitArgs a = {};
-            a.w = {l.direct ? (const char *)w : s + l.pw, l.direct ? ldw * 2 : l.pitch_p, (int64_t)l.pw2, (int)vocab};
-            a.x = {s + l.px + first * l.pitch_p, l.pitch_p, (int64_t)l.px2, 0};
+            a.w = whole; a.x = part;
             a.hdr = hdr; a.wanted = wanted; a.stats = (float *)(s + l.stats); a.hit = (float *)(s + l.hit);
             a.P = s + l.P; a.P2 = l.P2; a.pitch_P = l.pitch_P;
             a.first = (int)first; a.room = (int)l.room; a.ktiles = (int)(l.dp / kStageCols);
@@ -809,17 +791,15 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
         if (n > 0) {
             TurnArgs t = {};
             t.hdr = hdr; t.wanted = wanted; t.stats = (const float *)(s + l.stats); t.lse = (const float *)(s + l.lse); t.up = upstream;
-            t.P = s + l.P; t.GT = s + l.GT; t.P2 = l.P2; t.GT2 = l.GT2; t.pitch_P = l.pitch_P; t.pitch_GT = l.pitch_GT;
+            t.P = s + l.P; t.P2 = l.P2; t.pitch_P = l.pitch_P;
             t.first = (int)first; t.room = (int)l.room; t.vocab = (int)vocab; t.part = l.edge_l / 2;
-            const dim3 grid((unsigned)(up(vocab, 64) / 64), (unsigned)(up(n, 64) / 64));
+            const dim3 grid((unsigned)(up(vocab, 256) / 256), (unsigned)(up(n, kStageCols) / kTurnRows));
             if (l.split) hipLaunchKernelGGL(xent_turn_kernel<true>, grid, dim3(256), 0, st, t);
             else hipLaunchKernelGGL(xent_turn_kernel<false>, grid, dim3(256), 0, st, t);
         }
         GradArgs a = {};
-        a.G = {s + l.P, l.pitch_P, (int64_t)l.P2, 0};
-        a.wt = {s + l.tw, l.pitch_tw, (int64_t)l.tw2, (int)d};
-        a.GT = {s + l.GT, l.pitch_GT, (int64_t)l.GT2, (int)vocab};
-        a.xt = {s + l.tx + first * 2, l.pitch_tx, (int64_t)l.tx2, (int)d};
+        a.G = {s + l.P, l.pitch_P, (int64_t)l.P2, 0, (int)vocab};
+        a.w = whole; a.x = part;
         a.hdr = hdr; a.up = upstream; a.xparts = (float *)(s + l.xparts); a.wparts = (float *)(s + l.wparts);
         a.gw = gw; a.ldgw = ldgw; a.ktiles = (int)(up(vocab, kStageCols) / kStageCols);
         a.xslots = l.xslots; a.xgroups = gx && n > 0 ? l.xgroups : 0; a.wcut = l.wcut; a.through = l.through; a.first = (int)first; a.room = (int)l.room;
