@@ -363,7 +363,7 @@ int imunpack_rmsnorm_quantize(const void *x, int64_t ldx, const void *residual, 
  *     gweight_j = sum over rows of gy_j h_j rstd
  * gweight: device, weight_dtype, may be NULL (then no workspace is needed).  The sums over rows are taken in a fixed order:
  * equal inputs give equal bits.  gx may be gy or gh.  workspace: device, 16-byte aligned, of the size that
- * imunpack_rmsnorm_backward_workspace gives.  Errors: EINVAL as above; ESMALL. */
+ * imunpack_rmsnorm_backward_workspace gives (0 for few rows: NULL will do).  Errors: EINVAL as above; ESMALL. */
 int imunpack_rmsnorm_backward_workspace(int64_t rows, int64_t d, int dtype, size_t *bytes);
 int imunpack_rmsnorm_backward(const void *gy, int64_t ldgy, const void *x, int64_t ldx, const void *residual, int64_t ldres,
                               const void *gh, int64_t ldgh, const void *weight, const float *rstd, int64_t rows, int64_t d, int dtype, int weight_dtype,

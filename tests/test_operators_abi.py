@@ -46,9 +46,9 @@ def test_rmsnorm_backward(lib):
     lib.imunpack_rmsnorm_backward_workspace.argtypes = [i64, i64, i32, vp]
     assert lib.imunpack_rmsnorm_backward_workspace(2, 8, 0, None) == EINVAL
     assert lib.imunpack_rmsnorm_backward_workspace(2, 0, 0, C.byref(size)) == EINVAL
-    assert lib.imunpack_rmsnorm_backward_workspace(2, 8, 0, C.byref(size)) == 0 and size.value >= 32
+    assert lib.imunpack_rmsnorm_backward_workspace(2000, 8, 0, C.byref(size)) == 0 and size.value >= 32
     call = caller(lib.imunpack_rmsnorm_backward, [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i32, i32, vp, i64, vp, vp, C.c_size_t, vp],
-                  dict(gy=FAKE, ldgy=8, x=FAKE, ldx=8, res=FAKE, ldres=8, gh=FAKE, ldgh=8, w=FAKE, rstd=FAKE, rows=2, d=8, dtype=0, wtype=0, gx=FAKE, ldgx=8, gw=FAKE,
+                  dict(gy=FAKE, ldgy=8, x=FAKE, ldx=8, res=FAKE, ldres=8, gh=FAKE, ldgh=8, w=FAKE, rstd=FAKE, rows=2000, d=8, dtype=0, wtype=0, gx=FAKE, ldgx=8, gw=FAKE,
                        ws=FAKE, bytes=size.value, st=None))
     for bad in (dict(gy=None), dict(x=None), dict(w=None), dict(rstd=None), dict(gx=None), dict(ws=None), dict(ldgy=7), dict(ldx=7), dict(ldres=7), dict(ldgh=7), dict(ldgx=7),
                 dict(dtype=5), dict(d=-1), dict(rows=-3)):
