@@ -11,7 +11,7 @@
 // all on the matrix cores, and what is held does not grow with the rows.
 //
 // bfloat16 operands: products in bfloat16, G rounded to bfloat16.  fp32 operands: each value is the sum of two binary16 numbers
-// (22 bits of it; scaled by a power of two so that the operand's largest lies below 2^15) and a product is three of them, which is within
+// (22 bits of it; scaled by a power of two so that the operand's largest, or for the loss alone each row's, lies below 2^15) and a product is three of them, which is within
 // the rounding of a binary32 sum; three times the instructions at eight times and more the rate of the binary32 ones.
 #include "common.h"
 #include "elements.h"
@@ -29,6 +29,7 @@ constexpr int kXentSlots = 256;             // parts of the tiles of a gradient 
 constexpr int kPartTiles = 2;               // k-tiles of a part at least: below that its sums cost more than its products
 constexpr int kScanGroups = 512, kScanX = 64;  // workgroups that look for the largest magnitudes, those of x first
 constexpr int kJoinRows = 8;
+constexpr int kLargeRows = 1024;            // rows from which the logits may go in large tiles
 
 struct XentHeader {
     int32_t count;    // rows with a target
@@ -43,9 +44,24 @@ static_assert(sizeof(XentHeader) == 256 + 4 * kScanGroups, "header");
 // Rows of the piece that begins at row `first` and has room for `room`.
 __device__ __forceinline__ int rows_of(const XentHeader *hdr, int first, int room) { return max(0, min(hdr->count - first, room)); }
 
+// Edges of the tiles of the logits and of the gradients, from the rows of a piece: 256, which reads each operand half as often, where the rows
+// fill such tiles and the tiles fill the CUs.  The loss of 4096 x 2048 by 16000 columns: 260 us with edges of 128, 233 with 256 (bf16; fp32 721
+// and 678); of 200 rows: 40 and 60.  With its gradients, 868 and 783 (2176 and 2033); of 640 rows 188 and 204 (473 and 521).  Only the
+// device knows how many rows have a target: where both are possible both are launched, and one of them finds nothing to do.
+__host__ __device__ __forceinline__ int logits_edge(int rows, int d, int vocab) {
+    return rows >= kLargeRows && d >= 512 && (rows + 255) / 256 * ((vocab + 255) / 256) >= (int)kCus ? 256 : 128;
+}
+__host__ __device__ __forceinline__ int grads_edge(int rows, int d, int vocab) { return rows >= 1536 && (int64_t)vocab * d >= 1 << 23 ? 256 : 128; }
+__device__ __forceinline__ int rows_at_most(const XentHeader *hdr, int room) { return min(hdr->count, room); }
+
 // What 2 to its power an operand is multiplied by before it is split.
 __device__ __forceinline__ int scale_exponent(uint32_t amax) { return min(kTop - ((int)(amax >> 23) - 127), 126); }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// Where column col of a row lies, in 16 bits or as the first of two numbers, the second one kSecond bytes behind it (blocks of 32, see product.h).
+template <bool PAIRS>
+__host__ __device__ __forceinline__ int64_t byte_of(int64_t col) { return PAIRS ? (col / 32 * 64 + col % 32) * 2 : col * 2; }
+constexpr int kSecond = 64;
 
 struct ScanArgs {
     const int64_t *target;
@@ -139,9 +155,9 @@ struct PrepareArgs {
     XentHeader *hdr;
     const int32_t *source;
     char *px, *pw;            // x (gathered) and W in 16 bits, rows of `pieces` times 16 bytes
-    int64_t px2, pw2;         // from the first number of a value to the second, bytes
     int64_t xrows, wrows;     // rows there is room for; rows of W that are wanted
     int d, pieces, xgroups, nx, nw;  // workgroups that work on x; nx, nw: workgroups that looked for the largest magnitudes
+    int32_t *ex, *ew;         // the loss alone, fp32: what 2 to their power a row of x, of W is multiplied with
 };
 constexpr int kPrepareTurns = 4;
 // Eight columns of a row at a time: binary32 as two binary16 numbers, bfloat16 as it is; zeros behind the last column and, to a whole
@@ -154,11 +170,13 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(const PrepareArgs a) 
     const int group = isX ? blockIdx.x : blockIdx.x - a.xgroups;
     const int64_t count = isX ? a.hdr->count : a.wrows, rows = isX ? min((count + kStageCols - 1) / kStageCols * kStageCols, a.xrows) : count;
     float scale = 1.0f;
+    int e = 0;
     if constexpr (SPLIT) {  // the first workgroup of either operand leaves the largest magnitude for the kernels behind
         float m = 0.0f;
         for (int k = threadIdx.x; k < (isX ? a.nx : a.nw); k += 256) m = fmaxf(m, __uint_as_float(a.hdr->found[isX ? k : a.nx + k]));
         m = reduce_threads<256, true>(m, lds);
-        scale = power_of_two(scale_exponent(__float_as_uint(m)));
+        e = scale_exponent(__float_as_uint(m));
+        scale = power_of_two(e);
         if (threadIdx.x == 0 && group == 0) a.hdr->amax[isX ? 0 : 1] = __float_as_uint(m);
     }
     const int64_t at0 = (int64_t)group * 256 * kPrepareTurns + threadIdx.x;
@@ -178,7 +196,8 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(const PrepareArgs a) 
 #pragma unroll
     for (int i = 0; i < kPrepareTurns; ++i) {
         if (row[i] >= rows) continue;
-        char *to = (isX ? a.px : a.pw) + (row[i] * a.pieces * 8 + col[i]) * 2;
+        if (SPLIT && a.ex && col[i] == 0 && row[i] < count) (isX ? a.ex : a.ew)[row[i]] = e;
+        char *to = (isX ? a.px : a.pw) + row[i] * a.pieces * (SPLIT ? 32 : 16) + byte_of<SPLIT>(col[i]);
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -193,7 +212,7 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(const PrepareArgs a) 
             }
         }
         *reinterpret_cast<v4i32 *>(to) = v4i32{(int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-        if constexpr (SPLIT) *reinterpret_cast<v4i32 *>(to + (isX ? a.px2 : a.pw2)) = v4i32{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3]};
+        if constexpr (SPLIT) *reinterpret_cast<v4i32 *>(to + kSecond) = v4i32{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3]};
     }
 }
 
@@ -210,15 +229,74 @@ struct Upstream {
     __device__ __forceinline__ float one(const XentHeader *hdr) const { return ldexpf(whole(hdr), -exponent_of(whole(hdr))); }
 };
 
+// The same row by row, for the loss alone: each row by its own largest magnitude, which no other kernel has to look for.  A wave to a row,
+// which it reads twice (the second time out of a cache).
+struct PrepareRowsArgs {
+    const float *x, *w;
+    int64_t ldx, ldw;
+    const XentHeader *hdr;
+    const int32_t *source;
+    char *px, *pw;
+    int64_t pitch, wrows;
+    int32_t *ex, *ew;
+    int d, xgroups;
+};
+__global__ __launch_bounds__(256) void xent_prepare_rows_kernel(const PrepareRowsArgs a) {
+    const bool isX = (int)blockIdx.x < a.xgroups;
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)(isX ? blockIdx.x : blockIdx.x - a.xgroups) * 4 + (threadIdx.x >> 6), rows = isX ? a.hdr->count : a.wrows;
+    if (row >= rows) return;
+    const float *p = isX ? a.x + (int64_t)a.source[row] * a.ldx : a.w + row * a.ldw;
+    float m = 0.0f;
+    for (int col = lane * 8; col < a.d; col += 2048) {
+        piece_t<float, 4> f[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) f[i][k] = load_piece<float, 4>(p + col + 512 * i + 4 * k, a.d - (col + 512 * i + 4 * k));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) m = fmaxf(m, fabsf(f[i][k >> 2][k & 3]));
+    }
+    m = wave_max(m);
+    const int e = scale_exponent(__float_as_uint(m));
+    const float scale = power_of_two(e);
+    if (lane == 0) (isX ? a.ex : a.ew)[row] = e;
+    char *to = (isX ? a.px : a.pw) + row * a.pitch;
+    for (int col = lane * 8; col < a.pitch / 4; col += 2048) {
+        piece_t<float, 4> f[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) f[i][k] = load_piece<float, 4>(p + col + 512 * i + 4 * k, a.d - (col + 512 * i + 4 * k));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (col + 512 * i >= a.pitch / 4) break;
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float a0 = f[i][k >> 1][2 * (k & 1)] * scale, a1 = f[i][k >> 1][2 * (k & 1) + 1] * scale;
+                const _Float16 h0 = (_Float16)a0, h1 = (_Float16)a1;
+                hi[k] = pack(h0, h1);
+                lo[k] = pack((_Float16)(a0 - (float)h0), (_Float16)(a1 - (float)h1));
+            }
+            *reinterpret_cast<v4i32 *>(to + byte_of<true>(col + 512 * i)) = v4i32{(int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+            *reinterpret_cast<v4i32 *>(to + byte_of<true>(col + 512 * i) + kSecond) = v4i32{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3]};
+        }
+    }
+}
+
 struct LogitArgs {
     Operand w, x;             // rows of the vocabulary and of the piece
     const XentHeader *hdr;
     const int32_t *wanted;
+    const int32_t *ex, *ew;   // the loss alone, fp32: exponents of the rows' scales
     float *stats, *hit;       // [part of the vocabulary][row of the piece] largest logit and sum; the target's logit
     char *P;                  // [row of the piece][vocabulary] exponentials, relative to the largest of the row and part, times 2^kTop where they are binary16
-    int64_t P2, pitch_P;
+    int64_t pitch_P;
     int first, room;          // the piece's first row, and for how many there is room
-    int ktiles;
+    int d, ktiles;
 };
 constexpr float kLog2e = 1.44269504088896340736f;
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
@@ -241,7 +319,7 @@ __global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void 
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     constexpr int kEdge = 64 * T;
     const int count = rows_of(a.hdr, a.first, a.room), vocab = a.w.rows, mtiles = (vocab + kEdge - 1) / kEdge, ntiles = (count + kEdge - 1) / kEdge;
-    if ((int)blockIdx.x >= mtiles * ntiles) return;
+    if ((int)blockIdx.x >= mtiles * ntiles || logits_edge(rows_at_most(a.hdr, a.room), a.d, vocab) != kEdge) return;
     int tm, tn;
     tile_at(blockIdx.x, mtiles, ntiles, tm, tn);
     tm = __builtin_amdgcn_readfirstlane(tm);
@@ -249,11 +327,11 @@ __global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void 
     Operand x = a.x;
     x.rows = count;
     v16f32 acc[T][T];
-    product_tile<F16, T, T, F16 ? 3 : 1, DEPTH, false, false>(a.w, x, tm * kEdge, tn * kEdge, 0, a.ktiles, smem, acc);
+    product_tile<F16, T, T, DEPTH, false, false>(a.w, x, tm * kEdge, tn * kEdge, 0, a.ktiles, smem, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, lhalf = lane >> 5;
     const int vwave = tm * kEdge + (wave >> 1) * 32 * T, twave = tn * kEdge + (wave & 1) * 32 * T;  // the wave's first column and row of the piece
-    const int down = F16 ? -(scale_exponent(a.hdr->amax[0]) + scale_exponent(a.hdr->amax[1])) : 0;
-    auto logit = [&](float x) __attribute__((always_inline)) { return F16 ? ldexpf(x, down) : x; };
+    const int down = F16 && KEEP ? -(scale_exponent(a.hdr->amax[0]) + scale_exponent(a.hdr->amax[1])) : 0;
+    auto logit = [&](float x) __attribute__((always_inline)) { return F16 && KEEP ? ldexpf(x, down) : x; };
     // FULL: no column behind the vocabulary and no row behind the last one in the wave's part (nothing to compare)
     auto finish = [&](auto full) __attribute__((always_inline)) {
         constexpr bool FULL = decltype(full)::value;
@@ -265,6 +343,17 @@ __global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void 
             const bool hits = hit_at >= 0 && hit_at < 32 * T;
             const int left = vocab - vwave - 4 * lhalf, own = hit_at - 4 * lhalf;  // the lane has columns 32 i + 8 q + k
             float top = -__builtin_inff(), sum = 0.0f;
+            if constexpr (F16 && !KEEP) {
+                const int ex = in_rows ? a.ex[t] : 0;
+#pragma unroll
+                for (int i = 0; i < T; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const v4i32 ew = *reinterpret_cast<const v4i32 *>(a.ew + vwave + 32 * i + 8 * q + 4 * lhalf);  // (room for whole tiles)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) acc[i][j][4 * q + k] = ldexpf(acc[i][j][4 * q + k], -ex - ew[k]);
+                    }
+            }
 #pragma unroll
             for (int i = 0; i < T; ++i)
 #pragma unroll
@@ -281,7 +370,7 @@ __global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void 
                         if (32 * i + (r >> 2) * 8 + (r & 3) == own) hit = acc[i][j][r];
                 if (hits && ((hit_at >> 2) & 1) == lhalf) a.hit[a.first + t] = logit(hit);
             }
-            char *to = a.P + t * a.pitch_P + (vwave + 8 * lhalf) * 2;
+            char *to = a.P + t * a.pitch_P + byte_of<F16>(vwave) + 16 * lhalf;
 #pragma unroll
             for (int i = 0; i < T; ++i) {
                 float p[16];
@@ -292,13 +381,13 @@ __global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void 
                 }
                 if constexpr (KEEP) {
                     // columns 8 q .. 8 q + 7 lie in both halves of the wave; the halves trade, and each has eight in a row: 16 bytes to a store
-                    auto put = [&](const uint32_t (&w)[8], int64_t off) __attribute__((always_inline)) {
+                    auto put = [&](const uint32_t (&w)[8], int off) __attribute__((always_inline)) {
 #pragma unroll
                         for (int q = 0; q < 4; q += 2) {
                             const auto x = __builtin_amdgcn_permlane32_swap(w[2 * q], w[2 * q + 2], false, false);
                             const auto y = __builtin_amdgcn_permlane32_swap(w[2 * q + 1], w[2 * q + 3], false, false);
                             if (FULL || in_rows)
-                                *reinterpret_cast<v4i32 *>(to + off + (32 * i + 8 * q) * 2) = v4i32{(int)x[0], (int)y[0], (int)x[1], (int)y[1]};
+                                *reinterpret_cast<v4i32 *>(to + off + byte_of<F16>(32 * i + 8 * q)) = v4i32{(int)x[0], (int)y[0], (int)x[1], (int)y[1]};
                         }
                     };
                     uint32_t w[8];
@@ -314,7 +403,7 @@ __global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void 
                         put(w, 0);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) w[k] = pack((_Float16)p[2 * k], (_Float16)p[2 * k + 1]);
-                        put(w, a.P2);
+                        put(w, kSecond);
                     } else {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) w[k] = pack((__bf16)p[2 * k], (__bf16)p[2 * k + 1]);
@@ -333,7 +422,7 @@ __global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void 
 
 struct JoinArgs {
     const float *stats, *hit;
-    int parts, how, first, room;
+    int d, vocab, how, first, room;
     XentHeader *hdr;
     const int32_t *source;
     float *lse, *row_loss, *loss;
@@ -346,14 +435,21 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const JoinArgs a) {
     const int r = threadIdx.x % kJoinRows, g = threadIdx.x / kJoinRows, at = blockIdx.x * kJoinRows + r, t = a.first + at, count = a.hdr->count;
     const int groups = max(1, (count + kJoinRows - 1) / kJoinRows);  // of all pieces
     if ((int)blockIdx.x + a.first / kJoinRows >= groups) return;
+    const int edge = logits_edge(rows_at_most(a.hdr, a.room), a.d, a.vocab), parts = (a.vocab + edge - 1) / edge * 2;
     float top = -__builtin_inff(), sum = 0.0f;
     if (t < count)
-        for (int k = g; k < a.parts; k += 32) {
-            const float2 s = *reinterpret_cast<const float2 *>(a.stats + ((int64_t)k * a.room + at) * 2);
-            const float next = fmaxf(top, s.x);
-            if (next > -__builtin_inff()) sum = sum * fast_exp(top - next) + s.y * fast_exp(s.x - next);
-            else sum += s.y;  // (NaN stays)
-            top = next;
+        for (int k0 = g; k0 < parts; k0 += 128) {
+            float2 s[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                s[k] = k0 + 32 * k < parts ? *reinterpret_cast<const float2 *>(a.stats + ((int64_t)(k0 + 32 * k) * a.room + at) * 2) : make_float2(-__builtin_inff(), 0.0f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float next = fmaxf(top, s[k].x);
+                if (next > -__builtin_inff()) sum = sum * fast_exp(top - next) + s[k].y * fast_exp(s[k].x - next);
+                else sum += s[k].y;  // (NaN stays)
+                top = next;
+            }
         }
     tops[g][r] = top;
     sums[g][r] = sum;
@@ -400,27 +496,27 @@ struct TurnArgs {
     const float *stats, *lse;
     Upstream up;
     char *P;
-    int64_t P2, pitch_P;
-    int first, room, vocab, part;  // part: columns that share a largest logit
+    int64_t pitch_P;
+    int first, room, d, vocab;
 };
-constexpr int kTurnRows = 32;
-// Exponentials become G where they lie, 256 columns of 32 rows to a workgroup, eight columns to a lane: zeros behind the vocabulary and, to a
+// Exponentials become G where they lie, 256 columns of ROWS rows to a workgroup, eight columns to a lane: zeros behind the vocabulary and, to a
 // whole k-tile, behind the last row.
-template <bool F16>
+template <bool F16, int ROWS>
 __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
     const int rows = rows_of(a.hdr, a.first, a.room), last = (rows + kStageCols - 1) / kStageCols * kStageCols;
-    const int row0 = blockIdx.y * kTurnRows + (threadIdx.x >> 5), v0 = blockIdx.x * 256 + (threadIdx.x & 31) * 8, left = a.vocab - v0;
-    if ((int)blockIdx.y * kTurnRows >= last || v0 >= (a.vocab + kStageCols - 1) / kStageCols * kStageCols) return;
+    const int row0 = blockIdx.y * ROWS + (threadIdx.x >> 5), v0 = blockIdx.x * 256 + (threadIdx.x & 31) * 8, left = a.vocab - v0;
+    if ((int)blockIdx.y * ROWS >= last || v0 >= (a.vocab + kStageCols - 1) / kStageCols * kStageCols) return;
     const float all = a.up.g ? 0.0f : a.up.one(a.hdr);
-    constexpr int kTurns = kTurnRows / 8;
+    const int part = v0 / (logits_edge(rows_at_most(a.hdr, a.room), a.d, a.vocab) / 2);  // whose columns share a largest logit
+    constexpr int kTurns = ROWS / 8;
     v4i32 hi[kTurns], lo[kTurns];
-    char *const p0 = a.P + v0 * 2;
+    char *const p0 = a.P + byte_of<F16>(v0);
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const int t = row0 + 8 * i;
         if (t >= rows) continue;
         hi[i] = *reinterpret_cast<const v4i32 *>(p0 + t * a.pitch_P);
-        if (F16) lo[i] = *reinterpret_cast<const v4i32 *>(p0 + t * a.pitch_P + a.P2);
+        if (F16) lo[i] = *reinterpret_cast<const v4i32 *>(p0 + t * a.pitch_P + kSecond);
     }
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
@@ -428,7 +524,7 @@ __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
         if (t >= last) continue;
         uint32_t qh[4] = {0, 0, 0, 0}, ql[4] = {0, 0, 0, 0};
         if (t < rows) {
-            const float top = a.stats[((int64_t)(v0 / a.part) * a.room + t) * 2];
+            const float top = a.stats[((int64_t)part * a.room + t) * 2];
             const float g = a.up.g ? a.up.g[a.first + t] : all;
             const float down = __builtin_amdgcn_exp2f((top - a.lse[a.first + t]) * kLog2e) * g, one = F16 ? g * power_of_two(kTop) : g;
             const int own = a.wanted[a.first + t] - v0;
@@ -452,7 +548,7 @@ __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
             }
         }
         *reinterpret_cast<v4i32 *>(p0 + t * a.pitch_P) = v4i32{(int)qh[0], (int)qh[1], (int)qh[2], (int)qh[3]};
-        if (F16) *reinterpret_cast<v4i32 *>(p0 + t * a.pitch_P + a.P2) = v4i32{(int)ql[0], (int)ql[1], (int)ql[2], (int)ql[3]};
+        if (F16) *reinterpret_cast<v4i32 *>(p0 + t * a.pitch_P + kSecond) = v4i32{(int)ql[0], (int)ql[1], (int)ql[2], (int)ql[3]};
     }
 }
 
@@ -463,6 +559,11 @@ __host__ __device__ __forceinline__ int parts_of(int tiles, int slots, int ktile
     return n > 1 ? n : 1;
 }
 
+// How the gradients are cut with tiles of one size.
+struct Cut {
+    int xslots, xgroups, wcut;  // parts of tiles of gx that go at a time, and as many as there can be of this problem; parts of the tiles of gW
+    bool through;               // gW goes through sums in fp32
+};
 struct GradArgs {
     Operand G, w, x;   // [row of the piece][vocabulary], [vocabulary][feature], [row of the piece][feature]
     const XentHeader *hdr;
@@ -470,8 +571,8 @@ struct GradArgs {
     float *xparts, *wparts;  // [slot][tile]; wparts: where the tiles of gW are cut, or are sums over several pieces
     void *gw;
     int64_t ldgw;
-    int ktiles, xslots, xgroups, wcut, first, room;  // k-tiles of gx's contraction; parts of its tiles at a time, workgroups there are for them
-    bool through;            // gW goes through wparts
+    int d, ktiles, first, room;  // ktiles: of gx's contraction
+    Cut cut;
 };
 // A tile (or part of one) of gx = G W, with W across, or of gW = G^T x, both across and with rows of zeros to whole k-tiles.
 template <bool F16, int T, int DEPTH, bool X>
@@ -479,9 +580,10 @@ __device__ __forceinline__ void grad_tile(const GradArgs &a, int wg, char *smem)
     constexpr int kEdge = 64 * T;
     const int count = rows_of(a.hdr, a.first, a.room);
     if (!X && count == 0 && a.first > 0) return;  // (the first piece writes zeros)
-    const int height = X ? count : a.w.rows, width = a.w.cols;  // of the gradient
+    const int height = X ? count : a.w.rows, width = a.d;  // of the gradient
     const int mtiles = (height + kEdge - 1) / kEdge, ntiles = (width + kEdge - 1) / kEdge, tiles = mtiles * ntiles;
-    const int rtiles = (count + kStageCols - 1) / kStageCols, ktiles = X ? a.ktiles : rtiles, parts = X ? parts_of(tiles, a.xslots, a.ktiles) : a.wcut;
+    constexpr int R = kPlaces<F16>;
+    const int rtiles = (count + R - 1) / R, ktiles = X ? a.ktiles : rtiles, parts = X ? parts_of(tiles, a.cut.xslots, a.ktiles) : a.cut.wcut;
     if (wg >= tiles * parts) return;
     int tm, tn, part = 0, slot = 0;
     if (parts == 1) {
@@ -499,13 +601,14 @@ __device__ __forceinline__ void grad_tile(const GradArgs &a, int wg, char *smem)
     tn = __builtin_amdgcn_readfirstlane(tn);
     const int k0 = __builtin_amdgcn_readfirstlane((int)((int64_t)ktiles * part / parts)), k1 = __builtin_amdgcn_readfirstlane((int)((int64_t)ktiles * (part + 1) / parts));
     Operand G = a.G, x = a.x;
-    G.rows = X ? count : rtiles * kStageCols;
-    x.rows = rtiles * kStageCols;
+    G.rows = X ? count : rtiles * R;
+    if (X) G.cols = ktiles * kStageCols;  // (zeros behind the vocabulary)
+    x.rows = rtiles * R;
     v16f32 acc[T][T];
-    product_tile<F16, T, T, F16 ? 3 : 1, DEPTH, !X, true>(G, X ? a.w : x, tm * kEdge, tn * kEdge, k0, k1, smem, acc);
+    product_tile<F16, T, T, DEPTH, !X, true>(G, X ? a.w : x, tm * kEdge, tn * kEdge, k0, k1, smem, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r0 = (wave >> 1) * 32 * T, rl = 4 * (lane >> 5), c0 = (wave & 1) * 32 * T + (lane & 31);
-    if (X || a.through) {
+    if (X || a.cut.through) {
         float *to = (X ? a.xparts : a.wparts) + (int64_t)slot * kEdge * kEdge + r0 * kEdge;
         const bool add = !X && a.first > 0;
 #pragma unroll
@@ -556,8 +659,9 @@ __device__ __forceinline__ void grad_tile(const GradArgs &a, int wg, char *smem)
 template <bool F16, int T, int DEPTH>
 __global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void xent_grads_kernel(const GradArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    if ((int)blockIdx.x < a.xgroups) grad_tile<F16, T, DEPTH, true>(a, blockIdx.x, smem);
-    else grad_tile<F16, T, DEPTH, false>(a, blockIdx.x - a.xgroups, smem);
+    if (grads_edge(rows_at_most(a.hdr, a.room), a.d, a.w.rows) != 64 * T) return;
+    if ((int)blockIdx.x < a.cut.xgroups) grad_tile<F16, T, DEPTH, true>(a, blockIdx.x, smem);
+    else grad_tile<F16, T, DEPTH, false>(a, blockIdx.x - a.cut.xgroups, smem);
 }
 
 struct FoldArgs {
@@ -567,29 +671,49 @@ struct FoldArgs {
     const int32_t *place;
     void *gx, *gw;
     int64_t ldgx, ldgw, xrows, wrows;  // rows of gx and gW that are made here
-    int d, edge, ktiles, xslots, wcut, first, room;
+    int d, vocab, ktiles, first, room;
+    Cut cut[2];               // with tiles of 128 and of 256
 };
-// Rows of gx that belong to the piece (the first: zeros for those without a target) and of gW from the parts of their tiles.
-template <class T>
+// Rows of gx that belong to the piece (the first: zeros for those without a target) and of gW from the parts of their tiles, 256 columns to a
+// workgroup, four to a lane.  ROWS = 4: a row to a wave; 1: a row to the workgroup, a quarter of the parts to a wave, so that as many loads
+// are under way where there are many parts (76 parts of 74 rows of 168 columns: 22 us and 5; 2 of 8192 rows of 768 columns, bf16: 103 and 39).
+template <class T, int ROWS>
 __global__ __launch_bounds__(256) void xent_fold_kernel(const FoldArgs a) {
-    const bool isX = (int64_t)blockIdx.x < a.xrows;
-    const int64_t row = isX ? blockIdx.x : blockIdx.x - a.xrows;
-    const int col = (blockIdx.y * 256 + threadIdx.x) * 4, place = isX ? a.place[row] : (int)row, edge = a.edge;
-    const int rows = isX ? rows_of(a.hdr, a.first, a.room) : (int)a.wrows, at = isX && place >= 0 ? place - a.first : place;
-    if (col >= a.d || (isX && (place < 0 ? a.first > 0 : at < 0 || at >= rows))) return;
+    __shared__ float4 sums[4][64];
+    const int64_t xgroups = (a.xrows + ROWS - 1) / ROWS;
+    const bool isX = (int64_t)blockIdx.x < xgroups;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = (blockIdx.y * 64 + lane) * 4;
+    const int64_t row = (isX ? blockIdx.x : blockIdx.x - xgroups) * ROWS + (ROWS == 4 ? wave : 0);
+    const int edge = grads_edge(rows_at_most(a.hdr, a.room), a.d, a.vocab);
+    const Cut cut = a.cut[edge / 256];
+    if (row >= (isX ? a.xrows : a.wrows) || (!isX && !cut.through)) return;
+    const int place = isX ? a.place[row] : (int)row, rows = isX ? rows_of(a.hdr, a.first, a.room) : (int)a.wrows, at = place < 0 ? place : isX ? place - a.first : place;
+    if (place < 0 ? a.first > 0 : at < 0 || at >= rows) return;
+    const int mtiles = (rows + edge - 1) / edge, ntiles = (a.d + edge - 1) / edge, tiles = mtiles * ntiles;
+    const int n = place < 0 ? 0 : isX ? parts_of(tiles, cut.xslots, a.ktiles) : cut.wcut, last = ROWS == 4 ? n : n * (wave + 1) / 4;
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (at >= 0) {
-        const int mtiles = (rows + edge - 1) / edge, ntiles = (a.d + edge - 1) / edge, tiles = mtiles * ntiles;
-        const int n = isX ? parts_of(tiles, a.xslots, a.ktiles) : a.wcut, tile = col / edge * mtiles + at / edge;
-        const float *p = (isX ? a.xparts : a.wparts) + (int64_t)tile * edge * edge + (at % edge) * edge + col % edge;
-        for (int k = 0; k < n; ++k) {
-            const float4 f = *reinterpret_cast<const float4 *>(p + (int64_t)k * tiles * edge * edge);
-            s[0] += f.x; s[1] += f.y; s[2] += f.z; s[3] += f.w;
-        }
-        const int e = a.up.exponent(a.hdr) - (sizeof(T) == 4 ? kTop + scale_exponent(a.hdr->amax[isX ? 1 : 0]) : 0);
+    if (col < a.d) {
+        const float *p = (isX ? a.xparts : a.wparts) + (int64_t)(col / edge * mtiles + at / edge) * edge * edge + at % edge * edge + col % edge;
+        const int64_t step = (int64_t)tiles * edge * edge;
+        for (int k0 = ROWS == 4 ? 0 : n * wave / 4; k0 < last; k0 += 4) {
+            float4 f[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[k] = ldexpf(s[k], e);
+            for (int k = 0; k < 4; ++k) f[k] = k0 + k < last ? *reinterpret_cast<const float4 *>(p + (k0 + k) * step) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { s[0] += f[k].x; s[1] += f[k].y; s[2] += f[k].z; s[3] += f[k].w; }
+        }
     }
+    if constexpr (ROWS == 1) {
+        sums[wave][lane] = make_float4(s[0], s[1], s[2], s[3]);
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int w = 1; w < 4; ++w) { s[0] += sums[w][lane].x; s[1] += sums[w][lane].y; s[2] += sums[w][lane].z; s[3] += sums[w][lane].w; }
+    }
+    if (col >= a.d) return;
+    const int e = a.up.exponent(a.hdr) - (sizeof(T) == 4 ? kTop + scale_exponent(a.hdr->amax[isX ? 1 : 0]) : 0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k] = ldexpf(s[k], e);
     store_upto<T, 4>((T *)(isX ? a.gx : a.gw) + row * (isX ? a.ldgx : a.ldgw) + col, s, a.d - col);
 }
 
@@ -614,54 +738,57 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // Where everything lies in the workspace.
 struct XentLayout {
+    int64_t places;               // of a contraction in a k-tile
     int64_t dp, tp, vp;           // features, rows, vocabulary rounded up to what the products read
     bool split, direct;           // two numbers to a value; W read in place
     int64_t pitch_p, pitch_P;     // bytes from row to row of x and W in 16 bits, and of G
-    int edge_l, edge_g;           // tile edges of the logits and of the gradients
-    int parts_v;                  // parts of the vocabulary whose sums are joined
+    int edge_l, edge_g;           // largest tile edges that the rows allow, of the logits and of the gradients
     int64_t room, pieces;         // rows to a piece, pieces
-    int xslots, xgroups, wcut;    // parts of tiles of gx that go at a time, and as many as there can be of this problem; into how many parts the tiles of gW are cut
-    bool through;                 // gW goes through sums in fp32
-    size_t source, place, wanted, lse, row_loss, hit, g, stats, px, pw, P, xparts, wparts, bytes;
-    size_t px2, pw2, P2;
+    Cut cut[2];                   // of the gradients, with tiles of 128 and of 256
+    bool by_rows;                 // each row of x and W has a scale of its own
+    size_t source, place, wanted, lse, row_loss, hit, g, ex, ew, stats, px, pw, P, xparts, wparts, bytes;
 };
-// Large tiles where they fill half of the CUs at least.
-static int tile_edge(int64_t m, int64_t n) { return up(m, 256) / 256 * (up(n, 256) / 256) >= 128 ? 256 : 128; }
 static XentLayout xent_layout(const void *w, int64_t ldw, int64_t rows, int64_t d, int64_t vocab, int dtype, bool grad) {
     XentLayout l = {};
     l.split = dtype == IMUNPACK_F32;
     const int64_t numbers = l.split ? 2 : 1;
+    l.places = l.split ? kPlaces<true> : kPlaces<false>;
     l.dp = up(d, kStageCols);
     l.tp = up(std::max<int64_t>(rows, 1), 256);
     l.vp = up(vocab, 256);
-    l.direct = !l.split && d % kStageCols == 0 && ldw % 8 == 0 && (size_t)w % 16 == 0;
-    l.edge_l = tile_edge(vocab, rows);
-    l.edge_g = rows * d * vocab >= 1ll << 33 ? 256 : 128;
-    l.parts_v = (int)(2 * (up(vocab, l.edge_l) / l.edge_l));
+    l.direct = !l.split && d % 8 == 0 && ldw % 8 == 0 && ldw <= 1 << 22 && (size_t)w % 16 == 0;  // (a tile's rows lie within 32 bits)
     l.room = !grad ? l.tp : std::min(l.tp, std::max<int64_t>(256, kPieceBytes / (2 * numbers * l.vp) / 256 * 256));
     l.pieces = (l.tp + l.room - 1) / l.room;
+    l.edge_l = logits_edge((int)std::min(rows, l.room), (int)d, (int)vocab);
+    l.edge_g = grads_edge((int)std::min(rows, l.room), (int)d, (int)vocab);
     size_t at = sizeof(XentHeader);
     auto take = [&](int64_t bytes) { const size_t here = at; at = (at + (size_t)bytes + 255) & ~(size_t)255; return here; };
     l.source = take(rows * 4); l.place = take(rows * 4); l.wanted = take(rows * 4);
     l.lse = take(rows * 4); l.row_loss = take(rows * 4); l.hit = take(rows * 4); l.g = take(rows * 4);
-    l.stats = take((int64_t)l.parts_v * l.room * 8);
-    l.pitch_p = l.dp * 2;
-    l.px2 = (size_t)(l.tp * l.pitch_p);
-    l.px = take((int64_t)l.px2 * numbers);
-    l.pw2 = (size_t)up(vocab * l.pitch_p, 256);
-    l.pw = take(l.direct ? 0 : (int64_t)l.pw2 * numbers);
+    // (a wave to a row: 1418 x 1031 by 32003 rows 83 -> 60 us for both passes over the operands, but 64 x 85 by 16360 10 -> 16)
+    l.by_rows = l.split && !grad && d >= 512;
+    l.ex = take(grad ? 0 : rows * 4); l.ew = take(grad ? 0 : l.vp * 4);
+    l.stats = take(2 * (up(vocab, 128) / 128) * l.room * 8);  // (two parts to a tile)
+    l.pitch_p = l.dp * 2 * numbers;
+    l.px = take(l.tp * l.pitch_p);
+    l.pw = take(l.direct ? 0 : vocab * l.pitch_p);
     if (grad) {
-        l.pitch_P = l.vp * 2;
-        l.P2 = (size_t)(l.room * l.pitch_P);
-        l.P = take((int64_t)l.P2 * numbers);
-        const int64_t edge = l.edge_g, xtiles = up(l.room, edge) / edge * (up(d, edge) / edge), wtiles = up(vocab, edge) / edge * (up(d, edge) / edge);
-        l.xslots = (int)std::max<int64_t>(xtiles, kXentSlots);
-        const int64_t able = std::max<int64_t>(1, up(vocab, kStageCols) / kStageCols / kPartTiles);  // (as parts_of; a multiple of the XCDs)
-        l.xgroups = (int)up(std::max(xtiles, std::min<int64_t>(l.xslots, xtiles * able)), 8);
-        l.wcut = l.pieces == 1 && wtiles <= kXentSlots / 2 ? parts_of((int)wtiles, kXentSlots, (int)(up(rows, kStageCols) / kStageCols)) : 1;
-        l.through = l.wcut > 1 || l.pieces > 1;
-        l.xparts = take((int64_t)l.xgroups * edge * edge * 4);
-        l.wparts = take(l.through ? l.wcut * wtiles * edge * edge * 4 : 0);
+        l.pitch_P = l.vp * 2 * numbers;
+        l.P = take(l.room * l.pitch_P);
+        int64_t xbytes = 0, wbytes = 0;
+        for (int64_t edge = 128; edge <= l.edge_g; edge *= 2) {
+            Cut &c = l.cut[edge / 256];
+            const int64_t xtiles = up(l.room, edge) / edge * (up(d, edge) / edge), wtiles = up(vocab, edge) / edge * (up(d, edge) / edge);
+            c.xslots = (int)std::max<int64_t>(xtiles, kXentSlots);
+            const int64_t able = std::max<int64_t>(1, up(vocab, l.places) / l.places / kPartTiles);  // (as parts_of; a multiple of the XCDs)
+            c.xgroups = (int)up(std::max(xtiles, std::min<int64_t>(c.xslots, xtiles * able)), 8);
+            c.wcut = l.pieces == 1 && wtiles <= kXentSlots / 2 ? parts_of((int)wtiles, kXentSlots, (int)(up(rows, l.places) / l.places)) : 1;
+            c.through = c.wcut > 1 || l.pieces > 1;
+            xbytes = std::max(xbytes, (int64_t)c.xgroups * edge * edge * 4);
+            wbytes = std::max(wbytes, c.through ? c.wcut * wtiles * edge * edge * 4 : 0);
+        }
+        l.xparts = take(xbytes);
+        l.wparts = take(wbytes);
     }
     l.bytes = at;
     return l;
@@ -703,20 +830,29 @@ static void launch_logits(const LogitArgs &a, bool keep, unsigned groups, hipStr
 }
 template <bool F16>
 static void launch_logits(const LogitArgs &a, int edge, bool keep, int64_t rows, hipStream_t st) {
-    const unsigned groups = (unsigned)(up(a.w.rows, edge) / edge * (up(rows, edge) / edge));
-    if (edge == 256) launch_logits<F16, 4, 2>(a, keep, groups, st);
-    else if (groups > kCus) launch_logits<F16, 2, 2>(a, keep, groups, st);
-    else launch_logits<F16, 2, 4>(a, keep, groups, st);
+    auto groups = [&](int64_t edge) { return (unsigned)(up(a.w.rows, edge) / edge * (up(rows, edge) / edge)); };
+    if (edge == 256) {  // (a workgroup that finds nothing to do takes its time too: no more of them than would have something)
+        launch_logits<F16, 4, 2>(a, keep, groups(256), st);
+        if (logits_edge(kLargeRows, a.d, a.w.rows) == 256) rows = std::min<int64_t>(rows, kLargeRows);
+    }
+    if (groups(128) > kCus) launch_logits<F16, 2, 2>(a, keep, groups(128), st);
+    else launch_logits<F16, 2, 4>(a, keep, groups(128), st);
 }
 template <bool F16, int T, int DEPTH>
 static void launch_grads(const GradArgs &a, unsigned groups, hipStream_t st) {
     hipLaunchKernelGGL((xent_grads_kernel<F16, T, DEPTH>), dim3(groups), dim3(kProductThreads), product_lds(T, T, DEPTH), st, a);
 }
 template <bool F16>
-static void launch_grads(const GradArgs &a, int edge, unsigned groups, hipStream_t st) {
-    if (edge == 256) launch_grads<F16, 4, 2>(a, groups, st);
-    else if (groups > kCus) launch_grads<F16, 2, 2>(a, groups, st);
-    else launch_grads<F16, 2, 4>(a, groups, st);
+static void launch_grads(GradArgs a, const XentLayout &l, bool x, bool w, hipStream_t st) {
+    for (int edge = l.edge_g; edge >= 128; edge /= 2) {
+        a.cut = l.cut[edge / 256];
+        if (!x) a.cut.xgroups = 0;
+        const unsigned groups = (unsigned)(a.cut.xgroups + (w ? up(a.w.rows, edge) / edge * (up(a.d, edge) / edge) * a.cut.wcut : 0));
+        if (groups == 0) continue;
+        if (edge == 256) launch_grads<F16, 4, 2>(a, groups, st);
+        else if (groups > kCus) launch_grads<F16, 2, 2>(a, groups, st);
+        else launch_grads<F16, 2, 4>(a, groups, st);
+    }
 }
 }  // namespace imu
 
@@ -750,18 +886,24 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
     // (workgroups of 16 waves, a wave to four rows)
     const int nx = (int)std::min<int64_t>(up(rows, 64) / 64, kScanX), nw = (int)std::min<int64_t>(up(vocab, 64) / 64, kScanGroups - kScanX);
     c.nx = nx;
-    hipLaunchKernelGGL(xent_scan_kernel, dim3(l.split && rows > 0 ? 1 + nx + nw : 1), dim3(1024), 0, st, c);
+    hipLaunchKernelGGL(xent_scan_kernel, dim3(l.split && !l.by_rows && rows > 0 ? 1 + nx + nw : 1), dim3(1024), 0, st, c);
     Upstream upstream = {grad, nullptr, reduction == IMUNPACK_MEAN};
     if (back && reduction == IMUNPACK_NONE) {
         upstream.g = (const float *)(s + l.g);
         hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, grad, hdr, source, (float *)(s + l.g));
     }
-    if (rows > 0) {
+    if (rows > 0 && l.by_rows) {
+        PrepareRowsArgs p = {};
+        p.x = (const float *)x; p.w = (const float *)w; p.ldx = ldx; p.ldw = ldw; p.hdr = hdr; p.source = source;
+        p.px = s + l.px; p.pw = s + l.pw; p.pitch = l.pitch_p; p.wrows = vocab;
+        p.ex = (int32_t *)(s + l.ex); p.ew = (int32_t *)(s + l.ew); p.d = (int)d; p.xgroups = (int)(up(rows, 4) / 4);
+        hipLaunchKernelGGL(xent_prepare_rows_kernel, dim3((unsigned)(p.xgroups + up(vocab, 4) / 4)), dim3(256), 0, st, p);
+    } else if (rows > 0) {
         PrepareArgs p = {};
         p.x = x; p.w = w; p.ldx = ldx; p.ldw = ldw; p.hdr = hdr; p.source = source;
-        p.px = s + l.px; p.px2 = l.px2;
-        p.pw = s + l.pw; p.pw2 = l.pw2;
+        p.px = s + l.px; p.pw = s + l.pw;
         p.xrows = l.tp; p.wrows = l.direct ? 0 : vocab; p.d = (int)d; p.pieces = (int)(l.dp / 8); p.nx = nx; p.nw = nw;
+        p.ex = back ? nullptr : (int32_t *)(s + l.ex); p.ew = (int32_t *)(s + l.ew);
         const int64_t per = 256 * kPrepareTurns;
         p.xgroups = (int)((up(rows, kStageCols) * p.pieces + per - 1) / per);
         const dim3 grid((unsigned)(p.xgroups + (p.wrows * p.pieces + per - 1) / per));
@@ -770,19 +912,21 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
     }
     for (int64_t piece = 0; piece < l.pieces; ++piece) {
         const int64_t first = piece * l.room, n = std::min(l.room, rows - first);  // rows of the piece at most
-        const Operand whole = {l.direct ? (const char *)w : s + l.pw, l.direct ? ldw * 2 : l.pitch_p, (int64_t)l.pw2, (int)vocab, (int)d};
-        const Operand part = {s + l.px + first * l.pitch_p, l.pitch_p, (int64_t)l.px2, 0, (int)d};
+        const int held = (int)(l.pitch_p / 2);  // (zeros behind the features)
+        const Operand whole = {l.direct ? (const char *)w : s + l.pw, l.direct ? ldw * 2 : l.pitch_p, (int)vocab, l.direct ? (int)d : held};
+        const Operand part = {s + l.px + first * l.pitch_p, l.pitch_p, 0, held};
         if (n > 0) {
             LogitArgs a = {};
             a.w = whole; a.x = part;
+            a.ex = (const int32_t *)(s + l.ex); a.ew = (const int32_t *)(s + l.ew);
             a.hdr = hdr; a.wanted = wanted; a.stats = (float *)(s + l.stats); a.hit = (float *)(s + l.hit);
-            a.P = s + l.P; a.P2 = l.P2; a.pitch_P = l.pitch_P;
-            a.first = (int)first; a.room = (int)l.room; a.ktiles = (int)(l.dp / kStageCols);
+            a.P = s + l.P; a.pitch_P = l.pitch_P;
+            a.first = (int)first; a.room = (int)l.room; a.d = (int)d; a.ktiles = (int)(up(d, l.places) / l.places);
             l.split ? launch_logits<true>(a, l.edge_l, back, n, st) : launch_logits<false>(a, l.edge_l, back, n, st);
         }
         if (n > 0 || (loss && reduction != IMUNPACK_NONE)) {
             JoinArgs j = {};
-            j.stats = (const float *)(s + l.stats); j.hit = (const float *)(s + l.hit); j.parts = l.parts_v; j.first = (int)first; j.room = (int)l.room;
+            j.stats = (const float *)(s + l.stats); j.hit = (const float *)(s + l.hit); j.d = (int)d; j.vocab = (int)vocab; j.first = (int)first; j.room = (int)l.room;
             j.how = loss ? reduction : IMUNPACK_NONE;
             j.hdr = hdr; j.source = source; j.lse = (float *)(s + l.lse); j.row_loss = (float *)(s + l.row_loss); j.loss = loss;
             hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)(up(std::max<int64_t>(n, 1), kJoinRows) / kJoinRows)), dim3(256), 0, st, j);
@@ -791,32 +935,33 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
         if (n > 0) {
             TurnArgs t = {};
             t.hdr = hdr; t.wanted = wanted; t.stats = (const float *)(s + l.stats); t.lse = (const float *)(s + l.lse); t.up = upstream;
-            t.P = s + l.P; t.P2 = l.P2; t.pitch_P = l.pitch_P;
-            t.first = (int)first; t.room = (int)l.room; t.vocab = (int)vocab; t.part = l.edge_l / 2;
-            const dim3 grid((unsigned)(up(vocab, 256) / 256), (unsigned)(up(n, kStageCols) / kTurnRows));
-            if (l.split) hipLaunchKernelGGL(xent_turn_kernel<true>, grid, dim3(256), 0, st, t);
-            else hipLaunchKernelGGL(xent_turn_kernel<false>, grid, dim3(256), 0, st, t);
+            t.P = s + l.P; t.pitch_P = l.pitch_P;
+            t.first = (int)first; t.room = (int)l.room; t.d = (int)d; t.vocab = (int)vocab;
+            const unsigned across = (unsigned)(up(vocab, 256) / 256), down = (unsigned)up(n, kStageCols);
+            const bool few = across * down / 32 < 4 * kCus;  // (a workgroup to 32 rows, or where those are few to eight)
+            const dim3 grid(across, down / (few ? 8 : 32));
+            if (l.split) hipLaunchKernelGGL((few ? xent_turn_kernel<true, 8> : xent_turn_kernel<true, 32>), grid, dim3(256), 0, st, t);
+            else hipLaunchKernelGGL((few ? xent_turn_kernel<false, 8> : xent_turn_kernel<false, 32>), grid, dim3(256), 0, st, t);
         }
         GradArgs a = {};
-        a.G = {s + l.P, l.pitch_P, (int64_t)l.P2, 0, (int)vocab};
+        a.G = {s + l.P, l.pitch_P, 0, (int)(l.pitch_P / 2)};
         a.w = whole; a.x = part;
         a.hdr = hdr; a.up = upstream; a.xparts = (float *)(s + l.xparts); a.wparts = (float *)(s + l.wparts);
-        a.gw = gw; a.ldgw = ldgw; a.ktiles = (int)(up(vocab, kStageCols) / kStageCols);
-        a.xslots = l.xslots; a.xgroups = gx && n > 0 ? l.xgroups : 0; a.wcut = l.wcut; a.through = l.through; a.first = (int)first; a.room = (int)l.room;
-        const int64_t edge = l.edge_g, wgroups = gw ? up(vocab, edge) / edge * (up(d, edge) / edge) * l.wcut : 0;
-        const unsigned groups = (unsigned)(a.xgroups + wgroups);
-        if (groups > 0) {
-            l.split ? launch_grads<true>(a, l.edge_g, groups, st) : launch_grads<false>(a, l.edge_g, groups, st);
-        }
+        a.gw = gw; a.ldgw = ldgw; a.d = (int)d; a.ktiles = (int)(up(vocab, l.places) / l.places);
+        a.first = (int)first; a.room = (int)l.room;
+        l.split ? launch_grads<true>(a, l, gx && n > 0, gw, st) : launch_grads<false>(a, l, gx && n > 0, gw, st);
         FoldArgs f = {};
         f.xparts = a.xparts; f.wparts = a.wparts; f.hdr = hdr; f.up = upstream; f.place = place;
-        f.gx = gx; f.gw = gw; f.ldgx = ldgx; f.ldgw = ldgw;
-        f.xrows = a.xgroups ? rows : 0; f.wrows = gw && l.through && piece + 1 == l.pieces ? vocab : 0;
-        f.d = (int)d; f.edge = l.edge_g; f.ktiles = a.ktiles; f.xslots = l.xslots; f.wcut = l.wcut; f.first = a.first; f.room = a.room;
+        f.gx = gx; f.gw = gw; f.ldgx = ldgx; f.ldgw = ldgw; f.cut[0] = l.cut[0]; f.cut[1] = l.cut[1];
+        f.xrows = gx && n > 0 ? rows : 0; f.wrows = gw && (l.cut[0].through || l.cut[1].through) && piece + 1 == l.pieces ? vocab : 0;
+        f.d = (int)d; f.vocab = (int)vocab; f.ktiles = a.ktiles; f.first = a.first; f.room = a.room;
         if (f.xrows + f.wrows > 0) {
-            const dim3 grid((unsigned)(f.xrows + f.wrows), (unsigned)(up(d, 1024) / 1024));
-            if (l.split) hipLaunchKernelGGL(xent_fold_kernel<float>, grid, dim3(256), 0, st, f);
-            else hipLaunchKernelGGL(xent_fold_kernel<__bf16>, grid, dim3(256), 0, st, f);
+            const int64_t xtiles = up(std::min(rows, l.room), 128) / 128 * (up(d, 128) / 128);
+            const bool many = std::max(f.wrows > 0 ? l.cut[0].wcut : 0, f.xrows > 0 ? parts_of((int)xtiles, l.cut[0].xslots, a.ktiles) : 0) >= 8;
+            const int64_t each = many ? 1 : 4;
+            const dim3 grid((unsigned)(up(f.xrows, each) / each + up(f.wrows, each) / each), (unsigned)(up(d, 256) / 256));
+            if (l.split) hipLaunchKernelGGL((many ? xent_fold_kernel<float, 1> : xent_fold_kernel<float, 4>), grid, dim3(256), 0, st, f);
+            else hipLaunchKernelGGL((many ? xent_fold_kernel<__bf16, 1> : xent_fold_kernel<__bf16, 4>), grid, dim3(256), 0, st, f);
         }
     }
     return launch_status();

@@ -141,6 +141,39 @@ def test_pieces_of_the_rows(imu, dtype, share):
     assert abs(float(one) - float(got.to(F).sum())) <= (rows / 256 + 20) * U * float(got.sum())
 
 
+# rows with a target: large tiles in all products, in the logits alone, and in none although there is room for them
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("share", [1.0, 0.75, 0.3])
+def test_large_tiles(imu, dtype, share):
+    x, w, target, grad = inputs(1700, 520, 16500, dtype, share, 17)
+    valid, loss, gx, gw = reference(x, w, target, grad, dtype)
+    got, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+    a, b = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    within(got, loss)
+    within(a, gx)
+    within(b, gw)
+    alone, _ = imu.imunpack_xent(x, w, target, reduction="none")
+    within(alone, loss)
+    again = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    assert torch.equal(again[0], a) and torch.equal(again[1], b)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("share", [1.0, 0.3])
+def test_pieces_of_the_rows_in_large_tiles(imu, dtype, share):
+    rows, d, vocab = (4300, 130, 66000) if dtype == torch.float32 else (8500, 130, 66000)
+    x, w, target, grad = inputs(rows, d, vocab, dtype, share, 4)
+    got, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+    a, b = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    for part in range(0, rows, 1024):
+        r = slice(part, part + 1024)
+        _, loss, gx, gw = reference(x[r], w, target[r], grad[r], dtype)
+        within(got[r], loss)
+        within(a[r], gx)
+        total = gw if part == 0 else (total[0] + gw[0], total[1] + gw[1])
+    within(b, (total[0], total[1] + sums(rows, dtype) * total[0].abs()))
+
+
 def test_nothing_to_learn_from_and_targets_outside(imu):
     x, w, target, grad = inputs(70, 96, 150, torch.float32, 1.0, 5)
     none = torch.full_like(target, -100)
