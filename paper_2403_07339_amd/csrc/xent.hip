@@ -29,6 +29,7 @@ constexpr int kXentSlots = 256;             // parts of the tiles of a gradient 
 constexpr int kPartTiles = 2;               // k-tiles of a part at least: below that its sums cost more than its products
 constexpr int kScanGroups = 512, kScanX = 64;  // workgroups that look for the largest magnitudes, those of x first
 constexpr int kJoinRows = 8;
+constexpr int64_t kJoinVocab = 8192;        // the parts of a row up to which a load of each thread has them all
 constexpr int kLargeRows = 1024;            // rows from which the logits may go in large tiles
 
 struct XentHeader {
@@ -427,14 +428,13 @@ struct JoinArgs {
     const int32_t *source;
     float *lse, *row_loss, *loss;
 };
-// lse and loss of eight rows from the parts of the vocabulary, 32 threads to a row.  Where one value is wanted, the workgroup that comes last
-// adds the rows' losses, in a fixed order.
-__global__ __launch_bounds__(256) void xent_join_kernel(const JoinArgs a) {
-    __shared__ float tops[32][kJoinRows], sums[32][kJoinRows], lds[4];
-    __shared__ int last;
-    const int r = threadIdx.x % kJoinRows, g = threadIdx.x / kJoinRows, at = blockIdx.x * kJoinRows + r, t = a.first + at, count = a.hdr->count;
-    const int groups = max(1, (count + kJoinRows - 1) / kJoinRows);  // of all pieces
-    if ((int)blockIdx.x + a.first / kJoinRows >= groups) return;
+struct JoinShared {
+    float tops[32][kJoinRows], sums[32][kJoinRows], lds[4];
+    int last;
+};
+// lse of eight rows from the parts of the vocabulary, 32 threads to a row, in the first of them.
+__device__ __forceinline__ float join_rows(const JoinArgs &a, int group, JoinShared &sh) {
+    const int r = threadIdx.x % kJoinRows, g = threadIdx.x / kJoinRows, at = group * kJoinRows + r, t = a.first + at, count = a.hdr->count;
     const int edge = logits_edge(rows_at_most(a.hdr, a.room), a.d, a.vocab), parts = (a.vocab + edge - 1) / edge * 2;
     float top = -__builtin_inff(), sum = 0.0f;
     if (t < count)
@@ -451,31 +451,45 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const JoinArgs a) {
                 top = next;
             }
         }
-    tops[g][r] = top;
-    sums[g][r] = sum;
+    sh.tops[g][r] = top;
+    sh.sums[g][r] = sum;
     __syncthreads();
-    if (g == 0 && t < count) {
+    if (g > 0 || t >= count) return 0.0f;
 #pragma unroll
-        for (int k = 1; k < 32; ++k) top = fmaxf(top, tops[k][r]);
-        sum = 0.0f;
-        const float from = top == -__builtin_inff() ? 0.0f : top;
+    for (int k = 1; k < 32; ++k) top = fmaxf(top, sh.tops[k][r]);
+    sum = 0.0f;
+    const float from = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
-        for (int k = 0; k < 32; ++k) sum += sums[k][r] * fast_exp(tops[k][r] - from);
-        const float l = from + logf(sum), v = l - a.hit[t];
-        a.lse[t] = l;
+    for (int k = 0; k < 32; ++k) sum += sh.sums[k][r] * fast_exp(sh.tops[k][r] - from);
+    return from + logf(sum);
+}
+// Their losses.  Where one value is wanted, the workgroup that comes last adds the rows' losses, in a fixed order.
+__device__ __forceinline__ void rows_losses(const JoinArgs &a, int group, float lse, JoinShared &sh) {
+    const int t = a.first + group * kJoinRows + (int)threadIdx.x, count = a.hdr->count;
+    const int groups = max(1, (count + kJoinRows - 1) / kJoinRows);  // of all pieces
+    if (threadIdx.x < kJoinRows && t < count) {
+        const float v = lse - a.hit[t];
         __hip_atomic_store(a.row_loss + t, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // (past this XCD's cache: no fence has to write it back)
         if (a.how == IMUNPACK_NONE && a.loss) a.loss[a.source[t]] = v;
     }
     if (a.how == IMUNPACK_NONE) return;
     stores_done();
     __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(&a.hdr->joined, 1u) == (unsigned)groups - 1;
+    if (threadIdx.x == 0) sh.last = atomicAdd(&a.hdr->joined, 1u) == (unsigned)groups - 1;
     __syncthreads();
-    if (!last) return;
+    if (!sh.last) return;
     float s = 0.0f;
     for (int k = threadIdx.x; k < count; k += 256) s += __hip_atomic_load(a.row_loss + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s = reduce_threads<256, false>(s, lds);
+    s = reduce_threads<256, false>(s, sh.lds);
     if (threadIdx.x == 0) *a.loss = a.hdr->bad ? __builtin_nanf("") : a.how == IMUNPACK_MEAN && count > 0 ? s / (float)count : s;
+}
+__global__ __launch_bounds__(256) void xent_join_kernel(const JoinArgs a) {
+    __shared__ JoinShared sh;
+    const int count = a.hdr->count, t = a.first + blockIdx.x * kJoinRows + threadIdx.x;
+    if ((int)blockIdx.x + a.first / kJoinRows >= max(1, (count + kJoinRows - 1) / kJoinRows)) return;
+    const float l = join_rows(a, blockIdx.x, sh);
+    if (threadIdx.x < kJoinRows && t < count) a.lse[t] = l;
+    rows_losses(a, blockIdx.x, l, sh);
 }
 
 // Factors and exponent of the rows' own gradients.
@@ -491,43 +505,55 @@ __global__ __launch_bounds__(1024) void xent_factor_kernel(const float *grad, Xe
 }
 
 struct TurnArgs {
-    const XentHeader *hdr;
+    JoinArgs join;
     const int32_t *wanted;
-    const float *stats, *lse;
     Upstream up;
     char *P;
     int64_t pitch_P;
-    int first, room, d, vocab;
 };
 // Exponentials become G where they lie, 256 columns of ROWS rows to a workgroup, eight columns to a lane: zeros behind the vocabulary and, to a
-// whole k-tile, behind the last row.
-template <bool F16, int ROWS>
+// whole k-tile, behind the last row.  32 rows, or eight where that leaves CUs without a workgroup; JOIN: those join the parts of their rows
+// themselves, as the kernel above does (200 x 256 by 1000 fp32, forward and backward: TURNUS).
+template <bool F16, int ROWS, bool JOIN>
 __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
-    const int rows = rows_of(a.hdr, a.first, a.room), last = (rows + kStageCols - 1) / kStageCols * kStageCols;
-    const int row0 = blockIdx.y * ROWS + (threadIdx.x >> 5), v0 = blockIdx.x * 256 + (threadIdx.x & 31) * 8, left = a.vocab - v0;
-    if ((int)blockIdx.y * ROWS >= last || v0 >= (a.vocab + kStageCols - 1) / kStageCols * kStageCols) return;
-    const float all = a.up.g ? 0.0f : a.up.one(a.hdr);
-    const int part = v0 / (logits_edge(rows_at_most(a.hdr, a.room), a.d, a.vocab) / 2);  // whose columns share a largest logit
+    static_assert(!JOIN || ROWS == kJoinRows, "the rows of a workgroup");
+    const JoinArgs &j = a.join;
+    const int rows = rows_of(j.hdr, j.first, j.room), last = (rows + kStageCols - 1) / kStageCols * kStageCols;
+    const int row0 = blockIdx.y * ROWS + (threadIdx.x >> 5), v0 = blockIdx.x * 256 + (threadIdx.x & 31) * 8, left = j.vocab - v0;
+    const bool losses = JOIN && blockIdx.x == 0 && (int)blockIdx.y < max(1, (rows + ROWS - 1) / ROWS);
+    if ((int)blockIdx.y * ROWS >= last && !losses) return;
+    if (!JOIN && v0 >= (j.vocab + kStageCols - 1) / kStageCols * kStageCols) return;
+    const float all = a.up.g ? 0.0f : a.up.one(j.hdr);
+    const int part = v0 / (logits_edge(rows_at_most(j.hdr, j.room), j.d, j.vocab) / 2);  // whose columns share a largest logit
     constexpr int kTurns = ROWS / 8;
     v4i32 hi[kTurns], lo[kTurns];
     char *const p0 = a.P + byte_of<F16>(v0);
+    const int end = JOIN && v0 >= (j.vocab + kStageCols - 1) / kStageCols * kStageCols ? 0 : last, some = min(rows, end);  // rows of this lane's columns
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const int t = row0 + 8 * i;
-        if (t >= rows) continue;
+        if (t >= some) continue;
         hi[i] = *reinterpret_cast<const v4i32 *>(p0 + t * a.pitch_P);
         if (F16) lo[i] = *reinterpret_cast<const v4i32 *>(p0 + t * a.pitch_P + kSecond);
+    }
+    __shared__ JoinShared sh;
+    __shared__ float lse[kJoinRows];
+    float own_lse = 0.0f;
+    if constexpr (JOIN) {
+        own_lse = join_rows(j, blockIdx.y, sh);
+        if (threadIdx.x < kJoinRows) lse[threadIdx.x] = own_lse;
+        __syncthreads();
     }
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const int t = row0 + 8 * i;
-        if (t >= last) continue;
+        if (t >= end) continue;
         uint32_t qh[4] = {0, 0, 0, 0}, ql[4] = {0, 0, 0, 0};
         if (t < rows) {
-            const float top = a.stats[((int64_t)part * a.room + t) * 2];
-            const float g = a.up.g ? a.up.g[a.first + t] : all;
-            const float down = __builtin_amdgcn_exp2f((top - a.lse[a.first + t]) * kLog2e) * g, one = F16 ? g * power_of_two(kTop) : g;
-            const int own = a.wanted[a.first + t] - v0;
+            const float top = j.stats[((int64_t)part * j.room + t) * 2];
+            const float g = a.up.g ? a.up.g[j.first + t] : all, l = JOIN ? lse[threadIdx.x >> 5] : j.lse[j.first + t];
+            const float down = __builtin_amdgcn_exp2f((top - l) * kLog2e) * g, one = F16 ? g * power_of_two(kTop) : g;
+            const int own = a.wanted[j.first + t] - v0;
             float v[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -550,6 +576,8 @@ __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
         *reinterpret_cast<v4i32 *>(p0 + t * a.pitch_P) = v4i32{(int)qh[0], (int)qh[1], (int)qh[2], (int)qh[3]};
         if (F16) *reinterpret_cast<v4i32 *>(p0 + t * a.pitch_P + kSecond) = v4i32{(int)ql[0], (int)ql[1], (int)ql[2], (int)ql[3]};
     }
+    if constexpr (JOIN)
+        if (losses) rows_losses(j, blockIdx.y, own_lse, sh);
 }
 
 // Into how many parts the tiles of a gradient are cut along the contraction, so that every CU has one.
@@ -924,24 +952,21 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
             a.first = (int)first; a.room = (int)l.room; a.d = (int)d; a.ktiles = (int)(up(d, l.places) / l.places);
             l.split ? launch_logits<true>(a, l.edge_l, back, n, st) : launch_logits<false>(a, l.edge_l, back, n, st);
         }
-        if (n > 0 || (loss && reduction != IMUNPACK_NONE)) {
-            JoinArgs j = {};
-            j.stats = (const float *)(s + l.stats); j.hit = (const float *)(s + l.hit); j.d = (int)d; j.vocab = (int)vocab; j.first = (int)first; j.room = (int)l.room;
-            j.how = loss ? reduction : IMUNPACK_NONE;
-            j.hdr = hdr; j.source = source; j.lse = (float *)(s + l.lse); j.row_loss = (float *)(s + l.row_loss); j.loss = loss;
+        const unsigned across = (unsigned)(up(vocab, 256) / 256), down = (unsigned)up(n, kStageCols);
+        const bool few = across * down / 32 < 4 * kCus, joins = back && n > 0 && few && l.pieces == 1 && vocab <= kJoinVocab;
+        JoinArgs j = {};
+        j.stats = (const float *)(s + l.stats); j.hit = (const float *)(s + l.hit); j.d = (int)d; j.vocab = (int)vocab; j.first = (int)first; j.room = (int)l.room;
+        j.how = loss ? reduction : IMUNPACK_NONE;
+        j.hdr = hdr; j.source = source; j.lse = (float *)(s + l.lse); j.row_loss = (float *)(s + l.row_loss); j.loss = loss;
+        if (!joins && (n > 0 || (loss && reduction != IMUNPACK_NONE)))
             hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)(up(std::max<int64_t>(n, 1), kJoinRows) / kJoinRows)), dim3(256), 0, st, j);
-        }
         if (!back) continue;
         if (n > 0) {
             TurnArgs t = {};
-            t.hdr = hdr; t.wanted = wanted; t.stats = (const float *)(s + l.stats); t.lse = (const float *)(s + l.lse); t.up = upstream;
-            t.P = s + l.P; t.pitch_P = l.pitch_P;
-            t.first = (int)first; t.room = (int)l.room; t.d = (int)d; t.vocab = (int)vocab;
-            const unsigned across = (unsigned)(up(vocab, 256) / 256), down = (unsigned)up(n, kStageCols);
-            const bool few = across * down / 32 < 4 * kCus;  // (a workgroup to 32 rows, or where those are few to eight)
+            t.join = j; t.wanted = wanted; t.up = upstream; t.P = s + l.P; t.pitch_P = l.pitch_P;
             const dim3 grid(across, down / (few ? 8 : 32));
-            if (l.split) hipLaunchKernelGGL((few ? xent_turn_kernel<true, 8> : xent_turn_kernel<true, 32>), grid, dim3(256), 0, st, t);
-            else hipLaunchKernelGGL((few ? xent_turn_kernel<false, 8> : xent_turn_kernel<false, 32>), grid, dim3(256), 0, st, t);
+            if (l.split) hipLaunchKernelGGL((joins ? xent_turn_kernel<true, 8, true> : few ? xent_turn_kernel<true, 8, false> : xent_turn_kernel<true, 32, false>), grid, dim3(256), 0, st, t);
+            else hipLaunchKernelGGL((joins ? xent_turn_kernel<false, 8, true> : few ? xent_turn_kernel<false, 8, false> : xent_turn_kernel<false, 32, false>), grid, dim3(256), 0, st, t);
         }
         GradArgs a = {};
         a.G = {s + l.P, l.pitch_P, 0, (int)(l.pitch_P / 2)};
