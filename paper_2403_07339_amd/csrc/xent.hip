@@ -98,19 +98,10 @@ __device__ __forceinline__ float largest(const ScanArgs &a, const float *m, int6
     return top;
 }
 
-// Workgroup 0: rows with a target in order, their targets, and for every row its place among them (-1: none, -2: a target outside the
-// vocabulary).  The others (fp32): the largest magnitudes of x and W.
-__global__ __launch_bounds__(1024) void xent_scan_kernel(const ScanArgs a) {
-    __shared__ int32_t sums[2][16];
-    __shared__ float lds[16];
+// Rows with a target in order (also in `own`), their targets, and for every row its place among them (-1: none, -2: a target outside the
+// vocabulary).  A workgroup of 1024 threads; returns how many there are, to be left by the one that writes.
+__device__ __forceinline__ int scan_rows(const ScanArgs &a, int32_t (*sums)[16], int32_t *own, bool write) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (blockIdx.x > 0) {
-        const int g = blockIdx.x - 1, nx = a.nx;
-        float m = g < nx ? largest<true>(a, a.x, a.ldx, a.rows, g * 16 + wave, nx * 16) : largest<false>(a, a.w, a.ldw, a.vocab, (g - nx) * 16 + wave, ((int)gridDim.x - 1 - nx) * 16);
-        m = reduce_threads<1024, true>(m, lds);
-        if (threadIdx.x == 0) a.hdr->found[g] = __float_as_uint(m);
-        return;
-    }
     int base = 0, bad = 0, turn = 0;
     for (int t0 = 0; t0 < a.rows; t0 += 1024, turn ^= 1) {
         const int t = t0 + threadIdx.x;
@@ -127,22 +118,41 @@ __global__ __launch_bounds__(1024) void xent_scan_kernel(const ScanArgs a) {
             all += sums[turn][w];
         }
         const int at = before + __builtin_popcountll(mask & ((1ull << lane) - 1));
-        if (inside) {
-            a.source[at] = t;
-            a.wanted[at] = (int)v;
-        }
-        if (t < a.rows) {
-            a.place[t] = inside ? at : outside ? -2 : -1;
-            if (a.loss && !inside) a.loss[t] = outside ? __builtin_nanf("") : 0.0f;
+        if (own && inside) own[at] = t;
+        if (write) {
+            if (inside) {
+                a.source[at] = t;
+                a.wanted[at] = (int)v;
+            }
+            if (t < a.rows) {
+                a.place[t] = inside ? at : outside ? -2 : -1;
+                if (a.loss && !inside) a.loss[t] = outside ? __builtin_nanf("") : 0.0f;
+            }
         }
         base += all;
     }
     bad = __syncthreads_or(bad);
-    if (threadIdx.x == 0) {
+    if (write && threadIdx.x == 0) {
         a.hdr->count = base;
         a.hdr->bad = bad;
         a.hdr->joined = 0;
     }
+    return base;
+}
+
+// Workgroup 0: the rows.  The others (fp32): the largest magnitudes of x and W.
+__global__ __launch_bounds__(1024) void xent_scan_kernel(const ScanArgs a) {
+    __shared__ int32_t sums[2][16];
+    __shared__ float lds[16];
+    if (blockIdx.x > 0) {
+        const int wave = threadIdx.x >> 6;
+        const int g = blockIdx.x - 1, nx = a.nx;
+        float m = g < nx ? largest<true>(a, a.x, a.ldx, a.rows, g * 16 + wave, nx * 16) : largest<false>(a, a.w, a.ldw, a.vocab, (g - nx) * 16 + wave, ((int)gridDim.x - 1 - nx) * 16);
+        m = reduce_threads<1024, true>(m, lds);
+        if (threadIdx.x == 0) a.hdr->found[g] = __float_as_uint(m);
+        return;
+    }
+    scan_rows(a, sums, nullptr, true);
 }
 
 template <class E>
@@ -151,6 +161,7 @@ __device__ __forceinline__ uint32_t pack(E a, E b) {
 }
 
 struct PrepareArgs {
+    ScanArgs scan;
     const void *x, *w;
     int64_t ldx, ldw;
     XentHeader *hdr;
@@ -160,16 +171,28 @@ struct PrepareArgs {
     int d, pieces, xgroups, nx, nw;  // workgroups that work on x; nx, nw: workgroups that looked for the largest magnitudes
     int32_t *ex, *ew;         // the loss alone, fp32: what 2 to their power a row of x, of W is multiplied with
 };
-constexpr int kPrepareTurns = 4;
+constexpr int kPrepareTurns = 4, kScanHere = 1024;
 // Eight columns of a row at a time: binary32 as two binary16 numbers, bfloat16 as it is; zeros behind the last column and, to a whole
-// k-tile, behind the last row of x.
-template <class T>
-__global__ __launch_bounds__(256) void xent_prepare_kernel(const PrepareArgs a) {
+// k-tile, behind the last row of x.  SCAN: up to kScanHere rows, among which every workgroup finds those with a target itself (one launch less:
+// 197 x 256 by 1000, loss alone: 21.5 -> 18.3 us).
+template <class T, bool SCAN>
+__global__ __launch_bounds__(SCAN ? 1024 : 256) void xent_prepare_kernel(const PrepareArgs a) {
     constexpr bool SPLIT = sizeof(T) == 4;
+    constexpr int kThreads = SCAN ? 1024 : 256;
     __shared__ float lds[4];
+    __shared__ int32_t sums[2][16], own[SCAN ? kScanHere : 1];
     const bool isX = (int)blockIdx.x < a.xgroups;
     const int group = isX ? blockIdx.x : blockIdx.x - a.xgroups;
-    const int64_t count = isX ? a.hdr->count : a.wrows, rows = isX ? min((count + kStageCols - 1) / kStageCols * kStageCols, a.xrows) : count;
+    int64_t count = a.wrows;
+    if (isX) {
+        if constexpr (SCAN) {
+            count = scan_rows(a.scan, sums, own, group == 0);
+            __syncthreads();
+        } else {
+            count = a.hdr->count;
+        }
+    }
+    const int64_t rows = isX ? min((count + kStageCols - 1) / kStageCols * kStageCols, a.xrows) : count;
     float scale = 1.0f;
     int e = 0;
     if constexpr (SPLIT) {  // the first workgroup of either operand leaves the largest magnitude for the kernels behind
@@ -180,16 +203,16 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(const PrepareArgs a) 
         scale = power_of_two(e);
         if (threadIdx.x == 0 && group == 0) a.hdr->amax[isX ? 0 : 1] = __float_as_uint(m);
     }
-    const int64_t at0 = (int64_t)group * 256 * kPrepareTurns + threadIdx.x;
+    const int64_t at0 = (int64_t)group * kThreads * kPrepareTurns + threadIdx.x;
     int64_t row[kPrepareTurns];
     int col[kPrepareTurns];
     piece_t<T, 4> f[kPrepareTurns][2];
 #pragma unroll
     for (int i = 0; i < kPrepareTurns; ++i) {
-        const int64_t at = at0 + 256 * i;
+        const int64_t at = at0 + kThreads * i;
         row[i] = at / a.pieces;
         col[i] = (int)(at - row[i] * a.pieces) * 8;
-        const T *p = isX ? (const T *)a.x + (row[i] < count ? (int64_t)a.source[row[i]] : 0) * a.ldx : (const T *)a.w + row[i] * a.ldw;
+        const T *p = isX ? (const T *)a.x + (row[i] < count ? (int64_t)(SCAN ? own[row[i]] : a.source[row[i]]) : 0) * a.ldx : (const T *)a.w + row[i] * a.ldw;
         const int have = row[i] < count ? a.d - col[i] : 0;
 #pragma unroll
         for (int k = 0; k < 2; ++k) f[i][k] = load_piece<T, 4>(p + col[i] + 4 * k, have - 4 * k);
@@ -513,7 +536,7 @@ struct TurnArgs {
 };
 // Exponentials become G where they lie, 256 columns of ROWS rows to a workgroup, eight columns to a lane: zeros behind the vocabulary and, to a
 // whole k-tile, behind the last row.  32 rows, or eight where that leaves CUs without a workgroup; JOIN: those join the parts of their rows
-// themselves, as the kernel above does (200 x 256 by 1000 fp32, forward and backward: TURNUS).
+// themselves, as the kernel above does (200 x 256 by 1000 fp32, forward and backward: 43.3 -> 40.6 us).
 template <bool F16, int ROWS, bool JOIN>
 __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
     static_assert(!JOIN || ROWS == kJoinRows, "the rows of a workgroup");
@@ -914,12 +937,8 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
     // (workgroups of 16 waves, a wave to four rows)
     const int nx = (int)std::min<int64_t>(up(rows, 64) / 64, kScanX), nw = (int)std::min<int64_t>(up(vocab, 64) / 64, kScanGroups - kScanX);
     c.nx = nx;
-    hipLaunchKernelGGL(xent_scan_kernel, dim3(l.split && !l.by_rows && rows > 0 ? 1 + nx + nw : 1), dim3(1024), 0, st, c);
-    Upstream upstream = {grad, nullptr, reduction == IMUNPACK_MEAN};
-    if (back && reduction == IMUNPACK_NONE) {
-        upstream.g = (const float *)(s + l.g);
-        hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, grad, hdr, source, (float *)(s + l.g));
-    }
+    const bool scans = !l.split && rows > 0 && rows <= kScanHere;  // the kernel that gathers x does it
+    if (!scans) hipLaunchKernelGGL(xent_scan_kernel, dim3(l.split && !l.by_rows && rows > 0 ? 1 + nx + nw : 1), dim3(1024), 0, st, c);
     if (rows > 0 && l.by_rows) {
         PrepareRowsArgs p = {};
         p.x = (const float *)x; p.w = (const float *)w; p.ldx = ldx; p.ldw = ldw; p.hdr = hdr; p.source = source;
@@ -928,15 +947,21 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
         hipLaunchKernelGGL(xent_prepare_rows_kernel, dim3((unsigned)(p.xgroups + up(vocab, 4) / 4)), dim3(256), 0, st, p);
     } else if (rows > 0) {
         PrepareArgs p = {};
+        p.scan = c;
         p.x = x; p.w = w; p.ldx = ldx; p.ldw = ldw; p.hdr = hdr; p.source = source;
         p.px = s + l.px; p.pw = s + l.pw;
         p.xrows = l.tp; p.wrows = l.direct ? 0 : vocab; p.d = (int)d; p.pieces = (int)(l.dp / 8); p.nx = nx; p.nw = nw;
         p.ex = back ? nullptr : (int32_t *)(s + l.ex); p.ew = (int32_t *)(s + l.ew);
-        const int64_t per = 256 * kPrepareTurns;
+        const int64_t threads = scans ? 1024 : 256, per = threads * kPrepareTurns;
         p.xgroups = (int)((up(rows, kStageCols) * p.pieces + per - 1) / per);
         const dim3 grid((unsigned)(p.xgroups + (p.wrows * p.pieces + per - 1) / per));
-        if (l.split) hipLaunchKernelGGL(xent_prepare_kernel<float>, grid, dim3(256), 0, st, p);
-        else hipLaunchKernelGGL(xent_prepare_kernel<__bf16>, grid, dim3(256), 0, st, p);
+        if (l.split) hipLaunchKernelGGL((xent_prepare_kernel<float, false>), grid, dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((scans ? xent_prepare_kernel<__bf16, true> : xent_prepare_kernel<__bf16, false>), grid, dim3((unsigned)threads), 0, st, p);
+    }
+    Upstream upstream = {grad, nullptr, reduction == IMUNPACK_MEAN};
+    if (back && reduction == IMUNPACK_NONE) {
+        upstream.g = (const float *)(s + l.g);
+        hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, grad, hdr, source, (float *)(s + l.g));
     }
     for (int64_t piece = 0; piece < l.pieces; ++piece) {
         const int64_t first = piece * l.room, n = std::min(l.room, rows - first);  // rows of the piece at most
