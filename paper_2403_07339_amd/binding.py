@@ -572,7 +572,6 @@ def imunpack_price(stats_a: Stats, n: int, stats_b: Stats, h: int, d: int, b: in
 
 
 # ---- around the products: norm, optimiser's step -------------------------------------------------------
-_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 ADAMW_BLOCK = 256
 
 
@@ -586,7 +585,8 @@ class NormSaved:
 
 
 _tensors.bind(ImunpackError, *[C.cast(getattr(_lib, _name), _vp).value for _name in (
-    "imunpack_rmsnorm", "imunpack_rmsnorm_quantize", "imunpack_rmsnorm_backward_workspace", "imunpack_rmsnorm_backward", "imunpack_adamw")])
+    "imunpack_rmsnorm", "imunpack_rmsnorm_quantize", "imunpack_rmsnorm_backward_workspace", "imunpack_rmsnorm_backward", "imunpack_adamw",
+    "imunpack_xent_workspace", "imunpack_xent", "imunpack_xent_rescale")])
 
 
 def imunpack_rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None):
@@ -620,17 +620,6 @@ def imunpack_adamw(params, grads, exp_avg, exp_avg_sq, step: int, lr: float = 1e
     _tensors.adamw(params, grads, exp_avg, exp_avg_sq, m_scales, v_scales, copies, lr, beta1, beta2, eps, weight_decay, step, seed & 0xFFFFFFFF, _stream())
 
 
-def _spread(t: torch.Tensor, d: int):
-    """t as rows of d elements with unit stride, a pitch apart: (tensor, pitch); laid out anew where its strides are others."""
-    if t.is_contiguous():
-        return t, d
-    if t.dim() != 2:
-        t = t.reshape(-1, d)
-    if (t.stride(1) != 1 and d > 1) or (t.shape[0] > 1 and t.stride(0) < d):
-        t = t.contiguous()
-    return t, t.stride(0) if t.shape[0] > 1 else d
-
-
 REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
 
 
@@ -644,32 +633,6 @@ class XentSaved:
     gw: torch.Tensor | None = None
 
 
-def _xent_args(x, w, target):
-    if x.dtype not in _DTYPES or w.dtype != x.dtype or not (x.is_cuda and w.is_cuda):
-        raise ValueError("xent takes x and W as device tensors, both fp32 or both bfloat16")
-    if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
-        raise ValueError(f"x of shape {tuple(x.shape)} and W of shape {tuple(w.shape)} have no product x W^T")
-    if target.dtype != torch.int64 or target.shape != x.shape[:-1] or not target.is_cuda:
-        raise ValueError("target is an int64 device tensor of x's leading shape")
-    return w.shape[1], w.shape[0]
-
-
-def _xent(x, w, target, ignore_index, how, loss, grad, want_x, want_w):
-    """One call of the library: loss (a tensor to fill, or None) and the gradients that are wanted."""
-    d, vocab = _xent_args(x, w, target)
-    x2, ldx = _spread(x, d)
-    w2, ldw = _spread(w, d)
-    target = target.contiguous()
-    rows, dtype, size, at = target.numel(), _DTYPES[x.dtype], _sz(), w2.data_ptr()
-    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_x else None
-    gw = torch.empty(w.shape, dtype=w.dtype, device=x.device) if want_w else None
-    _check(_lib.imunpack_xent_workspace(at, ldw, rows, d, vocab, dtype, want_x or want_w, C.byref(size)), "imunpack_xent_workspace")
-    workspace = torch.empty(size.value, dtype=torch.uint8, device=x.device)
-    _check(_lib.imunpack_xent(x2.data_ptr(), ldx, at, ldw, target.data_ptr(), rows, d, vocab, dtype, ignore_index, how, _ptr(loss), _ptr(grad),
-                              _ptr(gx), d, _ptr(gw), d, workspace.data_ptr(), size.value, _stream()), "imunpack_xent")
-    return gx, gw
-
-
 def imunpack_xent(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, ignore_index: int = -100, reduction: str = "mean", want_grad: bool = False,
                   want_x: bool = True, want_w: bool = True):
     """Softmax cross entropy of x W^T against target (int64, x's leading shape), without keeping the logits.  Returns (loss, saved):
@@ -679,8 +642,7 @@ def imunpack_xent(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, ignore
         raise ValueError("reduction is none, sum or mean")
     how = REDUCTIONS[reduction]
     now = want_grad and how != 0
-    loss = torch.empty(target.shape if how == 0 else (), dtype=torch.float32, device=x.device)
-    gx, gw = _xent(x, w, target, ignore_index, how, loss, None, now and want_x, now and want_w)
+    loss, gx, gw = _tensors.xent(x, w, target, ignore_index, how, True, None, now and want_x, now and want_w, _stream())
     return loss, XentSaved(ignore_index, reduction, gx, gw) if want_grad else None
 
 
@@ -688,15 +650,14 @@ def imunpack_xent_backward(x: torch.Tensor, w: torch.Tensor, target: torch.Tenso
                            want_w: bool = True):
     """Gradients (gx, gw) of imunpack_xent(..., want_grad=True) for grad, the gradient of its loss (fp32); None where not wanted.  The
     first call for one loss hands out what the forward pass made, times grad; another one makes them anew."""
-    _xent_args(x, w, target)
     if grad.dtype != torch.float32 or not grad.is_cuda or grad.numel() != (target.numel() if saved.reduction == "none" else 1):
         raise ValueError("grad is fp32 and shaped like the loss")
     grad = grad.contiguous()
     gx, gw = saved.gx if want_x else None, saved.gw if want_w else None
     if (want_x and gx is None) or (want_w and gw is None):
-        return _xent(x, w, target, saved.ignore_index, REDUCTIONS[saved.reduction], None, grad, want_x, want_w)
+        _, gx, gw = _tensors.xent(x, w, target, saved.ignore_index, REDUCTIONS[saved.reduction], False, grad, want_x, want_w, _stream())
+        return gx, gw
     saved.gx = saved.gw = None
     if want_x or want_w:
-        _check(_lib.imunpack_xent_rescale(grad.data_ptr(), _ptr(gx), gx.numel() if want_x else 0, _ptr(gw), gw.numel() if want_w else 0, _DTYPES[x.dtype],
-                                          _stream()), "imunpack_xent_rescale")
+        _tensors.xent_rescale(x, w, target, grad, gx, gw, _stream())
     return gx, gw

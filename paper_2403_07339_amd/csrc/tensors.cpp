@@ -20,6 +20,9 @@ decltype(&imunpack_rmsnorm_quantize) g_rmsnorm_quantize = nullptr;
 decltype(&imunpack_rmsnorm_backward_workspace) g_rmsnorm_backward_workspace = nullptr;
 decltype(&imunpack_rmsnorm_backward) g_rmsnorm_backward = nullptr;
 decltype(&imunpack_adamw) g_adamw = nullptr;
+decltype(&imunpack_xent_workspace) g_xent_workspace = nullptr;
+decltype(&imunpack_xent) g_xent = nullptr;
+decltype(&imunpack_xent_rescale) g_xent_rescale = nullptr;
 
 struct Refused : std::runtime_error {  // becomes a ValueError
     using std::runtime_error::runtime_error;
@@ -241,6 +244,48 @@ PyObject *adamw(PyObject *const *a) {  // params, grads, exp_avg, exp_avg_sq, m_
 }
 
 // error class, then the addresses of the library's functions
+struct Xent {  // the arguments that the loss and its gradients take, checked
+    at::Tensor x, w, target;
+    int64_t d, vocab, rows;
+    int type;
+};
+Xent xent_arguments(PyObject *const *a) {  // x, w, target
+    Xent n = {tensor(a[0], "xent: x"), tensor(a[1], "xent: W"), tensor(a[2], "xent: target"), 0, 0, 0, 0};
+    n.type = type_of(n.x, "xent: x");
+    need(n.w.scalar_type() == n.x.scalar_type() && n.x.is_cuda() && n.w.is_cuda(), "xent takes x and W as device tensors, both fp32 or both bfloat16");
+    need(n.w.dim() == 2 && n.x.dim() >= 1 && n.x.size(-1) == n.w.size(1), "xent: x and W have no product x W^T");
+    need(n.target.scalar_type() == at::kLong && n.target.is_cuda() && n.target.sizes() == n.x.sizes().slice(0, n.x.dim() - 1), "xent: target is an int64 device tensor of x's leading shape");
+    n.d = n.w.size(1);
+    n.vocab = n.w.size(0);
+    n.rows = n.target.numel();
+    return n;
+}
+// One call of the library: the loss, where it is wanted, and the gradients of x and W that are.
+PyObject *xent(PyObject *const *a) {  // x, w, target, ignore_index, how, want_loss, grad, want_x, want_w, stream -> loss, gx, gw
+    const Xent n = xent_arguments(a);
+    const int how = (int)whole(a[4]);
+    const at::Tensor grad = maybe(a[6], "xent: grad"), target = n.target.contiguous();
+    const Rows x = spread(n.x, n.d), w = spread(n.w, n.d);
+    const at::TensorOptions floats = n.x.options().dtype(at::kFloat).requires_grad(false);
+    const at::Tensor loss = !truth(a[5]) ? at::Tensor() : how == IMUNPACK_NONE ? at::empty(n.target.sizes(), floats) : at::empty({}, floats);
+    const at::Tensor gx = truth(a[7]) ? dense_like(n.x, n.x.scalar_type()) : at::Tensor(), gw = truth(a[8]) ? dense_like(n.w, n.w.scalar_type()) : at::Tensor();
+    size_t bytes = 0;
+    check(g_xent_workspace(w.p, w.pitch, n.rows, n.d, n.vocab, n.type, gx.defined() || gw.defined(), &bytes), "imunpack_xent_workspace");
+    const at::Tensor workspace = at::empty({(int64_t)bytes}, floats.dtype(at::kByte));
+    check(g_xent(x.p, x.pitch, w.p, w.pitch, (const int64_t *)target.data_ptr(), n.rows, n.d, n.vocab, n.type, whole(a[3]), how, (float *)data(loss), (const float *)data(grad),
+                 data(gx), n.d, data(gw), n.d, workspace.data_ptr(), bytes, address(a[9])), "imunpack_xent");
+    return wrapped<3>({loss, gx, gw});
+}
+
+PyObject *xent_rescale(PyObject *const *a) {  // x, w, target, grad, gx, gw, stream: gx and gw (either may be None) times grad, in place
+    const Xent n = xent_arguments(a);
+    const at::Tensor &grad = tensor(a[3], "xent: grad");
+    const at::Tensor gx = maybe(a[4], "xent: gx"), gw = maybe(a[5], "xent: gw");
+    check(g_xent_rescale((const float *)grad.data_ptr(), data(gx), gx.defined() ? gx.numel() : 0, data(gw), gw.defined() ? gw.numel() : 0, n.type, address(a[6])),
+          "imunpack_xent_rescale");
+    Py_RETURN_NONE;
+}
+
 PyObject *bind(PyObject *const *a) {
     Py_INCREF(a[0]);
     Py_XDECREF(g_error);
@@ -250,6 +295,9 @@ PyObject *bind(PyObject *const *a) {
     g_rmsnorm_backward_workspace = (decltype(g_rmsnorm_backward_workspace))address(a[3]);
     g_rmsnorm_backward = (decltype(g_rmsnorm_backward))address(a[4]);
     g_adamw = (decltype(g_adamw))address(a[5]);
+    g_xent_workspace = (decltype(g_xent_workspace))address(a[6]);
+    g_xent = (decltype(g_xent))address(a[7]);
+    g_xent_rescale = (decltype(g_xent_rescale))address(a[8]);
     Py_RETURN_NONE;
 }
 
@@ -270,8 +318,9 @@ template <PyObject *(*F)(PyObject *const *), Py_ssize_t N>
 PyMethodDef method(const char *name) {
     return {name, (PyCFunction)(void (*)(void))entry<F, N>, METH_FASTCALL, nullptr};
 }
-PyMethodDef g_methods[] = {method<bind, 6>("bind"), method<rmsnorm, 5>("rmsnorm"), method<rmsnorm_quantize, 7>("rmsnorm_quantize"),
-                           method<rmsnorm_backward, 8>("rmsnorm_backward"), method<adamw, 15>("adamw"), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef g_methods[] = {method<bind, 9>("bind"), method<rmsnorm, 5>("rmsnorm"), method<rmsnorm_quantize, 7>("rmsnorm_quantize"),
+                           method<rmsnorm_backward, 8>("rmsnorm_backward"), method<adamw, 15>("adamw"),
+                           method<xent, 10>("xent"), method<xent_rescale, 7>("xent_rescale"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_tensors", "Argument marshalling of the calls whose host time counts.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 }  // namespace
 
