@@ -9,10 +9,12 @@
 //   backward: gx_j = gh_j + r (gy_j w_j - h_j r^2 mean_k(gy_k w_k h_k)),  gw_j = sum over rows of gy_j h_j r
 //
 // Bound by memory: every array is read once and written once.  A row stays in the registers of one wave (up to 256 pieces of 16
-// bytes), of a workgroup of 256 threads (up to 1024) or of 1024 threads (up to 4096) between the sums over it and its use;
+// bytes: 12608 rows of 768 fp32, both passes, 56 us, of a workgroup 64), of a workgroup of 256 threads (up to 1024: 2000 rows of 4096 fp32
+// 45.5 us, of 1024 threads 46.2) or of 1024 threads (up to 4096) between the sums over it and its use;
 // longer rows are read again for each.  Results leave past the caches where a call moves as much as the last-level cache holds (8192 x 4096
-// bfloat16, forward and backward: 121 -> 111 us; 12608 x 768 fp32, whose backward pass finds them there: 64, 69 that way).  Sums, statistics and products are binary32; what is stored as bfloat16 is rounded once, from
-// the binary32 value (y from the unrounded h).
+// bfloat16, forward and backward: 121 -> 111 us; 12608 x 768 fp32, whose backward pass finds them there: 64, 69 that way).  Of 8192 x 4096
+// bfloat16 the forward pass takes 42 us and the backward pass 50, 6.4 and 5.4 TB/s, where a copy of 1 GiB reaches 5.1.
+// Sums, statistics and products are binary32; what is stored as bfloat16 is rounded once, from the binary32 value (y from the unrounded h).
 #include "common.h"
 #include "elements.h"
 
@@ -23,8 +25,8 @@ namespace imu {
 constexpr int kNormThreads = 256;   // of a workgroup whose waves take a row each
 constexpr int kNormGroups = 2048;   // workgroups at most: they walk over the rows
 constexpr int kNormPartials = 512;  // workgroups of the backward pass at most: each leaves a row of partial sums of gw
-constexpr int kNormFewRows = 128;   // up to so many rows other workgroups of the same launch read them again, column by column, for gw: no second
-                                    // launch for the sums (8 rows of 544 fp32, forward and backward: 17.0 -> 12.6 us)
+constexpr int kNormFewRows = 256;   // up to so many rows other workgroups of the same launch read them again, column by column, for gw: no second
+                                    // launch for the sums (256 rows of 1024 fp32, forward and backward: 14.3 us and 17.2 with one; 500 rows: 20.5 and 17.0)
 
 struct NormArgs {
     const void *x, *res, *w;

@@ -6,8 +6,8 @@
 // sixteen lanes read four rows of sixteen elements and get a column of four each.  So no operand is ever transposed in memory.
 //
 // The walk over the contraction is that of the int8 GEMM, whose fragments have the same bytes: k-tiles of 64 places (128 bytes of a row, or 64
-// rows), loaded straight into LDS, a ring of 2 DEPTH + 1 half-stages (A and B of a k-tile in slots of their own), one barrier to a k-tile, loads
-// DEPTH k-tiles ahead: two, and four where a product has so few tiles that a CU has one small one to itself, whose time is that of its loads.
+// rows), loaded straight into LDS, a ring of five half-stages (A and B of a k-tile in slots of their own), one barrier to a k-tile, loads two
+// k-tiles ahead (four, where a product has so few tiles that a CU has a small one to itself, took as long: 100 x 1024 by 4000 fp32 62 us).
 // 16-byte piece c of row r lies at slot c ^ ((r >> 1) & 7) of the row (contraction contiguous: the 32 rows of a fragment fall on different banks)
 // or c ^ ((r & 3) << 2) (across: the four rows of a read do).
 //
@@ -33,7 +33,8 @@ constexpr int kStageCols = 64;     // 16-bit elements of it
 template <bool F16>
 constexpr int kPlaces = F16 ? 32 : 64;  // places of the contraction in a k-tile
 constexpr int kProductThreads = 256;
-constexpr int product_lds(int tm, int tn, int depth) { return (2 * depth + 1) * 64 * (tm > tn ? tm : tn) * kStageBytes; }
+constexpr int kRing = 5;           // slots
+constexpr int product_lds(int tm, int tn) { return kRing * 64 * (tm > tn ? tm : tn) * kStageBytes; }
 
 // One operand: rows of memory of 16-bit elements, `pitch` bytes apart (a multiple of 16, as is the base).  Rows from `rows` on are not read, nor
 // pieces of 16 bytes that hold nothing of the first `cols` elements of a row: the last one is, in their place.  (Where that is along the
@@ -73,12 +74,12 @@ __device__ __forceinline__ void tile_at(int wg, int mtiles, int ntiles, int &tm,
 
 // acc[i][j] of the wave: register r of lane l is the sum at row 32 i + (r / 4) * 8 + (l / 32) * 4 + r % 4 and column 32 j + l % 32 of the
 // wave's part of the tile.  k-tiles [k0, k1) of the contraction.  XA, XB: the operand lies across.
-template <bool F16, int TM, int TN, int DEPTH, bool XA, bool XB>
+template <bool F16, int TM, int TN, bool XA, bool XB>
 __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B, int m0, int n0, int k0, int k1, char *smem, v16f32 (&acc)[TM][TN]) {
     constexpr int N = F16 ? 2 : 1, R = kPlaces<F16>, kSteps = R / 16;  // numbers of a value; places and k-steps of a k-tile
     constexpr int kSlot = 64 * (TM > TN ? TM : TN) * kStageBytes;  // bytes of a slot of the ring
     constexpr int LA = 2 * TM, LB = 2 * TN;                        // loads of a wave for its share of a half-stage: 16 TM (16 TN) rows
-    constexpr int NF = N * (TM + TN), NM = TM * TN * (F16 ? 3 : 1), RING = 2 * DEPTH + 1;
+    constexpr int NF = N * (TM + TN), NM = TM * TN * (F16 ? 3 : 1);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -110,7 +111,7 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B,
     offsets(offB, colB, std::bool_constant<XB>(), std::integral_constant<int, TN>(), B, n0);
     const int64_t stepA = XA ? R * A.pitch : kStageBytes, stepB = XB ? R * B.pitch : kStageBytes;
     const char *gA = A.base + (XA ? m0 * 2 * N : m0 * A.pitch) + k0 * stepA, *gB = B.base + (XB ? n0 * 2 * N : n0 * B.pitch) + k0 * stepB;
-    auto ring = [](int slot, int k) { slot += k; return slot >= RING ? slot - RING : slot; };
+    auto ring = [](int slot, int k) { slot += k; return slot >= kRing ? slot - kRing : slot; };
     const char *pg = nullptr;
     unsigned dl = 0, last = 0;
     // k-tile kt (past the last one it is loaded again, into a slot that is not read) of A or B into a slot
@@ -184,7 +185,7 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B,
     };
     // k-tile 0 landed, the next ones on their way
 #pragma unroll
-    for (int p = 0; p < DEPTH; ++p) {
+    for (int p = 0; p < 2; ++p) {
         setup(true, p, 2 * p);
 #pragma unroll
         for (int u = 0; u < LA; ++u) fetch(true, u);
@@ -192,20 +193,20 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B,
 #pragma unroll
         for (int u = 0; u < LB; ++u) fetch(false, u);
     }
-    asm volatile("s_waitcnt vmcnt(%0)" ::"i"((DEPTH - 1) * (LA + LB)) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"i"(LA + LB) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int q = 0; q < NF; ++q) fragment(smem, smem + kSlot, 0, 0, q);
-    // The steps before the last load A(kt + DEPTH) into the slot that is free.  Behind them every fragment of k-tile kt has been read and this
+    // The steps before the last load A(kt + 2) into the slot that is free.  Behind them every fragment of k-tile kt has been read and this
     // wave's parts of k-tile kt + 1 have landed (all but the newest loads); past the barrier that holds for all waves, so that the last step may read
-    // k-tile kt + 1 and load B(kt + DEPTH) into the slot of A(kt).
+    // k-tile kt + 1 and load B(kt + 2) into the slot of A(kt).
     constexpr int c0 = (LA + 2) / 3, c1 = (LA - c0 + 1) / 2, c2 = LA - c0 - c1;
     int sa = 0;
     for (int kt = 0; kt < total; ++kt) {
         const char *stA = smem + sa * kSlot, *stB = smem + ring(sa, 1) * kSlot;
         const char *stA1 = smem + ring(sa, 2) * kSlot, *stB1 = smem + ring(sa, 3) * kSlot;
-        setup(true, kt + DEPTH, ring(sa, 2 * DEPTH));
+        setup(true, kt + 2, ring(sa, 4));
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (F16) {
             step(0, stA, stB, 1, true, 0, LA);
@@ -214,10 +215,10 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &B,
             step(1, stA, stB, 2, true, c0, c1);
             step(0, stA, stB, 3, true, c0 + c1, c2);
         }
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"((DEPTH - 2) * (LA + LB) + LA) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(LA) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        setup(false, kt + DEPTH, sa);
+        setup(false, kt + 2, sa);
         __builtin_amdgcn_sched_barrier(0);
         step(1, stA1, stB1, 0, false, 0, LB);
         sa = ring(sa, 2);

@@ -26,10 +26,10 @@ constexpr int64_t kPieceBytes = 2ll << 30;  // G of a piece of the rows at most 
 constexpr int kTop = 14;                    // the largest magnitude of a scaled operand is below 2^(kTop + 1)
 constexpr unsigned kCus = 256;
 constexpr int kXentSlots = 256;             // parts of the tiles of a gradient that go at a time: one to a CU
-constexpr int kPartTiles = 2;               // k-tiles of a part at least: below that its sums cost more than its products
+constexpr int kPartTiles = 2;               // k-tiles of a part at least (1: as fast; 4: 100 x 1024 by 16000 bf16 58.0 -> 59.5 us)
 constexpr int kScanGroups = 512, kScanX = 64;  // workgroups that look for the largest magnitudes, those of x first
 constexpr int kJoinRows = 8;
-constexpr int64_t kJoinVocab = 8192;        // the parts of a row up to which a load of each thread has them all
+constexpr int64_t kJoinReads = 1 << 22;     // parts read, by every workgroup of a row, up to which those join them that turn the exponentials
 constexpr int kLargeRows = 1024;            // rows from which the logits may go in large tiles
 
 struct XentHeader {
@@ -140,7 +140,7 @@ __device__ __forceinline__ int scan_rows(const ScanArgs &a, int32_t (*sums)[16],
     return base;
 }
 
-// Workgroup 0: the rows.  The others (fp32): the largest magnitudes of x and W.
+// Workgroup 0: the rows.  The others (fp32): the largest magnitudes of x and W (50265 x 768: 38 us, 4.1 TB/s).
 __global__ __launch_bounds__(1024) void xent_scan_kernel(const ScanArgs a) {
     __shared__ int32_t sums[2][16];
     __shared__ float lds[16];
@@ -173,8 +173,9 @@ struct PrepareArgs {
 };
 constexpr int kPrepareTurns = 4, kScanHere = 1024;
 // Eight columns of a row at a time: binary32 as two binary16 numbers, bfloat16 as it is; zeros behind the last column and, to a whole
-// k-tile, behind the last row of x.  SCAN: up to kScanHere rows, among which every workgroup finds those with a target itself (one launch less:
-// 197 x 256 by 1000, loss alone: 21.5 -> 18.3 us).
+// k-tile, behind the last row of x.  Bound by memory: 50265 x 768 fp32 55 us, 5.6 TB/s (what it reads is in the
+// last-level cache).  SCAN: up to kScanHere rows, among which every workgroup finds those with a target itself (one launch less: 197 x 256
+// by 1000, loss alone: 21.5 -> 18.3 us).
 template <class T, bool SCAN>
 __global__ __launch_bounds__(SCAN ? 1024 : 256) void xent_prepare_kernel(const PrepareArgs a) {
     constexpr bool SPLIT = sizeof(T) == 4;
@@ -254,7 +255,7 @@ struct Upstream {
 };
 
 // The same row by row, for the loss alone: each row by its own largest magnitude, which no other kernel has to look for.  A wave to a row,
-// which it reads twice (the second time out of a cache).
+// which it reads twice (the second time out of a cache).  32003 x 1031 60 us, 4.5 TB/s.
 struct PrepareRowsArgs {
     const float *x, *w;
     int64_t ldx, ldw;
@@ -337,9 +338,12 @@ __device__ __forceinline__ void quad_transpose(uint32_t &lo, uint32_t &hi, int l
 }
 
 // A tile of logits, vocabulary down, rows of x across: a lane holds one row of x per column block, so that the sums over the
-// vocabulary are sums over its registers and one exchange between the halves of the wave.
-template <bool F16, int T, int DEPTH, bool KEEP>
-__global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void xent_logits_kernel(const LogitArgs a) {
+// vocabulary are sums over its registers and one exchange between the halves of the wave.  Bound by the matrix cores: 4096 x 4096 by 32000
+// bfloat16 836 us, 1.28 PFLOP/s, where a library's product of 8192^3 reaches 1.37 (busy 75 % of the cycles at the clock that its power allows); 614 x 768
+// by 50265 fp32 160 us, 0.89 PFLOP/s of binary16 (busy 58 %: the contraction is short, and the exponentials are made
+// and stored behind it).
+template <bool F16, int T, bool KEEP>
+__global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_kernel(const LogitArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     constexpr int kEdge = 64 * T;
     const int count = rows_of(a.hdr, a.first, a.room), vocab = a.w.rows, mtiles = (vocab + kEdge - 1) / kEdge, ntiles = (count + kEdge - 1) / kEdge;
@@ -351,7 +355,7 @@ __global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void 
     Operand x = a.x;
     x.rows = count;
     v16f32 acc[T][T];
-    product_tile<F16, T, T, DEPTH, false, false>(a.w, x, tm * kEdge, tn * kEdge, 0, a.ktiles, smem, acc);
+    product_tile<F16, T, T, false, false>(a.w, x, tm * kEdge, tn * kEdge, 0, a.ktiles, smem, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, lhalf = lane >> 5;
     const int vwave = tm * kEdge + (wave >> 1) * 32 * T, twave = tn * kEdge + (wave & 1) * 32 * T;  // the wave's first column and row of the piece
     const int down = F16 && KEEP ? -(scale_exponent(a.hdr->amax[0]) + scale_exponent(a.hdr->amax[1])) : 0;
@@ -535,8 +539,10 @@ struct TurnArgs {
     int64_t pitch_P;
 };
 // Exponentials become G where they lie, 256 columns of ROWS rows to a workgroup, eight columns to a lane: zeros behind the vocabulary and, to a
-// whole k-tile, behind the last row.  32 rows, or eight where that leaves CUs without a workgroup; JOIN: those join the parts of their rows
-// themselves, as the kernel above does (200 x 256 by 1000 fp32, forward and backward: 43.3 -> 40.6 us).
+// whole k-tile, behind the last row.  614 x 50265 in binary16 pairs 50 us, 248 MB read and written.  32 rows, or eight where that leaves CUs
+// without a workgroup (500 x 512 by 8000 fp32, both passes: 83.6 us and 81.8).  JOIN: those join the parts of their rows themselves, as the
+// kernel above does, which saves its launch (both passes, fp32: 200 x 256 by 1000 43.3 -> 40.6 us, 50 x 256 by 16000 55.3 -> 51.8, 20 x 64 by
+// 50000 65.3 -> 61.5; but 300 x 768 by 16000 bf16 69.2 -> 70.4).
 template <bool F16, int ROWS, bool JOIN>
 __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
     static_assert(!JOIN || ROWS == kJoinRows, "the rows of a workgroup");
@@ -626,7 +632,7 @@ struct GradArgs {
     Cut cut;
 };
 // A tile (or part of one) of gx = G W, with W across, or of gW = G^T x, both across and with rows of zeros to whole k-tiles.
-template <bool F16, int T, int DEPTH, bool X>
+template <bool F16, int T, bool X>
 __device__ __forceinline__ void grad_tile(const GradArgs &a, int wg, char *smem) {
     constexpr int kEdge = 64 * T;
     const int count = rows_of(a.hdr, a.first, a.room);
@@ -656,7 +662,7 @@ __device__ __forceinline__ void grad_tile(const GradArgs &a, int wg, char *smem)
     if (X) G.cols = ktiles * kStageCols;  // (zeros behind the vocabulary)
     x.rows = rtiles * R;
     v16f32 acc[T][T];
-    product_tile<F16, T, T, DEPTH, !X, true>(G, X ? a.w : x, tm * kEdge, tn * kEdge, k0, k1, smem, acc);
+    product_tile<F16, T, T, !X, true>(G, X ? a.w : x, tm * kEdge, tn * kEdge, k0, k1, smem, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r0 = (wave >> 1) * 32 * T, rl = 4 * (lane >> 5), c0 = (wave & 1) * 32 * T + (lane & 31);
     if (X || a.cut.through) {
@@ -706,13 +712,14 @@ __device__ __forceinline__ void grad_tile(const GradArgs &a, int wg, char *smem)
         }
 }
 // Both gradients from a piece of the rows: the first xgroups workgroups take parts of the tiles of gx, those behind them tiles of gW (parts of
-// them, where there are few), so that neither waits for the other's last ones.
-template <bool F16, int T, int DEPTH>
-__global__ __launch_bounds__(kProductThreads, T == 4 || DEPTH > 2 ? 1 : 2) void xent_grads_kernel(const GradArgs a) {
+// them, where there are few), so that neither waits for the other's last ones.  4096 x 4096 by 32000 bfloat16 1700 us, 1.26 PFLOP/s; 614 x 768
+// by 50265 fp32 291 us, 0.98 of binary16.
+template <bool F16, int T>
+__global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_grads_kernel(const GradArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     if (grads_edge(rows_at_most(a.hdr, a.room), a.d, a.w.rows) != 64 * T) return;
-    if ((int)blockIdx.x < a.cut.xgroups) grad_tile<F16, T, DEPTH, true>(a, blockIdx.x, smem);
-    else grad_tile<F16, T, DEPTH, false>(a, blockIdx.x - a.cut.xgroups, smem);
+    if ((int)blockIdx.x < a.cut.xgroups) grad_tile<F16, T, true>(a, blockIdx.x, smem);
+    else grad_tile<F16, T, false>(a, blockIdx.x - a.cut.xgroups, smem);
 }
 
 struct FoldArgs {
@@ -855,43 +862,40 @@ static int more_lds(K kernel, int bytes) {
     IMU_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
     return IMUNPACK_OK;
 }
-template <bool F16, int T, int DEPTH>
+template <bool F16, int T>
 static int xent_lds() {
-    IMU_TRY(more_lds(xent_logits_kernel<F16, T, DEPTH, false>, product_lds(T, T, DEPTH)));
-    IMU_TRY(more_lds(xent_logits_kernel<F16, T, DEPTH, true>, product_lds(T, T, DEPTH)));
-    return more_lds(xent_grads_kernel<F16, T, DEPTH>, product_lds(T, T, DEPTH));
+    IMU_TRY(more_lds(xent_logits_kernel<F16, T, false>, product_lds(T, T)));
+    IMU_TRY(more_lds(xent_logits_kernel<F16, T, true>, product_lds(T, T)));
+    return more_lds(xent_grads_kernel<F16, T>, product_lds(T, T));
 }
 static int xent_lds_opt_in() {
     static std::atomic<int> done{0};  // (the attribute is idempotent: two threads set the same)
     if (done.load(std::memory_order_acquire)) return IMUNPACK_OK;
-    IMU_TRY((xent_lds<false, 4, 2>()));
-    IMU_TRY((xent_lds<false, 2, 2>()));
-    IMU_TRY((xent_lds<false, 2, 4>()));
-    IMU_TRY((xent_lds<true, 4, 2>()));
-    IMU_TRY((xent_lds<true, 2, 2>()));
-    IMU_TRY((xent_lds<true, 2, 4>()));
+    IMU_TRY((xent_lds<false, 4>()));
+    IMU_TRY((xent_lds<false, 2>()));
+    IMU_TRY((xent_lds<true, 4>()));
+    IMU_TRY((xent_lds<true, 2>()));
     done.store(1, std::memory_order_release);
     return IMUNPACK_OK;
 }
 
-template <bool F16, int T, int DEPTH>
+template <bool F16, int T>
 static void launch_logits(const LogitArgs &a, bool keep, unsigned groups, hipStream_t st) {
-    if (keep) hipLaunchKernelGGL((xent_logits_kernel<F16, T, DEPTH, true>), dim3(groups), dim3(kProductThreads), product_lds(T, T, DEPTH), st, a);
-    else hipLaunchKernelGGL((xent_logits_kernel<F16, T, DEPTH, false>), dim3(groups), dim3(kProductThreads), product_lds(T, T, DEPTH), st, a);
+    if (keep) hipLaunchKernelGGL((xent_logits_kernel<F16, T, true>), dim3(groups), dim3(kProductThreads), product_lds(T, T), st, a);
+    else hipLaunchKernelGGL((xent_logits_kernel<F16, T, false>), dim3(groups), dim3(kProductThreads), product_lds(T, T), st, a);
 }
 template <bool F16>
 static void launch_logits(const LogitArgs &a, int edge, bool keep, int64_t rows, hipStream_t st) {
     auto groups = [&](int64_t edge) { return (unsigned)(up(a.w.rows, edge) / edge * (up(rows, edge) / edge)); };
     if (edge == 256) {  // (a workgroup that finds nothing to do takes its time too: no more of them than would have something)
-        launch_logits<F16, 4, 2>(a, keep, groups(256), st);
+        launch_logits<F16, 4>(a, keep, groups(256), st);
         if (logits_edge(kLargeRows, a.d, a.w.rows) == 256) rows = std::min<int64_t>(rows, kLargeRows);
     }
-    if (groups(128) > kCus) launch_logits<F16, 2, 2>(a, keep, groups(128), st);
-    else launch_logits<F16, 2, 4>(a, keep, groups(128), st);
+    launch_logits<F16, 2>(a, keep, groups(128), st);
 }
-template <bool F16, int T, int DEPTH>
+template <bool F16, int T>
 static void launch_grads(const GradArgs &a, unsigned groups, hipStream_t st) {
-    hipLaunchKernelGGL((xent_grads_kernel<F16, T, DEPTH>), dim3(groups), dim3(kProductThreads), product_lds(T, T, DEPTH), st, a);
+    hipLaunchKernelGGL((xent_grads_kernel<F16, T>), dim3(groups), dim3(kProductThreads), product_lds(T, T), st, a);
 }
 template <bool F16>
 static void launch_grads(GradArgs a, const XentLayout &l, bool x, bool w, hipStream_t st) {
@@ -900,9 +904,8 @@ static void launch_grads(GradArgs a, const XentLayout &l, bool x, bool w, hipStr
         if (!x) a.cut.xgroups = 0;
         const unsigned groups = (unsigned)(a.cut.xgroups + (w ? up(a.w.rows, edge) / edge * (up(a.d, edge) / edge) * a.cut.wcut : 0));
         if (groups == 0) continue;
-        if (edge == 256) launch_grads<F16, 4, 2>(a, groups, st);
-        else if (groups > kCus) launch_grads<F16, 2, 2>(a, groups, st);
-        else launch_grads<F16, 2, 4>(a, groups, st);
+        if (edge == 256) launch_grads<F16, 4>(a, groups, st);
+        else launch_grads<F16, 2>(a, groups, st);
     }
 }
 }  // namespace imu
@@ -978,7 +981,7 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
             l.split ? launch_logits<true>(a, l.edge_l, back, n, st) : launch_logits<false>(a, l.edge_l, back, n, st);
         }
         const unsigned across = (unsigned)(up(vocab, 256) / 256), down = (unsigned)up(n, kStageCols);
-        const bool few = across * down / 32 < 4 * kCus, joins = back && n > 0 && few && l.pieces == 1 && vocab <= kJoinVocab;
+        const bool few = across * down / 32 < 4 * kCus, joins = back && n > 0 && few && l.pieces == 1 && (int64_t)across * n * (up(vocab, 128) / 64) <= kJoinReads;
         JoinArgs j = {};
         j.stats = (const float *)(s + l.stats); j.hit = (const float *)(s + l.hit); j.d = (int)d; j.vocab = (int)vocab; j.first = (int)first; j.room = (int)l.room;
         j.how = loss ? reduction : IMUNPACK_NONE;
