@@ -547,10 +547,11 @@ template <bool F16, int ROWS, bool JOIN>
 __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
     static_assert(!JOIN || ROWS == kJoinRows, "the rows of a workgroup");
     const JoinArgs &j = a.join;
+    const int across = (j.vocab + 255) / 256, group_y = blockIdx.x / across, group_x = blockIdx.x - group_y * across;  // (rows can be too many for a grid's second axis)
     const int rows = rows_of(j.hdr, j.first, j.room), last = (rows + kStageCols - 1) / kStageCols * kStageCols;
-    const int row0 = blockIdx.y * ROWS + (threadIdx.x >> 5), v0 = blockIdx.x * 256 + (threadIdx.x & 31) * 8, left = j.vocab - v0;
-    const bool losses = JOIN && blockIdx.x == 0 && (int)blockIdx.y < max(1, (rows + ROWS - 1) / ROWS);
-    if ((int)blockIdx.y * ROWS >= last && !losses) return;
+    const int row0 = group_y * ROWS + (threadIdx.x >> 5), v0 = group_x * 256 + (threadIdx.x & 31) * 8, left = j.vocab - v0;
+    const bool losses = JOIN && group_x == 0 && group_y < max(1, (rows + ROWS - 1) / ROWS);
+    if (group_y * ROWS >= last && !losses) return;
     if (!JOIN && v0 >= (j.vocab + kStageCols - 1) / kStageCols * kStageCols) return;
     const float all = a.up.g ? 0.0f : a.up.one(j.hdr);
     const int part = v0 / (logits_edge(rows_at_most(j.hdr, j.room), j.d, j.vocab) / 2);  // whose columns share a largest logit
@@ -569,7 +570,7 @@ __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
     __shared__ float lse[kJoinRows];
     float own_lse = 0.0f;
     if constexpr (JOIN) {
-        own_lse = join_rows(j, blockIdx.y, sh);
+        own_lse = join_rows(j, group_y, sh);
         if (threadIdx.x < kJoinRows) lse[threadIdx.x] = own_lse;
         __syncthreads();
     }
@@ -606,7 +607,7 @@ __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
         if (F16) *reinterpret_cast<v4i32 *>(p0 + t * a.pitch_P + kSecond) = v4i32{(int)ql[0], (int)ql[1], (int)ql[2], (int)ql[3]};
     }
     if constexpr (JOIN)
-        if (losses) rows_losses(j, blockIdx.y, own_lse, sh);
+        if (losses) rows_losses(j, group_y, own_lse, sh);
 }
 
 // Into how many parts the tiles of a gradient are cut along the contraction, so that every CU has one.
@@ -992,7 +993,7 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
         if (n > 0) {
             TurnArgs t = {};
             t.join = j; t.wanted = wanted; t.up = upstream; t.P = s + l.P; t.pitch_P = l.pitch_P;
-            const dim3 grid(across, down / (few ? 8 : 32));
+            const dim3 grid(across * (down / (few ? 8 : 32)));
             if (l.split) hipLaunchKernelGGL((joins ? xent_turn_kernel<true, 8, true> : few ? xent_turn_kernel<true, 8, false> : xent_turn_kernel<true, 32, false>), grid, dim3(256), 0, st, t);
             else hipLaunchKernelGGL((joins ? xent_turn_kernel<false, 8, true> : few ? xent_turn_kernel<false, 8, false> : xent_turn_kernel<false, 32, false>), grid, dim3(256), 0, st, t);
         }

@@ -174,6 +174,16 @@ def test_pieces_of_the_rows_in_large_tiles(imu, dtype, share):
     within(b, (total[0], total[1] + sums(rows, dtype) * total[0].abs()))
 
 
+def test_more_rows_than_a_grid_has_on_its_second_axis(imu):
+    x, w, target, grad = inputs(2200000, 8, 40, torch.bfloat16, 0.99, 6)
+    valid, loss, gx, gw = reference(x, w, target, grad, torch.bfloat16)
+    got, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+    a, b = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    within(got, loss)
+    within(a, gx)
+    within(b, gw)
+
+
 def test_nothing_to_learn_from_and_targets_outside(imu):
     x, w, target, grad = inputs(70, 96, 150, torch.float32, 1.0, 5)
     none = torch.full_like(target, -100)
