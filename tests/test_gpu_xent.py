@@ -184,6 +184,46 @@ def test_more_rows_than_a_grid_has_on_its_second_axis(imu):
     within(b, gw)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_weights_beyond_32_bits(imu, dtype):
+    """W of more than 2^31 elements; the formulas of `reference` over pieces of the vocabulary, gW at its first, middle and last rows."""
+    rows, d, vocab, step = 6, 2000, 1100000, 50000
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x = torch.randn(rows, d, generator=g, device="cuda").to(dtype)
+    w = torch.empty(vocab, d, dtype=dtype, device="cuda")
+    for v in range(0, vocab, step):
+        w[v:v + step] = torch.randn(step, d, generator=g, device="cuda") * (2.0 / d ** 0.5)
+    target = torch.tensor([0, vocab - 1, -100, vocab // 2, vocab - 2, 7], device="cuda")
+    grad = torch.randn(rows, generator=g, device="cuda")
+    low, valid, at = dtype == torch.bfloat16, target >= 0, torch.where(target >= 0, target, 0)[:, None]
+    x6, g6 = torch.where(valid[:, None], x.to(F), 0.0), torch.where(valid, grad.to(F), 0.0)
+    pieces = [slice(v, v + step) for v in range(0, vocab, step)]
+    l = torch.cat([x6 @ w[r].to(F).t().contiguous() for r in pieces], 1)
+    dl = sums(d, dtype) * torch.cat([x6.abs() @ w[r].to(F).abs().t().contiguous() for r in pieces], 1)
+    lse = torch.logsumexp(l, 1)
+    dlse = dl.amax(1) + (102 + vocab / 512) * U + 2 * U * lse.abs()
+    hit = l.gather(1, at)[:, 0]
+    loss = torch.where(valid, lse - hit, 0.0)
+    dloss = torch.where(valid, dlse + dl.gather(1, at)[:, 0] + 2 * U * (lse.abs() + hit.abs()), 0.0)
+    p = torch.exp(l - lse[:, None])
+    dp = p * (dl + dlse[:, None] + 3 * U * (l - lse[:, None]).abs() + 4 * U) + (2.0 ** -8 * p * 1.01 if low else 2.0 ** -22 * p + 2.0 ** -39)
+    G = p.scatter_add(1, at, torch.full_like(at, -1.0, dtype=F)) * g6[:, None]
+    dG = (dp + 2 * U) * g6.abs()[:, None] + (2.0 ** -8 * G.abs() if low else 2.0 ** -22 * G.abs() + 2.0 ** -38 * g6.abs().max())
+    gx, dgx = torch.zeros_like(x6), torch.zeros_like(x6)
+    for r in pieces:
+        w6 = w[r].to(F)
+        gx += G[:, r] @ w6
+        dgx += dG[:, r] @ w6.abs() + sums(vocab, dtype) * (G[:, r].abs() @ w6.abs())
+    got, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+    a, b = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    within(got, (loss, dloss))
+    within(a, (gx, dgx + (2.0 ** -8 if low else U) * gx.abs()))
+    for r in (pieces[0], pieces[len(pieces) // 2], pieces[-1]):
+        gw = G[:, r].t().contiguous() @ x6
+        dgw = dG[:, r].t().contiguous() @ x6.abs() + sums(rows, dtype) * (G[:, r].abs().t().contiguous() @ x6.abs())
+        within(b[r], (gw, dgw + (2.0 ** -8 if low else U) * gw.abs()))
+
+
 def test_nothing_to_learn_from_and_targets_outside(imu):
     x, w, target, grad = inputs(70, 96, 150, torch.float32, 1.0, 5)
     none = torch.full_like(target, -100)
