@@ -11,9 +11,9 @@
 // below m in the next step.
 //
 // Bound by memory: 28 bytes an element with 32-bit states and gradients, 16 with 8-bit states.  More than the last-level cache holds is read and
-// written past the caches (85 million elements: 464 -> 410 us with 32-bit states, 5.9 TB/s; 157 million 478 -> 455 with 8-bit ones, bfloat16
-// gradients and copies, 5.6 TB/s).  A wave takes 256 elements at a time, four to a lane, which is a block of the 8-bit states; tensors come as a
-// table in the kernel's arguments, 4096 elements to a workgroup.
+// written past the caches (85 million elements: 464 -> 410 us with 32-bit states; 157 million 478 -> 455 with 8-bit ones, bfloat16 gradients and
+// copies).  A wave takes 256 elements, four to a lane, which is a block of the 8-bit states; tensors come as a table in the kernel's
+// arguments.  85 million elements with 32-bit states take 383 us, 6.2 TB/s, 157 million with 8-bit ones 448 us, 5.6 TB/s.
 #include "common.h"
 #include "elements.h"
 
@@ -23,7 +23,7 @@
 namespace imu {
 constexpr int kAdamTensors = 48;      // to a launch: their table travels in the kernel's arguments (4 KiB)
 constexpr int kAdamBlock = 256;       // elements that share a scale
-constexpr int kAdamBlocks = 4;        // blocks of a wave
+constexpr int kAdamBlocks = 1;        // blocks of a wave (4: 85 million elements 383 -> 405 us, 0.27 million in 112 tensors 19 -> 25)
 constexpr int kAdamChunk = 4 * kAdamBlocks * kAdamBlock;  // elements of a workgroup
 constexpr float kE4m3Max = 448.0f, kNothing = 0x1p-96f;  // a block of no more than that is held as zeros
 
