@@ -448,6 +448,72 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
     else finish(std::false_type());
 }
 
+struct FewArgs {
+    const float *x, *w;
+    int64_t ldx, ldw;
+    const XentHeader *hdr;
+    const int32_t *source, *wanted;
+    float *stats, *hit;
+    int room, d, vocab;
+};
+constexpr int kFewRows = 8;
+// The loss alone of up to eight fp32 rows over weights that the last-level cache does not hold: W is read once, as it is, where splitting
+// it would move it three times.  64 columns (a part of a tile of 128) to a workgroup, eight at a time to a wave, sums in binary32.  Bound by
+// memory: 8 x 4096 by 32000 123 us (split: 412), by 128000 381 us (1386), 5.5 TB/s.  Weights that the cache holds go the way of all others.
+__global__ __launch_bounds__(256) void xent_few_kernel(const FewArgs a) {
+    __shared__ float logits[64][kFewRows];
+    const int count = a.hdr->count, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (count == 0) return;
+    const float *x[kFewRows];
+#pragma unroll
+    for (int r = 0; r < kFewRows; ++r) x[r] = a.x + (int64_t)a.source[min(r, count - 1)] * a.ldx;
+    for (int c0 = wave * 16; c0 < wave * 16 + 16; c0 += 8) {
+        const float *w[8];
+        float sum[8][kFewRows];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            w[c] = a.w + (int64_t)min((int)blockIdx.x * 64 + c0 + c, a.vocab - 1) * a.ldw;
+#pragma unroll
+            for (int r = 0; r < kFewRows; ++r) sum[c][r] = 0.0f;
+        }
+        for (int k0 = 0; k0 < a.d; k0 += 256) {
+            const int k = k0 + lane * 4;
+            piece_t<float, 4> fw[8], fx[kFewRows];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) fw[c] = load_piece<float, 4, true>(w[c] + k, a.d - k);
+#pragma unroll
+            for (int r = 0; r < kFewRows; ++r) fx[r] = load_piece<float, 4>(x[r] + k, a.d - k);
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+#pragma unroll
+                for (int r = 0; r < kFewRows; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[c][r] = fmaf(fw[c][e], fx[r][e], sum[c][r]);
+        }
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int r = 0; r < kFewRows; ++r) {
+                const float l = wave_sum(sum[c][r]);
+                if (lane == 0) logits[c0 + c][r] = l;
+            }
+    }
+    __syncthreads();
+    const int r = threadIdx.x >> 5, j = threadIdx.x & 31, v0 = (int)blockIdx.x * 64;  // 32 lanes to a row, two columns to a lane
+    if (r >= count) return;
+    const float l0 = v0 + j < a.vocab ? logits[j][r] : -__builtin_inff(), l1 = v0 + j + 32 < a.vocab ? logits[j + 32][r] : -__builtin_inff();
+    float top = fmaxf(l0, l1);
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+    const float from = top == -__builtin_inff() ? 0.0f : -top * kLog2e;
+    float s = __builtin_amdgcn_exp2f(fmaf(l0, kLog2e, from)) + __builtin_amdgcn_exp2f(fmaf(l1, kLog2e, from));
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) s += __shfl_xor(s, m);
+    const int own = a.wanted[r] - v0;
+    if (own == j || own == j + 32) a.hit[r] = own == j ? l0 : l1;
+    if (j == 0) *reinterpret_cast<float2 *>(a.stats + ((int64_t)blockIdx.x * a.room + r) * 2) = make_float2(top, s);
+}
+
 struct JoinArgs {
     const float *stats, *hit;
     int d, vocab, how, first, room;
@@ -804,6 +870,7 @@ struct XentLayout {
     int edge_l, edge_g;           // largest tile edges that the rows allow, of the logits and of the gradients
     int64_t room, pieces;         // rows to a piece, pieces
     Cut cut[2];                   // of the gradients, with tiles of 128 and of 256
+    bool few;                     // W is read as it is
     bool by_rows;                 // each row of x and W has a scale of its own
     size_t source, place, wanted, lse, row_loss, hit, g, ex, ew, stats, px, pw, P, xparts, wparts, bytes;
 };
@@ -825,12 +892,13 @@ static XentLayout xent_layout(const void *w, int64_t ldw, int64_t rows, int64_t 
     l.source = take(rows * 4); l.place = take(rows * 4); l.wanted = take(rows * 4);
     l.lse = take(rows * 4); l.row_loss = take(rows * 4); l.hit = take(rows * 4); l.g = take(rows * 4);
     // (a wave to a row: 1418 x 1031 by 32003 rows 83 -> 60 us for both passes over the operands, but 64 x 85 by 16360 10 -> 16)
-    l.by_rows = l.split && !grad && d >= 512;
+    l.few = l.split && !grad && rows <= kFewRows && vocab * d * 4 > kLastLevelCache;
+    l.by_rows = l.split && !grad && !l.few && d >= 512;
     l.ex = take(grad ? 0 : rows * 4); l.ew = take(grad ? 0 : l.vp * 4);
     l.stats = take(2 * (up(vocab, 128) / 128) * l.room * 8);  // (two parts to a tile)
     l.pitch_p = l.dp * 2 * numbers;
     l.px = take(l.tp * l.pitch_p);
-    l.pw = take(l.direct ? 0 : vocab * l.pitch_p);
+    l.pw = take(l.direct || l.few ? 0 : vocab * l.pitch_p);
     if (grad) {
         l.pitch_P = l.vp * 2 * numbers;
         l.P = take(l.room * l.pitch_P);
@@ -942,14 +1010,14 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
     const int nx = (int)std::min<int64_t>(up(rows, 64) / 64, kScanX), nw = (int)std::min<int64_t>(up(vocab, 64) / 64, kScanGroups - kScanX);
     c.nx = nx;
     const bool scans = !l.split && rows > 0 && rows <= kScanHere;  // the kernel that gathers x does it
-    if (!scans) hipLaunchKernelGGL(xent_scan_kernel, dim3(l.split && !l.by_rows && rows > 0 ? 1 + nx + nw : 1), dim3(1024), 0, st, c);
+    if (!scans) hipLaunchKernelGGL(xent_scan_kernel, dim3(l.split && !l.by_rows && !l.few && rows > 0 ? 1 + nx + nw : 1), dim3(1024), 0, st, c);
     if (rows > 0 && l.by_rows) {
         PrepareRowsArgs p = {};
         p.x = (const float *)x; p.w = (const float *)w; p.ldx = ldx; p.ldw = ldw; p.hdr = hdr; p.source = source;
         p.px = s + l.px; p.pw = s + l.pw; p.pitch = l.pitch_p; p.wrows = vocab;
         p.ex = (int32_t *)(s + l.ex); p.ew = (int32_t *)(s + l.ew); p.d = (int)d; p.xgroups = (int)(up(rows, 4) / 4);
         hipLaunchKernelGGL(xent_prepare_rows_kernel, dim3((unsigned)(p.xgroups + up(vocab, 4) / 4)), dim3(256), 0, st, p);
-    } else if (rows > 0) {
+    } else if (rows > 0 && !l.few) {
         PrepareArgs p = {};
         p.scan = c;
         p.x = x; p.w = w; p.ldx = ldx; p.ldw = ldw; p.hdr = hdr; p.source = source;
@@ -972,7 +1040,10 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
         const int held = (int)(l.pitch_p / 2);  // (zeros behind the features)
         const Operand whole = {l.direct ? (const char *)w : s + l.pw, l.direct ? ldw * 2 : l.pitch_p, (int)vocab, l.direct ? (int)d : held};
         const Operand part = {s + l.px + first * l.pitch_p, l.pitch_p, 0, held};
-        if (n > 0) {
+        if (n > 0 && l.few) {
+            FewArgs a = {(const float *)x, (const float *)w, ldx, ldw, hdr, source, wanted, (float *)(s + l.stats), (float *)(s + l.hit), (int)l.room, (int)d, (int)vocab};
+            hipLaunchKernelGGL(xent_few_kernel, dim3((unsigned)(2 * (up(vocab, 128) / 128))), dim3(256), 0, st, a);
+        } else if (n > 0) {
             LogitArgs a = {};
             a.w = whole; a.x = part;
             a.ex = (const int32_t *)(s + l.ex); a.ew = (const int32_t *)(s + l.ew);

@@ -224,6 +224,27 @@ def test_weights_beyond_32_bits(imu, dtype):
         within(b[r], (gw, dgw + (2.0 ** -8 if low else U) * gw.abs()))
 
 
+@pytest.mark.parametrize("rows,d,vocab", [(1, 4096, 17000), (8, 1031, 65100), (5, 2050, 33001)])
+def test_few_rows_over_weights_beyond_the_cache(imu, rows, d, vocab):
+    """fp32, the loss alone, W of more than 256 MB: sums of at most 4 d / 256 + 4 + 6 terms in a row, within what `reference` allows."""
+    x, w, target, grad = inputs(rows, d, vocab, torch.float32, 1.0, rows + d)
+    if rows > 2:
+        x[1], target[1] = float("nan"), -100
+        target[0], target[rows - 1] = vocab - 1, 0
+    valid, loss, _, _ = reference(x, w, target, grad, torch.float32)
+    got, _ = imu.imunpack_xent(x, w, target, reduction="none")
+    within(got, loss)
+    one, _ = imu.imunpack_xent(x, w, target, reduction="sum")
+    assert abs(float(one) - float(loss[0].sum())) <= float(loss[1].sum()) + 21 * U * float(loss[0].abs().sum())
+    wide = torch.nn.functional.pad(w, (0, 3))[:, :d]      # rows further apart, off 16 bytes
+    within(imu.imunpack_xent(x, wide, target, reduction="none")[0], loss)
+    none = torch.full_like(target, -100)
+    assert float(imu.imunpack_xent(x, w, none, reduction="sum")[0]) == 0.0
+    target[0] = vocab
+    bad, _ = imu.imunpack_xent(x, w, target, reduction="none")
+    assert torch.isnan(bad[0]) and torch.equal(bad[1:], got[1:])
+
+
 def test_nothing_to_learn_from_and_targets_outside(imu):
     x, w, target, grad = inputs(70, 96, 150, torch.float32, 1.0, 5)
     none = torch.full_like(target, -100)
