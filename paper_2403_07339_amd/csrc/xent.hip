@@ -11,8 +11,8 @@
 // all on the matrix cores, and what is held does not grow with the rows.
 //
 // bfloat16 operands: products in bfloat16, G rounded to bfloat16.  fp32 operands: each value is the sum of two binary16 numbers
-// (22 bits of it; scaled by a power of two so that the operand's largest, or for the loss alone each row's, lies below 2^15) and a product is three of them, which is within
-// the rounding of a binary32 sum; three times the instructions at eight times and more the rate of the binary32 ones.
+// (22 bits of it; scaled by a power of two so that the operand's largest, or for the loss alone each long row's, lies below 2^15) and a
+// product is three of them, which is within the rounding of a binary32 sum; three times the instructions at eight times and more the rate of the binary32 ones.
 #include "common.h"
 #include "elements.h"
 #include "product.h"
