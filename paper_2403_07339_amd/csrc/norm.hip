@@ -216,6 +216,12 @@ __device__ __forceinline__ void norm_columns(const NormBackArgs &a, int block) {
     else ((float *)a.gw)[col] = s;
 }
 
+// The same in a launch of its own, before the rows', where these write gx over what the columns read.
+template <class T, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_columns_kernel(const NormBackArgs a) {
+    norm_columns<T, THREADS>(a, blockIdx.x);
+}
+
 template <class T, int TPR, int NV, bool ONCE>
 __global__ __launch_bounds__(TPR == 64 ? kNormThreads : TPR) void norm_back_kernel(const NormBackArgs a) {
     constexpr int N = kVec<T>, kRows = TPR == 64 ? kNormThreads / 64 : 1;
@@ -393,6 +399,14 @@ static int launch_norm(const NormArgs &a, int pieces, hipStream_t st) {
     return launch_status();
 }
 
+template <class T>
+static int launch_norm_columns(const NormBackArgs &a, int pieces, hipStream_t st) {
+    const dim3 grid((unsigned)((a.d + 63) / 64));
+    if (pieces <= 1024) hipLaunchKernelGGL((norm_columns_kernel<T, kNormThreads>), grid, dim3(kNormThreads), 0, st, a);
+    else hipLaunchKernelGGL((norm_columns_kernel<T, 1024>), grid, dim3(1024), 0, st, a);
+    return launch_status();
+}
+
 template <class T, bool ONCE>
 static int launch_norm_back(const NormBackArgs &a, int pieces, hipStream_t st) {
     const dim3 grid((unsigned)(a.groups + (a.gw ? (a.d + 63) / 64 : 0)));
@@ -420,6 +434,13 @@ using namespace imu;
 // Sizes and strides that every call of this file takes.
 static bool norm_sizes(int64_t rows, int64_t d, int dtype, int w_dtype) {
     return rows >= 0 && rows <= (int64_t)1 << 31 && d > 0 && d <= 1 << 24 && known_type(dtype) && known_type(w_dtype);
+}
+
+// Whether rows of d elements of two arrays share memory.
+static bool rows_overlap(const void *p, int64_t ldp, const void *q, int64_t ldq, int64_t rows, int64_t d, int64_t size) {
+    if (!p || !q || rows == 0) return false;
+    const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+    return a < b + (uintptr_t)(((rows - 1) * ldq + d) * size) && b < a + (uintptr_t)(((rows - 1) * ldp + d) * size);
 }
 
 static int norm_forward(NormArgs &a, int64_t d, int dtype, int w_dtype, hipStream_t st) {
@@ -495,7 +516,13 @@ extern "C" int imunpack_rmsnorm_backward(const void *gy, int64_t ldgy, const voi
     a.ldgy = ldgy; a.ldx = ldx; a.ldres = ldres; a.ldgh = ldgh; a.ldgx = ldgx;
     a.rows = rows; a.d = (int)d; a.w_bf16 = weight_dtype == IMUNPACK_BF16;
     if (rows > 0) {
-        const bool once = rows * d * (dtype == IMUNPACK_F32 ? 4 : 2) * (3 + (residual != nullptr) + (gh != nullptr)) >= kLastLevelCache;
+        const int64_t size = dtype == IMUNPACK_F32 ? 4 : 2;
+        // gx may lie where gy does, of which the columns' workgroups read every row: they are done first then
+        if (a.gw && (rows_overlap(gx, ldgx, gy, ldgy, rows, d, size) || rows_overlap(gx, ldgx, x, ldx, rows, d, size) || rows_overlap(gx, ldgx, residual, ldres, rows, d, size))) {
+            IMU_TRY(dtype == IMUNPACK_F32 ? launch_norm_columns<float>(a, pieces, st) : launch_norm_columns<__bf16>(a, pieces, st));
+            a.gw = nullptr;
+        }
+        const bool once = rows * d * size * (3 + (residual != nullptr) + (gh != nullptr)) >= kLastLevelCache;
         if (dtype == IMUNPACK_F32) IMU_TRY((once ? launch_norm_back<float, true> : launch_norm_back<float, false>)(a, pieces, st));
         else IMU_TRY((once ? launch_norm_back<__bf16, true> : launch_norm_back<__bf16, false>)(a, pieces, st));
     }

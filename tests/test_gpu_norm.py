@@ -259,3 +259,32 @@ def test_refusals(imu):
         imu.imunpack_rmsnorm_backward(x, x.bfloat16(), w, imu.NormSaved(torch.ones(4, device="cuda")))
     with pytest.raises(ValueError):
         imu.imunpack_rmsnorm_backward(x, x, w, imu.NormSaved(torch.ones(3, device="cuda")))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,d", [(1, 64), (37, 1031), (200, 5000), (256, 768), (257, 768), (40, 20000)])
+def test_gradient_in_the_place_of_what_it_is_made_from(imu, rows, d, dtype):
+    """gx may be gy or gh (the entry point in C; the binding gives it memory of its own): the same bits as elsewhere, up to 256 rows and beyond."""
+    import ctypes as C
+    x, res, gy, gh, w = data(rows, d, dtype, rows + 2 * d)
+    w = w.cuda()
+    _, _, saved = imu.imunpack_rmsnorm(x, w, EPS, residual=res)
+    t, size = 1 if dtype == torch.bfloat16 else 0, C.c_size_t()
+    assert imu._lib.imunpack_rmsnorm_backward_workspace(rows, d, t, C.byref(size)) == 0
+    ws = torch.empty(size.value, dtype=torch.uint8, device="cuda")
+
+    def call(gy, gh, gx):
+        gw = torch.full((d,), 7.0, device="cuda")
+        assert imu._lib.imunpack_rmsnorm_backward(gy.data_ptr(), d, x.data_ptr(), d, res.data_ptr(), d, gh.data_ptr(), d, w.data_ptr(), saved.rstd.data_ptr(), rows, d, t, 0,
+                                                  gx.data_ptr(), d, gw.data_ptr(), ws.data_ptr(), size.value, imu._stream()) == 0
+        return gx, gw
+
+    want = call(gy, gh, torch.empty_like(gy))
+    check_backward(x.to(torch.float64) + res.to(torch.float64), gy, gh, w, want[0], want[1], dtype)
+    for _ in range(5):
+        at = gy.clone()
+        got = call(at, gh, at)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        at = gh.clone()
+        got = call(gy, at, at)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
