@@ -398,8 +398,12 @@ int imunpack_adamw(int64_t count, float *const *params, const void *const *grads
  * Rows whose target is ignore_index take no part, whatever x holds there: loss 0, gradient 0.  A target outside [0, vocab) makes the
  * row's loss (and a sum or mean) NaN and adds nothing to the gradients.
  * x, W, gx, gW: device, of type dtype, unit stride within a row, ld* elements from row to row (at least d).
- * bfloat16: products of bfloat16 operands, exponentials and G rounded to bfloat16, sums in fp32.  fp32: within what fp32 sums of fp32
- * products give (operands and G as sums of two binary16 numbers each, scaled by a power of two per operand).
+ * bfloat16: products of bfloat16 operands, exponentials and G rounded to bfloat16, sums in fp32.
+ * fp32: operands and G are sums of two binary16 numbers each, under a power of two.  Losses are within what fp32 sums of fp32 products give,
+ * whatever the sizes of the rows of x and W.  Softmax minus one-hot is held to 2^-22 of itself or 2^-38.  gx and gW are within what fp32 sums give with
+ * those, but add over rows that need one scale: gx[t] is besides off by up to 2^-38 |g_t| max |W| sum_v |softmax - one-hot|, gW[v] by up to
+ * 2^-38 max_t(|g_t| max_k |x[t, k]|) sum_t |softmax - one-hot|.
+ * Infinity or NaN in a row of x or in its gradient g_t: that row's loss and gx, and gW (both types); in W: every row.
  * reduction: IMUNPACK_NONE: loss has one fp32 per row; SUM, MEAN (over the rows that take part; 0 if there are none): one fp32.
  * loss (device) may be NULL if gradients are asked for, gx and gW (device) may each be NULL.  The gradients are made in the same call,
  * with the logits in memory for some rows at a time: they are those for grad, the gradient of loss (device, as many values; NULL: 1, not

@@ -11,8 +11,13 @@
 // all on the matrix cores, and what is held does not grow with the rows.
 //
 // bfloat16 operands: products in bfloat16, G rounded to bfloat16.  fp32 operands: each value is the sum of two binary16 numbers
-// (22 bits of it; scaled by a power of two so that the operand's largest, or for the loss alone each long row's, lies below 2^15) and a
+// (22 bits of it, and no finer than 2^-25 under a scale) and a
 // product is three of them, which is within the rounding of a binary32 sum; three times the instructions at eight times and more the rate of the binary32 ones.
+// The scale, a power of two, puts the largest finite magnitude below 2^15: the operand's where its rows are much alike, else (kSpan) each row's own, so
+// that a huge or infinite row costs its neighbours nothing.  A sum over the rows of an operand needs one scale for all: where they have
+// their own, the operand is split again in between, W for gx = G W and x for gW = G^T x.  What is then lost lies 2^-39 below the operand's largest value.  With a
+// gradient to each row's loss that goes to x for gW (which is split again with it) and to the finished rows of gx, so that a
+// row's own gradient is no coarser for a neighbour's.
 #include "common.h"
 #include "elements.h"
 #include "product.h"
@@ -24,6 +29,8 @@
 namespace imu {
 constexpr int64_t kPieceBytes = 2ll << 30;  // G of a piece of the rows at most (or 256 rows)
 constexpr int kTop = 14;                    // the largest magnitude of a scaled operand is below 2^(kTop + 1)
+constexpr int kSpan = 8;                    // powers of two between the rows' largest magnitudes beyond which each row has a scale of its own (up to
+                                            // there what one scale rounds off lies 2^-31 below the largest value of the row)
 constexpr unsigned kCus = 256;
 constexpr int kXentSlots = 256;             // parts of the tiles of a gradient that go at a time: one to a CU
 constexpr int kPartTiles = 2;               // k-tiles of a part at least (1: as fast; 4: 100 x 1024 by 16000 bf16 58.0 -> 59.5 us)
@@ -32,16 +39,26 @@ constexpr int kJoinRows = 8;
 constexpr int64_t kJoinReads = 1 << 22;     // parts read, by every workgroup of a row, up to which those join them that turn the exponentials
 constexpr int kLargeRows = 1024;            // rows from which the logits may go in large tiles
 
+// The largest finite magnitude in some rows (its bits) and the largest exponent of a row's scale (rows of zeros have none) plus kFinest.
+struct Largest {
+    int32_t top, finest;
+    __device__ void with(const Largest &o) {
+        top = max(top, o.top);
+        finest = max(finest, o.finest);
+    }
+};
+constexpr int kFinest = 1024;
 struct XentHeader {
     int32_t count;    // rows with a target
     int32_t bad;      // rows whose target is outside the vocabulary
-    uint32_t amax[2]; // bits of the largest magnitude of x (rows with a target) and of W
-    int32_t gexp;     // exponent of the largest gradient of a row (where each has its own)
+    uint32_t amax[2]; // bits of the largest finite magnitude of x (rows with a target) and of W
+    int32_t wide[2];  // rows of x, of W have scales of their own in the logits
+    int32_t gexp;     // where each row has a gradient: exponent of the largest (bfloat16), of the scale of x times them (fp32)
     uint32_t joined;  // workgroups that have left the losses of their rows
-    int32_t pad[58];
-    uint32_t found[kScanGroups];  // largest magnitudes as the workgroups found them
+    int32_t pad[56];
+    Largest found[kScanGroups];  // as the workgroups found them
 };
-static_assert(sizeof(XentHeader) == 256 + 4 * kScanGroups, "header");
+static_assert(sizeof(XentHeader) == 256 + 8 * kScanGroups, "header");
 // Rows of the piece that begins at row `first` and has room for `room`.
 __device__ __forceinline__ int rows_of(const XentHeader *hdr, int first, int room) { return max(0, min(hdr->count - first, room)); }
 
@@ -72,17 +89,21 @@ struct ScanArgs {
     float *loss;                 // where each row has a loss of its own
     const float *x, *w;          // fp32: whose largest magnitudes are wanted
     int64_t ldx, ldw;
+    int32_t *own_x, *own_w;      // exponents of the rows' own scales
     int rows, d, nx;             // nx: workgroups that look at x
 };
 __device__ __forceinline__ bool has_target(const ScanArgs &a, int64_t v) { return v >= 0 && v < a.vocab && v != a.ignore; }
 
-// The largest magnitude of rows first, first + step, ... of a matrix; x: of those with a target.  A wave takes four rows at a time.
+// What `largest` finds in rows first, first + step, ... of a matrix, and the exponent of each row's scale; x: of those with a target.  A wave takes
+// four rows at a time; all of its lanes have the results.
+__device__ __forceinline__ int over_wave(int v) { return from_lane63(wave_max_nonneg_lane63(v)); }
 template <bool X>
-__device__ __forceinline__ float largest(const ScanArgs &a, const float *m, int64_t ld, int64_t rows, int first, int step) {
+__device__ __forceinline__ Largest largest(const ScanArgs &a, const float *m, int64_t ld, int64_t rows, int first, int step, int32_t *own) {
     const int lane = threadIdx.x & 63;
-    float top = 0.0f;
+    Largest l = {0, 0};
     for (int64_t row = (int64_t)first * 4; row < rows; row += (int64_t)step * 4) {
         int n[4];
+        float top[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int r = 0; r < 4; ++r) n[r] = row + r < rows && (!X || has_target(a, a.target[row + r])) ? a.d : 0;
         for (int col = lane * 4; col < a.d; col += 256) {
@@ -92,10 +113,26 @@ __device__ __forceinline__ float largest(const ScanArgs &a, const float *m, int6
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) top = fmaxf(top, fabsf(f[r][k]));
+                for (int k = 0; k < 4; ++k) top[r] = fmaxf(top[r], fabsf(f[r][k]));
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (n[r] == 0) continue;
+            float t = __uint_as_float((uint32_t)over_wave((int)__float_as_uint(top[r])));
+            if (t == __builtin_inff()) {  // (the whole wave) once more, without what is infinite
+                t = 0.0f;
+                for (int col = lane; col < a.d; col += 64) {
+                    const float v = fabsf(m[(row + r) * ld + col]);
+                    t = v < __builtin_inff() ? fmaxf(t, v) : t;
+                }
+                t = __uint_as_float((uint32_t)over_wave((int)__float_as_uint(t)));
+            }
+            const int e = scale_exponent(__float_as_uint(t));
+            if (lane == 0) own[row + r] = e;
+            l.with({(int)__float_as_uint(t), t > 0.0f ? e + kFinest : 0});
         }
     }
-    return top;
+    return l;
 }
 
 // Rows with a target in order (also in `own`), their targets, and for every row its place among them (-1: none, -2: a target outside the
@@ -143,13 +180,19 @@ __device__ __forceinline__ int scan_rows(const ScanArgs &a, int32_t (*sums)[16],
 // Workgroup 0: the rows.  The others (fp32): the largest magnitudes of x and W (50265 x 768: 38 us, 4.1 TB/s).
 __global__ __launch_bounds__(1024) void xent_scan_kernel(const ScanArgs a) {
     __shared__ int32_t sums[2][16];
-    __shared__ float lds[16];
+    __shared__ Largest found[16];
     if (blockIdx.x > 0) {
         const int wave = threadIdx.x >> 6;
         const int g = blockIdx.x - 1, nx = a.nx;
-        float m = g < nx ? largest<true>(a, a.x, a.ldx, a.rows, g * 16 + wave, nx * 16) : largest<false>(a, a.w, a.ldw, a.vocab, (g - nx) * 16 + wave, ((int)gridDim.x - 1 - nx) * 16);
-        m = reduce_threads<1024, true>(m, lds);
-        if (threadIdx.x == 0) a.hdr->found[g] = __float_as_uint(m);
+        Largest l = g < nx ? largest<true>(a, a.x, a.ldx, a.rows, g * 16 + wave, nx * 16, a.own_x)
+                                 : largest<false>(a, a.w, a.ldw, a.vocab, (g - nx) * 16 + wave, ((int)gridDim.x - 1 - nx) * 16, a.own_w);
+        if ((threadIdx.x & 63) == 0) found[wave] = l;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int w = 1; w < 16; ++w) l.with(found[w]);
+            a.hdr->found[g] = l;
+        }
         return;
     }
     scan_rows(a, sums, nullptr, true);
@@ -169,8 +212,21 @@ struct PrepareArgs {
     char *px, *pw;            // x (gathered) and W in 16 bits, rows of `pieces` times 16 bytes
     int64_t xrows, wrows;     // rows there is room for; rows of W that are wanted
     int d, pieces, xgroups, nx, nw;  // workgroups that work on x; nx, nw: workgroups that looked for the largest magnitudes
-    int32_t *ex, *ew;         // the loss alone, fp32: what 2 to their power a row of x, of W is multiplied with
+    const int32_t *own_x;     // fp32: exponents of the scales of the rows of x before they are gathered
+    int32_t *ex, *ew;         // what 2 to their power a row of x, of W is multiplied with; ew: the rows' own before
 };
+// Eight columns of a row as two binary16 numbers each.
+__device__ __forceinline__ void store_split(char *to, const float (&f)[8]) {
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const _Float16 h0 = (_Float16)f[2 * k], h1 = (_Float16)f[2 * k + 1];
+        hi[k] = pack(h0, h1);
+        lo[k] = pack((_Float16)(f[2 * k] - (float)h0), (_Float16)(f[2 * k + 1] - (float)h1));
+    }
+    *reinterpret_cast<v4i32 *>(to) = v4i32{(int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    *reinterpret_cast<v4i32 *>(to + kSecond) = v4i32{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3]};
+}
 constexpr int kPrepareTurns = 4, kScanHere = 1024;
 // Eight columns of a row at a time: binary32 as two binary16 numbers, bfloat16 as it is; zeros behind the last column and, to a whole
 // k-tile, behind the last row of x.  Bound by memory: 50265 x 768 fp32 55 us, 5.6 TB/s (what it reads is in the
@@ -180,7 +236,7 @@ template <class T, bool SCAN>
 __global__ __launch_bounds__(SCAN ? 1024 : 256) void xent_prepare_kernel(const PrepareArgs a) {
     constexpr bool SPLIT = sizeof(T) == 4;
     constexpr int kThreads = SCAN ? 1024 : 256;
-    __shared__ float lds[4];
+    __shared__ Largest found[4];
     __shared__ int32_t sums[2][16], own[SCAN ? kScanHere : 1];
     const bool isX = (int)blockIdx.x < a.xgroups;
     const int group = isX ? blockIdx.x : blockIdx.x - a.xgroups;
@@ -194,15 +250,28 @@ __global__ __launch_bounds__(SCAN ? 1024 : 256) void xent_prepare_kernel(const P
         }
     }
     const int64_t rows = isX ? min((count + kStageCols - 1) / kStageCols * kStageCols, a.xrows) : count;
-    float scale = 1.0f;
-    int e = 0;
-    if constexpr (SPLIT) {  // the first workgroup of either operand leaves the largest magnitude for the kernels behind
-        float m = 0.0f;
-        for (int k = threadIdx.x; k < (isX ? a.nx : a.nw); k += 256) m = fmaxf(m, __uint_as_float(a.hdr->found[isX ? k : a.nx + k]));
-        m = reduce_threads<256, true>(m, lds);
-        e = scale_exponent(__float_as_uint(m));
-        scale = power_of_two(e);
-        if (threadIdx.x == 0 && group == 0) a.hdr->amax[isX ? 0 : 1] = __float_as_uint(m);
+    int common = 0;
+    bool wide = false;
+    if constexpr (SPLIT) {  // the first workgroup of either operand leaves what was found for the kernels behind
+        Largest l = {0, 0}, some[kScanGroups / 256];
+#pragma unroll
+        for (int i = 0; i < kScanGroups / 256; ++i) {
+            const int k = threadIdx.x + 256 * i;
+            some[i] = k < (isX ? a.nx : a.nw) ? a.hdr->found[isX ? k : a.nx + k] : Largest{0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < kScanGroups / 256; ++i) l.with(some[i]);
+        l = {over_wave(l.top), over_wave(l.finest)};
+        if ((threadIdx.x & 63) == 0) found[threadIdx.x >> 6] = l;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) l.with(found[w]);
+        common = scale_exponent((uint32_t)l.top);
+        wide = l.finest - kFinest - common > kSpan;
+        if (threadIdx.x == 0 && group == 0) {
+            a.hdr->amax[isX ? 0 : 1] = (uint32_t)l.top;
+            a.hdr->wide[isX ? 0 : 1] = wide;
+        }
     }
     const int64_t at0 = (int64_t)group * kThreads * kPrepareTurns + threadIdx.x;
     int64_t row[kPrepareTurns];
@@ -221,38 +290,90 @@ __global__ __launch_bounds__(SCAN ? 1024 : 256) void xent_prepare_kernel(const P
 #pragma unroll
     for (int i = 0; i < kPrepareTurns; ++i) {
         if (row[i] >= rows) continue;
-        if (SPLIT && a.ex && col[i] == 0 && row[i] < count) (isX ? a.ex : a.ew)[row[i]] = e;
         char *to = (isX ? a.px : a.pw) + row[i] * a.pieces * (SPLIT ? 32 : 16) + byte_of<SPLIT>(col[i]);
-        uint32_t hi[4], lo[4];
+        if constexpr (SPLIT) {
+            int e = common;
+            if (wide && row[i] < count) e = isX ? a.own_x[a.source[row[i]]] : a.ew[row[i]];
+            if (col[i] == 0 && row[i] < count && (isX || !wide)) (isX ? a.ex : a.ew)[row[i]] = e;
+            const float scale = power_of_two(e);
+            float v[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const T u = f[i][k >> 1][2 * (k & 1)], v = f[i][k >> 1][2 * (k & 1) + 1];
-            if constexpr (SPLIT) {
-                const float a0 = u * scale, a1 = v * scale;
-                const _Float16 h0 = (_Float16)a0, h1 = (_Float16)a1;
-                hi[k] = pack(h0, h1);
-                lo[k] = pack((_Float16)(a0 - (float)h0), (_Float16)(a1 - (float)h1));
-            } else {
-                hi[k] = pack(u, v);
-            }
+            for (int k = 0; k < 8; ++k) v[k] = f[i][k >> 2][k & 3] * scale;
+            store_split(to, v);
+        } else {
+            uint32_t q[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) q[k] = pack(f[i][k >> 1][2 * (k & 1)], f[i][k >> 1][2 * (k & 1) + 1]);
+            *reinterpret_cast<v4i32 *>(to) = v4i32{(int)q[0], (int)q[1], (int)q[2], (int)q[3]};
         }
-        *reinterpret_cast<v4i32 *>(to) = v4i32{(int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-        if constexpr (SPLIT) *reinterpret_cast<v4i32 *>(to + kSecond) = v4i32{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3]};
     }
 }
 
-// The gradient of each row's loss, as a factor between -2 and 2 and a power of two that the results are multiplied with at the end.
+// The gradient of each row's loss.  One for all: G has a factor between -2 and 2 of it, and the results are multiplied with a power of two at the end.
+// One for each row: G has them under one power of two (bfloat16), or not at all (fp32: gx and x have them, see below).
 struct Upstream {
-    const float *grad, *g;  // grad: nullptr for 1; g: the rows' factors where each has a gradient of its own, else nullptr
-    int mean;
+    const float *grad, *g;  // grad: nullptr for 1; g: bfloat16, the rows' factors where each has a gradient of its own, else nullptr
+    int mean, rows;         // rows: fp32, each row has a gradient of its own
     __device__ __forceinline__ float whole(const XentHeader *hdr) const {
         const float one = grad ? *grad : 1.0f;
         return mean ? one / (float)max(hdr->count, 1) : one;
     }
     __device__ __forceinline__ static int exponent_of(float m) { return fabsf(m) > 0.0f ? (int)(__float_as_uint(fabsf(m)) >> 23) - 127 : 0; }
-    __device__ __forceinline__ int exponent(const XentHeader *hdr) const { return g ? hdr->gexp : exponent_of(whole(hdr)); }
-    __device__ __forceinline__ float one(const XentHeader *hdr) const { return ldexpf(whole(hdr), -exponent_of(whole(hdr))); }
+    __device__ __forceinline__ int exponent(const XentHeader *hdr) const { return rows ? 0 : g ? hdr->gexp : exponent_of(whole(hdr)); }
+    __device__ __forceinline__ float one(const XentHeader *hdr) const { return rows ? 1.0f : ldexpf(whole(hdr), -exponent_of(whole(hdr))); }
+    // Of the scale of x in gW's product.
+    __device__ __forceinline__ int scale_x(const XentHeader *hdr) const { return rows ? hdr->gexp : scale_exponent(hdr->amax[0]); }
 };
+
+// fp32: the operands of the gradients' products whose rows have scales of their own are split again under one scale: W for gx, and x, with the rows'
+// gradients where each has one, for gW.  (Else nothing: the logits' operands are these.)  By all workgroups of a launch.
+struct AlignArgs {
+    const float *x, *w;       // nullptr: not wanted
+    int64_t ldx, ldw, pitch;
+    char *px, *pw;
+    const int32_t *source, *own_x, *ew;
+    int d, vocab;
+};
+template <class S>
+__device__ __forceinline__ void split_rows(const float *m, int64_t ld, char *to, int64_t pitch, int64_t rows, int d, S &&scaled) {
+    const int pieces = (int)(pitch / 32);  // (two numbers of eight columns)
+    for (int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; at < rows * pieces; at += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t row = at / pieces;
+        const int col = (int)(at - row * pieces) * 8;
+        const int64_t from = scaled.row(row);
+        float f[8];
+        load_upto<float, 8>(m + from * ld + col, f, d - col);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] = scaled(f[k], row, from);
+        store_split(to + row * pitch + byte_of<true>(col), f);
+    }
+}
+struct ScaledWeights {
+    const int32_t *ew;  // nullptr: one scale
+    int common;
+    __device__ int64_t row(int64_t v) const { return v; }
+    __device__ float operator()(float x, int64_t v, int64_t) const { return x * power_of_two(ew ? ew[v] : common); }
+};
+struct ScaledInputs {
+    const int32_t *source, *own;
+    const float *grad;  // nullptr: without
+    int common;
+    __device__ int64_t row(int64_t t) const { return source[t]; }
+    __device__ float operator()(float x, int64_t, int64_t t) const {
+        if (!grad) return x * power_of_two(common);
+        const int e = own[t], eg = Upstream::exponent_of(grad[t]);  // (neither factor nor their product leaves binary32's range; what the last step rounds is below 2^-39 of the largest)
+        return ldexpf(x * power_of_two(e) * ldexpf(grad[t], -eg), common - e + eg);
+    }
+};
+__device__ __forceinline__ void align_operands(const AlignArgs &a, const XentHeader *hdr, bool wide_x, bool wide_w, const Upstream &up, int first, int rows) {
+    if (a.w && wide_w) split_rows(a.w, a.ldw, a.pw, a.pitch, a.vocab, a.d, ScaledWeights{nullptr, scale_exponent(hdr->amax[1])});
+    if (a.x && (wide_x || up.rows))
+        split_rows(a.x, a.ldx, a.px + first * a.pitch, a.pitch, rows, a.d, ScaledInputs{a.source + first, a.own_x, up.rows ? up.grad : nullptr, up.scale_x(hdr)});
+}
+// Back to the rows' own scales, for the logits of the next piece.
+__global__ __launch_bounds__(256) void xent_weights_kernel(const AlignArgs a, const XentHeader *hdr) {
+    if (hdr->wide[1]) split_rows(a.w, a.ldw, a.pw, a.pitch, a.vocab, a.d, ScaledWeights{a.ew, 0});
+}
 
 // The same row by row, for the loss alone: each row by its own largest magnitude, which no other kernel has to look for.  A wave to a row,
 // which it reads twice (the second time out of a cache).  32003 x 1031 60 us, 4.5 TB/s.
@@ -298,16 +419,10 @@ __global__ __launch_bounds__(256) void xent_prepare_rows_kernel(const PrepareRow
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (col + 512 * i >= a.pitch / 4) break;
-            uint32_t hi[4], lo[4];
+            float v[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float a0 = f[i][k >> 1][2 * (k & 1)] * scale, a1 = f[i][k >> 1][2 * (k & 1) + 1] * scale;
-                const _Float16 h0 = (_Float16)a0, h1 = (_Float16)a1;
-                hi[k] = pack(h0, h1);
-                lo[k] = pack((_Float16)(a0 - (float)h0), (_Float16)(a1 - (float)h1));
-            }
-            *reinterpret_cast<v4i32 *>(to + byte_of<true>(col + 512 * i)) = v4i32{(int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-            *reinterpret_cast<v4i32 *>(to + byte_of<true>(col + 512 * i) + kSecond) = v4i32{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3]};
+            for (int k = 0; k < 8; ++k) v[k] = f[i][k >> 2][k & 3] * scale;
+            store_split(to + byte_of<true>(col + 512 * i), v);
         }
     }
 }
@@ -316,7 +431,7 @@ struct LogitArgs {
     Operand w, x;             // rows of the vocabulary and of the piece
     const XentHeader *hdr;
     const int32_t *wanted;
-    const int32_t *ex, *ew;   // the loss alone, fp32: exponents of the rows' scales
+    const int32_t *ex, *ew;   // fp32: exponents of the rows' scales
     float *stats, *hit;       // [part of the vocabulary][row of the piece] largest logit and sum; the target's logit
     char *P;                  // [row of the piece][vocabulary] exponentials, relative to the largest of the row and part, times 2^kTop where they are binary16
     int64_t pitch_P;
@@ -358,8 +473,6 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
     product_tile<F16, T, T, false, false>(a.w, x, tm * kEdge, tn * kEdge, 0, a.ktiles, smem, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, lhalf = lane >> 5;
     const int vwave = tm * kEdge + (wave >> 1) * 32 * T, twave = tn * kEdge + (wave & 1) * 32 * T;  // the wave's first column and row of the piece
-    const int down = F16 && KEEP ? -(scale_exponent(a.hdr->amax[0]) + scale_exponent(a.hdr->amax[1])) : 0;
-    auto logit = [&](float x) __attribute__((always_inline)) { return F16 && KEEP ? ldexpf(x, down) : x; };
     // FULL: no column behind the vocabulary and no row behind the last one in the wave's part (nothing to compare)
     auto finish = [&](auto full) __attribute__((always_inline)) {
         constexpr bool FULL = decltype(full)::value;
@@ -371,8 +484,8 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
             const bool hits = hit_at >= 0 && hit_at < 32 * T;
             const int left = vocab - vwave - 4 * lhalf, own = hit_at - 4 * lhalf;  // the lane has columns 32 i + 8 q + k
             float top = -__builtin_inff(), sum = 0.0f;
-            if constexpr (F16 && !KEEP) {
-                const int ex = in_rows ? a.ex[t] : 0;
+            if constexpr (F16) {
+                const int ex = in_rows ? a.ex[a.first + t] : 0;
 #pragma unroll
                 for (int i = 0; i < T; ++i)
 #pragma unroll
@@ -387,8 +500,8 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (FULL || 32 * i + (r >> 2) * 8 + (r & 3) < left) top = fmaxf(top, acc[i][j][r]);
-            top = logit(fmaxf(top, __shfl_xor(top, 32)));
-            const float from = top == -__builtin_inff() ? 0.0f : -top * kLog2e;  // (nothing of the vocabulary in this part)
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float from = top == -__builtin_inff() ? 0.0f : top;  // (nothing of the vocabulary in this part)
             if (__ballot(hits) != 0) {
                 float hit = 0.0f;
 #pragma unroll
@@ -396,7 +509,7 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
                         if (32 * i + (r >> 2) * 8 + (r & 3) == own) hit = acc[i][j][r];
-                if (hits && ((hit_at >> 2) & 1) == lhalf) a.hit[a.first + t] = logit(hit);
+                if (hits && ((hit_at >> 2) & 1) == lhalf) a.hit[a.first + t] = hit;
             }
             char *to = a.P + t * a.pitch_P + byte_of<F16>(vwave) + 16 * lhalf;
 #pragma unroll
@@ -404,7 +517,7 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
                 float p[16];
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    p[r] = __builtin_amdgcn_exp2f(fmaf(logit(acc[i][j][r]), kLog2e, from));
+                    p[r] = fast_exp(acc[i][j][r] - from);  // (not log2 e of either: of large logits the difference of the rounded products is none)
                     if (FULL || 32 * i + (r >> 2) * 8 + (r & 3) < left) sum += p[r];
                 }
                 if constexpr (KEEP) {
@@ -505,8 +618,8 @@ __global__ __launch_bounds__(256) void xent_few_kernel(const FewArgs a) {
     float top = fmaxf(l0, l1);
 #pragma unroll
     for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
-    const float from = top == -__builtin_inff() ? 0.0f : -top * kLog2e;
-    float s = __builtin_amdgcn_exp2f(fmaf(l0, kLog2e, from)) + __builtin_amdgcn_exp2f(fmaf(l1, kLog2e, from));
+    const float from = top == -__builtin_inff() ? 0.0f : top;
+    float s = fast_exp(l0 - from) + fast_exp(l1 - from);
 #pragma unroll
     for (int m = 16; m > 0; m >>= 1) s += __shfl_xor(s, m);
     const int own = a.wanted[r] - v0;
@@ -585,22 +698,30 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const JoinArgs a) {
     rows_losses(a, blockIdx.x, l, sh);
 }
 
-// Factors and exponent of the rows' own gradients.
-__global__ __launch_bounds__(1024) void xent_factor_kernel(const float *grad, XentHeader *hdr, const int32_t *source, float *g) {
+// Factors of the rows' own gradients (bfloat16) and their exponent, or that of the scale of x times them (fp32: each below 2^(kTop + 1)).  Gradients that are
+// infinite or NaN do not count: they would make zeros of the others.
+template <bool F16>
+__global__ __launch_bounds__(1024) void xent_factor_kernel(const float *grad, XentHeader *hdr, const int32_t *source, const int32_t *own_x, float *g) {
     __shared__ float lds[16];
     const int count = hdr->count;
-    float m = 0.0f;
-    for (int t = threadIdx.x; t < count; t += 1024) m = fmaxf(m, fabsf(grad[source[t]]));
-    m = reduce_threads<1024, true>(m, lds);
-    const int e = Upstream::exponent_of(m);
-    if (threadIdx.x == 0) hdr->gexp = e;
-    for (int t = threadIdx.x; t < count; t += 1024) g[t] = ldexpf(grad[source[t]], -e);
+    float top = -1024.0f;
+    for (int t = threadIdx.x; t < count; t += 1024) {
+        const int s = source[t];
+        const float m = fabsf(grad[s]);
+        if (m > 0.0f && m < __builtin_inff()) top = fmaxf(top, (float)(Upstream::exponent_of(m) - (F16 ? own_x[s] : 0)));
+    }
+    top = reduce_threads<1024, true>(top, lds);
+    const int e = top > -1024.0f ? (int)top : 0;
+    if (threadIdx.x == 0) hdr->gexp = F16 ? -1 - e : e;
+    if constexpr (!F16)
+        for (int t = threadIdx.x; t < count; t += 1024) g[t] = ldexpf(grad[source[t]], -e);
 }
 
 struct TurnArgs {
     JoinArgs join;
     const int32_t *wanted;
     Upstream up;
+    AlignArgs align;
     char *P;
     int64_t pitch_P;
 };
@@ -614,7 +735,9 @@ __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
     static_assert(!JOIN || ROWS == kJoinRows, "the rows of a workgroup");
     const JoinArgs &j = a.join;
     const int across = (j.vocab + 255) / 256, group_y = blockIdx.x / across, group_x = blockIdx.x - group_y * across;  // (rows can be too many for a grid's second axis)
+    const bool wide_x = F16 && j.hdr->wide[0], wide_w = F16 && j.hdr->wide[1];
     const int rows = rows_of(j.hdr, j.first, j.room), last = (rows + kStageCols - 1) / kStageCols * kStageCols;
+    if constexpr (F16) align_operands(a.align, j.hdr, wide_x, wide_w, a.up, j.first, rows);
     const int row0 = group_y * ROWS + (threadIdx.x >> 5), v0 = group_x * 256 + (threadIdx.x & 31) * 8, left = j.vocab - v0;
     const bool losses = JOIN && group_x == 0 && group_y < max(1, (rows + ROWS - 1) / ROWS);
     if (group_y * ROWS >= last && !losses) return;
@@ -746,7 +869,7 @@ __device__ __forceinline__ void grad_tile(const GradArgs &a, int wg, char *smem)
                 }
         return;
     }
-    const int e = a.up.exponent(a.hdr) - (F16 ? kTop + scale_exponent(a.hdr->amax[0]) : 0);
+    const int e = a.up.exponent(a.hdr) - (F16 ? kTop + a.up.scale_x(a.hdr) : 0);
     const int v0 = tm * kEdge + r0, f0 = tn * kEdge + c0;
 #pragma unroll
     for (int i = 0; i < T; ++i)
@@ -836,7 +959,14 @@ __global__ __launch_bounds__(256) void xent_fold_kernel(const FoldArgs a) {
         for (int w = 1; w < 4; ++w) { s[0] += sums[w][lane].x; s[1] += sums[w][lane].y; s[2] += sums[w][lane].z; s[3] += sums[w][lane].w; }
     }
     if (col >= a.d) return;
-    const int e = a.up.exponent(a.hdr) - (sizeof(T) == 4 ? kTop + scale_exponent(a.hdr->amax[isX ? 1 : 0]) : 0);
+    int e = a.up.exponent(a.hdr) - (sizeof(T) == 4 ? kTop + (isX ? scale_exponent(a.hdr->amax[1]) : a.up.scale_x(a.hdr)) : 0);
+    if (sizeof(T) == 4 && a.up.rows && isX && place >= 0) {  // the row's own gradient
+        const float g = a.up.grad[row];
+        const int eg = Upstream::exponent_of(g);
+        e += eg;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[k] *= ldexpf(g, -eg);
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) s[k] = ldexpf(s[k], e);
     store_upto<T, 4>((T *)(isX ? a.gx : a.gw) + row * (isX ? a.ldgx : a.ldgw) + col, s, a.d - col);
@@ -872,7 +1002,7 @@ struct XentLayout {
     Cut cut[2];                   // of the gradients, with tiles of 128 and of 256
     bool few;                     // W is read as it is
     bool by_rows;                 // each row of x and W has a scale of its own
-    size_t source, place, wanted, lse, row_loss, hit, g, ex, ew, stats, px, pw, P, xparts, wparts, bytes;
+    size_t source, place, wanted, lse, row_loss, hit, g, ex, ew, own_x, stats, px, pw, P, xparts, wparts, bytes;
 };
 static XentLayout xent_layout(const void *w, int64_t ldw, int64_t rows, int64_t d, int64_t vocab, int dtype, bool grad) {
     XentLayout l = {};
@@ -894,7 +1024,7 @@ static XentLayout xent_layout(const void *w, int64_t ldw, int64_t rows, int64_t 
     // (a wave to a row: 1418 x 1031 by 32003 rows 83 -> 60 us for both passes over the operands, but 64 x 85 by 16360 10 -> 16)
     l.few = l.split && !grad && rows <= kFewRows && vocab * d * 4 > kLastLevelCache;
     l.by_rows = l.split && !grad && !l.few && d >= 512;
-    l.ex = take(grad ? 0 : rows * 4); l.ew = take(grad ? 0 : l.vp * 4);
+    l.ex = take(l.split ? rows * 4 : 0); l.ew = take(l.split ? l.vp * 4 : 0); l.own_x = take(l.split ? rows * 4 : 0);
     l.stats = take(2 * (up(vocab, 128) / 128) * l.room * 8);  // (two parts to a tile)
     l.pitch_p = l.dp * 2 * numbers;
     l.px = take(l.tp * l.pitch_p);
@@ -1006,6 +1136,7 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
     c.target = target; c.vocab = vocab; c.ignore = ignore_index; c.hdr = hdr; c.source = source; c.place = place; c.wanted = wanted;
     c.loss = reduction == IMUNPACK_NONE ? loss : nullptr;
     c.x = (const float *)x; c.w = (const float *)w; c.ldx = ldx; c.ldw = ldw; c.rows = (int)rows; c.d = (int)d;
+    c.own_x = (int32_t *)(s + l.own_x); c.own_w = (int32_t *)(s + l.ew);
     // (workgroups of 16 waves, a wave to four rows)
     const int nx = (int)std::min<int64_t>(up(rows, 64) / 64, kScanX), nw = (int)std::min<int64_t>(up(vocab, 64) / 64, kScanGroups - kScanX);
     c.nx = nx;
@@ -1023,18 +1154,20 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
         p.x = x; p.w = w; p.ldx = ldx; p.ldw = ldw; p.hdr = hdr; p.source = source;
         p.px = s + l.px; p.pw = s + l.pw;
         p.xrows = l.tp; p.wrows = l.direct ? 0 : vocab; p.d = (int)d; p.pieces = (int)(l.dp / 8); p.nx = nx; p.nw = nw;
-        p.ex = back ? nullptr : (int32_t *)(s + l.ex); p.ew = (int32_t *)(s + l.ew);
+        p.own_x = c.own_x; p.ex = (int32_t *)(s + l.ex); p.ew = (int32_t *)(s + l.ew);
         const int64_t threads = scans ? 1024 : 256, per = threads * kPrepareTurns;
         p.xgroups = (int)((up(rows, kStageCols) * p.pieces + per - 1) / per);
         const dim3 grid((unsigned)(p.xgroups + (p.wrows * p.pieces + per - 1) / per));
         if (l.split) hipLaunchKernelGGL((xent_prepare_kernel<float, false>), grid, dim3(256), 0, st, p);
         else hipLaunchKernelGGL((scans ? xent_prepare_kernel<__bf16, true> : xent_prepare_kernel<__bf16, false>), grid, dim3((unsigned)threads), 0, st, p);
     }
-    Upstream upstream = {grad, nullptr, reduction == IMUNPACK_MEAN};
+    Upstream upstream = {grad, nullptr, reduction == IMUNPACK_MEAN, l.split && reduction == IMUNPACK_NONE};
     if (back && reduction == IMUNPACK_NONE) {
-        upstream.g = (const float *)(s + l.g);
-        hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, grad, hdr, source, (float *)(s + l.g));
+        if (!l.split) upstream.g = (const float *)(s + l.g);
+        hipLaunchKernelGGL((l.split ? xent_factor_kernel<true> : xent_factor_kernel<false>), dim3(1), dim3(1024), 0, st, grad, hdr, source, c.own_x, (float *)(s + l.g));
     }
+    const AlignArgs align = {gw ? (const float *)x : nullptr, gx ? (const float *)w : nullptr, ldx, ldw, l.pitch_p, s + l.px, s + l.pw, source, c.own_x,
+                             (const int32_t *)(s + l.ew), (int)d, (int)vocab};
     for (int64_t piece = 0; piece < l.pieces; ++piece) {
         const int64_t first = piece * l.room, n = std::min(l.room, rows - first);  // rows of the piece at most
         const int held = (int)(l.pitch_p / 2);  // (zeros behind the features)
@@ -1044,6 +1177,7 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
             FewArgs a = {(const float *)x, (const float *)w, ldx, ldw, hdr, source, wanted, (float *)(s + l.stats), (float *)(s + l.hit), (int)l.room, (int)d, (int)vocab};
             hipLaunchKernelGGL(xent_few_kernel, dim3((unsigned)(2 * (up(vocab, 128) / 128))), dim3(256), 0, st, a);
         } else if (n > 0) {
+            if (l.split && gx && piece > 0) hipLaunchKernelGGL(xent_weights_kernel, dim3(4 * kCus), dim3(256), 0, st, align, hdr);
             LogitArgs a = {};
             a.w = whole; a.x = part;
             a.ex = (const int32_t *)(s + l.ex); a.ew = (const int32_t *)(s + l.ew);
@@ -1063,7 +1197,7 @@ extern "C" int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t 
         if (!back) continue;
         if (n > 0) {
             TurnArgs t = {};
-            t.join = j; t.wanted = wanted; t.up = upstream; t.P = s + l.P; t.pitch_P = l.pitch_P;
+            t.join = j; t.wanted = wanted; t.up = upstream; t.align = align; t.P = s + l.P; t.pitch_P = l.pitch_P;
             const dim3 grid(across * (down / (few ? 8 : 32)));
             if (l.split) hipLaunchKernelGGL((joins ? xent_turn_kernel<true, 8, true> : few ? xent_turn_kernel<true, 8, false> : xent_turn_kernel<true, 32, false>), grid, dim3(256), 0, st, t);
             else hipLaunchKernelGGL((joins ? xent_turn_kernel<false, 8, true> : few ? xent_turn_kernel<false, 8, false> : xent_turn_kernel<false, 32, false>), grid, dim3(256), 0, st, t);

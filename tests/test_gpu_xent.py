@@ -396,3 +396,95 @@ def test_refusals(imu):
         imu.imunpack_xent_backward(x, w, t, saved, torch.ones((), device="cuda").double())
     with pytest.raises(ValueError):
         imu.imunpack_xent_backward(x, w[:, :7], t, saved, torch.ones((), device="cuda"))
+
+
+def of(value, rows):
+    """What `reference` gave, in some rows."""
+    return value[0][rows], value[1][rows]
+
+
+@pytest.mark.parametrize("d", [64, 128, 511, 520, 1031])
+@pytest.mark.parametrize("bad", ["inf", "nan", 1e6, 1e12, 1e30])
+def test_a_huge_or_infinite_row_stays_to_itself(imu, d, bad):
+    """fp32, rows from 1e-3 to a huge one: the others' losses and gradients are what they are without it.  gW adds over the rows, so that it
+    knows each to 2^-38 of the largest one's values."""
+    x, w, target, grad = inputs(60, d, 1000, torch.float32, 0.9, d)
+    x[3] *= 1e-3
+    x[7] = x[7] * bad if isinstance(bad, float) else x[7]
+    if bad in ("inf", "nan"):
+        x[7, d // 2] = float(bad)
+    target[7] = 11
+    keep = torch.arange(60, device="cuda") != 7
+    clean = torch.where(keep[:, None], x, 0.0)
+    valid, loss, gx, _ = reference(clean, w, target, grad, torch.float32)
+    got, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+    within(got[keep], of(loss, keep))
+    a, b = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    within(a[keep], of(gx, keep))
+    n = float(valid.sum())
+    _, saved = imu.imunpack_xent(x, w, target, reduction="mean", want_grad=True)
+    a1, b1 = imu.imunpack_xent_backward(x, w, target, saved, torch.ones((), device="cuda"))
+    _, _, gx, _ = reference(clean, w, target, torch.full_like(grad, 1.0 / n), torch.float32)
+    within(a1[keep], of(gx, keep))
+    if bad in ("inf", "nan"):
+        assert not torch.isfinite(got[7]) and not torch.isfinite(a[7]).any()
+        return
+    for upstream, gw in ((grad, b), (torch.full_like(grad, 1.0 / n), b1)):
+        _, _, _, want = reference(x, w, target, upstream, torch.float32)
+        p = torch.softmax(x.to(F) @ w.to(F).t(), 1)
+        p = p.scatter_add(1, torch.where(valid, target, 0)[:, None], torch.full((60, 1), -1.0, dtype=F, device="cuda")) * valid[:, None]
+        more = 2.0 ** -38 * float((upstream.to(F).abs()[:, None] * x.to(F).abs() * valid[:, None]).max()) * p.abs().sum(0)[:, None]
+        within(gw, (want[0], want[1] + more))
+
+
+@pytest.mark.parametrize("rows,d,vocab", [(60, 64, 1000), (60, 520, 700), (1100, 1024, 8300), (4300, 70, 66000)])
+@pytest.mark.parametrize("size", [1e6, 1e12])
+def test_a_huge_row_of_the_weights(imu, rows, d, vocab, size):
+    """fp32: a word that no row of x takes (its logits lie far below the others) changes nothing but the bound of gx, which adds over
+    the rows of W and knows each to 2^-38 of the largest one's values.  The last size goes through in two pieces."""
+    x, w, target, grad = inputs(rows, d, vocab, torch.float32, 0.9, rows + d)
+    x[:, 0] = x[:, 0].abs() + 0.5
+    w[5] = 0.0
+    w[5, 0] = -size
+    w[6] = 0.0
+    w[7] *= 1e-4
+    target[target == 5] = 9
+    others = torch.cat([w[:5], w[6:]])
+    shifted = torch.where(target > 5, target - 1, target)
+    got, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+    a, b = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    alone, _ = imu.imunpack_xent(x, w, target, reduction="none")
+    for part in range(0, rows, 1024):
+        r = slice(part, part + 1024)
+        valid, loss, gx, gw = reference(x[r], others, shifted[r], grad[r], torch.float32)
+        within(got[r], loss)
+        within(alone[r], loss)
+        l = x[r].to(F) @ others.to(F).t()
+        p = torch.exp(l - torch.logsumexp(l, 1, keepdim=True)).scatter_add(1, torch.where(valid, shifted[r], 0)[:, None], torch.full((l.shape[0], 1), -1.0, dtype=F, device="cuda"))
+        within(a[r], (gx[0], gx[1] + 2.0 ** -38 * size * (p.abs().sum(1) * grad[r].to(F).abs() * valid)[:, None]))
+        total = gw if part == 0 else (total[0] + gw[0], total[1] + gw[1])
+    within(torch.cat([b[:5], b[6:]]), (total[0], total[1] + sums(rows, torch.float32) * total[0].abs()))
+    assert not b[5].any()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradients_of_the_rows_far_apart(imu, dtype):
+    """Each row's loss has its own gradient, from 1e-15 to 1e15: gx of a row is as exact as if it were alone, and an infinite one stays in its row."""
+    x, w, target, grad = inputs(64, 96, 300, dtype, 1.0, 31)
+    grad = grad.sign() * (10.0 ** torch.linspace(-15, 15, 64, device="cuda"))
+    _, saved = imu.imunpack_xent(x, w, target, reduction="none", want_grad=True)
+    a, b = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    for t in range(64):
+        _, _, gx, _ = reference(x[t:t + 1], w, target[t:t + 1], grad[t:t + 1], dtype)
+        within(a[t:t + 1], gx)
+    _, _, _, gw = reference(x, w, target, grad, dtype)
+    within(b, gw)
+    grad[9] = float("inf")
+    grad[10] = float("nan")
+    a2, _ = imu.imunpack_xent_backward(x, w, target, saved, grad)
+    keep = torch.ones(64, dtype=torch.bool, device="cuda")
+    keep[[9, 10]] = False
+    assert not torch.isfinite(a2[9]).any() and torch.isnan(a2[10]).all()
+    for t in torch.nonzero(keep)[:, 0].tolist():
+        _, _, gx, _ = reference(x[t:t + 1], w, target[t:t + 1], grad[t:t + 1], dtype)
+        within(a2[t:t + 1], gx)
