@@ -3,7 +3,8 @@
     loss_t = log sum_v exp(x_t . W_v) - x_t . W_target(t)
 
 The head's product and its two gradients run inside the library, a piece of the rows at a time; the gradients of a mean or a sum are made
-by the forward pass, while the product is there, and multiplied with what arrives from above by the backward pass.  Rows whose target is
+by the forward pass, while the product is there, and multiplied with what arrives from above by the backward pass.  Where none will be
+asked for (``torch.no_grad``, operands without ``requires_grad``) the loss alone is taken.  Rows whose target is
 ``ignore_index`` take no part.  fp32 or bfloat16 (both operands alike).
 """
 from __future__ import annotations
@@ -34,6 +35,8 @@ class _LossFunction(torch.autograd.Function):
 def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, ignore_index: int = -100, reduction: str = "mean") -> torch.Tensor:
     """x [..., d], weight [vocab, d], target int64 [...]: the mean (over rows with a target; 0 if there are none), the sum, or with
     "none" the loss of every row, in fp32."""
+    if not (torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad)):  # (what an autograd function is told of its inputs does not know no_grad)
+        return imu.imunpack_xent(x, weight, target, ignore_index, reduction)[0]
     return _LossFunction.apply(x, weight, target, ignore_index, reduction)
 
 

@@ -488,3 +488,20 @@ def test_gradients_of_the_rows_far_apart(imu, dtype):
     for t in torch.nonzero(keep)[:, 0].tolist():
         _, _, gx, _ = reference(x[t:t + 1], w, target[t:t + 1], grad[t:t + 1], dtype)
         within(a2[t:t + 1], gx)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_module_without_gradients_takes_the_loss_alone(imu, dtype):
+    from paper_2403_07339_amd import loss as L
+    x, w, target, _ = inputs(300, 256, 20000, dtype, 0.8, 41)
+    head = L.LinearCrossEntropy(256, 20000, device="cuda", dtype=dtype)
+    with torch.no_grad():
+        head.weight.copy_(w)
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        torch.cuda.reset_peak_memory_stats()
+        value = head(x, target)
+        assert torch.cuda.max_memory_allocated() - before < (24 << 20 if dtype == torch.float32 else 6 << 20)   # the split operands or none, but neither gW nor G (24 MB)
+    assert torch.equal(value, imu.imunpack_xent(x, w, target)[0])
+    with_gradients = head(x, target)
+    assert with_gradients.requires_grad and abs(float(with_gradients.detach()) - float(value)) < 1e-4
