@@ -35,7 +35,11 @@ class AdamW(torch.optim.Optimizer):
         return st
 
     def load_state_dict(self, state_dict):
-        """As torch.optim.Optimizer, which turns states into the parameters' type; codes become codes again (exactly)."""
+        """As torch.optim.Optimizer, which turns states into the parameters' type; codes become codes again (exactly).  States of the other
+        width are refused: their numbers mean something else."""
+        for st in state_dict["state"].values():
+            if ("exp_avg_scale" in st) != (self.state_bits == 8):
+                raise ValueError(f"the states to load have {8 if 'exp_avg_scale' in st else 32} bits, this optimiser's {self.state_bits}")
         super().load_state_dict(state_dict)
         if self.state_bits == 8:
             for st in self.state.values():

@@ -35,3 +35,40 @@ def test_loss_makes_gradients_only_where_they_may_be_asked_for(imu, monkeypatch,
     assert head(x, target).requires_grad and asked[-1] == (True, False, True)
     loss.linear_cross_entropy(x.clone().requires_grad_(), head.weight.detach(), target, reduction=reduction)
     assert asked[-1] == (True, True, False)
+
+
+@pytest.fixture
+def adamw_calls(imu, monkeypatch):
+    """optim.AdamW on the CPU: the step's formulas in torch, and what each call of the binding was given."""
+    calls = []
+
+    def adamw(params, grads, exp_avg, exp_avg_sq, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, m_scales=None, v_scales=None, copies=None, seed=0):
+        calls.append(dict(params=params, grads=grads, step=step, seed=seed & 0xFFFFFFFF, copies=copies))
+        for k, (p, g, m, v) in enumerate(zip(params, grads, exp_avg, exp_avg_sq)):
+            if g.dtype not in (torch.float32, torch.bfloat16) or not all(t.is_contiguous() for t in (p, g, m, v)):
+                raise ValueError("adamw: a tensor of the wrong type or layout")
+            if m_scales is None:
+                m.lerp_(g.float(), 1 - beta1)
+                v.lerp_(g.float() ** 2, 1 - beta2)
+                p.mul_(1 - lr * weight_decay).addcdiv_(m, (v / (1 - beta2 ** step)).sqrt() + eps, value=-lr / (1 - beta1 ** step))
+                if copies is not None:
+                    copies[k].copy_(p)
+
+    monkeypatch.setattr(imu, "imunpack_adamw", adamw)
+    return calls
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_states_of_the_other_width_are_refused(adamw_calls, bits):
+    from paper_2403_07339_amd import optim
+    def make(bits):
+        p = torch.nn.Parameter(torch.ones(512))   # (as many codes as elements)
+        p.grad = torch.ones(512)
+        o = optim.AdamW([p], state_bits=bits)
+        o.step()
+        return o
+    mine, other = make(bits), make(40 - bits)
+    with pytest.raises(ValueError):
+        mine.load_state_dict(other.state_dict())
+    mine.load_state_dict(make(bits).state_dict())
+    optim.AdamW([torch.nn.Parameter(torch.ones(512))], state_bits=bits).load_state_dict(mine.state_dict())
