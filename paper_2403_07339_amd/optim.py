@@ -67,4 +67,5 @@ class AdamW(torch.optim.Optimizer):
                                    lr=group["lr"], beta1=group["betas"][0], beta2=group["betas"][1], eps=group["eps"], weight_decay=group["weight_decay"],
                                    m_scales=[s["exp_avg_scale"] for s in sts] if eight else None, v_scales=[s["exp_avg_sq_scale"] for s in sts] if eight else None,
                                    copies=[self.copies[p] for p in ps] if copied else None, seed=self.seed + 0x10001 * index)
+                torch.autograd.graph.increment_version(ps + [self.copies[p] for p in ps] if copied else ps)  # (the library writes past autograd)
         return loss

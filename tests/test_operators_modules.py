@@ -52,7 +52,7 @@ def adamw_calls(imu, monkeypatch):
                 v.lerp_(g.float() ** 2, 1 - beta2)
                 p.mul_(1 - lr * weight_decay).addcdiv_(m, (v / (1 - beta2 ** step)).sqrt() + eps, value=-lr / (1 - beta1 ** step))
                 if copies is not None:
-                    copies[k].copy_(p)
+                    copies[k].data.copy_(p)
 
     monkeypatch.setattr(imu, "imunpack_adamw", adamw)
     return calls
@@ -72,3 +72,17 @@ def test_states_of_the_other_width_are_refused(adamw_calls, bits):
         mine.load_state_dict(other.state_dict())
     mine.load_state_dict(make(bits).state_dict())
     optim.AdamW([torch.nn.Parameter(torch.ones(512))], state_bits=bits).load_state_dict(mine.state_dict())
+
+
+def test_a_step_is_seen_by_autograd(adamw_calls):
+    """A graph that saved a parameter before the step must not go backward with the new values."""
+    from paper_2403_07339_amd import optim
+    p, copy = torch.nn.Parameter(torch.ones(4)), torch.ones(4, dtype=torch.bfloat16)
+    idle = torch.nn.Parameter(torch.ones(4))
+    y = (p * p).sum() + (idle * idle).sum()
+    p.grad = torch.ones(4)
+    before = copy._version
+    optim.AdamW([p, idle], copies={p: copy}).step()
+    assert copy._version > before and idle._version == 0
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
