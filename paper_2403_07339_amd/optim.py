@@ -60,12 +60,12 @@ class AdamW(torch.optim.Optimizer):
                 st = self._state(p)
                 st["step"] += 1
                 calls.setdefault((st["step"], p.grad.dtype, p in self.copies), []).append((p, st))
-            for (step, _, copied), some in calls.items():
+            for number, ((step, _, copied), some) in enumerate(calls.items()):
                 ps, sts = [p for p, _ in some], [s for _, s in some]
                 eight = self.state_bits == 8
                 imu.imunpack_adamw([p.data for p in ps], [p.grad.contiguous() for p in ps], [s["exp_avg"] for s in sts], [s["exp_avg_sq"] for s in sts], step,
                                    lr=group["lr"], beta1=group["betas"][0], beta2=group["betas"][1], eps=group["eps"], weight_decay=group["weight_decay"],
                                    m_scales=[s["exp_avg_scale"] for s in sts] if eight else None, v_scales=[s["exp_avg_sq_scale"] for s in sts] if eight else None,
-                                   copies=[self.copies[p] for p in ps] if copied else None, seed=self.seed + 0x10001 * index)
+                                   copies=[self.copies[p] for p in ps] if copied else None, seed=self.seed + 0x10001 * index + 0x3C6EF35F * number)
                 torch.autograd.graph.increment_version(ps + [self.copies[p] for p in ps] if copied else ps)  # (the library writes past autograd)
         return loss

@@ -86,3 +86,23 @@ def test_a_step_is_seen_by_autograd(adamw_calls):
     assert copy._version > before and idle._version == 0
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.backward()
+
+
+def test_calls_of_one_step_round_with_their_own_random_bits(adamw_calls):
+    """Gradients of two types, or some parameters with copies, go in calls of their own, each of which numbers its tensors from 0."""
+    from paper_2403_07339_amd import optim
+    ps = [torch.nn.Parameter(torch.ones(4)) for _ in range(6)]
+    o = optim.AdamW([dict(params=ps[:3]), dict(params=ps[3:])], state_bits=8, seed=5, copies={p: torch.ones(4, dtype=torch.bfloat16) for p in (ps[1], ps[2], ps[4])})
+    for _ in range(2):
+        for p in ps:
+            p.grad = torch.ones(4)
+        o.step()
+    assert len(adamw_calls) == 8 and adamw_calls[0]["seed"] == 5
+    assert len({c["seed"] for c in adamw_calls[:4]}) == 4
+    # the kernel's key of a call is made of seed + step * 0x9E3779B1: no two calls of a few thousand steps meet there
+    seeds = [c["seed"] for c in adamw_calls[:4]]
+    keys = {(s + t * 0x9E3779B1) & 0xFFFFFFFF for s in seeds for t in range(1, 5001)}
+    assert len(keys) == 4 * 5000
+    again = optim.AdamW([dict(params=ps[:3]), dict(params=ps[3:])], state_bits=8, seed=5, copies=o.copies)
+    again.step()
+    assert [c["seed"] for c in adamw_calls[8:]] == seeds
