@@ -58,8 +58,7 @@ class AdamW(torch.optim.Optimizer):
                 if p.grad is None:
                     continue
                 st = self._state(p)
-                st["step"] += 1
-                calls.setdefault((st["step"], p.grad.dtype, p in self.copies), []).append((p, st))
+                calls.setdefault((st["step"] + 1, p.grad.dtype, p in self.copies), []).append((p, st))
             for number, ((step, _, copied), some) in enumerate(calls.items()):
                 ps, sts = [p for p, _ in some], [s for _, s in some]
                 eight = self.state_bits == 8
@@ -67,5 +66,7 @@ class AdamW(torch.optim.Optimizer):
                                    lr=group["lr"], beta1=group["betas"][0], beta2=group["betas"][1], eps=group["eps"], weight_decay=group["weight_decay"],
                                    m_scales=[s["exp_avg_scale"] for s in sts] if eight else None, v_scales=[s["exp_avg_sq_scale"] for s in sts] if eight else None,
                                    copies=[self.copies[p] for p in ps] if copied else None, seed=self.seed + 0x10001 * index + 0x3C6EF35F * number)
+                for st in sts:
+                    st["step"] = step
                 torch.autograd.graph.increment_version(ps + [self.copies[p] for p in ps] if copied else ps)  # (the library writes past autograd)
         return loss

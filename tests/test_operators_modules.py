@@ -106,3 +106,13 @@ def test_calls_of_one_step_round_with_their_own_random_bits(adamw_calls):
     again = optim.AdamW([dict(params=ps[:3]), dict(params=ps[3:])], state_bits=8, seed=5, copies=o.copies)
     again.step()
     assert [c["seed"] for c in adamw_calls[8:]] == seeds
+
+
+def test_a_refused_step_is_none(adamw_calls):
+    from paper_2403_07339_amd import optim
+    p = torch.nn.Parameter(torch.ones(4, dtype=torch.float64))
+    o = optim.AdamW([p])
+    p.grad = torch.ones(4, dtype=torch.float64)
+    with pytest.raises(ValueError):
+        o.step()
+    assert o.state[p]["step"] == 0
