@@ -6,11 +6,16 @@ import torch
 from . import binding as imu
 
 
+def _capturing() -> bool:
+    return torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing()
+
+
 class AdamW(torch.optim.Optimizer):
     """Decoupled weight decay, bias-corrected averages, fp32 parameters (``state_bits``: 32, or 8 for e4m3 codes of the first
     average and of the root of the second with a scale per 256 elements; ``seed``: of the rounding of 8-bit states).
     Parameters whose ``grad`` is None are left out of a step.  ``copies``: a dict from parameters to bfloat16 tensors that
-    every step refreshes (working copies for a product in bfloat16)."""
+    every step refreshes (working copies for a product in bfloat16; a gradient of theirs is not read).
+    A step is not for capture in a graph, which would repeat its number and its random bits."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, state_bits: int = 32,
                  seed: int = 0, copies: dict | None = None):
@@ -48,6 +53,8 @@ class AdamW(torch.optim.Optimizer):
 
     @torch.no_grad()
     def step(self, closure=None):
+        if _capturing():
+            raise RuntimeError("a step of AdamW cannot be captured: a graph would repeat its number and its random bits")
         loss = None
         if closure is not None:
             with torch.enable_grad():

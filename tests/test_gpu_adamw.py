@@ -214,3 +214,20 @@ def test_refusals(imu):
     from paper_2403_07339_amd import optim
     with pytest.raises(ValueError):
         optim.AdamW([torch.nn.Parameter(p)], state_bits=16)
+
+
+def test_a_step_in_a_graph_is_refused(imu):
+    from paper_2403_07339_amd import optim
+    p = torch.nn.Parameter(torch.ones(8, device="cuda"))
+    p.grad = torch.ones(8, device="cuda")
+    o = optim.AdamW([p])
+    o.step()
+    was = p.detach().clone()
+    scratch = torch.zeros(8, device="cuda")
+    with pytest.raises(RuntimeError, match="captured"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            scratch += 1.0
+            o.step()
+    assert torch.equal(p.detach(), was) and o.state[p]["step"] == 1
+    o.step()
+    assert o.state[p]["step"] == 2

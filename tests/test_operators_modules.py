@@ -116,3 +116,15 @@ def test_a_refused_step_is_none(adamw_calls):
     with pytest.raises(ValueError):
         o.step()
     assert o.state[p]["step"] == 0
+
+
+def test_a_step_is_not_captured(adamw_calls, monkeypatch):
+    """The step's number and its random bits are arguments: a graph would repeat those of the captured step."""
+    from paper_2403_07339_amd import optim
+    monkeypatch.setattr(optim, "_capturing", lambda: True)
+    p = torch.nn.Parameter(torch.ones(4))
+    p.grad = torch.ones(4)
+    o = optim.AdamW([p])
+    with pytest.raises(RuntimeError, match="captured"):
+        o.step()
+    assert not adamw_calls and not o.state
