@@ -31,7 +31,7 @@ class AdamW(torch.optim.Optimizer):
         if not st:
             st["step"] = 0
             if self.state_bits == 32:
-                st["exp_avg"], st["exp_avg_sq"] = torch.zeros_like(p), torch.zeros_like(p)
+                st["exp_avg"], st["exp_avg_sq"] = (torch.zeros_like(p, memory_format=torch.contiguous_format) for _ in range(2))
             else:
                 blocks = -(-p.numel() // imu.ADAMW_BLOCK)
                 for name in ("exp_avg", "exp_avg_sq"):
@@ -69,11 +69,14 @@ class AdamW(torch.optim.Optimizer):
             for number, ((step, _, copied), some) in enumerate(calls.items()):
                 ps, sts = [p for p, _ in some], [s for _, s in some]
                 eight = self.state_bits == 8
-                imu.imunpack_adamw([p.data for p in ps], [p.grad.contiguous() for p in ps], [s["exp_avg"] for s in sts], [s["exp_avg_sq"] for s in sts], step,
+                dense = [p.data if p.is_contiguous() else p.data.contiguous() for p in ps]
+                imu.imunpack_adamw(dense, [p.grad.contiguous() for p in ps], [s["exp_avg"] for s in sts], [s["exp_avg_sq"] for s in sts], step,
                                    lr=group["lr"], beta1=group["betas"][0], beta2=group["betas"][1], eps=group["eps"], weight_decay=group["weight_decay"],
                                    m_scales=[s["exp_avg_scale"] for s in sts] if eight else None, v_scales=[s["exp_avg_sq_scale"] for s in sts] if eight else None,
                                    copies=[self.copies[p] for p in ps] if copied else None, seed=self.seed + 0x10001 * index + 0x3C6EF35F * number)
-                for st in sts:
+                for p, q, st in zip(ps, dense, sts):
                     st["step"] = step
+                    if not p.is_contiguous():
+                        p.data.copy_(q)
                 torch.autograd.graph.increment_version(ps + [self.copies[p] for p in ps] if copied else ps)  # (the library writes past autograd)
         return loss

@@ -128,3 +128,31 @@ def test_a_step_is_not_captured(adamw_calls, monkeypatch):
     with pytest.raises(RuntimeError, match="captured"):
         o.step()
     assert not adamw_calls and not o.state
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_parameters_of_any_layout(adamw_calls, bits):
+    """Transposed, strided and channels-last parameters step as their contiguous copies do."""
+    from paper_2403_07339_amd import optim
+    torch.manual_seed(1)
+    start = [torch.randn(6, 5).t(), torch.randn(8, 6)[:, ::2], torch.randn(2, 3, 4, 4).contiguous(memory_format=torch.channels_last), torch.randn(7)]
+    mine = [torch.nn.Parameter(t) for t in start]
+    want = [torch.nn.Parameter(t.detach().clone(memory_format=torch.contiguous_format)) for t in start]
+    assert [p.is_contiguous() for p in mine] == [False, False, False, True]
+    a, b = optim.AdamW(mine, state_bits=bits, lr=0.1), optim.AdamW(want, state_bits=bits, lr=0.1)
+    for k in range(3):
+        for p, q in zip(mine, want):
+            q.grad = torch.randn(q.shape)
+            p.grad = q.grad.clone()
+        if k == 2:
+            again = optim.AdamW(mine, state_bits=bits, lr=0.1)
+            again.load_state_dict(a.state_dict())
+            a = again
+        a.step()
+        b.step()
+    for p, q in zip(mine, want):
+        assert torch.equal(p, q) and p.stride() == start[mine_index(mine, p)].stride()
+
+
+def mine_index(some, one):
+    return next(k for k, p in enumerate(some) if p is one)
