@@ -25,6 +25,7 @@ constexpr int kAdamTensors = 48;      // to a launch: their table travels in the
 constexpr int kAdamBlock = 256;       // elements that share a scale
 constexpr int kAdamBlocks = 1;        // blocks of a wave (4: 85 million elements 383 -> 405 us, 0.27 million in 112 tensors 19 -> 25)
 constexpr int kAdamChunk = 4 * kAdamBlocks * kAdamBlock;  // elements of a workgroup
+constexpr int64_t kAdamGroups = (1 << 24) - 1;  // workgroups of a launch at most: 2^32 threads are more than a grid may have along an axis
 constexpr float kE4m3Max = 448.0f, kNothing = 0x1p-96f;  // a block of no more than that is held as zeros
 
 struct AdamArgs {
@@ -36,6 +37,7 @@ struct AdamArgs {
     int64_t n[kAdamTensors];
     int32_t first[kAdamTensors];  // workgroups before the tensor's
     int32_t count, base;          // tensors of this launch, and before it
+    int64_t skip;                 // workgroups' worth of a tensor that is too large for one launch, before this one
     uint32_t key;
     float beta1, rest1, beta2, rest2, decay, rate, root_scale, eps;
 };
@@ -97,7 +99,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamArgs a) {
     float *p = a.p[k];
     const G *g = (const G *)a.g[k];
     __bf16 *copy = a.copy[k];
-    const int64_t chunk = (int64_t)((int)blockIdx.x - a.first[k]) * kAdamChunk;
+    const int64_t chunk = ((int)blockIdx.x - a.first[k] + a.skip) * kAdamChunk;
     const uint32_t key = mix32(a.key + (uint32_t)(a.base + k) * kGolden);
     const int64_t at0 = chunk + wave * kAdamBlock + lane * 4;  // the wave's blocks lie four apart
     float P[kAdamBlocks][4], M[kAdamBlocks][4], V[kAdamBlocks][4];
@@ -206,6 +208,12 @@ extern "C" int imunpack_adamw(int64_t count, float *const *params, const void *c
     a.rate = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
     a.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
     a.eps = (float)eps;
+    auto launch = [&](int64_t groups) {
+        const bool bf16 = grad_dtype == IMUNPACK_BF16;
+        if (state_bits == 8) bf16 ? launch_adamw<true, __bf16>(a, (unsigned)groups, once, st) : launch_adamw<true, float>(a, (unsigned)groups, once, st);
+        else bf16 ? launch_adamw<false, __bf16>(a, (unsigned)groups, once, st) : launch_adamw<false, float>(a, (unsigned)groups, once, st);
+        return launch_status();
+    };
     for (int64_t k = 0; k < count;) {
         a.count = 0;
         a.base = (int32_t)k;
@@ -213,7 +221,7 @@ extern "C" int imunpack_adamw(int64_t count, float *const *params, const void *c
         for (; k < count && a.count < kAdamTensors; ++k) {
             const int i = a.count;
             const int64_t more = (numel[k] + kAdamChunk - 1) / kAdamChunk;
-            if (i > 0 && groups + more > 0x7fffffff / 2) break;
+            if (i > 0 && groups + more > kAdamGroups) break;
             a.p[i] = params[k]; a.g[i] = grads[k]; a.m[i] = exp_avg[k]; a.v[i] = exp_avg_sq[k];
             a.ms[i] = state_bits == 8 ? m_scales[k] : nullptr;
             a.vs[i] = state_bits == 8 ? v_scales[k] : nullptr;
@@ -222,12 +230,12 @@ extern "C" int imunpack_adamw(int64_t count, float *const *params, const void *c
             a.first[i] = (int32_t)groups;
             groups += more;
             ++a.count;
+            if (groups > kAdamGroups) {  // a tensor by itself
+                ++k;
+                break;
+            }
         }
-        if (groups == 0) continue;
-        const bool bf16 = grad_dtype == IMUNPACK_BF16;
-        if (state_bits == 8) bf16 ? launch_adamw<true, __bf16>(a, (unsigned)groups, once, st) : launch_adamw<true, float>(a, (unsigned)groups, once, st);
-        else bf16 ? launch_adamw<false, __bf16>(a, (unsigned)groups, once, st) : launch_adamw<false, float>(a, (unsigned)groups, once, st);
-        IMU_TRY(launch_status());
+        for (a.skip = 0; a.skip < groups; a.skip += kAdamGroups) IMU_TRY(launch(std::min(groups - a.skip, kAdamGroups)));
     }
     return IMUNPACK_OK;
 }

@@ -231,3 +231,29 @@ def test_a_step_in_a_graph_is_refused(imu):
     assert torch.equal(p.detach(), was) and o.state[p]["step"] == 1
     o.step()
     assert o.state[p]["step"] == 2
+
+
+def test_more_elements_than_one_launch_takes(imu):
+    """A tensor of more than 2^34 elements, with small ones on both sides of it in the list: what lies near its ends, near the edge between the
+    launches and anywhere between is what a tensor of its own gives (the update, without the codes' random bits)."""
+    big = (1 << 34) + 70000
+    if torch.cuda.mem_get_info()[0] + torch.cuda.memory_reserved() - torch.cuda.memory_allocated() < 9 * big:
+        pytest.skip("needs 150 GB of device memory")
+    torch.cuda.empty_cache()
+    sizes = [700, big, 300]
+    p = [torch.zeros(n, device="cuda") for n in sizes]
+    g = [torch.zeros(n, dtype=torch.bfloat16, device="cuda") for n in sizes]
+    whole = [-(-n // 256) for n in sizes]
+    code = lambda: [torch.zeros(256 * b, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for b in whole]  # noqa: E731
+    m, v, ms, vs = code(), code(), [torch.zeros(b, device="cuda") for b in whole], [torch.zeros(b, device="cuda") for b in whole]
+    edge = ((1 << 24) - 1) * 1024
+    places = [(0, 3), (1, 0), (1, 1 << 31), (1, edge - 1), (1, edge), (1, edge + 1023), (1, big - 1), (2, 299)]
+    for k, at in places:
+        g[k][at] = 0.5
+    imu.imunpack_adamw(p, g, m, v, step=1, lr=0.25, weight_decay=0.0, m_scales=ms, v_scales=vs)
+    for k, at in places:
+        assert abs(float(p[k][at]) + 0.25) < 1e-5 and float(m[k][at].float() * ms[k][at // 256]) != 0.0
+    assert [int(torch.count_nonzero(t)) for t in p] == [1, len(places) - 2, 1]
+    assert sum(int(torch.count_nonzero(t)) for t in ms) == len({(k, at // 256) for k, at in places})
+    del p, g, m, v, ms, vs
+    torch.cuda.empty_cache()
