@@ -8,7 +8,7 @@
 // joins them to lse: for the loss alone nothing else of l is left.  For the gradients the rows go through in pieces (as many as kPieceBytes
 // allows): the tiles leave their exponentials in 16 bits, relative to the largest of the row and part; once lse stands they become G where
 // they lie; gx and gW are products of it, and the next piece takes the same memory.  So l is made once: 6 T V d operations,
-// all on the matrix cores, and what is held does not grow with the rows.
+// all on the matrix cores, and what is held of l does not grow with the rows beyond a piece (for the loss alone kPieceBytes bounds what the tiles keep).
 //
 // bfloat16 operands: products in bfloat16, G rounded to bfloat16.  fp32 operands: each value is the sum of two binary16 numbers
 // (22 bits of it, and no finer than 2^-25 under a scale) and a
@@ -27,7 +27,7 @@
 #include <type_traits>
 
 namespace imu {
-constexpr int64_t kPieceBytes = 2ll << 30;  // G of a piece of the rows at most (or 256 rows)
+constexpr int64_t kPieceBytes = 2ll << 30;  // G of a piece of the rows at most (or 256 rows); for the loss alone, the parts' largest logits and sums
 constexpr int kTop = 14;                    // the largest magnitude of a scaled operand is below 2^(kTop + 1)
 constexpr int kSpan = 8;                    // powers of two between the rows' largest magnitudes beyond which each row has a scale of its own (up to
                                             // there what one scale rounds off lies 2^-31 below the largest value of the row)
@@ -1013,7 +1013,9 @@ static XentLayout xent_layout(const void *w, int64_t ldw, int64_t rows, int64_t 
     l.tp = up(std::max<int64_t>(rows, 1), 256);
     l.vp = up(vocab, 256);
     l.direct = !l.split && d % 8 == 0 && ldw % 8 == 0 && ldw <= 1 << 22 && (size_t)w % 16 == 0;  // (a tile's rows lie within 32 bits)
-    l.room = !grad ? l.tp : std::min(l.tp, std::max<int64_t>(256, kPieceBytes / (2 * numbers * l.vp) / 256 * 256));
+    // (for the loss alone that is 2^34 logits, whose tiles are few enough for a grid: with 2^38 its threads would pass 32 bits)
+    const int64_t row_bytes = grad ? 2 * numbers * l.vp : up(vocab, 128) / 64 * 8;
+    l.room = std::min(l.tp, std::max<int64_t>(256, kPieceBytes / row_bytes / 256 * 256));
     l.pieces = (l.tp + l.room - 1) / l.room;
     l.edge_l = logits_edge((int)std::min(rows, l.room), (int)d, (int)vocab);
     l.edge_g = grads_edge((int)std::min(rows, l.room), (int)d, (int)vocab);

@@ -505,3 +505,21 @@ def test_module_without_gradients_takes_the_loss_alone(imu, dtype):
     assert torch.equal(value, imu.imunpack_xent(x, w, target)[0])
     with_gradients = head(x, target)
     assert with_gradients.requires_grad and abs(float(with_gradients.detach()) - float(value)) < 1e-4
+
+
+@pytest.mark.parametrize("rows,vocab", [(1 << 21, 8300), (1 << 22, 66000)])
+def test_more_logits_than_one_launch_takes(imu, rows, vocab):
+    """The loss alone of more than 2^34 logits goes through in pieces; 2^38 of them in one launch would be more threads than a grid has.  The same
+    bits as its rows taken in parts, whose sizes do not come near that."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn(rows, 8, generator=g, device="cuda").bfloat16()
+    w = torch.randn(vocab, 8, generator=g, device="cuda").bfloat16()
+    target = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    target[::5] = -100
+    got, _ = imu.imunpack_xent(x, w, target, reduction="none")
+    for part in (slice(0, 4096), slice(rows // 2 - 1000, rows // 2 + 1000), slice(rows - 5000, rows)):
+        want, _ = imu.imunpack_xent(x[part], w, target[part], reduction="none")
+        assert torch.equal(got[part], want) and (want[target[part] >= 0] > 0).all()
+    one, _ = imu.imunpack_xent(x, w, target)
+    n = int((target >= 0).sum())
+    assert abs(float(one) - float(got.to(F).sum()) / n) <= (rows / 256 + 20) * U * float(got.to(F).sum()) / n
