@@ -4,6 +4,7 @@
 // the library returns.  No arithmetic, no GPU code; the library's functions come as addresses from the binding, which has loaded it.
 #include <Python.h>
 #include <ATen/ATen.h>
+#include <c10/core/impl/DeviceGuardImplInterface.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <array>
@@ -86,6 +87,10 @@ PyObject *wrapped(const std::array<at::Tensor, N> &ts) {
     return r;
 }
 
+// A kernel reads and writes one GPU's memory, and the stream that it is given is the current GPU's.
+bool beside(const at::Tensor &t, const at::Tensor &x) { return !t.defined() || t.device() == x.device(); }
+void need_current(const at::Device &device) { need(device == c10::impl::getDeviceGuardImpl(at::kCUDA)->getDevice(), "tensors of a GPU that is not the current one"); }
+
 // IMUNPACK_F32, IMUNPACK_BF16 or a refusal.
 int type_of(const at::Tensor &t, const char *what) {
     if (t.scalar_type() == at::kFloat) return IMUNPACK_F32;
@@ -122,6 +127,7 @@ Norm norm_arguments(const at::Tensor &x, const at::Tensor &weight, const at::Ten
     need(x.dim() >= 1, "rmsnorm: x has no dimension");
     const Norm n = {x.size(-1), type_of(x, "rmsnorm: x"), type_of(weight, "rmsnorm: weight")};
     need(weight.dim() == 1 && weight.size(0) == n.d && weight.is_contiguous(), "rmsnorm: weight is one dense row like x's");
+    need(beside(weight, x) && beside(residual, x), "rmsnorm: tensors of different devices");
     need(!residual.defined() || (residual.is_cuda() && residual.scalar_type() == x.scalar_type() && residual.sizes() == x.sizes()), "rmsnorm: residual must be like x");
     return n;
 }
@@ -131,6 +137,7 @@ PyObject *rmsnorm(PyObject *const *a) {  // x, weight, eps, residual, stream -> 
     const at::Tensor &x = tensor(a[0], "rmsnorm: x"), &weight = tensor(a[1], "rmsnorm: weight");
     const at::Tensor residual = maybe(a[3], "rmsnorm: residual");
     const Norm n = norm_arguments(x, weight, residual);
+    need_current(x.device());
     const Rows rx = spread(x, n.d), rr = spread(residual, n.d);
     const at::Tensor y = dense_like(x, x.scalar_type()), h = residual.defined() ? dense_like(x, x.scalar_type()) : x, rstd = per_row(x);
     check(g_rmsnorm(rx.p, rx.pitch, rr.p, rr.pitch, weight.data_ptr(), rstd.numel(), n.d, n.type, n.weight_type, (float)number(a[2]), y.data_ptr(), n.d,
@@ -142,6 +149,7 @@ PyObject *rmsnorm_quantize(PyObject *const *a) {  // x, weight, eps, b, residual
     const at::Tensor &x = tensor(a[0], "rmsnorm: x"), &weight = tensor(a[1], "rmsnorm: weight");
     const at::Tensor residual = maybe(a[4], "rmsnorm: residual");
     const Norm n = norm_arguments(x, weight, residual);
+    need_current(x.device());
     const Rows rx = spread(x, n.d), rr = spread(residual, n.d);
     const at::Tensor q = dense_like(x, at::kChar), scale = per_row(x), h = residual.defined() ? dense_like(x, x.scalar_type()) : x;
     const at::Tensor values = truth(a[5]) ? dense_like(x, x.scalar_type()) : at::Tensor();
@@ -159,6 +167,8 @@ PyObject *rmsnorm_backward(PyObject *const *a) {  // gy, x, residual, gh, weight
     need(like(gy) && (!gh.defined() || like(gh)), "rmsnorm: h, gy and gh must be like x");
     need(rstd.is_cuda() && rstd.scalar_type() == at::kFloat && rstd.is_contiguous() && rstd.sizes() == x.sizes().slice(0, x.dim() - 1),
          "rmsnorm: saved must be what imunpack_rmsnorm returned");
+    need(beside(gy, x) && beside(gh, x) && beside(rstd, x), "rmsnorm: tensors of different devices");
+    need_current(x.device());
     const Rows rg = spread(gy, n.d), rx = spread(x, n.d), rr = spread(residual, n.d), rh = spread(gh, n.d);
     const int64_t rows = rstd.numel();
     const at::Tensor gx = dense_like(x, x.scalar_type());
@@ -237,13 +247,13 @@ PyObject *adamw(PyObject *const *a) {  // params, grads, exp_avg, exp_avg_sq, m_
         vs = table(a[5], at::kFloat, blocks, device, "v_scales");
     }
     if (a[6] != Py_None) copies = table(a[6], at::kBFloat16, numel, device, "copies");
+    if (n > 0) need_current(device);
     check(g_adamw(n, (float *const *)p.data(), g.data(), m.data(), v.data(), eight ? (float *const *)ms.data() : nullptr, eight ? (float *const *)vs.data() : nullptr,
                   a[6] != Py_None ? copies.data() : nullptr, numel.data(), gtype == at::kFloat ? IMUNPACK_F32 : IMUNPACK_BF16, eight ? 8 : 32, number(a[7]), number(a[8]),
                   number(a[9]), number(a[10]), number(a[11]), whole(a[12]), (uint32_t)whole(a[13]), address(a[14])), "imunpack_adamw");
     Py_RETURN_NONE;
 }
 
-// error class, then the addresses of the library's functions
 struct Xent {  // the arguments that the loss and its gradients take, checked
     at::Tensor x, w, target;
     int64_t d, vocab, rows;
@@ -255,6 +265,7 @@ Xent xent_arguments(PyObject *const *a) {  // x, w, target
     need(n.w.scalar_type() == n.x.scalar_type() && n.x.is_cuda() && n.w.is_cuda(), "xent takes x and W as device tensors, both fp32 or both bfloat16");
     need(n.w.dim() == 2 && n.x.dim() >= 1 && n.x.size(-1) == n.w.size(1), "xent: x and W have no product x W^T");
     need(n.target.scalar_type() == at::kLong && n.target.is_cuda() && n.target.sizes() == n.x.sizes().slice(0, n.x.dim() - 1), "xent: target is an int64 device tensor of x's leading shape");
+    need(beside(n.w, n.x) && beside(n.target, n.x), "xent: tensors of different devices");
     n.d = n.w.size(1);
     n.vocab = n.w.size(0);
     n.rows = n.target.numel();
@@ -265,6 +276,8 @@ PyObject *xent(PyObject *const *a) {  // x, w, target, ignore_index, how, want_l
     const Xent n = xent_arguments(a);
     const int how = (int)whole(a[4]);
     const at::Tensor grad = maybe(a[6], "xent: grad"), target = n.target.contiguous();
+    need(beside(grad, n.x), "xent: tensors of different devices");
+    need_current(n.x.device());
     const Rows x = spread(n.x, n.d), w = spread(n.w, n.d);
     const at::TensorOptions floats = n.x.options().dtype(at::kFloat).requires_grad(false);
     const at::Tensor loss = !truth(a[5]) ? at::Tensor() : how == IMUNPACK_NONE ? at::empty(n.target.sizes(), floats) : at::empty({}, floats);
@@ -281,12 +294,14 @@ PyObject *xent_rescale(PyObject *const *a) {  // x, w, target, grad, gx, gw, str
     const Xent n = xent_arguments(a);
     const at::Tensor &grad = tensor(a[3], "xent: grad");
     const at::Tensor gx = maybe(a[4], "xent: gx"), gw = maybe(a[5], "xent: gw");
+    need(beside(grad, n.x) && beside(gx, n.x) && beside(gw, n.x), "xent: tensors of different devices");
+    need_current(n.x.device());
     check(g_xent_rescale((const float *)grad.data_ptr(), data(gx), gx.defined() ? gx.numel() : 0, data(gw), gw.defined() ? gw.numel() : 0, n.type, address(a[6])),
           "imunpack_xent_rescale");
     Py_RETURN_NONE;
 }
 
-PyObject *bind(PyObject *const *a) {
+PyObject *bind(PyObject *const *a) {  // error class, then the addresses of the library's functions
     Py_INCREF(a[0]);
     Py_XDECREF(g_error);
     g_error = a[0];

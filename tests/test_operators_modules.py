@@ -156,3 +156,43 @@ def test_parameters_of_any_layout(adamw_calls, bits):
 
 def mine_index(some, one):
     return next(k for k, p in enumerate(some) if p is one)
+
+
+def refused_on_other_devices(imu, one, other):
+    """Calls with a tensor of another device than the rest are refused, before anything is read or launched (fake tensors have no memory)."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    with FakeTensorMode():
+        def at(device, *shape, dtype=torch.float32):
+            return torch.empty(shape, device=device, dtype=dtype)
+        x, w, rstd = (lambda d: at(d, 4, 8)), (lambda d: at(d, 8)), (lambda d: at(d, 4))
+        target = lambda d: at(d, 4, dtype=torch.int64)  # noqa: E731
+        scalar, head = (lambda d: at(d)), (lambda d: at(d, 20, 8))
+        xent = imu.XentSaved
+        for make, call in (
+                ((x, w, x), lambda a, b, c: imu.imunpack_rmsnorm(a, b, residual=c)),
+                ((x, w, x), lambda a, b, c: imu.imunpack_rmsnorm_quantize(a, b, residual=c)),
+                ((x, x, w, rstd, x), lambda g, h, w, r, gh: imu.imunpack_rmsnorm_backward(g, h, w, imu.NormSaved(r), gh)),
+                ((x, head, target), lambda a, b, t: imu.imunpack_xent(a, b, t)),
+                ((x, head, target, scalar), lambda a, b, t, g: imu.imunpack_xent_backward(a, b, t, xent(-100, "mean"), g)),
+                ((x, head, target, scalar, x, head), lambda a, b, t, g, gx, gw: imu.imunpack_xent_backward(a, b, t, xent(-100, "mean", gx, gw), g)),
+                ((w, w, w, w), lambda p, g, m, v: imu.imunpack_adamw([p], [g], [m], [v], step=1))):
+            for k in range(len(make)):
+                with pytest.raises(ValueError):
+                    call(*[f(other if i == k else one) for i, f in enumerate(make)])
+
+
+def test_tensors_of_several_devices_are_refused(imu, monkeypatch):
+    monkeypatch.setattr(imu, "_stream", lambda: 0)
+    refused_on_other_devices(imu, "cuda:0", "cuda:1")
+
+
+@pytest.mark.gpu
+def test_tensors_of_another_device_than_the_current_are_refused(imu):
+    if torch.cuda.device_count() < 2:
+        pytest.skip("needs two devices")
+    x, w = torch.zeros(4, 8, device="cuda:1"), torch.zeros(8, device="cuda:1")
+    with torch.cuda.device(0):
+        for call in (lambda: imu.imunpack_rmsnorm(x, w), lambda: imu.imunpack_rmsnorm_quantize(x, w), lambda: imu.imunpack_adamw([w], [w], [w], [w], step=1),
+                     lambda: imu.imunpack_xent(x, torch.zeros(20, 8, device="cuda:1"), torch.zeros(4, dtype=torch.int64, device="cuda:1"))):
+            with pytest.raises(ValueError):
+                call()
