@@ -348,7 +348,7 @@ int imunpack_rmsnorm(const void *x, int64_t ldx, const void *residual, int64_t l
 /* The same norm with its output as integers that are In-Bound for bit width b (Sec. 4: |q| <= 2^(b-1) - 1, so as an operand of
  * imunpack_plan they are never split), in 8 bits with a step per row:
  *     scale = max_j |y_j| / (2^(b-1) - 1),   q_j = rint(y_j / scale)        (binary32 division, half to even)
- * scale: device, one fp32 per row; 1 for a row of zeros; NaN for a row that holds a NaN or an infinity (its q are 0).
+ * scale: device, one fp32 per row (below 2^-126 rounded up where its few bits would put a q_j beyond b bits); 1 for a row of zeros; NaN for a row that holds a NaN or an infinity (its q are 0).
  * values (device, dtype, may be NULL): q_j * scale, for callers that go on in dtype.  Other arguments and errors as above
  * (also EINVAL for b outside [2,8]). */
 int imunpack_rmsnorm_quantize(const void *x, int64_t ldx, const void *residual, int64_t ldres, const void *weight,

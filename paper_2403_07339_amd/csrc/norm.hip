@@ -41,7 +41,9 @@ struct NormArgs {
 
 // What a row's integers count; NaN for a row that holds a NaN or an infinity, 1 for a row of zeros.
 __device__ __forceinline__ float quant_scale(float amax, bool finite, float qmax) {
-    const float s = amax / qmax;
+    float s = amax / qmax;
+    // a step below 2^-126 has few bits: rounded down it would put the largest value beyond b bits, or be none
+    if (s < 0x1p-126f && amax > 0.0f && (s == 0.0f || rintf(amax / s) > qmax)) s = __uint_as_float(__float_as_uint(s) + 1);
     return !finite ? __builtin_nanf("") : s > 0.0f ? s : 1.0f;
 }
 template <class T, int N, bool ONCE>

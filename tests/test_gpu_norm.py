@@ -288,3 +288,17 @@ def test_gradient_in_the_place_of_what_it_is_made_from(imu, rows, d, dtype):
         at = gh.clone()
         got = call(gy, at, at)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("b", [8, 4, 2])
+def test_integers_of_next_to_nothing_are_in_bound(imu, b):
+    """y of 2 to 800 times 2^-149: rows with one element (their 1 / rms is exactly 2), weights of a few steps of binary32 below 2^-126."""
+    top, f = 2 ** (b - 1) - 1, torch.float64
+    x = torch.eye(4, device="cuda")
+    for first in range(1, 401, 4):
+        w = torch.arange(first, first + 4, dtype=torch.int32, device="cuda").view(torch.float32)
+        q, scale, _, values = imu.imunpack_rmsnorm_quantize(x, w, 0.0, b, want_values=True)
+        y = torch.diag(2.0 * w.to(f))
+        assert int(q.abs().max()) <= top and (torch.diag(q) != 0).all()
+        assert ((q.to(f) * scale.to(f)[:, None] - y).abs() <= 0.5 * scale.to(f)[:, None]).all()
+        assert torch.equal(values.to(f), q.to(f) * scale.to(f)[:, None])
