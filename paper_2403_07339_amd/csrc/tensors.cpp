@@ -8,6 +8,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <array>
+#include <optional>
 #include <stdexcept>
 #include <string>
 #include <vector>
@@ -184,19 +185,24 @@ PyObject *rmsnorm_backward(PyObject *const *a) {  // gy, x, residual, gh, weight
     return wrapped<2>({gx, gw});
 }
 
+// What can be iterated over, as a list that holds its tensors until the call is over (an iterator may be all that does).
+struct Listed {
+    PyObject *o;
+    explicit Listed(PyObject *list) : o(PySequence_Fast(list, "adamw takes lists of tensors")) {
+        if (!o) throw Raised();
+    }
+    Listed(const Listed &) = delete;
+    ~Listed() { Py_DECREF(o); }
+    Py_ssize_t size() const { return PySequence_Fast_GET_SIZE(o); }
+    const at::Tensor &operator()(Py_ssize_t k, const char *what) const { return tensor(PySequence_Fast_GET_ITEM(o, k), what); }
+};
 // The addresses of a list of dense tensors of one type, of given sizes, on one GPU.
-std::vector<void *> table(PyObject *list, at::ScalarType type, const std::vector<int64_t> &sizes, const at::Device &device, const char *what) {
-    PyObject *seq = PySequence_Fast(list, "adamw takes lists of tensors");
-    if (!seq) throw Raised();
-    struct Held {
-        PyObject *o;
-        ~Held() { Py_DECREF(o); }
-    } held{seq};
-    const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
+std::vector<void *> table(const Listed &list, at::ScalarType type, const std::vector<int64_t> &sizes, const at::Device &device, const char *what) {
+    const Py_ssize_t n = list.size();
     if ((size_t)n != sizes.size()) throw Refused("adamw: lists of different lengths");
     std::vector<void *> at(n);
     for (Py_ssize_t k = 0; k < n; ++k) {
-        const at::Tensor &t = tensor(PySequence_Fast_GET_ITEM(seq, k), what);
+        const at::Tensor &t = list(k, what);
         if (t.scalar_type() != type || t.device() != device || !t.is_contiguous() || t.numel() != sizes[k])
             throw Refused(std::string("adamw: ") + what + ": a tensor of the wrong type, size, device or layout");
         at[k] = t.data_ptr();
@@ -205,51 +211,39 @@ std::vector<void *> table(PyObject *list, at::ScalarType type, const std::vector
 }
 
 PyObject *adamw(PyObject *const *a) {  // params, grads, exp_avg, exp_avg_sq, m_scales, v_scales, copies, lr, beta1, beta2, eps, decay, step, seed, stream
-    PyObject *params = PySequence_Fast(a[0], "adamw takes lists of tensors");
-    if (!params) throw Raised();
+    const bool eight = a[4] != Py_None, copied = a[6] != Py_None;
+    const Listed params(a[0]), grads(a[1]), exp_avg(a[2]), exp_avg_sq(a[3]);
     std::vector<int64_t> numel, held, blocks;
     at::Device device(at::kCPU);
-    const Py_ssize_t n = PySequence_Fast_GET_SIZE(params);
-    const bool eight = a[4] != Py_None;
-    bool tensors = true;
-    for (Py_ssize_t k = 0; k < n && tensors; ++k) {
-        PyObject *o = PySequence_Fast_GET_ITEM(params, k);
-        tensors = THPVariable_Check(o);
-        if (!tensors) break;
-        const at::Tensor &t = THPVariable_Unpack(o);
+    const Py_ssize_t n = params.size();
+    for (Py_ssize_t k = 0; k < n; ++k) {
+        const at::Tensor &t = params(k, "adamw: params");
         if (k == 0) device = t.device();
         numel.push_back(t.numel());
         blocks.push_back((t.numel() + IMUNPACK_ADAMW_BLOCK - 1) / IMUNPACK_ADAMW_BLOCK);
         held.push_back(eight ? blocks.back() * IMUNPACK_ADAMW_BLOCK : t.numel());
     }
-    Py_DECREF(params);
-    need(tensors, "adamw: params: not a tensor");
     need(eight == (a[5] != Py_None), "adamw: scales for both states or for none");
     const at::ScalarType state = eight ? at::kFloat8_e4m3fn : at::kFloat;
     at::ScalarType gtype = at::kFloat;
     if (n > 0) {
         need(device.is_cuda(), "adamw takes device tensors");
-        PyObject *first = PySequence_GetItem(a[1], 0);
-        if (!first) {
-            PyErr_Clear();
-            throw Refused("adamw: lists of different lengths");
-        }
-        const bool is = THPVariable_Check(first);
-        if (is) gtype = THPVariable_Unpack(first).scalar_type();
-        Py_DECREF(first);
-        need(is && (gtype == at::kFloat || gtype == at::kBFloat16), "adamw: gradients are fp32 or bfloat16 tensors");
+        need(grads.size() == n, "adamw: lists of different lengths");
+        gtype = grads(0, "adamw: grads").scalar_type();
+        need(gtype == at::kFloat || gtype == at::kBFloat16, "adamw: gradients are fp32 or bfloat16 tensors");
     }
-    const auto p = table(a[0], at::kFloat, numel, device, "params"), g = table(a[1], gtype, numel, device, "grads");
-    const auto m = table(a[2], state, held, device, "exp_avg"), v = table(a[3], state, held, device, "exp_avg_sq");
+    const auto p = table(params, at::kFloat, numel, device, "params"), g = table(grads, gtype, numel, device, "grads");
+    const auto m = table(exp_avg, state, held, device, "exp_avg"), v = table(exp_avg_sq, state, held, device, "exp_avg_sq");
     std::vector<void *> ms, vs, copies;
+    std::optional<Listed> m_scales, v_scales, copy_list;
     if (eight) {
-        ms = table(a[4], at::kFloat, blocks, device, "m_scales");
-        vs = table(a[5], at::kFloat, blocks, device, "v_scales");
+        ms = table(m_scales.emplace(a[4]), at::kFloat, blocks, device, "m_scales");
+        vs = table(v_scales.emplace(a[5]), at::kFloat, blocks, device, "v_scales");
     }
-    if (a[6] != Py_None) copies = table(a[6], at::kBFloat16, numel, device, "copies");
+    if (copied) copies = table(copy_list.emplace(a[6]), at::kBFloat16, numel, device, "copies");
     if (n > 0) need_current(device);
     check(g_adamw(n, (float *const *)p.data(), g.data(), m.data(), v.data(), eight ? (float *const *)ms.data() : nullptr, eight ? (float *const *)vs.data() : nullptr,
-                  a[6] != Py_None ? copies.data() : nullptr, numel.data(), gtype == at::kFloat ? IMUNPACK_F32 : IMUNPACK_BF16, eight ? 8 : 32, number(a[7]), number(a[8]),
+                  copied ? copies.data() : nullptr, numel.data(), gtype == at::kFloat ? IMUNPACK_F32 : IMUNPACK_BF16, eight ? 8 : 32, number(a[7]), number(a[8]),
                   number(a[9]), number(a[10]), number(a[11]), whole(a[12]), (uint32_t)whole(a[13]), address(a[14])), "imunpack_adamw");
     Py_RETURN_NONE;
 }

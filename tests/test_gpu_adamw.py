@@ -257,3 +257,18 @@ def test_more_elements_than_one_launch_takes(imu):
     assert sum(int(torch.count_nonzero(t)) for t in ms) == len({(k, at // 256) for k, at in places})
     del p, g, m, v, ms, vs
     torch.cuda.empty_cache()
+
+
+def test_iterators_of_tensors(imu):
+    """Whatever yields the tensors, they are held until the kernels are launched."""
+    def make():
+        p, g = tensors([100, 3000, 7], 3)
+        copies = [torch.zeros_like(t, dtype=torch.bfloat16) for t in p]
+        return [p, g, [torch.zeros_like(t) for t in p], [torch.zeros_like(t) for t in p]], copies
+    (lists, copies), (other, copies2) = make(), make()
+    imu.imunpack_adamw(*lists, step=1, copies=copies)
+    imu.imunpack_adamw(*[(t[:] for t in some) for some in other], step=1, copies=tuple(copies2))
+    for a, b in zip(lists + [copies], other + [copies2]):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+    with pytest.raises(TypeError):
+        imu.imunpack_adamw(*lists[:3], 5, step=1)
