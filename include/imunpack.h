@@ -380,8 +380,9 @@ int imunpack_rmsnorm_backward(const void *gy, int64_t ldgy, const void *x, int64
  * state_bits 8: exp_avg[k] holds m and exp_avg_sq[k] the square root of v, as 8-bit floating-point codes (e4m3) times a scale (fp32)
  * for every IMUNPACK_ADAMW_BLOCK elements, m_scales[k] and v_scales[k]; codes go over whole blocks
  * (ceil(numel / block) * block bytes, what lies behind the tensor's end zero).  Codes are rounded up or down at random, with the
- * probability that leaves the mean unchanged, by a hash of seed, step, k and the element: the same call gives the same bits; a
- * root that is not zero keeps at least the smallest code.  All zeros is the state before the first step.
+ * probability that leaves the means of m and of the root unchanged, by a hash of seed, step, k and the element: the same call gives the same bits.  v,
+ * the root's square, is thereby about 5 % too large under gradients that keep their size, and the root scatters by some 16 %.  A root that is not zero keeps at
+ * least the smallest code, 2^-18 of the largest of its block.  All zeros is the state before the first step.
  * NaN and infinity in a gradient go into the element (32 bits) or the whole block (8 bits).
  * Errors: EINVAL (null pointers, lr, eps or weight_decay negative or not finite, a beta outside [0, 1), step < 1, unknown
  * types). */
@@ -407,9 +408,10 @@ int imunpack_adamw(int64_t count, float *const *params, const void *const *grads
  * reduction: IMUNPACK_NONE: loss has one fp32 per row; SUM, MEAN (over the rows that take part; 0 if there are none): one fp32.
  * loss (device) may be NULL if gradients are asked for, gx and gW (device) may each be NULL.  The gradients are made in the same call,
  * with the logits in memory for some rows at a time: they are those for grad, the gradient of loss (device, as many values; NULL: 1, not
- * with NONE).  imunpack_xent_rescale multiplies gradients that were made for 1 with *grad, in place, and leaves them alone if that is 1.
+ * with NONE).  imunpack_xent_rescale multiplies gradients that were made for 1 with *grad, in place, and leaves them alone if that is 1 (bfloat16: rounded
+ * once more, unless by a power of two).
  * workspace: device, 16-byte aligned, of the size that imunpack_xent_workspace gives: x and W in the forms the products read and, for
- * gradients, G of a piece of the rows (2 GiB at most, unless 256 rows take more) and partial sums.
+ * gradients, G of a piece of the rows (2 GiB at most, unless 256 rows take more) and partial sums; for the loss alone up to 2 GiB of these.
  * All sums are taken in a fixed order: equal inputs give equal bits.  rows == 0 is allowed.
  * Errors: EINVAL (null pointers, rows or vocab above 2^22, d above 2^20, a pitch < d, unknown types); ESMALL; EHIP. */
 enum { IMUNPACK_NONE = 0, IMUNPACK_SUM = 1, IMUNPACK_MEAN = 2 };

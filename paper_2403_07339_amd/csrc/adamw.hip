@@ -7,8 +7,9 @@
 // root is held, not v: with the same codes it covers twice the range in powers of two.  A code's step is 6 to 12 % of its value and a step of
 // the average moves it by 0.1 %: rounded to nearest, nearly every state would stand still.  So codes are rounded up
 // with the probability of what is left over (stochastic rounding), by 16 bits for each state of a hash of seed, step, tensor and
-// element, so that a step can be repeated.  A root that is not zero keeps the smallest code at least: as zero it would leave eps alone
-// below m in the next step.
+// element, so that a step can be repeated.  That leaves the means of m and of the root as they are; v, the root's square, comes out about 5 % too
+// large where the gradients keep their size (for beta2 0.99 and 0.999 alike), and the root scatters by some 16 %.  A root that is not zero keeps the
+// smallest code at least, 2^-18 of its block's largest: as zero it would leave eps alone below m in the next step.
 //
 // Bound by memory: 28 bytes an element with 32-bit states and gradients, 16 with 8-bit states.  More than the last-level cache holds is read and
 // written past the caches (85 million elements: 464 -> 410 us with 32-bit states; 157 million 478 -> 455 with 8-bit ones, bfloat16 gradients and
@@ -23,7 +24,8 @@
 namespace imu {
 constexpr int kAdamTensors = 48;      // to a launch: their table travels in the kernel's arguments (4 KiB)
 constexpr int kAdamBlock = 256;       // elements that share a scale
-constexpr int kAdamBlocks = 1;        // blocks of a wave (4: 85 million elements 383 -> 405 us, 0.27 million in 112 tensors 19 -> 25)
+constexpr int kAdamBlocks = 1;        // blocks of a wave (4: 85 million elements 383 -> 405 us, 0.27 million in 112 tensors 19 -> 25; 1, but written
+                                      // without the loops over them: 390, the compiler then puts the loads of a tensor's last elements in line)
 constexpr int kAdamChunk = 4 * kAdamBlocks * kAdamBlock;  // elements of a workgroup
 constexpr int64_t kAdamGroups = (1 << 24) - 1;  // workgroups of a launch at most: 2^32 threads are more than a grid may have along an axis
 constexpr float kE4m3Max = 448.0f, kNothing = 0x1p-96f;  // a block of no more than that is held as zeros
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamArgs a) {
     __bf16 *copy = a.copy[k];
     const int64_t chunk = ((int)blockIdx.x - a.first[k] + a.skip) * kAdamChunk;
     const uint32_t key = mix32(a.key + (uint32_t)(a.base + k) * kGolden);
-    const int64_t at0 = chunk + wave * kAdamBlock + lane * 4;  // the wave's blocks lie four apart
+    const int64_t at0 = chunk + wave * kAdamBlock + lane * 4;
     float P[kAdamBlocks][4], M[kAdamBlocks][4], V[kAdamBlocks][4];
     piece_t<G, 4> g4[kAdamBlocks];
     uint32_t mw[kAdamBlocks], vw[kAdamBlocks];

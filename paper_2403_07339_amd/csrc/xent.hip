@@ -572,7 +572,7 @@ struct FewArgs {
 constexpr int kFewRows = 8;
 // The loss alone of up to eight fp32 rows over weights that the last-level cache does not hold: W is read once, as it is, where splitting
 // it would move it three times.  64 columns (a part of a tile of 128) to a workgroup, eight at a time to a wave, sums in binary32.  Bound by
-// memory: 8 x 4096 by 32000 123 us (split: 412), by 128000 381 us (1386), 5.5 TB/s.  Weights that the cache holds go the way of all others.
+// memory: 8 x 4096 by 32000 123 us (split: 412), by 128000 381 us (1386), 4.3 and 5.5 TB/s.  Weights that the cache holds go the way of all others.
 __global__ __launch_bounds__(256) void xent_few_kernel(const FewArgs a) {
     __shared__ float logits[64][kFewRows];
     const int count = a.hdr->count, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -972,7 +972,8 @@ __global__ __launch_bounds__(256) void xent_fold_kernel(const FoldArgs a) {
     store_upto<T, 4>((T *)(isX ? a.gx : a.gw) + row * (isX ? a.ldgx : a.ldgw) + col, s, a.d - col);
 }
 
-// What the gradients, which may have been made for a gradient of 1, are multiplied with.
+// What the gradients, which may have been made for a gradient of 1, are multiplied with.  bfloat16 ones are rounded a second time (a scale of the loss
+// is a power of two as a rule, which rounds nothing); only a second pass over the products would save that.
 template <class T>
 __global__ __launch_bounds__(256) void xent_rescale_kernel(const float *grad, T *gx, int64_t nx, T *gw, int64_t nw) {
     const float g = *grad;
