@@ -473,6 +473,8 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
     product_tile<F16, T, T, false, false>(a.w, x, tm * kEdge, tn * kEdge, 0, a.ktiles, smem, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, lhalf = lane >> 5;
     const int vwave = tm * kEdge + (wave >> 1) * 32 * T, twave = tn * kEdge + (wave & 1) * 32 * T;  // the wave's first column and row of the piece
+    const bool own_scales = F16 && KEEP && (a.hdr->wide[0] || a.hdr->wide[1]);
+    const int down = F16 && KEEP ? -(scale_exponent(a.hdr->amax[0]) + scale_exponent(a.hdr->amax[1])) : 0;  // (of one scale for each operand)
     // FULL: no column behind the vocabulary and no row behind the last one in the wave's part (nothing to compare)
     auto finish = [&](auto full) __attribute__((always_inline)) {
         constexpr bool FULL = decltype(full)::value;
@@ -485,15 +487,22 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void xent_logits_k
             const int left = vocab - vwave - 4 * lhalf, own = hit_at - 4 * lhalf;  // the lane has columns 32 i + 8 q + k
             float top = -__builtin_inff(), sum = 0.0f;
             if constexpr (F16) {
-                const int ex = in_rows ? a.ex[a.first + t] : 0;
+                if (KEEP && !own_scales) {
 #pragma unroll
-                for (int i = 0; i < T; ++i)
+                    for (int i = 0; i < T; ++i)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const v4i32 ew = *reinterpret_cast<const v4i32 *>(a.ew + vwave + 32 * i + 8 * q + 4 * lhalf);  // (room for whole tiles)
+                        for (int r = 0; r < 16; ++r) acc[i][j][r] = ldexpf(acc[i][j][r], down);
+                } else {
+                    const int ex = in_rows ? a.ex[a.first + t] : 0;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) acc[i][j][4 * q + k] = ldexpf(acc[i][j][4 * q + k], -ex - ew[k]);
-                    }
+                    for (int i = 0; i < T; ++i)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const v4i32 ew = *reinterpret_cast<const v4i32 *>(a.ew + vwave + 32 * i + 8 * q + 4 * lhalf);  // (room for whole tiles)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) acc[i][j][4 * q + k] = ldexpf(acc[i][j][4 * q + k], -ex - ew[k]);
+                        }
+                }
             }
 #pragma unroll
             for (int i = 0; i < T; ++i)
