@@ -229,7 +229,7 @@ __device__ __forceinline__ void store_split(char *to, const float (&f)[8]) {
 }
 constexpr int kPrepareTurns = 4, kScanHere = 1024;
 // Eight columns of a row at a time: binary32 as two binary16 numbers, bfloat16 as it is; zeros behind the last column and, to a whole
-// k-tile, behind the last row of x.  Bound by memory: 50265 x 768 fp32 55 us, 5.6 TB/s (what it reads is in the
+// k-tile, behind the last row of x.  Bound by memory: 50265 x 768 fp32 59 us, 5.2 TB/s (what it reads is in the
 // last-level cache).  SCAN: up to kScanHere rows, among which every workgroup finds those with a target itself (one launch less: 197 x 256
 // by 1000, loss alone: 21.5 -> 18.3 us).
 template <class T, bool SCAN>
@@ -735,10 +735,11 @@ struct TurnArgs {
     int64_t pitch_P;
 };
 // Exponentials become G where they lie, 256 columns of ROWS rows to a workgroup, eight columns to a lane: zeros behind the vocabulary and, to a
-// whole k-tile, behind the last row.  614 x 50265 in binary16 pairs 50 us, 248 MB read and written.  32 rows, or eight where that leaves CUs
+// whole k-tile, behind the last row.  614 x 50265 in binary16 pairs 55 us, 248 MB read and written.  32 rows, or eight where that leaves CUs
 // without a workgroup (500 x 512 by 8000 fp32, both passes: 83.6 us and 81.8).  JOIN: those join the parts of their rows themselves, as the
 // kernel above does, which saves its launch (both passes, fp32: 200 x 256 by 1000 43.3 -> 40.6 us, 50 x 256 by 16000 55.3 -> 51.8, 20 x 64 by
-// 50000 65.3 -> 61.5; but 300 x 768 by 16000 bf16 69.2 -> 70.4).
+// 50000 65.3 -> 61.5; but 300 x 768 by 16000 bf16 69.2 -> 70.4).  fp32: what the gradients' products read is split again here where it has to be (see
+// AlignArgs; 50265 x 768 for one huge row 38 us).
 template <bool F16, int ROWS, bool JOIN>
 __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
     static_assert(!JOIN || ROWS == kJoinRows, "the rows of a workgroup");
