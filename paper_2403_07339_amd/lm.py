@@ -64,9 +64,9 @@ class MaskedLM(torch.nn.Module):
 
     def __init__(self, c: Config, quant: QuantConfig | None = None, device="cuda"):
         super().__init__()
-        # (the gradient of a matrix of attention weights is next to nothing but in the rows of masked tokens: its 95th percentile may lie seven
-        # orders of magnitude below its largest entry, more than 32-bit integers hold)
-        quant = quant or QuantConfig(beta_x=31.0, beta_w=31.0, beta_g=255.0, p=99.9, strategy_a=imu.ROW, strategy_b=imu.COL)
+        # (steps from the largest entry: the gradient of a matrix of attention weights is next to nothing but where a masked token looks at a few others, so
+        # that any percentile below may lie further under its largest entry than 32-bit integers reach, and the product refuses it)
+        quant = quant or QuantConfig(beta_x=255.0, beta_w=255.0, beta_g=1023.0, p=100.0, strategy_a=imu.ROW, strategy_b=imu.COL)
         self.embed = torch.nn.Embedding(c.vocab + 1, c.width, device=device)   # the last one stands for a masked token
         self.place = torch.nn.Parameter(0.02 * torch.randn(c.tokens, c.width, device=device))
         self.blocks = torch.nn.ModuleList(Block(c, quant, device) for _ in range(c.layers))

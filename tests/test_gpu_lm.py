@@ -71,3 +71,11 @@ def test_integer_head(lm):
             # and exactly the product of the integers, scaled
             exact = (q.to(f) @ head.Q.to(f).t()) * (scale.to(f)[..., None] * head.step)
             assert ((got.to(f) - exact).abs() <= 3 * 2.0 ** -24 * exact.abs()).all()
+
+
+@pytest.mark.parametrize("bits,seed", [(8, 0), (32, 1), (32, 3)])
+def test_training_goes_on(lm, bits, seed):
+    """The model as it comes: attention that looks at few tokens leaves gradients of which all but a few entries are next to nothing, and no product may refuse them."""
+    model, losses = lm.train(lm.Config(), 150, state_bits=bits, seed=seed)
+    assert losses.numel() == 150 and torch.isfinite(losses).all()
+    assert float(losses[-20:].mean()) < 0.8 * 6.9     # log 1000 at random
