@@ -309,8 +309,10 @@ __global__ __launch_bounds__(SCAN ? 1024 : 256) void xent_prepare_kernel(const P
     }
 }
 
-// The gradient of each row's loss.  One for all: G has a factor between -2 and 2 of it, and the results are multiplied with a power of two at the end.
-// One for each row: G has them under one power of two (bfloat16), or not at all (fp32: gx and x have them, see below).
+// The gradient of each row's loss.  One for all: the results are multiplied with it (a factor between -2 and 2 and a power of two), and G is without: a row's
+// largest entry is the target's, next to -1, where bfloat16 has its finest steps (with the factor of a mean over 614 rows in it, gx and gW were off by up to 2.3 times
+// what the rounding of the results makes, and 1.1 times without).  One for each row: G has them under one power of two (bfloat16), or not at all (fp32: gx
+// and x have them, see below).
 struct Upstream {
     const float *grad, *g;  // grad: nullptr for 1; g: bfloat16, the rows' factors where each has a gradient of its own, else nullptr
     int mean, rows;         // rows: fp32, each row has a gradient of its own
@@ -320,7 +322,7 @@ struct Upstream {
     }
     __device__ __forceinline__ static int exponent_of(float m) { return fabsf(m) > 0.0f ? (int)(__float_as_uint(fabsf(m)) >> 23) - 127 : 0; }
     __device__ __forceinline__ int exponent(const XentHeader *hdr) const { return rows ? 0 : g ? hdr->gexp : exponent_of(whole(hdr)); }
-    __device__ __forceinline__ float one(const XentHeader *hdr) const { return rows ? 1.0f : ldexpf(whole(hdr), -exponent_of(whole(hdr))); }
+    __device__ __forceinline__ float factor(const XentHeader *hdr) const { return rows || g || hdr->count == 0 ? 1.0f : ldexpf(whole(hdr), -exponent_of(whole(hdr))); }
     // Of the scale of x in gW's product.
     __device__ __forceinline__ int scale_x(const XentHeader *hdr) const { return rows ? hdr->gexp : scale_exponent(hdr->amax[0]); }
 };
@@ -752,7 +754,6 @@ __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
     const bool losses = JOIN && group_x == 0 && group_y < max(1, (rows + ROWS - 1) / ROWS);
     if (group_y * ROWS >= last && !losses) return;
     if (!JOIN && v0 >= (j.vocab + kStageCols - 1) / kStageCols * kStageCols) return;
-    const float all = a.up.g ? 0.0f : a.up.one(j.hdr);
     const int part = v0 / (logits_edge(rows_at_most(j.hdr, j.room), j.d, j.vocab) / 2);  // whose columns share a largest logit
     constexpr int kTurns = ROWS / 8;
     v4i32 hi[kTurns], lo[kTurns];
@@ -780,7 +781,7 @@ __global__ __launch_bounds__(256) void xent_turn_kernel(const TurnArgs a) {
         uint32_t qh[4] = {0, 0, 0, 0}, ql[4] = {0, 0, 0, 0};
         if (t < rows) {
             const float top = j.stats[((int64_t)part * j.room + t) * 2];
-            const float g = a.up.g ? a.up.g[j.first + t] : all, l = JOIN ? lse[threadIdx.x >> 5] : j.lse[j.first + t];
+            const float g = a.up.g ? a.up.g[j.first + t] : 1.0f, l = JOIN ? lse[threadIdx.x >> 5] : j.lse[j.first + t];
             const float down = __builtin_amdgcn_exp2f((top - l) * kLog2e) * g, one = F16 ? g * power_of_two(kTop) : g;
             const int own = a.wanted[j.first + t] - v0;
             float v[8];
@@ -880,6 +881,8 @@ __device__ __forceinline__ void grad_tile(const GradArgs &a, int wg, char *smem)
         return;
     }
     const int e = a.up.exponent(a.hdr) - (F16 ? kTop + a.up.scale_x(a.hdr) : 0);
+    const float factor = a.up.factor(a.hdr);
+    auto done = [&](float v) __attribute__((always_inline)) { return ldexpf(v * factor, e); };
     const int v0 = tm * kEdge + r0, f0 = tn * kEdge + c0;
 #pragma unroll
     for (int i = 0; i < T; ++i)
@@ -891,14 +894,14 @@ __device__ __forceinline__ void grad_tile(const GradArgs &a, int wg, char *smem)
                 for (int k = 0; k < 4; ++k)
 #pragma unroll
                     for (int j = 0; j < T; ++j)
-                        if (v0 + 32 * i + 8 * q + rl + k < height && f0 + 32 * j < width) to[(rl + k) * a.ldgw + f0 + 32 * j] = ldexpf(acc[i][j][4 * q + k], e);
+                        if (v0 + 32 * i + 8 * q + rl + k < height && f0 + 32 * j < width) to[(rl + k) * a.ldgw + f0 + 32 * j] = done(acc[i][j][4 * q + k]);
             } else {  // four rows by four columns trade places among four lanes: 8 bytes to a store
                 const int v = v0 + 32 * i + 8 * q + rl + (lane & 3);
                 uint16_t *to = (uint16_t *)a.gw + (int64_t)v * a.ldgw;
 #pragma unroll
                 for (int j = 0; j < T; ++j) {
-                    uint32_t lo = pack((__bf16)ldexpf(acc[i][j][4 * q], e), (__bf16)ldexpf(acc[i][j][4 * q + 1], e));
-                    uint32_t hi = pack((__bf16)ldexpf(acc[i][j][4 * q + 2], e), (__bf16)ldexpf(acc[i][j][4 * q + 3], e));
+                    uint32_t lo = pack((__bf16)done(acc[i][j][4 * q]), (__bf16)done(acc[i][j][4 * q + 1]));
+                    uint32_t hi = pack((__bf16)done(acc[i][j][4 * q + 2]), (__bf16)done(acc[i][j][4 * q + 3]));
                     quad_transpose(lo, hi, lane);
                     const int f = (f0 & ~3) + 32 * j;
                     if (v >= height) continue;
@@ -970,15 +973,15 @@ __global__ __launch_bounds__(256) void xent_fold_kernel(const FoldArgs a) {
     }
     if (col >= a.d) return;
     int e = a.up.exponent(a.hdr) - (sizeof(T) == 4 ? kTop + (isX ? scale_exponent(a.hdr->amax[1]) : a.up.scale_x(a.hdr)) : 0);
+    float factor = place < 0 ? 1.0f : a.up.factor(a.hdr);  // (zeros stay zeros)
     if (sizeof(T) == 4 && a.up.rows && isX && place >= 0) {  // the row's own gradient
         const float g = a.up.grad[row];
         const int eg = Upstream::exponent_of(g);
         e += eg;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) s[k] *= ldexpf(g, -eg);
+        factor = ldexpf(g, -eg);
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) s[k] = ldexpf(s[k], e);
+    for (int k = 0; k < 4; ++k) s[k] = ldexpf(s[k] * factor, e);
     store_upto<T, 4>((T *)(isX ? a.gx : a.gw) + row * (isX ? a.ldgx : a.ldgw) + col, s, a.d - col);
 }
 

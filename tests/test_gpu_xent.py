@@ -523,3 +523,35 @@ def test_more_logits_than_one_launch_takes(imu, rows, vocab):
     one, _ = imu.imunpack_xent(x, w, target)
     n = int((target >= 0).sum())
     assert abs(float(one) - float(got.to(F).sum()) / n) <= (rows / 256 + 20) * U * float(got.to(F).sum()) / n
+
+
+@pytest.mark.parametrize("rows,d,vocab", [(63, 200, 300), (125, 96, 500), (251, 256, 1000), (1004, 128, 200)])
+def test_bfloat16_gradients_of_a_mean_keep_what_their_type_holds(imu, rows, d, vocab):
+    """1 / rows is a little more than a power of two: with it in G, the target's entries (next to -1, the largest of their rows) would lie where bfloat16 is coarsest.
+    Without, they lie below 1: an entry 1 - p is off by up to 2^-9, its square 1 / 3 of that in the mean, the others (off by 2^-8 of themselves, twice) weigh
+    little; what the rounding of the results makes is up to 2^-8 and 1 / 3 likewise, over mantissas even in the logarithm 2^-8 times 0.43.  So both together are at most
+    (1 + (2^-9 / sqrt 3)^2 / (2^-8 0.43)^2)^0.5 = 1.2 times the results' own; 1.35 is allowed for what is random."""
+    x, w, target, _ = inputs(rows, d, vocab, torch.bfloat16, 1.0, rows)
+    loss, saved = imu.imunpack_xent(x, w, target, reduction="mean", want_grad=True)
+    a, b = imu.imunpack_xent_backward(x, w, target, saved, torch.ones((), device="cuda"))
+    x6, w6 = x.to(F), w.to(F)
+    G = torch.softmax(x6 @ w6.t(), 1).scatter_add(1, target[:, None], torch.full((rows, 1), -1.0, dtype=F, device="cuda")) / rows
+    for got, want in ((a, G @ w6), (b, G.t().contiguous() @ x6)):
+        least = (want.to(torch.bfloat16).to(F) - want).norm()
+        assert (got.to(F) - want).norm() <= 1.35 * least
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_an_upstream_gradient_that_is_not_finite(imu, dtype):
+    """It reaches what it multiplies: rows without a target keep gradients of zero, and so does W where no row has one."""
+    x, w, target, _ = inputs(40, 64, 100, dtype, 0.5, 51)
+    for bad in ("inf", "nan"):
+        up = torch.tensor(float(bad), device="cuda")
+        for reduction in ("sum", "mean"):
+            _, saved = imu.imunpack_xent(x, w, target, reduction=reduction, want_grad=True)
+            saved.gx = saved.gw = None      # made anew, with the gradient inside
+            a, b = imu.imunpack_xent_backward(x, w, target, saved, up)
+            assert not torch.isfinite(a[target >= 0]).any() and not a[target < 0].any() and not torch.isfinite(b).any()
+            none = torch.full_like(target, -100)
+            a, b = imu.imunpack_xent_backward(x, w, none, saved, up)
+            assert not a.any() and not b.any()
