@@ -124,10 +124,10 @@ def _rounded(x, fmt, square=False):
 
 
 def _stored(x, fmt, square=False):
-    """Codes with the columns filled up to whole blocks, a power of two for every row and block as a byte: a line of bytes for every block, whole sixteens long."""
+    """Codes with the columns filled up to whole blocks, a power of two for every row and block as a byte, whole sixteens of them to a row."""
     q, e = _blocks(x, fmt, square)
-    scales = torch.full((e.shape[1], -(-e.shape[0] // 16) * 16), 127, dtype=torch.uint8, device=x.device)
-    scales[:, :e.shape[0]] = (e + 127).t().to(torch.uint8)
+    scales = torch.full((e.shape[0], -(-e.shape[1] // 16) * 16), 127, dtype=torch.uint8, device=x.device)
+    scales[:, :e.shape[1]] = (e + 127).to(torch.uint8)
     return q.to(CODES[fmt]), scales.view(torch.float8_e8m0fnu)
 
 
@@ -168,7 +168,7 @@ def prepare(case, seed):
 # ---- plain forms -----------------------------------------------------------------------------------
 def _values(codes, scales):
     rows, f = codes.shape[0], torch.float32
-    s = _pow2(scales.view(torch.uint8)[:, :rows].t().to(torch.int32) - 127)
+    s = _pow2(scales.view(torch.uint8)[:, :codes.shape[1] // BLOCK].to(torch.int32) - 127)
     return (codes.to(f).view(rows, -1, BLOCK) * s[:, :, None]).view(rows, -1)
 
 
@@ -289,7 +289,7 @@ def _exact8(x, fmt, square=False):
 def exact(case, seed):
     c, s, f = case, prepare(case, seed), torch.float64
     if c["kind"] == "product":
-        a, b = (torch.ldexp(s[k].to(f).reshape(s[k].shape[0], -1, BLOCK), (s["s" + k].view(torch.uint8).to(f).t()[:s[k].shape[0]] - 127)[:, :, None]).flatten(1) for k in "ab")
+        a, b = (torch.ldexp(s[k].to(f).reshape(s[k].shape[0], -1, BLOCK), (s["s" + k].view(torch.uint8)[:, :s[k].shape[1] // BLOCK].to(f) - 127)[:, :, None]).flatten(1) for k in "ab")
         y = torch.mm(a, b.t())
         return {"y": y if s["bias"] is None else y.add_(s["bias"].to(f))}
     if c["kind"] == "linear":
