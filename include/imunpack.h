@@ -423,6 +423,90 @@ int imunpack_xent(const void *x, int64_t ldx, const void *w, int64_t ldw, const 
                   imunpack_stream_t stream);
 int imunpack_xent_rescale(const float *grad, void *gx, int64_t nx, void *gw, int64_t nw, int dtype, imunpack_stream_t stream);
 
+/* ---- tensors in 8-bit floating point, a power of two for every block of 128 ------------------------
+ * A tensor x of `rows` rows of `cols` elements is held as codes of one of the formats below and, for each row and each 128 consecutive
+ * columns (a block; the last one may be shorter), a byte that stands for 2^(byte - 127):
+ *     e = the smallest whole number >= -127 with max |x| over the block <= top 2^e   (0 for a block of zeros),   byte = e + 127,
+ *     code = x 2^-e, rounded to nearest with ties to even,                       value = code 2^e.
+ * top is 448 (E4M3: four exponent bits, three of fraction, no infinity) or 57344 (E5M2).  A value is within 2^-4 (E4M3) or 2^-3 (E5M2) of x relative to x, or
+ * within 2^-10 2^e (2^-17 2^e).  Infinities and NaN do not count for max |x|; they become NaN codes (E5M2: infinity stays).
+ * "Square" blocks are 128 rows x 128 columns: their byte stands in each of their rows.
+ * codes: device, row r at codes + r ldc, ldc bytes at least 128 ceil(cols / 128): the codes behind a row's end, up to a whole block, are
+ * zeros (the calls that write codes see to that, the product counts on it).  scales: device, the byte of row r and block j at
+ * scales + r lds + j, lds at least ceil(cols / 128); a row may be read up to a whole 16 bytes.  Both bases 16-byte aligned, both pitches multiples of 16.
+ * No output of the calls below may overlap an input.  All sums are taken in a fixed order: equal inputs give equal bits. */
+enum { IMUNPACK_E4M3 = 0, IMUNPACK_E5M2 = 1 };
+#define IMUNPACK_BLOCK8 128
+
+/* x (device, dtype, unit stride within a row, ldx elements from row to row) in 8 bits: as it lies (codes, scales; both NULL: not), and turned
+ * (turned, turned_scales; NULL: not): the tensor x^T of `cols` rows of `rows` elements, whose blocks run along x's columns.  square: square
+ * blocks; turned then holds the same values.  rows == 0 is allowed.
+ * Errors: EINVAL (null pointers, rows outside [0, 2^31], with turned 2^24, cols outside [1, 2^24], pitches or alignments as above, unknown types); EHIP. */
+int imunpack_block8_quantize(const void *x, int64_t ldx, int64_t rows, int64_t cols, int dtype, int format, int square,
+                             void *codes, int64_t ldc, void *scales, int64_t lds,
+                             void *turned, int64_t ldt, void *turned_scales, int64_t ldts, imunpack_stream_t stream);
+
+/* The same of a tensor that is in 8 bits already (rows x cols, any blocks): its values, turned, in blocks along its columns.  A value of e4m3 or e5m2
+ * under another power of two is the same value, unless it falls below that block's smallest codes and is rounded to those. */
+int imunpack_block8_turn(const void *codes, int64_t ldc, const void *scales, int64_t lds, int64_t rows, int64_t cols, int format,
+                         void *turned, int64_t ldt, void *turned_scales, int64_t ldts, imunpack_stream_t stream);
+
+/* out (device, dtype, ldo elements from row to row) = the values of a tensor in 8 bits (bfloat16 holds them exactly, but for magnitudes from 2^128 on or below
+ * 2^-133).  Errors as above. */
+int imunpack_block8_values(const void *codes, int64_t ldc, const void *scales, int64_t lds, int64_t rows, int64_t cols, int format,
+                           void *out, int64_t ldo, int dtype, imunpack_stream_t stream);
+
+/* out = A B^T (+ bias, fp32, one per column; NULL: none) for A: m x k and B: n x k in 8 bits, out: device, dtype, row stride ldo >= n elements.
+ * fp32 results: products exact, sums in fp32.
+ * workspace: device, 16-byte aligned, of the size that imunpack_block8_gemm_workspace gives (0: NULL will do).
+ * Errors: EINVAL (null pointers, k outside [1, 2^24], m or n outside [0, 2^24], layouts as above, unknown types); ESMALL; EHIP. */
+int imunpack_block8_gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, size_t *bytes);
+int imunpack_block8_gemm(const void *a, int64_t lda, const void *a_scales, int64_t ldsa, int a_format,
+                         const void *b, int64_t ldb, const void *b_scales, int64_t ldsb, int b_format,
+                         int64_t m, int64_t n, int64_t k, const float *bias, void *out, int64_t ldo, int dtype,
+                         void *workspace, size_t workspace_bytes, imunpack_stream_t stream);
+
+/* ---- activation functions that keep their input in 8 bits -------------------------------------------
+ * y = f(u), f = GELU: u Phi(u) (the normal distribution's), or SiLU: u / (1 + exp(-u)); gated: u has 2 cols columns and y = f(u[:, :cols]) u[:, cols:].
+ * u, y: device, dtype, ld* elements from row to row.  y_codes, y_scales (NULL: not): y in 8 bits (E4M3, blocks along the rows), the operand of the
+ * next product; y (may then be NULL) receives those values.  kept, kept_scales (NULL: not, for serving): u in 8 bits (E4M3); gated: its first cols columns,
+ * and kept2, kept2_scales the others, pitches alike.
+ * imunpack_act8_backward: with v the values that were kept,  gu = g f'(v);  gated:  gu = (g f'(v1) v2, g f(v1)), 2 cols columns.
+ * rows == 0 is allowed.  Errors: EINVAL (null pointers, sizes as for imunpack_block8_quantize, pitches, alignments, unknown types or functions); EHIP. */
+enum { IMUNPACK_GELU = 0, IMUNPACK_SILU = 1 };
+int imunpack_act8(const void *u, int64_t ldu, int64_t rows, int64_t cols, int dtype, int act, int gated, void *y, int64_t ldy,
+                  void *y_codes, int64_t ldyc, void *y_scales, int64_t ldys, void *kept, void *kept2, int64_t ldk,
+                  void *kept_scales, void *kept2_scales, int64_t ldks, imunpack_stream_t stream);
+int imunpack_act8_backward(const void *g, int64_t ldg, int64_t rows, int64_t cols, int dtype, int act, int gated,
+                           const void *kept, const void *kept2, int64_t ldk, const void *kept_scales, const void *kept2_scales, int64_t ldks,
+                           void *gu, int64_t ldgu, imunpack_stream_t stream);
+
+/* ---- log probabilities of given tokens, entropy, top alternatives ------------------------------------
+ * For each of `rows` rows l of `vocab` logits (device, dtype, unit stride within a row, ldl elements from row to row):
+ *     lse = log sum_v exp l_v,   logp_j = l_[token_j] - lse for `count` tokens (device int64, row r's at tokens + r count),
+ *     entropy = lse - sum_v p_v l_v  with  p = exp(l - lse),
+ *     top_index, top_logp: the `top` largest logits' places (int64), largest first, of equals the lowest place first, and l - lse there.
+ * A logit of -infinity has probability 0 and adds nothing to the entropy; NaN counts as -infinity for the order.
+ * A row of nothing but -infinity: lse, logp and top_logp -infinity, entropy 0, places 0, 1, ...  +infinity or NaN in a row: its numbers are NaN.
+ * A token that is ignore_index: logp 0, no gradient; another one outside [0, vocab): logp NaN, no gradient.
+ * logp (rows x count), lse, entropy, top_logp (rows x top): device fp32, dense; lse and entropy may be NULL, logp with count == 0, the last two with top == 0.
+ * stats (device fp32, two for each row, may be NULL): the row's maximum m and log sum_v exp(l_v - m), for the backward pass.
+ * imunpack_logprobs_backward: with g_logp (rows x count), g_entropy, g_top (rows x top, for top_index's tokens) the gradients (fp32; each may be NULL):
+ *     gl_v = sum_j g_j ([v = token_j] - p_v) - g_entropy p_v (l_v - lse + entropy)
+ * over both kinds of tokens (0 for p_v times anything where l_v is -infinity); gl: device, dtype, ldg elements from row to row, 0 for a row of nothing but
+ * -infinity.  gl may be l, with the same pitch.  stats and entropy are those of the forward call (entropy may be NULL without g_entropy).
+ * workspace: device, 16-byte aligned, of the size that imunpack_logprobs_workspace gives (0: NULL will do).  Statistics in fp32, equal inputs give equal bits.
+ * rows == 0 is allowed.  Errors: EINVAL (null pointers, rows outside [0, 2^31 - 1], vocab outside [1, 2^30], count outside [0, 1024], top outside [0, min(64, vocab)], a pitch < vocab,
+ * unknown types); ESMALL; EHIP. */
+#define IMUNPACK_LOGPROBS_TOP 64
+int imunpack_logprobs_workspace(int64_t rows, int64_t vocab, int64_t count, int64_t top, int dtype, size_t *bytes);
+int imunpack_logprobs(const void *logits, int64_t ldl, int64_t rows, int64_t vocab, int dtype, const int64_t *tokens, int64_t count, int64_t ignore_index, int64_t top,
+                      float *logp, float *lse, float *stats, float *entropy, float *top_logp, int64_t *top_index, void *workspace, size_t workspace_bytes,
+                      imunpack_stream_t stream);
+int imunpack_logprobs_backward(const void *logits, int64_t ldl, int64_t rows, int64_t vocab, int dtype, const int64_t *tokens, int64_t count, int64_t ignore_index, int64_t top,
+                               const int64_t *top_index, const float *stats, const float *entropy, const float *g_logp, const float *g_entropy, const float *g_top,
+                               void *gl, int64_t ldg, imunpack_stream_t stream);
+
 /* ---- diagnostics ------------------------------------------------------------------------------- */
 /* Per-kernel device time of the last call of each stage on this plan is not kept; callers time
  * with events.  These two describe errors. */

@@ -34,6 +34,8 @@ EXPORTS = [
     "imunpack_plan_digits", "imunpack_plan_keep_weights", "imunpack_plan_weights_reused", "imunpack_diag_gemm_parts", "imunpack_diag_gemm_halves", "imunpack_diag_list_columns",
     "imunpack_rmsnorm", "imunpack_rmsnorm_quantize", "imunpack_rmsnorm_backward_workspace", "imunpack_rmsnorm_backward", "imunpack_adamw",
     "imunpack_xent_workspace", "imunpack_xent", "imunpack_xent_rescale",
+    "imunpack_block8_quantize", "imunpack_block8_turn", "imunpack_block8_values", "imunpack_block8_gemm_workspace", "imunpack_block8_gemm",
+    "imunpack_act8", "imunpack_act8_backward", "imunpack_logprobs_workspace", "imunpack_logprobs", "imunpack_logprobs_backward",
 ]
 DIGITS_INT8, DIGITS_FP6 = 0, 1
 
@@ -586,7 +588,9 @@ class NormSaved:
 
 _tensors.bind(ImunpackError, *[C.cast(getattr(_lib, _name), _vp).value for _name in (
     "imunpack_rmsnorm", "imunpack_rmsnorm_quantize", "imunpack_rmsnorm_backward_workspace", "imunpack_rmsnorm_backward", "imunpack_adamw",
-    "imunpack_xent_workspace", "imunpack_xent", "imunpack_xent_rescale")])
+    "imunpack_xent_workspace", "imunpack_xent", "imunpack_xent_rescale", "imunpack_block8_quantize", "imunpack_block8_turn", "imunpack_block8_values",
+    "imunpack_block8_gemm_workspace", "imunpack_block8_gemm", "imunpack_act8", "imunpack_act8_backward", "imunpack_logprobs_workspace", "imunpack_logprobs",
+    "imunpack_logprobs_backward")])
 
 
 def imunpack_rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None):
@@ -661,3 +665,108 @@ def imunpack_xent_backward(x: torch.Tensor, w: torch.Tensor, target: torch.Tenso
     if want_x or want_w:
         _tensors.xent_rescale(x, w, target, grad, gx, gw, _stream())
     return gx, gw
+
+
+# ---- 8-bit floating point: tensors, products, activations kept in it ---------------------------------------
+BLOCK8 = 128
+FORMATS = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+ACTIVATIONS = {"gelu": 0, "silu": 1}
+
+
+@dataclass
+class Blocks8:
+    """A matrix of `cols` columns in 8-bit floating point with a power of two for every row and block of 128 columns: codes (float8_e4m3fn or
+    float8_e5m2, rows x cols, filled with zeros up to a whole block) and scales (float8_e8m0fnu, rows x blocks, filled up to a multiple of 16)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    cols: int
+
+    @property
+    def rows(self) -> int:
+        return self.codes.shape[0]
+
+    def values(self, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+        return imunpack_block8_values(self, dtype)
+
+
+def _is_bf16(dtype: torch.dtype) -> bool:
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("results are float32 or bfloat16")
+    return dtype == torch.bfloat16
+
+
+def imunpack_block8_quantize(x: torch.Tensor, format: str = "e4m3", square: bool = False, turned: bool = False, lying: bool = True):
+    """x [..., cols] (fp32 or bfloat16) in 8 bits, its leading dimensions as rows.  Returns (as it lies, turned): Blocks8 each, None where not
+    wanted; turned is x^T with its blocks along x's columns.  square: one power of two for 128 x 128, the same for both."""
+    if format not in FORMATS:
+        raise ValueError("format is e4m3 or e5m2")
+    if not (lying or turned):
+        raise ValueError("as it lies, turned or both")
+    q, qs, t, ts = _tensors.block8_quantize(x, format == "e5m2", square, lying, turned, _stream())
+    cols = x.shape[-1]
+    return Blocks8(q, qs, cols) if lying else None, Blocks8(t, ts, x.numel() // cols) if turned else None
+
+
+def imunpack_block8_turn(x: Blocks8) -> Blocks8:
+    """x^T in 8 bits, in blocks along x's columns (rows of x), from x in 8 bits."""
+    codes, scales = _tensors.block8_turn(x.codes, x.scales, x.cols, _stream())
+    return Blocks8(codes, scales, x.rows)
+
+
+def imunpack_block8_values(x: Blocks8, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    return _tensors.block8_values(x.codes, x.scales, x.cols, _is_bf16(dtype), _stream())
+
+
+def imunpack_block8_gemm(a: Blocks8, b: Blocks8, dtype: torch.dtype = torch.float32, bias: torch.Tensor | None = None) -> torch.Tensor:
+    """A B^T (+ bias, fp32, one for each row of B) of two matrices in 8 bits, in dtype (float32 or bfloat16)."""
+    return _tensors.block8_gemm(a.codes, a.scales, b.codes, b.scales, a.cols, b.cols, _is_bf16(dtype), bias, _stream())
+
+
+def imunpack_act8(u: torch.Tensor, act: str = "gelu", gated: bool = False, quantize: bool = False, keep: bool = True, want_y: bool = True):
+    """y = f(u), f GELU or SiLU; gated: f of the first half of u's columns times the second half.  Returns (y, codes, kept): codes is y in 8 bits (with
+    quantize; y then holds its values; None otherwise; y is None without want_y), kept the tuple of Blocks8 that imunpack_act8_backward takes: u in 8 bits, half by
+    half (None without keep)."""
+    if act not in ACTIVATIONS:
+        raise ValueError("act is gelu or silu")
+    if not (want_y or quantize):
+        raise ValueError("y, its codes or both")
+    y, q, qs, k, ks, k2, k2s = _tensors.act8(u, ACTIVATIONS[act], gated, quantize, keep, want_y, _stream())
+    cols = u.shape[-1] // 2 if gated else u.shape[-1]
+    kept = (Blocks8(k, ks, cols), Blocks8(k2, k2s, cols)) if keep and gated else (Blocks8(k, ks, cols),) if keep else None
+    return y, Blocks8(q, qs, cols) if quantize else None, kept
+
+
+def imunpack_act8_backward(g: torch.Tensor, kept, act: str = "gelu", gated: bool = False) -> torch.Tensor:
+    """The gradient of u for g, that of y, with the values of u that were kept."""
+    if act not in ACTIVATIONS:
+        raise ValueError("act is gelu or silu")
+    if kept is None or len(kept) != (2 if gated else 1):
+        raise ValueError("kept is what imunpack_act8 returned for the same `gated`")
+    first, second = kept[0], kept[1] if gated else None
+    return _tensors.act8_backward(g, ACTIVATIONS[act], first.codes, first.scales, second.codes if gated else None, second.scales if gated else None, first.cols, _stream())
+
+
+# ---- log probabilities ---------------------------------------------------------------------------------
+@dataclass
+class Logprobs:
+    """Of rows of logits: logp of the given tokens, lse, entropy, the largest log probabilities and their places (None where not asked for);
+    stats (maximum and log of the sum relative to it) goes to imunpack_logprobs_backward."""
+    logp: torch.Tensor | None
+    lse: torch.Tensor
+    stats: torch.Tensor
+    entropy: torch.Tensor | None
+    top_logp: torch.Tensor | None
+    top_index: torch.Tensor | None
+
+
+def imunpack_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: int = 0, want_entropy: bool = True, ignore_index: int = -100) -> Logprobs:
+    """Log probabilities of logits [..., vocab] (fp32 or bfloat16): of tokens (int64, the logits' leading shape, or with several to a row behind it), the
+    entropy, and the `top` largest with their places, of equals the lowest place first; all in fp32."""
+    return Logprobs(*_tensors.logprobs(logits, tokens, ignore_index, top, want_entropy, _stream()))
+
+
+def imunpack_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor | None, saved: Logprobs, g_logp: torch.Tensor | None = None, g_entropy: torch.Tensor | None = None,
+                               g_top: torch.Tensor | None = None, ignore_index: int = -100) -> torch.Tensor:
+    """The gradient of the logits, in their type, for those (fp32) of logp, entropy and top_logp as imunpack_logprobs returned them."""
+    dense = [g if g is None else g.contiguous() for g in (g_logp, g_entropy, g_top)]
+    return _tensors.logprobs_backward(logits, tokens, ignore_index, saved.top_index if g_top is not None else None, saved.stats, saved.entropy, *dense, _stream())

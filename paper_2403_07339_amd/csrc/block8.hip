@@ -1,0 +1,400 @@
+// Tensors into 8-bit floating point with a power of two per block (block8.h says how), back, turned; activation functions whose input is kept that way.
+//
+// All of it is bound by memory.  Along rows, sixteen lanes hold a block (eight elements each), so that its largest magnitude is a maximum over
+// registers and four rotations within a row of lanes, nothing goes through LDS, and the blocks of a matrix of any width fill whole waves.
+// For the turned tensor (codes of x^T with blocks along x's columns), a workgroup holds 128 x 128 elements in registers, eight rows by eight columns a
+// lane; column maxima meet in LDS, and so do the codes, eight rows of a column at a time.
+#include "block8.h"
+
+namespace imu {
+constexpr int kLaunchBlocks = 1 << 26;  // blocks of a launch: far below 2^32 threads, indexes in 32 bits
+
+// ---- along rows -------------------------------------------------------------------------------------------------------------
+struct RowsArgs {
+    const void *x;
+    uint8_t *codes, *scales;
+    int64_t ldx, ldc, lds;
+    int rows, cols, kb;
+};
+constexpr int kRowsUnroll = 4;  // blocks of 16 lanes, one after the other
+
+template <class T, int FORMAT>
+__global__ __launch_bounds__(256) void block8_rows_kernel(const RowsArgs a) {
+    const int total = a.rows * a.kb, lane16 = threadIdx.x & 15;
+    const int first = (int)blockIdx.x * (16 * kRowsUnroll) + (threadIdx.x >> 4);
+    int row[kRowsUnroll], kb[kRowsUnroll];
+    piece_t<T, 8> in[kRowsUnroll];
+#pragma unroll
+    for (int u = 0; u < kRowsUnroll; ++u) {
+        const int block = min(first + 16 * u, total - 1);
+        row[u] = block / a.kb;
+        kb[u] = block - row[u] * a.kb;
+        const int col = kb[u] * kBlock8 + lane16 * 8;
+        in[u] = load_piece<T, 8>((const T *)a.x + row[u] * a.ldx + col, a.cols - col);
+    }
+#pragma unroll
+    for (int u = 0; u < kRowsUnroll; ++u) {
+        if (first + 16 * u >= total) break;
+        float x[8];
+        to_floats<T, 8>(in[u], x);
+        const int byte = block8_of<FORMAT>(x);
+        *reinterpret_cast<uint2 *>(a.codes + row[u] * a.ldc + kb[u] * kBlock8 + lane16 * 8) = encode8<FORMAT>(x, block8_inverse(byte));
+        if (lane16 == 0) a.scales[row[u] * a.lds + kb[u]] = (uint8_t)byte;
+    }
+}
+
+// ---- both ways, or turned alone -----------------------------------------------------------------------------------------------
+struct TileArgs {
+    const void *x;                // T, or codes with their scales
+    const uint8_t *xs;
+    uint8_t *codes, *scales;      // may be null
+    uint8_t *turned, *tscales;
+    int64_t ldx, ldxs, ldc, lds, ldt, ldts;
+    int64_t rows;
+    int cols, kb, square;
+};
+
+// Where the eight codes of rows 8 p .. 8 p + 7 of column c lie in LDS: sixteen bytes at a time at places that turn with the column, so that the
+// sixteen lanes of a row of lanes, eight columns apart, fall on different banks.
+__device__ __forceinline__ int turned_at(int c, int p) { return c * 128 + ((((p >> 1) ^ (c >> 3)) & 7) << 4) + (p & 1) * 8; }
+
+// T: float, __bf16, or uint8_t for codes in FORMAT (turned alone).
+template <class T, int FORMAT>
+__global__ __launch_bounds__(256) void block8_tile_kernel(const TileArgs a) {
+    constexpr bool kCodes = std::is_same<T, uint8_t>::value;
+    __shared__ __attribute__((aligned(16))) uint8_t tile[128 * 128];
+    __shared__ int tops[4][128];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, group = lane >> 4, l16 = lane & 15;
+    const int kb = (int)(blockIdx.x % a.kb);
+    const int64_t rb = blockIdx.x / a.kb, row0 = rb * 128 + wave * 32 + group * 8;
+    const int col = kb * 128 + l16 * 8, have = a.cols - col;
+    float x[8][8];
+    piece_t<T, 8> in[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) in[i] = load_piece<T, 8>((const T *)a.x + (row0 + i) * a.ldx + col, row0 + i < a.rows ? have : 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (kCodes) {
+            const int byte = row0 + i < a.rows ? a.xs[(row0 + i) * a.ldxs + kb] : 127;
+            decode8<FORMAT>(__builtin_bit_cast(uint2, in[i]), block8_scale(byte), x[i]);
+        } else {
+            to_floats<T, 8>(in[i], x[i]);
+        }
+    }
+    // the columns' maxima (or the square's)
+    int top[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        top[j] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top[j] = max(top[j], finite_bits(x[i][j]));
+        top[j] = max(top[j], __shfl_xor(top[j], 16));
+        top[j] = max(top[j], __shfl_xor(top[j], 32));
+    }
+    if (lane < 16)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) tops[wave][lane * 8 + j] = top[j];
+    __syncthreads();
+    int all = 0, bytes[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        top[j] = max(max(tops[0][l16 * 8 + j], tops[1][l16 * 8 + j]), max(tops[2][l16 * 8 + j], tops[3][l16 * 8 + j]));
+        all = max(all, top[j]);
+    }
+    if (a.square) {
+        all = max16(all);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top[j] = all;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bytes[j] = block8_byte<FORMAT>(top[j]);
+    if constexpr (!kCodes) {
+        if (a.codes) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int byte = a.square ? bytes[0] : block8_of<FORMAT>(x[i]);
+                if (row0 + i < a.rows) {
+                    *reinterpret_cast<uint2 *>(a.codes + (row0 + i) * a.ldc + col) = encode8<FORMAT>(x[i], block8_inverse(byte));
+                    if (l16 == 0) a.scales[(row0 + i) * a.lds + kb] = (uint8_t)byte;
+                }
+            }
+        }
+    }
+    if (!a.turned) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = x[i][j];
+        *reinterpret_cast<uint2 *>(tile + turned_at(l16 * 8 + j, wave * 4 + group)) = encode8<FORMAT>(v, block8_inverse(bytes[j]));
+    }
+    if (wave == 0 && group == 0)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < have) a.tscales[(int64_t)(col + j) * a.ldts + rb] = (uint8_t)bytes[j];
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {  // sixteen rows of a column to a thread
+        const int c = u * 32 + (threadIdx.x >> 3), p = (threadIdx.x & 7) * 2;
+        if (kb * 128 + c < a.cols)
+            *reinterpret_cast<uint4 *>(a.turned + (int64_t)(kb * 128 + c) * a.ldt + rb * 128 + p * 8) = *reinterpret_cast<const uint4 *>(tile + turned_at(c, p));
+    }
+}
+
+// ---- values -------------------------------------------------------------------------------------------------------------------
+struct ValuesArgs {
+    const uint8_t *codes, *scales;
+    void *out;
+    int64_t ldc, lds, ldo;
+    int rows, cols, kb;
+};
+template <class T, int FORMAT>
+__global__ __launch_bounds__(256) void block8_values_kernel(const ValuesArgs a) {
+    const int block = (int)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (block >= a.rows * a.kb) return;
+    const int row = block / a.kb, kb = block - row * a.kb, col = kb * kBlock8 + (threadIdx.x & 15) * 8;
+    float f[8];
+    decode8<FORMAT>(*reinterpret_cast<const uint2 *>(a.codes + row * a.ldc + col), block8_scale(a.scales[row * a.lds + kb]), f);
+    if (col < a.cols) store_upto<T, 8>((T *)a.out + row * a.ldo + col, f, a.cols - col);
+}
+
+// ---- activation functions -------------------------------------------------------------------------------------------------------
+// f(u) and f'(u).  GELU: u Phi(u), Phi + u phi; SiLU: u sig(u), sig (1 + u (1 - sig)).
+template <int ACT>
+__device__ __forceinline__ float act_value(float u) {
+    if constexpr (ACT == IMUNPACK_GELU) return u * (0.5f * (1.0f + erff(u * 0.70710678f)));
+    else return u / (1.0f + expf(-u));
+}
+template <int ACT>
+__device__ __forceinline__ float act_slope(float u, float &value) {
+    if constexpr (ACT == IMUNPACK_GELU) {
+        const float phi = 0.5f * (1.0f + erff(u * 0.70710678f));
+        value = u * phi;
+        return fmaf(u, expf(-0.5f * u * u) * 0.39894228f, phi);
+    } else {
+        const float sig = 1.0f / (1.0f + expf(-u));
+        value = u * sig;
+        return sig * fmaf(u, 1.0f - sig, 1.0f);
+    }
+}
+
+struct ActArgs {
+    const void *u;
+    void *y;
+    Blocks8 yq, kept, kept2;  // codes may be null
+    int64_t ldu, ldy;
+    int rows, cols, kb;
+};
+template <class T, int ACT, bool GATED>
+__global__ __launch_bounds__(256) void act8_kernel(const ActArgs a) {
+    constexpr int F = IMUNPACK_E4M3;
+    const int block = (int)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (block >= a.rows * a.kb) return;
+    const int row = block / a.kb, kb = block - row * a.kb, l16 = threadIdx.x & 15, col = kb * kBlock8 + l16 * 8, have = a.cols - col;
+    const T *u = (const T *)a.u + row * a.ldu + col;
+    const piece_t<T, 8> in = load_piece<T, 8>(u, have);
+    piece_t<T, 8> in2;
+    if constexpr (GATED) in2 = load_piece<T, 8>(u + a.cols, have);
+    float x[8], x2[8], y[8];
+    to_floats<T, 8>(in, x);
+    if constexpr (GATED) to_floats<T, 8>(in2, x2);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        y[k] = act_value<ACT>(x[k]);
+        if constexpr (GATED) y[k] *= x2[k];
+    }
+    auto keep = [&](const Blocks8 &to, const float (&v)[8]) __attribute__((always_inline)) {
+        const int byte = block8_of<F>(v);
+        const uint2 w = encode8<F>(v, block8_inverse(byte));
+        *reinterpret_cast<uint2 *>(to.codes + row * to.ldc + col) = w;
+        if (l16 == 0) to.scales[row * to.lds + kb] = (uint8_t)byte;
+        return make_uint3(w.x, w.y, (uint32_t)byte);
+    };
+    if (a.kept.codes) {
+        keep(a.kept, x);
+        if constexpr (GATED) keep(a.kept2, x2);
+    }
+    if (a.yq.codes) {
+        const uint3 w = keep(a.yq, y);
+        decode8<F>(make_uint2(w.x, w.y), block8_scale((int)w.z), y);
+    }
+    if (a.y && have > 0) store_upto<T, 8>((T *)a.y + row * a.ldy + col, y, have);
+}
+
+struct ActBackArgs {
+    const void *g;
+    void *gu;
+    Blocks8 kept, kept2;
+    int64_t ldg, ldgu;
+    int rows, cols, kb;
+};
+template <class T, int ACT, bool GATED>
+__global__ __launch_bounds__(256) void act8_back_kernel(const ActBackArgs a) {
+    constexpr int F = IMUNPACK_E4M3;
+    const int block = (int)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (block >= a.rows * a.kb) return;
+    const int row = block / a.kb, kb = block - row * a.kb, col = kb * kBlock8 + (threadIdx.x & 15) * 8, have = a.cols - col;
+    const piece_t<T, 8> in = load_piece<T, 8>((const T *)a.g + row * a.ldg + col, have);
+    float g[8], u[8], u2[8];
+    decode8<F>(*reinterpret_cast<const uint2 *>(a.kept.codes + row * a.kept.ldc + col), block8_scale(a.kept.scales[row * a.kept.lds + kb]), u);
+    if constexpr (GATED)
+        decode8<F>(*reinterpret_cast<const uint2 *>(a.kept2.codes + row * a.kept2.ldc + col), block8_scale(a.kept2.scales[row * a.kept2.lds + kb]), u2);
+    to_floats<T, 8>(in, g);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        float value;
+        const float slope = act_slope<ACT>(u[k], value);
+        if constexpr (GATED) {
+            const float first = g[k] * slope * u2[k];
+            u2[k] = g[k] * value;
+            u[k] = first;
+        } else {
+            u[k] = g[k] * slope;
+        }
+    }
+    if (have <= 0) return;
+    T *gu = (T *)a.gu + row * a.ldgu + col;
+    store_upto<T, 8>(gu, u, have);
+    if constexpr (GATED) store_upto<T, 8>(gu + a.cols, u2, have);
+}
+
+// ---- entry points ---------------------------------------------------------------------------------------------------------------
+static bool sizes_fit(int64_t rows, int64_t cols) { return rows >= 0 && rows <= kBlock8Rows && cols >= 1 && cols <= kBlock8Cols; }
+static bool type_fits(int dtype) { return dtype == IMUNPACK_F32 || dtype == IMUNPACK_BF16; }
+static bool format_fits(int format) { return format == IMUNPACK_E4M3 || format == IMUNPACK_E5M2; }
+static int64_t element(int dtype) { return dtype == IMUNPACK_F32 ? 4 : 2; }
+static int blocks_of(int64_t cols) { return (int)((cols + kBlock8 - 1) / kBlock8); }
+
+// launch(first row, rows) for pieces of the rows that a launch takes.
+template <class L>
+static int in_pieces(int64_t rows, int kb, int64_t whole, L launch) {
+    const int64_t most = std::max<int64_t>(kLaunchBlocks / kb / whole * whole, whole);
+    for (int64_t r = 0; r < rows; r += most) {
+        launch(r, std::min(most, rows - r));
+        IMU_TRY(launch_status());
+    }
+    return IMUNPACK_OK;
+}
+// f(float or __bf16, format) by what the call says.
+template <class F>
+static auto by_type(int dtype, int format, F f) {
+    using E4 = std::integral_constant<int, IMUNPACK_E4M3>;
+    using E5 = std::integral_constant<int, IMUNPACK_E5M2>;
+    if (dtype == IMUNPACK_F32) return format == IMUNPACK_E4M3 ? f(0.0f, E4()) : f(0.0f, E5());
+    return format == IMUNPACK_E4M3 ? f((__bf16)0.0f, E4()) : f((__bf16)0.0f, E5());
+}
+
+static int tiles(const TileArgs &whole, int dtype, int format, bool codes, hipStream_t st) {
+    return in_pieces(whole.rows, whole.kb, 128, [&](int64_t r, int64_t n) {
+        TileArgs a = whole;
+        a.rows = n;
+        a.x = (const char *)a.x + r * a.ldx * (codes ? 1 : element(dtype));
+        if (a.xs) a.xs += r * a.ldxs;
+        if (a.codes) a.codes += r * a.ldc, a.scales += r * a.lds;
+        if (a.turned) a.turned += r, a.tscales += r / 128;
+        const dim3 grid((unsigned)((n + 127) / 128 * a.kb));
+        if (codes) {
+            if (format == IMUNPACK_E4M3) hipLaunchKernelGGL((block8_tile_kernel<uint8_t, IMUNPACK_E4M3>), grid, dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((block8_tile_kernel<uint8_t, IMUNPACK_E5M2>), grid, dim3(256), 0, st, a);
+        } else {
+            by_type(dtype, format, [&](auto t, auto f) { hipLaunchKernelGGL((block8_tile_kernel<decltype(t), decltype(f)::value>), grid, dim3(256), 0, st, a); });
+        }
+    });
+}
+}  // namespace imu
+
+using namespace imu;
+
+extern "C" int imunpack_block8_quantize(const void *x, int64_t ldx, int64_t rows, int64_t cols, int dtype, int format, int square, void *codes, int64_t ldc, void *scales,
+                                        int64_t lds, void *turned, int64_t ldt, void *turned_scales, int64_t ldts, imunpack_stream_t stream) {
+    if (!sizes_fit(rows, cols) || !type_fits(dtype) || !format_fits(format) || ldx < cols) return IMUNPACK_EINVAL;
+    if (turned && rows > kBlock8Cols) return IMUNPACK_EINVAL;
+    if (rows == 0) return IMUNPACK_OK;
+    const Blocks8 q = {(uint8_t *)codes, (uint8_t *)scales, ldc, lds}, t = {(uint8_t *)turned, (uint8_t *)turned_scales, ldt, ldts};
+    if (!x || (!codes && !turned) || (codes && !blocks8_fit(q, cols)) || (turned && !blocks8_fit(t, rows))) return IMUNPACK_EINVAL;
+    const hipStream_t st = (hipStream_t)stream;
+    const int kb = blocks_of(cols);
+    if (turned || square) return tiles({x, nullptr, q.codes, q.scales, t.codes, t.scales, ldx, 0, ldc, lds, ldt, ldts, rows, (int)cols, kb, square}, dtype, format, false, st);
+    return in_pieces(rows, kb, 1, [&](int64_t r, int64_t n) {
+        const RowsArgs a = {(const char *)x + r * ldx * element(dtype), q.codes + r * ldc, q.scales + r * lds, ldx, ldc, lds, (int)n, (int)cols, kb};
+        const dim3 grid((unsigned)((n * kb + 16 * kRowsUnroll - 1) / (16 * kRowsUnroll)));
+        by_type(dtype, format, [&](auto e, auto f) { hipLaunchKernelGGL((block8_rows_kernel<decltype(e), decltype(f)::value>), grid, dim3(256), 0, st, a); });
+    });
+}
+
+extern "C" int imunpack_block8_turn(const void *codes, int64_t ldc, const void *scales, int64_t lds, int64_t rows, int64_t cols, int format, void *turned, int64_t ldt,
+                                    void *turned_scales, int64_t ldts, imunpack_stream_t stream) {
+    if (!sizes_fit(rows, cols) || rows > kBlock8Cols || !format_fits(format)) return IMUNPACK_EINVAL;
+    if (rows == 0) return IMUNPACK_OK;
+    const Blocks8 q = {(uint8_t *)codes, (uint8_t *)scales, ldc, lds}, t = {(uint8_t *)turned, (uint8_t *)turned_scales, ldt, ldts};
+    if (!blocks8_fit(q, cols) || !blocks8_fit(t, rows)) return IMUNPACK_EINVAL;
+    return tiles({q.codes, q.scales, nullptr, nullptr, t.codes, t.scales, ldc, lds, 0, 0, ldt, ldts, rows, (int)cols, blocks_of(cols), 0}, IMUNPACK_F32, format, true,
+                 (hipStream_t)stream);
+}
+
+extern "C" int imunpack_block8_values(const void *codes, int64_t ldc, const void *scales, int64_t lds, int64_t rows, int64_t cols, int format, void *out, int64_t ldo, int dtype,
+                                      imunpack_stream_t stream) {
+    if (!sizes_fit(rows, cols) || !type_fits(dtype) || !format_fits(format) || ldo < cols) return IMUNPACK_EINVAL;
+    if (rows == 0) return IMUNPACK_OK;
+    const Blocks8 q = {(uint8_t *)codes, (uint8_t *)scales, ldc, lds};
+    if (!out || !blocks8_fit(q, cols)) return IMUNPACK_EINVAL;
+    const int kb = blocks_of(cols);
+    return in_pieces(rows, kb, 1, [&](int64_t r, int64_t n) {
+        const ValuesArgs a = {q.codes + r * ldc, q.scales + r * lds, (char *)out + r * ldo * element(dtype), ldc, lds, ldo, (int)n, (int)cols, kb};
+        const dim3 grid((unsigned)((n * kb + 15) / 16));
+        by_type(dtype, format, [&](auto e, auto f) { hipLaunchKernelGGL((block8_values_kernel<decltype(e), decltype(f)::value>), grid, dim3(256), 0, (hipStream_t)stream, a); });
+    });
+}
+
+// f(float or __bf16, function, gated or not) by what the call says.
+template <class F>
+static void by_act(int dtype, int act, int gated, F f) {
+    auto typed = [&](auto t) {
+        using G = std::integral_constant<int, IMUNPACK_GELU>;
+        using S = std::integral_constant<int, IMUNPACK_SILU>;
+        if (act == IMUNPACK_GELU) gated ? f(t, G(), std::true_type()) : f(t, G(), std::false_type());
+        else gated ? f(t, S(), std::true_type()) : f(t, S(), std::false_type());
+    };
+    if (dtype == IMUNPACK_F32) typed(0.0f);
+    else typed((__bf16)0.0f);
+}
+static bool act_fits(int64_t rows, int64_t cols, int dtype, int act) {
+    return sizes_fit(rows, cols) && type_fits(dtype) && (act == IMUNPACK_GELU || act == IMUNPACK_SILU);
+}
+
+extern "C" int imunpack_act8(const void *u, int64_t ldu, int64_t rows, int64_t cols, int dtype, int act, int gated, void *y, int64_t ldy, void *y_codes, int64_t ldyc,
+                             void *y_scales, int64_t ldys, void *kept, void *kept2, int64_t ldk, void *kept_scales, void *kept2_scales, int64_t ldks, imunpack_stream_t stream) {
+    if (!act_fits(rows, cols, dtype, act) || ldu < cols * (gated ? 2 : 1) || (y && ldy < cols)) return IMUNPACK_EINVAL;
+    if (rows == 0) return IMUNPACK_OK;
+    const Blocks8 q = {(uint8_t *)y_codes, (uint8_t *)y_scales, ldyc, ldys}, k = {(uint8_t *)kept, (uint8_t *)kept_scales, ldk, ldks},
+                  k2 = {(uint8_t *)kept2, (uint8_t *)kept2_scales, ldk, ldks};
+    if (!u || (!y && !y_codes) || (y_codes && !blocks8_fit(q, cols)) || (kept && !blocks8_fit(k, cols)) || (kept && gated && !blocks8_fit(k2, cols))) return IMUNPACK_EINVAL;
+    const int kb = blocks_of(cols);
+    auto from = [](Blocks8 t, int64_t r) { return t.codes ? Blocks8{t.codes + r * t.ldc, t.scales + r * t.lds, t.ldc, t.lds} : t; };
+    return in_pieces(rows, kb, 1, [&](int64_t r, int64_t n) {
+        const int64_t size = element(dtype);
+        const ActArgs a = {(const char *)u + r * ldu * size, y ? (char *)y + r * ldy * size : nullptr, from(q, r), from(k, r), from(k2, r), ldu, ldy, (int)n, (int)cols, kb};
+        const dim3 grid((unsigned)((n * kb + 15) / 16));
+        by_act(dtype, act, gated, [&](auto t, auto f, auto g) {
+            hipLaunchKernelGGL((act8_kernel<decltype(t), decltype(f)::value, decltype(g)::value>), grid, dim3(256), 0, (hipStream_t)stream, a);
+        });
+    });
+}
+
+extern "C" int imunpack_act8_backward(const void *g, int64_t ldg, int64_t rows, int64_t cols, int dtype, int act, int gated, const void *kept, const void *kept2, int64_t ldk,
+                                      const void *kept_scales, const void *kept2_scales, int64_t ldks, void *gu, int64_t ldgu, imunpack_stream_t stream) {
+    if (!act_fits(rows, cols, dtype, act) || ldg < cols || ldgu < cols * (gated ? 2 : 1)) return IMUNPACK_EINVAL;
+    if (rows == 0) return IMUNPACK_OK;
+    const Blocks8 k = {(uint8_t *)kept, (uint8_t *)kept_scales, ldk, ldks}, k2 = {(uint8_t *)kept2, (uint8_t *)kept2_scales, ldk, ldks};
+    if (!g || !gu || !blocks8_fit(k, cols) || (gated && !blocks8_fit(k2, cols))) return IMUNPACK_EINVAL;
+    const int kb = blocks_of(cols);
+    auto from = [](Blocks8 t, int64_t r) { return t.codes ? Blocks8{t.codes + r * t.ldc, t.scales + r * t.lds, t.ldc, t.lds} : t; };
+    return in_pieces(rows, kb, 1, [&](int64_t r, int64_t n) {
+        const int64_t size = element(dtype);
+        const ActBackArgs a = {(const char *)g + r * ldg * size, (char *)gu + r * ldgu * size, from(k, r), from(k2, r), ldg, ldgu, (int)n, (int)cols, kb};
+        const dim3 grid((unsigned)((n * kb + 15) / 16));
+        by_act(dtype, act, gated, [&](auto t, auto f, auto gt) {
+            hipLaunchKernelGGL((act8_back_kernel<decltype(t), decltype(f)::value, decltype(gt)::value>), grid, dim3(256), 0, (hipStream_t)stream, a);
+        });
+    });
+}

@@ -25,6 +25,16 @@ decltype(&imunpack_adamw) g_adamw = nullptr;
 decltype(&imunpack_xent_workspace) g_xent_workspace = nullptr;
 decltype(&imunpack_xent) g_xent = nullptr;
 decltype(&imunpack_xent_rescale) g_xent_rescale = nullptr;
+decltype(&imunpack_block8_quantize) g_block8_quantize = nullptr;
+decltype(&imunpack_block8_turn) g_block8_turn = nullptr;
+decltype(&imunpack_block8_values) g_block8_values = nullptr;
+decltype(&imunpack_block8_gemm_workspace) g_block8_gemm_workspace = nullptr;
+decltype(&imunpack_block8_gemm) g_block8_gemm = nullptr;
+decltype(&imunpack_act8) g_act8 = nullptr;
+decltype(&imunpack_act8_backward) g_act8_backward = nullptr;
+decltype(&imunpack_logprobs_workspace) g_logprobs_workspace = nullptr;
+decltype(&imunpack_logprobs) g_logprobs = nullptr;
+decltype(&imunpack_logprobs_backward) g_logprobs_backward = nullptr;
 
 struct Refused : std::runtime_error {  // becomes a ValueError
     using std::runtime_error::runtime_error;
@@ -295,6 +305,201 @@ PyObject *xent_rescale(PyObject *const *a) {  // x, w, target, grad, gx, gw, str
     Py_RETURN_NONE;
 }
 
+// A tensor in 8 bits: codes over whole blocks and a power of two (a byte) for every row and block.
+constexpr int64_t kBlock = IMUNPACK_BLOCK8;
+int64_t whole_of(int64_t n, int64_t of) { return (n + of - 1) / of * of; }
+struct Eight {
+    at::Tensor codes, scales;
+    int64_t cols = 0, ldc = 0, lds = 0;
+    int format = 0;
+    void *c() const { return data(codes); }
+    void *s() const { return data(scales); }
+    int64_t rows() const { return codes.size(0); }
+};
+int format_of(at::ScalarType t, const char *what) {
+    if (t == at::kFloat8_e4m3fn) return IMUNPACK_E4M3;
+    if (t == at::kFloat8_e5m2) return IMUNPACK_E5M2;
+    throw Refused(std::string(what) + ": codes are float8_e4m3fn or float8_e5m2");
+}
+Eight eight(PyObject *codes, PyObject *scales, PyObject *cols, const char *what) {
+    Eight e = {tensor(codes, what), tensor(scales, what), whole(cols)};
+    const at::Tensor &c = e.codes, &s = e.scales;
+    e.format = format_of(c.scalar_type(), what);
+    auto dense = [](const at::Tensor &t, int64_t least) {
+        return t.is_cuda() && t.dim() == 2 && t.size(1) >= least && (t.stride(1) == 1 || t.size(1) == 1) && (t.size(0) <= 1 || (t.stride(0) >= t.size(1) && t.stride(0) % 16 == 0)) &&
+               (uintptr_t)t.data_ptr() % 16 == 0;
+    };
+    if (e.cols < 1 || s.scalar_type() != at::kFloat8_e8m0fnu || !dense(c, whole_of(e.cols, kBlock)) || !dense(s, whole_of((e.cols + kBlock - 1) / kBlock, 16)) || s.size(0) != c.size(0) ||
+        !beside(s, c))
+        throw Refused(std::string(what) + ": not a tensor in 8 bits as imunpack_block8_quantize lays it out");
+    e.ldc = c.size(0) > 1 ? c.stride(0) : whole_of(c.size(1), 16);
+    e.lds = s.size(0) > 1 ? s.stride(0) : whole_of(s.size(1), 16);
+    return e;
+}
+Eight new_eight(int64_t rows, int64_t cols, at::ScalarType type, const at::Tensor &like) {
+    Eight e;
+    e.cols = cols, e.ldc = whole_of(cols, kBlock), e.lds = whole_of(e.ldc / kBlock, 16);
+    e.codes = at::empty({rows, e.ldc}, like.options().dtype(type).requires_grad(false));
+    e.scales = at::empty({rows, e.lds}, like.options().dtype(at::kFloat8_e8m0fnu).requires_grad(false));
+    return e;
+}
+int64_t rows_of(const at::Tensor &x, int64_t cols) { return cols ? x.numel() / cols : 0; }
+
+PyObject *block8_quantize(PyObject *const *a) {  // x, e5m2, square, lying, turned, stream -> codes, scales, turned codes, turned scales
+    const at::Tensor &x = tensor(a[0], "block8: x");
+    const int type = type_of(x, "block8: x"), format = truth(a[1]) ? IMUNPACK_E5M2 : IMUNPACK_E4M3;
+    need(x.is_cuda() && x.dim() >= 1 && x.size(-1) >= 1, "block8: x is a device tensor with columns");
+    need_current(x.device());
+    const int64_t cols = x.size(-1), rows = rows_of(x, cols);
+    const Rows r = spread(x, cols);
+    const at::ScalarType code = format == IMUNPACK_E5M2 ? at::kFloat8_e5m2 : at::kFloat8_e4m3fn;
+    Eight q, t;
+    if (truth(a[3])) q = new_eight(rows, cols, code, x);
+    if (truth(a[4])) {
+        need(rows >= 1, "block8: a tensor without rows cannot be turned");
+        t = new_eight(cols, rows, code, x);
+    }
+    check(g_block8_quantize(r.p, r.pitch, rows, cols, type, format, truth(a[2]), q.c(), q.ldc, q.s(), q.lds, t.c(), t.ldc, t.s(), t.lds, address(a[5])), "imunpack_block8_quantize");
+    return wrapped<4>({q.codes, q.scales, t.codes, t.scales});
+}
+
+PyObject *block8_turn(PyObject *const *a) {  // codes, scales, cols, stream -> codes, scales
+    const Eight q = eight(a[0], a[1], a[2], "block8: x");
+    need(q.rows() >= 1, "block8: a tensor without rows cannot be turned");
+    need_current(q.codes.device());
+    const Eight t = new_eight(q.cols, q.rows(), q.codes.scalar_type(), q.codes);
+    check(g_block8_turn(q.c(), q.ldc, q.s(), q.lds, q.rows(), q.cols, q.format, t.c(), t.ldc, t.s(), t.lds, address(a[3])), "imunpack_block8_turn");
+    return wrapped<2>({t.codes, t.scales});
+}
+
+PyObject *block8_values(PyObject *const *a) {  // codes, scales, cols, bf16, stream -> values
+    const Eight q = eight(a[0], a[1], a[2], "block8: x");
+    need_current(q.codes.device());
+    const bool half = truth(a[3]);
+    const at::Tensor out = at::empty({q.rows(), q.cols}, q.codes.options().dtype(half ? at::kBFloat16 : at::kFloat));
+    check(g_block8_values(q.c(), q.ldc, q.s(), q.lds, q.rows(), q.cols, q.format, out.data_ptr(), q.cols, half ? IMUNPACK_BF16 : IMUNPACK_F32, address(a[4])), "imunpack_block8_values");
+    return wrap(out);
+}
+
+PyObject *block8_gemm(PyObject *const *a) {  // codes, scales of A, codes, scales of B, cols of A, of B, bf16, bias, stream -> out
+    const Eight x = eight(a[0], a[1], a[4], "block8_gemm: A"), w = eight(a[2], a[3], a[5], "block8_gemm: B");
+    const at::Tensor bias = maybe(a[7], "block8_gemm: bias");
+    need(x.cols == w.cols, "block8_gemm: A and B have no product A B^T");
+    need(beside(w.codes, x.codes) && beside(bias, x.codes), "block8_gemm: tensors of different devices");
+    need(!bias.defined() || (bias.scalar_type() == at::kFloat && bias.is_contiguous() && bias.dim() == 1 && bias.size(0) == w.rows()), "block8_gemm: bias is fp32, one for each row of B");
+    need_current(x.codes.device());
+    const int64_t m = x.rows(), n = w.rows();
+    const int type = truth(a[6]) ? IMUNPACK_BF16 : IMUNPACK_F32;
+    const at::Tensor out = at::empty({m, n}, x.codes.options().dtype(type == IMUNPACK_BF16 ? at::kBFloat16 : at::kFloat));
+    size_t bytes = 0;
+    check(g_block8_gemm_workspace(m, n, x.cols, type, &bytes), "imunpack_block8_gemm_workspace");
+    at::Tensor workspace;
+    if (bytes) workspace = at::empty({(int64_t)bytes}, x.codes.options().dtype(at::kByte));
+    check(g_block8_gemm(x.c(), x.ldc, x.s(), x.lds, x.format, w.c(), w.ldc, w.s(), w.lds, w.format, m, n, x.cols, (const float *)data(bias), out.data_ptr(), n, type,
+                        data(workspace), bytes, address(a[8])), "imunpack_block8_gemm");
+    return wrap(out);
+}
+
+PyObject *act8(PyObject *const *a) {  // u, act, gated, quantize, keep, want_y, stream -> y, codes, scales, kept codes, scales, kept2 codes, scales
+    const at::Tensor &u = tensor(a[0], "act8: u");
+    const int type = type_of(u, "act8: u"), act = (int)whole(a[1]);
+    const bool gated = truth(a[2]), keep = truth(a[4]);
+    need(u.is_cuda() && u.dim() >= 1 && u.size(-1) >= 1 && (!gated || u.size(-1) % 2 == 0), "act8: u is a device tensor with columns, twice as many where it is gated");
+    need_current(u.device());
+    const int64_t wide = u.size(-1), cols = gated ? wide / 2 : wide, rows = rows_of(u, wide);
+    const Rows r = spread(u, wide);
+    auto shape = u.sizes().vec();
+    shape.back() = cols;
+    Eight q, k, k2;
+    at::Tensor y;
+    if (truth(a[5])) y = at::empty(shape, u.options().requires_grad(false));
+    if (truth(a[3])) q = new_eight(rows, cols, at::kFloat8_e4m3fn, u);
+    if (keep) k = new_eight(rows, cols, at::kFloat8_e4m3fn, u);
+    if (keep && gated) k2 = new_eight(rows, cols, at::kFloat8_e4m3fn, u);
+    check(g_act8(r.p, r.pitch, rows, cols, type, act, gated, data(y), cols, q.c(), q.ldc, q.s(), q.lds, k.c(), k2.c(), k.ldc, k.s(), k2.s(), k.lds, address(a[6])), "imunpack_act8");
+    return wrapped<7>({y, q.codes, q.scales, k.codes, k.scales, k2.codes, k2.scales});
+}
+
+PyObject *act8_backward(PyObject *const *a) {  // g, act, kept codes, scales, kept2 codes, scales (None: not gated), cols, stream -> gu
+    const at::Tensor &g = tensor(a[0], "act8: g");
+    const int type = type_of(g, "act8: g");
+    const bool gated = a[4] != Py_None;
+    const Eight k = eight(a[2], a[3], a[6], "act8: kept"), k2 = gated ? eight(a[4], a[5], a[6], "act8: kept") : Eight();
+    const int64_t cols = k.cols, rows = k.rows();
+    need(g.is_cuda() && g.dim() >= 1 && g.size(-1) == cols && g.numel() == rows * cols, "act8: g is shaped like y");
+    need(k.format == IMUNPACK_E4M3 && (!gated || (k2.format == IMUNPACK_E4M3 && k2.rows() == rows && k2.ldc == k.ldc && k2.lds == k.lds)), "act8: kept must be what imunpack_act8 returned");
+    need(beside(k.codes, g) && beside(k2.codes, g), "act8: tensors of different devices");
+    need_current(g.device());
+    const Rows r = spread(g, cols);
+    auto shape = g.sizes().vec();
+    shape.back() = gated ? 2 * cols : cols;
+    const at::Tensor gu = at::empty(shape, g.options().requires_grad(false));
+    check(g_act8_backward(r.p, r.pitch, rows, cols, type, (int)whole(a[1]), gated, k.c(), k2.c(), k.ldc, k.s(), k2.s(), k.lds, gu.data_ptr(), shape.back(), address(a[7])),
+          "imunpack_act8_backward");
+    return wrap(gu);
+}
+
+struct Logprobs {  // the arguments that log probabilities and their gradients take, checked
+    at::Tensor logits, tokens;
+    int64_t vocab, rows, count;
+    int type;
+};
+Logprobs logprobs_arguments(PyObject *const *a) {  // logits, tokens (None: none)
+    Logprobs n = {tensor(a[0], "logprobs: logits"), maybe(a[1], "logprobs: tokens"), 0, 0, 0, 0};
+    n.type = type_of(n.logits, "logprobs: logits");
+    need(n.logits.is_cuda() && n.logits.dim() >= 1 && n.logits.size(-1) >= 1, "logprobs: logits are a device tensor with columns");
+    n.vocab = n.logits.size(-1);
+    n.rows = rows_of(n.logits, n.vocab);
+    if (n.tokens.defined()) {
+        const auto lead = n.logits.sizes().slice(0, n.logits.dim() - 1), given = n.tokens.sizes();
+        const bool one = given == lead, some = given.size() == lead.size() + 1 && given.slice(0, lead.size()) == lead;
+        need(n.tokens.is_cuda() && n.tokens.scalar_type() == at::kLong && (one || some), "logprobs: tokens are an int64 device tensor of the logits' leading shape, or with some to a row behind it");
+        need(beside(n.tokens, n.logits), "logprobs: tensors of different devices");
+        n.count = one ? 1 : given.back();
+        n.tokens = n.tokens.contiguous();
+    }
+    need_current(n.logits.device());
+    return n;
+}
+PyObject *logprobs(PyObject *const *a) {  // logits, tokens, ignore_index, top, want_entropy, stream -> logp, lse, stats, entropy, top_logp, top_index
+    const Logprobs n = logprobs_arguments(a);
+    const int64_t top = whole(a[3]);
+    need(top >= 0 && top <= IMUNPACK_LOGPROBS_TOP && top <= n.vocab, "logprobs: top is 0 to 64 and no more than there are logits");
+    const Rows l = spread(n.logits, n.vocab);
+    const at::TensorOptions floats = n.logits.options().dtype(at::kFloat).requires_grad(false);
+    const auto lead = n.logits.sizes().slice(0, n.logits.dim() - 1);
+    auto shape = lead.vec();
+    shape.push_back(top);
+    const at::Tensor logp = n.tokens.defined() ? at::empty(n.tokens.sizes(), floats) : at::Tensor(), lse = at::empty(lead, floats), stats = at::empty({n.rows, 2}, floats), entropy = truth(a[4]) ? at::empty(lead, floats) : at::Tensor();
+    const at::Tensor top_logp = top ? at::empty(shape, floats) : at::Tensor(), top_index = top ? at::empty(shape, floats.dtype(at::kLong)) : at::Tensor();
+    size_t bytes = 0;
+    check(g_logprobs_workspace(n.rows, n.vocab, n.count, top, n.type, &bytes), "imunpack_logprobs_workspace");
+    at::Tensor workspace;
+    if (bytes) workspace = at::empty({(int64_t)bytes}, floats.dtype(at::kByte));
+    check(g_logprobs(l.p, l.pitch, n.rows, n.vocab, n.type, (const int64_t *)data(n.tokens), n.count, whole(a[2]), top, (float *)data(logp), (float *)data(lse), (float *)data(stats),
+                     (float *)data(entropy), (float *)data(top_logp), (int64_t *)data(top_index), data(workspace), bytes, address(a[5])), "imunpack_logprobs");
+    return wrapped<6>({logp, lse, stats, entropy, top_logp, top_index});
+}
+PyObject *logprobs_backward(PyObject *const *a) {  // logits, tokens, ignore_index, top_index, stats, entropy, g_logp, g_entropy, g_top, stream -> gl
+    const Logprobs n = logprobs_arguments(a);
+    const at::Tensor index = maybe(a[3], "logprobs: top_index"), stats = tensor(a[4], "logprobs: saved"), entropy = maybe(a[5], "logprobs: saved"), gp = maybe(a[6], "logprobs: g_logp"),
+                     gh = maybe(a[7], "logprobs: g_entropy"), gt = maybe(a[8], "logprobs: g_top");
+    auto floats = [&](const at::Tensor &t, int64_t each) {
+        return !t.defined() || (t.is_cuda() && t.scalar_type() == at::kFloat && t.is_contiguous() && t.numel() == n.rows * each && beside(t, n.logits));
+    };
+    const int64_t top = index.defined() ? index.size(-1) : 0;
+    need(floats(stats, 2) && floats(entropy, 1) && (!index.defined() || (index.is_cuda() && index.scalar_type() == at::kLong && index.is_contiguous() && index.numel() == n.rows * top && beside(index, n.logits))),
+         "logprobs: saved must be what imunpack_logprobs returned");
+    need(floats(gp, n.count) && floats(gh, 1) && floats(gt, top), "logprobs: gradients are fp32 device tensors shaped like what they belong to");
+    need((!gp.defined() || n.tokens.defined()) && (!gh.defined() || entropy.defined()) && (!gt.defined() || index.defined()), "logprobs: a gradient of something that was not asked for");
+    const Rows l = spread(n.logits, n.vocab);
+    const at::Tensor gl = dense_like(n.logits, n.logits.scalar_type());
+    check(g_logprobs_backward(l.p, l.pitch, n.rows, n.vocab, n.type, (const int64_t *)data(n.tokens), n.count, whole(a[2]), top, (const int64_t *)data(index), (const float *)data(stats),
+                              (const float *)data(entropy), (const float *)data(gp), (const float *)data(gh), (const float *)data(gt), gl.data_ptr(), n.vocab, address(a[9])),
+          "imunpack_logprobs_backward");
+    return wrap(gl);
+}
+
 PyObject *bind(PyObject *const *a) {  // error class, then the addresses of the library's functions
     Py_INCREF(a[0]);
     Py_XDECREF(g_error);
@@ -307,6 +512,16 @@ PyObject *bind(PyObject *const *a) {  // error class, then the addresses of the 
     g_xent_workspace = (decltype(g_xent_workspace))address(a[6]);
     g_xent = (decltype(g_xent))address(a[7]);
     g_xent_rescale = (decltype(g_xent_rescale))address(a[8]);
+    g_block8_quantize = (decltype(g_block8_quantize))address(a[9]);
+    g_block8_turn = (decltype(g_block8_turn))address(a[10]);
+    g_block8_values = (decltype(g_block8_values))address(a[11]);
+    g_block8_gemm_workspace = (decltype(g_block8_gemm_workspace))address(a[12]);
+    g_block8_gemm = (decltype(g_block8_gemm))address(a[13]);
+    g_act8 = (decltype(g_act8))address(a[14]);
+    g_act8_backward = (decltype(g_act8_backward))address(a[15]);
+    g_logprobs_workspace = (decltype(g_logprobs_workspace))address(a[16]);
+    g_logprobs = (decltype(g_logprobs))address(a[17]);
+    g_logprobs_backward = (decltype(g_logprobs_backward))address(a[18]);
     Py_RETURN_NONE;
 }
 
@@ -327,9 +542,12 @@ template <PyObject *(*F)(PyObject *const *), Py_ssize_t N>
 PyMethodDef method(const char *name) {
     return {name, (PyCFunction)(void (*)(void))entry<F, N>, METH_FASTCALL, nullptr};
 }
-PyMethodDef g_methods[] = {method<bind, 9>("bind"), method<rmsnorm, 5>("rmsnorm"), method<rmsnorm_quantize, 7>("rmsnorm_quantize"),
+PyMethodDef g_methods[] = {method<bind, 19>("bind"), method<rmsnorm, 5>("rmsnorm"), method<rmsnorm_quantize, 7>("rmsnorm_quantize"),
                            method<rmsnorm_backward, 8>("rmsnorm_backward"), method<adamw, 15>("adamw"),
-                           method<xent, 10>("xent"), method<xent_rescale, 7>("xent_rescale"), {nullptr, nullptr, 0, nullptr}};
+                           method<xent, 10>("xent"), method<xent_rescale, 7>("xent_rescale"),
+                           method<block8_quantize, 6>("block8_quantize"), method<block8_turn, 4>("block8_turn"), method<block8_values, 5>("block8_values"),
+                           method<block8_gemm, 9>("block8_gemm"), method<act8, 7>("act8"), method<act8_backward, 8>("act8_backward"), method<logprobs, 6>("logprobs"),
+                           method<logprobs_backward, 10>("logprobs_backward"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_tensors", "Argument marshalling of the calls whose host time counts.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 }  // namespace
 
