@@ -4,11 +4,14 @@
 //
 // The codes with their power of two are numbers of bfloat16, so that products on v_mfma_f32_32x32x16_bf16 are exact and sums binary32's.
 #include "block8.h"
+#include "product.h"
+
+#include <algorithm>
+#include <atomic>
 
 namespace imu {
-typedef float v16f32 __attribute__((ext_vector_type(16)));
 typedef __bf16 v2bf16 __attribute__((ext_vector_type(2)));
-typedef __bf16 v8bf16 __attribute__((ext_vector_type(8)));
+typedef int v8i32 __attribute__((ext_vector_type(8)));
 
 struct GemmArgs {
     const uint8_t *a, *sa, *b, *sb;
@@ -17,6 +20,8 @@ struct GemmArgs {
     int64_t lda, ldsa, ldb, ldsb, ldo;
     int m, n, kt;       // kt: blocks of the contraction
     int mtiles, ntiles;
+    int parts, per;     // of the contraction, blocks of each; with several, `out` is the workspace: fp32, m x n for each
+    int half;           // bfloat16 results
 };
 
 // Eight codes times their power of two as bfloat16 (exact).
@@ -31,6 +36,256 @@ __device__ __forceinline__ v8bf16 widen(uint32_t lo, uint32_t hi, float scale) {
         p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, false), p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, true);
     }
     return v8bf16{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
+}
+
+
+// ---- large products: tiles of (64 TM) x (64 TN), 2 x 2 waves of (32 TM) x (32 TN) -------------------------------------------------
+// The walk over the contraction is that of product.h, whose k-tiles of 128 bytes are blocks of 128 places here: loads straight into LDS, a ring of five
+// half-stages (A and B of a k-tile in slots of their own), one barrier to a k-tile, loads two k-tiles ahead; 16-byte piece c of row r at slot c ^ ((r >> 1) & 7).
+// Powers of two are bytes beside the codes: a lane holds those of its rows for 4 G k-tiles, loaded ahead.
+//
+// NATIVE: v_mfma_scale_f32_32x32x64_f8f6f4, which takes codes and bytes as they are.  It adds eight products at a time and cuts each of them below 2^-13 of the
+// largest's power of two, so that a result of random operands is off by 1.5e-5 of its size: a hundredth of what rounding it to bfloat16 leaves, too much for fp32.
+// Otherwise codes become bfloat16 numbers times their power of two between LDS and the matrix instruction (exact), at half the rate.
+template <bool NATIVE, int FA, int FB, int TM, int TN, int G>
+__device__ __forceinline__ void product8_tile(const GemmArgs &g, int m0, int n0, int k0, int k1, char *smem, v16f32 (&acc)[TM][TN]) {
+    constexpr int kSlot = 64 * (TM > TN ? TM : TN) * kStageBytes, LA = 2 * TM, LB = 2 * TN, NF = TM + TN, NM = TM * TN, kSteps = NATIVE ? 2 : 4;
+    constexpr bool kFour = TM == 4 && TN == 4;
+    typedef int wide_t __attribute__((ext_vector_type(G)));
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    const int total = k1 - k0, lrow = lane & 31, lhalf = lane >> 5;
+    const unsigned lds0 = (unsigned)(size_t)smem;
+    // where the lane's part of load 0 lies; load u is 8 u rows on, the last row at most (offsets stay below 2^32: a pitch is 2^24 at most)
+    const unsigned offA = (unsigned)(16 * TM * wave + (lane >> 3)) * (unsigned)g.lda, offB = (unsigned)(16 * TN * wave + (lane >> 3)) * (unsigned)g.ldb;
+    const unsigned lastA = (unsigned)(min(g.m - 1 - m0, 64 * TM - 1)) * (unsigned)g.lda, lastB = (unsigned)(min(g.n - 1 - n0, 64 * TN - 1)) * (unsigned)g.ldb;
+    unsigned col[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) col[u] = (unsigned)(((lane & 7) ^ (((8 * u + (lane >> 3)) >> 1) & 7)) * 16);  // (rows 16 apart have the same)
+    const char *gA = (const char *)g.a + m0 * g.lda + k0 * 128, *gB = (const char *)g.b + n0 * g.ldb + k0 * 128;
+    // the bytes of the lane's rows
+    const uint8_t *tileA = g.sa + m0 * g.ldsa + k0, *tileB = g.sb + n0 * g.ldsb + k0;
+    unsigned rowA[TM], rowB[TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) rowA[i] = (unsigned)min(32 * (TM * wm + i) + lrow, g.m - 1 - m0) * (unsigned)g.ldsa;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) rowB[j] = (unsigned)min(32 * (TN * wn + j) + lrow, g.n - 1 - n0) * (unsigned)g.ldsb;
+    wide_t nextA[TM], nextB[TN];
+    int sA[TM], sB[TN];
+    auto load_bytes = [&](int kt) __attribute__((always_inline)) {
+        const int at = min(kt, (total - 1) / (4 * G) * (4 * G));
+#pragma unroll
+        for (int i = 0; i < TM; ++i) nextA[i] = *reinterpret_cast<const wide_t *>(tileA + at + rowA[i]);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) nextB[j] = *reinterpret_cast<const wide_t *>(tileB + at + rowB[j]);
+    };
+    auto take_bytes = [&]() __attribute__((always_inline)) {  // the next four k-tiles' become the current ones
+        auto shift = [](wide_t &w) __attribute__((always_inline)) {
+            const int x = w[0];
+#pragma unroll
+            for (int d = 1; d < G; ++d) w[d - 1] = w[d];
+            return x;
+        };
+#pragma unroll
+        for (int i = 0; i < TM; ++i) sA[i] = shift(nextA[i]);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sB[j] = shift(nextB[j]);
+    };
+    load_bytes(0);
+    take_bytes();
+    if constexpr (G == 1) load_bytes(4);
+
+    auto ring = [](int slot, int k) { slot += k; return slot >= kRing ? slot - kRing : slot; };
+    const char *pg = nullptr;
+    unsigned dl = 0;
+    auto setup = [&](bool isA, int kt, int slot) {  // (past the last k-tile it is loaded again, into a slot that is not read)
+        pg = uniform_address((isA ? gA : gB) + min(kt, total - 1) * 128);
+        dl = __builtin_amdgcn_readfirstlane(lds0 + (unsigned)(slot * kSlot) + (unsigned)(wave * (isA ? LA : LB) * 1024));
+    };
+    auto fetch = [&](bool isA, int u) __attribute__((always_inline)) { fetch_to_lds(dl + u * 1024, (isA ? min(offA + (unsigned)u * 8u * (unsigned)g.lda, lastA) : min(offB + (unsigned)u * 8u * (unsigned)g.ldb, lastB)) + col[u & 1], pg); };
+
+    const int swz = (lrow >> 1) & 7;
+    const unsigned baseA = (unsigned)((wm * 32 * TM + lrow) * kStageBytes), baseB = (unsigned)((wn * 32 * TN + lrow) * kStageBytes);
+    auto piece = [&](int c) { return (unsigned)((c ^ swz) << 4); };
+    v4i32 fa[2][TM][NATIVE ? 2 : 1], fb[2][TN][NATIVE ? 2 : 1];
+    constexpr int isA4[8] = {1, 0, 0, 1, 0, 0, 1, 1}, idx4[8] = {0, 0, 1, 1, 2, 3, 2, 3};
+    auto which = [&](int q, bool &isA, int &idx) __attribute__((always_inline)) {  // fragment q in the order in which the products need them
+        isA = kFour ? isA4[q] : q == 0 || q > TN;
+        idx = kFour ? idx4[q] : q == 0 ? 0 : q > TN ? q - TN : q - 1;
+    };
+    auto fragment = [&](const char *sa, const char *sb, int ks, int buf, int q) __attribute__((always_inline)) {
+        bool isA;
+        int idx;
+        which(q, isA, idx);
+        const char *p = isA ? sa + baseA + idx * 32 * kStageBytes : sb + baseB + idx * 32 * kStageBytes;
+        auto &f = isA ? fa[buf][idx] : fb[buf][idx];
+        if constexpr (NATIVE) {
+            f[0] = *reinterpret_cast<const v4i32 *>(p + piece(4 * ks + 2 * lhalf));
+            f[1] = *reinterpret_cast<const v4i32 *>(p + piece(4 * ks + 2 * lhalf + 1));
+        } else {
+            f[0] = *reinterpret_cast<const v4i32 *>(p + piece(2 * ks + lhalf));
+        }
+    };
+    v8bf16 ca[NATIVE ? 1 : TM][2], cb[NATIVE ? 1 : TN][2];
+    auto convert = [&](int buf, int q) __attribute__((always_inline)) {
+        if constexpr (!NATIVE) {
+            bool isA;
+            int idx;
+            which(q, isA, idx);
+            if (isA) {
+                const float s = __int_as_float((sA[idx] & 255) << 23);
+                const v4i32 w = fa[buf][idx][0];
+                ca[idx][0] = widen<FA>(w[0], w[1], s), ca[idx][1] = widen<FA>(w[2], w[3], s);
+            } else {
+                const float s = __int_as_float((sB[idx] & 255) << 23);
+                const v4i32 w = fb[buf][idx][0];
+                cb[idx][0] = widen<FB>(w[0], w[1], s), cb[idx][1] = widen<FB>(w[2], w[3], s);
+            }
+        }
+    };
+    auto multiply = [&](int buf, int m) __attribute__((always_inline)) {
+        constexpr int mi4[16] = {0, 0, 1, 1, 0, 0, 1, 1, 2, 2, 3, 3, 2, 2, 3, 3}, mj4[16] = {0, 1, 0, 1, 2, 3, 2, 3, 0, 1, 0, 1, 2, 3, 2, 3};
+        const int i = kFour ? mi4[m] : m / TN, j = kFour ? mj4[m] : m % TN;
+        if constexpr (NATIVE) {
+            const v4i32 a0 = fa[buf][i][0], a1 = fa[buf][i][1], b0 = fb[buf][j][0], b1 = fb[buf][j][1];
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(v8i32{b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]},
+                                                                        v8i32{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]}, acc[i][j], FB, FA, 0, sB[j], 0, sA[i]);
+        } else {
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cb[j][0], ca[i][0], acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cb[j][1], ca[i][1], acc[i][j], 0, 0, 0);
+        }
+    };
+    // the products of a k-step, the fragments of the next one and `count` loads from number `from` on among them
+    auto step = [&](int cur, const char *sa, const char *sb, int next_ks, bool isA, int from, int count) {
+        constexpr int kFirst = NM / NF >= 2 ? 3 : 2;  // fragments that the first products need
+        if constexpr (!NATIVE) {
+#pragma unroll
+            for (int q = 0; q < kFirst; ++q) convert(cur, q);
+        }
+#pragma unroll
+        for (int q = 0; q < NF; ++q) {
+            fragment(sa, sb, next_ks, cur ^ 1, q);
+            if constexpr (!NATIVE) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (kFirst + 2 * q + c < NF) convert(cur, kFirst + 2 * q + c);
+            }
+#pragma unroll
+            for (int m = q * NM / NF; m < (q + 1) * NM / NF; ++m) multiply(cur, m);
+#pragma unroll
+            for (int u = q * count / NF; u < (q + 1) * count / NF; ++u) fetch(isA, from + u);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        setup(true, p, 2 * p);
+#pragma unroll
+        for (int u = 0; u < LA; ++u) fetch(true, u);
+        setup(false, p, 2 * p + 1);
+#pragma unroll
+        for (int u = 0; u < LB; ++u) fetch(false, u);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"i"(LA + LB) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int q = 0; q < NF; ++q) fragment(smem, smem + kSlot, 0, 0, q);
+    // Before the last step of a k-tile every fragment of it has been read and this wave's parts of the next one have landed (all but the newest loads); past the
+    // barrier that holds for all waves, so that the last step may read k-tile kt + 1 and load B(kt + 2) into the slot of A(kt).
+    int sa = 0;
+    for (int kt = 0; kt < total; ++kt) {
+        const char *stA = smem + sa * kSlot, *stB = smem + ring(sa, 1) * kSlot;
+        const char *stA1 = smem + ring(sa, 2) * kSlot, *stB1 = smem + ring(sa, 3) * kSlot;
+        setup(true, kt + 2, ring(sa, 4));
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (NATIVE) {
+            step(0, stA, stB, 1, true, 0, LA);
+        } else {
+            constexpr int c0 = (LA + 2) / 3, c1 = (LA - c0 + 1) / 2;
+            step(0, stA, stB, 1, true, 0, c0);
+            step(1, stA, stB, 2, true, c0, c1);
+            step(0, stA, stB, 3, true, c0 + c1, LA - c0 - c1);
+        }
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(LA) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        setup(false, kt + 2, sa);
+        __builtin_amdgcn_sched_barrier(0);
+        step((kSteps - 1) & 1, stA1, stB1, 0, false, 0, LB);
+        sa = ring(sa, 2);
+        if ((kt & 3) == 3) {
+            take_bytes();
+            if (((kt + 5) & (4 * G - 1)) == 0) load_bytes(kt + 5);
+        } else {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) sA[i] = (int)((unsigned)sA[i] >> 8);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) sB[j] = (int)((unsigned)sB[j] >> 8);
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may land in LDS any more
+    __syncthreads();
+}
+
+template <bool NATIVE, int FA, int FB, int T>
+__global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void block8_tile_gemm_kernel(const GemmArgs g) {
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int tiles = g.mtiles * g.ntiles, part = (int)blockIdx.x / tiles;
+    int tm, tn;
+    tile_at((int)blockIdx.x - part * tiles, g.mtiles, g.ntiles, tm, tn);
+    v16f32 acc[T][T];
+    product8_tile<NATIVE, FA, FB, T, T, T == 4 ? 2 : 1>(g, tm * 64 * T, tn * 64 * T, part * g.per, min((part + 1) * g.per, g.kt), smem, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lrow = lane & 31, lhalf = lane >> 5;
+    const int m0 = tm * 64 * T + (wave >> 1) * 32 * T + lrow, n0 = tn * 64 * T + (wave & 1) * 32 * T + lhalf * 4;
+    float *sums = g.parts > 1 ? (float *)g.out + (int64_t)part * g.m * g.n : nullptr;
+#pragma unroll
+    for (int j = 0; j < T; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int n = n0 + 32 * j + 8 * q;
+            if (n >= g.n) continue;
+            float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (g.bias && !sums) load_upto<float, 4>(g.bias + n, bias, g.n - n);
+#pragma unroll
+            for (int i = 0; i < T; ++i) {
+                const int m = m0 + 32 * i;
+                if (m >= g.m) continue;
+                float f[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) f[r] = acc[i][j][q * 4 + r] + bias[r];
+                if (sums) store_upto<float, 4>(sums + (int64_t)m * g.n + n, f, g.n - n);
+                else if (NATIVE) store_upto<__bf16, 4>((__bf16 *)g.out + m * g.ldo + n, f, g.n - n);
+                else store_upto<float, 4>((float *)g.out + m * g.ldo + n, f, g.n - n);
+            }
+        }
+}
+
+// The sum of the parts in their order, four columns to a thread.
+template <class T>
+__global__ __launch_bounds__(256) void block8_fold_kernel(const float *__restrict__ sums, const float *__restrict__ bias, T *__restrict__ out, int64_t ldo, int parts, int m, int n) {
+    const int across = (n + 3) / 4;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / across;
+    const int col = (int)(at - row * across) * 4;
+    if (row >= m) return;
+    float f[4], s[4];
+    load_upto<float, 4>(sums + row * n + col, f, n - col);
+    for (int p = 1; p < parts; ++p) {
+        load_upto<float, 4>(sums + ((int64_t)p * m + row) * n + col, s, n - col);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[k] += s[k];
+    }
+    if (bias) {
+        load_upto<float, 4>(bias + col, s, n - col);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[k] += s[k];
+    }
+    store_upto<T, 4>(out + row * ldo + col, f, n - col);
 }
 
 // 64 x 64 results to a workgroup, 32 x 32 to a wave, operands straight from memory.
@@ -64,8 +319,35 @@ __global__ __launch_bounds__(256) void block8_gemm_kernel(const GemmArgs g) {
     }
 }
 
+// How a product is cut: tiles of 64 T, the contraction in parts of `per` blocks (multiples of 8 blocks for large tiles, of 4 for small ones).
+struct Cut {
+    int tile, parts, per;
+};
+static Cut cut_of(int64_t m, int64_t n, int64_t kt) {
+    const int64_t large = ((m + 255) / 256) * ((n + 255) / 256), small = ((m + 127) / 128) * ((n + 127) / 128);
+    if (large >= 160) return {4, 1, (int)((kt + 7) / 8 * 8)};
+    if (small * 4 < 64) return {1, 1, (int)kt};
+    int64_t parts = std::max<int64_t>(1, std::min<int64_t>(512 / small, kt / 8));
+    const int64_t per = ((kt + parts - 1) / parts + 3) / 4 * 4;
+    parts = (kt + per - 1) / per;
+    return {2, (int)parts, (int)per};
+}
+
+template <bool NATIVE, int FA, int FB, int T>
+static int launch_tiles(const GemmArgs &g, hipStream_t st) {
+    const auto kernel = block8_tile_gemm_kernel<NATIVE, FA, FB, T>;
+    static std::atomic<int> done{0};  // (the attribute is idempotent: two threads set the same)
+    if (!done.load(std::memory_order_acquire)) {
+        IMU_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, product_lds(T, T)));
+        done.store(1, std::memory_order_release);
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)g.mtiles * g.ntiles * g.parts)), dim3(kProductThreads), product_lds(T, T), st, g);
+    return launch_status();
+}
+
+constexpr int64_t kPitch = 1 << 24;  // bytes from row to row at most: offsets within a tile have 32 bits
 static bool operand_fits(const Blocks8 &t, int64_t rows, int64_t cols, int format) {
-    return blocks8_fit(t, cols) && rows >= 1 && (format == IMUNPACK_E4M3 || format == IMUNPACK_E5M2);
+    return blocks8_fit(t, cols) && rows >= 1 && t.ldc <= kPitch && (format == IMUNPACK_E4M3 || format == IMUNPACK_E5M2);
 }
 }  // namespace imu
 
@@ -75,7 +357,8 @@ constexpr int64_t kGemmRows = 1 << 24;
 
 extern "C" int imunpack_block8_gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, size_t *bytes) {
     if (m < 0 || n < 0 || k < 1 || m > kGemmRows || n > kGemmRows || k > kBlock8Cols || (dtype != IMUNPACK_F32 && dtype != IMUNPACK_BF16) || !bytes) return IMUNPACK_EINVAL;
-    *bytes = 0;
+    const Cut c = cut_of(m, n, (k + kBlock8 - 1) / kBlock8);
+    *bytes = c.parts > 1 ? (size_t)c.parts * (size_t)m * (size_t)n * sizeof(float) : 0;
     return IMUNPACK_OK;
 }
 
@@ -89,18 +372,31 @@ extern "C" int imunpack_block8_gemm(const void *a, int64_t lda, const void *a_sc
     if (!operand_fits(A, m, k, a_format) || !operand_fits(B, n, k, b_format) || !out || ldo < n) return IMUNPACK_EINVAL;
     if (need && (!workspace || ((uintptr_t)workspace & 15))) return IMUNPACK_EINVAL;
     if (workspace_bytes < need) return IMUNPACK_ESMALL;
-    GemmArgs g = {A.codes, A.scales, B.codes, B.scales, bias, out, lda, ldsa, ldb, ldsb, ldo, (int)m, (int)n, (int)((k + kBlock8 - 1) / kBlock8), 0, 0};
-    g.mtiles = (int)((m + 63) / 64);
-    g.ntiles = (int)((n + 63) / 64);
-    const int64_t groups = (int64_t)g.mtiles * g.ntiles;
-    if (groups > (1 << 23)) return IMUNPACK_EINVAL;
-    auto launch = [&](auto fa, auto fb, auto t) {
-        hipLaunchKernelGGL((block8_gemm_kernel<decltype(fa)::value, decltype(fb)::value, decltype(t)>), dim3((unsigned)groups), dim3(256), 0, (hipStream_t)stream, g);
+    const int kt = (int)((k + kBlock8 - 1) / kBlock8);
+    const Cut c = cut_of(m, n, kt);
+    const hipStream_t st = (hipStream_t)stream;
+    GemmArgs g = {A.codes, A.scales, B.codes, B.scales, bias, c.parts > 1 ? workspace : out, lda, ldsa, ldb, ldsb, ldo, (int)m, (int)n, kt, 0, 0, c.parts, c.per, dtype == IMUNPACK_BF16};
+    g.mtiles = (int)((m + 64 * c.tile - 1) / (64 * c.tile));
+    g.ntiles = (int)((n + 64 * c.tile - 1) / (64 * c.tile));
+    if ((int64_t)g.mtiles * g.ntiles * c.parts > (1 << 23)) return IMUNPACK_EINVAL;
+    const bool native = dtype == IMUNPACK_BF16;
+    auto launch = [&](auto fa, auto fb) {
+        constexpr int FA = decltype(fa)::value, FB = decltype(fb)::value;
+        if (c.tile == 4) return native ? launch_tiles<true, FA, FB, 4>(g, st) : launch_tiles<false, FA, FB, 4>(g, st);
+        if (c.tile == 2) return native ? launch_tiles<true, FA, FB, 2>(g, st) : launch_tiles<false, FA, FB, 2>(g, st);
+        const dim3 grid((unsigned)(g.mtiles * g.ntiles));
+        if (native) hipLaunchKernelGGL((block8_gemm_kernel<FA, FB, __bf16>), grid, dim3(256), 0, st, g);
+        else hipLaunchKernelGGL((block8_gemm_kernel<FA, FB, float>), grid, dim3(256), 0, st, g);
+        return launch_status();
     };
     using E4 = std::integral_constant<int, IMUNPACK_E4M3>;
     using E5 = std::integral_constant<int, IMUNPACK_E5M2>;
-    auto typed = [&](auto fa, auto fb) { dtype == IMUNPACK_F32 ? launch(fa, fb, 0.0f) : launch(fa, fb, (__bf16)0.0f); };
-    if (a_format == IMUNPACK_E4M3) b_format == IMUNPACK_E4M3 ? typed(E4(), E4()) : typed(E4(), E5());
-    else b_format == IMUNPACK_E4M3 ? typed(E5(), E4()) : typed(E5(), E5());
+    if (a_format == IMUNPACK_E4M3) IMU_TRY(b_format == IMUNPACK_E4M3 ? launch(E4(), E4()) : launch(E4(), E5()));
+    else IMU_TRY(b_format == IMUNPACK_E4M3 ? launch(E5(), E4()) : launch(E5(), E5()));
+    if (c.parts == 1) return IMUNPACK_OK;
+    const int64_t threads = m * ((n + 3) / 4);
+    const dim3 grid((unsigned)((threads + 255) / 256));
+    if (native) hipLaunchKernelGGL(block8_fold_kernel<__bf16>, grid, dim3(256), 0, st, (const float *)workspace, bias, (__bf16 *)out, ldo, c.parts, (int)m, (int)n);
+    else hipLaunchKernelGGL(block8_fold_kernel<float>, grid, dim3(256), 0, st, (const float *)workspace, bias, (float *)out, ldo, c.parts, (int)m, (int)n);
     return launch_status();
 }
