@@ -21,7 +21,6 @@ struct GemmArgs {
     int m, n, kt;       // kt: blocks of the contraction
     int mtiles, ntiles;
     int parts, per;     // of the contraction, blocks of each; with several, `out` is the workspace: fp32, m x n for each
-    int half;           // bfloat16 results
 };
 
 // Eight codes times their power of two as bfloat16 (exact).
@@ -77,28 +76,30 @@ __device__ __forceinline__ void product8_tile(const GemmArgs &g, int m0, int n0,
     for (int j = 0; j < TN; ++j) rowB[j] = (unsigned)min(32 * (TN * wn + j) + lrow, g.n - 1 - n0) * (unsigned)g.ldsb;
     wide_t nextA[TM], nextB[TN];
     int sA[TM], sB[TN];
+    auto shift = [](wide_t &w) __attribute__((always_inline)) {
+        const int x = w[0];
+#pragma unroll
+        for (int d = 1; d < G; ++d) w[d - 1] = w[d];
+        return x;
+    };
     auto load_bytes = [&](int kt) __attribute__((always_inline)) {
         const int at = min(kt, (total - 1) / (4 * G) * (4 * G));
+        const char *pA = uniform_address((const char *)tileA + at), *pB = uniform_address((const char *)tileB + at);
+        // (the row's offset is made opaque here: widened to 64 bits outside the loop it took two registers and an addition)
 #pragma unroll
-        for (int i = 0; i < TM; ++i) nextA[i] = *reinterpret_cast<const wide_t *>(tileA + at + rowA[i]);
+        for (int i = 0; i < TM; ++i) {
+            unsigned r = rowA[i];
+            asm volatile("" : "+v"(r));
+            nextA[i] = *reinterpret_cast<const wide_t *>(pA + r);
+        }
 #pragma unroll
-        for (int j = 0; j < TN; ++j) nextB[j] = *reinterpret_cast<const wide_t *>(tileB + at + rowB[j]);
-    };
-    auto take_bytes = [&]() __attribute__((always_inline)) {  // the next four k-tiles' become the current ones
-        auto shift = [](wide_t &w) __attribute__((always_inline)) {
-            const int x = w[0];
-#pragma unroll
-            for (int d = 1; d < G; ++d) w[d - 1] = w[d];
-            return x;
-        };
-#pragma unroll
-        for (int i = 0; i < TM; ++i) sA[i] = shift(nextA[i]);
-#pragma unroll
-        for (int j = 0; j < TN; ++j) sB[j] = shift(nextB[j]);
+        for (int j = 0; j < TN; ++j) {
+            unsigned r = rowB[j];
+            asm volatile("" : "+v"(r));
+            nextB[j] = *reinterpret_cast<const wide_t *>(pB + r);
+        }
     };
     load_bytes(0);
-    take_bytes();
-    if constexpr (G == 1) load_bytes(4);
 
     auto ring = [](int slot, int k) { slot += k; return slot >= kRing ? slot - kRing : slot; };
     const char *pg = nullptr;
@@ -154,7 +155,7 @@ __device__ __forceinline__ void product8_tile(const GemmArgs &g, int m0, int n0,
         if constexpr (NATIVE) {
             const v4i32 a0 = fa[buf][i][0], a1 = fa[buf][i][1], b0 = fb[buf][j][0], b1 = fb[buf][j][1];
             acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(v8i32{b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]},
-                                                                        v8i32{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]}, acc[i][j], FB, FA, 0, sB[j], 0, sA[i]);
+                                                                v8i32{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]}, acc[i][j], FB, FA, 0, sB[j], 0, sA[i]);
         } else {
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cb[j][0], ca[i][0], acc[i][j], 0, 0, 0);
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cb[j][1], ca[i][1], acc[i][j], 0, 0, 0);
@@ -198,39 +199,96 @@ __device__ __forceinline__ void product8_tile(const GemmArgs &g, int m0, int n0,
     for (int q = 0; q < NF; ++q) fragment(smem, smem + kSlot, 0, 0, q);
     // Before the last step of a k-tile every fragment of it has been read and this wave's parts of the next one have landed (all but the newest loads); past the
     // barrier that holds for all waves, so that the last step may read k-tile kt + 1 and load B(kt + 2) into the slot of A(kt).
+    // (The bytes are taken in loops of their own around the k-tiles: a branch among the products lets the compiler move them behind it, and a load in one copies what
+    // it loads, which waits for it at once.  Taking them waits for the k-tiles on their way as well, which is why a group is as long as registers allow.)
     int sa = 0;
-    for (int kt = 0; kt < total; ++kt) {
-        const char *stA = smem + sa * kSlot, *stB = smem + ring(sa, 1) * kSlot;
-        const char *stA1 = smem + ring(sa, 2) * kSlot, *stB1 = smem + ring(sa, 3) * kSlot;
-        setup(true, kt + 2, ring(sa, 4));
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (NATIVE) {
-            step(0, stA, stB, 1, true, 0, LA);
-        } else {
-            constexpr int c0 = (LA + 2) / 3, c1 = (LA - c0 + 1) / 2;
-            step(0, stA, stB, 1, true, 0, c0);
-            step(1, stA, stB, 2, true, c0, c1);
-            step(0, stA, stB, 3, true, c0 + c1, LA - c0 - c1);
-        }
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(LA) : "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        setup(false, kt + 2, sa);
-        __builtin_amdgcn_sched_barrier(0);
-        step((kSteps - 1) & 1, stA1, stB1, 0, false, 0, LB);
-        sa = ring(sa, 2);
-        if ((kt & 3) == 3) {
-            take_bytes();
-            if (((kt + 5) & (4 * G - 1)) == 0) load_bytes(kt + 5);
-        } else {
+    for (int group = 0; group < total; group += 4 * G) {
+        wide_t nowA[TM], nowB[TN];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) sA[i] = (int)((unsigned)sA[i] >> 8);
+        for (int i = 0; i < TM; ++i) nowA[i] = nextA[i];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) sB[j] = (int)((unsigned)sB[j] >> 8);
+        for (int j = 0; j < TN; ++j) nowB[j] = nextB[j];
+        load_bytes(group + 4 * G);
+        for (int four = group; four < min(group + 4 * G, total); four += 4) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) sA[i] = shift(nowA[i]);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) sB[j] = shift(nowB[j]);
+            for (int kt = four; kt < min(four + 4, total); ++kt) {
+                const char *stA = smem + sa * kSlot, *stB = smem + ring(sa, 1) * kSlot;
+                const char *stA1 = smem + ring(sa, 2) * kSlot, *stB1 = smem + ring(sa, 3) * kSlot;
+                setup(true, kt + 2, ring(sa, 4));
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (NATIVE) {
+                    step(0, stA, stB, 1, true, 0, LA);
+                } else {
+                    constexpr int c0 = (LA + 2) / 3, c1 = (LA - c0 + 1) / 2;
+                    step(0, stA, stB, 1, true, 0, c0);
+                    step(1, stA, stB, 2, true, c0, c1);
+                    step(0, stA, stB, 3, true, c0 + c1, LA - c0 - c1);
+                }
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(LA) : "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                setup(false, kt + 2, sa);
+                __builtin_amdgcn_sched_barrier(0);
+                step((kSteps - 1) & 1, stA1, stB1, 0, false, 0, LB);
+                sa = ring(sa, 2);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) sA[i] = (int)((unsigned)sA[i] >> 8);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) sB[j] = (int)((unsigned)sB[j] >> 8);
+            }
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may land in LDS any more
     __syncthreads();
+}
+
+// A wave's results, 32 T x 32 T, to memory: a lane holds four neighbours at a time of 32 rows, so they go through LDS (the wave's own 32 T rows of 256 bytes; piece c of
+// row r at slot c ^ r) and leave in whole rows of it.  Straight from the registers 4096 x 4096 results took 8 us more.
+template <bool HALF, int T>
+__device__ __forceinline__ void store_tile(const v16f32 (&acc)[T][T], char *lds, int m0, int n0, int m, int n, const float *bias, void *out, int64_t ldo) {
+    using E = std::conditional_t<HALF, __bf16, float>;
+    constexpr int kRow = HALF ? 64 * T : 256, kPieces = kRow / 16, kPasses = HALF ? 1 : T / 2, kCols = T / kPasses, kEach = 16 / (int)sizeof(E);
+    const int lane = threadIdx.x & 63, lrow = lane & 31, lhalf = lane >> 5;
+#pragma unroll
+    for (int pass = 0; pass < kPasses; ++pass) {
+#pragma unroll
+        for (int jj = 0; jj < kCols; ++jj)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int j = pass * kCols + jj, col = n0 + 32 * j + 8 * q + 4 * lhalf;
+                float b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (bias && col < n) load_upto<float, 4>(bias + col, b, n - col);
+                const int piece = HALF ? 4 * jj + q : 8 * jj + 2 * q + lhalf;
+#pragma unroll
+                for (int i = 0; i < T; ++i) {
+                    const int row = 32 * i + lrow;
+                    piece_t<E, 4> v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[r] = (E)(acc[i][j][q * 4 + r] + b[r]);
+                    typedef E aligned_t __attribute__((ext_vector_type(4)));
+                    *reinterpret_cast<aligned_t *>(lds + row * kRow + ((piece ^ row) & (kPieces - 1)) * 16 + (HALF ? lhalf * 8 : 0)) = v;
+                }
+            }
+        const int piece = lane & (kPieces - 1), col = n0 + pass * 32 * kCols + piece * kEach;
+#pragma unroll 4
+        for (int r = 0; r < 32 * T * kPieces / 64; ++r) {
+            const int row = r * (64 / kPieces) + lane / kPieces;
+            typedef E aligned_t __attribute__((ext_vector_type(kEach)));
+            const aligned_t v = *reinterpret_cast<const aligned_t *>(lds + row * kRow + ((piece ^ row) & (kPieces - 1)) * 16);
+            if (m0 + row >= m || col >= n) continue;
+            E *to = (E *)out + (int64_t)(m0 + row) * ldo + col;
+            if (n - col >= kEach) {
+                *reinterpret_cast<piece_t<E, kEach> *>(to) = v;
+            } else {
+#pragma unroll
+                for (int k = 0; k < kEach; ++k)
+                    if (k < n - col) to[k] = v[k];
+            }
+        }
+    }
 }
 
 template <bool NATIVE, int FA, int FB, int T>
@@ -240,30 +298,12 @@ __global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void block8_tile_g
     int tm, tn;
     tile_at((int)blockIdx.x - part * tiles, g.mtiles, g.ntiles, tm, tn);
     v16f32 acc[T][T];
-    product8_tile<NATIVE, FA, FB, T, T, T == 4 ? 2 : 1>(g, tm * 64 * T, tn * 64 * T, part * g.per, min((part + 1) * g.per, g.kt), smem, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lrow = lane & 31, lhalf = lane >> 5;
-    const int m0 = tm * 64 * T + (wave >> 1) * 32 * T + lrow, n0 = tn * 64 * T + (wave & 1) * 32 * T + lhalf * 4;
-    float *sums = g.parts > 1 ? (float *)g.out + (int64_t)part * g.m * g.n : nullptr;
-#pragma unroll
-    for (int j = 0; j < T; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int n = n0 + 32 * j + 8 * q;
-            if (n >= g.n) continue;
-            float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (g.bias && !sums) load_upto<float, 4>(g.bias + n, bias, g.n - n);
-#pragma unroll
-            for (int i = 0; i < T; ++i) {
-                const int m = m0 + 32 * i;
-                if (m >= g.m) continue;
-                float f[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) f[r] = acc[i][j][q * 4 + r] + bias[r];
-                if (sums) store_upto<float, 4>(sums + (int64_t)m * g.n + n, f, g.n - n);
-                else if (NATIVE) store_upto<__bf16, 4>((__bf16 *)g.out + m * g.ldo + n, f, g.n - n);
-                else store_upto<float, 4>((float *)g.out + m * g.ldo + n, f, g.n - n);
-            }
-        }
+    product8_tile<NATIVE, FA, FB, T, T, T == 4 ? 4 : 1>(g, tm * 64 * T, tn * 64 * T, part * g.per, min((part + 1) * g.per, g.kt), smem, acc);
+    const int wave = threadIdx.x >> 6;
+    const int m0 = tm * 64 * T + (wave >> 1) * 32 * T, n0 = tn * 64 * T + (wave & 1) * 32 * T;
+    char *own = smem + wave * 32 * T * 256;
+    if (g.parts > 1) store_tile<false, T>(acc, own, m0, n0, g.m, g.n, nullptr, (float *)g.out + (int64_t)part * g.m * g.n, g.n);
+    else store_tile<NATIVE, T>(acc, own, m0, n0, g.m, g.n, g.bias, g.out, g.ldo);
 }
 
 // The sum of the parts in their order, four columns to a thread.
@@ -319,13 +359,13 @@ __global__ __launch_bounds__(256) void block8_gemm_kernel(const GemmArgs g) {
     }
 }
 
-// How a product is cut: tiles of 64 T, the contraction in parts of `per` blocks (multiples of 8 blocks for large tiles, of 4 for small ones).
+// How a product is cut: tiles of 64 T, the contraction in parts of `per` blocks (multiples of 16 blocks for large tiles, of 4 for small ones).
 struct Cut {
     int tile, parts, per;
 };
 static Cut cut_of(int64_t m, int64_t n, int64_t kt) {
     const int64_t large = ((m + 255) / 256) * ((n + 255) / 256), small = ((m + 127) / 128) * ((n + 127) / 128);
-    if (large >= 160) return {4, 1, (int)((kt + 7) / 8 * 8)};
+    if (large >= 160) return {4, 1, (int)((kt + 15) / 16 * 16)};
     if (small * 4 < 64) return {1, 1, (int)kt};
     int64_t parts = std::max<int64_t>(1, std::min<int64_t>(512 / small, kt / 8));
     const int64_t per = ((kt + parts - 1) / parts + 3) / 4 * 4;
@@ -363,8 +403,8 @@ extern "C" int imunpack_block8_gemm_workspace(int64_t m, int64_t n, int64_t k, i
 }
 
 extern "C" int imunpack_block8_gemm(const void *a, int64_t lda, const void *a_scales, int64_t ldsa, int a_format, const void *b, int64_t ldb, const void *b_scales, int64_t ldsb,
-                                    int b_format, int64_t m, int64_t n, int64_t k, const float *bias, void *out, int64_t ldo, int dtype, void *workspace, size_t workspace_bytes,
-                                    imunpack_stream_t stream) {
+                            int b_format, int64_t m, int64_t n, int64_t k, const float *bias, void *out, int64_t ldo, int dtype, void *workspace, size_t workspace_bytes,
+                            imunpack_stream_t stream) {
     size_t need = 0;
     IMU_TRY(imunpack_block8_gemm_workspace(m, n, k, dtype, &need));
     if (m == 0 || n == 0) return IMUNPACK_OK;
@@ -375,7 +415,7 @@ extern "C" int imunpack_block8_gemm(const void *a, int64_t lda, const void *a_sc
     const int kt = (int)((k + kBlock8 - 1) / kBlock8);
     const Cut c = cut_of(m, n, kt);
     const hipStream_t st = (hipStream_t)stream;
-    GemmArgs g = {A.codes, A.scales, B.codes, B.scales, bias, c.parts > 1 ? workspace : out, lda, ldsa, ldb, ldsb, ldo, (int)m, (int)n, kt, 0, 0, c.parts, c.per, dtype == IMUNPACK_BF16};
+    GemmArgs g = {A.codes, A.scales, B.codes, B.scales, bias, c.parts > 1 ? workspace : out, lda, ldsa, ldb, ldsb, ldo, (int)m, (int)n, kt, 0, 0, c.parts, c.per};
     g.mtiles = (int)((m + 64 * c.tile - 1) / (64 * c.tile));
     g.ntiles = (int)((n + 64 * c.tile - 1) / (64 * c.tile));
     if ((int64_t)g.mtiles * g.ntiles * c.parts > (1 << 23)) return IMUNPACK_EINVAL;
