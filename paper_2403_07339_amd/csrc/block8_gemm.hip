@@ -250,7 +250,7 @@ __device__ __forceinline__ void product8_tile(const GemmArgs &g, int m0, int n0,
 template <bool HALF, int T>
 __device__ __forceinline__ void store_tile(const v16f32 (&acc)[T][T], char *lds, int m0, int n0, int m, int n, const float *bias, void *out, int64_t ldo) {
     using E = std::conditional_t<HALF, __bf16, float>;
-    constexpr int kRow = HALF ? 64 * T : 256, kPieces = kRow / 16, kPasses = HALF ? 1 : T / 2, kCols = T / kPasses, kEach = 16 / (int)sizeof(E);
+    constexpr int kWide = 32 * T * (int)sizeof(E), kRow = kWide < 256 ? kWide : 256, kPieces = kRow / 16, kPasses = kWide / kRow, kCols = T / kPasses, kEach = 16 / (int)sizeof(E);
     const int lane = threadIdx.x & 63, lrow = lane & 31, lhalf = lane >> 5;
 #pragma unroll
     for (int pass = 0; pass < kPasses; ++pass) {
@@ -292,7 +292,7 @@ __device__ __forceinline__ void store_tile(const v16f32 (&acc)[T][T], char *lds,
 }
 
 template <bool NATIVE, int FA, int FB, int T>
-__global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : 2) void block8_tile_gemm_kernel(const GemmArgs g) {
+__global__ __launch_bounds__(kProductThreads, T == 4 ? 1 : T == 2 ? 2 : 4) void block8_tile_gemm_kernel(const GemmArgs g) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tiles = g.mtiles * g.ntiles, part = (int)blockIdx.x / tiles;
     int tm, tn;
@@ -328,49 +328,100 @@ __global__ __launch_bounds__(256) void block8_fold_kernel(const float *__restric
     store_upto<T, 4>(out + row * ldo + col, f, n - col);
 }
 
-// 64 x 64 results to a workgroup, 32 x 32 to a wave, operands straight from memory.
-template <int FA, int FB, class T>
-__global__ __launch_bounds__(256) void block8_gemm_kernel(const GemmArgs g) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 31, half = lane >> 5;
-    const int m = ((int)blockIdx.x % g.mtiles) * 64 + (wave >> 1) * 32 + row, n0 = ((int)blockIdx.x / g.mtiles) * 64 + (wave & 1) * 32;
-    const int ma = min(m, g.m - 1), nb = min(n0 + row, g.n - 1);
-    const uint8_t *a = g.a + ma * g.lda + half * 64, *b = g.b + nb * g.ldb + half * 64;
-    v16f32 acc;
+// ---- up to sixteen rows: the contraction is dealt to a workgroup's waves -----------------------------------------------------------------
+// What counts is that B is read once, at once: a wave takes every eighth block of 16 rows of B straight into registers (four lanes to a row, a quarter of its
+// block's first half and of its second to each, so that a load takes 64 bytes of every row), four blocks ahead of the products, with the blocks of A's rows, which the
+// caches hold.  The waves' sums meet in LDS.  16 x 4096 by 4096: 7.6 us a call, of which the kernel's reading takes 2.7 (6 TB/s).  32 rows of B to a workgroup
+// were slower (10.2), a second set of registers under way as well (16 x 4096 by 11008: 18.0, 19.5).
+constexpr int kFewRows = 16, kFewWaves = 8, kFewAhead = 4;
+template <bool NATIVE, int FA, int FB>
+__global__ __launch_bounds__(64 * kFewWaves) void block8_few_kernel(const GemmArgs g) {
+    typedef float v4f32 __attribute__((ext_vector_type(4)));
+    __shared__ __attribute__((aligned(16))) float sums[kFewWaves][64][4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, quarter = lane >> 4;
+    const int n0 = (int)blockIdx.x * 16, ma = min(row, g.m - 1), nb = min(n0 + row, g.n - 1);
+    const uint8_t *a = g.a + ma * g.lda + quarter * 16, *sa = g.sa + ma * g.ldsa, *b = g.b + nb * g.ldb + quarter * 16, *sb = g.sb + nb * g.ldsb;
+    v4f32 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int first = wave; first < g.kt; first += kFewWaves * kFewAhead) {
+        v4i32 xa[kFewAhead][2], xb[kFewAhead][2];
+        int ea[kFewAhead], eb[kFewAhead];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
-    for (int kt = 0; kt < g.kt; ++kt) {
-        const float sa = block8_scale(g.sa[ma * g.ldsa + kt]), sb = block8_scale(g.sb[nb * g.ldsb + kt]);
+        for (int u = 0; u < kFewAhead; ++u) {
+            const int kb = min(first + u * kFewWaves, g.kt - 1);
+            xb[u][0] = *reinterpret_cast<const v4i32 *>(b + kb * 128), xb[u][1] = *reinterpret_cast<const v4i32 *>(b + kb * 128 + 64);
+            xa[u][0] = *reinterpret_cast<const v4i32 *>(a + kb * 128), xa[u][1] = *reinterpret_cast<const v4i32 *>(a + kb * 128 + 64);
+            eb[u] = sb[kb], ea[u] = sa[kb];
+        }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint4 wa = *reinterpret_cast<const uint4 *>(a + kt * 128 + q * 16), wb = *reinterpret_cast<const uint4 *>(b + kt * 128 + q * 16);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen<FB>(wb.x, wb.y, sb), widen<FA>(wa.x, wa.y, sa), acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen<FB>(wb.z, wb.w, sb), widen<FA>(wa.z, wa.w, sa), acc, 0, 0, 0);
+        for (int u = 0; u < kFewAhead; ++u) {
+            if (first + u * kFewWaves >= g.kt) break;
+            const v4i32 a0 = xa[u][0], a1 = xa[u][1], b0 = xb[u][0], b1 = xb[u][1];
+            if constexpr (NATIVE) {
+                acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v8i32{b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]},
+                                                                       v8i32{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]}, acc, FB, FA, 0, eb[u], 0, ea[u]);
+            } else {
+                const float pb = __int_as_float(eb[u] << 23), pa = __int_as_float(ea[u] << 23);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FB>(b0[0], b0[1], pb), widen<FA>(a0[0], a0[1], pa), acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FB>(b0[2], b0[3], pb), widen<FA>(a0[2], a0[3], pa), acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FB>(b1[0], b1[1], pb), widen<FA>(a1[0], a1[1], pa), acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FB>(b1[2], b1[3], pb), widen<FA>(a1[2], a1[3], pa), acc, 0, 0, 0);
+            }
         }
     }
-    // the lane's row of A with the columns 8 (r / 4) + 4 half + r % 4 of the wave's 32
-    if (m >= g.m) return;
+    *reinterpret_cast<v4f32 *>(sums[wave][lane]) = acc;
+    __syncthreads();
+    // lane l holds row l % 16 of A with the columns 4 (l / 16) .. + 3; the waves' sums in their order
+    if (threadIdx.x >= 64) return;
+    const int n = n0 + 4 * quarter;
+    if (row >= g.m || n >= g.n) return;
+    float f[4], bias[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int n = n0 + q * 8 + half * 4;
-        float f[4];
+    for (int k = 0; k < 4; ++k) f[k] = sums[0][lane][k];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) f[r] = acc[q * 4 + r] + (g.bias && n + r < g.n ? g.bias[n + r] : 0.0f);
-        if (n < g.n) store_upto<T, 4>((T *)g.out + m * g.ldo + n, f, g.n - n);
+    for (int w = 1; w < kFewWaves; ++w)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[k] += sums[w][lane][k];
+    if (g.bias) {
+        load_upto<float, 4>(g.bias + n, bias, g.n - n);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[k] += bias[k];
     }
+    if (NATIVE) store_upto<__bf16, 4>((__bf16 *)g.out + row * g.ldo + n, f, g.n - n);
+    else store_upto<float, 4>((float *)g.out + row * g.ldo + n, f, g.n - n);
 }
 
-// How a product is cut: tiles of 64 T, the contraction in parts of `per` blocks (multiples of 16 blocks for large tiles, of 4 for small ones).
+// How a product is cut: tiles of 64 T (T = 0: the kernel for few rows), the contraction in parts of `per` blocks, multiples of what a tile's bytes are taken in.
 struct Cut {
     int tile, parts, per;
 };
-static Cut cut_of(int64_t m, int64_t n, int64_t kt) {
-    const int64_t large = ((m + 255) / 256) * ((n + 255) / 256), small = ((m + 127) / 128) * ((n + 127) / 128);
-    if (large >= 160) return {4, 1, (int)((kt + 15) / 16 * 16)};
-    if (small * 4 < 64) return {1, 1, (int)kt};
-    int64_t parts = std::max<int64_t>(1, std::min<int64_t>(512 / small, kt / 8));
-    const int64_t per = ((kt + parts - 1) / parts + 3) / 4 * 4;
-    parts = (kt + per - 1) / per;
-    return {2, (int)parts, (int)per};
+// The cut that should take the least time, in nanoseconds, from what the kernels were seen to take: a workgroup costs `fixed` and `each` for every block, a CU works on one after
+// the other (or on several at once, no faster in all); with no more workgroups than CUs small tiles wait for their loads (`alone`; longer still with one row of tiles, where nobody else has
+// fetched B).  Parts cost a launch and their sums' way to memory and back.  Microseconds, bfloat16 / fp32 results, by tiles of 64, 128 and 256:
+//   1024^3 5.8, 7.4, 17.3 / 7.2, 12.1, 30.2;  2048^3 17.9, 12.6, 26.9 / 23.9, 22.6, 49.2;  256 x 4096 by 4096 12.7, 18.3, 39.4 / 18.4, 32.4, -;
+//   12608 x 768 by 768 20.2, 16.4, 18.7 / 25.2, 24.3, 31.2;  4096^3 -, -, 54 / -, -, 110;  768 x 12608 by 768 in 4 parts of 64 24.3 / 26.9, in 7 of 128 22.3 / 27.3, in 2 of 128 36 / 54;
+//   64 x 4096 by 4096 in 1, 2 and 4 parts of 64 12.1, 11.1, 10.4 / 16.9, 13.2, 11.4;  16 x 4096 by 11008 with few rows' kernel 18, in 1, 2 and 4 parts of 64 17.4, 14.0, 13.1
+static Cut cut_of(int64_t m, int64_t n, int64_t kt, bool native) {
+    struct Cost {
+        int tile, whole, fixed, alone, first, each;
+    };
+    static const Cost costs[2][3] = {{{1, 4, 200, 420, 420, 310}, {2, 4, 500, 1020, 1020, 1020}, {4, 16, 10000, 2750, 2750, 2750}},
+                                     {{1, 4, 200, 240, 370, 210}, {2, 4, 500, 550, 550, 550}, {4, 16, 8000, 1300, 1300, 1300}}};
+    Cut best = {0, 1, (int)kt};
+    double least = m <= kFewRows ? (double)((n + 4095) / 4096) * (300.0 + 115.0 * (double)kt) : 1e30;
+    for (const Cost &c : costs[native]) {
+        const int64_t edge = 64 * c.tile, down = (m + edge - 1) / edge, tiles = down * ((n + edge - 1) / edge);
+        for (int64_t p = 1, last = 0; p <= 64 && (p == 1 || p * c.whole <= kt); ++p) {
+            const int64_t per = ((kt + p - 1) / p + c.whole - 1) / c.whole * c.whole, parts = (kt + per - 1) / per, groups = tiles * parts;
+            if (parts == last) continue;
+            last = parts;
+            const int64_t block = groups > 256 ? c.each : down > 1 ? c.alone : c.first;
+            const double walk = (double)((groups + 255) / 256) * (double)(c.fixed + std::min(per, kt) * block);
+            const double time = walk + (parts > 1 ? 3500.0 + (double)parts * (double)m * (double)n * 8.0 / 6000.0 : 0.0);
+            if (time < least) best = {c.tile, (int)parts, (int)per}, least = time;
+            if (groups > 2048) break;
+        }
+    }
+    return best;
 }
 
 template <bool NATIVE, int FA, int FB, int T>
@@ -397,7 +448,7 @@ constexpr int64_t kGemmRows = 1 << 24;
 
 extern "C" int imunpack_block8_gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, size_t *bytes) {
     if (m < 0 || n < 0 || k < 1 || m > kGemmRows || n > kGemmRows || k > kBlock8Cols || (dtype != IMUNPACK_F32 && dtype != IMUNPACK_BF16) || !bytes) return IMUNPACK_EINVAL;
-    const Cut c = cut_of(m, n, (k + kBlock8 - 1) / kBlock8);
+    const Cut c = cut_of(m, n, (k + kBlock8 - 1) / kBlock8, dtype == IMUNPACK_BF16);
     *bytes = c.parts > 1 ? (size_t)c.parts * (size_t)m * (size_t)n * sizeof(float) : 0;
     return IMUNPACK_OK;
 }
@@ -413,27 +464,28 @@ extern "C" int imunpack_block8_gemm(const void *a, int64_t lda, const void *a_sc
     if (need && (!workspace || ((uintptr_t)workspace & 15))) return IMUNPACK_EINVAL;
     if (workspace_bytes < need) return IMUNPACK_ESMALL;
     const int kt = (int)((k + kBlock8 - 1) / kBlock8);
-    const Cut c = cut_of(m, n, kt);
+    const Cut c = cut_of(m, n, kt, dtype == IMUNPACK_BF16);
     const hipStream_t st = (hipStream_t)stream;
     GemmArgs g = {A.codes, A.scales, B.codes, B.scales, bias, c.parts > 1 ? workspace : out, lda, ldsa, ldb, ldsb, ldo, (int)m, (int)n, kt, 0, 0, c.parts, c.per};
-    g.mtiles = (int)((m + 64 * c.tile - 1) / (64 * c.tile));
-    g.ntiles = (int)((n + 64 * c.tile - 1) / (64 * c.tile));
-    if ((int64_t)g.mtiles * g.ntiles * c.parts > (1 << 23)) return IMUNPACK_EINVAL;
+    const int64_t tall = c.tile ? 64 * c.tile : kFewRows, wide = c.tile ? 64 * c.tile : 16;
+    g.mtiles = (int)((m + tall - 1) / tall);
+    g.ntiles = (int)((n + wide - 1) / wide);
+    if ((int64_t)g.mtiles * g.ntiles * g.parts > (1 << 23)) return IMUNPACK_EINVAL;
     const bool native = dtype == IMUNPACK_BF16;
     auto launch = [&](auto fa, auto fb) {
         constexpr int FA = decltype(fa)::value, FB = decltype(fb)::value;
         if (c.tile == 4) return native ? launch_tiles<true, FA, FB, 4>(g, st) : launch_tiles<false, FA, FB, 4>(g, st);
         if (c.tile == 2) return native ? launch_tiles<true, FA, FB, 2>(g, st) : launch_tiles<false, FA, FB, 2>(g, st);
-        const dim3 grid((unsigned)(g.mtiles * g.ntiles));
-        if (native) hipLaunchKernelGGL((block8_gemm_kernel<FA, FB, __bf16>), grid, dim3(256), 0, st, g);
-        else hipLaunchKernelGGL((block8_gemm_kernel<FA, FB, float>), grid, dim3(256), 0, st, g);
+        if (c.tile == 1) return native ? launch_tiles<true, FA, FB, 1>(g, st) : launch_tiles<false, FA, FB, 1>(g, st);
+        if (native) hipLaunchKernelGGL((block8_few_kernel<true, FA, FB>), dim3((unsigned)g.ntiles), dim3(64 * kFewWaves), 0, st, g);
+        else hipLaunchKernelGGL((block8_few_kernel<false, FA, FB>), dim3((unsigned)g.ntiles), dim3(64 * kFewWaves), 0, st, g);
         return launch_status();
     };
     using E4 = std::integral_constant<int, IMUNPACK_E4M3>;
     using E5 = std::integral_constant<int, IMUNPACK_E5M2>;
     if (a_format == IMUNPACK_E4M3) IMU_TRY(b_format == IMUNPACK_E4M3 ? launch(E4(), E4()) : launch(E4(), E5()));
     else IMU_TRY(b_format == IMUNPACK_E4M3 ? launch(E5(), E4()) : launch(E5(), E5()));
-    if (c.parts == 1) return IMUNPACK_OK;
+    if (g.parts == 1) return IMUNPACK_OK;
     const int64_t threads = m * ((n + 3) / 4);
     const dim3 grid((unsigned)((threads + 255) / 256));
     if (native) hipLaunchKernelGGL(block8_fold_kernel<__bf16>, grid, dim3(256), 0, st, (const float *)workspace, bias, (__bf16 *)out, ldo, c.parts, (int)m, (int)n);
