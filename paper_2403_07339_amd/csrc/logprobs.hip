@@ -3,7 +3,12 @@
 //   m = max l,  S = sum exp(l - m),  A = sum exp(l - m) (l - m)       lse = m + log S,   entropy = log S - A / S
 //   gl_v = sum_j g_j ([v = t_j] - p_v) - g_H p_v (l_v - lse + H)
 //
-// One pass over the row with the running maximum; where it moves by d <= 0, S -> S e^d, A -> e^d (A + d S).
+// Forward: one pass over the row with the running maximum of a thread; where it moves by d <= 0, S -> S e^d, A -> e^d (A + d S).  Exponents are kept in
+// units of log 2.  Few rows are cut into parts, a workgroup to each, which a second launch joins.
+// The largest `top`: a wave keeps its best 64 in order, one to a lane, as a number that grows with the logit and falls with the place.  A chunk of the row whose
+// maximum does not beat the last of them is passed over (which is nearly every chunk after the first ones); what beats it is gathered in LDS and, 64 at a time, sorted
+// and merged with the list.  The first chunk would be gathered whole: there the top-th largest of the lanes' maxima, found bit by bit, is a bound that no more than `top` lanes' worth of
+// elements reach, but for ties.
 #include "common.h"
 #include "elements.h"
 
@@ -11,106 +16,237 @@
 
 namespace imu {
 constexpr int64_t kLogprobRows = 1 << 22;  // of a launch
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+constexpr int kScanPieces = 4;             // pieces of 16 bytes that a thread loads at a time
+constexpr int kMostParts = 64;
 
 struct LogprobArgs {
     const void *l;
     const int64_t *tokens;
     float *logp, *lse, *stats, *entropy, *top_logp;
     int64_t *top_index;
+    float *part_stats;        // several parts: three numbers and `top` keys of each
+    uint64_t *part_keys;
     int64_t ldl, ignore;
-    int vocab, count, top;
+    int vocab, count, top, parts, per;
 };
 
-// Maximum, S and A of a part of a row.
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Maximum m, S and A / log 2 of a part of a row.
 struct Moments {
     float m = -__builtin_inff(), s = 0.0f, a = 0.0f;
-    __device__ __forceinline__ void add(float x) {
-        if (x == -__builtin_inff()) return;
-        if (x > m) rebase(x);
-        const float d = x - m, e = expf(d);
-        s += e;
-        if (e > 0.0f) a += e * d;  // (d may be -infinity: a logit of the type's lowest value)
-    }
-    __device__ __forceinline__ void rebase(float to) {
-        const float d = m - to, e = expf(d);
+    __device__ __forceinline__ void rebase(float to) {  // to >= m
+        const float d = m == to ? 0.0f : (m - to) * kLog2e, e = exp2_of(d);  // (m == to: both may be infinite)
         a = e > 0.0f ? e * fmaf(d, s, a) : 0.0f;
-        s = e * s;
+        s *= e;
         m = to;
+    }
+    __device__ __forceinline__ void add(float x) {      // x <= m, m > -infinity
+        const float t = (x - m) * kLog2e, e = exp2_of(t);
+        s += e;
+        a = fmaf(e, fmaxf(t, -1e4f), a);                // (e is 0 there; t may be -infinity)
     }
     __device__ __forceinline__ void join(Moments o) {
         const float to = fmaxf(m, o.m);
-        if (to == -__builtin_inff()) {  // (nothing, or NaN in s)
-            s += o.s;
-            a += o.a;
-            return;
-        }
-        if (m < to) m == -__builtin_inff() ? (void)(m = to) : rebase(to);
-        if (o.m < to) o.m == -__builtin_inff() ? (void)(o.m = to) : o.rebase(to);
+        rebase(to);
+        o.rebase(to);
         s += o.s;
         a += o.a;
     }
 };
-// The order of a logit among a row's: larger first, then the lower place.  NaN stands with -infinity.
-__device__ __forceinline__ uint64_t order_of(float x, int place) {
-    const uint32_t b = x == x ? __float_as_uint(x + 0.0f) : 0xff800000u;
-    return ((uint64_t)(b >> 31 ? ~b : b | 0x80000000u) << 32) | (uint32_t)~place;
-}
-
-template <class T>
-__global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
-    __shared__ float part[4][3];
-    __shared__ uint64_t best[4];
-    const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const T *l = (const T *)a.l + row * a.ldl;
-    Moments mine;
-    for (int v = threadIdx.x; v < a.vocab; v += 256) mine.add((float)l[v]);
+__device__ __forceinline__ Moments wave_join(Moments v) {
 #pragma unroll
     for (int k = 32; k; k >>= 1) {
         Moments o;
-        o.m = __shfl_xor(mine.m, k), o.s = __shfl_xor(mine.s, k), o.a = __shfl_xor(mine.a, k);
-        mine.join(o);
+        o.m = __shfl_xor(v.m, k), o.s = __shfl_xor(v.s, k), o.a = __shfl_xor(v.a, k);
+        v.join(o);
     }
+    return v;
+}
+
+// The order of a logit among a row's: larger first, then the lower place.  NaN stands with -infinity.  0 is below all.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t b = x == x ? __float_as_uint(x + 0.0f) : 0xff800000u;
+    return b >> 31 ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float logit_of(uint64_t key) {
+    const uint32_t b = (uint32_t)(key >> 32);
+    return __uint_as_float(b >> 31 ? b & 0x7fffffffu : ~b);
+}
+__device__ __forceinline__ uint64_t key_of(float x, int place) { return ((uint64_t)order_of(x) << 32) | (uint32_t)~place; }
+__device__ __forceinline__ uint64_t other_lane(uint64_t k, int mask) { return (uint64_t)__shfl_xor((unsigned long long)k, mask); }
+
+// A wave's best 64, largest in lane 0.
+struct Best {
+    uint64_t key = 0;
+    __device__ __forceinline__ static uint64_t step(uint64_t k, int lane, int mask, bool down) {
+        const uint64_t o = other_lane(k, mask);
+        return (((lane & mask) == 0) == down) == (k > o) ? k : o;
+    }
+    // the keys of the lanes in order, largest first
+    __device__ __forceinline__ static uint64_t sorted(uint64_t k, int lane) {
+#pragma unroll
+        for (int size = 2; size <= 64; size *= 2)
+#pragma unroll
+            for (int mask = size / 2; mask; mask /= 2) k = step(k, lane, mask, (lane & size) == 0);
+        return k;
+    }
+    __device__ __forceinline__ void merge(uint64_t other, int lane) {  // other in order too
+        const uint64_t o = other_lane(other, 63);
+        key = key > o ? key : o;
+#pragma unroll
+        for (int mask = 32; mask; mask /= 2) key = step(key, lane, mask, true);
+    }
+};
+
+// What a row's outputs are made of, by one workgroup (or wave): threads `at` of `of`.
+__device__ __forceinline__ void logprob_outputs(const LogprobArgs &a, int64_t row, const void *l, bool bf16, const Moments &all, int at, int of, uint64_t key, bool lists) {
+    const bool none = all.m == -__builtin_inff() && all.s == 0.0f;
+    // (log p = (l - m) - log S: m may be so large that log S is lost beside it)
+    const float logs = none ? 0.0f : logf(all.s);
+    auto logp = [&](float x) { return none ? all.m : (x - all.m) - logs; };
+    if (at == 0) {
+        if (a.lse) a.lse[row] = all.m + logs;
+        if (a.stats) a.stats[2 * row] = all.m, a.stats[2 * row + 1] = logs;
+        if (a.entropy) a.entropy[row] = none ? 0.0f : logs - kLn2 * (all.a / all.s);
+    }
+    for (int j = at; j < a.count; j += of) {
+        const int64_t t = a.tokens[row * a.count + j];
+        float v = 0.0f;
+        if (t != a.ignore) v = t < 0 || t >= a.vocab ? __builtin_nanf("") : logp(bf16 ? (float)((const __bf16 *)l)[t] : ((const float *)l)[t]);
+        a.logp[row * a.count + j] = v;
+    }
+    if (lists && at < a.top) {
+        a.top_index[row * a.top + at] = (int)~(uint32_t)key;
+        a.top_logp[row * a.top + at] = logp(logit_of(key));
+    }
+}
+
+template <class T, bool TOP, bool ONCE>
+__global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
+    constexpr int V = kVec<T>, E = V * kScanPieces, kChunk = 256 * E;
+    __shared__ float part[4][3];
+    __shared__ uint64_t gathered[4][TOP ? 128 : 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row = (int64_t)blockIdx.x / a.parts;
+    const int which = (int)((int64_t)blockIdx.x - row * a.parts), from = which * a.per, to = min(a.vocab, from + a.per);
+    const T *l = (const T *)a.l + row * a.ldl;
+    Moments mine;
+    Best best;
+    float last = -__builtin_inff();  // the top-th logit so far
+    bool full = false;               // ... if there are so many
+    int held = 0;                    // in `gathered`
+    auto flush = [&](int n) __attribute__((always_inline)) {
+        best.merge(Best::sorted(lane < n ? gathered[wave][lane] : 0, lane), lane);
+        const uint64_t k = (uint64_t)__shfl((unsigned long long)best.key, a.top - 1);
+        full = k != 0;
+        last = full ? logit_of(k) : -__builtin_inff();
+    };
+    for (int base = from; base < to; base += kChunk) {
+        piece_t<T, V> in[kScanPieces];
+#pragma unroll
+        for (int u = 0; u < kScanPieces; ++u) {
+            const int at = base + (u * 256 + (int)threadIdx.x) * V;
+            in[u] = load_piece<T, V, ONCE>(l + at, to - at);
+        }
+        float x[E];
+#pragma unroll
+        for (int u = 0; u < kScanPieces; ++u) {
+            const int have = to - (base + (u * 256 + (int)threadIdx.x) * V);
+#pragma unroll
+            for (int k = 0; k < V; ++k) x[u * V + k] = k < have ? (float)in[u][k] : -__builtin_inff();
+        }
+        float high = x[0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) high = fmaxf(high, x[e]);  // (NaN is passed over, unless all are)
+        if (high > mine.m) mine.rebase(high);
+        if (mine.m > -__builtin_inff()) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) mine.add(x[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) mine.s += x[e] == x[e] ? 0.0f : x[e];
+        }
+        if constexpr (TOP) {
+            if (__ballot(!full || high > last)) {
+                const int first = base + (int)threadIdx.x * V;
+                uint32_t bound = 0;  // where the list is not full: what the top-th of the lanes' largest has at least
+                if (!full) {
+                    const uint32_t own = first < to ? order_of(high) : 0;
+                    for (int b = 31; b >= 0; --b)
+                        if (__builtin_popcountll(__ballot(own >= (bound | (1u << b)))) >= a.top) bound |= 1u << b;
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int place = first + (e / V) * 256 * V + e % V;
+                    const bool wanted = place < to && (full ? x[e] > last : order_of(x[e]) >= bound);
+                    const uint64_t who = __ballot(wanted);
+                    if (who == 0) continue;
+                    if (wanted) gathered[wave][held + __builtin_popcountll(who & ((1ull << lane) - 1))] = key_of(x[e], place);
+                    held += __builtin_popcountll(who);
+                    if (held < 64) continue;
+                    const uint64_t rest = gathered[wave][64 + lane];
+                    const bool was = full;
+                    const float was_last = last;
+                    flush(64);
+                    full = was, last = was_last;  // (of this chunk everything beyond the bound it began with is wanted: a tie may have a lower place)
+                    held -= 64;
+                    if (lane < held) gathered[wave][lane] = rest;
+                }
+                if (held >= 32 || !full) {
+                    flush(held);
+                    held = 0;
+                } else {
+                    const uint64_t k = (uint64_t)__shfl((unsigned long long)best.key, a.top - 1);
+                    full = k != 0;
+                    last = full ? logit_of(k) : -__builtin_inff();
+                }
+            }
+        }
+    }
+    if constexpr (TOP) flush(held);
+    mine = wave_join(mine);
     if (lane == 0) part[wave][0] = mine.m, part[wave][1] = mine.s, part[wave][2] = mine.a;
+    if constexpr (TOP) gathered[wave][lane] = best.key;
     __syncthreads();
     Moments all;
+#pragma unroll
     for (int w = 0; w < 4; ++w) {
         Moments o;
         o.m = part[w][0], o.s = part[w][1], o.a = part[w][2];
         all.join(o);
     }
-    const bool none = all.m == -__builtin_inff() && all.s == 0.0f;
-    // (log p = (l - m) - log S: m may be so large that log S is lost beside it)
-    const float logs = none ? 0.0f : logf(all.s);
-    auto logp = [&](int64_t v) { return none ? all.m : ((float)l[v] - all.m) - logs; };
-    if (threadIdx.x == 0) {
-        if (a.lse) a.lse[row] = all.m + logs;
-        if (a.stats) a.stats[2 * row] = all.m, a.stats[2 * row + 1] = logs;
-        if (a.entropy) a.entropy[row] = none ? 0.0f : logs - all.a / all.s;
-    }
-    for (int j = threadIdx.x; j < a.count; j += 256) {
-        const int64_t t = a.tokens[row * a.count + j];
-        a.logp[row * a.count + j] = t == a.ignore ? 0.0f : t < 0 || t >= a.vocab ? __builtin_nanf("") : logp(t);
-    }
-    uint64_t last = ~0ull;
-    for (int k = 0; k < a.top; ++k) {
-        uint64_t found = 0;
-        for (int v = threadIdx.x; v < a.vocab; v += 256) {
-            const uint64_t o = order_of((float)l[v], v);
-            if (o < last && o > found) found = o;
-        }
+    if constexpr (TOP) {
+        if (wave == 0)
 #pragma unroll
-        for (int d = 32; d; d >>= 1) found = max(found, (uint64_t)__shfl_xor((unsigned long long)found, d));
-        if (lane == 0) best[wave] = found;
-        __syncthreads();
-        last = max(max(best[0], best[1]), max(best[2], best[3]));
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            const int v = (int)~(uint32_t)last;
-            a.top_index[row * a.top + k] = v;
-            a.top_logp[row * a.top + k] = logp(v);
-        }
+            for (int w = 1; w < 4; ++w) best.merge(gathered[w][lane], lane);
     }
+    if (a.parts == 1) {
+        logprob_outputs(a, row, l, std::is_same<T, __bf16>::value, all, (int)threadIdx.x, 256, best.key, TOP && wave == 0);
+        return;
+    }
+    if (threadIdx.x == 0) {
+        float *p = a.part_stats + (row * a.parts + which) * 3;
+        p[0] = all.m, p[1] = all.s, p[2] = all.a;
+    }
+    if (TOP && wave == 0 && lane < a.top) a.part_keys[(row * a.parts + which) * a.top + lane] = best.key;
+}
+
+// The parts of a row, a wave to a row.
+template <class T>
+__global__ __launch_bounds__(64) void logprobs_join_kernel(const LogprobArgs a) {
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x;
+    Moments all;
+    if (lane < a.parts) {
+        const float *p = a.part_stats + (row * a.parts + lane) * 3;
+        all.m = p[0], all.s = p[1], all.a = p[2];
+    }
+    all = wave_join(all);
+    Best best;
+    for (int p = 0; p < a.parts && a.top; ++p) best.merge(lane < a.top ? a.part_keys[(row * a.parts + p) * a.top + lane] : 0, lane);
+    logprob_outputs(a, row, (const T *)a.l + row * a.ldl, std::is_same<T, __bf16>::value, all, lane, 64, best.key, true);
 }
 
 struct LogprobBackArgs {
@@ -119,13 +255,15 @@ struct LogprobBackArgs {
     const float *stats, *entropy, *g_logp, *g_entropy, *g_top;
     void *gl;
     int64_t ldl, ldg, ignore;
-    int vocab, count, top;
+    int vocab, count, top, parts, per;
 };
 
-template <class T>
+template <class T, bool ONCE>
 __global__ __launch_bounds__(256) void logprobs_back_kernel(const LogprobBackArgs a) {
+    constexpr int V = kVec<T>, kChunk = 256 * V * kScanPieces;
     __shared__ float part[4];
-    const int64_t row = blockIdx.x;
+    const int64_t row = (int64_t)blockIdx.x / a.parts;
+    const int which = (int)((int64_t)blockIdx.x - row * a.parts), from = which * a.per, to = min(a.vocab, from + a.per);
     const T *l = (const T *)a.l + row * a.ldl;
     T *gl = (T *)a.gl + row * a.ldg;
     const float m = a.stats[2 * row], logs = a.stats[2 * row + 1], gh = a.g_entropy ? a.g_entropy[row] : 0.0f, h = a.g_entropy ? a.entropy[row] : 0.0f;
@@ -144,9 +282,11 @@ __global__ __launch_bounds__(256) void logprobs_back_kernel(const LogprobBackArg
     }
     sum = reduce_threads<256, false>(sum, part);
     const bool none = m == -__builtin_inff() && logs == 0.0f;
+    const float constant = -fmaf(gh, h, sum), slope = -gh;
+    // (p from d as it is, so that NaN goes through; beside it d is kept finite: p is 0 there)
     auto dense = [&](float x) {
-        const float d = (x - m) - logs, p = expf(d);
-        return none || p == 0.0f ? 0.0f : -p * (sum + (a.g_entropy ? gh * (d + h) : 0.0f));
+        const float d = (x - m) - logs;
+        return exp2_of(d * kLog2e) * fmaf(slope, fmaxf(d, -1e4f), constant);
     };
     // the tokens' own logits before anything is overwritten (up to 1088 of them), then the row, then the tokens
     constexpr int kEach = (1024 + IMUNPACK_LOGPROBS_TOP + 255) / 256;
@@ -156,17 +296,32 @@ __global__ __launch_bounds__(256) void logprobs_back_kernel(const LogprobBackArg
         const int j = threadIdx.x + 256 * u;
         float g;
         const int t = j < listed ? token(j, g) : -1;
-        own[u] = t >= 0 ? (float)l[t] : 0.0f;
+        own[u] = t >= from && t < to ? (float)l[t] : 0.0f;
     }
     __syncthreads();
-    for (int v = threadIdx.x; v < a.vocab; v += 256) gl[v] = (T)dense((float)l[v]);
+    for (int base = from; base < to; base += kChunk) {
+        piece_t<T, V> in[kScanPieces];
+#pragma unroll
+        for (int u = 0; u < kScanPieces; ++u) {
+            const int at = base + (u * 256 + (int)threadIdx.x) * V;
+            in[u] = load_piece<T, V, ONCE>(l + at, to - at);
+        }
+#pragma unroll
+        for (int u = 0; u < kScanPieces; ++u) {
+            const int at = base + (u * 256 + (int)threadIdx.x) * V;
+            float f[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) f[k] = none ? 0.0f : dense((float)in[u][k]);
+            if (at < to) store_upto<T, V, ONCE>(gl + at, f, to - at);
+        }
+    }
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
         const int j = threadIdx.x + 256 * u;
         float g;
         const int t = j < listed ? token(j, g) : -1;
-        if (t < 0 || none) continue;
+        if (t < from || t >= to || none) continue;
         bool first = true;
         float add = 0.0f;
         for (int i = 0; i < listed; ++i) {  // all gradients of one token, in the lists' order
@@ -183,13 +338,24 @@ static bool logprob_sizes(int64_t rows, int64_t vocab, int64_t count, int64_t to
     return rows >= 0 && rows < (1ll << 31) && vocab >= 1 && vocab <= (1 << 30) && count >= 0 && count <= 1024 && top >= 0 && top <= IMUNPACK_LOGPROBS_TOP && top <= vocab &&
            (dtype == IMUNPACK_F32 || dtype == IMUNPACK_BF16);
 }
+// How many workgroups share a row, and how much of it each takes (whole chunks).
+struct Parts {
+    int parts, per;
+};
+static Parts parts_of(int64_t rows, int64_t vocab, int dtype) {
+    const int64_t chunk = 256 * kScanPieces * (dtype == IMUNPACK_F32 ? 4 : 8), chunks = (vocab + chunk - 1) / chunk;
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(chunks, kMostParts), 1024 / std::max<int64_t>(rows, 1)));
+    const int64_t each = (chunks + parts - 1) / parts;
+    return {(int)((chunks + each - 1) / each), (int)std::min(each * chunk, vocab)};
+}
 }  // namespace imu
 
 using namespace imu;
 
 extern "C" int imunpack_logprobs_workspace(int64_t rows, int64_t vocab, int64_t count, int64_t top, int dtype, size_t *bytes) {
     if (!logprob_sizes(rows, vocab, count, top, dtype) || !bytes) return IMUNPACK_EINVAL;
-    *bytes = 0;
+    const int64_t parts = parts_of(rows, vocab, dtype).parts;
+    *bytes = parts == 1 ? 0 : (size_t)rows * (size_t)parts * ((size_t)top * sizeof(uint64_t) + 3 * sizeof(float));
     return IMUNPACK_OK;
 }
 
@@ -203,13 +369,23 @@ extern "C" int imunpack_logprobs(const void *logits, int64_t ldl, int64_t rows, 
     if (need && (!workspace || ((uintptr_t)workspace & 15))) return IMUNPACK_EINVAL;
     if (workspace_bytes < need) return IMUNPACK_ESMALL;
     const int64_t size = dtype == IMUNPACK_F32 ? 4 : 2;
-    for (int64_t r = 0; r < rows; r += kLogprobRows) {
-        const LogprobArgs a = {(const char *)logits + r * ldl * size, tokens ? tokens + r * count : nullptr, logp ? logp + r * count : nullptr, lse ? lse + r : nullptr, stats ? stats + 2 * r : nullptr,
-                               entropy ? entropy + r : nullptr, top_logp ? top_logp + r * top : nullptr, top_index ? top_index + r * top : nullptr, ldl, ignore_index,
-                               (int)vocab, (int)count, (int)top};
-        const dim3 grid((unsigned)std::min(kLogprobRows, rows - r));
-        if (dtype == IMUNPACK_F32) hipLaunchKernelGGL(logprobs_kernel<float>, grid, dim3(256), 0, (hipStream_t)stream, a);
-        else hipLaunchKernelGGL(logprobs_kernel<__bf16>, grid, dim3(256), 0, (hipStream_t)stream, a);
+    const Parts p = parts_of(rows, vocab, dtype);
+    const bool once = rows * vocab * size >= kLastLevelCache;
+    const hipStream_t st = (hipStream_t)stream;
+    for (int64_t r = 0; r < rows; r += kLogprobRows) {  // (one launch wherever a row has parts)
+        const LogprobArgs a = {(const char *)logits + r * ldl * size, tokens ? tokens + r * count : nullptr, logp ? logp + r * count : nullptr, lse ? lse + r : nullptr,
+                               stats ? stats + 2 * r : nullptr, entropy ? entropy + r : nullptr, top_logp ? top_logp + r * top : nullptr, top_index ? top_index + r * top : nullptr,
+                               (float *)((uint64_t *)workspace + rows * p.parts * top), (uint64_t *)workspace, ldl, ignore_index, (int)vocab, (int)count, (int)top, p.parts, p.per};
+        const int64_t some = std::min(kLogprobRows, rows - r);
+        const dim3 grid((unsigned)(some * p.parts));
+        auto typed = [&](auto t) {
+            using T = decltype(t);
+            if (top) hipLaunchKernelGGL((once ? logprobs_kernel<T, true, true> : logprobs_kernel<T, true, false>), grid, dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((once ? logprobs_kernel<T, false, true> : logprobs_kernel<T, false, false>), grid, dim3(256), 0, st, a);
+            if (p.parts > 1) hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3((unsigned)some), dim3(64), 0, st, a);
+        };
+        if (dtype == IMUNPACK_F32) typed(0.0f);
+        else typed((__bf16)0.0f);
         IMU_TRY(launch_status());
     }
     return IMUNPACK_OK;
@@ -223,12 +399,14 @@ extern "C" int imunpack_logprobs_backward(const void *logits, int64_t ldl, int64
     if (!logits || !stats || !gl || (g_logp && count && !tokens) || (g_entropy && !entropy) || (g_top && top && !top_index) || (gl == logits && ldg != ldl)) return IMUNPACK_EINVAL;
     const int64_t size = dtype == IMUNPACK_F32 ? 4 : 2;
     auto at = [](auto *p, int64_t k) { return p ? p + k : p; };
+    const Parts p = parts_of(rows, vocab, dtype);
+    const bool once = rows * vocab * size >= kLastLevelCache;
     for (int64_t r = 0; r < rows; r += kLogprobRows) {
         const LogprobBackArgs a = {(const char *)logits + r * ldl * size, at(tokens, r * count), at(top_index, r * top), stats + 2 * r, at(entropy, r), count ? at(g_logp, r * count) : nullptr,
-                                   at(g_entropy, r), top ? at(g_top, r * top) : nullptr, (char *)gl + r * ldg * size, ldl, ldg, ignore_index, (int)vocab, (int)count, (int)top};
-        const dim3 grid((unsigned)std::min(kLogprobRows, rows - r));
-        if (dtype == IMUNPACK_F32) hipLaunchKernelGGL(logprobs_back_kernel<float>, grid, dim3(256), 0, (hipStream_t)stream, a);
-        else hipLaunchKernelGGL(logprobs_back_kernel<__bf16>, grid, dim3(256), 0, (hipStream_t)stream, a);
+                                   at(g_entropy, r), top ? at(g_top, r * top) : nullptr, (char *)gl + r * ldg * size, ldl, ldg, ignore_index, (int)vocab, (int)count, (int)top, p.parts, p.per};
+        const dim3 grid((unsigned)(std::min(kLogprobRows, rows - r) * p.parts));
+        if (dtype == IMUNPACK_F32) hipLaunchKernelGGL((once ? logprobs_back_kernel<float, true> : logprobs_back_kernel<float, false>), grid, dim3(256), 0, (hipStream_t)stream, a);
+        else hipLaunchKernelGGL((once ? logprobs_back_kernel<__bf16, true> : logprobs_back_kernel<__bf16, false>), grid, dim3(256), 0, (hipStream_t)stream, a);
         IMU_TRY(launch_status());
     }
     return IMUNPACK_OK;
