@@ -75,28 +75,57 @@ __device__ __forceinline__ float logit_of(uint64_t key) {
     return __uint_as_float(b >> 31 ? b & 0x7fffffffu : ~b);
 }
 __device__ __forceinline__ uint64_t key_of(float x, int place) { return ((uint64_t)order_of(x) << 32) | (uint32_t)~place; }
-__device__ __forceinline__ uint64_t other_lane(uint64_t k, int mask) { return (uint64_t)__shfl_xor((unsigned long long)k, mask); }
+// The value of the lane whose number differs by MASK, on the vector ALU's lane moves: within a row of 16 lanes permutations of four, a rotation by half, mirrors (7 - i and then 3 - i is
+// i ^ 4); across rows and halves the swap of registers, of which each side keeps what it has not.  (Through LDS a step of a sort waits for it.)
+template <int MASK>
+__device__ __forceinline__ uint32_t other_lane(uint32_t v, int lane) {
+    if constexpr (MASK == 1) return (uint32_t)IMU_DPP(v, 0xb1, 0xf, true);
+    if constexpr (MASK == 2) return (uint32_t)IMU_DPP(v, 0x4e, 0xf, true);
+    if constexpr (MASK == 4) return (uint32_t)IMU_DPP(IMU_DPP(v, 0x141, 0xf, true), 0x1b, 0xf, true);
+    if constexpr (MASK == 8) return (uint32_t)IMU_DPP(v, 0x128, 0xf, true);
+    if constexpr (MASK == 15) return (uint32_t)IMU_DPP(v, 0x140, 0xf, true);
+    if constexpr (MASK == 16) {
+        const auto both = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return lane & 16 ? both[0] : both[1];
+    }
+    if constexpr (MASK == 32) {
+        const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return lane & 32 ? both[0] : both[1];
+    }
+    if constexpr (MASK == 63) return other_lane<32>(other_lane<16>(other_lane<15>(v, lane), lane), lane);
+}
+template <int MASK>
+__device__ __forceinline__ uint64_t other_lane(uint64_t k, int lane) {
+    return (uint64_t)other_lane<MASK>((uint32_t)(k >> 32), lane) << 32 | other_lane<MASK>((uint32_t)k, lane);
+}
 
 // A wave's best 64, largest in lane 0.
 struct Best {
     uint64_t key = 0;
-    __device__ __forceinline__ static uint64_t step(uint64_t k, int lane, int mask, bool down) {
-        const uint64_t o = other_lane(k, mask);
-        return (((lane & mask) == 0) == down) == (k > o) ? k : o;
+    template <int MASK>
+    __device__ __forceinline__ static uint64_t step(uint64_t k, int lane, bool down) {
+        const uint64_t o = other_lane<MASK>(k, lane);
+        return (((lane & MASK) == 0) == down) == (k > o) ? k : o;
     }
-    // the keys of the lanes in order, largest first
-    __device__ __forceinline__ static uint64_t sorted(uint64_t k, int lane) {
-#pragma unroll
-        for (int size = 2; size <= 64; size *= 2)
-#pragma unroll
-            for (int mask = size / 2; mask; mask /= 2) k = step(k, lane, mask, (lane & size) == 0);
+    template <int MASK>
+    __device__ __forceinline__ static uint64_t steps(uint64_t k, int lane, bool down) {  // MASK, MASK / 2, ... 1
+        k = step<MASK>(k, lane, down);
+        if constexpr (MASK > 1) k = steps<MASK / 2>(k, lane, down);
         return k;
     }
+    // the keys of the lanes in order, largest first; behind lane `n` there are none (0)
+    __device__ __forceinline__ static uint64_t sorted(uint64_t k, int lane, int n) {
+        k = steps<1>(k, lane, (lane & 2) == 0);
+        k = steps<2>(k, lane, (lane & 4) == 0);
+        k = steps<4>(k, lane, (lane & 8) == 0);
+        k = steps<8>(k, lane, (lane & 16) == 0);
+        if (n <= 16) return k;
+        k = steps<16>(k, lane, (lane & 32) == 0);
+        return steps<32>(k, lane, true);
+    }
     __device__ __forceinline__ void merge(uint64_t other, int lane) {  // other in order too
-        const uint64_t o = other_lane(other, 63);
-        key = key > o ? key : o;
-#pragma unroll
-        for (int mask = 32; mask; mask /= 2) key = step(key, lane, mask, true);
+        const uint64_t o = other_lane<63>(other, lane);
+        key = steps<32>(key > o ? key : o, lane, true);
     }
 };
 
@@ -138,7 +167,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
     bool full = false;               // ... if there are so many
     int held = 0;                    // in `gathered`
     auto flush = [&](int n) __attribute__((always_inline)) {
-        best.merge(Best::sorted(lane < n ? gathered[wave][lane] : 0, lane), lane);
+        if (n) best.merge(Best::sorted(lane < n ? gathered[wave][lane] : 0, lane, n), lane);
         const uint64_t k = (uint64_t)__shfl((unsigned long long)best.key, a.top - 1);
         full = k != 0;
         last = full ? logit_of(k) : -__builtin_inff();
@@ -157,9 +186,14 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
 #pragma unroll
             for (int k = 0; k < V; ++k) x[u * V + k] = k < have ? (float)in[u][k] : -__builtin_inff();
         }
-        float high = x[0];
+        float highs[kScanPieces], high;  // (NaN is passed over, unless all are)
 #pragma unroll
-        for (int e = 1; e < E; ++e) high = fmaxf(high, x[e]);  // (NaN is passed over, unless all are)
+        for (int u = 0; u < kScanPieces; ++u) {
+            highs[u] = x[u * V];
+#pragma unroll
+            for (int k = 1; k < V; ++k) highs[u] = fmaxf(highs[u], x[u * V + k]);
+            high = u ? fmaxf(high, highs[u]) : highs[u];
+        }
         if (high > mine.m) mine.rebase(high);
         if (mine.m > -__builtin_inff()) {
 #pragma unroll
@@ -178,21 +212,26 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
                         if (__builtin_popcountll(__ballot(own >= (bound | (1u << b)))) >= a.top) bound |= 1u << b;
                 }
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int place = first + (e / V) * 256 * V + e % V;
-                    const bool wanted = place < to && (full ? x[e] > last : order_of(x[e]) >= bound);
-                    const uint64_t who = __ballot(wanted);
-                    if (who == 0) continue;
-                    if (wanted) gathered[wave][held + __builtin_popcountll(who & ((1ull << lane) - 1))] = key_of(x[e], place);
-                    held += __builtin_popcountll(who);
-                    if (held < 64) continue;
-                    const uint64_t rest = gathered[wave][64 + lane];
-                    const bool was = full;
-                    const float was_last = last;
-                    flush(64);
-                    full = was, last = was_last;  // (of this chunk everything beyond the bound it began with is wanted: a tie may have a lower place)
-                    held -= 64;
-                    if (lane < held) gathered[wave][lane] = rest;
+                for (int u = 0; u < kScanPieces; ++u) {
+                    if (__ballot(full ? highs[u] > last : order_of(highs[u]) >= bound) == 0) continue;
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        const float v = x[u * V + k];
+                        const int place = first + u * 256 * V + k;
+                        const bool wanted = place < to && (full ? v > last : order_of(v) >= bound);
+                        const uint64_t who = __ballot(wanted);
+                        if (who == 0) continue;
+                        if (wanted) gathered[wave][held + __builtin_popcountll(who & ((1ull << lane) - 1))] = key_of(v, place);
+                        held += __builtin_popcountll(who);
+                        if (held < 64) continue;
+                        const uint64_t rest = gathered[wave][64 + lane];
+                        const bool was = full;
+                        const float was_last = last;
+                        flush(64);
+                        full = was, last = was_last;  // (of this chunk everything beyond the bound it began with is wanted: a tie may have a lower place)
+                        held -= 64;
+                        if (lane < held) gathered[wave][lane] = rest;
+                    }
                 }
                 if (held >= 32 || !full) {
                     flush(held);
@@ -245,7 +284,14 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(const LogprobArgs a) 
     }
     all = wave_join(all);
     Best best;
-    for (int p = 0; p < a.parts && a.top; ++p) best.merge(lane < a.top ? a.part_keys[(row * a.parts + p) * a.top + lane] : 0, lane);
+    for (int p = 0; p < a.parts && a.top; p += 8) {  // (all loads before the first merge)
+        uint64_t k[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) k[u] = lane < a.top && p + u < a.parts ? a.part_keys[(row * a.parts + p + u) * a.top + lane] : 0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (p + u < a.parts) best.merge(k[u], lane);
+    }
     logprob_outputs(a, row, (const T *)a.l + row * a.ldl, std::is_same<T, __bf16>::value, all, lane, 64, best.key, true);
 }
 
