@@ -33,19 +33,32 @@ struct LogprobArgs {
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Maximum m, S and A / log 2 of a part of a row.
+// Maximum m, S and A / log 2 of a part of a row.  Exponents are x log2(e) - M with M = m log2(e) rounded, one operation; S and A are relative to M, and what its
+// rounding left is given back at the end.  Where M would overflow (a row of the type's lowest values) they are (x - m) log2(e).
 struct Moments {
     float m = -__builtin_inff(), s = 0.0f, a = 0.0f;
+    __device__ __forceinline__ static bool plain(float m) { return fabsf(m) < 0x1p100f; }
+    __device__ __forceinline__ float residue() const { return plain(m) ? kLn2 * -fmaf(m, kLog2e, -__fmul_rn(m, kLog2e)) : 0.0f; }  // log 2 times (M - m log2(e))
     __device__ __forceinline__ void rebase(float to) {  // to >= m
-        const float d = m == to ? 0.0f : (m - to) * kLog2e, e = exp2_of(d);  // (m == to: both may be infinite)
+        const float d = m == to ? 0.0f : plain(m) && plain(to) ? __fsub_rn(__fmul_rn(m, kLog2e), __fmul_rn(to, kLog2e)) : (m - to) * kLog2e, e = exp2_of(d);  // (m == to: both may be infinite)
         a = e > 0.0f ? e * fmaf(d, s, a) : 0.0f;
         s *= e;
         m = to;
     }
-    __device__ __forceinline__ void add(float x) {      // x <= m, m > -infinity
-        const float t = (x - m) * kLog2e, e = exp2_of(t);
-        s += e;
-        a = fmaf(e, fmaxf(t, -1e4f), a);                // (e is 0 there; t may be -infinity)
+    template <int N>
+    __device__ __forceinline__ void add(const float (&x)[N]) {  // x <= m, m > -infinity
+        auto one = [&](float t) __attribute__((always_inline)) {
+            const float e = exp2_of(t);
+            s += e;
+            a = fmaf(e, fmaxf(t, -1e4f), a);  // (e is 0 there; t may be -infinity)
+        };
+        if (plain(m)) {
+            const float up = __fmul_rn(m, kLog2e);
+#pragma unroll
+            for (int k = 0; k < N; ++k) one(fmaf(x[k], kLog2e, -up));
+        } else {
+            for (int k = 0; k < N; ++k) one((x[k] - m) * kLog2e);
+        }
     }
     __device__ __forceinline__ void join(Moments o) {
         const float to = fmaxf(m, o.m);
@@ -133,7 +146,7 @@ struct Best {
 __device__ __forceinline__ void logprob_outputs(const LogprobArgs &a, int64_t row, const void *l, bool bf16, const Moments &all, int at, int of, uint64_t key, bool lists) {
     const bool none = all.m == -__builtin_inff() && all.s == 0.0f;
     // (log p = (l - m) - log S: m may be so large that log S is lost beside it)
-    const float logs = none ? 0.0f : logf(all.s);
+    const float logs = none ? 0.0f : logf(all.s) + all.residue();
     auto logp = [&](float x) { return none ? all.m : (x - all.m) - logs; };
     if (at == 0) {
         if (a.lse) a.lse[row] = all.m + logs;
@@ -154,7 +167,7 @@ __device__ __forceinline__ void logprob_outputs(const LogprobArgs &a, int64_t ro
 
 template <class T, bool TOP, bool ONCE>
 __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
-    constexpr int V = kVec<T>, E = V * kScanPieces, kChunk = 256 * E;
+    constexpr int V = kVec<T>;
     __shared__ float part[4][3];
     __shared__ uint64_t gathered[4][TOP ? 128 : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -172,23 +185,27 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
         full = k != 0;
         last = full ? logit_of(k) : -__builtin_inff();
     };
-    for (int base = from; base < to; base += kChunk) {
-        piece_t<T, V> in[kScanPieces];
+    // a chunk of several pieces to a thread or of one, a whole one without a look at the row's end
+    auto fetch = [&](int base, auto whole, auto &in) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < kScanPieces; ++u) {
+        for (int u = 0; u < (int)(sizeof(in) / sizeof(in[0])); ++u) {
             const int at = base + (u * 256 + (int)threadIdx.x) * V;
-            in[u] = load_piece<T, V, ONCE>(l + at, to - at);
+            in[u] = load_piece<T, V, ONCE>(l + at, decltype(whole)::value ? V : to - at);
         }
+    };
+    auto scan = [&](int base, auto whole, const auto &in) __attribute__((always_inline)) {
+        constexpr bool kWhole = decltype(whole)::value;
+        constexpr int P = sizeof(in) / sizeof(in[0]), E = V * P;
         float x[E];
 #pragma unroll
-        for (int u = 0; u < kScanPieces; ++u) {
+        for (int u = 0; u < P; ++u) {
             const int have = to - (base + (u * 256 + (int)threadIdx.x) * V);
 #pragma unroll
-            for (int k = 0; k < V; ++k) x[u * V + k] = k < have ? (float)in[u][k] : -__builtin_inff();
+            for (int k = 0; k < V; ++k) x[u * V + k] = kWhole || k < have ? (float)in[u][k] : -__builtin_inff();
         }
-        float highs[kScanPieces], high;  // (NaN is passed over, unless all are)
+        float highs[P], high;  // (NaN is passed over, unless all are)
 #pragma unroll
-        for (int u = 0; u < kScanPieces; ++u) {
+        for (int u = 0; u < P; ++u) {
             highs[u] = x[u * V];
 #pragma unroll
             for (int k = 1; k < V; ++k) highs[u] = fmaxf(highs[u], x[u * V + k]);
@@ -196,8 +213,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
         }
         if (high > mine.m) mine.rebase(high);
         if (mine.m > -__builtin_inff()) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) mine.add(x[e]);
+            mine.add(x);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) mine.s += x[e] == x[e] ? 0.0f : x[e];
@@ -207,18 +223,18 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
                 const int first = base + (int)threadIdx.x * V;
                 uint32_t bound = 0;  // where the list is not full: what the top-th of the lanes' largest has at least
                 if (!full) {
-                    const uint32_t own = first < to ? order_of(high) : 0;
+                    const uint32_t own = kWhole || first < to ? order_of(high) : 0;
                     for (int b = 31; b >= 0; --b)
                         if (__builtin_popcountll(__ballot(own >= (bound | (1u << b)))) >= a.top) bound |= 1u << b;
                 }
 #pragma unroll
-                for (int u = 0; u < kScanPieces; ++u) {
+                for (int u = 0; u < P; ++u) {
                     if (__ballot(full ? highs[u] > last : order_of(highs[u]) >= bound) == 0) continue;
 #pragma unroll
                     for (int k = 0; k < V; ++k) {
                         const float v = x[u * V + k];
                         const int place = first + u * 256 * V + k;
-                        const bool wanted = place < to && (full ? v > last : order_of(v) >= bound);
+                        const bool wanted = (kWhole || place < to) && (full ? v > last : order_of(v) >= bound);
                         const uint64_t who = __ballot(wanted);
                         if (who == 0) continue;
                         if (wanted) gathered[wave][held + __builtin_popcountll(who & ((1ull << lane) - 1))] = key_of(v, place);
@@ -243,6 +259,24 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
                 }
             }
         }
+    };
+    int base = from;
+    constexpr int kMany = 256 * V * kScanPieces;
+    piece_t<T, V> now[kScanPieces], next[kScanPieces], last_ones[1];
+    if (base + kMany <= to) fetch(base, std::true_type(), now);
+    for (; base + kMany <= to; base += kMany) {  // (the next chunk is on its way while this one is looked at)
+        if (base + 2 * kMany <= to) fetch(base + kMany, std::true_type(), next);
+        scan(base, std::true_type(), now);
+#pragma unroll
+        for (int u = 0; u < kScanPieces; ++u) now[u] = next[u];
+    }
+    for (; base + 256 * V <= to; base += 256 * V) {
+        fetch(base, std::true_type(), last_ones);
+        scan(base, std::true_type(), last_ones);
+    }
+    if (base < to) {
+        fetch(base, std::false_type(), last_ones);
+        scan(base, std::false_type(), last_ones);
     }
     if constexpr (TOP) flush(held);
     mine = wave_join(mine);
@@ -306,7 +340,7 @@ struct LogprobBackArgs {
 
 template <class T, bool ONCE>
 __global__ __launch_bounds__(256) void logprobs_back_kernel(const LogprobBackArgs a) {
-    constexpr int V = kVec<T>, kChunk = 256 * V * kScanPieces;
+    constexpr int V = kVec<T>;
     __shared__ float part[4];
     const int64_t row = (int64_t)blockIdx.x / a.parts;
     const int which = (int)((int64_t)blockIdx.x - row * a.parts), from = which * a.per, to = min(a.vocab, from + a.per);
@@ -345,22 +379,30 @@ __global__ __launch_bounds__(256) void logprobs_back_kernel(const LogprobBackArg
         own[u] = t >= from && t < to ? (float)l[t] : 0.0f;
     }
     __syncthreads();
-    for (int base = from; base < to; base += kChunk) {
-        piece_t<T, V> in[kScanPieces];
+    auto turn = [&](int base, auto pieces, auto whole) __attribute__((always_inline)) {
+        constexpr bool kWhole = decltype(whole)::value;
+        constexpr int P = decltype(pieces)::value;
+        piece_t<T, V> in[P];
 #pragma unroll
-        for (int u = 0; u < kScanPieces; ++u) {
+        for (int u = 0; u < P; ++u) {
             const int at = base + (u * 256 + (int)threadIdx.x) * V;
-            in[u] = load_piece<T, V, ONCE>(l + at, to - at);
+            in[u] = load_piece<T, V, ONCE>(l + at, kWhole ? V : to - at);
         }
 #pragma unroll
-        for (int u = 0; u < kScanPieces; ++u) {
+        for (int u = 0; u < P; ++u) {
             const int at = base + (u * 256 + (int)threadIdx.x) * V;
             float f[V];
 #pragma unroll
             for (int k = 0; k < V; ++k) f[k] = none ? 0.0f : dense((float)in[u][k]);
-            if (at < to) store_upto<T, V, ONCE>(gl + at, f, to - at);
+            if (kWhole || at < to) store_upto<T, V, ONCE>(gl + at, f, kWhole ? V : to - at);
         }
-    }
+    };
+    int base = from;
+    using Some = std::integral_constant<int, kScanPieces>;
+    using One = std::integral_constant<int, 1>;
+    for (; base + 256 * V * kScanPieces <= to; base += 256 * V * kScanPieces) turn(base, Some(), std::true_type());
+    for (; base + 256 * V <= to; base += 256 * V) turn(base, One(), std::true_type());
+    if (base < to) turn(base, One(), std::false_type());
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
@@ -390,7 +432,7 @@ struct Parts {
 };
 static Parts parts_of(int64_t rows, int64_t vocab, int dtype) {
     const int64_t chunk = 256 * kScanPieces * (dtype == IMUNPACK_F32 ? 4 : 8), chunks = (vocab + chunk - 1) / chunk;
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(chunks, kMostParts), 1024 / std::max<int64_t>(rows, 1)));
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(chunks, kMostParts), 2048 / std::max<int64_t>(rows, 1)));
     const int64_t each = (chunks + parts - 1) / parts;
     return {(int)((chunks + each - 1) / each), (int)std::min(each * chunk, vocab)};
 }
@@ -446,7 +488,7 @@ extern "C" int imunpack_logprobs_backward(const void *logits, int64_t ldl, int64
     const int64_t size = dtype == IMUNPACK_F32 ? 4 : 2;
     auto at = [](auto *p, int64_t k) { return p ? p + k : p; };
     const Parts p = parts_of(rows, vocab, dtype);
-    const bool once = rows * vocab * size >= kLastLevelCache;
+    const bool once = 2 * rows * vocab * size >= kLastLevelCache * 3 / 4;
     for (int64_t r = 0; r < rows; r += kLogprobRows) {
         const LogprobBackArgs a = {(const char *)logits + r * ldl * size, at(tokens, r * count), at(top_index, r * top), stats + 2 * r, at(entropy, r), count ? at(g_logp, r * count) : nullptr,
                                    at(g_entropy, r), top ? at(g_top, r * top) : nullptr, (char *)gl + r * ldg * size, ldl, ldg, ignore_index, (int)vocab, (int)count, (int)top, p.parts, p.per};
