@@ -5,10 +5,11 @@
 //
 // Forward: one pass over the row with the running maximum of a thread; where it moves by d <= 0, S -> S e^d, A -> e^d (A + d S).  Exponents are kept in
 // units of log 2.  Few rows are cut into parts, a workgroup to each, which a second launch joins.
-// The largest `top`: a wave keeps its best 64 in order, one to a lane, as a number that grows with the logit and falls with the place.  A chunk of the row whose
-// maximum does not beat the last of them is passed over (which is nearly every chunk after the first ones); what beats it is gathered in LDS and, 64 at a time, sorted
-// and merged with the list.  The first chunk would be gathered whole: there the top-th largest of the lanes' maxima, found bit by bit, is a bound that no more than `top` lanes' worth of
-// elements reach, but for ties.
+// The largest `top`: a wave gathers in LDS what may be among them.  The first chunk of the row gives a bound, the top-th largest of the lanes' maxima (found bit by bit), which
+// at least `top` elements reach and, but for ties, no more than `top` lanes' worth; chunks whose maximum stays below it are passed over, which is nearly every one after the
+// first few.  64 gathered elements are sorted, one to a lane, and merged with the wave's best 64, whose top-th is the next bound; mostly that happens once, for what the workgroup's waves
+// gathered together.  An element is a number that grows with the logit and falls with the place.  -infinity (and NaN) is never gathered: where fewer than `top` others exist, the
+// lowest of the remaining places follow them.
 #include "common.h"
 #include "elements.h"
 
@@ -78,9 +79,9 @@ __device__ __forceinline__ Moments wave_join(Moments v) {
     return v;
 }
 
-// The order of a logit among a row's: larger first, then the lower place.  NaN stands with -infinity.  0 is below all.
+// The order of a logit among a row's: larger first, then the lower place.  0 is below all.
 __device__ __forceinline__ uint32_t order_of(float x) {
-    const uint32_t b = x == x ? __float_as_uint(x + 0.0f) : 0xff800000u;
+    const uint32_t b = __float_as_uint(x + 0.0f);
     return b >> 31 ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float logit_of(uint64_t key) {
@@ -159,9 +160,26 @@ __device__ __forceinline__ void logprob_outputs(const LogprobArgs &a, int64_t ro
         if (t != a.ignore) v = t < 0 || t >= a.vocab ? __builtin_nanf("") : logp(bf16 ? (float)((const __bf16 *)l)[t] : ((const float *)l)[t]);
         a.logp[row * a.count + j] = v;
     }
-    if (lists && at < a.top) {
-        a.top_index[row * a.top + at] = (int)~(uint32_t)key;
-        a.top_logp[row * a.top + at] = logp(logit_of(key));
+    if (!lists) return;  // (a whole wave that holds the largest, in order)
+    const int some = __builtin_popcountll(__ballot(key != 0));
+    int place = (int)~(uint32_t)key;
+    if (some < a.top) {  // the lowest places that are not among them: fewer than 64 are, so they lie below 128
+        uint64_t low = 0, high = 0;
+        for (int k = 0; k < some; ++k) {
+            const int p = __shfl(place, k);
+            if (p < 64) low |= 1ull << p;
+            else if (p < 128) high |= 1ull << (p - 64);
+        }
+        int skip = at - some, found = 0;  // the skip-th free place, from 0
+        for (int p = 0; p < 128; ++p) {
+            const bool taken = ((p < 64 ? low >> p : high >> (p - 64)) & 1) != 0;
+            if (!taken && skip-- == 0) found = p;
+        }
+        if (at >= some) place = found;
+    }
+    if (at < a.top) {
+        a.top_index[row * a.top + at] = place;
+        a.top_logp[row * a.top + at] = key ? logp(logit_of(key)) : logp(-__builtin_inff());
     }
 }
 
@@ -169,33 +187,31 @@ template <class T, bool TOP, bool ONCE>
 __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
     constexpr int V = kVec<T>;
     __shared__ float part[4][3];
-    __shared__ uint64_t gathered[4][TOP ? 128 : 1];
+    __shared__ uint64_t gathered[4][TOP ? 128 : 1], lists[4][TOP ? 64 : 1];
+    __shared__ int counts[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t row = (int64_t)blockIdx.x / a.parts;
     const int which = (int)((int64_t)blockIdx.x - row * a.parts), from = which * a.per, to = min(a.vocab, from + a.per);
     const T *l = (const T *)a.l + row * a.ldl;
     Moments mine;
     Best best;
-    float last = -__builtin_inff();  // the top-th logit so far
-    bool full = false;               // ... if there are so many
-    int held = 0;                    // in `gathered`
+    float least = -__builtin_inff();  // what an element has to reach (or, `beyond`, to exceed) to be gathered
+    bool beyond = true, flushed = false;
+    int held = 0;                     // in `gathered`
     auto flush = [&](int n) __attribute__((always_inline)) {
-        if (n) best.merge(Best::sorted(lane < n ? gathered[wave][lane] : 0, lane, n), lane);
-        const uint64_t k = (uint64_t)__shfl((unsigned long long)best.key, a.top - 1);
-        full = k != 0;
-        last = full ? logit_of(k) : -__builtin_inff();
+        best.merge(Best::sorted(lane < n ? gathered[wave][lane] : 0, lane, n), lane);
+        flushed = true;
     };
-    // a chunk of several pieces to a thread or of one, a whole one without a look at the row's end
-    auto fetch = [&](int base, auto whole, auto &in) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < (int)(sizeof(in) / sizeof(in[0])); ++u) {
-            const int at = base + (u * 256 + (int)threadIdx.x) * V;
-            in[u] = load_piece<T, V, ONCE>(l + at, decltype(whole)::value ? V : to - at);
-        }
-    };
-    auto scan = [&](int base, auto whole, const auto &in) __attribute__((always_inline)) {
+    // a chunk, a whole one without a look at the row's end
+    auto scan = [&](int base, auto whole) __attribute__((always_inline)) {
         constexpr bool kWhole = decltype(whole)::value;
-        constexpr int P = sizeof(in) / sizeof(in[0]), E = V * P;
+        constexpr int P = kScanPieces, E = V * P;
+        piece_t<T, V> in[P];
+#pragma unroll
+        for (int u = 0; u < P; ++u) {
+            const int at = base + (u * 256 + (int)threadIdx.x) * V;
+            in[u] = load_piece<T, V, ONCE>(l + at, kWhole ? V : to - at);
+        }
         float x[E];
 #pragma unroll
         for (int u = 0; u < P; ++u) {
@@ -219,69 +235,52 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
             for (int e = 0; e < E; ++e) mine.s += x[e] == x[e] ? 0.0f : x[e];
         }
         if constexpr (TOP) {
-            if (__ballot(!full || high > last)) {
-                const int first = base + (int)threadIdx.x * V;
-                uint32_t bound = 0;  // where the list is not full: what the top-th of the lanes' largest has at least
-                if (!full) {
-                    const uint32_t own = kWhole || first < to ? order_of(high) : 0;
-                    for (int b = 31; b >= 0; --b)
-                        if (__builtin_popcountll(__ballot(own >= (bound | (1u << b)))) >= a.top) bound |= 1u << b;
+            auto wanted = [&](float v) { return beyond ? v > least : v >= least; };
+            if (__ballot(wanted(high))) {
+                if (least == -__builtin_inff()) {  // (the upper half of the order's bits will do)
+                    const uint32_t own = high > least ? order_of(high) >> 16 : 0;
+                    uint32_t bound = 0;
+                    for (uint32_t bit = 0x8000u; bit; bit >>= 1)
+                        if (__builtin_popcountll(__ballot(own >= (bound | bit))) >= a.top) bound |= bit;
+                    if (bound) least = logit_of((uint64_t)bound << 48), beyond = false;
                 }
+                const int first = base + (int)threadIdx.x * V;
+                bool sorted = false;
 #pragma unroll
                 for (int u = 0; u < P; ++u) {
-                    if (__ballot(full ? highs[u] > last : order_of(highs[u]) >= bound) == 0) continue;
+                    if (__ballot(wanted(highs[u])) == 0) continue;
 #pragma unroll
                     for (int k = 0; k < V; ++k) {
                         const float v = x[u * V + k];
-                        const int place = first + u * 256 * V + k;
-                        const bool wanted = (kWhole || place < to) && (full ? v > last : order_of(v) >= bound);
-                        const uint64_t who = __ballot(wanted);
+                        const uint64_t who = __ballot(wanted(v));  // (places behind the row's end hold -infinity)
                         if (who == 0) continue;
-                        if (wanted) gathered[wave][held + __builtin_popcountll(who & ((1ull << lane) - 1))] = key_of(v, place);
+                        if (wanted(v)) gathered[wave][held + __builtin_popcountll(who & ((1ull << lane) - 1))] = key_of(v, first + u * 256 * V + k);
                         held += __builtin_popcountll(who);
                         if (held < 64) continue;
                         const uint64_t rest = gathered[wave][64 + lane];
-                        const bool was = full;
-                        const float was_last = last;
                         flush(64);
-                        full = was, last = was_last;  // (of this chunk everything beyond the bound it began with is wanted: a tie may have a lower place)
                         held -= 64;
                         if (lane < held) gathered[wave][lane] = rest;
+                        sorted = true;
                     }
                 }
-                if (held >= 32 || !full) {
-                    flush(held);
-                    held = 0;
-                } else {
+                // (only now: of this chunk what equals the new bound may have a lower place)
+                if (sorted) {
                     const uint64_t k = (uint64_t)__shfl((unsigned long long)best.key, a.top - 1);
-                    full = k != 0;
-                    last = full ? logit_of(k) : -__builtin_inff();
+                    if (k && logit_of(k) >= least) least = logit_of(k), beyond = true;
                 }
             }
         }
     };
     int base = from;
-    constexpr int kMany = 256 * V * kScanPieces;
-    piece_t<T, V> now[kScanPieces], next[kScanPieces], last_ones[1];
-    if (base + kMany <= to) fetch(base, std::true_type(), now);
-    for (; base + kMany <= to; base += kMany) {  // (the next chunk is on its way while this one is looked at)
-        if (base + 2 * kMany <= to) fetch(base + kMany, std::true_type(), next);
-        scan(base, std::true_type(), now);
-#pragma unroll
-        for (int u = 0; u < kScanPieces; ++u) now[u] = next[u];
-    }
-    for (; base + 256 * V <= to; base += 256 * V) {
-        fetch(base, std::true_type(), last_ones);
-        scan(base, std::true_type(), last_ones);
-    }
-    if (base < to) {
-        fetch(base, std::false_type(), last_ones);
-        scan(base, std::false_type(), last_ones);
-    }
-    if constexpr (TOP) flush(held);
+    for (; base + 256 * V * kScanPieces <= to; base += 256 * V * kScanPieces) scan(base, std::true_type());
+    if (base < to) scan(base, std::false_type());
     mine = wave_join(mine);
     if (lane == 0) part[wave][0] = mine.m, part[wave][1] = mine.s, part[wave][2] = mine.a;
-    if constexpr (TOP) gathered[wave][lane] = best.key;
+    if constexpr (TOP) {
+        lists[wave][lane] = best.key;
+        if (lane == 0) counts[wave] = flushed ? held | 0x1000 : held;
+    }
     __syncthreads();
     Moments all;
 #pragma unroll
@@ -291,9 +290,19 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
         all.join(o);
     }
     if constexpr (TOP) {
-        if (wave == 0)
+        if (wave == 0) {  // the waves' lists, where there are any, and what they gathered last, 64 at a time
+            int before[5] = {0, 0, 0, 0, 0};
 #pragma unroll
-            for (int w = 1; w < 4; ++w) best.merge(gathered[w][lane], lane);
+            for (int w = 0; w < 4; ++w) {
+                before[w + 1] = before[w] + (counts[w] & 0xfff);
+                if (w && counts[w] & 0x1000) best.merge(lists[w][lane], lane);
+            }
+            for (int i = 0; i < before[4]; i += 64) {
+                const int at = i + lane, w = (at >= before[1]) + (at >= before[2]) + (at >= before[3]);
+                const uint64_t k = at < before[4] ? gathered[w][at - (w == 0 ? 0 : w == 1 ? before[1] : w == 2 ? before[2] : before[3])] : 0;
+                best.merge(Best::sorted(k, lane, before[4] - i), lane);
+            }
+        }
     }
     if (a.parts == 1) {
         logprob_outputs(a, row, l, std::is_same<T, __bf16>::value, all, (int)threadIdx.x, 256, best.key, TOP && wave == 0);
