@@ -5,7 +5,7 @@
 //
 // Forward: one pass over the row with the running maximum of a thread; where it moves by d <= 0, S -> S e^d, A -> e^d (A + d S).  Exponents are kept in
 // units of log 2.  Few rows are cut into parts, a workgroup to each, which a second launch joins.
-// The largest `top`: a wave gathers in LDS what may be among them.  The first chunk of the row gives a bound, the top-th largest of the lanes' maxima (found bit by bit), which
+// The largest `top`: a wave gathers in LDS what may be among them.  The top-th largest of the lanes' maxima so far (found bit by bit) is a bound, which
 // at least `top` elements reach and, but for ties, no more than `top` lanes' worth; chunks whose maximum stays below it are passed over, which is nearly every one after the
 // first few.  64 gathered elements are sorted, one to a lane, and merged with the wave's best 64, whose top-th is the next bound; mostly that happens once, for what the workgroup's waves
 // gathered together.  An element is a number that grows with the logit and falls with the place.  -infinity (and NaN) is never gathered: where fewer than `top` others exist, the
@@ -198,7 +198,14 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
     float least = -__builtin_inff();  // what an element has to reach (or, `beyond`, to exceed) to be gathered
     bool beyond = true, flushed = false;
     int held = 0;                     // in `gathered`
+    // (What a lane wrote is read by another of its wave: in order for the hardware, and here for the compiler, which moved loads over stores of other lanes' words
+    // where a loop stood around them.)
+    auto written = []() __attribute__((always_inline)) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
     auto flush = [&](int n) __attribute__((always_inline)) {
+        written();
         best.merge(Best::sorted(lane < n ? gathered[wave][lane] : 0, lane, n), lane);
         flushed = true;
     };
@@ -237,12 +244,14 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
         if constexpr (TOP) {
             auto wanted = [&](float v) { return beyond ? v > least : v >= least; };
             if (__ballot(wanted(high))) {
-                if (least == -__builtin_inff()) {  // (the upper half of the order's bits will do)
-                    const uint32_t own = high > least ? order_of(high) >> 16 : 0;
+                {  // what at least `top` lanes have seen (the upper half of the order's bits will do)
+                    const uint32_t own = mine.m > -__builtin_inff() ? order_of(mine.m) >> 16 : 0;
                     uint32_t bound = 0;
+#pragma unroll 1
                     for (uint32_t bit = 0x8000u; bit; bit >>= 1)
                         if (__builtin_popcountll(__ballot(own >= (bound | bit))) >= a.top) bound |= bit;
-                    if (bound) least = logit_of((uint64_t)bound << 48), beyond = false;
+                    const float reach = logit_of((uint64_t)bound << 48);
+                    if (bound && reach > least) least = reach, beyond = false;
                 }
                 const int first = base + (int)threadIdx.x * V;
                 bool sorted = false;
@@ -257,10 +266,13 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
                         if (wanted(v)) gathered[wave][held + __builtin_popcountll(who & ((1ull << lane) - 1))] = key_of(v, first + u * 256 * V + k);
                         held += __builtin_popcountll(who);
                         if (held < 64) continue;
+                        written();
                         const uint64_t rest = gathered[wave][64 + lane];
                         flush(64);
                         held -= 64;
+                        written();
                         if (lane < held) gathered[wave][lane] = rest;
+                        written();
                         sorted = true;
                     }
                 }
@@ -435,15 +447,15 @@ static bool logprob_sizes(int64_t rows, int64_t vocab, int64_t count, int64_t to
     return rows >= 0 && rows < (1ll << 31) && vocab >= 1 && vocab <= (1 << 30) && count >= 0 && count <= 1024 && top >= 0 && top <= IMUNPACK_LOGPROBS_TOP && top <= vocab &&
            (dtype == IMUNPACK_F32 || dtype == IMUNPACK_BF16);
 }
-// How many workgroups share a row, and how much of it each takes (whole chunks).
+// How many workgroups share a row, and how much of it each takes (whole pieces).
 struct Parts {
     int parts, per;
 };
 static Parts parts_of(int64_t rows, int64_t vocab, int dtype) {
-    const int64_t chunk = 256 * kScanPieces * (dtype == IMUNPACK_F32 ? 4 : 8), chunks = (vocab + chunk - 1) / chunk;
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(chunks, kMostParts), 2048 / std::max<int64_t>(rows, 1)));
-    const int64_t each = (chunks + parts - 1) / parts;
-    return {(int)((chunks + each - 1) / each), (int)std::min(each * chunk, vocab)};
+    const int64_t piece = 256 * (dtype == IMUNPACK_F32 ? 4 : 8), pieces = (vocab + piece - 1) / piece;
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((pieces + kScanPieces - 1) / kScanPieces, kMostParts), 2048 / std::max<int64_t>(rows, 1)));
+    const int64_t each = (pieces + parts - 1) / parts;
+    return {(int)((pieces + each - 1) / each), (int)std::min(each * piece, vocab)};
 }
 }  // namespace imu
 
