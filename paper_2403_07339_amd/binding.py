@@ -752,7 +752,7 @@ class Logprobs:
     """Of rows of logits: logp of the given tokens, lse, entropy, the largest log probabilities and their places (None where not asked for);
     stats (maximum and log of the sum relative to it) goes to imunpack_logprobs_backward."""
     logp: torch.Tensor | None
-    lse: torch.Tensor
+    lse: torch.Tensor | None
     stats: torch.Tensor
     entropy: torch.Tensor | None
     top_logp: torch.Tensor | None

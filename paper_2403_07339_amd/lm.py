@@ -1,11 +1,13 @@
 """A small encoder trained on masked tokens: the layers, the norm, the loss and the optimiser of this package together.
 
-    python -m paper_2403_07339_amd.lm [--steps N] [--state-bits 8|32]
+    python -m paper_2403_07339_amd.lm [--steps N] [--state-bits 8|32] [--mlp integer|block8]
 
-Every product of the blocks runs on the exact low-bit integer path (``linear``, ``attention``); between them stands ``norm.RMSNorm``,
+Every product of the blocks runs on the exact low-bit integer path (``linear``, ``attention``), or those of the MLP in 8-bit floating point with
+activations kept that way (``block8``); between them stands ``norm.RMSNorm``,
 which carries the residual stream in fp32; the head's loss over the vocabulary (``loss``) is taken where a token is masked; one call of
 ``optim.AdamW`` steps all parameters.  ``IntegerHead`` is the serving end: the last norm gives In-Bound integers with a step per
-row, and their product with the head's weights, quantised and unpacked when they are loaded, is exact.
+row, and their product with the head's weights, quantised and unpacked when they are loaded, is exact; ``score`` takes log probabilities, entropy and
+alternatives from its logits (``logprobs``).
 The data are synthetic: sequences that a rule continues, so that a masked token follows from its neighbours.
 """
 from __future__ import annotations
@@ -17,7 +19,9 @@ import torch
 
 from . import binding as imu
 from .attention import IMUnpackAttention
+from .block8 import Block8MLP
 from .linear import IMUnpackLinear, QuantConfig
+from .logprobs import Scores, log_probs
 from .loss import LinearCrossEntropy
 from .norm import RMSNorm
 from .optim import AdamW
@@ -34,6 +38,7 @@ class Config:
     heads: int = 4
     layers: int = 2
     mask: float = 0.15
+    mlp: str = "integer"   # or "block8": 8-bit floating point
 
 
 class Block(torch.nn.Module):
@@ -45,8 +50,14 @@ class Block(torch.nn.Module):
         self.norm1, self.norm2 = RMSNorm(c.width, device=device), RMSNorm(c.width, device=device)
         self.qkv = IMUnpackLinear(c.width, 3 * c.width, cfg=quant, device=device)
         self.out = IMUnpackLinear(c.width, c.width, cfg=quant, device=device)
-        self.up = IMUnpackLinear(c.width, c.hidden, cfg=quant, device=device)
-        self.down = IMUnpackLinear(c.hidden, c.width, cfg=quant, device=device)
+        if c.mlp == "block8":
+            self.mlp = Block8MLP(c.width, c.hidden, device=device)
+        elif c.mlp == "integer":
+            self.up = IMUnpackLinear(c.width, c.hidden, cfg=quant, device=device)
+            self.down = IMUnpackLinear(c.hidden, c.width, cfg=quant, device=device)
+        else:
+            raise ValueError("mlp is integer or block8")
+        self.eight = c.mlp == "block8"
         self.attention = IMUnpackAttention(quant)
 
     def forward(self, x: torch.Tensor, stream: torch.Tensor):
@@ -55,6 +66,8 @@ class Block(torch.nn.Module):
         q, k, v = self.qkv(y).view(b, t, 3, self.heads, w // self.heads).permute(2, 0, 3, 1, 4).contiguous()  # (one batch of products, not a loop of them)
         x = self.out(self.attention(q, k, v).transpose(1, 2).reshape(b, t, w))
         y, stream = self.norm2(x, stream)
+        if self.eight:
+            return self.mlp(y), stream
         return self.down(torch.nn.functional.gelu(self.up(y))), stream
 
 
@@ -108,6 +121,12 @@ class IntegerHead:
         return (out * scale.view(-1, 1)).view(*x.shape[:-1], -1)
 
 
+@torch.no_grad()
+def score(model: MaskedLM, head: IntegerHead, tokens: torch.Tensor, target: torch.Tensor, top: int = 5) -> Scores:
+    """Log probabilities of target under the integer head (0 where it is IGNORE), the entropy of every position and its `top` likeliest tokens."""
+    return log_probs(head(*model.encode(tokens)), target, top, IGNORE)
+
+
 def batch(c: Config, sequences: int, generator: torch.Generator, device="cuda"):
     """(tokens, target): sequences a, a + s, a + 2 s, ... modulo the vocabulary with s of a few steps; some tokens masked."""
     start = torch.randint(0, c.vocab, (sequences, 1), generator=generator)
@@ -141,14 +160,16 @@ def main():
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--sequences", type=int, default=32)
     ap.add_argument("--state-bits", type=int, default=8, choices=(8, 32))
+    ap.add_argument("--mlp", default="integer", choices=("integer", "block8"))
     a = ap.parse_args()
-    c = Config()
+    c = Config(mlp=a.mlp)
     model, _ = train(c, a.steps, a.sequences, state_bits=a.state_bits, tell=lambda s: print(s, flush=True))
     tokens, target = batch(c, 64, torch.Generator().manual_seed(1))
-    with torch.no_grad():
-        scores = IntegerHead(model)(*model.encode(tokens))
+    got = score(model, IntegerHead(model), tokens, target)
     at = target != IGNORE
-    print(f"masked tokens guessed from the integer head's logits: {float((scores.argmax(-1)[at] == target[at]).float().mean()):.3f}")
+    print(f"masked tokens guessed from the integer head's logits: {float((got.top_index[..., 0][at] == target[at]).float().mean()):.3f}, "
+          f"among the first five {float((got.top_index[at] == target[at][:, None]).any(-1).float().mean()):.3f}; "
+          f"log probability {float(got.logp[at].mean()):.3f}, entropy {float(got.entropy[at].mean()):.3f}")
 
 
 if __name__ == "__main__":
