@@ -74,13 +74,23 @@ __device__ __forceinline__ void decode8(uint2 w, float scale, float (&f)[8]) {
     decode4<FORMAT>(w.x, scale, f);
     decode4<FORMAT>(w.y, scale, f + 4);
 }
+// The largest magnitude's bits of N values that count for a scale.  Infinity and NaN are looked for only where the plain maximum shows one.
+template <int N>
+__device__ __forceinline__ int top_bits(const float (&x)[N]) {
+    int top = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) top = max(top, __float_as_int(x[k]) & 0x7fffffff);
+    if (top >= 0x7f800000) {
+        top = 0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) top = max(top, finite_bits(x[k]));
+    }
+    return top;
+}
 // Eight consecutive elements of a block to a lane, the block's 16 lanes together: its byte.
 template <int FORMAT>
 __device__ __forceinline__ int block8_of(const float (&x)[8]) {
-    int top = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) top = max(top, finite_bits(x[k]));
-    return block8_byte<FORMAT>(max16(top));
+    return block8_byte<FORMAT>(max16(top_bits<8>(x)));
 }
 #endif
 }  // namespace imu

@@ -2,8 +2,8 @@
 //
 // All of it is bound by memory.  Along rows, sixteen lanes hold a block (eight elements each), so that its largest magnitude is a maximum over
 // registers and four rotations within a row of lanes, nothing goes through LDS, and the blocks of a matrix of any width fill whole waves.
-// For the turned tensor (codes of x^T with blocks along x's columns), a workgroup holds 128 x 128 elements in registers, eight rows by eight columns a
-// lane; column maxima meet in LDS, and so do the codes, eight rows of a column at a time.
+// For the turned tensor (codes of x^T with blocks along x's columns), a workgroup holds 128 x 128 elements in registers, four rows by eight columns a
+// lane; column maxima meet in LDS, and so do the codes, four rows of a column at a time.
 #include "block8.h"
 
 namespace imu {
@@ -54,64 +54,87 @@ struct TileArgs {
     int cols, kb, square;
 };
 
-// Where the eight codes of rows 8 p .. 8 p + 7 of column c lie in LDS: sixteen bytes at a time at places that turn with the column, so that the
+// Where the four codes of rows 4 p .. 4 p + 3 of column c lie in LDS: sixteen bytes at a time at places that turn with the column, so that the
 // sixteen lanes of a row of lanes, eight columns apart, fall on different banks.
-__device__ __forceinline__ int turned_at(int c, int p) { return c * 128 + ((((p >> 1) ^ (c >> 3)) & 7) << 4) + (p & 1) * 8; }
+__device__ __forceinline__ int turned_at(int c, int p) { return c * 128 + ((((p >> 2) ^ (c >> 3)) & 7) << 4) + (p & 3) * 4; }
 
-// T: float, __bf16, or uint8_t for codes in FORMAT (turned alone).
+// T: float, __bf16, or uint8_t for codes in FORMAT (turned alone).  128 x 128 elements to a workgroup of eight waves, four rows by eight columns to a lane
+// (eight rows by eight columns to one of four waves needed 200 registers: 4096 x 4096 bfloat16 both ways 21.5 us).
+constexpr int kTileWaves = 8;
 template <class T, int FORMAT>
-__global__ __launch_bounds__(256) void block8_tile_kernel(const TileArgs a) {
+__global__ __launch_bounds__(64 * kTileWaves) void block8_tile_kernel(const TileArgs a) {
     constexpr bool kCodes = std::is_same<T, uint8_t>::value;
+    constexpr int R = 4;
     __shared__ __attribute__((aligned(16))) uint8_t tile[128 * 128];
-    __shared__ int tops[4][128];
+    __shared__ __attribute__((aligned(16))) int tops[kTileWaves][128];
+    __shared__ __attribute__((aligned(16))) uint8_t columns[128];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, group = lane >> 4, l16 = lane & 15;
     const int kb = (int)(blockIdx.x % a.kb);
-    const int64_t rb = blockIdx.x / a.kb, row0 = rb * 128 + wave * 32 + group * 8;
+    const int64_t rb = blockIdx.x / a.kb, row0 = rb * 128 + wave * 16 + group * R;
     const int col = kb * 128 + l16 * 8, have = a.cols - col;
-    float x[8][8];
-    piece_t<T, 8> in[8];
+    float x[R][8];
+    {
+        const T *p = (const T *)a.x + row0 * a.ldx + col;
+        piece_t<T, 8> in[R];
+        if (rb * 128 + 128 <= a.rows && kb * 128 + 128 <= a.cols) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) in[i] = load_piece<T, 8>((const T *)a.x + (row0 + i) * a.ldx + col, row0 + i < a.rows ? have : 0);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if constexpr (kCodes) {
-            const int byte = row0 + i < a.rows ? a.xs[(row0 + i) * a.ldxs + kb] : 127;
-            decode8<FORMAT>(__builtin_bit_cast(uint2, in[i]), block8_scale(byte), x[i]);
+            for (int i = 0; i < R; ++i) in[i] = load_piece<T, 8>(p + i * a.ldx, 8);
         } else {
-            to_floats<T, 8>(in[i], x[i]);
+#pragma unroll
+            for (int i = 0; i < R; ++i) in[i] = load_piece<T, 8>(p + i * a.ldx, row0 + i < a.rows ? have : 0);
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if constexpr (kCodes) {
+                const int byte = row0 + i < a.rows ? a.xs[(row0 + i) * a.ldxs + kb] : 127;
+                decode8<FORMAT>(__builtin_bit_cast(uint2, in[i]), block8_scale(byte), x[i]);
+            } else {
+                to_floats<T, 8>(in[i], x[i]);
+            }
         }
     }
     // the columns' maxima (or the square's)
     int top[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        top[j] = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top[j] = max(top[j], finite_bits(x[i][j]));
-        top[j] = max(top[j], __shfl_xor(top[j], 16));
-        top[j] = max(top[j], __shfl_xor(top[j], 32));
+        const float column[R] = {x[0][j], x[1][j], x[2][j], x[3][j]};
+        top[j] = top_bits<R>(column);
+        const auto far = __builtin_amdgcn_permlane32_swap(top[j], top[j], false, false);  // (either half's in both)
+        top[j] = max((int)far[0], (int)far[1]);
+        const auto next = __builtin_amdgcn_permlane16_swap(top[j], top[j], false, false);
+        top[j] = max((int)next[0], (int)next[1]);
     }
-    if (lane < 16)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) tops[wave][lane * 8 + j] = top[j];
+    if (lane < 16) {
+        *reinterpret_cast<int4 *>(&tops[wave][lane * 8]) = make_int4(top[0], top[1], top[2], top[3]);
+        *reinterpret_cast<int4 *>(&tops[wave][lane * 8 + 4]) = make_int4(top[4], top[5], top[6], top[7]);
+    }
     __syncthreads();
-    int all = 0, bytes[8];
+    int bytes[8];
+    {
+        int all = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        top[j] = max(max(tops[0][l16 * 8 + j], tops[1][l16 * 8 + j]), max(tops[2][l16 * 8 + j], tops[3][l16 * 8 + j]));
-        all = max(all, top[j]);
+        for (int h = 0; h < 2; ++h) {
+            int4 t = make_int4(0, 0, 0, 0);
+#pragma unroll
+            for (int w = 0; w < kTileWaves; ++w) {
+                const int4 v = *reinterpret_cast<const int4 *>(&tops[w][l16 * 8 + 4 * h]);
+                t.x = max(t.x, v.x), t.y = max(t.y, v.y), t.z = max(t.z, v.z), t.w = max(t.w, v.w);
+            }
+            top[4 * h] = t.x, top[4 * h + 1] = t.y, top[4 * h + 2] = t.z, top[4 * h + 3] = t.w;
+            all = max(all, max(max(t.x, t.y), max(t.z, t.w)));
+        }
+        if (a.square) {
+            all = max16(all);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top[j] = all;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bytes[j] = block8_byte<FORMAT>(top[j]);
     }
-    if (a.square) {
-        all = max16(all);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top[j] = all;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) bytes[j] = block8_byte<FORMAT>(top[j]);
     if constexpr (!kCodes) {
         if (a.codes) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < R; ++i) {
                 const int byte = a.square ? bytes[0] : block8_of<FORMAT>(x[i]);
                 if (row0 + i < a.rows) {
                     *reinterpret_cast<uint2 *>(a.codes + (row0 + i) * a.ldc + col) = encode8<FORMAT>(x[i], block8_inverse(byte));
@@ -123,21 +146,18 @@ __global__ __launch_bounds__(256) void block8_tile_kernel(const TileArgs a) {
     if (!a.turned) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = x[i][j];
-        *reinterpret_cast<uint2 *>(tile + turned_at(l16 * 8 + j, wave * 4 + group)) = encode8<FORMAT>(v, block8_inverse(bytes[j]));
+        const float inverse = block8_inverse(bytes[j]);
+        *reinterpret_cast<uint32_t *>(tile + turned_at(l16 * 8 + j, wave * 4 + group)) = encode4<FORMAT>(x[0][j] * inverse, x[1][j] * inverse, x[2][j] * inverse, x[3][j] * inverse);
     }
-    if (wave == 0 && group == 0)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < have) a.tscales[(int64_t)(col + j) * a.ldts + rb] = (uint8_t)bytes[j];
+    if (threadIdx.x < 16)
+        *reinterpret_cast<uint2 *>(columns + l16 * 8) = make_uint2(bytes[0] | bytes[1] << 8 | bytes[2] << 16 | (unsigned)bytes[3] << 24, bytes[4] | bytes[5] << 8 | bytes[6] << 16 | (unsigned)bytes[7] << 24);
     __syncthreads();
+    if (threadIdx.x < 128 && kb * 128 + (int)threadIdx.x < a.cols) a.tscales[(int64_t)(kb * 128 + threadIdx.x) * a.ldts + rb] = columns[threadIdx.x];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {  // sixteen rows of a column to a thread
-        const int c = u * 32 + (threadIdx.x >> 3), p = (threadIdx.x & 7) * 2;
+    for (int u = 0; u < 2; ++u) {  // sixteen rows of a column to a thread
+        const int c = u * 64 + (threadIdx.x >> 3), p = (threadIdx.x & 7) * 4;
         if (kb * 128 + c < a.cols)
-            *reinterpret_cast<uint4 *>(a.turned + (int64_t)(kb * 128 + c) * a.ldt + rb * 128 + p * 8) = *reinterpret_cast<const uint4 *>(tile + turned_at(c, p));
+            *reinterpret_cast<uint4 *>(a.turned + (int64_t)(kb * 128 + c) * a.ldt + rb * 128 + p * 4) = *reinterpret_cast<const uint4 *>(tile + turned_at(c, p));
     }
 }
 
@@ -294,10 +314,10 @@ static int tiles(const TileArgs &whole, int dtype, int format, bool codes, hipSt
         if (a.turned) a.turned += r, a.tscales += r / 128;
         const dim3 grid((unsigned)((n + 127) / 128 * a.kb));
         if (codes) {
-            if (format == IMUNPACK_E4M3) hipLaunchKernelGGL((block8_tile_kernel<uint8_t, IMUNPACK_E4M3>), grid, dim3(256), 0, st, a);
-            else hipLaunchKernelGGL((block8_tile_kernel<uint8_t, IMUNPACK_E5M2>), grid, dim3(256), 0, st, a);
+            if (format == IMUNPACK_E4M3) hipLaunchKernelGGL((block8_tile_kernel<uint8_t, IMUNPACK_E4M3>), grid, dim3(64 * kTileWaves), 0, st, a);
+            else hipLaunchKernelGGL((block8_tile_kernel<uint8_t, IMUNPACK_E5M2>), grid, dim3(64 * kTileWaves), 0, st, a);
         } else {
-            by_type(dtype, format, [&](auto t, auto f) { hipLaunchKernelGGL((block8_tile_kernel<decltype(t), decltype(f)::value>), grid, dim3(256), 0, st, a); });
+            by_type(dtype, format, [&](auto t, auto f) { hipLaunchKernelGGL((block8_tile_kernel<decltype(t), decltype(f)::value>), grid, dim3(64 * kTileWaves), 0, st, a); });
         }
     });
 }
