@@ -205,40 +205,52 @@ struct ActArgs {
     int64_t ldu, ldy;
     int rows, cols, kb;
 };
-template <class T, int ACT, bool GATED>
+constexpr int kActBlocks = 2;  // blocks of 16 lanes, one after the other, all loads before the first is used
+template <class T, int ACT, bool GATED, bool ONCE>
 __global__ __launch_bounds__(256) void act8_kernel(const ActArgs a) {
     constexpr int F = IMUNPACK_E4M3;
-    const int block = (int)blockIdx.x * 16 + (threadIdx.x >> 4);
-    if (block >= a.rows * a.kb) return;
-    const int row = block / a.kb, kb = block - row * a.kb, l16 = threadIdx.x & 15, col = kb * kBlock8 + l16 * 8, have = a.cols - col;
-    const T *u = (const T *)a.u + row * a.ldu + col;
-    const piece_t<T, 8> in = load_piece<T, 8>(u, have);
-    piece_t<T, 8> in2;
-    if constexpr (GATED) in2 = load_piece<T, 8>(u + a.cols, have);
-    float x[8], x2[8], y[8];
-    to_floats<T, 8>(in, x);
-    if constexpr (GATED) to_floats<T, 8>(in2, x2);
+    const int total = a.rows * a.kb, l16 = threadIdx.x & 15, first = (int)blockIdx.x * (16 * kActBlocks) + (threadIdx.x >> 4);
+    piece_t<T, 8> in[kActBlocks], in2[kActBlocks];
+    int rows[kActBlocks], kbs[kActBlocks];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        y[k] = act_value<ACT>(x[k]);
-        if constexpr (GATED) y[k] *= x2[k];
+    for (int v = 0; v < kActBlocks; ++v) {
+        const int block = min(first + 16 * v, total - 1);
+        rows[v] = block / a.kb;
+        kbs[v] = block - rows[v] * a.kb;
+        const int col = kbs[v] * kBlock8 + l16 * 8;
+        const T *u = (const T *)a.u + rows[v] * a.ldu + col;
+        in[v] = load_piece<T, 8, ONCE>(u, a.cols - col);
+        if constexpr (GATED) in2[v] = load_piece<T, 8, ONCE>(u + a.cols, a.cols - col);
     }
-    auto keep = [&](const Blocks8 &to, const float (&v)[8]) __attribute__((always_inline)) {
-        const int byte = block8_of<F>(v);
-        const uint2 w = encode8<F>(v, block8_inverse(byte));
-        *reinterpret_cast<uint2 *>(to.codes + row * to.ldc + col) = w;
-        if (l16 == 0) to.scales[row * to.lds + kb] = (uint8_t)byte;
-        return make_uint3(w.x, w.y, (uint32_t)byte);
-    };
-    if (a.kept.codes) {
-        keep(a.kept, x);
-        if constexpr (GATED) keep(a.kept2, x2);
+#pragma unroll
+    for (int v = 0; v < kActBlocks; ++v) {
+        if (first + 16 * v >= total) return;
+        const int row = rows[v], kb = kbs[v], col = kb * kBlock8 + l16 * 8, have = a.cols - col;
+        float x[8], x2[8], y[8];
+        to_floats<T, 8>(in[v], x);
+        if constexpr (GATED) to_floats<T, 8>(in2[v], x2);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            y[k] = act_value<ACT>(x[k]);
+            if constexpr (GATED) y[k] *= x2[k];
+        }
+        auto keep = [&](const Blocks8 &to, const float (&f)[8]) __attribute__((always_inline)) {
+            const int byte = block8_of<F>(f);
+            const uint2 w = encode8<F>(f, block8_inverse(byte));
+            *reinterpret_cast<uint2 *>(to.codes + row * to.ldc + col) = w;
+            if (l16 == 0) to.scales[row * to.lds + kb] = (uint8_t)byte;
+            return make_uint3(w.x, w.y, (uint32_t)byte);
+        };
+        if (a.kept.codes) {
+            keep(a.kept, x);
+            if constexpr (GATED) keep(a.kept2, x2);
+        }
+        if (a.yq.codes) {
+            const uint3 w = keep(a.yq, y);
+            decode8<F>(make_uint2(w.x, w.y), block8_scale((int)w.z), y);
+        }
+        if (a.y && have > 0) store_upto<T, 8, ONCE>((T *)a.y + row * a.ldy + col, y, have);
     }
-    if (a.yq.codes) {
-        const uint3 w = keep(a.yq, y);
-        decode8<F>(make_uint2(w.x, w.y), block8_scale((int)w.z), y);
-    }
-    if (a.y && have > 0) store_upto<T, 8>((T *)a.y + row * a.ldy + col, y, have);
 }
 
 struct ActBackArgs {
@@ -248,34 +260,52 @@ struct ActBackArgs {
     int64_t ldg, ldgu;
     int rows, cols, kb;
 };
-template <class T, int ACT, bool GATED>
+template <class T, int ACT, bool GATED, bool ONCE>
 __global__ __launch_bounds__(256) void act8_back_kernel(const ActBackArgs a) {
     constexpr int F = IMUNPACK_E4M3;
-    const int block = (int)blockIdx.x * 16 + (threadIdx.x >> 4);
-    if (block >= a.rows * a.kb) return;
-    const int row = block / a.kb, kb = block - row * a.kb, col = kb * kBlock8 + (threadIdx.x & 15) * 8, have = a.cols - col;
-    const piece_t<T, 8> in = load_piece<T, 8>((const T *)a.g + row * a.ldg + col, have);
-    float g[8], u[8], u2[8];
-    decode8<F>(*reinterpret_cast<const uint2 *>(a.kept.codes + row * a.kept.ldc + col), block8_scale(a.kept.scales[row * a.kept.lds + kb]), u);
-    if constexpr (GATED)
-        decode8<F>(*reinterpret_cast<const uint2 *>(a.kept2.codes + row * a.kept2.ldc + col), block8_scale(a.kept2.scales[row * a.kept2.lds + kb]), u2);
-    to_floats<T, 8>(in, g);
+    const int total = a.rows * a.kb, l16 = threadIdx.x & 15, first = (int)blockIdx.x * (16 * kActBlocks) + (threadIdx.x >> 4);
+    piece_t<T, 8> in[kActBlocks];
+    uint2 codes[kActBlocks], codes2[kActBlocks];
+    int rows[kActBlocks], kbs[kActBlocks], byte[kActBlocks], byte2[kActBlocks];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        float value;
-        const float slope = act_slope<ACT>(u[k], value);
+    for (int v = 0; v < kActBlocks; ++v) {
+        const int block = min(first + 16 * v, total - 1);
+        rows[v] = block / a.kb;
+        kbs[v] = block - rows[v] * a.kb;
+        const int row = rows[v], kb = kbs[v], col = kb * kBlock8 + l16 * 8;
+        in[v] = load_piece<T, 8, ONCE>((const T *)a.g + row * a.ldg + col, a.cols - col);
+        codes[v] = *reinterpret_cast<const uint2 *>(a.kept.codes + row * a.kept.ldc + col);
+        byte[v] = a.kept.scales[row * a.kept.lds + kb];
         if constexpr (GATED) {
-            const float first = g[k] * slope * u2[k];
-            u2[k] = g[k] * value;
-            u[k] = first;
-        } else {
-            u[k] = g[k] * slope;
+            codes2[v] = *reinterpret_cast<const uint2 *>(a.kept2.codes + row * a.kept2.ldc + col);
+            byte2[v] = a.kept2.scales[row * a.kept2.lds + kb];
         }
     }
-    if (have <= 0) return;
-    T *gu = (T *)a.gu + row * a.ldgu + col;
-    store_upto<T, 8>(gu, u, have);
-    if constexpr (GATED) store_upto<T, 8>(gu + a.cols, u2, have);
+#pragma unroll
+    for (int v = 0; v < kActBlocks; ++v) {
+        if (first + 16 * v >= total) return;
+        const int row = rows[v], col = kbs[v] * kBlock8 + l16 * 8, have = a.cols - col;
+        float g[8], u[8], u2[8];
+        decode8<F>(codes[v], block8_scale(byte[v]), u);
+        if constexpr (GATED) decode8<F>(codes2[v], block8_scale(byte2[v]), u2);
+        to_floats<T, 8>(in[v], g);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            float value;
+            const float slope = act_slope<ACT>(u[k], value);
+            if constexpr (GATED) {
+                const float one = g[k] * slope * u2[k];
+                u2[k] = g[k] * value;
+                u[k] = one;
+            } else {
+                u[k] = g[k] * slope;
+            }
+        }
+        if (have <= 0) continue;
+        T *gu = (T *)a.gu + row * a.ldgu + col;
+        store_upto<T, 8, ONCE>(gu, u, have);
+        if constexpr (GATED) store_upto<T, 8, ONCE>(gu + a.cols, u2, have);
+    }
 }
 
 // ---- entry points ---------------------------------------------------------------------------------------------------------------
@@ -390,13 +420,17 @@ extern "C" int imunpack_act8(const void *u, int64_t ldu, int64_t rows, int64_t c
                   k2 = {(uint8_t *)kept2, (uint8_t *)kept2_scales, ldk, ldks};
     if (!u || (!y && !y_codes) || (y_codes && !blocks8_fit(q, cols)) || (kept && !blocks8_fit(k, cols)) || (kept && gated && !blocks8_fit(k2, cols))) return IMUNPACK_EINVAL;
     const int kb = blocks_of(cols);
+    const bool once = rows * cols * element(dtype) * (gated ? 3 : 2) >= kLastLevelCache;  // u, y and what is kept, or their gradients
     auto from = [](Blocks8 t, int64_t r) { return t.codes ? Blocks8{t.codes + r * t.ldc, t.scales + r * t.lds, t.ldc, t.lds} : t; };
     return in_pieces(rows, kb, 1, [&](int64_t r, int64_t n) {
         const int64_t size = element(dtype);
         const ActArgs a = {(const char *)u + r * ldu * size, y ? (char *)y + r * ldy * size : nullptr, from(q, r), from(k, r), from(k2, r), ldu, ldy, (int)n, (int)cols, kb};
-        const dim3 grid((unsigned)((n * kb + 15) / 16));
+        const dim3 grid((unsigned)((n * kb + 16 * kActBlocks - 1) / (16 * kActBlocks)));
         by_act(dtype, act, gated, [&](auto t, auto f, auto g) {
-            hipLaunchKernelGGL((act8_kernel<decltype(t), decltype(f)::value, decltype(g)::value>), grid, dim3(256), 0, (hipStream_t)stream, a);
+            using T = decltype(t);
+            constexpr int A = decltype(f)::value;
+            constexpr bool G = decltype(g)::value;
+            hipLaunchKernelGGL((once ? act8_kernel<T, A, G, true> : act8_kernel<T, A, G, false>), grid, dim3(256), 0, (hipStream_t)stream, a);
         });
     });
 }
@@ -408,13 +442,17 @@ extern "C" int imunpack_act8_backward(const void *g, int64_t ldg, int64_t rows, 
     const Blocks8 k = {(uint8_t *)kept, (uint8_t *)kept_scales, ldk, ldks}, k2 = {(uint8_t *)kept2, (uint8_t *)kept2_scales, ldk, ldks};
     if (!g || !gu || !blocks8_fit(k, cols) || (gated && !blocks8_fit(k2, cols))) return IMUNPACK_EINVAL;
     const int kb = blocks_of(cols);
+    const bool once = rows * cols * element(dtype) * (gated ? 3 : 2) >= kLastLevelCache;  // u, y and what is kept, or their gradients
     auto from = [](Blocks8 t, int64_t r) { return t.codes ? Blocks8{t.codes + r * t.ldc, t.scales + r * t.lds, t.ldc, t.lds} : t; };
     return in_pieces(rows, kb, 1, [&](int64_t r, int64_t n) {
         const int64_t size = element(dtype);
         const ActBackArgs a = {(const char *)g + r * ldg * size, (char *)gu + r * ldgu * size, from(k, r), from(k2, r), ldg, ldgu, (int)n, (int)cols, kb};
-        const dim3 grid((unsigned)((n * kb + 15) / 16));
+        const dim3 grid((unsigned)((n * kb + 16 * kActBlocks - 1) / (16 * kActBlocks)));
         by_act(dtype, act, gated, [&](auto t, auto f, auto gt) {
-            hipLaunchKernelGGL((act8_back_kernel<decltype(t), decltype(f)::value, decltype(gt)::value>), grid, dim3(256), 0, (hipStream_t)stream, a);
+            using T = decltype(t);
+            constexpr int A = decltype(f)::value;
+            constexpr bool G = decltype(gt)::value;
+            hipLaunchKernelGGL((once ? act8_back_kernel<T, A, G, true> : act8_back_kernel<T, A, G, false>), grid, dim3(256), 0, (hipStream_t)stream, a);
         });
     });
 }
