@@ -436,9 +436,9 @@ static int launch_tiles(const GemmArgs &g, hipStream_t st) {
     return launch_status();
 }
 
-constexpr int64_t kPitch = 1 << 24;  // bytes from row to row at most: offsets within a tile have 32 bits
+constexpr int64_t kPitch = 1 << 24;  // bytes from row to row at most, of codes and scales: offsets within a tile have 32 bits
 static bool operand_fits(const Blocks8 &t, int64_t rows, int64_t cols, int format) {
-    return blocks8_fit(t, cols) && rows >= 1 && t.ldc <= kPitch && (format == IMUNPACK_E4M3 || format == IMUNPACK_E5M2);
+    return blocks8_fit(t, cols) && rows >= 1 && t.ldc <= kPitch && t.lds <= kPitch && (format == IMUNPACK_E4M3 || format == IMUNPACK_E5M2);
 }
 }  // namespace imu
 

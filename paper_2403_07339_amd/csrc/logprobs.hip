@@ -69,26 +69,6 @@ struct Moments {
         a += o.a;
     }
 };
-__device__ __forceinline__ Moments wave_join(Moments v) {
-#pragma unroll
-    for (int k = 32; k; k >>= 1) {
-        Moments o;
-        o.m = __shfl_xor(v.m, k), o.s = __shfl_xor(v.s, k), o.a = __shfl_xor(v.a, k);
-        v.join(o);
-    }
-    return v;
-}
-
-// The order of a logit among a row's: larger first, then the lower place.  0 is below all.
-__device__ __forceinline__ uint32_t order_of(float x) {
-    const uint32_t b = __float_as_uint(x + 0.0f);
-    return b >> 31 ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float logit_of(uint64_t key) {
-    const uint32_t b = (uint32_t)(key >> 32);
-    return __uint_as_float(b >> 31 ? b & 0x7fffffffu : ~b);
-}
-__device__ __forceinline__ uint64_t key_of(float x, int place) { return ((uint64_t)order_of(x) << 32) | (uint32_t)~place; }
 // The value of the lane whose number differs by MASK, on the vector ALU's lane moves: within a row of 16 lanes permutations of four, a rotation by half, mirrors (7 - i and then 3 - i is
 // i ^ 4); across rows and halves the swap of registers, of which each side keeps what it has not.  (Through LDS a step of a sort waits for it.)
 template <int MASK>
@@ -113,6 +93,29 @@ __device__ __forceinline__ uint64_t other_lane(uint64_t k, int lane) {
     return (uint64_t)other_lane<MASK>((uint32_t)(k >> 32), lane) << 32 | other_lane<MASK>((uint32_t)k, lane);
 }
 
+template <int MASK>
+__device__ __forceinline__ void join_lanes(Moments &v, int lane) {
+    Moments o;
+    o.m = __uint_as_float(other_lane<MASK>(__float_as_uint(v.m), lane));
+    o.s = __uint_as_float(other_lane<MASK>(__float_as_uint(v.s), lane));
+    o.a = __uint_as_float(other_lane<MASK>(__float_as_uint(v.a), lane));
+    v.join(o);
+}
+__device__ __forceinline__ Moments wave_join(Moments v, int lane) {
+    join_lanes<32>(v, lane), join_lanes<16>(v, lane), join_lanes<8>(v, lane), join_lanes<4>(v, lane), join_lanes<2>(v, lane), join_lanes<1>(v, lane);
+    return v;
+}
+
+// The order of a logit among a row's: larger first, then the lower place.  0 is below all.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return b >> 31 ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float logit_of(uint64_t key) {
+    const uint32_t b = (uint32_t)(key >> 32);
+    return __uint_as_float(b >> 31 ? b & 0x7fffffffu : ~b);
+}
+__device__ __forceinline__ uint64_t key_of(float x, int place) { return ((uint64_t)order_of(x) << 32) | (uint32_t)~place; }
 // A wave's best 64, largest in lane 0.
 struct Best {
     uint64_t key = 0;
@@ -143,8 +146,20 @@ struct Best {
     }
 };
 
-// What a row's outputs are made of, by one workgroup (or wave): threads `at` of `of`.
-__device__ __forceinline__ void logprob_outputs(const LogprobArgs &a, int64_t row, const void *l, bool bf16, const Moments &all, int at, int of, uint64_t key, bool lists) {
+// Token j of a row, and its logit (of one that is none: 0).
+struct Given {
+    int64_t t = -1;
+    float x = 0.0f;
+};
+__device__ __forceinline__ Given given_of(const LogprobArgs &a, int64_t row, const void *l, bool bf16, int j) {
+    Given k;
+    if (j >= a.count) return k;
+    k.t = a.tokens[row * a.count + j];
+    if (k.t >= 0 && k.t < a.vocab) k.x = bf16 ? (float)((const __bf16 *)l)[k.t] : ((const float *)l)[k.t];
+    return k;
+}
+// What a row's outputs are made of, by one workgroup (or wave): threads `at` of `of`, each with its first token.
+__device__ __forceinline__ void logprob_outputs(const LogprobArgs &a, int64_t row, const void *l, bool bf16, const Moments &all, int at, int of, const Given &own, uint64_t key, bool lists) {
     const bool none = all.m == -__builtin_inff() && all.s == 0.0f;
     // (log p = (l - m) - log S: m may be so large that log S is lost beside it)
     const float logs = none ? 0.0f : logf(all.s) + all.residue();
@@ -155,10 +170,8 @@ __device__ __forceinline__ void logprob_outputs(const LogprobArgs &a, int64_t ro
         if (a.entropy) a.entropy[row] = none ? 0.0f : logs - kLn2 * (all.a / all.s);
     }
     for (int j = at; j < a.count; j += of) {
-        const int64_t t = a.tokens[row * a.count + j];
-        float v = 0.0f;
-        if (t != a.ignore) v = t < 0 || t >= a.vocab ? __builtin_nanf("") : logp(bf16 ? (float)((const __bf16 *)l)[t] : ((const float *)l)[t]);
-        a.logp[row * a.count + j] = v;
+        const Given k = j == at ? own : given_of(a, row, l, bf16, j);
+        a.logp[row * a.count + j] = k.t == a.ignore ? 0.0f : k.t < 0 || k.t >= a.vocab ? __builtin_nanf("") : logp(k.x);
     }
     if (!lists) return;  // (a whole wave that holds the largest, in order)
     const int some = __builtin_popcountll(__ballot(key != 0));
@@ -195,9 +208,9 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
     const T *l = (const T *)a.l + row * a.ldl;
     Moments mine;
     Best best;
-    float least = -__builtin_inff();  // what an element has to reach (or, `beyond`, to exceed) to be gathered
-    bool beyond = true, flushed = false;
-    int held = 0;                     // in `gathered`
+    float reach = -__FLT_MAX__;  // what an element has to reach to be gathered
+    bool flushed = false;
+    int held = 0;                // in `gathered`
     // (What a lane wrote is read by another of its wave: in order for the hardware, and here for the compiler, which moved loads over stores of other lanes' words
     // where a loop stood around them.)
     auto written = []() __attribute__((always_inline)) {
@@ -242,7 +255,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
             for (int e = 0; e < E; ++e) mine.s += x[e] == x[e] ? 0.0f : x[e];
         }
         if constexpr (TOP) {
-            auto wanted = [&](float v) { return beyond ? v > least : v >= least; };
+            auto wanted = [&](float v) { return v >= reach; };
             if (__ballot(wanted(high))) {
                 {  // what at least `top` lanes have seen (the upper half of the order's bits will do)
                     const uint32_t own = mine.m > -__builtin_inff() ? order_of(mine.m) >> 16 : 0;
@@ -250,8 +263,8 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
 #pragma unroll 1
                     for (uint32_t bit = 0x8000u; bit; bit >>= 1)
                         if (__builtin_popcountll(__ballot(own >= (bound | bit))) >= a.top) bound |= bit;
-                    const float reach = logit_of((uint64_t)bound << 48);
-                    if (bound && reach > least) least = reach, beyond = false;
+                    const float all = logit_of((uint64_t)bound << 48);
+                    if (bound && all > reach) reach = all;
                 }
                 const int first = base + (int)threadIdx.x * V;
                 bool sorted = false;
@@ -276,10 +289,11 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
                         sorted = true;
                     }
                 }
-                // (only now: of this chunk what equals the new bound may have a lower place)
+                // (only now: of this chunk what equals the list's last may have a lower place; later ones have to exceed it)
                 if (sorted) {
                     const uint64_t k = (uint64_t)__shfl((unsigned long long)best.key, a.top - 1);
-                    if (k && logit_of(k) >= least) least = logit_of(k), beyond = true;
+                    const float above = logit_of(k + (1ull << 32));
+                    if (k && above > reach) reach = above;
                 }
             }
         }
@@ -287,7 +301,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
     int base = from;
     for (; base + 256 * V * kScanPieces <= to; base += 256 * V * kScanPieces) scan(base, std::true_type());
     if (base < to) scan(base, std::false_type());
-    mine = wave_join(mine);
+    mine = wave_join(mine, lane);
     if (lane == 0) part[wave][0] = mine.m, part[wave][1] = mine.s, part[wave][2] = mine.a;
     if constexpr (TOP) {
         lists[wave][lane] = best.key;
@@ -317,7 +331,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
         }
     }
     if (a.parts == 1) {
-        logprob_outputs(a, row, l, std::is_same<T, __bf16>::value, all, (int)threadIdx.x, 256, best.key, TOP && wave == 0);
+        logprob_outputs(a, row, l, std::is_same<T, __bf16>::value, all, (int)threadIdx.x, 256, given_of(a, row, l, std::is_same<T, __bf16>::value, (int)threadIdx.x), best.key, TOP && wave == 0);
         return;
     }
     if (threadIdx.x == 0) {
@@ -330,24 +344,37 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const LogprobArgs a) {
 // The parts of a row, a wave to a row.
 template <class T>
 __global__ __launch_bounds__(64) void logprobs_join_kernel(const LogprobArgs a) {
+    constexpr bool kHalf = std::is_same<T, __bf16>::value;
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x;
+    const T *l = (const T *)a.l + row * a.ldl;
+    // (every load is asked for before anything waits)
+    auto keys = [&](int p) { return lane < a.top && p < a.parts ? a.part_keys[(row * a.parts + p) * a.top + lane] : 0; };
+    uint64_t k[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) k[u] = keys(u);
     Moments all;
     if (lane < a.parts) {
         const float *p = a.part_stats + (row * a.parts + lane) * 3;
         all.m = p[0], all.s = p[1], all.a = p[2];
     }
-    all = wave_join(all);
+    const Given own = given_of(a, row, l, kHalf, lane);
+    all = wave_join(all, lane);
     Best best;
-    for (int p = 0; p < a.parts && a.top; p += 8) {  // (all loads before the first merge)
-        uint64_t k[8];
+    if (a.top) {
+#pragma unroll 1
+        for (int p = 0; p < a.parts; p += 8) {
+            uint64_t next[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) k[u] = lane < a.top && p + u < a.parts ? a.part_keys[(row * a.parts + p + u) * a.top + lane] : 0;
+            for (int u = 0; u < 8; ++u) next[u] = keys(p + 8 + u);
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (p + u < a.parts) best.merge(k[u], lane);
+            for (int u = 0; u < 8; ++u)
+                if (p + u < a.parts) best.merge(k[u], lane);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) k[u] = next[u];
+        }
     }
-    logprob_outputs(a, row, (const T *)a.l + row * a.ldl, std::is_same<T, __bf16>::value, all, lane, 64, best.key, true);
+    logprob_outputs(a, row, l, kHalf, all, lane, 64, own, best.key, true);
 }
 
 struct LogprobBackArgs {

@@ -53,6 +53,20 @@ def test_linear(b8, lead, d, out, dtype):
         assert torch.equal(layer(x), y.detach())
 
 
+def test_activations_and_parameters_of_different_types(b8):
+    torch.manual_seed(1)
+    layer = b8.Block8Linear(130, 70, device="cuda")
+    x = torch.randn(40, 130, device="cuda").bfloat16().requires_grad_()
+    gy = torch.randn(40, 70, device="cuda").bfloat16()
+    y = layer(x)
+    y.backward(gy)
+    vx, vw = value(x), value(layer.weight, True)
+    near(y.detach(), vx @ vw.t() + layer.bias.to(F), torch.bfloat16)
+    near(x.grad, value(gy) @ vw, torch.bfloat16)
+    near(layer.weight.grad, value(gy.t()) @ value(vx.t().cpu()).t(), torch.float32)
+    near(layer.bias.grad, gy.to(F).sum(0), torch.float32)
+
+
 def test_what_is_kept_between_the_passes(b8):
     layer = b8.Block8MLP(256, 512, act="silu", gated=True, device="cuda")
     x = torch.randn(1024, 256, device="cuda", requires_grad=True)

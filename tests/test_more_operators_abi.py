@@ -57,7 +57,7 @@ def test_gemm(lib):
     assert ws() == 0
     call = caller(lib.imunpack_block8_gemm, [vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, i64, i64, i64, vp, vp, i64, i32, vp, sz, vp],
                   dict(a=FAKE, lda=256, sa=FAKE, ldsa=16, fa=0, b=FAKE, ldb=256, sb=FAKE, ldsb=16, fb=0, m=10, n=20, k=200, bias=None, out=FAKE, ldo=20, dtype=0, ws=FAKE, bytes=1 << 30, st=None))
-    for bad in (dict(a=None), dict(sa=None), dict(a=FAKE + 8), dict(lda=128), dict(lda=260), dict(ldsa=0), dict(ldsa=8), dict(fa=2), dict(b=None), dict(sb=None), dict(ldb=240), dict(ldsb=1),
+    for bad in (dict(a=None), dict(sa=None), dict(a=FAKE + 8), dict(lda=(1 << 24) + 16), dict(ldsa=(1 << 24) + 16), dict(lda=128), dict(lda=260), dict(ldsa=0), dict(ldsa=8), dict(fa=2), dict(b=None), dict(sb=None), dict(ldb=240), dict(ldsb=1),
                 dict(fb=-1), dict(out=None), dict(ldo=19), dict(m=-1), dict(k=0), dict(dtype=3)):
         assert call(**bad) == EINVAL, bad
     assert call(m=0, a=None) == 0 and call(n=0, out=None) == 0
