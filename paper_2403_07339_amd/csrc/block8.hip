@@ -4,6 +4,8 @@
 // registers and four rotations within a row of lanes, nothing goes through LDS, and the blocks of a matrix of any width fill whole waves.
 // For the turned tensor (codes of x^T with blocks along x's columns), a workgroup holds 128 x 128 elements in registers, four rows by eight columns a
 // lane; column maxima meet in LDS, and so do the codes, four rows of a column at a time.
+// 4096 x 11008 bfloat16: along rows 21 us (6.4 TB/s), both ways 36 (5.1), codes turned 21 (4.4); gated SiLU that keeps its input and gives its result in 8 bits 74 (5.5), its
+// gradient 59 (6.1).
 #include "block8.h"
 
 namespace imu {

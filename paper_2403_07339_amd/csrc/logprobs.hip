@@ -10,6 +10,8 @@
 // first few.  64 gathered elements are sorted, one to a lane, and merged with the wave's best 64, whose top-th is the next bound; mostly that happens once, for what the workgroup's waves
 // gathered together.  An element is a number that grows with the logit and falls with the place.  -infinity (and NaN) is never gathered: where fewer than `top` others exist, the
 // lowest of the remaining places follow them.
+// Bound by memory where rows are many: 4096 x 32000 bfloat16 47 us without alternatives (5.6 TB/s), 67 with 8, its gradient 80 (6.6 TB/s, past the last-level cache: what it
+// left there dirty was written back while the next call read, 167 -> 136 us for both).
 #include "common.h"
 #include "elements.h"
 
