@@ -255,8 +255,14 @@ __device__ __forceinline__ void store_tile(const v16f32 (&acc)[T][T], char *lds,
     using E = std::conditional_t<HALF, __bf16, float>;
     constexpr int kWide = 32 * T * (int)sizeof(E), kRow = kWide < 256 ? kWide : 256, kPieces = kRow / 16, kPasses = kWide / kRow, kCols = T / kPasses, kEach = 16 / (int)sizeof(E);
     const int lane = threadIdx.x & 63, lrow = lane & 31, lhalf = lane >> 5;
+    // (what a lane writes is read by another of its wave: in order for the hardware, and told to the compiler)
+    auto written = []() __attribute__((always_inline)) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
 #pragma unroll
     for (int pass = 0; pass < kPasses; ++pass) {
+        if (pass) written();
 #pragma unroll
         for (int jj = 0; jj < kCols; ++jj)
 #pragma unroll
@@ -275,6 +281,7 @@ __device__ __forceinline__ void store_tile(const v16f32 (&acc)[T][T], char *lds,
                     *reinterpret_cast<aligned_t *>(lds + row * kRow + ((piece ^ row) & (kPieces - 1)) * 16 + (HALF ? lhalf * 8 : 0)) = v;
                 }
             }
+        written();
         const int piece = lane & (kPieces - 1), col = n0 + pass * 32 * kCols + piece * kEach;
 #pragma unroll 4
         for (int r = 0; r < 32 * T * kPieces / 64; ++r) {
