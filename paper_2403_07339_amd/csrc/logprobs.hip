@@ -36,14 +36,21 @@ struct LogprobArgs {
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Maximum m, S and A / log 2 of a part of a row.  Exponents are x log2(e) - M with M = m log2(e) rounded, one operation; S and A are relative to M, and what its
-// rounding left is given back at the end.  Where M would overflow (a row of the type's lowest values) they are (x - m) log2(e).
+// Maximum m, S and A / log 2 of a part of a row.  Exponents are x log2(e) - M with M = m log2(e) rounded, one operation; S and A are relative to M, of which every step
+// takes the rounded value (products and differences of it are not contracted), and what its rounding left is given back to log S at the end.  That is at most 1 / 16 where
+// |m| < 2^20; beyond it (a row of a mask's number) exponents are (x - m) log2(e).
 struct Moments {
     float m = -__builtin_inff(), s = 0.0f, a = 0.0f;
-    __device__ __forceinline__ static bool plain(float m) { return fabsf(m) < 0x1p100f; }
-    __device__ __forceinline__ float residue() const { return plain(m) ? kLn2 * -fmaf(m, kLog2e, -__fmul_rn(m, kLog2e)) : 0.0f; }  // log 2 times (M - m log2(e))
+    __device__ __forceinline__ static bool plain(float m) { return fabsf(m) < 0x1p20f; }
+    __device__ __forceinline__ static float base(float m) {
+#pragma clang fp contract(off)
+        return m * kLog2e;
+    }
+    __device__ __forceinline__ static float left(float m) { return plain(m) ? -fmaf(m, kLog2e, -base(m)) : 0.0f; }  // M - m log2(e)
     __device__ __forceinline__ void rebase(float to) {  // to >= m
-        const float d = m == to ? 0.0f : plain(m) && plain(to) ? __fsub_rn(__fmul_rn(m, kLog2e), __fmul_rn(to, kLog2e)) : (m - to) * kLog2e, e = exp2_of(d);  // (m == to: both may be infinite)
+#pragma clang fp contract(off)
+        const float d = m == to ? 0.0f : plain(m) && plain(to) ? base(m) - base(to) : (m - to) * kLog2e + (left(m) - left(to));  // (m == to: both may be infinite)
+        const float e = exp2_of(d);
         a = e > 0.0f ? e * fmaf(d, s, a) : 0.0f;
         s *= e;
         m = to;
@@ -56,7 +63,7 @@ struct Moments {
             a = fmaf(e, fmaxf(t, -1e4f), a);  // (e is 0 there; t may be -infinity)
         };
         if (plain(m)) {
-            const float up = __fmul_rn(m, kLog2e);
+            const float up = base(m);
 #pragma unroll
             for (int k = 0; k < N; ++k) one(fmaf(x[k], kLog2e, -up));
         } else {
@@ -164,12 +171,12 @@ __device__ __forceinline__ Given given_of(const LogprobArgs &a, int64_t row, con
 __device__ __forceinline__ void logprob_outputs(const LogprobArgs &a, int64_t row, const void *l, bool bf16, const Moments &all, int at, int of, const Given &own, uint64_t key, bool lists) {
     const bool none = all.m == -__builtin_inff() && all.s == 0.0f;
     // (log p = (l - m) - log S: m may be so large that log S is lost beside it)
-    const float logs = none ? 0.0f : logf(all.s) + all.residue();
+    const float sum = none ? 0.0f : logf(all.s), logs = none ? 0.0f : fmaf(kLn2, Moments::left(all.m), sum);
     auto logp = [&](float x) { return none ? all.m : (x - all.m) - logs; };
     if (at == 0) {
         if (a.lse) a.lse[row] = all.m + logs;
         if (a.stats) a.stats[2 * row] = all.m, a.stats[2 * row + 1] = logs;
-        if (a.entropy) a.entropy[row] = none ? 0.0f : logs - kLn2 * (all.a / all.s);
+        if (a.entropy) a.entropy[row] = none ? 0.0f : sum - kLn2 * (all.a / all.s);  // (both relative to M)
     }
     for (int j = at; j < a.count; j += of) {
         const Given k = j == at ? own : given_of(a, row, l, bf16, j);

@@ -50,6 +50,55 @@ def test_results_with_a_pitch(imu, m, n, k):
             assert torch.equal(out[:m, :n], want) and untouched(out, m, n)
 
 
+@pytest.mark.parametrize("m,n,k", [(5, 60, 200), (100, 200, 640), (700, 523, 1300), (2600, 2300, 384)])
+def test_bytes_behind_the_blocks(imu, m, n, k):
+    """Nothing is taken from the scales behind a row's blocks: 255 there would make NaN of zeros."""
+    a, b = (imu.imunpack_block8_quantize(torch.randn(r, k, device="cuda"))[0] for r in (m, n))
+    blocks = -(-k // 128)
+    for dtype in (torch.float32, torch.bfloat16):
+        want = imu.imunpack_block8_gemm(a, b, dtype)
+        scales = [torch.full((len(t.scales) + 1, 32), 255, dtype=torch.uint8, device="cuda") for t in (a, b)]
+        for buf, t in zip(scales, (a, b)):
+            buf[:-1, :blocks] = t.scales.view(torch.uint8)[:, :blocks]
+        out, ws = torch.empty_like(want), torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+        call(imu, "imunpack_block8_gemm", a.codes, a.codes.stride(0), scales[0], 32, 0, b.codes, b.codes.stride(0), scales[1], 32, 0, m, n, k, None, out, n, int(dtype == torch.bfloat16), ws, ws.numel())
+        assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("low", [-1e4, -1e5, -1e6, -2.0 ** 20, -1e7, -1e9, -1e10, -1e30, 1e10, 1e30])
+def test_logits_of_large_numbers(imu, low, dtype):
+    """Rows that a mask's number fills, alone or but for a few.  Log probabilities of elements that the maximum does not outweigh have the size of the spread, which is what their
+    tolerance is relative to; l - m is exact or rounded at its own size."""
+    vocab = 5000
+    x = torch.full((6, vocab), low)
+    x[1, 7] += 1.5                     # (what becomes of it is up to the type)
+    x[2, 3000:] *= 1 + 2.0 ** -7
+    x[3, ::3] *= 1 + 2.0 ** -6
+    x[4, 11], x[4, 12] = 0.25, -0.5
+    x[5] = low + torch.randn(vocab, generator=torch.Generator().manual_seed(2)) * 2
+    x = x.to(dtype)
+    tokens = torch.tensor([[0, 7, 11, 12, 3000, 4999]]).expand(6, -1).contiguous()
+    got = imu.imunpack_logprobs(x.cuda(), tokens.cuda(), top=8)
+    d = x.double() - x.double().amax(1, keepdim=True)
+    logs = torch.log(torch.exp(d).sum(1, keepdim=True))
+    logp = d - logs
+    p = torch.exp(logp)
+    h = -torch.where(p > 0, p * logp, torch.zeros_like(p)).sum(1)
+    near = torch.where(d > -100, d, torch.zeros_like(d)).abs().amax(1)
+    want = logp.gather(1, tokens)
+    assert ((got.logp.cpu().double() - want).abs() <= 2.0 ** -18 + 2.0 ** -22 * want.abs()).all()
+    assert ((got.entropy.cpu().double() - h).abs() <= 2.0 ** -18 * (1 + near)).all()
+    lse = x.double().amax(1) + logs[:, 0]
+    assert ((got.lse.cpu().double() - lse).abs() <= 2.0 ** -18 + 2.0 ** -22 * lse.abs()).all()
+    gp, gh = torch.randn(6, 6), torch.randn(6)
+    gl = imu.imunpack_logprobs_backward(x.cuda(), tokens.cuda(), got, gp.cuda(), gh.cuda(), None).cpu().double()
+    g = -p * gp.double().sum(1, keepdim=True) - gh.double()[:, None] * torch.where(p > 0, p * (logp + h[:, None]), torch.zeros_like(p))
+    g.scatter_add_(1, tokens, gp.double())
+    size = 2.0 ** -17 * (p * (gp.abs().double().sum(1, keepdim=True) + gh.abs().double()[:, None] * (10 + 2 * near[:, None])) + 1e-3 * gp.abs().double().amax())
+    assert ((gl - g).abs() <= size + g.abs() * torch.finfo(dtype).eps).all()
+
+
 @pytest.mark.parametrize("rows,cols", [(1, 5), (130, 300), (257, 128)])
 def test_codes_with_a_pitch(imu, rows, cols):
     x = torch.randn(rows, cols, device="cuda")
