@@ -486,6 +486,12 @@ int imunpack_act8_backward(const void *g, int64_t ldg, int64_t rows, int64_t col
                            const void *kept, const void *kept2, int64_t ldk, const void *kept_scales, const void *kept2_scales, int64_t ldks,
                            void *gu, int64_t ldgu, imunpack_stream_t stream);
 
+/* out (device fp32, dense) = the sums of the columns of x (device, dtype, unit stride within a row, ldx elements from row to row), in fp32, in an order that depends on the sizes
+ * alone: the gradient of a bias.  rows == 0 gives zeros.  workspace: device, 16-byte aligned, of the size that imunpack_column_sums_workspace gives (0: NULL will do).
+ * Errors: EINVAL (null pointers, rows outside [0, 2^31], cols outside [1, 2^24], a pitch < cols, unknown types); ESMALL; EHIP. */
+int imunpack_column_sums_workspace(int64_t rows, int64_t cols, int dtype, size_t *bytes);
+int imunpack_column_sums(const void *x, int64_t ldx, int64_t rows, int64_t cols, int dtype, float *out, void *workspace, size_t workspace_bytes, imunpack_stream_t stream);
+
 /* ---- log probabilities of given tokens, entropy, top alternatives ------------------------------------
  * For each of `rows` rows l of `vocab` logits (device, dtype, unit stride within a row, ldl elements from row to row):
  *     lse = log sum_v exp l_v,   logp_j = l_[token_j] - lse for `count` tokens (device int64, row r's at tokens + r count),

@@ -36,6 +36,7 @@ EXPORTS = [
     "imunpack_xent_workspace", "imunpack_xent", "imunpack_xent_rescale",
     "imunpack_block8_quantize", "imunpack_block8_turn", "imunpack_block8_values", "imunpack_block8_gemm_workspace", "imunpack_block8_gemm",
     "imunpack_act8", "imunpack_act8_backward", "imunpack_logprobs_workspace", "imunpack_logprobs", "imunpack_logprobs_backward",
+    "imunpack_column_sums_workspace", "imunpack_column_sums",
 ]
 DIGITS_INT8, DIGITS_FP6 = 0, 1
 
@@ -590,7 +591,7 @@ _tensors.bind(ImunpackError, *[C.cast(getattr(_lib, _name), _vp).value for _name
     "imunpack_rmsnorm", "imunpack_rmsnorm_quantize", "imunpack_rmsnorm_backward_workspace", "imunpack_rmsnorm_backward", "imunpack_adamw",
     "imunpack_xent_workspace", "imunpack_xent", "imunpack_xent_rescale", "imunpack_block8_quantize", "imunpack_block8_turn", "imunpack_block8_values",
     "imunpack_block8_gemm_workspace", "imunpack_block8_gemm", "imunpack_act8", "imunpack_act8_backward", "imunpack_logprobs_workspace", "imunpack_logprobs",
-    "imunpack_logprobs_backward")])
+    "imunpack_logprobs_backward", "imunpack_column_sums_workspace", "imunpack_column_sums")])
 
 
 def imunpack_rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None):
@@ -744,6 +745,11 @@ def imunpack_act8_backward(g: torch.Tensor, kept, act: str = "gelu", gated: bool
         raise ValueError("kept is what imunpack_act8 returned for the same `gated`")
     first, second = kept[0], kept[1] if gated else None
     return _tensors.act8_backward(g, ACTIVATIONS[act], first.codes, first.scales, second.codes if gated else None, second.scales if gated else None, first.cols, _stream())
+
+
+def imunpack_column_sums(x: torch.Tensor) -> torch.Tensor:
+    """The sums of x [..., cols] (fp32 or bfloat16) over all but its last dimension, in fp32: the gradient of a bias."""
+    return _tensors.column_sums(x, _stream())
 
 
 # ---- log probabilities ---------------------------------------------------------------------------------

@@ -71,7 +71,7 @@ class _LinearFunction(torch.autograd.Function):
             gx = imu.imunpack_block8_gemm(gq, wt, dtype).view(x_shape)
         if need_w:
             gw = imu.imunpack_block8_gemm(gt, imu.imunpack_block8_turn(xq), w_dtype)
-        return gx, gw, g.sum(0, dtype=torch.float32).to(b_dtype) if need_b else None, None
+        return gx, gw, imu.imunpack_column_sums(g).to(b_dtype) if need_b else None, None
 
 
 class _MLPFunction(torch.autograd.Function):
@@ -118,13 +118,13 @@ class _MLPFunction(torch.autograd.Function):
             if need_w1:
                 gw1 = imu.imunpack_block8_gemm(gt, imu.imunpack_block8_turn(xq), w1_dtype)
             if need_b1:
-                gb1 = gu.sum(0, dtype=torch.float32).to(b1_dtype)
-        return gx, gw1, gb1, gw2, g.sum(0, dtype=torch.float32).to(b2_dtype) if need_b2 else None, None, None, None
+                gb1 = imu.imunpack_column_sums(gu).to(b1_dtype)
+        return gx, gw1, gb1, gw2, imu.imunpack_column_sums(g).to(b2_dtype) if need_b2 else None, None, None, None
 
 
 def block8_linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None) -> torch.Tensor:
     """x [..., in], weight [out, in], bias [out] -> [..., out]."""
-    if x.shape[-1] != weight.shape[1]:
+    if x.shape[-1] != weight.shape[1] or weight.numel() == 0:
         raise ValueError(f"shapes {tuple(x.shape)} and {tuple(weight.shape)} do not form x W^T")
     return _LinearFunction.apply(x, weight, bias, torch.is_grad_enabled())
 
@@ -134,7 +134,7 @@ def block8_mlp(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, b1: torch.Te
     """f(x W1^T + b1) W2^T + b2 with f GELU or SiLU; gated: f of the first half of W1's rows times the second half's product."""
     if act not in imu.ACTIVATIONS:
         raise ValueError("act is gelu or silu")
-    if x.shape[-1] != w1.shape[1] or w1.shape[0] != w2.shape[1] * (2 if gated else 1):
+    if x.shape[-1] != w1.shape[1] or w1.numel() == 0 or w2.numel() == 0 or w1.shape[0] != w2.shape[1] * (2 if gated else 1):
         raise ValueError(f"shapes {tuple(x.shape)}, {tuple(w1.shape)} and {tuple(w2.shape)} do not form an MLP")
     return _MLPFunction.apply(x, w1, b1, w2, b2, act, gated, torch.is_grad_enabled())
 

@@ -9,7 +9,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libimunpack.so")
-SOURCES = ["api.hip", "percentile.hip", "quantize.hip", "plan.hip", "unpack.hip", "gemm.hip", "batched.hip", "norm.hip", "adamw.hip", "xent.hip", "block8.hip", "block8_gemm.hip", "logprobs.hip"]
+SOURCES = ["api.hip", "percentile.hip", "quantize.hip", "plan.hip", "unpack.hip", "gemm.hip", "batched.hip", "norm.hip", "adamw.hip", "xent.hip", "block8.hip", "block8_gemm.hip", "column_sums.hip", "logprobs.hip"]
 TENSORS = os.path.join(HERE, "_tensors.so")
 CXX = os.environ.get("CXX", "g++")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

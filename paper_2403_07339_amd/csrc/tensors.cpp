@@ -35,6 +35,8 @@ decltype(&imunpack_act8_backward) g_act8_backward = nullptr;
 decltype(&imunpack_logprobs_workspace) g_logprobs_workspace = nullptr;
 decltype(&imunpack_logprobs) g_logprobs = nullptr;
 decltype(&imunpack_logprobs_backward) g_logprobs_backward = nullptr;
+decltype(&imunpack_column_sums_workspace) g_column_sums_workspace = nullptr;
+decltype(&imunpack_column_sums) g_column_sums = nullptr;
 
 struct Refused : std::runtime_error {  // becomes a ValueError
     using std::runtime_error::runtime_error;
@@ -439,6 +441,22 @@ PyObject *act8_backward(PyObject *const *a) {  // g, act, kept codes, scales, ke
     return wrap(gu);
 }
 
+PyObject *column_sums(PyObject *const *a) {  // x, stream -> sums
+    const at::Tensor &x = tensor(a[0], "column_sums: x");
+    const int type = type_of(x, "column_sums: x");
+    need(x.is_cuda() && x.dim() >= 1 && x.size(-1) >= 1, "column_sums: x is a device tensor with columns");
+    need_current(x.device());
+    const int64_t cols = x.size(-1), rows = rows_of(x, cols);
+    const Rows r = spread(x, cols);
+    const at::Tensor out = at::empty({cols}, x.options().dtype(at::kFloat).requires_grad(false));
+    size_t bytes = 0;
+    check(g_column_sums_workspace(rows, cols, type, &bytes), "imunpack_column_sums_workspace");
+    at::Tensor workspace;
+    if (bytes) workspace = at::empty({(int64_t)bytes}, x.options().dtype(at::kByte).requires_grad(false));
+    check(g_column_sums(r.p, r.pitch, rows, cols, type, (float *)out.data_ptr(), data(workspace), bytes, address(a[1])), "imunpack_column_sums");
+    return wrap(out);
+}
+
 struct Logprobs {  // the arguments that log probabilities and their gradients take, checked
     at::Tensor logits, tokens;
     int64_t vocab, rows, count;
@@ -522,6 +540,8 @@ PyObject *bind(PyObject *const *a) {  // error class, then the addresses of the 
     g_logprobs_workspace = (decltype(g_logprobs_workspace))address(a[16]);
     g_logprobs = (decltype(g_logprobs))address(a[17]);
     g_logprobs_backward = (decltype(g_logprobs_backward))address(a[18]);
+    g_column_sums_workspace = (decltype(g_column_sums_workspace))address(a[19]);
+    g_column_sums = (decltype(g_column_sums))address(a[20]);
     Py_RETURN_NONE;
 }
 
@@ -542,12 +562,12 @@ template <PyObject *(*F)(PyObject *const *), Py_ssize_t N>
 PyMethodDef method(const char *name) {
     return {name, (PyCFunction)(void (*)(void))entry<F, N>, METH_FASTCALL, nullptr};
 }
-PyMethodDef g_methods[] = {method<bind, 19>("bind"), method<rmsnorm, 5>("rmsnorm"), method<rmsnorm_quantize, 7>("rmsnorm_quantize"),
+PyMethodDef g_methods[] = {method<bind, 21>("bind"), method<rmsnorm, 5>("rmsnorm"), method<rmsnorm_quantize, 7>("rmsnorm_quantize"),
                            method<rmsnorm_backward, 8>("rmsnorm_backward"), method<adamw, 15>("adamw"),
                            method<xent, 10>("xent"), method<xent_rescale, 7>("xent_rescale"),
                            method<block8_quantize, 6>("block8_quantize"), method<block8_turn, 4>("block8_turn"), method<block8_values, 5>("block8_values"),
                            method<block8_gemm, 9>("block8_gemm"), method<act8, 7>("act8"), method<act8_backward, 8>("act8_backward"), method<logprobs, 6>("logprobs"),
-                           method<logprobs_backward, 10>("logprobs_backward"), {nullptr, nullptr, 0, nullptr}};
+                           method<logprobs_backward, 10>("logprobs_backward"), method<column_sums, 2>("column_sums"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_tensors", "Argument marshalling of the calls whose host time counts.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 }  // namespace
 

@@ -100,3 +100,17 @@ def test_logprobs(lib):
     for bad in (dict(l=None), dict(ldl=49), dict(ldg=49), dict(t=None), dict(ti=None), dict(stats=None), dict(h=None), dict(gl=None), dict(gl=FAKE, ldg=60), dict(count=2000), dict(vocab=1)):
         assert call(**bad) == EINVAL, bad
     assert call(rows=0, l=None) == 0
+
+
+def test_column_sums(lib):
+    call = caller(lib.imunpack_column_sums, [vp, i64, i64, i64, i32, vp, vp, sz, vp],
+                  dict(x=FAKE, ldx=40, rows=5000, cols=40, dtype=0, out=FAKE, ws=FAKE, bytes=1 << 30, st=None))
+    for bad in (dict(x=None), dict(ldx=39), dict(rows=-1), dict(rows=(1 << 31) + 1), dict(cols=0), dict(cols=(1 << 24) + 1), dict(dtype=2), dict(out=None), dict(ws=None), dict(ws=FAKE + 8)):
+        assert call(**bad) == EINVAL, bad
+    assert call(bytes=0) == ESMALL
+    bytes_ = sz(7)
+    f = lib.imunpack_column_sums_workspace
+    f.restype, f.argtypes = i32, [i64, i64, i32, C.POINTER(sz)]
+    assert f(100, 40, 0, C.byref(bytes_)) == 0 and bytes_.value == 0
+    assert f(5000, 40, 0, C.byref(bytes_)) == 0 and call(bytes=bytes_.value - 1) == ESMALL
+    assert f(5000, 40, 0, None) == EINVAL
