@@ -11,6 +11,8 @@ What the backward pass needs of x is the operand itself, one byte an element; a 
 rounding (but below the smallest codes).  The MLP keeps the activation function's input in 8 bits as well and takes the slope there.
 Beside ``linear.IMUnpackLinear``, whose integer products are exact: here a product takes a fraction of the time and its operands keep four significant bits.
 fp32 or bfloat16, parameters alike or not; results are in x's type, gradients of parameters in theirs.
+Both passes may be captured in a graph; as with every function of torch, no eager autograd graph of the same leaves may live meanwhile, or autograd would add their
+gradients up on the stream where that one was made.
 """
 from __future__ import annotations
 

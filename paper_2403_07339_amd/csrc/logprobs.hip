@@ -483,13 +483,16 @@ static bool logprob_sizes(int64_t rows, int64_t vocab, int64_t count, int64_t to
     return rows >= 0 && rows < (1ll << 31) && vocab >= 1 && vocab <= (1 << 30) && count >= 0 && count <= 1024 && top >= 0 && top <= IMUNPACK_LOGPROBS_TOP && top <= vocab &&
            (dtype == IMUNPACK_F32 || dtype == IMUNPACK_BF16);
 }
-// How many workgroups share a row, and how much of it each takes (whole pieces).
+// How many workgroups share a row, and how much of it each takes (whole pieces).  Forward a part costs its own bound and sort, and what is in one part needs no join: 1024 workgroups, four to a
+// CU, were the best of 512, 768, 1024, 1536 and 2048 (microseconds with five alternatives, 1024 and 2048: 130 x 128000 bfloat16 25, 31; 256 x 128000 28.5, 31.3; 614 x 50265 fp32 34.5, 39.4;
+// 1000 x 32000 bfloat16 23.6, 29.7; 700 x 128000 50.6, 50.0).  Backward a part costs nothing: 2048 (614 x 50265 fp32 54.6, in 1024 59.5).
+constexpr int kForwardGroups = 1024, kBackwardGroups = 2048;
 struct Parts {
     int parts, per;
 };
-static Parts parts_of(int64_t rows, int64_t vocab, int dtype) {
+static Parts parts_of(int64_t rows, int64_t vocab, int dtype, int groups) {
     const int64_t piece = 256 * (dtype == IMUNPACK_F32 ? 4 : 8), pieces = (vocab + piece - 1) / piece;
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((pieces + kScanPieces - 1) / kScanPieces, kMostParts), 2048 / std::max<int64_t>(rows, 1)));
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((pieces + kScanPieces - 1) / kScanPieces, kMostParts), groups / std::max<int64_t>(rows, 1)));
     const int64_t each = (pieces + parts - 1) / parts;
     return {(int)((pieces + each - 1) / each), (int)std::min(each * piece, vocab)};
 }
@@ -499,7 +502,7 @@ using namespace imu;
 
 extern "C" int imunpack_logprobs_workspace(int64_t rows, int64_t vocab, int64_t count, int64_t top, int dtype, size_t *bytes) {
     if (!logprob_sizes(rows, vocab, count, top, dtype) || !bytes) return IMUNPACK_EINVAL;
-    const int64_t parts = parts_of(rows, vocab, dtype).parts;
+    const int64_t parts = parts_of(rows, vocab, dtype, kForwardGroups).parts;
     *bytes = parts == 1 ? 0 : (size_t)rows * (size_t)parts * ((size_t)top * sizeof(uint64_t) + 3 * sizeof(float));
     return IMUNPACK_OK;
 }
@@ -514,7 +517,7 @@ extern "C" int imunpack_logprobs(const void *logits, int64_t ldl, int64_t rows, 
     if (need && (!workspace || ((uintptr_t)workspace & 15))) return IMUNPACK_EINVAL;
     if (workspace_bytes < need) return IMUNPACK_ESMALL;
     const int64_t size = dtype == IMUNPACK_F32 ? 4 : 2;
-    const Parts p = parts_of(rows, vocab, dtype);
+    const Parts p = parts_of(rows, vocab, dtype, kForwardGroups);
     const bool once = rows * vocab * size >= kLastLevelCache;
     const hipStream_t st = (hipStream_t)stream;
     for (int64_t r = 0; r < rows; r += kLogprobRows) {  // (one launch wherever a row has parts)
@@ -544,7 +547,7 @@ extern "C" int imunpack_logprobs_backward(const void *logits, int64_t ldl, int64
     if (!logits || !stats || !gl || (g_logp && count && !tokens) || (g_entropy && !entropy) || (g_top && top && !top_index) || (gl == logits && ldg != ldl)) return IMUNPACK_EINVAL;
     const int64_t size = dtype == IMUNPACK_F32 ? 4 : 2;
     auto at = [](auto *p, int64_t k) { return p ? p + k : p; };
-    const Parts p = parts_of(rows, vocab, dtype);
+    const Parts p = parts_of(rows, vocab, dtype, kBackwardGroups);
     const bool once = 2 * rows * vocab * size >= kLastLevelCache * 3 / 4;
     for (int64_t r = 0; r < rows; r += kLogprobRows) {
         const LogprobBackArgs a = {(const char *)logits + r * ldl * size, at(tokens, r * count), at(top_index, r * top), stats + 2 * r, at(entropy, r), count ? at(g_logp, r * count) : nullptr,
