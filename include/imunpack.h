@@ -451,6 +451,28 @@ int imunpack_block8_quantize(const void *x, int64_t ldx, int64_t rows, int64_t c
 int imunpack_block8_turn(const void *codes, int64_t ldc, const void *scales, int64_t lds, int64_t rows, int64_t cols, int format,
                          void *turned, int64_t ldt, void *turned_scales, int64_t ldts, imunpack_stream_t stream);
 
+/* Up to four tensors by one launch, with the results of the two calls above for each: `imunpack_block8_quantize` where x_scales is NULL, otherwise
+ * `imunpack_block8_turn` of the codes x with these scales (dtype is not looked at then, codes and square are 0).  All arguments are checked before anything is launched.
+ * Errors: EINVAL (count outside [1, 4], and as above for each tensor); EHIP. */
+#define IMUNPACK_BLOCK8_MANY 4
+typedef struct imunpack_block8_job {
+    const void *x;
+    int64_t ldx;
+    const void *x_scales;
+    int64_t ldxs;
+    int64_t rows, cols;
+    int dtype, square;
+    void *codes;
+    int64_t ldc;
+    void *scales;
+    int64_t lds;
+    void *turned;
+    int64_t ldt;
+    void *turned_scales;
+    int64_t ldts;
+} imunpack_block8_job;
+int imunpack_block8_many(int count, const imunpack_block8_job *jobs, int format, imunpack_stream_t stream);
+
 /* out (device, dtype, ldo elements from row to row) = the values of a tensor in 8 bits (bfloat16 holds them exactly, but for magnitudes from 2^128 on or below
  * 2^-133).  Errors as above. */
 int imunpack_block8_values(const void *codes, int64_t ldc, const void *scales, int64_t lds, int64_t rows, int64_t cols, int format,

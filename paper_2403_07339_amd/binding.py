@@ -36,7 +36,7 @@ EXPORTS = [
     "imunpack_xent_workspace", "imunpack_xent", "imunpack_xent_rescale",
     "imunpack_block8_quantize", "imunpack_block8_turn", "imunpack_block8_values", "imunpack_block8_gemm_workspace", "imunpack_block8_gemm",
     "imunpack_act8", "imunpack_act8_backward", "imunpack_logprobs_workspace", "imunpack_logprobs", "imunpack_logprobs_backward",
-    "imunpack_column_sums_workspace", "imunpack_column_sums",
+    "imunpack_column_sums_workspace", "imunpack_column_sums", "imunpack_block8_many",
 ]
 DIGITS_INT8, DIGITS_FP6 = 0, 1
 
@@ -591,7 +591,7 @@ _tensors.bind(ImunpackError, *[C.cast(getattr(_lib, _name), _vp).value for _name
     "imunpack_rmsnorm", "imunpack_rmsnorm_quantize", "imunpack_rmsnorm_backward_workspace", "imunpack_rmsnorm_backward", "imunpack_adamw",
     "imunpack_xent_workspace", "imunpack_xent", "imunpack_xent_rescale", "imunpack_block8_quantize", "imunpack_block8_turn", "imunpack_block8_values",
     "imunpack_block8_gemm_workspace", "imunpack_block8_gemm", "imunpack_act8", "imunpack_act8_backward", "imunpack_logprobs_workspace", "imunpack_logprobs",
-    "imunpack_logprobs_backward", "imunpack_column_sums_workspace", "imunpack_column_sums")])
+    "imunpack_logprobs_backward", "imunpack_column_sums_workspace", "imunpack_column_sums", "imunpack_block8_many")])
 
 
 def imunpack_rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None):
@@ -712,6 +712,20 @@ def imunpack_block8_turn(x: Blocks8) -> Blocks8:
     """x^T in 8 bits, in blocks along x's columns (rows of x), from x in 8 bits."""
     codes, scales = _tensors.block8_turn(x.codes, x.scales, x.cols, _stream())
     return Blocks8(codes, scales, x.rows)
+
+
+def imunpack_block8_many(*wanted, format: str = "e4m3") -> list:
+    """Up to four tensors by one launch: each (x, square, lying, turned) as imunpack_block8_quantize takes them, or a Blocks8 to be turned.  Returns (as it lies, turned) of each."""
+    if format not in FORMATS:
+        raise ValueError("format is e4m3 or e5m2")
+    jobs = tuple((w.codes, w.scales, w.cols, False, False, True) if isinstance(w, Blocks8) else (w[0], None, 0, *w[1:]) for w in wanted)
+    got = _tensors.block8_many(jobs, format == "e5m2", _stream())
+    out = []
+    for k, w in enumerate(wanted):
+        q, qs, t, ts = got[4 * k: 4 * k + 4]
+        cols, rows = (w.cols, w.rows) if isinstance(w, Blocks8) else (w[0].shape[-1], w[0].numel() // w[0].shape[-1])
+        out.append((Blocks8(q, qs, cols) if q is not None else None, Blocks8(t, ts, rows) if t is not None else None))
+    return out
 
 
 def imunpack_block8_values(x: Blocks8, dtype: torch.dtype = torch.float32) -> torch.Tensor:

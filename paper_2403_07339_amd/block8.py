@@ -38,6 +38,14 @@ def _unpack(tensors, cols) -> list:
     return [imu.Blocks8(c, s, n) if c is not None else None for c, s, n in zip(tensors[::2], tensors[1::2], cols)]
 
 
+def _both_ways(g: torch.Tensor, lying: bool, x) -> tuple:
+    """A gradient for the products that take it: as it lies, and turned with x (None: not)."""
+    if x is not None:
+        (gq, gt), (_, xt) = imu.imunpack_block8_many((g, False, lying, True), x)
+        return gq, gt, xt
+    return imu.imunpack_block8_quantize(g)[0] if lying else None, None, None
+
+
 # (What an autograd function is told of its inputs does not know no_grad: `train` says whether anything is kept.)
 def _empty_backward(ctx, gy, shapes):
     """Gradients of a call without rows."""
@@ -51,8 +59,7 @@ class _LinearFunction(torch.autograd.Function):
         if x.numel() == 0:
             return x.new_empty(*x.shape[:-1], weight.shape[0])
         need_x, need_w = (train and n for n in ctx.needs_input_grad[:2])
-        xq, _ = imu.imunpack_block8_quantize(_rows(x))
-        wq, turned = imu.imunpack_block8_quantize(weight, square=True, turned=need_x)
+        (xq, _), (wq, turned) = imu.imunpack_block8_many((_rows(x), False, True, False), (weight, True, True, need_x))
         y = imu.imunpack_block8_gemm(xq, wq, x.dtype, _bias(bias))
         ctx.save_for_backward(*_pack(xq if need_w else None, turned))
         return y.view(*x.shape[:-1], weight.shape[0])
@@ -67,12 +74,11 @@ class _LinearFunction(torch.autograd.Function):
         xq, wt = _unpack(ctx.saved_tensors, (w_shape[1], w_shape[0]))
         g = _rows(gy)
         gx = gw = None
-        if need_x or need_w:
-            gq, gt = imu.imunpack_block8_quantize(g, turned=need_w, lying=need_x)
+        gq, gt, xt = _both_ways(g, need_x, xq if need_w else None)
         if need_x:
             gx = imu.imunpack_block8_gemm(gq, wt, dtype).view(x_shape)
         if need_w:
-            gw = imu.imunpack_block8_gemm(gt, imu.imunpack_block8_turn(xq), w_dtype)
+            gw = imu.imunpack_block8_gemm(gt, xt, w_dtype)
         return gx, gw, imu.imunpack_column_sums(g).to(b_dtype) if need_b else None, None
 
 
@@ -85,12 +91,10 @@ class _MLPFunction(torch.autograd.Function):
             return x.new_empty(*x.shape[:-1], w2.shape[0])
         need_x, need_w1, need_b1, need_w2 = (train and n for n in ctx.needs_input_grad[:4])
         first = need_x or need_w1 or need_b1
-        xq, _ = imu.imunpack_block8_quantize(_rows(x))
-        wq, t1 = imu.imunpack_block8_quantize(w1, square=True, turned=need_x)
+        (xq, _), (wq, t1), (wq2, t2) = imu.imunpack_block8_many((_rows(x), False, True, False), (w1, True, True, need_x), (w2, True, True, first))
         u = imu.imunpack_block8_gemm(xq, wq, x.dtype, _bias(b1))
         _, aq, kept = imu.imunpack_act8(u, act, gated, quantize=True, keep=first, want_y=False)
-        wq, t2 = imu.imunpack_block8_quantize(w2, square=True, turned=first)
-        y = imu.imunpack_block8_gemm(aq, wq, x.dtype, _bias(b2))
+        y = imu.imunpack_block8_gemm(aq, wq2, x.dtype, _bias(b2))
         ctx.save_for_backward(*_pack(xq if need_w1 else None, t1, aq if need_w2 else None, t2, *(kept or ())))
         return y.view(*x.shape[:-1], w2.shape[0])
 
@@ -107,18 +111,16 @@ class _MLPFunction(torch.autograd.Function):
         g = _rows(gy)
         first = need_x or need_w1 or need_b1
         gx = gw1 = gb1 = gw2 = None
-        if first or need_w2:
-            gq, gt = imu.imunpack_block8_quantize(g, turned=need_w2, lying=first)
+        gq, gt, at = _both_ways(g, first, aq if need_w2 else None)
         if need_w2:
-            gw2 = imu.imunpack_block8_gemm(gt, imu.imunpack_block8_turn(aq), w2_dtype)
+            gw2 = imu.imunpack_block8_gemm(gt, at, w2_dtype)
         if first:
             gu = imu.imunpack_act8_backward(imu.imunpack_block8_gemm(gq, t2, dtype), tuple(kept), act, gated)
-            if need_x or need_w1:
-                gq, gt = imu.imunpack_block8_quantize(gu, turned=need_w1, lying=need_x)
+            gq, gt, xt = _both_ways(gu, need_x, xq if need_w1 else None)
             if need_x:
                 gx = imu.imunpack_block8_gemm(gq, t1, dtype).view(x_shape)
             if need_w1:
-                gw1 = imu.imunpack_block8_gemm(gt, imu.imunpack_block8_turn(xq), w1_dtype)
+                gw1 = imu.imunpack_block8_gemm(gt, xt, w1_dtype)
             if need_b1:
                 gb1 = imu.imunpack_column_sums(gu).to(b1_dtype)
         return gx, gw1, gb1, gw2, imu.imunpack_column_sums(g).to(b2_dtype) if need_b2 else None, None, None, None

@@ -35,6 +35,7 @@ decltype(&imunpack_act8_backward) g_act8_backward = nullptr;
 decltype(&imunpack_logprobs_workspace) g_logprobs_workspace = nullptr;
 decltype(&imunpack_logprobs) g_logprobs = nullptr;
 decltype(&imunpack_logprobs_backward) g_logprobs_backward = nullptr;
+decltype(&imunpack_block8_many) g_block8_many = nullptr;
 decltype(&imunpack_column_sums_workspace) g_column_sums_workspace = nullptr;
 decltype(&imunpack_column_sums) g_column_sums = nullptr;
 
@@ -374,6 +375,51 @@ PyObject *block8_turn(PyObject *const *a) {  // codes, scales, cols, stream -> c
     return wrapped<2>({t.codes, t.scales});
 }
 
+PyObject *block8_many(PyObject *const *a) {  // jobs (tuples of x or codes, scales or None, cols of codes, square, lying, turned), e5m2, stream -> codes, scales, turned codes, turned scales of each
+    need(PyTuple_Check(a[0]) && PyTuple_GET_SIZE(a[0]) >= 1 && PyTuple_GET_SIZE(a[0]) <= IMUNPACK_BLOCK8_MANY, "block8: one to four tensors at a time");
+    const int count = (int)PyTuple_GET_SIZE(a[0]), format = truth(a[1]) ? IMUNPACK_E5M2 : IMUNPACK_E4M3;
+    const at::ScalarType code = format == IMUNPACK_E5M2 ? at::kFloat8_e5m2 : at::kFloat8_e4m3fn;
+    imunpack_block8_job jobs[IMUNPACK_BLOCK8_MANY] = {};
+    Eight q[IMUNPACK_BLOCK8_MANY], t[IMUNPACK_BLOCK8_MANY], from[IMUNPACK_BLOCK8_MANY];
+    Rows r[IMUNPACK_BLOCK8_MANY];
+    at::Tensor first;
+    for (int k = 0; k < count; ++k) {
+        PyObject *const job = PyTuple_GET_ITEM(a[0], k);
+        need(PyTuple_Check(job) && PyTuple_GET_SIZE(job) == 6, "block8: a tensor comes with how it is wanted");
+        PyObject *const *p = ((PyTupleObject *)job)->ob_item;
+        imunpack_block8_job &j = jobs[k];
+        const at::Tensor &x = tensor(p[0], "block8: x");
+        if (k == 0) first = x;
+        need(beside(x, first), "block8: tensors of different devices");
+        const bool lying = truth(p[4]), turned = truth(p[5]);
+        if (p[1] != Py_None) {
+            from[k] = eight(p[0], p[1], p[2], "block8: x");
+            need(from[k].format == format && turned && !lying, "block8: a tensor in 8 bits is turned, in its own format");
+            j.x = from[k].c(), j.ldx = from[k].ldc, j.x_scales = from[k].s(), j.ldxs = from[k].lds, j.rows = from[k].rows(), j.cols = from[k].cols;
+        } else {
+            j.dtype = type_of(x, "block8: x");
+            need(x.is_cuda() && x.dim() >= 1 && x.size(-1) >= 1 && (lying || turned), "block8: x is a device tensor with columns, wanted as it lies, turned or both");
+            j.cols = x.size(-1), j.rows = rows_of(x, j.cols), j.square = truth(p[3]);
+            r[k] = spread(x, j.cols);
+            j.x = r[k].p, j.ldx = r[k].pitch;
+        }
+        if (k == 0) need_current(x.device());
+        if (lying) {
+            q[k] = new_eight(j.rows, j.cols, code, x);
+            j.codes = q[k].c(), j.ldc = q[k].ldc, j.scales = q[k].s(), j.lds = q[k].lds;
+        }
+        if (turned) {
+            need(j.rows >= 1, "block8: a tensor without rows cannot be turned");
+            t[k] = new_eight(j.cols, j.rows, code, x);
+            j.turned = t[k].c(), j.ldt = t[k].ldc, j.turned_scales = t[k].s(), j.ldts = t[k].lds;
+        }
+    }
+    check(g_block8_many(count, jobs, format, address(a[2])), "imunpack_block8_many");
+    std::array<at::Tensor, 4 * IMUNPACK_BLOCK8_MANY> all;
+    for (int k = 0; k < count; ++k) all[4 * k] = q[k].codes, all[4 * k + 1] = q[k].scales, all[4 * k + 2] = t[k].codes, all[4 * k + 3] = t[k].scales;
+    return wrapped<4 * IMUNPACK_BLOCK8_MANY>(all);
+}
+
 PyObject *block8_values(PyObject *const *a) {  // codes, scales, cols, bf16, stream -> values
     const Eight q = eight(a[0], a[1], a[2], "block8: x");
     need_current(q.codes.device());
@@ -542,6 +588,7 @@ PyObject *bind(PyObject *const *a) {  // error class, then the addresses of the 
     g_logprobs_backward = (decltype(g_logprobs_backward))address(a[18]);
     g_column_sums_workspace = (decltype(g_column_sums_workspace))address(a[19]);
     g_column_sums = (decltype(g_column_sums))address(a[20]);
+    g_block8_many = (decltype(g_block8_many))address(a[21]);
     Py_RETURN_NONE;
 }
 
@@ -562,12 +609,12 @@ template <PyObject *(*F)(PyObject *const *), Py_ssize_t N>
 PyMethodDef method(const char *name) {
     return {name, (PyCFunction)(void (*)(void))entry<F, N>, METH_FASTCALL, nullptr};
 }
-PyMethodDef g_methods[] = {method<bind, 21>("bind"), method<rmsnorm, 5>("rmsnorm"), method<rmsnorm_quantize, 7>("rmsnorm_quantize"),
+PyMethodDef g_methods[] = {method<bind, 22>("bind"), method<rmsnorm, 5>("rmsnorm"), method<rmsnorm_quantize, 7>("rmsnorm_quantize"),
                            method<rmsnorm_backward, 8>("rmsnorm_backward"), method<adamw, 15>("adamw"),
                            method<xent, 10>("xent"), method<xent_rescale, 7>("xent_rescale"),
                            method<block8_quantize, 6>("block8_quantize"), method<block8_turn, 4>("block8_turn"), method<block8_values, 5>("block8_values"),
                            method<block8_gemm, 9>("block8_gemm"), method<act8, 7>("act8"), method<act8_backward, 8>("act8_backward"), method<logprobs, 6>("logprobs"),
-                           method<logprobs_backward, 10>("logprobs_backward"), method<column_sums, 2>("column_sums"), {nullptr, nullptr, 0, nullptr}};
+                           method<logprobs_backward, 10>("logprobs_backward"), method<column_sums, 2>("column_sums"), method<block8_many, 3>("block8_many"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_tensors", "Argument marshalling of the calls whose host time counts.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 }  // namespace
 

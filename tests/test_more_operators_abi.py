@@ -114,3 +114,26 @@ def test_column_sums(lib):
     assert f(100, 40, 0, C.byref(bytes_)) == 0 and bytes_.value == 0
     assert f(5000, 40, 0, C.byref(bytes_)) == 0 and call(bytes=bytes_.value - 1) == ESMALL
     assert f(5000, 40, 0, None) == EINVAL
+
+
+class Job(C.Structure):
+    _fields_ = [("x", vp), ("ldx", i64), ("xs", vp), ("ldxs", i64), ("rows", i64), ("cols", i64), ("dtype", i32), ("square", i32), ("q", vp), ("ldq", i64), ("s", vp), ("lds", i64), ("t", vp), ("ldt", i64),
+                ("ts", vp), ("ldts", i64)]
+
+
+def test_several_tensors(lib):
+    f = lib.imunpack_block8_many
+    f.restype, f.argtypes = i32, [i32, C.POINTER(Job), i32, vp]
+    plain = dict(x=FAKE, ldx=200, rows=300, cols=200, dtype=0, square=0, q=FAKE, ldq=256, s=FAKE, lds=16, t=FAKE, ldt=384, ts=FAKE, ldts=16)
+    turn = dict(x=FAKE, ldx=256, xs=FAKE, ldxs=16, rows=300, cols=200, t=FAKE, ldt=384, ts=FAKE, ldts=16)
+    def call(first, second, count=2, fmt=0):
+        jobs = (Job * 5)(Job(**first), Job(**second))
+        return f(count, jobs, fmt, None)
+    bads = [{**plain, **c} for c in (dict(x=None), dict(ldx=199), dict(rows=-1), dict(rows=(1 << 31) + 1), dict(rows=(1 << 24) + 1), dict(cols=0), dict(cols=(1 << 24) + 1), dict(dtype=2),
+                                     dict(q=None, t=None), dict(q=FAKE + 8), dict(s=None), dict(ldq=255), dict(lds=1), dict(lds=17), dict(t=FAKE + 1), dict(ldt=256), dict(ts=None), dict(ldts=24))]
+    bads += [{**turn, **c} for c in (dict(x=None), dict(ldx=200), dict(ldx=255), dict(xs=FAKE + 8), dict(ldxs=1), dict(rows=-1), dict(rows=(1 << 24) + 1), dict(cols=0), dict(t=None), dict(ldt=256),
+                                     dict(q=FAKE, ldq=256, s=FAKE, lds=16), dict(square=1))]
+    for bad in bads:
+        assert call(plain, bad) == EINVAL and call(bad, turn) == EINVAL, bad
+    assert call(plain, turn, count=0) == EINVAL and call(plain, turn, count=5) == EINVAL and call(plain, turn, fmt=2) == EINVAL and f(1, None, 0, None) == EINVAL
+    assert call({**plain, "rows": 0}, {**turn, "rows": 0}) == 0
