@@ -479,7 +479,8 @@ int imunpack_block8_values(const void *codes, int64_t ldc, const void *scales, i
                            void *out, int64_t ldo, int dtype, imunpack_stream_t stream);
 
 /* out = A B^T (+ bias, fp32, one per column; NULL: none) for A: m x k and B: n x k in 8 bits, out: device, dtype, row stride ldo >= n elements.
- * fp32 results: products exact (of bfloat16 numbers, which codes times their power of two are), sums in fp32.
+ * fp32 results: products exact, or within 2^-126, and sums in fp32.  (Codes times their power of two are taken as bfloat16 numbers; where they are none, below 2^-133 or from 2^128 on, and it counts, the
+ * 32 to 128 rows and columns around such a block take another way, several times as long.)
  * bfloat16 results: the matrix instruction takes codes and bytes as they are, at twice the rate.  It adds eight products at a time and cuts each of them below 2^-13 of
  * the largest's power of two before sums in fp32: a result is off by up to 2^-10 of the sum of its products' magnitudes, by 2^-16 of its size for random operands,
  * and then rounded to bfloat16.  Up to 16 rows of A both kinds may take other kernels with the same bounds.
