@@ -429,7 +429,7 @@ int imunpack_xent_rescale(const float *grad, void *gx, int64_t nx, void *gw, int
  *     e = the smallest whole number >= -127 with max |x| over the block <= top 2^e   (0 for a block of zeros),   byte = e + 127,
  *     code = x 2^-e, rounded to nearest with ties to even,                       value = code 2^e.
  * top is 448 (E4M3: four exponent bits, three of fraction, no infinity) or 57344 (E5M2).  A value is within 2^-4 (E4M3) or 2^-3 (E5M2) of x relative to x, or
- * within 2^-10 2^e (2^-17 2^e).  Infinities and NaN do not count for max |x|; they become NaN codes (E5M2: infinity stays).
+ * within 2^-10 2^e (2^-17 2^e); what rounds to 2^128 is infinite where it becomes fp32 or bfloat16 again.  Infinities and NaN do not count for max |x|; they become NaN codes (E5M2: infinity stays).
  * "Square" blocks are 128 rows x 128 columns: their byte stands in each of their rows.
  * codes: device, row r at codes + r ldc, ldc bytes at least 128 ceil(cols / 128): the codes behind a row's end, up to a whole block, are
  * zeros (the calls that write codes see to that, the product counts on it).  scales: device, the byte of row r and block j at
@@ -447,7 +447,7 @@ int imunpack_block8_quantize(const void *x, int64_t ldx, int64_t rows, int64_t c
                              void *turned, int64_t ldt, void *turned_scales, int64_t ldts, imunpack_stream_t stream);
 
 /* The same of a tensor that is in 8 bits already (rows x cols, any blocks): its values, turned, in blocks along its columns.  A value of e4m3 or e5m2
- * under another power of two is the same value, unless it falls below that block's smallest codes and is rounded to those. */
+ * under another power of two is the same value, unless it falls below that block's smallest codes and is rounded to those.  (From 2^129 on, which no call here writes, values count as infinite.) */
 int imunpack_block8_turn(const void *codes, int64_t ldc, const void *scales, int64_t lds, int64_t rows, int64_t cols, int format,
                          void *turned, int64_t ldt, void *turned_scales, int64_t ldts, imunpack_stream_t stream);
 

@@ -31,10 +31,11 @@ inline bool blocks8_fit(const Blocks8 &t, int64_t cols) {
 #if defined(__HIPCC__)
 // The byte of a block whose largest finite magnitude has these bits (not negative).  One bit pattern decides: with E the exponent's field,
 // x <= 1.75 2^(8 + e) is e >= E - 127 - 8, or one more where the fraction is above 0.75.
-template <int FORMAT>
+// UP: the bits are those of the magnitude times 2^-UP.
+template <int FORMAT, int UP = 0>
 __device__ __forceinline__ int block8_byte(int bits) {
     constexpr int up = FORMAT == IMUNPACK_E4M3 ? 8 : 15;
-    const int e = (bits >> 23) - up + ((bits & 0x7fffff) > 0x600000);
+    const int e = (bits >> 23) - up + UP + ((bits & 0x7fffff) > 0x600000);
     return bits == 0 ? 127 : max(e, 0);
 }
 __device__ __forceinline__ float block8_scale(int byte) { return __int_as_float(byte ? byte << 23 : 0x400000); }  // 2^(byte - 127)

@@ -77,6 +77,8 @@ template <class T, int FORMAT>
 __device__ __forceinline__ void tile_into(const TileArgs &a, unsigned which, TileShared &shared) {
     constexpr bool kCodes = std::is_same<T, uint8_t>::value;
     constexpr int R = 4;
+    // (Codes are held as half their values: binary32's largest rounds up to a code of 2^128.)
+    constexpr int kHalved = kCodes ? 1 : 0;
     auto &tile = shared.tile;
     auto &tops = shared.tops;
     auto &columns = shared.columns;
@@ -99,7 +101,7 @@ __device__ __forceinline__ void tile_into(const TileArgs &a, unsigned which, Til
         for (int i = 0; i < R; ++i) {
             if constexpr (kCodes) {
                 const int byte = row0 + i < a.rows ? a.xs[(row0 + i) * a.ldxs + kb] : 127;
-                decode8<FORMAT>(__builtin_bit_cast(uint2, in[i]), block8_scale(byte), x[i]);
+                decode8<FORMAT>(__builtin_bit_cast(uint2, in[i]), block8_scale(byte) * 0.5f, x[i]);
             } else {
                 to_floats<T, 8>(in[i], x[i]);
             }
@@ -141,7 +143,7 @@ __device__ __forceinline__ void tile_into(const TileArgs &a, unsigned which, Til
             for (int j = 0; j < 8; ++j) top[j] = all;
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) bytes[j] = block8_byte<FORMAT>(top[j]);
+        for (int j = 0; j < 8; ++j) bytes[j] = block8_byte<FORMAT, kHalved>(top[j]);
     }
     if constexpr (!kCodes) {
         if (a.codes) {
@@ -158,8 +160,14 @@ __device__ __forceinline__ void tile_into(const TileArgs &a, unsigned which, Til
     if (!a.turned) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float inverse = block8_inverse(bytes[j]);
-        *reinterpret_cast<uint32_t *>(tile + turned_at(l16 * 8 + j, wave * 4 + group)) = encode4<FORMAT>(x[0][j] * inverse, x[1][j] * inverse, x[2][j] * inverse, x[3][j] * inverse);
+        uint32_t &to = *reinterpret_cast<uint32_t *>(tile + turned_at(l16 * 8 + j, wave * 4 + group));
+        if constexpr (kCodes) {  // (a factor of 2^128, of half a value in a block of byte 0, is no number of binary32)
+            const int up = 127 + kHalved - bytes[j];
+            to = encode4<FORMAT>(__builtin_ldexpf(x[0][j], up), __builtin_ldexpf(x[1][j], up), __builtin_ldexpf(x[2][j], up), __builtin_ldexpf(x[3][j], up));
+        } else {
+            const float inverse = block8_inverse(bytes[j]);
+            to = encode4<FORMAT>(x[0][j] * inverse, x[1][j] * inverse, x[2][j] * inverse, x[3][j] * inverse);
+        }
     }
     if (threadIdx.x < 16)
         *reinterpret_cast<uint2 *>(columns + l16 * 8) = make_uint2(bytes[0] | bytes[1] << 8 | bytes[2] << 16 | (unsigned)bytes[3] << 24, bytes[4] | bytes[5] << 8 | bytes[6] << 16 | (unsigned)bytes[7] << 24);

@@ -1,4 +1,4 @@
-"""Products of tensors in 8 bits whose powers of two lie at the ends of a byte, in every kernel: codes times such a power are no numbers of bfloat16 (which ends at 2^-133 and below 2^128), and their
+"""Tensors in 8 bits whose powers of two lie at the ends of a byte: turned, and in products by every kernel: codes times such a power are no numbers of bfloat16 (which ends at 2^-133 and below 2^128), and their
 products are the contract's all the same.
 
 Tolerances.  One product alone is rounded once, 2^-24 (2^-8) of itself, which is compared as equality with the exact value rounded; what an operand loses below 2^-133 counts at most 2^-126.  Sums of K products:
@@ -104,3 +104,23 @@ def test_blocks_at_the_ends_among_others(imu, m, n, k, fa, fb, dtype):
     for behind in (0, 255):
         other = imu.imunpack_block8_gemm(blocks(imu, a.view(torch.uint8), sa, fa, behind), blocks(imu, b.view(torch.uint8), sb, fb, behind), dtype)
         assert torch.equal(other.view(torch.uint8), got.view(torch.uint8))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_the_largest_values_turned(imu, fmt):
+    """Codes of what binary32 has next to 2^128 stand for 2^128, which binary32 has not: turned they are the same values.  No tolerance."""
+    from test_gpu_block8 import check_codes, definition
+    g = torch.Generator().manual_seed(7)
+    x = torch.randn(200, 300, generator=g) * torch.exp2(torch.randint(-140, 120, (1, 300), generator=g).float())
+    most = torch.finfo(torch.float32).max
+    x[3, 7], x[150, 7], x[5, 200], x[6, 200], x[199, 299], x[8] = most, -most / 3, 1.98 * 2.0 ** 127, 2.0 ** -100, 1.75 * 2.0 ** 127, most
+    want, e = definition(x, fmt)
+    assert float(want.abs().max()) == 2.0 ** 128
+    q, t = imu.imunpack_block8_quantize(x.cuda(), fmt, turned=True)
+    check_codes(q, want, e, fmt, 300)
+    check_codes(t, *definition(x.t(), fmt), fmt, 200)
+    again = definition(want.t(), fmt)
+    check_codes(imu.imunpack_block8_turn(q), *again, fmt, 200)
+    (_, many), (_, alone) = imu.imunpack_block8_many(q, (x.cuda(), False, False, True), format=fmt)
+    check_codes(many, *again, fmt, 200)
+    check_codes(alone, *definition(x.t(), fmt), fmt, 200)
