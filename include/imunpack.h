@@ -500,6 +500,7 @@ int imunpack_block8_gemm(const void *a, int64_t lda, const void *a_scales, int64
  * next product; y (may then be NULL) receives those values.  kept, kept_scales (NULL: not, for serving): u in 8 bits (E4M3); gated: its first cols columns,
  * and kept2, kept2_scales the others, pitches alike.
  * imunpack_act8_backward: with v the values that were kept,  gu = g f'(v);  gated:  gu = (g f'(v1) v2, g f(v1)), 2 cols columns.
+ * f is within (16 + u^2) 2^-24 (GELU) or 2^-20 (SiLU) of itself, or 2^-120, before it is rounded to dtype or codes.
  * rows == 0 is allowed.  Errors: EINVAL (null pointers, sizes as for imunpack_block8_quantize, pitches, alignments, unknown types or functions); EHIP. */
 enum { IMUNPACK_GELU = 0, IMUNPACK_SILU = 1 };
 int imunpack_act8(const void *u, int64_t ldu, int64_t rows, int64_t cols, int dtype, int act, int gated, void *y, int64_t ldy,

@@ -236,17 +236,31 @@ __global__ __launch_bounds__(256) void block8_values_kernel(const ValuesArgs a) 
 
 // ---- activation functions -------------------------------------------------------------------------------------------------------
 // f(u) and f'(u).  GELU: u Phi(u), Phi + u phi; SiLU: u sig(u), sig (1 + u (1 - sig)).
+// Phi(-x) = phi(x) R(x) for x >= 0 with Mills' ratio R = (1 - Phi) / phi, and 1 - that above 0: as (1 + erf) / 2 it cancels where u is negative (at -4 1e-3 of the value was wrong, at -6 nothing
+// right, and a block of such inputs has a power of two of its own).  R(x) = t P(t), t = 1 / (1 + 0.3 x), with the P of degree 7 whose largest relative error up to x = 14.5, where phi leaves binary32, is the
+// least: 1.6e-7, in binary32 8 2^-24.  phi's exponent leaves it off by u^2 2^-24 more; below 2^-126 it is 0.  4096 x 11008 gated bfloat16, forward and
+// backward: 62 + 55 us; by erff 62 + 67, by erfcf 83 + 95.
+struct Normal {
+    float below, density;  // Phi(u), phi(u)
+};
+__device__ __forceinline__ Normal normal_of(float u) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, fabsf(u), 1.0f)), density = __builtin_amdgcn_exp2f(u * u * -0.72134752f) * 0.39894228f;
+    float p = 0.08879409f;
+    p = fmaf(p, t, -0.39143094f), p = fmaf(p, t, 0.51274735f), p = fmaf(p, t, -0.13042958f), p = fmaf(p, t, 0.32007563f), p = fmaf(p, t, 0.25110391f), p = fmaf(p, t, 0.30258045f), p = fmaf(p, t, 0.29987299f);
+    const float tail = density * (p * t);
+    return {u < 0.0f ? tail : 1.0f - tail, density};
+}
 template <int ACT>
 __device__ __forceinline__ float act_value(float u) {
-    if constexpr (ACT == IMUNPACK_GELU) return u * (0.5f * (1.0f + erff(u * 0.70710678f)));
+    if constexpr (ACT == IMUNPACK_GELU) return u * normal_of(u).below;
     else return u / (1.0f + expf(-u));
 }
 template <int ACT>
 __device__ __forceinline__ float act_slope(float u, float &value) {
     if constexpr (ACT == IMUNPACK_GELU) {
-        const float phi = 0.5f * (1.0f + erff(u * 0.70710678f));
-        value = u * phi;
-        return fmaf(u, expf(-0.5f * u * u) * 0.39894228f, phi);
+        const Normal n = normal_of(u);
+        value = u * n.below;
+        return fmaf(u, n.density, n.below);
     } else {
         const float sig = 1.0f / (1.0f + expf(-u));
         value = u * sig;
