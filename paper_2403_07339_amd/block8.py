@@ -46,12 +46,12 @@ def _both_ways(g: torch.Tensor, lying: bool, x) -> tuple:
     return imu.imunpack_block8_quantize(g)[0] if lying else None, None, None
 
 
-# (What an autograd function is told of its inputs does not know no_grad: `train` says whether anything is kept.)
 def _empty_backward(ctx, gy, shapes):
     """Gradients of a call without rows."""
     return [torch.zeros(shape, dtype=dtype, device=gy.device) if needed else None for (shape, dtype), needed in zip(shapes, ctx.needs_input_grad)]
 
 
+# (What an autograd function is told of its inputs does not know no_grad: `train` says whether anything is kept.)
 class _LinearFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, train):
@@ -158,18 +158,42 @@ class Block8Linear(torch.nn.Module):
         return FrozenLinear(self.weight, self.bias)
 
 
+class _FrozenFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, layer):
+        w = layer.weight
+        ctx.like = [(x.shape, x.dtype), (None, None)]
+        ctx.cols = w.cols
+        ctx.save_for_backward(w.codes, w.scales)
+        return layer._product(x)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, gy):
+        if gy.numel() == 0:
+            return tuple(_empty_backward(ctx, gy, ctx.like))
+        shape, dtype = ctx.like[0]
+        turned = imu.imunpack_block8_turn(imu.Blocks8(*ctx.saved_tensors, ctx.cols))
+        return imu.imunpack_block8_gemm(imu.imunpack_block8_quantize(_rows(gy))[0], turned, dtype).view(shape), None
+
+
 class FrozenLinear:
-    """A linear layer for serving: its weights are brought to 8 bits once, by this constructor."""
+    """A linear layer for serving: its weights are brought to 8 bits once, by this constructor, and are no parameters.  An input that requires a gradient gets it,
+    Q(gy) Q(w), for which a backward pass turns the weights' codes (they are not kept both ways)."""
 
     @torch.no_grad()
     def __init__(self, weight: torch.Tensor, bias: torch.Tensor | None = None):
         self.weight, _ = imu.imunpack_block8_quantize(weight.detach(), square=True)
         self.bias = _bias(bias)
 
-    @torch.no_grad()
-    def __call__(self, x: torch.Tensor) -> torch.Tensor:
+    def _product(self, x: torch.Tensor) -> torch.Tensor:
         y = imu.imunpack_block8_gemm(imu.imunpack_block8_quantize(x)[0], self.weight, x.dtype, self.bias)
         return y.view(*x.shape[:-1], self.weight.rows)
+
+    def __call__(self, x: torch.Tensor) -> torch.Tensor:
+        if x.requires_grad and torch.is_grad_enabled():
+            return _FrozenFunction.apply(x, self)
+        return self._product(x)
 
 
 class Block8MLP(torch.nn.Module):
