@@ -584,6 +584,10 @@ int imunpack_diag_gemm_halves(const imunpack_plan_t *plan);
  * (B_eu holds them like any other).  Errors: EINVAL (no valid plan). */
 int imunpack_diag_list_columns(const imunpack_plan_t *plan);
 
+/* Which kernel imunpack_block8_gemm takes for these sizes (tests and benchmark reporting only; nothing is launched): *tile = 1, 2 or 4 for tiles of 64, 128 or 256 squared, 0 for the kernel of up to 16
+ * rows; *parts: into how many parts the contraction is cut.  Errors: EINVAL as for imunpack_block8_gemm_workspace. */
+int imunpack_diag_block8_cut(int64_t m, int64_t n, int64_t k, int dtype, int *tile, int *parts);
+
 /* Shader clock under the GEMM's own load (benchmark reporting only).  While `ticks` (device, two
  * elements, owned by the caller) is set, every fused imunpack_gemm launch of this process has its
  * first workgroup write ticks[0] = shader clock cycles and ticks[1] = ticks of the constant 100 MHz

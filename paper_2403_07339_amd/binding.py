@@ -36,7 +36,7 @@ EXPORTS = [
     "imunpack_xent_workspace", "imunpack_xent", "imunpack_xent_rescale",
     "imunpack_block8_quantize", "imunpack_block8_turn", "imunpack_block8_values", "imunpack_block8_gemm_workspace", "imunpack_block8_gemm",
     "imunpack_act8", "imunpack_act8_backward", "imunpack_logprobs_workspace", "imunpack_logprobs", "imunpack_logprobs_backward",
-    "imunpack_column_sums_workspace", "imunpack_column_sums", "imunpack_block8_many",
+    "imunpack_column_sums_workspace", "imunpack_column_sums", "imunpack_block8_many", "imunpack_diag_block8_cut",
 ]
 DIGITS_INT8, DIGITS_FP6 = 0, 1
 
@@ -68,6 +68,7 @@ _lib.imunpack_plan_keep_weights.argtypes = [_vp, _i32]
 _lib.imunpack_diag_gemm_parts.argtypes = [_vp]
 _lib.imunpack_diag_gemm_halves.argtypes = [_vp]
 _lib.imunpack_diag_list_columns.argtypes = [_vp]
+_lib.imunpack_diag_block8_cut.argtypes = [_i64, _i64, _i64, _i32, C.POINTER(_i32), C.POINTER(_i32)]
 _lib.imunpack_plan_weights_reused.argtypes = [_vp]
 _lib.imunpack_unpack.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp]
 _lib.imunpack_unpack_canonical.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp]
@@ -543,6 +544,14 @@ def imunpack_diag_copy(src: torch.Tensor, dst: torch.Tensor) -> int:
     assert nbytes == dst.numel() * dst.element_size()
     _check(_lib.imunpack_diag_copy(src.data_ptr(), dst.data_ptr(), nbytes, _stream()), "imunpack_diag_copy")
     return 2 * nbytes
+
+
+def imunpack_diag_block8_cut(m: int, n: int, k: int, dtype: torch.dtype = torch.float32) -> tuple[int, int]:
+    """(tile, parts) of the kernel that imunpack_block8_gemm takes for an m x n result in dtype over k places: tile 1, 2 or 4 for tiles of 64, 128 or 256, 0 for the
+    kernel of few rows; parts of the contraction.  For tests."""
+    tile, parts = _i32(), _i32()
+    _check(_lib.imunpack_diag_block8_cut(m, n, k, int(_is_bf16(dtype)), C.byref(tile), C.byref(parts)), "imunpack_diag_block8_cut")
+    return tile.value, parts.value
 
 
 def imunpack_diag_clock_probe(ticks: torch.Tensor | None) -> None:

@@ -582,10 +582,21 @@ using namespace imu;
 
 constexpr int64_t kGemmRows = 1 << 24;
 
+static bool gemm_sizes(int64_t m, int64_t n, int64_t k, int dtype) {
+    return m >= 0 && n >= 0 && k >= 1 && m <= kGemmRows && n <= kGemmRows && k <= kBlock8Cols && (dtype == IMUNPACK_F32 || dtype == IMUNPACK_BF16);
+}
+
 extern "C" int imunpack_block8_gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, size_t *bytes) {
-    if (m < 0 || n < 0 || k < 1 || m > kGemmRows || n > kGemmRows || k > kBlock8Cols || (dtype != IMUNPACK_F32 && dtype != IMUNPACK_BF16) || !bytes) return IMUNPACK_EINVAL;
+    if (!gemm_sizes(m, n, k, dtype) || !bytes) return IMUNPACK_EINVAL;
     const Cut c = cut_of(m, n, (k + kBlock8 - 1) / kBlock8, dtype == IMUNPACK_BF16);
     *bytes = c.parts > 1 ? (size_t)c.parts * (size_t)m * (size_t)n * sizeof(float) : 0;
+    return IMUNPACK_OK;
+}
+
+extern "C" int imunpack_diag_block8_cut(int64_t m, int64_t n, int64_t k, int dtype, int *tile, int *parts) {
+    if (!gemm_sizes(m, n, k, dtype) || !tile || !parts) return IMUNPACK_EINVAL;
+    const Cut c = cut_of(m, n, (k + kBlock8 - 1) / kBlock8, dtype == IMUNPACK_BF16);
+    *tile = c.tile, *parts = c.parts;
     return IMUNPACK_OK;
 }
 
