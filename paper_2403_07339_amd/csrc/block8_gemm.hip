@@ -535,7 +535,10 @@ struct Cut {
 // fetched B).  Parts cost a launch and their sums' way to memory and back.  Microseconds, bfloat16 / fp32 results, by tiles of 64, 128 and 256:
 //   1024^3 5.8, 7.4, 17.3 / 7.2, 12.1, 30.2;  2048^3 17.9, 12.6, 26.9 / 23.9, 22.6, 49.2;  256 x 4096 by 4096 12.7, 18.3, 39.4 / 18.4, 32.4, -;
 //   12608 x 768 by 768 20.2, 16.4, 18.7 / 25.2, 24.3, 31.2;  4096^3 -, -, 54 / -, -, 110;  768 x 12608 by 768 in 4 parts of 64 24.3 / 26.9, in 7 of 128 22.3 / 27.3, in 2 of 128 36 / 54;
-//   64 x 4096 by 4096 in 1, 2 and 4 parts of 64 12.1, 11.1, 10.4 / 16.9, 13.2, 11.4;  16 x 4096 by 11008 with few rows' kernel 18, in 1, 2 and 4 parts of 64 17.4, 14.0, 13.1
+//   64 x 4096 by 4096 in 1, 2 and 4 parts of 64 12.1, 11.1, 10.4 / 16.9, 13.2, 11.4
+// Up to 16 rows, the kernel for few rows and 1, 2, 4 and 8 parts of 64: 16 x 4096 by 5120 12.4 and 10.7, 9.5, 9.4, 10.6 / 12.6 and 17.1, 12.5, 11.2, 11.8;  by 11008 17.8 and 16.8, 13.5, 12.8, 15.8 /
+//   17.9 and 19.5, 16.1, 13.9, 16.4;  1 x 4096 by 11008 11.8 and 16.5, 13.1, 12.0, 14.5 / 11.8 and 19.4, 15.6, 13.3, 15.5;  16 x 4096 by 4096 7.3 and 10.7, 9.5, 8.8, 9.8 / 7.7 and 17.2, 12.5, 9.9, 10.7.
+// A CU takes its workgroups of 16 columns one after the other, and those behind the first (more than 4096 columns) have A's rows to wait for as well: 101 and 4 for each row, a block.
 static Cut cut_of(int64_t m, int64_t n, int64_t kt, bool native) {
     struct Cost {
         int tile, whole, fixed, alone, first, each;
@@ -543,7 +546,8 @@ static Cut cut_of(int64_t m, int64_t n, int64_t kt, bool native) {
     static const Cost costs[2][3] = {{{1, 4, 200, 420, 420, 310}, {2, 4, 500, 1020, 1020, 1020}, {4, 16, 10000, 2750, 2750, 2750}},
                                      {{1, 4, 200, 240, 370, 210}, {2, 4, 500, 550, 550, 550}, {4, 16, 8000, 1300, 1300, 1300}}};
     Cut best = {0, 1, (int)kt};
-    double least = m <= kFewRows ? (double)((n + 4095) / 4096) * (300.0 + 115.0 * (double)kt) : 1e30;
+    const double rounds = (double)((n + 4095) / 4096);
+    double least = m <= kFewRows ? rounds * 300.0 + (115.0 + (rounds - 1.0) * (101.0 + 4.0 * (double)m)) * (double)kt : 1e30;
     for (const Cost &c : costs[native]) {
         const int64_t edge = 64 * c.tile, down = (m + edge - 1) / edge, tiles = down * ((n + edge - 1) / edge);
         for (int64_t p = 1, last = 0; p <= 64 && (p == 1 || p * c.whole <= kt); ++p) {

@@ -51,3 +51,12 @@ def test_rows_of_logits_that_are_cut_need_their_workspace(lib):
     for dtype in (0, 1):
         assert ws(dtype=dtype) == 0 and size.value > 0
         assert call(dtype=dtype, bytes=size.value - 1) == ESMALL and call(dtype=dtype, ws=None) == EINVAL and call(dtype=dtype, ws=FAKE + 4) == EINVAL
+
+
+def test_few_rows_take_what_was_measured_as_the_faster(cut):
+    """(rows, columns, places; fp32 or bfloat16): the kernel for few rows where a CU has one workgroup of it or one row to multiply, parts where it has several and sixteen rows."""
+    for m, n, k, dtype in ((16, 4096, 4096, 0), (16, 4096, 4096, 1), (1, 11008, 4096, 0), (1, 8192, 4096, 0), (16, 2048, 4096, 1), (16, 1024, 1024, 0)):
+        assert cut(m=m, n=n, k=k, dtype=dtype) == (0, 1), (m, n, k, dtype)
+    for m, n, k, dtype in ((16, 11008, 4096, 0), (16, 11008, 4096, 1), (16, 8192, 4096, 0), (16, 8192, 4096, 1), (16, 11008, 11008, 0), (16, 5120, 4096, 0)):
+        tile, parts = cut(m=m, n=n, k=k, dtype=dtype)
+        assert tile == 1 and parts > 1, (m, n, k, dtype)
