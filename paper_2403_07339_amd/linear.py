@@ -11,6 +11,8 @@ Each is computed as in Sec. 2: both operands are RTN-quantised with the step alp
 int8 MFMA GEMM, recombination) and the result is scaled back (Eq. (quantized_gemm)) -- all inside
 ``imunpack_gemm_batched`` of the C ABI, which keeps the steps on the device.  The weights stay in fp32
 (master copy).  Integration only: every arithmetic step of the method runs in the HIP library.
+Not for capture in a graph: the products wait for the device (their plans' sizes come back to the host), and the bias's gradient is a library sum, which clears a counter that replays
+of a graph have found uncleared; ``block8`` has layers whose passes may be captured.
 """
 from __future__ import annotations
 
