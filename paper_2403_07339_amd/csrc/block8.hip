@@ -237,16 +237,17 @@ __global__ __launch_bounds__(256) void block8_values_kernel(const ValuesArgs a) 
 // ---- activation functions -------------------------------------------------------------------------------------------------------
 // f(u) and f'(u).  GELU: u Phi(u), Phi + u phi; SiLU: u sig(u), sig (1 + u (1 - sig)).
 // Phi(-x) = phi(x) R(x) for x >= 0 with Mills' ratio R = (1 - Phi) / phi, and 1 - that above 0: as (1 + erf) / 2 it cancels where u is negative (at -4 1e-3 of the value was wrong, at -6 nothing
-// right, and a block of such inputs has a power of two of its own).  R(x) = t P(t), t = 1 / (1 + 0.3 x), with the P of degree 7 whose largest relative error up to x = 14.5, where phi leaves binary32, is the
-// least: 1.6e-7, in binary32 8 2^-24.  phi's exponent leaves it off by u^2 2^-24 more; below 2^-126 it is 0.  4096 x 11008 gated bfloat16, forward and
-// backward: 62 + 55 us; by erff 62 + 67, by erfcf 83 + 95.
+// right, and a block of such inputs has a power of two of its own).  R(x) = t P(1 - t), t = 1 / (1 + 0.35 x), with the P of degree 8 whose largest relative error up to x = 14.5, where phi
+// leaves binary32, is the least: 3.2e-8, in binary32 with its roundings 7 2^-24 (a P(t) 7.5, most of it where x is small).  phi's exponent leaves it off by u^2 2^-24 more; below 2^-126 it is 0.
+// 4096 x 11008 bfloat16, forward and backward, gated 63 + 55 us, plain 41 + 41; by erff 62 + 67 and 44 + 55, by erfcf 83 + 95 and 63 + 82.
 struct Normal {
     float below, density;  // Phi(u), phi(u)
 };
 __device__ __forceinline__ Normal normal_of(float u) {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, fabsf(u), 1.0f)), density = __builtin_amdgcn_exp2f(u * u * -0.72134752f) * 0.39894228f;
-    float p = 0.08879409f;
-    p = fmaf(p, t, -0.39143094f), p = fmaf(p, t, 0.51274735f), p = fmaf(p, t, -0.13042958f), p = fmaf(p, t, 0.32007563f), p = fmaf(p, t, 0.25110391f), p = fmaf(p, t, 0.30258045f), p = fmaf(p, t, 0.29987299f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.35f, fabsf(u), 1.0f)), w = 1.0f - t, density = __builtin_amdgcn_exp2f(u * u * -0.72134752f) * 0.39894228f;
+    float p = -0.073087960f;
+    p = fmaf(p, w, 0.22367178f), p = fmaf(p, w, -0.16053279f), p = fmaf(p, w, -0.040340196f), p = fmaf(p, w, -0.16084722f), p = fmaf(p, w, 0.25727892f), p = fmaf(p, w, 0.65434307f);
+    p = fmaf(p, w, -1.6038210f), p = fmaf(p, w, 1.2533141f);
     const float tail = density * (p * t);
     return {u < 0.0f ? tail : 1.0f - tail, density};
 }
