@@ -486,7 +486,7 @@ int imunpack_block8_values(const void *codes, int64_t ldc, const void *scales, i
  * and then rounded to bfloat16.  Up to 16 rows of A both kinds may take other kernels with the same bounds.
  * A byte of 255, which no call here writes, makes the results it takes part in undefined.
  * workspace: device, 16-byte aligned, of the size that imunpack_block8_gemm_workspace gives (0: NULL will do).
- * Errors: EINVAL (null pointers, k outside [1, 2^24], m or n outside [0, 2^24], more than 2^23 tiles of 256 x 256, layouts as above, pitches above 2^24, unknown
+ * Errors: EINVAL (null pointers, k outside [1, 2^24], m or n outside [0, 2^24], more than 2^23 tiles of the kernel that takes it, layouts as above, pitches above 2^24, unknown
  * types); ESMALL; EHIP. */
 int imunpack_block8_gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, size_t *bytes);
 int imunpack_block8_gemm(const void *a, int64_t lda, const void *a_scales, int64_t ldsa, int a_format,

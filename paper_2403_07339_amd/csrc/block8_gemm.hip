@@ -449,8 +449,8 @@ __global__ __launch_bounds__(256) void block8_fold_kernel(const float *__restric
 // ---- up to sixteen rows: the contraction is dealt to a workgroup's waves -----------------------------------------------------------------
 // What counts is that B is read once, at once: a wave takes every eighth block of 16 rows of B straight into registers (four lanes to a row, a quarter of its
 // block's first half and of its second to each, so that a load takes 64 bytes of every row), four blocks ahead of the products, with the blocks of A's rows, which the
-// caches hold.  The waves' sums meet in LDS.  16 x 4096 by 4096: 7.6 us a call, of which the kernel's reading takes 2.7 (6 TB/s).  32 rows of B to a workgroup
-// were slower (10.2), a second set of registers under way as well (16 x 4096 by 11008: 18.0, 19.5).
+// caches hold.  The waves' sums meet in LDS.  16 x 4096 by 4096: 7.5 us a call, fp32 results 7.7; the kernel 7.8 by the profiler's clock, 7.1 also where it is one workgroup alone (by 16), 1.6 where that has
+// one block: the way of a wave's loads and what comes behind them bounds it, not bytes (2.7 at 6.5 TB/s).  32 rows of B to a workgroup were slower (10.2), a second set of registers under way as well (16 x 4096 by 11008: 18.0, 19.5).
 constexpr int kFewRows = 16, kFewWaves = 8, kFewAhead = 4;
 template <bool NATIVE, int FA, int FB>
 __global__ __launch_bounds__(64 * kFewWaves) void block8_few_kernel(const GemmArgs g) {
