@@ -124,3 +124,25 @@ def test_the_largest_values_turned(imu, fmt):
     (_, many), (_, alone) = imu.imunpack_block8_many(q, (x.cuda(), False, False, True), format=fmt)
     check_codes(many, *again, fmt, 200)
     check_codes(alone, *definition(x.t(), fmt), fmt, 200)
+
+
+@pytest.mark.parametrize("fb", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("fa", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_the_least_that_does_not_count(imu, rows, fa, fb):
+    """The smallest powers of two beside the largest numbers for which they are left as bfloat16 has them: half a place of 2^-133, 2^-134, times less than 2^8.  And beside the next power of two: rounded once."""
+    every = torch.arange(256, dtype=torch.uint8)
+    v = every.view(FORMATS[fa]).to(F)
+    every, v = every[torch.isfinite(v)], v[torch.isfinite(v)]
+    largest = {"e4m3": 448.0, "e5m2": 57344.0}[fb]
+    code = int(torch.tensor(largest).to(FORMATS[fb]).view(torch.uint8))
+    for other in {"e4m3": (126, 127), "e5m2": (119, 120)}[fb]:
+        b = single(imu, torch.full((rows,), code, dtype=torch.uint8), other, fb)
+        for byte in range(12):
+            a = single(imu, every, byte, fa)
+            want = (v * 2.0 ** (byte - 127) * largest * 2.0 ** (other - 127))[None]
+            for got in (imu.imunpack_block8_gemm(b, a), imu.imunpack_block8_gemm(a, b).t()):
+                off = (got.to(F).cpu() - want).abs()
+                assert (off <= 2.0 ** -126).all()
+                if largest * 2.0 ** (other - 127) >= 2.0 ** 8:
+                    assert (off <= 2.0 ** -24 * want.abs() + 2.0 ** -150).all()
